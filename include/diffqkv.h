@@ -49,7 +49,8 @@ typedef enum {
   DIFFQKV_ERR_WORKSPACE = 4,   /* workspace missing or smaller than the *_workspace_bytes answer   */
   DIFFQKV_ERR_CUDA = 5,        /* a CUDA runtime or driver call failed                             */
   DIFFQKV_ERR_TIMEOUT = 6,     /* device: a bounded wait on a copy ran out                         */
-  DIFFQKV_ERR_INDEX = 7        /* device: page id outside [0, num_blocks)                          */
+  DIFFQKV_ERR_INDEX = 7,       /* device: page id outside [0, num_blocks)                          */
+  DIFFQKV_ERR_PAGES = 8        /* device: a sequence was denied pages because the pool has too few */
 } diffqkv_status;
 
 typedef enum { DIFFQKV_BF16 = 0, DIFFQKV_F32 = 1 } diffqkv_dtype;
@@ -327,6 +328,173 @@ diffqkv_status diffqkv_decode_topk(const void *q, const diffqkv_cache *cache, co
 diffqkv_status diffqkv_decode_topk_ids(const void *q, const diffqkv_cache *cache, const diffqkv_shape *shape,
                                        int32_t topk, void *workspace, size_t workspace_bytes, void *out, float *lse,
                                        int32_t *kept_ids, int32_t *dev_status, void *stream);
+
+/* ------------------------------------------------------------------------------------------------------------------
+ * Ragged batches over the paged cache: what an engine step with sequences at different stages needs (some decode one
+ * token, some verify a few, some work off a long prompt in chunks).  The paper stops at one attention call; these
+ * entry points are this library's own.  All of them describe the step by the same two arrays: the new rows of
+ * sequence b are rows cu_q[b] .. cu_q[b + 1] - 1 of every ragged tensor (n_b = cu_q[b + 1] - cu_q[b], which may be 0),
+ * and seqlens[b] = past_b is the number of tokens cached BEFORE the step (diffqkv_prefill's convention, not
+ * diffqkv_decode's), so that one pair of arrays serves every layer:
+ *     diffqkv_pages_reserve -> per layer: diffqkv_rope_append, diffqkv_extend -> the caller adds n_b to seqlens[b]
+ *   cu_q     [batch + 1] int32, cu_q[0] = 0, not decreasing, cu_q[batch] <= total_q
+ *   total_q  rows the ragged tensors hold; rows from cu_q[batch] on are neither read nor written, so a step of fixed
+ *            capacity can be captured into a graph and replayed with other lengths
+ * A sequence whose rows do not fit (past_b + n_b > max_seqlen, or cu_q out of order or beyond total_q) is reported as
+ * DIFFQKV_ERR_INDEX in *dev_status and skipped; its rows stay as they were.
+ * ------------------------------------------------------------------------------------------------------------------ */
+
+/*
+ * diffqkv_extend -- causal attention of ragged chunks of new tokens over the cache (Section 2 formulation, head map of
+ * Eq. (idx)).  Row i of sequence b sits at position past_b + i and sees tokens 0 .. past_b + i; the chunk's own K and V
+ * rows are in the cache already (diffqkv_rope_append, diffqkv_cache_append or diffqkv_decode_frontend wrote them).
+ *   q     [total_q, n_q, d_qk] shape.dtype
+ *   out   [total_q, n_q, d_v]  shape.out_dtype         lse [total_q, n_q] fp32 natural log, or NULL
+ *   shape.batch sequences; cache, scale, dev_status as in diffqkv_prefill
+ *   workspace  diffqkv_extend_workspace_bytes(shape, total_q) bytes, 256-byte aligned; contents on entry are ignored.
+ *              Two calls that may run at the same time (streams without an order, graphs replayed side by side) need
+ *              a workspace each.
+ * bf16 with (d_qk, d_v) = (128, 128), (64, 64) or (64, 128), a positive scale, up to 128 query heads per (K head,
+ * V head) pair and pages of 8 to 64 tokens (a power of two) or a multiple of 128 runs on the tensor cores; everything
+ * else diffqkv_decode accepts runs on fp32 FMAs.  Results do not depend on how sequences are batched beyond fp32
+ * summation order, and are bitwise reproducible from call to call.
+ * As in any tensor-core attention a weight of zero multiplies the V rows of later tokens of the same chunk; those rows
+ * must be finite.  What lies behind the last cached token in its page may hold anything.
+ */
+size_t diffqkv_extend_workspace_bytes(const diffqkv_shape *shape, int32_t total_q);
+diffqkv_status diffqkv_extend(const void *q, const int32_t *cu_q, int32_t total_q, const diffqkv_cache *cache,
+                              const diffqkv_shape *shape, void *workspace, size_t workspace_bytes, void *out, float *lse,
+                              int32_t *dev_status, void *stream);
+
+/*
+ * Rotary positions.  Channel pairs of the first rot_dim channels of every q and k head are turned by the angle
+ * pos * inv_freq[i]; the other channels pass through:
+ *     (y_a, y_b) = magnitude * (x_a cos - x_b sin, x_b cos + x_a sin),   pair i = (i, i + rot_dim / 2), or
+ *     (2 i, 2 i + 1) when interleaved
+ * The angle is formed and reduced to one turn in fp64 (in fp32 a position of 10^5 would already cost 8e-3 of a turn's
+ * radian), the turn itself is fp32, each result is rounded once to the storage type.
+ */
+typedef struct {
+  const double *inv_freq;   /* [rot_dim / 2] device, radians per position                                  */
+  const int32_t *positions; /* [total_q] device, or NULL: row i of sequence b is at position past_b + i    */
+  int32_t rot_dim;          /* 0 (no rotation) to d_qk, a multiple of 16 (bf16) or 8 (fp32)                */
+  int32_t interleaved;      /* 0 = rotate-half pairs, 1 = neighbouring pairs                               */
+  float magnitude;          /* multiplies the rotated channels; 1 except for diffqkv_rope_frequencies YARN */
+} diffqkv_rope;
+
+/*
+ * diffqkv_rope_frequencies -- the table of inverse frequencies, on the HOST (nothing is launched), f_i = theta^(-2 i /
+ * rot_dim) and its adaptations to contexts longer than the trained length L = original_length, factor s >= 1:
+ *   PLAIN   f_i
+ *   LINEAR  f_i / s (position interpolation)
+ *   NTK     theta replaced by theta * s^(rot_dim / (rot_dim - 2))
+ *   YARN    f_i (1 - g_i) + f_i / s * g_i with g_i = clamp((i - lo) / (hi - lo), 0, 1), lo = floor(c(fast)),
+ *           hi = ceil(c(slow)), both kept within 0 .. rot_dim - 1, c(r) = rot_dim ln(L / (2 pi r)) / (2 ln theta);
+ *           magnitude = 0.1 ln s + 1
+ *   BANDS   wavelengths 2 pi / f_i below L / fast keep f_i, above L / slow take f_i / s, and in between
+ *           (1 - t) f_i / s + t f_i with t = (L f_i / (2 pi) - slow) / (fast - slow)
+ *   inv_freq  HOST [rot_dim / 2] fp64      magnitude  HOST, or NULL
+ */
+typedef enum {
+  DIFFQKV_ROPE_PLAIN = 0,
+  DIFFQKV_ROPE_LINEAR = 1,
+  DIFFQKV_ROPE_NTK = 2,
+  DIFFQKV_ROPE_YARN = 3,
+  DIFFQKV_ROPE_BANDS = 4
+} diffqkv_rope_scaling;
+diffqkv_status diffqkv_rope_frequencies(int32_t rot_dim, double theta, diffqkv_rope_scaling scaling, double factor,
+                                        double original_length, double fast, double slow, double *inv_freq,
+                                        float *magnitude);
+
+/*
+ * diffqkv_rope_append -- rotates the q and k rows of a ragged step and writes k and v to positions past_b + i of the
+ * cache, in one launch (diffqkv_cache_append for ragged chunks, with the rotation of the appendix attention listing).
+ *   q      [total_q, n_q, d_qk], or NULL for keys and values alone      q_out  [total_q, n_q, d_qk] dense; may be q
+ *   k_new  [total_q, n_k, d_qk]      v_new  [total_q, n_v, d_v]      all of shape.dtype, heads dense within a row
+ *   *_stride_tok  elements between rows (slices of a fused projection); 0 = dense.  q_out == q needs a dense q.
+ * The rotation moves with `positions`, the place in the cache does not.  Positions whose page id lies outside the
+ * pool are skipped and reported as DIFFQKV_ERR_INDEX.
+ */
+diffqkv_status diffqkv_rope_append(const void *q, const void *k_new, const void *v_new, const int32_t *cu_q,
+                                   int32_t total_q, int64_t q_stride_tok, int64_t k_stride_tok, int64_t v_stride_tok,
+                                   const diffqkv_rope *rope, const diffqkv_cache *cache, const diffqkv_shape *shape,
+                                   void *q_out, int32_t *dev_status, void *stream);
+
+/*
+ * Upkeep of the pages.  A page is a block of both pools (one id for K and V, as in diffqkv_cache).  The state is three
+ * device arrays of the caller: the page table, the lengths, and the number of table entries that name each page.
+ * Entry -1 means no page; a sequence's pages fill its row from the front.  A page whose count is 0 is free, and free
+ * pages are always handed out lowest id first, in the order of the sequences, so every call is deterministic.  Counts
+ * may also be raised by the caller (a prefix that is kept pinned).  No call synchronises or tells the host anything:
+ * a serving loop can run them inside a captured step.
+ * Sequence ids outside [0, num_seqs) and page ids outside [0, num_pages) are reported as DIFFQKV_ERR_INDEX, skipped.
+ */
+typedef struct {
+  int32_t *page_table; /* [num_seqs, max_pages_per_seq]                              */
+  int32_t *seqlens;    /* [num_seqs] tokens cached                                   */
+  int32_t *ref_counts; /* [num_pages] table entries (and pins) that name the page    */
+  int32_t num_seqs, max_pages_per_seq, num_pages, page_size;
+} diffqkv_pages;
+
+/*
+ * diffqkv_pages_free -- gives back the pages of n sequences behind their first keep_tokens[i] tokens (NULL: all of
+ * them): entries become -1, counts go down by one, seqlens = min(seqlens, keep).  A sequence may be listed twice.
+ */
+diffqkv_status diffqkv_pages_free(const int32_t *seq_ids, const int32_t *keep_tokens, int32_t n,
+                                  const diffqkv_pages *pages, int32_t *dev_status, void *stream);
+
+/*
+ * diffqkv_pages_fork -- children[i] becomes a copy of parents[i] that shares its pages (no token is copied): what the
+ * child held is given back, its row names the pages of the parent's seqlens tokens, its length is the parent's.  All
+ * parents are read as they were before the call, so a child may be a parent too (beams that change places) or its own.
+ * A sequence that is listed as a child twice takes the first of its parents; the others are reported as
+ * DIFFQKV_ERR_INDEX.
+ *   workspace  diffqkv_pages_fork_workspace_bytes(pages, n) bytes, 256-byte aligned
+ */
+size_t diffqkv_pages_fork_workspace_bytes(const diffqkv_pages *pages, int32_t n);
+diffqkv_status diffqkv_pages_fork(const int32_t *parents, const int32_t *children, int32_t n, const diffqkv_pages *pages,
+                                  void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream);
+
+/*
+ * diffqkv_pages_reserve -- makes the cache writable for the step's rows: sequence b gets a page of its own for every
+ * position past_b .. past_b + n_b - 1.  Missing pages are taken from the free ones; pages that another holder shares
+ * (count > 1 at the start of the call) are replaced, and where past_b lies inside such a page its contents are copied
+ * to the new one (copy on write).  If all holders of a page write in the same call each gets a copy.
+ * A sequence gets all it needs or nothing: b is denied when the demands of sequences 0 .. b together exceed the free
+ * pages (DIFFQKV_ERR_PAGES) or its row is too short (DIFFQKV_ERR_INDEX).
+ *   cache, shape  the pools (pointers, strides, num_blocks = pages->num_pages); shape gives n_k, n_v, d_qk, d_v, dtype;
+ *                 cache->page_table and cache->seqlens are not used
+ *   granted       [num_seqs] int32: 1 = its rows may be written, 0 = denied; or NULL
+ *   workspace     diffqkv_pages_reserve_workspace_bytes(pages) bytes, 256-byte aligned
+ */
+size_t diffqkv_pages_reserve_workspace_bytes(const diffqkv_pages *pages);
+diffqkv_status diffqkv_pages_reserve(const int32_t *cu_q, const diffqkv_pages *pages, const diffqkv_cache *cache,
+                                     const diffqkv_shape *shape, int32_t *granted, void *workspace,
+                                     size_t workspace_bytes, int32_t *dev_status, void *stream);
+
+/*
+ * diffqkv_pages_copy -- pages src_ids[i] of `src` become pages dst_ids[i] of `dst`, K and V (the same cache, or two
+ * with equal page_size whose strides may differ: moving a sequence to another pool).  Within one cache no page may be
+ * both a source and a destination, and no destination may be listed twice.  Tables and counts are not touched.
+ */
+diffqkv_status diffqkv_pages_copy(const int32_t *src_ids, const int32_t *dst_ids, int32_t n, const diffqkv_cache *src,
+                                  const diffqkv_cache *dst, const diffqkv_shape *shape, int32_t *dev_status,
+                                  void *stream);
+
+/*
+ * diffqkv_pages_compact -- moves the pages in use to the front of the pool: with `live` of them in use, the i-th lowest
+ * page in use with an id >= live moves to the i-th lowest free id below live; everything else stays.  Afterwards
+ * exactly the ids 0 .. live - 1 are in use.
+ *   table_out, refs_out  the new page table and counts; may be pages->page_table / ref_counts themselves.  Where they
+ *                        are other buffers the old ones stay valid for readers already enqueued: a moved page keeps
+ *                        its contents at its old id until that id is handed out again
+ *   live                 one int32 that receives the number of pages in use, or NULL
+ *   workspace            diffqkv_pages_compact_workspace_bytes(pages) bytes, 256-byte aligned
+ */
+size_t diffqkv_pages_compact_workspace_bytes(const diffqkv_pages *pages);
+diffqkv_status diffqkv_pages_compact(const diffqkv_pages *pages, const diffqkv_cache *cache, const diffqkv_shape *shape,
+                                     int32_t *table_out, int32_t *refs_out, int32_t *live, void *workspace,
+                                     size_t workspace_bytes, int32_t *dev_status, void *stream);
 
 /* Static, never-null description of a status value. */
 const char *diffqkv_status_string(diffqkv_status status);

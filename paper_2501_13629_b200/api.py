@@ -22,7 +22,7 @@ if not os.path.exists(LIB_PATH):
         "(there is no CPU or PyTorch fallback)")
 _lib = C.CDLL(LIB_PATH)
 
-OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT, ERR_INDEX = range(8)
+OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT, ERR_INDEX, ERR_PAGES = range(9)
 BF16, F32 = 0, 1
 
 EXPORTS = (
@@ -34,6 +34,10 @@ EXPORTS = (
     "diffqkv_decode_topk", "diffqkv_decode_topk_workspace_bytes", "diffqkv_decode_frontend",
     "diffqkv_decode_frontend_workspace_bytes", "diffqkv_decode_host", "diffqkv_fold_k_up",
     "diffqkv_set_tail_reserve", "diffqkv_debug_decode_timeout", "diffqkv_decode_topk_ids", "diffqkv_debug_decode_per_head_only", "diffqkv_debug_decode_cluster",
+    "diffqkv_extend", "diffqkv_extend_workspace_bytes", "diffqkv_rope_append", "diffqkv_rope_frequencies",
+    "diffqkv_pages_free", "diffqkv_pages_fork", "diffqkv_pages_fork_workspace_bytes", "diffqkv_pages_reserve",
+    "diffqkv_pages_reserve_workspace_bytes", "diffqkv_pages_copy", "diffqkv_pages_compact",
+    "diffqkv_pages_compact_workspace_bytes",
 )
 
 
@@ -54,6 +58,17 @@ class ShapeStruct(C.Structure):
         ("d_qk", C.c_int32), ("d_v", C.c_int32),
         ("dtype", C.c_int), ("out_dtype", C.c_int), ("scale", C.c_float),
     ]
+
+
+class RopeStruct(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("positions", C.c_void_p), ("rot_dim", C.c_int32), ("interleaved", C.c_int32),
+                ("magnitude", C.c_float)]
+
+
+class PagesStruct(C.Structure):
+    _fields_ = [("page_table", C.c_void_p), ("seqlens", C.c_void_p), ("ref_counts", C.c_void_p),
+                ("num_seqs", C.c_int32), ("max_pages_per_seq", C.c_int32), ("num_pages", C.c_int32),
+                ("page_size", C.c_int32)]
 
 
 _lib.diffqkv_decode_num_splits.restype = C.c_int32
@@ -130,6 +145,32 @@ _lib.diffqkv_set_max_blocks.restype = None
 _lib.diffqkv_set_max_blocks.argtypes = [C.c_int32]
 _lib.diffqkv_profile_split_events.restype = None
 _lib.diffqkv_profile_split_events.argtypes = [C.c_void_p, C.c_void_p]
+
+
+_SHAPE, _CACHE, _PAGES = C.POINTER(ShapeStruct), C.POINTER(CacheStruct), C.POINTER(PagesStruct)
+for _name, _res, _args in (
+        ("diffqkv_extend_workspace_bytes", C.c_size_t, [_SHAPE, C.c_int32]),
+        ("diffqkv_extend", C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, _CACHE, _SHAPE, C.c_void_p, C.c_size_t,
+                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+        ("diffqkv_rope_frequencies", C.c_int, [C.c_int32, C.c_double, C.c_int, C.c_double, C.c_double, C.c_double,
+                                               C.c_double, C.POINTER(C.c_double), C.POINTER(C.c_float)]),
+        ("diffqkv_rope_append", C.c_int, [C.c_void_p] * 4 + [C.c_int32, C.c_int64, C.c_int64, C.c_int64,
+                                                             C.POINTER(RopeStruct), _CACHE, _SHAPE, C.c_void_p,
+                                                             C.c_void_p, C.c_void_p]),
+        ("diffqkv_pages_free", C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, _PAGES, C.c_void_p, C.c_void_p]),
+        ("diffqkv_pages_fork_workspace_bytes", C.c_size_t, [_PAGES, C.c_int32]),
+        ("diffqkv_pages_fork", C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, _PAGES, C.c_void_p, C.c_size_t, C.c_void_p,
+                                         C.c_void_p]),
+        ("diffqkv_pages_reserve_workspace_bytes", C.c_size_t, [_PAGES]),
+        ("diffqkv_pages_reserve", C.c_int, [C.c_void_p, _PAGES, _CACHE, _SHAPE, C.c_void_p, C.c_void_p, C.c_size_t,
+                                            C.c_void_p, C.c_void_p]),
+        ("diffqkv_pages_copy", C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, _CACHE, _CACHE, _SHAPE, C.c_void_p,
+                                         C.c_void_p]),
+        ("diffqkv_pages_compact_workspace_bytes", C.c_size_t, [_PAGES]),
+        ("diffqkv_pages_compact", C.c_int, [_PAGES, _CACHE, _SHAPE, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                            C.c_size_t, C.c_void_p, C.c_void_p])):
+    getattr(_lib, _name).restype = _res
+    getattr(_lib, _name).argtypes = _args
 
 
 class DiffQKVError(RuntimeError):
@@ -567,3 +608,221 @@ def diffqkv_decode_topk(q: torch.Tensor, cache: KVCache, n_k: int, n_v: int, sca
     if st != OK:
         raise DiffQKVError(st, "diffqkv_decode_topk")
     return out
+
+
+# ---- ragged batches over the cache: a step's new rows of sequence b are rows cu_q[b] .. cu_q[b + 1] - 1 of every ragged
+# tensor, cache.seqlens[b] is the number of tokens cached before the step (the caller adds the chunk lengths after it)
+
+def _on_device(*tensors: Optional[torch.Tensor]) -> None:
+    """The launch goes to the current device: every tensor has to be there."""
+    for t in tensors:
+        if t is not None and t.get_device() < 0:
+            raise ValueError(f"expected a CUDA tensor, got one on {t.device}")
+    current = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != current:
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{current}")
+
+
+def _on_device_cache(cache: KVCache, *tensors: Optional[torch.Tensor]) -> None:
+    _on_device(cache.k, cache.v, cache.seqlens, cache.page_table, *tensors)
+
+
+def _cu_q(cu_q: torch.Tensor, batch: int) -> C.c_void_p:
+    assert cu_q.dtype == torch.int32 and cu_q.is_contiguous() and cu_q.numel() == batch + 1
+    return _p(cu_q)
+
+
+def _workspace(workspace: Optional[torch.Tensor], nbytes: int, device) -> torch.Tensor:
+    return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device) if workspace is None else workspace
+
+
+def diffqkv_extend_workspace_bytes(shape: ShapeStruct, total_q: int) -> int:
+    return int(_lib.diffqkv_extend_workspace_bytes(C.byref(shape), int(total_q)))
+
+
+def diffqkv_extend(q: torch.Tensor, cu_q: torch.Tensor, cache: KVCache, n_k: int, n_v: int, scale: float,
+                   workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                   lse: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
+                   out_dtype: Optional[torch.dtype] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Causal attention of ragged chunks: q [total_q, n_q, d_qk] against the cache, which holds the chunks' own rows
+    already; returns out [total_q, n_q, d_v].  Rows behind the last chunk stay as they are (a fresh out holds
+    anything there)."""
+    total_q, n_q, d_qk = q.shape
+    d_v = cache.v.shape[-1]
+    batch = cache.seqlens.numel()
+    _on_device_cache(cache, q, cu_q, workspace, out, lse, dev_status)
+    assert cache.k.dtype == q.dtype and cache.v.dtype == q.dtype
+    assert q.is_contiguous() and (out is None or out.is_contiguous()) and (lse is None or lse.is_contiguous())
+    out_dtype = out_dtype or (out.dtype if out is not None else q.dtype)
+    shape = make_shape(batch, n_q, n_k, n_v, d_qk, d_v, q.dtype, out_dtype, scale)
+    workspace = _workspace(workspace, _lib.diffqkv_extend_workspace_bytes(C.byref(shape), total_q), q.device)
+    if out is None:
+        out = torch.empty((total_q, n_q, d_v), dtype=out_dtype, device=q.device)
+    cs = cache.c_struct()
+    st = _lib.diffqkv_extend(_p(q), _cu_q(cu_q, batch), total_q, C.byref(cs), C.byref(shape), _p(workspace),
+                             workspace.numel(), _p(out), _p(lse), _p(dev_status), _stream_ptr(stream))
+    if st != OK:
+        raise DiffQKVError(st, "diffqkv_extend")
+    return out
+
+
+ROPE_SCALINGS = {"plain": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}
+
+
+def rope_frequencies(rot_dim: int, theta: float, scaling: str = "plain", factor: float = 1.0,
+                     original_length: float = 0.0, fast: float = 0.0, slow: float = 0.0,
+                     device=None) -> Tuple[torch.Tensor, float]:
+    """The table of inverse frequencies (float64 [rot_dim / 2], on ``device``) and the magnitude that goes with it."""
+    table = (C.c_double * max(rot_dim // 2, 1))()
+    magnitude = C.c_float()
+    st = _lib.diffqkv_rope_frequencies(rot_dim, theta, ROPE_SCALINGS[scaling], factor, original_length, fast, slow, table,
+                                       C.byref(magnitude))
+    if st != OK:
+        raise DiffQKVError(st, "diffqkv_rope_frequencies")
+    return torch.tensor(list(table), dtype=torch.float64, device=device), float(magnitude.value)
+
+
+def _row_stride(x: torch.Tensor) -> int:
+    """Elements between the rows of x [rows, heads, d] whose heads are dense (a slice of a fused projection, say)."""
+    assert x.dim() == 3 and x.stride(2) == 1 and (x.shape[1] == 1 or x.stride(1) == x.shape[2])
+    return int(x.stride(0)) if x.shape[0] > 1 else 0
+
+
+def diffqkv_rope_append(q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: torch.Tensor, cu_q: torch.Tensor,
+                        cache: KVCache, inv_freq: Optional[torch.Tensor], interleaved: bool = False,
+                        magnitude: float = 1.0, positions: Optional[torch.Tensor] = None,
+                        q_out: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
+                        stream: Optional[torch.cuda.Stream] = None):
+    """Rotate q [total_q, n_q, d_qk] and k_new [total_q, n_k, d_qk] and write k_new / v_new [total_q, n_v, d_v] to cache
+    positions seqlens[b] + i; returns the rotated q (q_out may be q).  ``inv_freq`` float64 [rot_dim / 2], None for no
+    rotation; ``positions`` int32 [total_q] replaces the rotation's position seqlens[b] + i."""
+    total_q, n_k, d_qk = k_new.shape
+    n_v, d_v = v_new.shape[1], v_new.shape[2]
+    batch = cache.seqlens.numel()
+    n_q = n_k * n_v if q is None else q.shape[1]  # without queries any count both head counts divide does
+    _on_device_cache(cache, q, k_new, v_new, cu_q, inv_freq, positions, q_out, dev_status)
+    assert cache.k.dtype == k_new.dtype and cache.v.dtype == k_new.dtype
+    assert v_new.shape[0] == total_q and (q is None or (q.shape[0] == total_q and q.shape[2] == d_qk))
+    assert v_new.dtype == k_new.dtype and (q is None or q.dtype == k_new.dtype)
+    assert inv_freq is None or (inv_freq.dtype == torch.float64 and inv_freq.is_contiguous())
+    assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and
+                                 positions.numel() == total_q)
+    if q is not None and q_out is None:
+        q_out = torch.empty((total_q, n_q, d_qk), dtype=q.dtype, device=q.device)
+    assert q_out is None or q_out.is_contiguous()
+    shape = make_shape(batch, n_q, n_k, n_v, d_qk, d_v, k_new.dtype, k_new.dtype, 1.0)
+    rope = RopeStruct(None if inv_freq is None else inv_freq.data_ptr(), None if positions is None else positions.data_ptr(),
+                      0 if inv_freq is None else 2 * inv_freq.numel(), int(bool(interleaved)), float(magnitude))
+    cs = cache.c_struct()
+    st = _lib.diffqkv_rope_append(_p(q), _p(k_new), _p(v_new), _cu_q(cu_q, batch), total_q,
+                                  0 if q is None else _row_stride(q), _row_stride(k_new), _row_stride(v_new),
+                                  C.byref(rope), C.byref(cs), C.byref(shape), _p(q_out), _p(dev_status),
+                                  _stream_ptr(stream))
+    if st != OK:
+        raise DiffQKVError(st, "diffqkv_rope_append")
+    return q_out
+
+
+# ---- upkeep of the pages: cache.page_table [num_seqs, max_pages_per_seq], cache.seqlens and ref_counts [num_pages] are
+# written by these calls
+
+def _ints(t: Optional[torch.Tensor], n: Optional[int] = None):
+    assert t is None or (t.dtype == torch.int32 and t.is_contiguous() and (n is None or t.numel() == n))
+    return _p(t)
+
+
+def _pages(cache: KVCache, ref_counts: torch.Tensor) -> PagesStruct:
+    pt = cache.page_table
+    assert pt is not None and pt.dtype == torch.int32 and pt.is_contiguous() and pt.dim() == 2
+    assert cache.seqlens.dtype == torch.int32 and cache.seqlens.is_contiguous() and cache.seqlens.numel() == pt.shape[0]
+    assert ref_counts.dtype == torch.int32 and ref_counts.is_contiguous()
+    return PagesStruct(pt.data_ptr(), cache.seqlens.data_ptr(), ref_counts.data_ptr(), pt.shape[0], pt.shape[1],
+                       ref_counts.numel(), int(cache.page_size))
+
+
+def _pool_shape(cache: KVCache, n_k: int, n_v: int) -> ShapeStruct:
+    assert cache.k.dtype == cache.v.dtype
+    return make_shape(1, n_k * n_v, n_k, n_v, cache.k.shape[-1], cache.v.shape[-1], cache.k.dtype, cache.k.dtype, 1.0)
+
+
+def diffqkv_pages_free(seq_ids: torch.Tensor, cache: KVCache, ref_counts: torch.Tensor,
+                       keep_tokens: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Give back the pages of the sequences ``seq_ids`` (int32 [n]) behind their first ``keep_tokens`` tokens."""
+    _on_device_cache(cache, seq_ids, keep_tokens, ref_counts, dev_status)
+    g = _pages(cache, ref_counts)
+    n = seq_ids.numel()
+    st = _lib.diffqkv_pages_free(_ints(seq_ids), _ints(keep_tokens, n), n, C.byref(g), _p(dev_status), _stream_ptr(stream))
+    if st != OK:
+        raise DiffQKVError(st, "diffqkv_pages_free")
+
+
+def diffqkv_pages_fork(parents: torch.Tensor, children: torch.Tensor, cache: KVCache, ref_counts: torch.Tensor,
+                       workspace: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Sequence children[i] becomes a copy of sequence parents[i] that shares its pages."""
+    _on_device_cache(cache, parents, children, ref_counts, workspace, dev_status)
+    g = _pages(cache, ref_counts)
+    n = children.numel()
+    workspace = _workspace(workspace, _lib.diffqkv_pages_fork_workspace_bytes(C.byref(g), n), ref_counts.device)
+    st = _lib.diffqkv_pages_fork(_ints(parents, n), _ints(children), n, C.byref(g), _p(workspace), workspace.numel(),
+                                 _p(dev_status), _stream_ptr(stream))
+    if st != OK:
+        raise DiffQKVError(st, "diffqkv_pages_fork")
+
+
+def diffqkv_pages_reserve(cu_q: torch.Tensor, cache: KVCache, ref_counts: torch.Tensor, n_k: int, n_v: int,
+                          granted: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                          dev_status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Give every sequence pages of its own for its next cu_q[b + 1] - cu_q[b] tokens (copy on write)."""
+    _on_device_cache(cache, cu_q, ref_counts, granted, workspace, dev_status)
+    g = _pages(cache, ref_counts)
+    shape = _pool_shape(cache, n_k, n_v)
+    cs = cache.c_struct()
+    workspace = _workspace(workspace, _lib.diffqkv_pages_reserve_workspace_bytes(C.byref(g)), ref_counts.device)
+    st = _lib.diffqkv_pages_reserve(_cu_q(cu_q, g.num_seqs), C.byref(g), C.byref(cs), C.byref(shape),
+                                    _ints(granted, g.num_seqs), _p(workspace), workspace.numel(), _p(dev_status),
+                                    _stream_ptr(stream))
+    if st != OK:
+        raise DiffQKVError(st, "diffqkv_pages_reserve")
+
+
+def diffqkv_pages_copy(src_ids: torch.Tensor, dst_ids: torch.Tensor, cache: KVCache, n_k: int, n_v: int,
+                       dst_cache: Optional[KVCache] = None, dev_status: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> None:
+    """Pages src_ids[i] of ``cache`` become pages dst_ids[i] of ``dst_cache`` (default: of the same cache)."""
+    _on_device(cache.k, cache.v, src_ids, dst_ids, dev_status)
+    if dst_cache is not None:
+        _on_device(dst_cache.k, dst_cache.v)
+        assert dst_cache.k.dtype == cache.k.dtype and dst_cache.v.dtype == cache.v.dtype
+        assert dst_cache.k.shape[-1] == cache.k.shape[-1] and dst_cache.v.shape[-1] == cache.v.shape[-1]
+    shape = _pool_shape(cache, n_k, n_v)
+    src = cache.c_struct()
+    dst = src if dst_cache is None else dst_cache.c_struct()
+    n = src_ids.numel()
+    st = _lib.diffqkv_pages_copy(_ints(src_ids), _ints(dst_ids, n), n, C.byref(src), C.byref(dst), C.byref(shape),
+                                 _p(dev_status), _stream_ptr(stream))
+    if st != OK:
+        raise DiffQKVError(st, "diffqkv_pages_copy")
+
+
+def diffqkv_pages_compact(cache: KVCache, ref_counts: torch.Tensor, n_k: int, n_v: int,
+                          table_out: Optional[torch.Tensor] = None, refs_out: Optional[torch.Tensor] = None,
+                          live: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                          dev_status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Move the pages in use to the front of the pool; returns the new (page table, counts), which are the cache's own
+    tensors changed in place unless others are passed."""
+    _on_device_cache(cache, ref_counts, table_out, refs_out, live, workspace, dev_status)
+    g = _pages(cache, ref_counts)
+    shape = _pool_shape(cache, n_k, n_v)
+    cs = cache.c_struct()
+    table_out = cache.page_table if table_out is None else table_out
+    refs_out = ref_counts if refs_out is None else refs_out
+    workspace = _workspace(workspace, _lib.diffqkv_pages_compact_workspace_bytes(C.byref(g)), ref_counts.device)
+    st = _lib.diffqkv_pages_compact(C.byref(g), C.byref(cs), C.byref(shape), _ints(table_out, cache.page_table.numel()),
+                                    _ints(refs_out, ref_counts.numel()), _ints(live, 1), _p(workspace),
+                                    workspace.numel(), _p(dev_status), _stream_ptr(stream))
+    if st != OK:
+        raise DiffQKVError(st, "diffqkv_pages_compact")
+    return table_out, refs_out

@@ -440,6 +440,191 @@ diffqkv_status diffqkv_decode_topk(const void* q, const diffqkv_cache* cache, co
   return diffqkv_decode_topk_ids(q, cache, shape, topk, workspace, workspace_bytes, out, lse, nullptr, dev_status, stream);
 }
 
+size_t diffqkv_extend_workspace_bytes(const diffqkv_shape* shape, int32_t total_q) {
+  if (check_shape(shape) != DIFFQKV_OK || total_q < 0) return 0;
+  return 256;
+}
+
+diffqkv_status diffqkv_extend(const void* q, const int32_t* cu_q, int32_t total_q, const diffqkv_cache* cache,
+                              const diffqkv_shape* shape, void* workspace, size_t workspace_bytes, void* out, float* lse,
+                              int32_t* dev_status, void* stream) {
+  diffqkv_status st = check_shape(shape);
+  if (st != DIFFQKV_OK) return st;
+  if (total_q < 0) return DIFFQKV_ERR_INVALID_ARG;
+  if (shape->batch == 0 || total_q == 0) return DIFFQKV_OK;  // empty tensors may come without memory
+  if (!q || !cu_q || !out) return DIFFQKV_ERR_INVALID_ARG;
+  st = check_cache(cache, shape);
+  if (st != DIFFQKV_OK) return st;
+  if (!aligned16(q) || !aligned16(out)) return DIFFQKV_ERR_ALIGNMENT;
+  if (!workspace || workspace_bytes < diffqkv_extend_workspace_bytes(shape, total_q)) return DIFFQKV_ERR_WORKSPACE;
+  if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return DIFFQKV_ERR_ALIGNMENT;
+  cudaStream_t st_ = static_cast<cudaStream_t>(stream);
+  DecodeParams p;
+  p.q = q;
+  p.cache = view_of(cache);
+  p.batch = shape->batch; p.n_q = shape->n_q; p.n_k = shape->n_k; p.n_v = shape->n_v;
+  p.d_qk = shape->d_qk; p.d_v = shape->d_v;
+  p.scale_log2 = shape->scale * kLog2e;
+  p.chunk = 0; p.splits = 1;
+  p.o_partial = nullptr; p.lse_partial = nullptr;
+  p.dev_status = dev_status;
+  const cudaError_t err = launch_extend_generic(p, shape->dtype, cu_q, total_q, out, shape->out_dtype == DIFFQKV_F32, lse, st_);
+  if (err == cudaErrorNotSupported) return DIFFQKV_ERR_UNSUPPORTED;
+  return err == cudaSuccess ? DIFFQKV_OK : DIFFQKV_ERR_CUDA;
+}
+
+diffqkv_status diffqkv_rope_frequencies(int32_t rot_dim, double theta, diffqkv_rope_scaling scaling, double factor,
+                                        double original_length, double fast, double slow, double* inv_freq,
+                                        float* magnitude) {
+  return rope_frequencies(rot_dim, theta, (int)scaling, factor, original_length, fast, slow, inv_freq, magnitude)
+             ? DIFFQKV_OK
+             : DIFFQKV_ERR_INVALID_ARG;
+}
+
+diffqkv_status diffqkv_rope_append(const void* q, const void* k_new, const void* v_new, const int32_t* cu_q,
+                                   int32_t total_q, int64_t q_stride_tok, int64_t k_stride_tok, int64_t v_stride_tok,
+                                   const diffqkv_rope* rope, const diffqkv_cache* cache, const diffqkv_shape* shape,
+                                   void* q_out, int32_t* dev_status, void* stream) {
+  diffqkv_status st = check_shape(shape);
+  if (st != DIFFQKV_OK) return st;
+  if (!rope || total_q < 0) return DIFFQKV_ERR_INVALID_ARG;
+  if (shape->batch == 0 || total_q == 0) return DIFFQKV_OK;
+  if (!k_new || !v_new || !cu_q || (q && !q_out)) return DIFFQKV_ERR_INVALID_ARG;
+  st = check_cache(cache, shape);
+  if (st != DIFFQKV_OK) return st;
+  const int vec = shape->dtype == DIFFQKV_BF16 ? 8 : 4;
+  if (rope->rot_dim < 0 || rope->rot_dim > shape->d_qk || (rope->rot_dim > 0 && !rope->inv_freq))
+    return DIFFQKV_ERR_INVALID_ARG;
+  if (rope->rot_dim % (2 * vec) != 0) return DIFFQKV_ERR_UNSUPPORTED;
+  if (!(rope->magnitude == rope->magnitude)) return DIFFQKV_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_out)) return DIFFQKV_ERR_ALIGNMENT;
+  if ((reinterpret_cast<uintptr_t>(rope->inv_freq) & 7u) != 0) return DIFFQKV_ERR_ALIGNMENT;
+  const int64_t strides[3] = {q_stride_tok, k_stride_tok, v_stride_tok};
+  const int64_t widths[3] = {(int64_t)shape->n_q * shape->d_qk, (int64_t)shape->n_k * shape->d_qk,
+                             (int64_t)shape->n_v * shape->d_v};
+  for (int i = q ? 0 : 1; i < 3; ++i) {
+    if (strides[i] == 0) continue;
+    if (strides[i] < widths[i]) return DIFFQKV_ERR_INVALID_ARG;
+    if (strides[i] % vec != 0) return DIFFQKV_ERR_ALIGNMENT;
+  }
+  if (q && q == q_out && q_stride_tok != 0 && q_stride_tok != widths[0]) return DIFFQKV_ERR_INVALID_ARG;
+  const cudaError_t err = launch_rope_append(q, k_new, v_new, cu_q, total_q, q_stride_tok, k_stride_tok, v_stride_tok,
+                                             *rope, view_of(cache), *shape, q_out, dev_status,
+                                             static_cast<cudaStream_t>(stream));
+  return err == cudaSuccess ? DIFFQKV_OK : DIFFQKV_ERR_CUDA;
+}
+
+static diffqkv_status check_pages(const diffqkv_pages* g) {
+  if (!g || !g->page_table || !g->seqlens || !g->ref_counts) return DIFFQKV_ERR_INVALID_ARG;
+  if (g->num_seqs < 0 || g->max_pages_per_seq <= 0 || g->num_pages <= 0 || g->page_size <= 0) return DIFFQKV_ERR_INVALID_ARG;
+  if (g->num_seqs > 65535 || g->num_pages > (1 << 20)) return DIFFQKV_ERR_UNSUPPORTED;
+  return DIFFQKV_OK;
+}
+
+static diffqkv_status check_pools(const diffqkv_cache* c, const diffqkv_shape* s, int page_size) {
+  const diffqkv_status st = check_shape(s);
+  if (st != DIFFQKV_OK) return st;
+  if (!c || !c->k_cache || !c->v_cache || c->num_blocks < 0) return DIFFQKV_ERR_INVALID_ARG;
+  if (c->page_size <= 0 || c->page_size != page_size) return DIFFQKV_ERR_INVALID_ARG;
+  const int vec = s->dtype == DIFFQKV_BF16 ? 8 : 4;
+  const long long strides[6] = {c->k_stride_blk, c->k_stride_head, c->k_stride_tok,
+                                c->v_stride_blk, c->v_stride_head, c->v_stride_tok};
+  for (long long x : strides)
+    if (x < 0 || x % vec != 0) return DIFFQKV_ERR_ALIGNMENT;
+  if (c->k_stride_tok < s->d_qk || c->v_stride_tok < s->d_v) return DIFFQKV_ERR_INVALID_ARG;
+  if ((long long)page_size * s->n_k * s->d_qk > 0x3fffffffLL || (long long)page_size * s->n_v * s->d_v > 0x3fffffffLL)
+    return DIFFQKV_ERR_UNSUPPORTED;
+  if (!aligned16(c->k_cache) || !aligned16(c->v_cache)) return DIFFQKV_ERR_ALIGNMENT;
+  return DIFFQKV_OK;
+}
+
+static diffqkv_status check_workspace(const void* workspace, size_t have, size_t need) {
+  if (!workspace || have < need) return DIFFQKV_ERR_WORKSPACE;
+  return (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 ? DIFFQKV_ERR_ALIGNMENT : DIFFQKV_OK;
+}
+
+diffqkv_status diffqkv_pages_free(const int32_t* seq_ids, const int32_t* keep_tokens, int32_t n,
+                                  const diffqkv_pages* pages, int32_t* dev_status, void* stream) {
+  const diffqkv_status st = check_pages(pages);
+  if (st != DIFFQKV_OK) return st;
+  if (n < 0 || (n > 0 && !seq_ids)) return DIFFQKV_ERR_INVALID_ARG;
+  if (n == 0) return DIFFQKV_OK;
+  const cudaError_t err = launch_pages_free(seq_ids, keep_tokens, n, *pages, dev_status, static_cast<cudaStream_t>(stream));
+  return err == cudaSuccess ? DIFFQKV_OK : DIFFQKV_ERR_CUDA;
+}
+
+size_t diffqkv_pages_fork_workspace_bytes(const diffqkv_pages* pages, int32_t n) {
+  if (check_pages(pages) != DIFFQKV_OK || n < 0) return 0;
+  return pages_fork_workspace_bytes(*pages, n);
+}
+
+diffqkv_status diffqkv_pages_fork(const int32_t* parents, const int32_t* children, int32_t n, const diffqkv_pages* pages,
+                                  void* workspace, size_t workspace_bytes, int32_t* dev_status, void* stream) {
+  diffqkv_status st = check_pages(pages);
+  if (st != DIFFQKV_OK) return st;
+  if (n < 0 || (n > 0 && (!parents || !children))) return DIFFQKV_ERR_INVALID_ARG;
+  if (n == 0) return DIFFQKV_OK;
+  st = check_workspace(workspace, workspace_bytes, pages_fork_workspace_bytes(*pages, n));
+  if (st != DIFFQKV_OK) return st;
+  const cudaError_t err = launch_pages_fork(parents, children, n, *pages, workspace, dev_status,
+                                            static_cast<cudaStream_t>(stream));
+  return err == cudaSuccess ? DIFFQKV_OK : DIFFQKV_ERR_CUDA;
+}
+
+size_t diffqkv_pages_reserve_workspace_bytes(const diffqkv_pages* pages) {
+  return check_pages(pages) == DIFFQKV_OK ? pages_reserve_workspace_bytes(*pages) : 0;
+}
+
+diffqkv_status diffqkv_pages_reserve(const int32_t* cu_q, const diffqkv_pages* pages, const diffqkv_cache* cache,
+                                     const diffqkv_shape* shape, int32_t* granted, void* workspace,
+                                     size_t workspace_bytes, int32_t* dev_status, void* stream) {
+  diffqkv_status st = check_pages(pages);
+  if (st != DIFFQKV_OK) return st;
+  if (!cu_q) return DIFFQKV_ERR_INVALID_ARG;
+  st = check_pools(cache, shape, pages->page_size);
+  if (st != DIFFQKV_OK) return st;
+  if (cache->num_blocks != pages->num_pages) return DIFFQKV_ERR_INVALID_ARG;
+  if (pages->num_seqs == 0) return DIFFQKV_OK;
+  st = check_workspace(workspace, workspace_bytes, pages_reserve_workspace_bytes(*pages));
+  if (st != DIFFQKV_OK) return st;
+  const cudaError_t err = launch_pages_reserve(cu_q, *pages, *cache, *shape, granted, workspace, dev_status,
+                                               static_cast<cudaStream_t>(stream));
+  return err == cudaSuccess ? DIFFQKV_OK : DIFFQKV_ERR_CUDA;
+}
+
+diffqkv_status diffqkv_pages_copy(const int32_t* src_ids, const int32_t* dst_ids, int32_t n, const diffqkv_cache* src,
+                                  const diffqkv_cache* dst, const diffqkv_shape* shape, int32_t* dev_status, void* stream) {
+  if (!src || !dst || n < 0 || (n > 0 && (!src_ids || !dst_ids))) return DIFFQKV_ERR_INVALID_ARG;
+  diffqkv_status st = check_pools(src, shape, src->page_size);
+  if (st != DIFFQKV_OK) return st;
+  st = check_pools(dst, shape, src->page_size);
+  if (st != DIFFQKV_OK) return st;
+  if (n == 0) return DIFFQKV_OK;
+  const cudaError_t err = launch_pages_copy(src_ids, dst_ids, n, *src, *dst, *shape, dev_status,
+                                            static_cast<cudaStream_t>(stream));
+  return err == cudaSuccess ? DIFFQKV_OK : DIFFQKV_ERR_CUDA;
+}
+
+size_t diffqkv_pages_compact_workspace_bytes(const diffqkv_pages* pages) {
+  return check_pages(pages) == DIFFQKV_OK ? pages_compact_workspace_bytes(*pages) : 0;
+}
+
+diffqkv_status diffqkv_pages_compact(const diffqkv_pages* pages, const diffqkv_cache* cache, const diffqkv_shape* shape,
+                                     int32_t* table_out, int32_t* refs_out, int32_t* live, void* workspace,
+                                     size_t workspace_bytes, int32_t* dev_status, void* stream) {
+  diffqkv_status st = check_pages(pages);
+  if (st != DIFFQKV_OK) return st;
+  if (!table_out || !refs_out) return DIFFQKV_ERR_INVALID_ARG;
+  st = check_pools(cache, shape, pages->page_size);
+  if (st != DIFFQKV_OK) return st;
+  if (cache->num_blocks != pages->num_pages) return DIFFQKV_ERR_INVALID_ARG;
+  st = check_workspace(workspace, workspace_bytes, pages_compact_workspace_bytes(*pages));
+  if (st != DIFFQKV_OK) return st;
+  const cudaError_t err = launch_pages_compact(*pages, *cache, *shape, table_out, refs_out, live, workspace, dev_status,
+                                               static_cast<cudaStream_t>(stream));
+  return err == cudaSuccess ? DIFFQKV_OK : DIFFQKV_ERR_CUDA;
+}
+
 const char* diffqkv_status_string(diffqkv_status status) {
   switch (status) {
     case DIFFQKV_OK: return "ok";
@@ -450,6 +635,7 @@ const char* diffqkv_status_string(diffqkv_status status) {
     case DIFFQKV_ERR_CUDA: return "CUDA call failed";
     case DIFFQKV_ERR_TIMEOUT: return "device wait ran out";
     case DIFFQKV_ERR_INDEX: return "page id out of range";
+    case DIFFQKV_ERR_PAGES: return "not enough free pages";
   }
   return "unknown status";
 }

@@ -133,4 +133,29 @@ cudaError_t launch_decode_topk(const void* q, const diffqkv_cache& c, const diff
                                void* workspace, void* out, float* lse, int* dev_status, cudaStream_t stream,
                                int* kept_ids = nullptr);
 
+// Ragged batches over the cache.  rope_append.cu: rotation of q and k and the cache write; host frequency tables.
+cudaError_t launch_rope_append(const void* q, const void* k_new, const void* v_new, const int* cu_q, int total_q,
+                               long long q_st, long long k_st, long long v_st, const diffqkv_rope& rope,
+                               const CacheView& cache, const diffqkv_shape& s, void* q_out, int* dev_status,
+                               cudaStream_t stream);
+bool rope_frequencies(int rot_dim, double theta, int scaling, double s, double L, double fast, double slow,
+                      double* inv_freq, float* magnitude);
+// Chunk attention: one block per (row, query head) on plain FMAs (decode_generic.cu).
+cudaError_t launch_extend_generic(const DecodeParams& p, diffqkv_dtype dtype, const int* cu_q, int total_q, void* out,
+                                  int out_is_f32, float* lse, cudaStream_t stream);
+// Page upkeep (pages.cu).
+cudaError_t launch_pages_free(const int* seq_ids, const int* keep_tokens, int n, const diffqkv_pages& g, int* dev_status,
+                              cudaStream_t stream);
+size_t pages_fork_workspace_bytes(const diffqkv_pages& g, int n);
+cudaError_t launch_pages_fork(const int* parents, const int* children, int n, const diffqkv_pages& g, void* workspace,
+                              int* dev_status, cudaStream_t stream);
+size_t pages_reserve_workspace_bytes(const diffqkv_pages& g);
+cudaError_t launch_pages_reserve(const int* cu_q, const diffqkv_pages& g, const diffqkv_cache& c, const diffqkv_shape& s,
+                                 int* granted, void* workspace, int* dev_status, cudaStream_t stream);
+cudaError_t launch_pages_copy(const int* src_ids, const int* dst_ids, int n, const diffqkv_cache& from,
+                              const diffqkv_cache& to, const diffqkv_shape& s, int* dev_status, cudaStream_t stream);
+size_t pages_compact_workspace_bytes(const diffqkv_pages& g);
+cudaError_t launch_pages_compact(const diffqkv_pages& g, const diffqkv_cache& c, const diffqkv_shape& s, int* table_out,
+                                 int* refs_out, int* live, void* workspace, int* dev_status, cudaStream_t stream);
+
 }  // namespace diffqkv

@@ -485,6 +485,44 @@ __global__ void __launch_bounds__(kThreads) prefill_generic_kernel(DecodeParams 
   if (lse && tid == 0) lse[row] = l_run > 0.f ? (m_run + log2f(l_run)) * kLn2 : -INFINITY;
 }
 
+// Attention of ragged chunks, one block per (row, query head): the row's sequence is the number of chunk ends at or
+// below it.  Rows that belong to no chunk, and chunks that do not fit the cache, are left alone.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) extend_generic_kernel(DecodeParams p, const int* cu_q, int total_q, void* out,
+                                                                 int out_is_f32, float* lse) {
+  extern __shared__ float q_s[];  // [d_qk]
+  __shared__ GenericSmem sm;
+  const int t = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
+  const CacheView& c = p.cache;
+  int count = 0;
+  for (int b0 = 0; b0 < p.batch; b0 += kThreads) {
+    const int b = b0 + tid;
+    count += __syncthreads_count(b < p.batch && cu_q[b + 1] <= t);
+  }
+  if (count >= p.batch) return;
+  const int b = count, lo = cu_q[b], hi = cu_q[b + 1], past = c.seqlens[b];
+  if (lo < 0 || t < lo || t >= hi || hi > total_q || past < 0 || (long long)past + (hi - lo) > c.max_seqlen) {
+    if (tid == 0) report(p.dev_status, DIFFQKV_ERR_INDEX);
+    return;
+  }
+  const long long row = (long long)t * p.n_q + h;
+  const T* q = reinterpret_cast<const T*>(p.q) + row * p.d_qk;
+  for (int e = tid; e < p.d_qk; e += kThreads) q_s[e] = to_float(q[e]) * p.scale_log2;
+  __syncthreads();
+  float m_run, l_run, acc[kMaxAccPerThread];
+  attend_range<T>(p, b, h, 0, past + (t - lo) + 1, q_s, sm, m_run, l_run, acc);
+  const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
+#pragma unroll
+  for (int e = 0; e < kMaxAccPerThread; ++e) {
+    const int ch = tid + e * kThreads;
+    if (ch < p.d_v) {
+      if (out_is_f32) reinterpret_cast<float*>(out)[row * p.d_v + ch] = acc[e] * inv;
+      else reinterpret_cast<__nv_bfloat16*>(out)[row * p.d_v + ch] = __float2bfloat16_rn(acc[e] * inv);
+    }
+  }
+  if (lse && tid == 0) lse[row] = l_run > 0.f ? (m_run + log2f(l_run)) * kLn2 : -INFINITY;
+}
+
 }  // namespace
 
 // The unit kernel takes head counts whose groups nest (min(n_k, n_v) divides both), at most 8 query heads per unit
@@ -545,6 +583,18 @@ cudaError_t launch_prefill_generic(const DecodeParams& p, diffqkv_dtype dtype, i
     prefill_generic_kernel<float><<<grid, kThreads, smem, stream>>>(p, q_len, out, out_is_f32, lse);
   else
     prefill_generic_kernel<__nv_bfloat16><<<grid, kThreads, smem, stream>>>(p, q_len, out, out_is_f32, lse);
+  count_launch();
+  return cudaGetLastError();
+}
+
+cudaError_t launch_extend_generic(const DecodeParams& p, diffqkv_dtype dtype, const int* cu_q, int total_q, void* out,
+                                  int out_is_f32, float* lse, cudaStream_t stream) {
+  const dim3 grid(total_q, p.n_q);
+  const size_t smem = sizeof(float) * p.d_qk;
+  if (dtype == DIFFQKV_F32)
+    extend_generic_kernel<float><<<grid, kThreads, smem, stream>>>(p, cu_q, total_q, out, out_is_f32, lse);
+  else
+    extend_generic_kernel<__nv_bfloat16><<<grid, kThreads, smem, stream>>>(p, cu_q, total_q, out, out_is_f32, lse);
   count_launch();
   return cudaGetLastError();
 }
