@@ -442,7 +442,7 @@ diffqkv_status diffqkv_decode_topk(const void* q, const diffqkv_cache* cache, co
 
 size_t diffqkv_extend_workspace_bytes(const diffqkv_shape* shape, int32_t total_q) {
   if (check_shape(shape) != DIFFQKV_OK || total_q < 0) return 0;
-  return 256;
+  return extend_workspace_bytes(*shape, total_q);
 }
 
 diffqkv_status diffqkv_extend(const void* q, const int32_t* cu_q, int32_t total_q, const diffqkv_cache* cache,
@@ -456,9 +456,11 @@ diffqkv_status diffqkv_extend(const void* q, const int32_t* cu_q, int32_t total_
   st = check_cache(cache, shape);
   if (st != DIFFQKV_OK) return st;
   if (!aligned16(q) || !aligned16(out)) return DIFFQKV_ERR_ALIGNMENT;
-  if (!workspace || workspace_bytes < diffqkv_extend_workspace_bytes(shape, total_q)) return DIFFQKV_ERR_WORKSPACE;
+  if (!workspace || workspace_bytes < extend_workspace_bytes(*shape, total_q)) return DIFFQKV_ERR_WORKSPACE;
   if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return DIFFQKV_ERR_ALIGNMENT;
   cudaStream_t st_ = static_cast<cudaStream_t>(stream);
+  cudaError_t err = launch_extend(q, cu_q, total_q, *cache, *shape, workspace, out, lse, dev_status, st_);
+  if (err != cudaErrorNotSupported) return err == cudaSuccess ? DIFFQKV_OK : DIFFQKV_ERR_CUDA;
   DecodeParams p;
   p.q = q;
   p.cache = view_of(cache);
@@ -468,7 +470,7 @@ diffqkv_status diffqkv_extend(const void* q, const int32_t* cu_q, int32_t total_
   p.chunk = 0; p.splits = 1;
   p.o_partial = nullptr; p.lse_partial = nullptr;
   p.dev_status = dev_status;
-  const cudaError_t err = launch_extend_generic(p, shape->dtype, cu_q, total_q, out, shape->out_dtype == DIFFQKV_F32, lse, st_);
+  err = launch_extend_generic(p, shape->dtype, cu_q, total_q, out, shape->out_dtype == DIFFQKV_F32, lse, st_);
   if (err == cudaErrorNotSupported) return DIFFQKV_ERR_UNSUPPORTED;
   return err == cudaSuccess ? DIFFQKV_OK : DIFFQKV_ERR_CUDA;
 }

@@ -1,0 +1,1013 @@
+// Causal attention of ragged chunks of new tokens over the cache on the sm_100a tensor cores (diffqkv_extend; paper
+// Section 2 formulation, head map of Eq. (idx)).
+//
+// Mathematics: row i of sequence b sits at position past_b + i and sees cached tokens 0 .. past_b + i:
+//     s_j = scale <q, k_j>,  out = sum_j 2^(s_j log2 e - m) v_j / sum_j 2^(s_j log2 e - m),  one pass over the tokens
+// with a running reference m per row (raised only when exceeded by 2^8, the accumulator is then rescaled).  Scores,
+// statistics and the accumulator are fp32; the weights are rounded to bf16 for the second product (the tensor core
+// takes 16-bit operands), their sum is of the unrounded values.
+//
+// Rows.  The G query heads that share both their K head and their V head read the same tokens, so a tile of 128 matrix
+// rows holds T = 128 / G tokens of the chunk times G heads (row = token * G + head): one token of 32/4/8 heads already
+// fills four rows, and K and V are staged once for all of them.
+//
+// Work.  A chunk is cut into items of 2 T tokens.  An item of more than T tokens ("wide") has two row tiles that share
+// every 128-token K/V tile; one of at most T tokens ("narrow": decode rows, short chunks, the end of a long one) has a
+// single row tile, which is given to both softmax groups: one takes the even K/V tiles, the other the odd ones, and the
+// first joins the two results at the end (softmax does not care which tokens it has seen).  All (sequence, head group,
+// item, K/V tile) form one flat list, wide tiles counting twice, that is divided evenly over the persistent blocks, so
+// that a single row over a long cache and a thousand short chunks both fill the SMs.  A block's run inside an item is
+// a segment; an item that is cut leaves normalised partial rows in the workspace, which extend_combine_kernel joins.
+// Lengths are known on the device alone: each block finds its place by a closed-form sum (floor_sum) and walks from there.
+// Head groups that differ only in their V head (or only in their K head) are given to a team of neighbouring blocks
+// that walk the same tiles at the same time, so that the shared K (V) tiles come out of the second-level cache.
+//
+// Roles of the twelve warps, as in prefill.cu: warp 0 TMA producer, one thread of warp 1 issues the products, warps 4-7
+// and 8-11 are the two softmax groups (one thread per row).  The producer walks the segments and hands them to the other
+// roles through a small ring; the roles meet only at mbarriers, so the next segment's K, V and Q are on their way while the last one is being written out.  Every wait is
+// bounded; on expiry the block reports DIFFQKV_ERR_TIMEOUT, drains and frees its tensor memory.
+#include <atomic>
+#include <numeric>
+
+#include "attn_math.cuh"
+#include "common.cuh"
+#include "ptx.cuh"
+#include "tcgen05.cuh"
+#include "tmap.cuh"
+
+namespace diffqkv {
+namespace {
+
+constexpr int kRows = 128;  // matrix rows of a tile
+constexpr int kKT = 128;    // cached tokens of a K/V tile
+constexpr int kExtendThreads = 384;
+constexpr int kSoftmaxWarp0 = 4;
+constexpr int kTmemCols = 512;
+constexpr int kDMax = 128;
+// Shared memory: two Q tiles, rings of K and V tiles of 160 KB together, the exchange of the two softmax groups.
+constexpr int kRingBytes = 5 * kKT * kDMax * 2;
+constexpr int kExtendSmem = 1024 + 2 * (kRows * kDMax * 2) + kRingBytes + 1024 + 320;
+constexpr float kRescaleThreshold = 8.f;  // log2 domain
+constexpr int kWideCost = 2, kNarrowCost = 1;  // of a K/V tile, in the division of the work
+constexpr int kMaxBlocks = 256;
+
+struct ExtendMeta {  // an item that is cut, left by the block that has its first tile
+  int valid, row_lo, rows, head0, cost, nt, member;
+  long long lo;  // place of the item in the flat list
+};
+
+// A segment as the producer hands it to the other roles, through a ring in shared memory.
+struct Segment {
+  int row_lo, n, past;  // the sequence: first row, rows, tokens cached before
+  int tok0, head0;      // first token of the item within the chunk, first head of the group
+  int ta, tb;           // K/V tiles
+  int nst0;             // tiles of the first softmax group
+  int flags;
+};
+constexpr int kSegRing = 4;
+constexpr int kSegEnd = 1, kSegWide = 2, kSegWhole = 4, kSegFirst = 8;  // first: holds the item's first tile
+
+struct ExtendParams {
+  const int* cu_q;
+  const int* seqlens;
+  const int* page_table;
+  int page_size, max_pages_per_seq, num_blocks, max_seqlen;
+  int batch, total_q, n_q;
+  int G, T;            // heads per group, tokens per row tile
+  int n_units, team, n_teams;  // head groups = n_units * team; blocks = n_teams * team
+  int heads_per_k, heads_per_v;
+  int box_tok;         // tokens per TMA box of the cache maps
+  float scale_log2;
+  void* out;
+  int out_is_f32;
+  float* lse;
+  int* dev_status;
+  float* part_o;       // [2 blocks][slot_rows][d_v] normalised partial rows
+  float* part_lse;     // [2 blocks][slot_rows] base-2 log-sum-exp
+  ExtendMeta* meta;    // [blocks]
+  long long* total_cost;
+  int slot_rows;
+};
+
+// sum of floor((a x + b) / m) for x = 0 .. n - 1, all arguments >= 0, m > 0: the Euclid-like recursion on (m, a).
+__device__ long long floor_sum(long long n, long long m, long long a, long long b) {
+  long long ans = 0;
+  while (n > 0) {
+    if (a >= m) { ans += (n - 1) * n / 2 * (a / m); a %= m; }
+    if (b >= m) { ans += n * (b / m); b %= m; }
+    const long long y = a * n + b;
+    if (y < m) break;
+    n = y / m;
+    b = y % m;
+    const long long t = m; m = a; a = t;
+  }
+  return ans;
+}
+
+// One sequence of the step.
+struct Seq {
+  int lo, n, past, items;  // first row, rows, tokens cached before, items per head group
+  bool bad;                // does not fit
+  __device__ void load(const ExtendParams& p, int b) {
+    lo = p.cu_q[b];
+    const int hi = p.cu_q[b + 1];
+    past = p.seqlens[b];
+    n = hi - lo;
+    bad = lo < 0 || n < 0 || hi > p.total_q || past < 0 || (long long)past + n > p.max_seqlen;
+    if (bad) { n = 0; past = 0; }
+    items = (n + 2 * p.T - 1) / (2 * p.T);
+  }
+  // cost of the first i items, i < items
+  __device__ long long cost_before(const ExtendParams& p, int i) const {
+    return kWideCost * floor_sum(i, kKT, 2 * p.T, (long long)past + 2 * p.T + kKT - 1);
+  }
+  __device__ bool wide(const ExtendParams& p, int i) const { return n - i * 2 * p.T > p.T; }
+  __device__ int tiles(const ExtendParams& p, int i) const {  // K/V tiles of item i
+    return (past + min(n, (i + 1) * 2 * p.T) + kKT - 1) / kKT;
+  }
+  __device__ long long cost(const ExtendParams& p) const {  // of one head group
+    if (n == 0) return 0;
+    return cost_before(p, items - 1) + (wide(p, items - 1) ? kWideCost : kNarrowCost) * (long long)tiles(p, items - 1);
+  }
+};
+
+// The segments of one block, in order.
+struct Walk {
+  int b, u, item;
+  long long item_lo, end, begin;
+  Seq seq;
+  // of the current segment
+  bool wide;
+  int nt, ta, tb, nst0;
+
+  // from the sequence b0 in which the block's range begins, whose flat place is lo
+  __device__ void start(const ExtendParams& p, long long w0, long long w1, int b0, long long lo) {
+    begin = w0; end = w1;
+    b = b0;
+    if (w0 >= w1) { item_lo = w1; b = p.batch; return; }
+    seq.load(p, b);
+    const long long per = seq.cost(p);
+    u = (int)((w0 - lo) / per);
+    const long long r = (w0 - lo) - u * per;
+    int a = 0, z = seq.items;  // largest item whose start is not behind r
+    while (z - a > 1) {
+      const int mid = (a + z) >> 1;
+      if (seq.cost_before(p, mid) <= r) a = mid; else z = mid;
+    }
+    item = a;
+    item_lo = lo + u * per + seq.cost_before(p, item);
+  }
+  __device__ bool next(const ExtendParams& p) {  // false: no more segments
+    while (b < p.batch && item_lo < end) {
+      wide = seq.wide(p, item);
+      nt = seq.tiles(p, item);
+      const int cost = wide ? kWideCost : kNarrowCost;
+      const long long size = (long long)cost * nt;
+      ta = item_lo >= begin ? 0 : (int)((begin - item_lo + cost - 1) / cost);
+      tb = end - item_lo >= size ? nt : (int)((end - item_lo + cost - 1) / cost);
+      if (ta < tb) {
+        if (wide) {
+          const int nt0 = (seq.past + item * 2 * p.T + p.T + kKT - 1) / kKT;  // tiles that the first row tile sees
+          nst0 = max(0, min(tb, nt0) - ta);
+        } else {
+          nst0 = (tb - ta + 1) / 2;
+        }
+        return true;
+      }
+      advance(p);
+    }
+    return false;
+  }
+  __device__ void advance(const ExtendParams& p) {
+    item_lo += (long long)(seq.wide(p, item) ? kWideCost : kNarrowCost) * seq.tiles(p, item);
+    if (++item < seq.items) return;
+    item = 0;
+    if (++u < p.n_units) return;
+    u = 0;
+    do {
+      if (++b >= p.batch) return;
+      seq.load(p, b);
+    } while (seq.n == 0);
+  }
+  __device__ int tok0(const ExtendParams& p) const { return item * 2 * p.T; }
+};
+
+template <int kDQK, int kD>  // channels per head of Q/K and of V: (128, 128), (64, 64) or (64, 128)
+__global__ void __launch_bounds__(kExtendThreads, 1)
+extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
+                   const __grid_constant__ CUtensorMap tmap_v, const ExtendParams p) {
+  constexpr int kHalvesK = kDQK / 64, kHalves = kD / 64;  // 64-channel halves of a Q/K row and of a V row
+  constexpr int kHalvesMax = kHalvesK > kHalves ? kHalvesK : kHalves;
+  constexpr int kQBytes = kRows * kDQK * 2;
+  constexpr int kKBytes = kKT * kDQK * 2;
+  constexpr int kTBytes = kKT * kD * 2;
+  constexpr int kKSlots = 3 * kDMax / kDQK, kVSlots = 2 * kDMax / kD;
+  // With 64-channel values P has tensor-memory columns of its own: [S0 128][S1 128][O0 64][O1 64][P0 64][P1 64], and the
+  // next tile's scores are issued once the current ones are in registers; otherwise P lies over its scores' columns.
+  constexpr bool kSepP = kD == 64;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  unsigned char* q_s = smem;                      // 2 row tiles
+  unsigned char* k_s = q_s + 2 * kQBytes;         // ring of K tiles
+  unsigned char* v_s = k_s + kKSlots * kKBytes;   // ring of V tiles
+  float2* xch_s = reinterpret_cast<float2*>(v_s + kVSlots * kTBytes);  // [128] (m, l) of the second softmax group
+  uint64_t* bars = reinterpret_cast<uint64_t*>(xch_s + kRows);
+  const uint32_t q_full = ptx::smem_u32(bars), q_empty = q_full + 8;
+  const uint32_t k_full0 = q_empty + 8, k_empty0 = k_full0 + 8 * kKSlots;
+  const uint32_t v_full0 = k_empty0 + 8 * kKSlots, v_empty0 = v_full0 + 8 * kVSlots;
+  const uint32_t s_full0 = v_empty0 + 8 * kVSlots, p_half0 = s_full0 + 16, p_full0 = p_half0 + 16;
+  const uint32_t o_done0 = p_full0 + 16, o_free0 = o_done0 + 16, s_free0 = o_free0 + 16;
+  const uint32_t x_full = s_free0 + 16, drain = x_full + 8;
+  const uint32_t seg_full0 = drain + 8, seg_empty0 = seg_full0 + 8 * kSegRing;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 + 2 * kKSlots + 2 * kVSlots + 14 + 2 * kSegRing);
+  volatile int* abort_flag = reinterpret_cast<int*>(tmem_slot + 1);
+  __shared__ Segment seg_s[kSegRing];
+  __shared__ long long scan_s[kExtendThreads / 32 + 1];
+  __shared__ long long seek_lo_s;
+  __shared__ int seek_b_s;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid == 0) {
+    *abort_flag = 0;
+    seek_b_s = p.batch;
+    seek_lo_s = 0;
+    ptx::mbar_init(q_full, 1);
+    ptx::mbar_init(q_empty, 1);
+    for (int s = 0; s < kKSlots; ++s) {
+      ptx::mbar_init(k_full0 + 8 * s, 1);
+      ptx::mbar_init(k_empty0 + 8 * s, 1);
+    }
+    for (int s = 0; s < kVSlots; ++s) {
+      ptx::mbar_init(v_full0 + 8 * s, 1);
+      ptx::mbar_init(v_empty0 + 8 * s, 1);
+    }
+    for (int t = 0; t < 2; ++t) {
+      ptx::mbar_init(s_full0 + 8 * t, 1);
+      ptx::mbar_init(p_half0 + 8 * t, 4);
+      ptx::mbar_init(p_full0 + 8 * t, 4);
+      ptx::mbar_init(o_done0 + 8 * t, 1);
+      ptx::mbar_init(o_free0 + 8 * t, 4);
+      ptx::mbar_init(s_free0 + 8 * t, 4);
+    }
+    ptx::mbar_init(x_full, 4);
+    for (int s = 0; s < kSegRing; ++s) {
+      ptx::mbar_init(seg_full0 + 8 * s, 1);
+      ptx::mbar_init(seg_empty0 + 8 * s, 9);  // the MMA thread and eight softmax warps
+    }
+    ptx::mbar_init(drain, 1);
+    ptx::fence_barrier_init();
+    ptx::prefetch_tmap(&tmap_q);
+    ptx::prefetch_tmap(&tmap_k);
+    ptx::prefetch_tmap(&tmap_v);
+  }
+  if (warp == 1) {
+    tc::tmem_alloc(ptx::smem_u32(tmem_slot), kTmemCols);
+    tc::tmem_relinquish();
+  }
+  // ---- this block's range of the flat list: every thread sums the cost of its share of the sequences
+  const int per_thread = (p.batch + kExtendThreads - 1) / kExtendThreads;
+  const int b_lo = min(tid * per_thread, p.batch), b_hi = min(b_lo + per_thread, p.batch);
+  long long mine = 0;
+  for (int b = b_lo; b < b_hi; ++b) {
+    Seq s;
+    s.load(p, b);
+    if (s.bad && blockIdx.x == 0) report(p.dev_status, DIFFQKV_ERR_INDEX);
+    mine += p.n_units * s.cost(p);
+  }
+  long long incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += y;
+  }
+  if (lane == 31) scan_s[warp + 1] = incl;
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;
+  long long before = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kExtendThreads / 32; ++w) {
+    if (w < warp) before += scan_s[w + 1];
+    total += scan_s[w + 1];
+  }
+  const int team = (int)blockIdx.x / p.team, member = (int)blockIdx.x - team * p.team;
+  const long long w0 = total * team / p.n_teams, w1 = total * (team + 1) / p.n_teams;
+  {
+    long long at = before + incl - mine;
+    if (w0 < w1 && at <= w0 && w0 < at + mine)
+      for (int b = b_lo; b < b_hi; ++b) {
+        Seq s;
+        s.load(p, b);
+        const long long c = p.n_units * s.cost(p);
+        if (w0 < at + c) {
+          seek_b_s = b;
+          seek_lo_s = at;
+          break;
+        }
+        at += c;
+      }
+  }
+  if (blockIdx.x == 0 && tid == 0) *p.total_cost = total;
+  __syncthreads();
+  const uint32_t q_u32 = ptx::smem_u32(q_s), k_u32 = ptx::smem_u32(k_s), v_u32 = ptx::smem_u32(v_s);
+
+  if (warp < kSoftmaxWarp0) {
+  // 12 x 168 = 4 x 72 + 8 x 216: the producer walks the segments in 64-bit arithmetic (56 spilled it)
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+  if (warp == 0) {
+    // ------------------------------------------------------------------ TMA producer
+    // One box per (token part, channel half) of a tile: lane x owns box x of every K tile and of every V tile.
+    const int parts = kKT / p.box_tok;
+    const int boxes = kHalvesMax * parts;
+    const int my_part = lane / kHalvesMax, my_half = lane % kHalvesMax;
+    const uint32_t my_off = my_half * (kKT * 128) + my_part * (p.box_tok * 128);
+    int kc = 0, vc = 0, segs = 0;  // K tiles, V tiles, Q loads requested so far
+    bool ok = true, cut = false;
+    ExtendMeta m = {};
+    Walk w;
+    w.start(p, w0, w1, seek_b_s, seek_lo_s);
+    auto hand_out = [&](const Segment& d) -> bool {
+      const int s = segs % kSegRing;
+      if (!wait_warp(seg_empty0 + 8 * s, ((segs / kSegRing) & 1) ^ 1, abort_flag)) return false;
+      if (lane == 0) {
+        seg_s[s] = d;
+        ptx::mbar_arrive(seg_full0 + 8 * s);  // releases the stores above
+      }
+      __syncwarp();
+      return true;
+    };
+    for (; ok && w.next(p); w.advance(p), ++segs) {
+      const int kv_len = w.seq.past + w.seq.n;
+      const int g = w.u * p.team + member;
+      const int head0 = g * p.G;
+      const int hk = head0 / p.heads_per_k, hv = head0 / p.heads_per_v;  // Eq. (idx)
+      const int tok0 = w.tok0(p);
+      if (w.ta == 0 && w.tb < w.nt) {
+        cut = true;
+        m.valid = 1; m.row_lo = w.seq.lo + tok0; m.rows = min(w.seq.n - tok0, 2 * p.T) * p.G; m.head0 = head0;
+        m.cost = w.wide ? kWideCost : kNarrowCost; m.nt = w.nt; m.member = member; m.lo = w.item_lo;
+      }
+      if (!hand_out({w.seq.lo, w.seq.n, w.seq.past, tok0, head0, w.ta, w.tb, w.nst0,
+                     (w.wide ? kSegWide : 0) | (w.ta == 0 ? kSegFirst : 0) |
+                         (w.ta == 0 && w.tb == w.nt ? kSegWhole : 0)})) {
+        ok = false;
+        break;
+      }
+      const int per_step = w.wide ? 1 : 2;
+      // page of this lane's box of a tile (fetched a step ahead)
+      auto fetch = [&](int tile) -> int {
+        if (!p.page_table) return w.b;
+        const int tok = tile * kKT + my_part * p.box_tok;
+        if (tile >= w.tb || lane >= boxes || tok >= kv_len) return 0;
+        return p.page_table[(long long)w.b * p.max_pages_per_seq + tok / p.page_size];
+      };
+      int blk[2];
+#pragma unroll
+      for (int x = 0; x < 2; ++x) blk[x] = x < per_step ? fetch(w.ta + x) : 0;
+      for (int tile = w.ta; tile < w.tb && ok; tile += per_step) {
+        const int count = min(per_step, w.tb - tile);
+        int now[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          now[x] = blk[x];
+          if (x < count && lane < boxes && tile * kKT + my_part * p.box_tok < kv_len &&
+              (now[x] < 0 || now[x] >= p.num_blocks)) {  // never read outside the pool: flag it, read block 0 instead
+            report(p.dev_status, DIFFQKV_ERR_INDEX);
+            now[x] = 0;
+          }
+          blk[x] = x < per_step ? fetch(tile + per_step + x) : 0;
+        }
+        for (int kv = 0; kv < 2 && ok; ++kv) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            if (x >= count || !ok) continue;
+            const int tok = (tile + x) * kKT;
+            const int parts_valid = min(parts, (kv_len - tok + p.box_tok - 1) / p.box_tok);
+            const int first = tok + my_part * p.box_tok;
+            const int slot_tok = p.page_table ? first % p.page_size : first;
+            const bool here = lane < boxes && my_part < parts_valid;
+            if (kv == 0) {
+              const int s = kc % kKSlots;
+              if (!wait_warp(k_empty0 + 8 * s, ((kc / kKSlots) & 1) ^ 1, abort_flag)) { ok = false; continue; }
+              if (lane == 0) ptx::mbar_arrive_expect_tx(k_full0 + 8 * s, (uint32_t)parts_valid * p.box_tok * 128u * kHalvesK);
+              __syncwarp();
+              if (here && my_half < kHalvesK)
+                ptx::tma_load_5d(k_u32 + s * kKBytes + my_off, &tmap_k, k_full0 + 8 * s, 0, slot_tok, my_half, hk, now[x]);
+              ++kc;
+            } else {
+              const int s = vc % kVSlots;
+              if (!wait_warp(v_empty0 + 8 * s, ((vc / kVSlots) & 1) ^ 1, abort_flag)) { ok = false; continue; }
+              if (lane == 0) ptx::mbar_arrive_expect_tx(v_full0 + 8 * s, (uint32_t)parts_valid * p.box_tok * 128u * kHalves);
+              __syncwarp();
+              if (here && my_half < kHalves)
+                ptx::tma_load_5d(v_u32 + s * kTBytes + my_off, &tmap_v, v_full0 + 8 * s, 0, slot_tok, my_half, hv, now[x]);
+              ++vc;
+            }
+          }
+          if (kv == 0 && tile == w.ta && ok) {  // the segment's Q behind its first K tiles
+            if (!wait_warp(q_empty, (segs & 1) ^ 1, abort_flag)) { ok = false; continue; }
+            if (lane == 0) {
+              const int tiles = w.wide ? 2 : 1;
+              ptx::mbar_arrive_expect_tx(q_full, (uint32_t)(tiles * kHalvesK * p.G * p.T) * 128u);
+              for (int t = 0; t < tiles; ++t)
+#pragma unroll
+                for (int h = 0; h < kHalvesK; ++h)
+                  ptx::tma_load_4d(q_u32 + t * kQBytes + h * (kRows * 128), &tmap_q, q_full, 0, head0, w.seq.lo + tok0 + t * p.T, h);
+            }
+            __syncwarp();
+          }
+        }
+      }
+      if (!ok) break;
+    }
+    if (ok) ok = hand_out({0, 0, 0, 0, 0, 0, 0, 0, kSegEnd});
+    if (lane == 0) {
+      if (!cut) m.valid = 0;
+      p.meta[blockIdx.x] = m;
+    }
+    ptx::grid_launch_dependents();
+    if (!ok) {
+      report(p.dev_status, DIFFQKV_ERR_TIMEOUT);
+      // give copies in flight a bounded chance to land before the block's shared memory is released (a Q request is
+      // counted once its segment is over, so the last one may be one more)
+      if (segs > 0) ptx::mbar_wait(q_full, (uint32_t)(segs - 1) & 1u, nullptr);
+      ptx::mbar_wait(q_full, (uint32_t)segs & 1u, nullptr);
+      for (int s = 0; s < min(kc, kKSlots); ++s)
+        ptx::mbar_wait(k_full0 + 8 * s, (uint32_t)((kc - s + kKSlots - 1) / kKSlots - 1) & 1u, nullptr);
+      for (int s = 0; s < min(vc, kVSlots); ++s)
+        ptx::mbar_wait(v_full0 + 8 * s, (uint32_t)((vc - s + kVSlots - 1) / kVSlots - 1) & 1u, nullptr);
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ MMA issuer (one thread)
+    constexpr uint32_t idesc = tc::idesc_bf16_f32(kRows, kKT, 0, 0);    // S: Q and K both K-major, N = 128 tokens
+    constexpr uint32_t idesc_pv = tc::idesc_bf16_f32(kRows, kD, 0, 1);  // O: V is N-major, N = kD channels
+    constexpr uint32_t hi = tc::smem_desc_hi_sw128(1024);
+    if (lane == 0) {
+      bool ok = true;
+      const uint32_t q_lo = tc::smem_desc_lo(q_u32, 16), k_lo = tc::smem_desc_lo(k_u32, 16);
+      const uint32_t v_lo = tc::smem_desc_lo(v_u32, kKT * 128);  // 64-channel chunks of V are one half tile apart
+      auto issue_s = [&](int t, int qt, int slot) {  // S_t = Q_qt . K^T
+        const uint32_t qa = q_lo + qt * (kQBytes >> 4), ka = k_lo + slot * (kKBytes >> 4);
+        const uint32_t d = tmem_base + t * 128;
+        tc::mma_ss_halves<false>(d, qa, hi, ka, hi, idesc);
+#pragma unroll
+        for (int ks = 1; ks < kDQK / 16; ++ks) {
+          const uint32_t step = ((ks / 4) * (128 * 128) + (ks % 4) * 32) >> 4;
+          tc::mma_ss_halves<true>(d, qa + step, hi, ka + step, hi, idesc);
+        }
+        tc::commit(s_full0 + 8 * t);
+      };
+      auto issue_pv = [&](int t, int slot, bool first, int half) {  // O_t += P_t . V, 64 tokens at a time
+        const uint32_t va = v_lo + slot * (kTBytes >> 4);
+        const uint32_t d = tmem_base + 256 + t * kD, pa = kSepP ? tmem_base + 384 + t * 64 : tmem_base + t * 128;
+        constexpr int kSteps = kKT / 32;
+        if (half == 0) {
+          if (first) tc::mma_ts_halves<false>(d, pa, va, hi, idesc_pv);
+          else tc::mma_ts_halves<true>(d, pa, va, hi, idesc_pv);
+#pragma unroll
+          for (int k = 1; k < kSteps; ++k) tc::mma_ts_halves<true>(d, pa + k * 8, va + ((k * 16 * 128) >> 4), hi, idesc_pv);
+        } else {
+#pragma unroll
+          for (int k = kSteps; k < 2 * kSteps; ++k)
+            tc::mma_ts_halves<true>(d, pa + k * 8, va + ((k * 16 * 128) >> 4), hi, idesc_pv);
+          tc::commit(o_done0 + 8 * t);
+        }
+      };
+      int base = 0, segs = 0;       // K/V tiles and segments before this one
+      int tiles_done[2] = {0, 0};   // products O_t += P_t V issued
+      int scores_done[2] = {0, 0};  // products S_t issued
+      int uses[2] = {0, 0};         // segments in which O_t has been used
+      for (;; ++segs) {
+        const int slot = segs % kSegRing;
+        if (!ptx::mbar_wait(seg_full0 + 8 * slot, (segs / kSegRing) & 1, abort_flag)) { ok = false; break; }
+        const int flags = seg_s[slot].flags, tiles = seg_s[slot].tb - seg_s[slot].ta, nst0 = seg_s[slot].nst0;
+        ptx::mbar_arrive(seg_empty0 + 8 * slot);
+        if (flags & kSegEnd) break;
+        const bool wide = flags & kSegWide;
+        const int steps = wide ? tiles : nst0;
+        const int nst[2] = {nst0, wide ? tiles : tiles - nst0};
+        auto tile_of = [&](int i, int t) { return base + (wide ? i : 2 * i + t); };
+        auto scores = [&](int i, int t) -> bool {  // S_t of step i
+          const int idx = tile_of(i, t), s = idx % kKSlots;
+          if (!ptx::mbar_wait(k_full0 + 8 * s, (idx / kKSlots) & 1, abort_flag)) return false;
+          if (kSepP && scores_done[t] > 0 && !ptx::mbar_wait(s_free0 + 8 * t, (scores_done[t] - 1) & 1, abort_flag)) return false;
+          tc::fence_after_sync();
+          issue_s(t, wide ? t : 0, s);
+          ++scores_done[t];
+          if (!wide) tc::commit(k_empty0 + 8 * s);
+          return true;
+        };
+        auto values = [&](int i, int t) -> bool {  // O_t += P_t V of step i
+          const int idx = tile_of(i, t), s = idx % kVSlots;
+          if (i == 0) {  // the accumulator of the segment before has been read out
+            if (uses[t] > 0 && !ptx::mbar_wait(o_free0 + 8 * t, (uses[t] - 1) & 1, abort_flag)) return false;
+            ++uses[t];
+          }
+          if (!ptx::mbar_wait(p_half0 + 8 * t, tiles_done[t] & 1, abort_flag)) return false;
+          if (!ptx::mbar_wait(v_full0 + 8 * s, (idx / kVSlots) & 1, abort_flag)) return false;
+          tc::fence_after_sync();
+          issue_pv(t, s, i == 0, 0);
+          if (!ptx::mbar_wait(p_full0 + 8 * t, tiles_done[t] & 1, abort_flag)) return false;
+          tc::fence_after_sync();
+          issue_pv(t, s, i == 0, 1);
+          ++tiles_done[t];
+          if (!wide) tc::commit(v_empty0 + 8 * s);
+          return true;
+        };
+        if (!ptx::mbar_wait(q_full, segs & 1, abort_flag)) { ok = false; break; }
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          if (ok && nst[t] > 0) ok = scores(0, t);
+        if (ok && wide) tc::commit(k_empty0 + 8 * (base % kKSlots));
+        if (ok && steps == 1) tc::commit(q_empty);
+        for (int i = 0; i < steps && ok; ++i) {
+          if (kSepP) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+              if (ok && i + 1 < nst[t]) ok = scores(i + 1, t);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+              if (ok && i < nst[t]) ok = values(i, t);
+          } else {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              if (ok && i < nst[t]) ok = values(i, t);
+              // P_t of step i is consumed first (same pipe, in order): S_t may be overwritten
+              if (ok && i + 1 < nst[t]) ok = scores(i + 1, t);
+            }
+          }
+          if (!ok) break;
+          if (wide) {  // every product that reads V tile i and K tile i + 1 has been issued
+            tc::commit(v_empty0 + 8 * ((base + i) % kVSlots));
+            if (i + 1 < steps) tc::commit(k_empty0 + 8 * ((base + i + 1) % kKSlots));
+          }
+          if (i + 2 == steps) tc::commit(q_empty);
+        }
+        if (!ok) break;
+        base += tiles;
+      }
+      if (!ok) report(p.dev_status, DIFFQKV_ERR_TIMEOUT);
+      tc::commit(drain);
+    }
+    __syncwarp();
+  }
+  } else {
+    // ------------------------------------------------------------------ softmax warps
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    const int t = (warp - kSoftmaxWarp0) >> 2;  // softmax group
+    const int quarter = warp & 3;               // tensor-memory lanes this warp may touch
+    const int r = quarter * 32 + lane;          // row
+    const uint32_t lane_base = tmem_base + ((uint32_t)(quarter * 32) << 16);
+    const uint32_t s_taddr = lane_base + t * 128;
+    const uint32_t p_taddr = kSepP ? lane_base + 384 + t * 64 : s_taddr;
+    const uint32_t o_taddr = lane_base + 256 + t * kD;
+    int base = 0;      // K/V tiles before this segment
+    int c = 0;         // tiles of this group so far
+    int joins = 0;     // narrow segments in which both groups had tiles
+    bool ok = true;
+    for (int segs = 0;; ++segs) {
+      const int slot = segs % kSegRing;
+      if (!wait_warp(seg_full0 + 8 * slot, (segs / kSegRing) & 1, abort_flag)) { ok = false; break; }
+      const Segment& w = seg_s[slot];  // released at the end of the segment
+      if (w.flags & kSegEnd) break;
+      const bool wide = w.flags & kSegWide;
+      const int ta = w.ta, tiles = w.tb - ta, nst1 = wide ? tiles : tiles - w.nst0;
+      const int n = t == 0 ? w.nst0 : nst1;
+      const int tok0 = w.tok0 + (wide ? t * p.T : 0);  // first token of this group's rows, within the chunk
+      const int kv_len = w.past + w.n;
+      const int first_pos = w.past + tok0;
+      const int qpos = min(first_pos + r / p.G, kv_len - 1);
+      const int rows = min(p.T, w.n - tok0) * p.G;  // rows in use
+      const bool busy = quarter * 32 < rows;            // some row of this warp is in use
+      float m_ref = -INFINITY, l = 0.f;
+      for (int i = 0; i < n; ++i, ++c) {
+        const int j = ta + (wide ? i : 2 * i + t);
+        if (!wait_warp(s_full0 + 8 * t, c & 1, abort_flag)) { ok = false; break; }
+        tc::fence_after_sync();
+        const int k0 = j * kKT;
+        if (k0 + kKT > kv_len) {
+          // ragged last tile: V rows past the sequence end hold whatever followed in memory; zero them before any
+          // product reads the tile (0 * NaN would poison it).  Both groups may do this; they write the same zeros.
+          const int idx = base + j - ta, vslot = idx % kVSlots;
+          if (!wait_warp(v_full0 + 8 * vslot, (idx / kVSlots) & 1, abort_flag)) { ok = false; break; }
+          if (r >= kv_len - k0) {
+#pragma unroll
+            for (int half = 0; half < kHalves; ++half) {
+              uint4* dst = reinterpret_cast<uint4*>(v_s + vslot * kTBytes + half * (kKT * 128) + r * 128);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) dst[e] = make_uint4(0, 0, 0, 0);
+            }
+          }
+          ptx::fence_proxy_async();
+        }
+        if (!busy) {  // nothing to compute, but the barriers count this warp
+          if (kSepP) {
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(s_free0 + 8 * t);
+            if (i > 0 && !wait_warp(o_done0 + 8 * t, (c - 1) & 1, abort_flag)) { ok = false; break; }
+          }
+          __syncwarp();
+          if (lane == 0) {
+            ptx::mbar_arrive(p_half0 + 8 * t);
+            ptx::mbar_arrive(p_full0 + 8 * t);
+          }
+          continue;
+        }
+        // ---- all 128 scores of the row into registers; row maximum of the raw scores (scale > 0 keeps the order)
+        uint32_t s[128];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) tc::ld_32x32b_x32(s_taddr + x * 32, *reinterpret_cast<uint32_t(*)[32]>(&s[x * 32]));
+        tc::wait_ld();
+        if (kSepP) {  // the score columns may take the next tile's scores from here on
+          tc::fence_before_sync();
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(s_free0 + 8 * t);
+        }
+        if (k0 + kKT - 1 > first_pos) {  // the tile reaches past some row's position
+#pragma unroll
+          for (int e = 0; e < 128; ++e)
+            if (k0 + e > qpos) s[e] = 0xff800000u;  // -inf
+        }
+        float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 128; e += 8) {
+          mx0 = max3(mx0, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+          mx1 = max3(mx1, __uint_as_float(s[e + 2]), __uint_as_float(s[e + 3]));
+          mx2 = max3(mx2, __uint_as_float(s[e + 4]), __uint_as_float(s[e + 5]));
+          mx3 = max3(mx3, __uint_as_float(s[e + 6]), __uint_as_float(s[e + 7]));
+        }
+        const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3)) * p.scale_log2;
+        float alpha = 1.f;
+        const bool bump = mx > m_ref + kRescaleThreshold;  // true on the first tile that the row sees (m_ref = -inf)
+        if (bump) {
+          alpha = exp2f(m_ref - mx);
+          m_ref = mx;
+        }
+        if (i > 0 && __any_sync(0xffffffffu, bump)) {  // rescale this warp's rows of O in tensor memory
+          if (!wait_warp(o_done0 + 8 * t, (c - 1) & 1, abort_flag)) { ok = false; break; }
+          tc::fence_after_sync();
+#pragma unroll 1
+          for (int x = 0; x < kD / 32; ++x) {
+            uint32_t o[32];
+            tc::ld_32x32b_x32(o_taddr + x * 32, o);
+            tc::wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+            tc::st_32x32b_x32(o_taddr + x * 32, o);
+          }
+          tc::wait_st();
+        }
+        l *= alpha;
+        const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;  // a segment may begin behind a row's position
+        if (kSepP && i > 0) {  // P's own columns still hold the previous tile's P until its product is done
+          if (!wait_warp(o_done0 + 8 * t, (c - 1) & 1, abort_flag)) { ok = false; break; }
+          tc::fence_after_sync();
+        }
+        // ---- P = 2^(S scale - m_ref) as packed bf16; fp32 row sum.  The first 64 tokens are announced on their own,
+        // so that their half of the product runs during the second half's work.
+        uint64_t l2 = 0;
+        const uint64_t scale2 = pair(p.scale_log2, p.scale_log2), negm2 = pair(neg_m, neg_m);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          uint32_t pw[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) {
+            float x0, x1;
+            unpair(fma2(pair(s[x * 64 + 2 * e], s[x * 64 + 2 * e + 1]), scale2, negm2), x0, x1);
+            const float p0 = ex2(x0), p1 = ex2(x1);
+            pw[e] = pack2(p0, p1);
+            l2 = add2(l2, pair(p0, p1));
+          }
+          tc::st_32x32b_x32(p_taddr + x * 32, pw);
+          if (x == 0) {
+            tc::wait_st();
+            tc::fence_before_sync();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(p_half0 + 8 * t);
+          }
+        }
+        float l0, l1;
+        unpair(l2, l0, l1);
+        l += l0 + l1;
+        tc::wait_st();
+        tc::fence_before_sync();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(p_full0 + 8 * t);
+      }
+      if (!ok) break;
+      base += tiles;
+      // ---- the segment's result
+      if (n > 0) {
+        if (!wait_warp(o_done0 + 8 * t, (c - 1) & 1, abort_flag)) { ok = false; break; }
+        tc::fence_after_sync();
+      }
+      float weight = l > 0.f ? 1.f / l : 0.f, weight1 = 0.f, lse2 = l > 0.f ? m_ref + log2f(l) : -INFINITY;
+      const bool join = !wide && nst1 > 0;
+      if (join && t == 1) {  // hand over to the first group, which reads both accumulators
+        xch_s[r] = make_float2(m_ref, l);
+        tc::fence_before_sync();
+        __syncwarp();
+        if (lane == 0) {
+          ptx::mbar_arrive(x_full);
+          ptx::mbar_arrive(seg_empty0 + 8 * slot);
+        }
+        continue;
+      }
+      if (!wide && t == 1) {
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(seg_empty0 + 8 * slot);
+        continue;
+      }
+      if (join) {
+        if (!wait_warp(x_full, joins & 1, abort_flag)) { ok = false; break; }
+        ++joins;
+        tc::fence_after_sync();
+        const float2 o = xch_s[r];
+        const float top = fmaxf(l > 0.f ? m_ref : -INFINITY, o.y > 0.f ? o.x : -INFINITY);
+        const float e0 = l > 0.f ? exp2f(m_ref - top) : 0.f, e1 = o.y > 0.f ? exp2f(o.x - top) : 0.f;
+        const float sum = l * e0 + o.y * e1;
+        weight = sum > 0.f ? e0 / sum : 0.f;
+        weight1 = sum > 0.f ? e1 / sum : 0.f;
+        lse2 = sum > 0.f ? top + log2f(sum) : -INFINITY;
+      }
+      if (busy) {
+        const bool store = r < rows;
+        const bool whole = w.flags & kSegWhole;
+        const int row_tok = r / p.G;
+        const long long row = (long long)(w.row_lo + tok0 + row_tok) * p.n_q + w.head0 + (r - row_tok * p.G);
+        const long long prow = (2LL * blockIdx.x + ((w.flags & kSegFirst) ? 1 : 0)) * p.slot_rows + (wide ? t * p.T * p.G : 0) + r;
+        const bool as_f32 = !whole || p.out_is_f32;
+        float* dst32 = whole ? reinterpret_cast<float*>(p.out) + row * kD : p.part_o + prow * kD;
+        __nv_bfloat16* dst16 = reinterpret_cast<__nv_bfloat16*>(p.out) + row * kD;
+        if (n > 0) {
+#pragma unroll 1
+          for (int x = 0; x < kD / 32; ++x) {
+            uint32_t o[32], o1[32];
+            tc::ld_32x32b_x32(o_taddr + x * 32, o);
+            if (join) tc::ld_32x32b_x32(o_taddr + kD + x * 32, o1);
+            tc::wait_ld();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              float y = __uint_as_float(o[e]) * weight;
+              if (join) y = fmaf(__uint_as_float(o1[e]), weight1, y);
+              o[e] = __float_as_uint(y);
+            }
+            if (!store) continue;
+            if (as_f32) {
+              uint4* dst = reinterpret_cast<uint4*>(dst32 + x * 32);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) dst[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+            } else {
+              uint4* dst = reinterpret_cast<uint4*>(dst16 + x * 32);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                uint32_t y[4];
+#pragma unroll
+                for (int z = 0; z < 4; ++z)
+                  y[z] = pack2(__uint_as_float(o[8 * e + 2 * z]), __uint_as_float(o[8 * e + 2 * z + 1]));
+                dst[e] = make_uint4(y[0], y[1], y[2], y[3]);
+              }
+            }
+          }
+        }
+        if (store) {
+          if (!whole) p.part_lse[prow] = lse2;
+          else if (p.lse) p.lse[row] = lse2 * kLn2;
+        }
+      }
+      // the accumulators may be overwritten
+      tc::fence_before_sync();
+      __syncwarp();
+      if (lane == 0) {
+        if (n > 0) ptx::mbar_arrive(o_free0 + 8 * t);
+        if (join) ptx::mbar_arrive(o_free0 + 8);
+        ptx::mbar_arrive(seg_empty0 + 8 * slot);
+      }
+    }
+    if (!ok) report(p.dev_status, DIFFQKV_ERR_TIMEOUT);
+  }
+
+  // ---- teardown: all MMAs this block issued must be done before its tensor memory is released
+  tc::fence_before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    ptx::mbar_wait(drain, 0, nullptr);
+    tc::fence_after_sync();
+    tc::tmem_dealloc(tmem_base, kTmemCols);
+  }
+}
+
+// Joins the partial rows of the items that were cut: block (x, y) takes every gridDim.y-th group of rows of the item
+// that block x of the attention kernel began, a warp per row.
+template <int kD>
+__global__ void __launch_bounds__(256) extend_combine_kernel(const ExtendParams p) {
+  ptx::grid_dependency_wait();
+  const ExtendMeta m = p.meta[blockIdx.x];
+  constexpr int kWarps = 8;
+  const int row0 = blockIdx.y * kWarps;
+  if (!m.valid || row0 >= m.rows) return;
+  __shared__ int slots[kMaxBlocks];
+  __shared__ int count_s;
+  const long long total = *p.total_cost;
+  const int first = (int)blockIdx.x / p.team;
+  if (threadIdx.x == 0) count_s = 0;
+  __syncthreads();
+  // the teams that own tiles of the item, from the first on (in order: sums do not depend on timing)
+  const int k = first + threadIdx.x;
+  if (k < p.n_teams) {
+    const long long a = total * k / p.n_teams, z = total * (k + 1) / p.n_teams;
+    int slot = -1;
+    if (a < m.lo + (long long)m.cost * m.nt) {
+      const int ta = a <= m.lo ? 0 : (int)((a - m.lo + m.cost - 1) / m.cost);
+      const int tb = (int)min((long long)m.nt, (z - m.lo + m.cost - 1) / m.cost);
+      if (ta < tb) slot = 2 * (k * p.team + m.member) + (ta == 0);
+      atomicMax(&count_s, k - first + 1);
+    }
+    slots[threadIdx.x] = slot;
+  }
+  __syncthreads();
+  const int n = count_s, lane = threadIdx.x & 31;
+  constexpr int kC = kD / 32;  // channels per lane
+  const int r = row0 + (threadIdx.x >> 5);
+  if (r >= m.rows) return;
+  float top = -INFINITY;
+  for (int i = lane; i < n; i += 32)
+    if (slots[i] >= 0) top = fmaxf(top, p.part_lse[(long long)slots[i] * p.slot_rows + r]);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  float acc[kC], sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < kC; ++e) acc[e] = 0.f;
+#pragma unroll 4
+  for (int i = 0; i < n; ++i) {
+    const int slot = slots[i];
+    if (slot < 0) continue;
+    const long long at = (long long)slot * p.slot_rows + r;
+    const float ls = p.part_lse[at];
+    if (ls == -INFINITY) continue;  // the part saw no token of this row
+    const float f = exp2f(ls - top);
+    sum += f;
+    const float* o = p.part_o + at * kD + lane * kC;
+#pragma unroll
+    for (int e = 0; e < kC; ++e) acc[e] = fmaf(f, o[e], acc[e]);
+  }
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  const int tok = r / p.G;
+  const long long row = (long long)(m.row_lo + tok) * p.n_q + m.head0 + (r - tok * p.G);
+  if (p.out_is_f32) {
+    float* dst = reinterpret_cast<float*>(p.out) + row * kD + lane * kC;
+#pragma unroll
+    for (int e = 0; e < kC; ++e) dst[e] = acc[e] * inv;
+  } else {
+    uint32_t* dst = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(p.out) + row * kD + lane * kC);
+#pragma unroll
+    for (int e = 0; e < kC; e += 2) dst[e / 2] = pack2(acc[e] * inv, acc[e + 1] * inv);
+  }
+  if (p.lse && lane == 0) p.lse[row] = sum > 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+}
+
+// Tensor map over one cache pool: dims (64 channels, token slot, channel half, head, block); a box brings box_tok tokens
+// of one 64-channel half.
+bool make_cache_map(CUtensorMap* map, const void* base, int d, long long tok_extent, int heads, long long blocks,
+                    long long st_tok, long long st_head, long long st_blk, int box_tok) {
+  const cuuint64_t dims[5] = {64, (cuuint64_t)tok_extent, (cuuint64_t)(d / 64), (cuuint64_t)heads, (cuuint64_t)blocks};
+  const cuuint64_t strides[4] = {(cuuint64_t)st_tok * 2, 128, (cuuint64_t)st_head * 2, (cuuint64_t)st_blk * 2};
+  const cuuint32_t box[5] = {64, (cuuint32_t)box_tok, 1, 1, 1};
+  return make_tmap_bf16_sw128(map, base, 5, dims, strides, box);
+}
+
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+struct Plan {
+  int G, T, groups, team, n_teams, slot_rows;
+};
+
+int sm_count() {
+  static std::atomic<int> cached{0};
+  int n = cached.load();
+  if (n == 0) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+        n <= 0)
+      n = 148;  // without a device (workspace sizes are asked on the host)
+    else
+      cached = n;
+  }
+  return n < kMaxBlocks ? n : kMaxBlocks;
+}
+
+// Head groups, rows per tile and teams; the same for the workspace's size and the launch.
+Plan make_plan(const diffqkv_shape& s, int total_q) {
+  Plan pl;
+  const int per_k = s.n_q / s.n_k, per_v = s.n_q / s.n_v;
+  int G = std::gcd(per_k, per_v);
+  if (G > kRows) {  // the largest divisor that fits a tile
+    int d = kRows;
+    while (G % d != 0) --d;
+    G = d;
+  }
+  pl.G = G;
+  pl.T = kRows / G;
+  pl.groups = s.n_q / G;
+  // groups of one K head (V head) that differ in the other head only sit next to each other
+  const int share = (per_k > per_v ? per_k : per_v) / G;
+  int team = share < 8 ? share : 8;
+  while (share % team != 0 || pl.groups % team != 0) --team;
+  pl.team = team;
+  pl.n_teams = sm_count() / team;
+  const long long rows = 2LL * pl.T * G, asked = (long long)total_q * G;
+  pl.slot_rows = (int)(asked < rows ? asked : rows);
+  return pl;
+}
+
+size_t plan_bytes(const Plan& pl, int d_v) {
+  const size_t slots = 2 * (size_t)pl.n_teams * pl.team;
+  return 256 + up256(sizeof(ExtendMeta) * kMaxBlocks) + up256(slots * pl.slot_rows * sizeof(float)) +
+         up256(slots * pl.slot_rows * d_v * sizeof(float));
+}
+
+bool dims_supported(const diffqkv_shape& s) {
+  if (s.dtype != DIFFQKV_BF16 || !(s.scale > 0.f)) return false;
+  return (s.d_qk == 128 && s.d_v == 128) || (s.d_qk == 64 && s.d_v == 64) || (s.d_qk == 64 && s.d_v == 128);
+}
+
+}  // namespace
+
+size_t extend_workspace_bytes(const diffqkv_shape& s, int total_q) {
+  return dims_supported(s) ? plan_bytes(make_plan(s, total_q), s.d_v) : 256;
+}
+
+// cudaErrorNotSupported, with nothing launched, where the plain kernel has to take the call.
+cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const diffqkv_cache& c, const diffqkv_shape& s,
+                          void* workspace, void* out, float* lse, int* dev_status, cudaStream_t stream) {
+  if (!dims_supported(s) || c.max_seqlen < 1 || c.max_seqlen > 0x7ffffe00 || c.num_blocks < 1) return cudaErrorNotSupported;
+  int box_tok = kKT;
+  if (c.page_table) {
+    if (c.page_size >= kKT) {
+      if (c.page_size % kKT != 0) return cudaErrorNotSupported;
+    } else {
+      if (c.page_size < 8 || kKT % c.page_size != 0) return cudaErrorNotSupported;
+      box_tok = c.page_size;
+    }
+  }
+  const Plan pl = make_plan(s, total_q);
+  CUtensorMap mq, mk, mv;
+  {
+    const cuuint64_t dims[4] = {64, (cuuint64_t)s.n_q, (cuuint64_t)total_q, (cuuint64_t)(s.d_qk / 64)};
+    const cuuint64_t strides[3] = {(cuuint64_t)s.d_qk * 2, (cuuint64_t)s.n_q * s.d_qk * 2, 128};
+    const cuuint32_t box[4] = {64, (cuuint32_t)pl.G, (cuuint32_t)pl.T, 1};
+    if (!make_tmap_bf16_sw128(&mq, q, 4, dims, strides, box)) return cudaErrorNotSupported;
+  }
+  const long long tok_extent = c.page_table ? c.page_size : c.max_seqlen;
+  if (!make_cache_map(&mk, c.k_cache, s.d_qk, tok_extent, s.n_k, c.num_blocks, c.k_stride_tok, c.k_stride_head,
+                      c.k_stride_blk, box_tok) ||
+      !make_cache_map(&mv, c.v_cache, s.d_v, tok_extent, s.n_v, c.num_blocks, c.v_stride_tok, c.v_stride_head,
+                      c.v_stride_blk, box_tok))
+    return cudaErrorNotSupported;
+
+  ExtendParams p = {};
+  p.cu_q = cu_q; p.seqlens = c.seqlens; p.page_table = c.page_table;
+  p.page_size = c.page_size; p.max_pages_per_seq = c.max_pages_per_seq; p.num_blocks = c.num_blocks; p.max_seqlen = c.max_seqlen;
+  p.batch = s.batch; p.total_q = total_q; p.n_q = s.n_q;
+  p.G = pl.G; p.T = pl.T; p.team = pl.team; p.n_teams = pl.n_teams; p.n_units = pl.groups / pl.team;
+  p.heads_per_k = s.n_q / s.n_k; p.heads_per_v = s.n_q / s.n_v;
+  p.box_tok = box_tok;
+  p.scale_log2 = s.scale * kLog2e;
+  p.out = out; p.out_is_f32 = s.out_dtype == DIFFQKV_F32; p.lse = lse; p.dev_status = dev_status;
+  p.slot_rows = pl.slot_rows;
+  const int blocks = pl.n_teams * pl.team;
+  char* at = static_cast<char*>(workspace);
+  p.total_cost = reinterpret_cast<long long*>(at);
+  at += 256;
+  p.meta = reinterpret_cast<ExtendMeta*>(at);
+  at += up256(sizeof(ExtendMeta) * kMaxBlocks);
+  p.part_lse = reinterpret_cast<float*>(at);
+  at += up256(2 * (size_t)blocks * pl.slot_rows * sizeof(float));
+  p.part_o = reinterpret_cast<float*>(at);
+
+  using ExtendFn = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const ExtendParams);
+  const ExtendFn fn = s.d_v == 64 ? extend_attn_kernel<64, 64>
+                                  : (s.d_qk == 128 ? extend_attn_kernel<128, 128> : extend_attn_kernel<64, 128>);
+  cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kExtendSmem);
+  if (err != cudaSuccess) return err;
+  fn<<<blocks, kExtendThreads, kExtendSmem, stream>>>(mq, mk, mv, p);
+  count_launch();
+  err = cudaGetLastError();
+  if (err != cudaSuccess) return err;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)blocks, (unsigned)((pl.slot_rows + 7) / 8));
+  cfg.blockDim = dim3(256);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  err = cudaLaunchKernelEx(&cfg, s.d_v == 64 ? extend_combine_kernel<64> : extend_combine_kernel<128>, p);
+  if (err != cudaSuccess) return err;
+  count_launch();
+  return cudaGetLastError();
+}
+
+}  // namespace diffqkv
