@@ -62,6 +62,7 @@ struct Segment {
   int tok0, head0;      // first token of the item within the chunk, first head of the group
   int ta, tb;           // K/V tiles
   int nst0;             // tiles of the first softmax group
+  int v0;               // V tiles requested before the segment (the ring's position)
   int flags;
 };
 constexpr int kSegRing = 4;
@@ -348,7 +349,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         m.valid = 1; m.row_lo = w.seq.lo + tok0; m.rows = min(w.seq.n - tok0, 2 * p.T) * p.G; m.head0 = head0;
         m.cost = w.wide ? kWideCost : kNarrowCost; m.nt = w.nt; m.member = member; m.lo = w.item_lo;
       }
-      if (!hand_out({w.seq.lo, w.seq.n, w.seq.past, tok0, head0, w.ta, w.tb, w.nst0,
+      if (!hand_out({w.seq.lo, w.seq.n, w.seq.past, tok0, head0, w.ta, w.tb, w.nst0, vc,
                      (w.wide ? kSegWide : 0) | (w.ta == 0 ? kSegFirst : 0) |
                          (w.ta == 0 && w.tb == w.nt ? kSegWhole : 0)})) {
         ok = false;
@@ -421,7 +422,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       }
       if (!ok) break;
     }
-    if (ok) ok = hand_out({0, 0, 0, 0, 0, 0, 0, 0, kSegEnd});
+    if (ok) ok = hand_out({0, 0, 0, 0, 0, 0, 0, 0, 0, kSegEnd});
     if (lane == 0) {
       if (!cut) m.valid = 0;
       p.meta[blockIdx.x] = m;
@@ -474,78 +475,63 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
           tc::commit(o_done0 + 8 * t);
         }
       };
-      int base = 0, segs = 0;       // K/V tiles and segments before this one
-      int tiles_done[2] = {0, 0};   // products O_t += P_t V issued
-      int scores_done[2] = {0, 0};  // products S_t issued
-      int uses[2] = {0, 0};         // segments in which O_t has been used
+      // Ring positions of the next K tile to score and the next V tile to use, with the parities of their passes; the
+      // parity of the next tile of either group; and the parity of the last release of O_t (none for the first use).
+      int ks = 0, vs = 0, segs = 0;
+      uint32_t kph = 0, vph = 0, tp0 = 0, tp1 = 0, of0 = 1, of1 = 1;
       for (;; ++segs) {
         const int slot = segs % kSegRing;
         if (!ptx::mbar_wait(seg_full0 + 8 * slot, (segs / kSegRing) & 1, abort_flag)) { ok = false; break; }
-        const int flags = seg_s[slot].flags, tiles = seg_s[slot].tb - seg_s[slot].ta, nst0 = seg_s[slot].nst0;
+        const int flags = seg_s[slot].flags, tiles = seg_s[slot].tb - seg_s[slot].ta, n0 = seg_s[slot].nst0;
         ptx::mbar_arrive(seg_empty0 + 8 * slot);
         if (flags & kSegEnd) break;
         const bool wide = flags & kSegWide;
-        const int steps = wide ? tiles : nst0;
-        const int nst[2] = {nst0, wide ? tiles : tiles - nst0};
-        auto tile_of = [&](int i, int t) { return base + (wide ? i : 2 * i + t); };
-        auto scores = [&](int i, int t) -> bool {  // S_t of step i
-          const int idx = tile_of(i, t), s = idx % kKSlots;
-          if (!ptx::mbar_wait(k_full0 + 8 * s, (idx / kKSlots) & 1, abort_flag)) return false;
-          if (kSepP && scores_done[t] > 0 && !ptx::mbar_wait(s_free0 + 8 * t, (scores_done[t] - 1) & 1, abort_flag)) return false;
-          tc::fence_after_sync();
-          issue_s(t, wide ? t : 0, s);
-          ++scores_done[t];
-          if (!wide) tc::commit(k_empty0 + 8 * s);
-          return true;
-        };
-        auto values = [&](int i, int t) -> bool {  // O_t += P_t V of step i
-          const int idx = tile_of(i, t), s = idx % kVSlots;
-          if (i == 0) {  // the accumulator of the segment before has been read out
-            if (uses[t] > 0 && !ptx::mbar_wait(o_free0 + 8 * t, (uses[t] - 1) & 1, abort_flag)) return false;
-            ++uses[t];
-          }
-          if (!ptx::mbar_wait(p_half0 + 8 * t, tiles_done[t] & 1, abort_flag)) return false;
-          if (!ptx::mbar_wait(v_full0 + 8 * s, (idx / kVSlots) & 1, abort_flag)) return false;
-          tc::fence_after_sync();
-          issue_pv(t, s, i == 0, 0);
-          if (!ptx::mbar_wait(p_full0 + 8 * t, tiles_done[t] & 1, abort_flag)) return false;
-          tc::fence_after_sync();
-          issue_pv(t, s, i == 0, 1);
-          ++tiles_done[t];
-          if (!wide) tc::commit(v_empty0 + 8 * s);
-          return true;
-        };
+        const int n1 = wide ? tiles : tiles - n0, steps = wide ? tiles : n0;
         if (!ptx::mbar_wait(q_full, segs & 1, abort_flag)) { ok = false; break; }
+        // step -1 scores the first tiles; step i uses tile i's weights and scores tile i + 1.  Wide: both groups take the
+        // same K and V tile, the rings move on behind the second group; narrow: a tile each, in turn.
+        for (int i = -1; i < steps && ok; ++i) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-          if (ok && nst[t] > 0) ok = scores(0, t);
-        if (ok && wide) tc::commit(k_empty0 + 8 * (base % kKSlots));
-        if (ok && steps == 1) tc::commit(q_empty);
-        for (int i = 0; i < steps && ok; ++i) {
-          if (kSepP) {
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-              if (ok && i + 1 < nst[t]) ok = scores(i + 1, t);
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-              if (ok && i < nst[t]) ok = values(i, t);
-          } else {
-#pragma unroll
-            for (int t = 0; t < 2; ++t) {
-              if (ok && i < nst[t]) ok = values(i, t);
-              // P_t of step i is consumed first (same pipe, in order): S_t may be overwritten
-              if (ok && i + 1 < nst[t]) ok = scores(i + 1, t);
+          for (int t = 0; t < 2; ++t) {
+            const int n = t == 0 ? n0 : n1;
+            const bool last = t == 1 || !wide;  // the ring moves on
+            auto scores = [&](uint32_t tile) __attribute__((always_inline)) {  // parity of the tile whose scores they replace
+              if (i + 1 < n) {
+                if (!ptx::mbar_wait(k_full0 + 8 * ks, kph, abort_flag)) { ok = false; return; }
+                // (kSepP) the last scores have been read; otherwise P_t lies there and has been issued to the same pipe
+                if (kSepP && !ptx::mbar_wait(s_free0 + 8 * t, tile, abort_flag)) { ok = false; return; }
+                tc::fence_after_sync();
+                issue_s(t, wide ? t : 0, ks);
+                if (last) {
+                  tc::commit(k_empty0 + 8 * ks);
+                  if (++ks == kKSlots) { ks = 0; kph ^= 1; }
+                }
+              }
+            };
+            if (kSepP) scores((t == 0 ? tp0 : tp1) ^ (i < 0));
+            if (ok && i >= 0 && i < n) {
+              if (i == 0) {  // the accumulator of the segment before has been read out
+                if (!ptx::mbar_wait(o_free0 + 8 * t, t == 0 ? of0 : of1, abort_flag)) { ok = false; break; }
+                if (t == 0) of0 ^= 1; else of1 ^= 1;
+              }
+              if (!ptx::mbar_wait(p_half0 + 8 * t, t == 0 ? tp0 : tp1, abort_flag) ||
+                  !ptx::mbar_wait(v_full0 + 8 * vs, vph, abort_flag)) { ok = false; break; }
+              tc::fence_after_sync();
+              issue_pv(t, vs, i == 0, 0);
+              if (!ptx::mbar_wait(p_full0 + 8 * t, t == 0 ? tp0 : tp1, abort_flag)) { ok = false; break; }
+              tc::fence_after_sync();
+              issue_pv(t, vs, i == 0, 1);
+              if (t == 0) tp0 ^= 1; else tp1 ^= 1;
+              if (last) {
+                tc::commit(v_empty0 + 8 * vs);
+                if (++vs == kVSlots) { vs = 0; vph ^= 1; }
+              }
             }
+            if (!kSepP && ok) scores(0);
           }
-          if (!ok) break;
-          if (wide) {  // every product that reads V tile i and K tile i + 1 has been issued
-            tc::commit(v_empty0 + 8 * ((base + i) % kVSlots));
-            if (i + 1 < steps) tc::commit(k_empty0 + 8 * ((base + i + 1) % kKSlots));
-          }
-          if (i + 2 == steps) tc::commit(q_empty);
+          if (ok && i + 2 == steps) tc::commit(q_empty);  // the segment's last scores have been issued
         }
         if (!ok) break;
-        base += tiles;
       }
       if (!ok) report(p.dev_status, DIFFQKV_ERR_TIMEOUT);
       tc::commit(drain);
@@ -558,40 +544,42 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     const int t = (warp - kSoftmaxWarp0) >> 2;  // softmax group
     const int quarter = warp & 3;               // tensor-memory lanes this warp may touch
     const int r = quarter * 32 + lane;          // row
-    const uint32_t lane_base = tmem_base + ((uint32_t)(quarter * 32) << 16);
-    const uint32_t s_taddr = lane_base + t * 128;
-    const uint32_t p_taddr = kSepP ? lane_base + 384 + t * 64 : s_taddr;
-    const uint32_t o_taddr = lane_base + 256 + t * kD;
-    int base = 0;      // K/V tiles before this segment
-    int c = 0;         // tiles of this group so far
-    int joins = 0;     // narrow segments in which both groups had tiles
+    // What a row needs next to its 128 scores has to fit 216 registers: one word for this group's barriers, one for its
+    // tensor memory, a parity bit, the tile; the rest is read from the segment's words when it is wanted.
+    const uint32_t gbar = s_full0 + 8 * t;
+    const uint32_t s_taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + t * 128;
+    const uint32_t p_taddr = kSepP ? s_taddr + 384 - t * 64 : s_taddr;
+    const uint32_t o_taddr = s_taddr + 256 - t * (128 - kD);
+    constexpr uint32_t kPHalf = 16, kPFull = 32, kODone = 48, kOFree = 64, kSFree = 80;  // from gbar
+    uint32_t par = 0;  // parity of the next tile's barriers
+    uint32_t joins = 0;  // narrow segments in which both groups had tiles
     bool ok = true;
-    for (int segs = 0;; ++segs) {
-      const int slot = segs % kSegRing;
-      if (!wait_warp(seg_full0 + 8 * slot, (segs / kSegRing) & 1, abort_flag)) { ok = false; break; }
-      const Segment& w = seg_s[slot];  // released at the end of the segment
+    // first token of this group's rows within the chunk, and the rows in use
+    auto tok0_of = [&](const Segment& w) { return w.tok0 + ((w.flags & kSegWide) ? t * p.T : 0); };
+    auto rows_of = [&](const Segment& w) { return min(p.T, w.n - tok0_of(w)) * p.G; };
+    for (uint32_t segs = 0;; ++segs) {
+      const Segment& w = seg_s[segs % kSegRing];  // released at the end of the segment
+      if (!wait_warp(seg_full0 + 8 * (segs % kSegRing), (segs / kSegRing) & 1, abort_flag)) { ok = false; break; }
       if (w.flags & kSegEnd) break;
       const bool wide = w.flags & kSegWide;
-      const int ta = w.ta, tiles = w.tb - ta, nst1 = wide ? tiles : tiles - w.nst0;
-      const int n = t == 0 ? w.nst0 : nst1;
-      const int tok0 = w.tok0 + (wide ? t * p.T : 0);  // first token of this group's rows, within the chunk
-      const int kv_len = w.past + w.n;
-      const int first_pos = w.past + tok0;
-      const int qpos = min(first_pos + r / p.G, kv_len - 1);
-      const int rows = min(p.T, w.n - tok0) * p.G;  // rows in use
-      const bool busy = quarter * 32 < rows;            // some row of this warp is in use
+      const int n = t == 0 ? w.nst0 : (wide ? w.tb - w.ta : w.tb - w.ta - w.nst0);  // tiles of this group
+      const bool busy = quarter * 32 < rows_of(w);                                 // some row of this warp is in use
+      // tiles from here on reach past some row's position (a ragged last tile is one of them)
+      const int j_diag = (w.past + tok0_of(w) + 1) / kKT;
       float m_ref = -INFINITY, l = 0.f;
-      for (int i = 0; i < n; ++i, ++c) {
-        const int j = ta + (wide ? i : 2 * i + t);
-        if (!wait_warp(s_full0 + 8 * t, c & 1, abort_flag)) { ok = false; break; }
+      int j = w.ta + (wide ? 0 : t);
+      const int j_end = j + (wide ? n : 2 * n);
+      bool later = false;  // not the segment's first tile
+#pragma unroll 1
+      for (; j < j_end; j += wide ? 1 : 2, par ^= 1, later = true) {
+        if (!wait_warp(gbar, par, abort_flag)) { ok = false; break; }
         tc::fence_after_sync();
-        const int k0 = j * kKT;
-        if (k0 + kKT > kv_len) {
+        if (j >= j_diag && j * kKT + kKT > w.past + w.n) {
           // ragged last tile: V rows past the sequence end hold whatever followed in memory; zero them before any
           // product reads the tile (0 * NaN would poison it).  Both groups may do this; they write the same zeros.
-          const int idx = base + j - ta, vslot = idx % kVSlots;
+          const int idx = w.v0 + j - w.ta, vslot = idx % kVSlots;
           if (!wait_warp(v_full0 + 8 * vslot, (idx / kVSlots) & 1, abort_flag)) { ok = false; break; }
-          if (r >= kv_len - k0) {
+          if (r >= w.past + w.n - j * kKT) {
 #pragma unroll
             for (int half = 0; half < kHalves; ++half) {
               uint4* dst = reinterpret_cast<uint4*>(v_s + vslot * kTBytes + half * (kKT * 128) + r * 128);
@@ -604,13 +592,13 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         if (!busy) {  // nothing to compute, but the barriers count this warp
           if (kSepP) {
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(s_free0 + 8 * t);
-            if (i > 0 && !wait_warp(o_done0 + 8 * t, (c - 1) & 1, abort_flag)) { ok = false; break; }
+            if (lane == 0) ptx::mbar_arrive(gbar + kSFree);
+            if (later && !wait_warp(gbar + kODone, par ^ 1, abort_flag)) { ok = false; break; }
           }
           __syncwarp();
           if (lane == 0) {
-            ptx::mbar_arrive(p_half0 + 8 * t);
-            ptx::mbar_arrive(p_full0 + 8 * t);
+            ptx::mbar_arrive(gbar + kPHalf);
+            ptx::mbar_arrive(gbar + kPFull);
           }
           continue;
         }
@@ -622,12 +610,13 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         if (kSepP) {  // the score columns may take the next tile's scores from here on
           tc::fence_before_sync();
           __syncwarp();
-          if (lane == 0) ptx::mbar_arrive(s_free0 + 8 * t);
+          if (lane == 0) ptx::mbar_arrive(gbar + kSFree);
         }
-        if (k0 + kKT - 1 > first_pos) {  // the tile reaches past some row's position
+        if (j >= j_diag) {
+          const int sees = min(w.past + tok0_of(w) + r / p.G, w.past + w.n - 1) - j * kKT;  // last column the row sees
 #pragma unroll
           for (int e = 0; e < 128; ++e)
-            if (k0 + e > qpos) s[e] = 0xff800000u;  // -inf
+            if (e > sees) s[e] = 0xff800000u;  // -inf
         }
         float mx0 = -INFINITY, mx1 = -INFINITY, mx2 = -INFINITY, mx3 = -INFINITY;
 #pragma unroll
@@ -644,8 +633,8 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
           alpha = exp2f(m_ref - mx);
           m_ref = mx;
         }
-        if (i > 0 && __any_sync(0xffffffffu, bump)) {  // rescale this warp's rows of O in tensor memory
-          if (!wait_warp(o_done0 + 8 * t, (c - 1) & 1, abort_flag)) { ok = false; break; }
+        if (later && __any_sync(0xffffffffu, bump)) {  // rescale this warp's rows of O in tensor memory
+          if (!wait_warp(gbar + kODone, par ^ 1, abort_flag)) { ok = false; break; }
           tc::fence_after_sync();
 #pragma unroll 1
           for (int x = 0; x < kD / 32; ++x) {
@@ -660,8 +649,8 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         }
         l *= alpha;
         const float neg_m = m_ref == -INFINITY ? 0.f : -m_ref;  // a segment may begin behind a row's position
-        if (kSepP && i > 0) {  // P's own columns still hold the previous tile's P until its product is done
-          if (!wait_warp(o_done0 + 8 * t, (c - 1) & 1, abort_flag)) { ok = false; break; }
+        if (kSepP && later) {  // P's own columns still hold the previous tile's P until its product is done
+          if (!wait_warp(gbar + kODone, par ^ 1, abort_flag)) { ok = false; break; }
           tc::fence_after_sync();
         }
         // ---- P = 2^(S scale - m_ref) as packed bf16; fp32 row sum.  The first 64 tokens are announced on their own,
@@ -684,7 +673,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
             tc::wait_st();
             tc::fence_before_sync();
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(p_half0 + 8 * t);
+            if (lane == 0) ptx::mbar_arrive(gbar + kPHalf);
           }
         }
         float l0, l1;
@@ -693,30 +682,29 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         tc::wait_st();
         tc::fence_before_sync();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(p_full0 + 8 * t);
+        if (lane == 0) ptx::mbar_arrive(gbar + kPFull);
       }
       if (!ok) break;
-      base += tiles;
       // ---- the segment's result
       if (n > 0) {
-        if (!wait_warp(o_done0 + 8 * t, (c - 1) & 1, abort_flag)) { ok = false; break; }
+        if (!wait_warp(gbar + kODone, par ^ 1, abort_flag)) { ok = false; break; }
         tc::fence_after_sync();
       }
       float weight = l > 0.f ? 1.f / l : 0.f, weight1 = 0.f, lse2 = l > 0.f ? m_ref + log2f(l) : -INFINITY;
-      const bool join = !wide && nst1 > 0;
+      const bool join = !wide && w.tb - w.ta > 1;
       if (join && t == 1) {  // hand over to the first group, which reads both accumulators
         xch_s[r] = make_float2(m_ref, l);
         tc::fence_before_sync();
         __syncwarp();
         if (lane == 0) {
           ptx::mbar_arrive(x_full);
-          ptx::mbar_arrive(seg_empty0 + 8 * slot);
+          ptx::mbar_arrive(seg_empty0 + 8 * (segs % kSegRing));
         }
         continue;
       }
       if (!wide && t == 1) {
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(seg_empty0 + 8 * slot);
+        if (lane == 0) ptx::mbar_arrive(seg_empty0 + 8 * (segs % kSegRing));
         continue;
       }
       if (join) {
@@ -732,10 +720,10 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         lse2 = sum > 0.f ? top + log2f(sum) : -INFINITY;
       }
       if (busy) {
-        const bool store = r < rows;
+        const bool store = r < rows_of(w);
         const bool whole = w.flags & kSegWhole;
         const int row_tok = r / p.G;
-        const long long row = (long long)(w.row_lo + tok0 + row_tok) * p.n_q + w.head0 + (r - row_tok * p.G);
+        const long long row = (long long)(w.row_lo + tok0_of(w) + row_tok) * p.n_q + w.head0 + (r - row_tok * p.G);
         const long long prow = (2LL * blockIdx.x + ((w.flags & kSegFirst) ? 1 : 0)) * p.slot_rows + (wide ? t * p.T * p.G : 0) + r;
         const bool as_f32 = !whole || p.out_is_f32;
         float* dst32 = whole ? reinterpret_cast<float*>(p.out) + row * kD : p.part_o + prow * kD;
@@ -780,9 +768,9 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       tc::fence_before_sync();
       __syncwarp();
       if (lane == 0) {
-        if (n > 0) ptx::mbar_arrive(o_free0 + 8 * t);
+        if (n > 0) ptx::mbar_arrive(gbar + kOFree);
         if (join) ptx::mbar_arrive(o_free0 + 8);
-        ptx::mbar_arrive(seg_empty0 + 8 * slot);
+        ptx::mbar_arrive(seg_empty0 + 8 * (segs % kSegRing));
       }
     }
     if (!ok) report(p.dev_status, DIFFQKV_ERR_TIMEOUT);
