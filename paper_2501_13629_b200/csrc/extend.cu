@@ -31,6 +31,7 @@
 
 #include "attn_math.cuh"
 #include "common.cuh"
+#include "extend.cuh"
 #include "ptx.cuh"
 #include "tcgen05.cuh"
 #include "tmap.cuh"
@@ -38,23 +39,11 @@
 namespace diffqkv {
 namespace {
 
-constexpr int kRows = 128;  // matrix rows of a tile
-constexpr int kKT = 128;    // cached tokens of a K/V tile
 constexpr int kExtendThreads = 384;
 constexpr int kSoftmaxWarp0 = 4;
-constexpr int kTmemCols = 512;
-constexpr int kDMax = 128;
-// Shared memory: two Q tiles, rings of K and V tiles of 160 KB together, the exchange of the two softmax groups.
-constexpr int kRingBytes = 5 * kKT * kDMax * 2;
+// Shared memory: two Q tiles, the rings of K and V tiles, the exchange of the two softmax groups, barriers.
 constexpr int kExtendSmem = 1024 + 2 * (kRows * kDMax * 2) + kRingBytes + 1024 + 320;
-constexpr float kRescaleThreshold = 8.f;  // log2 domain
 constexpr int kWideCost = 2, kNarrowCost = 1;  // of a K/V tile, in the division of the work
-constexpr int kMaxBlocks = 256;
-
-struct ExtendMeta {  // an item that is cut, left by the block that has its first tile
-  int valid, row_lo, rows, head0, cost, nt, member;
-  long long lo;  // place of the item in the flat list
-};
 
 // A segment as the producer hands it to the other roles, through a ring in shared memory.
 struct Segment {
@@ -67,28 +56,6 @@ struct Segment {
 };
 constexpr int kSegRing = 4;
 constexpr int kSegEnd = 1, kSegWide = 2, kSegWhole = 4, kSegFirst = 8;  // first: holds the item's first tile
-
-struct ExtendParams {
-  const int* cu_q;
-  const int* seqlens;
-  const int* page_table;
-  int page_size, max_pages_per_seq, num_blocks, max_seqlen;
-  int batch, total_q, n_q;
-  int G, T;            // heads per group, tokens per row tile
-  int n_units, team, n_teams;  // head groups = n_units * team; blocks = n_teams * team
-  int heads_per_k, heads_per_v;
-  int box_tok;         // tokens per TMA box of the cache maps
-  float scale_log2;
-  void* out;
-  int out_is_f32;
-  float* lse;
-  int* dev_status;
-  float* part_o;       // [2 blocks][slot_rows][d_v] normalised partial rows
-  float* part_lse;     // [2 blocks][slot_rows] base-2 log-sum-exp
-  ExtendMeta* meta;    // [blocks]
-  long long* total_cost;
-  int slot_rows;
-};
 
 // sum of floor((a x + b) / m) for x = 0 .. n - 1, all arguments >= 0, m > 0: the Euclid-like recursion on (m, a).
 __device__ long long floor_sum(long long n, long long m, long long a, long long b) {
@@ -107,15 +74,11 @@ __device__ long long floor_sum(long long n, long long m, long long a, long long 
 
 // One sequence of the step.
 struct Seq {
-  int lo, n, past, items;  // first row, rows, tokens cached before, items per head group
+  int lo, n, past, items;  // first row, rows (0: not in this list), tokens cached before, items per head group
   bool bad;                // does not fit
   __device__ void load(const ExtendParams& p, int b) {
-    lo = p.cu_q[b];
-    const int hi = p.cu_q[b + 1];
-    past = p.seqlens[b];
-    n = hi - lo;
-    bad = lo < 0 || n < 0 || hi > p.total_q || past < 0 || (long long)past + n > p.max_seqlen;
-    if (bad) { n = 0; past = 0; }
+    bad = !load_rows(p, b, lo, n, past);
+    if (n <= p.thin_max) n = 0;
     items = (n + 2 * p.T - 1) / (2 * p.T);
   }
   // cost of the first i items, i < items
@@ -228,6 +191,22 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   __shared__ int seek_b_s;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  {  // a step of thin sequences alone (decode): nothing to do here
+    bool any = false;
+    for (int b = tid; b < p.batch; b += kExtendThreads) {
+      Seq s;
+      s.load(p, b);
+      any |= s.n > 0 || s.bad;
+    }
+    if (!__syncthreads_or(any)) {
+      if (tid == 0) {
+        p.list.meta[blockIdx.x].valid = 0;
+        if (blockIdx.x == 0) *p.list.total = 0;
+      }
+      ptx::grid_dependency_wait();
+      return;
+    }
+  }
   if (tid == 0) {
     *abort_flag = 0;
     seek_b_s = p.batch;
@@ -292,8 +271,8 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     if (w < warp) before += scan_s[w + 1];
     total += scan_s[w + 1];
   }
-  const int team = (int)blockIdx.x / p.team, member = (int)blockIdx.x - team * p.team;
-  const long long w0 = total * team / p.n_teams, w1 = total * (team + 1) / p.n_teams;
+  const int team = (int)blockIdx.x / p.list.team, member = (int)blockIdx.x - team * p.list.team;
+  const long long w0 = share_start(total, team, p.list.n_teams), w1 = share_start(total, team + 1, p.list.n_teams);
   {
     long long at = before + incl - mine;
     if (w0 < w1 && at <= w0 && w0 < at + mine)
@@ -309,7 +288,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         at += c;
       }
   }
-  if (blockIdx.x == 0 && tid == 0) *p.total_cost = total;
+  if (blockIdx.x == 0 && tid == 0) *p.list.total = total;
   __syncthreads();
   const uint32_t q_u32 = ptx::smem_u32(q_s), k_u32 = ptx::smem_u32(k_s), v_u32 = ptx::smem_u32(v_s);
 
@@ -340,13 +319,13 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     };
     for (; ok && w.next(p); w.advance(p), ++segs) {
       const int kv_len = w.seq.past + w.seq.n;
-      const int g = w.u * p.team + member;
+      const int g = w.u * p.list.team + member;
       const int head0 = g * p.G;
       const int hk = head0 / p.heads_per_k, hv = head0 / p.heads_per_v;  // Eq. (idx)
       const int tok0 = w.tok0(p);
       if (w.ta == 0 && w.tb < w.nt) {
         cut = true;
-        m.valid = 1; m.row_lo = w.seq.lo + tok0; m.rows = min(w.seq.n - tok0, 2 * p.T) * p.G; m.head0 = head0;
+        m.valid = 1; m.row_lo = w.seq.lo + tok0; m.rows = min(w.seq.n - tok0, 2 * p.T) * p.G; m.part_rows = m.rows; m.head0 = head0;
         m.cost = w.wide ? kWideCost : kNarrowCost; m.nt = w.nt; m.member = member; m.lo = w.item_lo;
       }
       if (!hand_out({w.seq.lo, w.seq.n, w.seq.past, tok0, head0, w.ta, w.tb, w.nst0, vc,
@@ -425,7 +404,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     if (ok) ok = hand_out({0, 0, 0, 0, 0, 0, 0, 0, 0, kSegEnd});
     if (lane == 0) {
       if (!cut) m.valid = 0;
-      p.meta[blockIdx.x] = m;
+      p.list.meta[blockIdx.x] = m;
     }
     ptx::grid_launch_dependents();
     if (!ok) {
@@ -724,9 +703,9 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         const bool whole = w.flags & kSegWhole;
         const int row_tok = r / p.G;
         const long long row = (long long)(w.row_lo + tok0_of(w) + row_tok) * p.n_q + w.head0 + (r - row_tok * p.G);
-        const long long prow = (2LL * blockIdx.x + ((w.flags & kSegFirst) ? 1 : 0)) * p.slot_rows + (wide ? t * p.T * p.G : 0) + r;
+        const long long prow = (2LL * blockIdx.x + ((w.flags & kSegFirst) ? 1 : 0)) * p.list.slot_rows + (wide ? t * p.T * p.G : 0) + r;
         const bool as_f32 = !whole || p.out_is_f32;
-        float* dst32 = whole ? reinterpret_cast<float*>(p.out) + row * kD : p.part_o + prow * kD;
+        float* dst32 = whole ? reinterpret_cast<float*>(p.out) + row * kD : p.list.part_o + prow * kD;
         __nv_bfloat16* dst16 = reinterpret_cast<__nv_bfloat16*>(p.out) + row * kD;
         if (n > 0) {
 #pragma unroll 1
@@ -760,7 +739,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
           }
         }
         if (store) {
-          if (!whole) p.part_lse[prow] = lse2;
+          if (!whole) p.list.part_lse[prow] = lse2;
           else if (p.lse) p.lse[row] = lse2 * kLn2;
         }
       }
@@ -784,75 +763,81 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     tc::fence_after_sync();
     tc::tmem_dealloc(tmem_base, kTmemCols);
   }
+  // The kernel for thin sequences was launched before this one and runs beside it; the joining kernel, which depends on
+  // this one alone, may only follow when both are over.
+  ptx::grid_dependency_wait();
 }
 
-// Joins the partial rows of the items that were cut: block (x, y) takes every gridDim.y-th group of rows of the item
-// that block x of the attention kernel began, a warp per row.
+// Joins the partial rows of the items that were cut: blocks x = 0 .. take the items that the blocks of the first kernel
+// began, then those of the second's; the rows of an item are dealt to gridDim.y blocks, and there to groups of kD / 4
+// lanes with four channels each.
+constexpr int kCombineThreads = 256;
+
 template <int kD>
-__global__ void __launch_bounds__(256) extend_combine_kernel(const ExtendParams p) {
-  ptx::grid_dependency_wait();
-  const ExtendMeta m = p.meta[blockIdx.x];
-  constexpr int kWarps = 8;
-  const int row0 = blockIdx.y * kWarps;
-  if (!m.valid || row0 >= m.rows) return;
+__global__ void __launch_bounds__(kCombineThreads) extend_combine_kernel(const ExtendParams p, const ExtendList thin,
+                                                                       const int thin_blocks) {
+  constexpr int kLanes = kD / 4, kGroups = kCombineThreads / kLanes;
   __shared__ int slots[kMaxBlocks];
   __shared__ int count_s;
-  const long long total = *p.total_cost;
-  const int first = (int)blockIdx.x / p.team;
+  const bool first_list = (int)blockIdx.x < thin_blocks;
+  const ExtendList& list = first_list ? thin : p.list;
+  const int block = first_list ? blockIdx.x : blockIdx.x - thin_blocks;
+  const int first = block / list.team;
   if (threadIdx.x == 0) count_s = 0;
+  ptx::grid_dependency_wait();
+  const ExtendMeta m = list.meta[block];
+  if (!m.valid || (int)blockIdx.y * kGroups >= m.rows) return;
+  const long long total = *list.total;
   __syncthreads();
   // the teams that own tiles of the item, from the first on (in order: sums do not depend on timing)
   const int k = first + threadIdx.x;
-  if (k < p.n_teams) {
-    const long long a = total * k / p.n_teams, z = total * (k + 1) / p.n_teams;
+  if (k < list.n_teams) {
+    const long long a = share_start(total, k, list.n_teams), z = share_start(total, k + 1, list.n_teams);
     int slot = -1;
     if (a < m.lo + (long long)m.cost * m.nt) {
-      const int ta = a <= m.lo ? 0 : (int)((a - m.lo + m.cost - 1) / m.cost);
-      const int tb = (int)min((long long)m.nt, (z - m.lo + m.cost - 1) / m.cost);
-      if (ta < tb) slot = 2 * (k * p.team + m.member) + (ta == 0);
+      const int ta = a <= m.lo ? 0 : (int)(((uint32_t)(a - m.lo) + m.cost - 1) / (uint32_t)m.cost);
+      const int tb = z - m.lo >= (long long)m.cost * m.nt ? m.nt : (int)(((uint32_t)(z - m.lo) + m.cost - 1) / (uint32_t)m.cost);
+      if (ta < tb) slot = 2 * (k * list.team + m.member) + (ta == 0);
       atomicMax(&count_s, k - first + 1);
     }
     slots[threadIdx.x] = slot;
   }
   __syncthreads();
-  const int n = count_s, lane = threadIdx.x & 31;
-  constexpr int kC = kD / 32;  // channels per lane
-  const int r = row0 + (threadIdx.x >> 5);
-  if (r >= m.rows) return;
-  float top = -INFINITY;
-  for (int i = lane; i < n; i += 32)
-    if (slots[i] >= 0) top = fmaxf(top, p.part_lse[(long long)slots[i] * p.slot_rows + r]);
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  float acc[kC], sum = 0.f;
-#pragma unroll
-  for (int e = 0; e < kC; ++e) acc[e] = 0.f;
+  const int n = count_s, lane = threadIdx.x % kLanes;
+  for (int r = blockIdx.y * kGroups + threadIdx.x / kLanes; r < m.rows; r += gridDim.y * kGroups) {
+    float top = -INFINITY;
 #pragma unroll 4
-  for (int i = 0; i < n; ++i) {
-    const int slot = slots[i];
-    if (slot < 0) continue;
-    const long long at = (long long)slot * p.slot_rows + r;
-    const float ls = p.part_lse[at];
-    if (ls == -INFINITY) continue;  // the part saw no token of this row
-    const float f = exp2f(ls - top);
-    sum += f;
-    const float* o = p.part_o + at * kD + lane * kC;
-#pragma unroll
-    for (int e = 0; e < kC; ++e) acc[e] = fmaf(f, o[e], acc[e]);
+    for (int i = 0; i < n; ++i)
+      if (slots[i] >= 0) top = fmaxf(top, list.part_lse[(long long)slots[i] * list.slot_rows + r]);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+      const int slot = slots[i];
+      if (slot < 0) continue;
+      const long long at = (long long)slot * list.slot_rows + r;
+      const float ls = list.part_lse[at];
+      const float4 o = *reinterpret_cast<const float4*>(list.part_o + at * kD + lane * 4);
+      if (ls == -INFINITY) continue;  // the part saw no token of this row (and wrote no values)
+      const float f = exp2f(ls - top);
+      sum += f;
+      acc.x = fmaf(f, o.x, acc.x);
+      acc.y = fmaf(f, o.y, acc.y);
+      acc.z = fmaf(f, o.z, acc.z);
+      acc.w = fmaf(f, o.w, acc.w);
+    }
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    const int g = r / m.part_rows, lr = r - g * m.part_rows, tok = lr / p.G;
+    const long long row = (long long)(m.row_lo + tok) * p.n_q + m.head0 + g * p.G + (lr - tok * p.G);
+    if (p.out_is_f32) {
+      *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + row * kD + lane * 4) =
+          make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    } else {
+      *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(p.out) + row * kD + lane * 4) =
+          make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
+    }
+    if (p.lse && lane == 0) p.lse[row] = sum > 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
   }
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
-  const int tok = r / p.G;
-  const long long row = (long long)(m.row_lo + tok) * p.n_q + m.head0 + (r - tok * p.G);
-  if (p.out_is_f32) {
-    float* dst = reinterpret_cast<float*>(p.out) + row * kD + lane * kC;
-#pragma unroll
-    for (int e = 0; e < kC; ++e) dst[e] = acc[e] * inv;
-  } else {
-    uint32_t* dst = reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(p.out) + row * kD + lane * kC);
-#pragma unroll
-    for (int e = 0; e < kC; e += 2) dst[e / 2] = pack2(acc[e] * inv, acc[e + 1] * inv);
-  }
-  if (p.lse && lane == 0) p.lse[row] = sum > 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
 }
 
 // Tensor map over one cache pool: dims (64 channels, token slot, channel half, head, block); a box brings box_tok tokens
@@ -868,7 +853,10 @@ bool make_cache_map(CUtensorMap* map, const void* base, int d, long long tok_ext
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 struct Plan {
-  int G, T, groups, team, n_teams, slot_rows;
+  int G, T, groups, parts, region, thin_max;
+  int blocks;              // of the thin kernel
+  int n_teams;             // of the other one, parts blocks each
+  int slot_rows, thin_rows;
 };
 
 int sm_count() {
@@ -890,6 +878,7 @@ Plan make_plan(const diffqkv_shape& s, int total_q) {
   Plan pl;
   const int per_k = s.n_q / s.n_k, per_v = s.n_q / s.n_v;
   int G = std::gcd(per_k, per_v);
+  const bool nested = G == per_k || G == per_v;  // one kind of head groups lies within the other
   if (G > kRows) {  // the largest divisor that fits a tile
     int d = kRows;
     while (G % d != 0) --d;
@@ -898,21 +887,43 @@ Plan make_plan(const diffqkv_shape& s, int total_q) {
   pl.G = G;
   pl.T = kRows / G;
   pl.groups = s.n_q / G;
-  // groups of one K head (V head) that differ in the other head only sit next to each other
-  const int share = (per_k > per_v ? per_k : per_v) / G;
-  int team = share < 8 ? share : 8;
-  while (share % team != 0 || pl.groups % team != 0) --team;
-  pl.team = team;
-  pl.n_teams = sm_count() / team;
-  const long long rows = 2LL * pl.T * G, asked = (long long)total_q * G;
+  // groups of one K head (V head) that differ in the other head only sit next to each other: a unit of at most four
+  const int share = nested ? (per_k > per_v ? per_k : per_v) / G : 1;
+  int parts = share < 4 ? share : 4;
+  while (share % parts != 0 || pl.groups % parts != 0) --parts;
+  pl.parts = parts;
+  pl.region = parts == 1 ? kThinCols : (parts == 2 ? kThinCols / 2 : kThinCols / 4);
+  pl.thin_max = pl.region / G;
+  pl.blocks = sm_count();
+  pl.n_teams = pl.blocks / parts;
+  const long long rows = 2LL * pl.T * G, asked = (long long)total_q * G, thin = (long long)pl.thin_max * G;
   pl.slot_rows = (int)(asked < rows ? asked : rows);
+  pl.thin_rows = (int)(asked < thin ? asked : thin) * parts;
   return pl;
 }
 
-size_t plan_bytes(const Plan& pl, int d_v) {
-  const size_t slots = 2 * (size_t)pl.n_teams * pl.team;
-  return 256 + up256(sizeof(ExtendMeta) * kMaxBlocks) + up256(slots * pl.slot_rows * sizeof(float)) +
-         up256(slots * pl.slot_rows * d_v * sizeof(float));
+// Parts of the workspace; with a base their addresses.
+size_t place(const Plan& pl, int d_v, char* base, ExtendList* wide, ExtendList* thin) {
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t was = at;
+    at += up256(bytes);
+    return base ? base + was : nullptr;
+  };
+  const int rows[2] = {pl.slot_rows, pl.thin_rows}, blocks[2] = {pl.n_teams * pl.parts, pl.blocks};
+  ExtendList* lists[2] = {wide, thin};
+  for (int i = 0; i < 2; ++i) {
+    ExtendList l = {};
+    l.total = reinterpret_cast<long long*>(take(8));
+    l.meta = reinterpret_cast<ExtendMeta*>(take(sizeof(ExtendMeta) * kMaxBlocks));
+    l.part_lse = reinterpret_cast<float*>(take(2 * sizeof(float) * (size_t)blocks[i] * rows[i]));
+    l.part_o = reinterpret_cast<float*>(take(2 * sizeof(float) * (size_t)blocks[i] * rows[i] * d_v));
+    l.slot_rows = rows[i];
+    l.team = i == 0 ? pl.parts : 1;
+    l.n_teams = i == 0 ? pl.n_teams : pl.blocks;
+    if (lists[i]) *lists[i] = l;
+  }
+  return at;
 }
 
 bool dims_supported(const diffqkv_shape& s) {
@@ -923,7 +934,7 @@ bool dims_supported(const diffqkv_shape& s) {
 }  // namespace
 
 size_t extend_workspace_bytes(const diffqkv_shape& s, int total_q) {
-  return dims_supported(s) ? plan_bytes(make_plan(s, total_q), s.d_v) : 256;
+  return dims_supported(s) ? place(make_plan(s, total_q), s.d_v, nullptr, nullptr, nullptr) : 256;
 }
 
 // cudaErrorNotSupported, with nothing launched, where the plain kernel has to take the call.
@@ -940,12 +951,14 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
     }
   }
   const Plan pl = make_plan(s, total_q);
-  CUtensorMap mq, mk, mv;
+  CUtensorMap mq, mq_thin, mk, mv;
   {
     const cuuint64_t dims[4] = {64, (cuuint64_t)s.n_q, (cuuint64_t)total_q, (cuuint64_t)(s.d_qk / 64)};
     const cuuint64_t strides[3] = {(cuuint64_t)s.d_qk * 2, (cuuint64_t)s.n_q * s.d_qk * 2, 128};
     const cuuint32_t box[4] = {64, (cuuint32_t)pl.G, (cuuint32_t)pl.T, 1};
+    const cuuint32_t thin[4] = {64, (cuuint32_t)pl.G, (cuuint32_t)pl.thin_max, 1};
     if (!make_tmap_bf16_sw128(&mq, q, 4, dims, strides, box)) return cudaErrorNotSupported;
+    if (pl.thin_max > 0 && !make_tmap_bf16_sw128(&mq_thin, q, 4, dims, strides, thin)) return cudaErrorNotSupported;
   }
   const long long tok_extent = c.page_table ? c.page_size : c.max_seqlen;
   if (!make_cache_map(&mk, c.k_cache, s.d_qk, tok_extent, s.n_k, c.num_blocks, c.k_stride_tok, c.k_stride_head,
@@ -958,41 +971,59 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
   p.cu_q = cu_q; p.seqlens = c.seqlens; p.page_table = c.page_table;
   p.page_size = c.page_size; p.max_pages_per_seq = c.max_pages_per_seq; p.num_blocks = c.num_blocks; p.max_seqlen = c.max_seqlen;
   p.batch = s.batch; p.total_q = total_q; p.n_q = s.n_q;
-  p.G = pl.G; p.T = pl.T; p.team = pl.team; p.n_teams = pl.n_teams; p.n_units = pl.groups / pl.team;
+  p.G = pl.G; p.T = pl.T; p.parts = pl.parts; p.n_units = pl.groups / pl.parts;
+  p.thin_max = pl.thin_max; p.region = pl.region;
   p.heads_per_k = s.n_q / s.n_k; p.heads_per_v = s.n_q / s.n_v;
+  p.k_parts = p.heads_per_k < p.heads_per_v ? pl.parts : 1;
+  p.v_parts = p.heads_per_v < p.heads_per_k ? pl.parts : 1;
+  {  // 160 KB of tiles: K of two token tiles where there is room, the rest V; an even number where V tiles go in pairs
+    const int slots = kRingBytes / (kKT * 2 * (s.d_qk > s.d_v ? s.d_qk : s.d_v));
+    p.k_ring = 2 * p.k_parts < slots - p.v_parts ? 2 * p.k_parts : slots - p.v_parts;
+    p.v_ring = slots - p.k_ring;
+    if (s.d_v == 64 && p.v_parts % 2 == 0) p.v_ring &= ~1;
+  }
   p.box_tok = box_tok;
   p.scale_log2 = s.scale * kLog2e;
   p.out = out; p.out_is_f32 = s.out_dtype == DIFFQKV_F32; p.lse = lse; p.dev_status = dev_status;
-  p.slot_rows = pl.slot_rows;
-  const int blocks = pl.n_teams * pl.team;
-  char* at = static_cast<char*>(workspace);
-  p.total_cost = reinterpret_cast<long long*>(at);
-  at += 256;
-  p.meta = reinterpret_cast<ExtendMeta*>(at);
-  at += up256(sizeof(ExtendMeta) * kMaxBlocks);
-  p.part_lse = reinterpret_cast<float*>(at);
-  at += up256(2 * (size_t)blocks * pl.slot_rows * sizeof(float));
-  p.part_o = reinterpret_cast<float*>(at);
+  ExtendList wide, thin;
+  place(pl, s.d_v, static_cast<char*>(workspace), &wide, &thin);
+  const int thin_blocks = pl.thin_max > 0 ? pl.blocks : 0, blocks = pl.n_teams * pl.parts;
 
+  // Which sequences are thin is known on the device alone, so both kernels are launched; the second may start as soon as
+  // the first has, and takes the SMs that the first leaves (an SM has room for one block of either).
+  cudaError_t err;
+  if (thin_blocks > 0) {
+    p.list = thin;
+    err = launch_extend_thin(mq_thin, mk, mv, p, s.d_qk, s.d_v, thin_blocks, stream);
+    if (err != cudaSuccess) return err;
+  }
+  p.list = wide;
   using ExtendFn = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const ExtendParams);
   const ExtendFn fn = s.d_v == 64 ? extend_attn_kernel<64, 64>
                                   : (s.d_qk == 128 ? extend_attn_kernel<128, 128> : extend_attn_kernel<64, 128>);
-  cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kExtendSmem);
-  if (err != cudaSuccess) return err;
-  fn<<<blocks, kExtendThreads, kExtendSmem, stream>>>(mq, mk, mv, p);
-  count_launch();
-  err = cudaGetLastError();
+  err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kExtendSmem);
   if (err != cudaSuccess) return err;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)blocks, (unsigned)((pl.slot_rows + 7) / 8));
-  cfg.blockDim = dim3(256);
   cfg.stream = stream;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3(kExtendThreads);
+  cfg.dynamicSmemBytes = kExtendSmem;
+  cfg.numAttrs = thin_blocks > 0 ? 1 : 0;
+  err = cudaLaunchKernelEx(&cfg, fn, mq, mk, mv, p);
+  if (err != cudaSuccess) return err;
+  count_launch();
+  const int rows = pl.slot_rows > pl.thin_rows ? pl.slot_rows : pl.thin_rows;
+  const int per = kCombineThreads / (s.d_v / 4) * 2;  // rows of a block: two per group of lanes
+  cfg.gridDim = dim3((unsigned)(thin_blocks + blocks), (unsigned)((rows + per - 1) / per));
+  cfg.blockDim = dim3(kCombineThreads);
+  cfg.dynamicSmemBytes = 0;
   cfg.numAttrs = 1;
-  err = cudaLaunchKernelEx(&cfg, s.d_v == 64 ? extend_combine_kernel<64> : extend_combine_kernel<128>, p);
+  err = cudaLaunchKernelEx(&cfg, s.d_v == 64 ? extend_combine_kernel<64> : extend_combine_kernel<128>,
+                           p, thin, thin_blocks);
   if (err != cudaSuccess) return err;
   count_launch();
   return cudaGetLastError();

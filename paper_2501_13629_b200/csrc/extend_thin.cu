@@ -1,0 +1,674 @@
+// Chunk attention for sequences with a few new rows (decode, verification of guessed tokens): the thin half of
+// diffqkv_extend; extend.cu has the mathematics and takes the longer chunks.
+//
+// A row tile of 128 matrix rows is nearly empty here, and the softmax of a nearly empty tile still takes 128 scores per
+// row and thread.  So the products are transposed: the 128 cached tokens of a tile are the matrix rows,
+//     S^T[token][column] = K q^T          (128 x N x d_qk)      column = (head group, row of the chunk, head of the group)
+//     O^T[channel][column] += V^T P^T     (d_v x N x 128)
+// with N <= 64 columns for all the query heads that share a K head (or a V head), so that K and V pass through an SM
+// once for all of them, and the work of the softmax is proportional to the columns in use: one thread per token, N
+// exponentials each, row sums kept per thread until the end of the segment.  P^T goes to the tensor core through shared
+// memory (its B operand), 128 bytes per token, channels of V straight from their token-major tile (M-major A operand).
+//
+// The reference maximum of a column has to be one for all four warps of a softmax group (their tokens meet in one
+// accumulator): each tile's scores are compared with it, the four warps agree through one barrier whether some score
+// exceeds it by 2^8, and only then (and on a segment's first tile) the maxima are taken, lanes by shuffles that halve the
+// columns in every step, warps through shared memory.
+//
+// Work: one flat list of (sequence, unit of heads, 128-token tile), divided evenly over one persistent block per SM, whose
+// two softmax groups take alternate tiles and are joined at the end of a segment; cut items leave partial rows as in
+// extend.cu.  Bound by memory: a tile of a unit with one K and two V heads of 128 channels is 96 KB, 2.2 us at an SM's
+// share of the bandwidth; its products take about 0.6 us and its softmax less.
+// Warp 0 TMA producer, one thread of warp 1 issues the products, warps 2-9 and 10-17 the softmax groups.  Every wait is
+// bounded.
+#include "attn_math.cuh"
+#include "extend.cuh"
+#include "ptx.cuh"
+#include "tcgen05.cuh"
+
+namespace diffqkv {
+namespace {
+
+constexpr int kSoftmaxWarp0 = 2, kGroupWarps = 8;
+constexpr int kHalfCols = kThinCols / 2;
+constexpr int kQRegion = 4 * 16384;  // two Q buffers and two P^T buffers of 16 KB
+
+struct ThinSegment {
+  int row_lo, n, past, head0;  // the sequence: first row, rows, tokens cached before; first head of the unit
+  int ta, tb;                  // tiles
+  int v0;                      // V tiles requested before the segment (the ring's position)
+  int flags;
+};
+constexpr int kSegRing = 2;
+constexpr int kSegEnd = 1, kSegWhole = 2, kSegFirst = 4;
+
+struct Scratch {
+  float m[2][kThinCols];        // reference maximum of every column, per softmax group; weights at a segment's end
+  float part[2][4][kThinCols];  // per warp: maxima, or sums at a segment's end
+  uint64_t bars[42];
+  ThinSegment seg[kSegRing];
+  long long seek_lo;
+  int seek_b;
+  uint32_t tmem;
+  int abort;
+};
+constexpr int kThinSmem = kQRegion + kRingBytes + (int)sizeof(Scratch);
+static_assert(kThinSmem <= 232448, "shared memory of a block");
+
+// The four warps of a (softmax group, half of the columns): does the condition hold anywhere; and a plain barrier.
+__device__ __forceinline__ bool group_any(int id, bool x) {
+  uint32_t y;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+      "barrier.cta.red.or.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+      : "=r"(y)
+      : "r"((uint32_t)x), "r"(id)
+      : "memory");
+  return y != 0;
+}
+__device__ __forceinline__ void group_sync(int id) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(id) : "memory"); }
+
+template <int kDQK, int kD>
+__global__ void __launch_bounds__(kExtendThinThreads, 1)
+extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
+                   const __grid_constant__ CUtensorMap tmap_v, const ExtendParams p) {
+  constexpr int kHalvesK = kDQK / 64, kHalves = kD / 64;
+  constexpr int kHalvesMax = kHalvesK > kHalves ? kHalvesK : kHalves;
+  constexpr int kKBytes = kKT * kDQK * 2, kVBytes = kKT * kD * 2;
+  constexpr int kSlotBytes = kKBytes > kVBytes ? kKBytes : kVBytes;
+  constexpr int kSlots = kRingBytes / kSlotBytes;  // 5 tiles of 32 KB or 10 of 16 KB: a ring of K, then one of V
+  extern __shared__ __align__(1024) unsigned char smem[];
+  unsigned char* q_s = smem;                     // [buffer][half][64 columns][128 B]
+  unsigned char* p_s = smem + 2 * 16384;         // [group][128 tokens][128 B]
+  unsigned char* ring_s = smem + kQRegion;
+  Scratch& sc = *reinterpret_cast<Scratch*>(smem + kQRegion + kRingBytes);
+  const uint32_t bar0 = ptx::smem_u32(sc.bars);
+  const uint32_t full0 = bar0, empty0 = full0 + 8 * kSlots;
+  const uint32_t q_full0 = empty0 + 8 * kSlots, q_empty0 = q_full0 + 16;
+  const uint32_t s_full0 = q_empty0 + 16, p_full0 = s_full0 + 16, o_done0 = p_full0 + 16, o_free0 = o_done0 + 16;
+  const uint32_t x_full = o_free0 + 16, x_empty = x_full + 8, drain = x_empty + 8;
+  const uint32_t seg_full0 = drain + 8, seg_empty0 = seg_full0 + 8 * kSegRing;
+  static_assert(2 * kSlots + 4 + 8 + 3 + 2 * kSegRing <= 42, "barriers");
+  volatile int* abort_flag = &sc.abort;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if ((ptx::smem_u32(smem) & 1023u) != 0) {  // swizzled tiles start on multiples of 1024 bytes
+    if (tid == 0) report(p.dev_status, DIFFQKV_ERR_ALIGNMENT);
+    return;
+  }
+  ptx::grid_launch_dependents();  // the kernel for longer chunks works on other rows: it may take SMs as they fall free
+  if (tid == 0) {
+    sc.abort = 0;
+    sc.seek_b = p.batch;
+    sc.seek_lo = 0;
+    for (int s = 0; s < kSlots; ++s) {
+      ptx::mbar_init(full0 + 8 * s, 1);
+      ptx::mbar_init(empty0 + 8 * s, 1);
+    }
+    for (int t = 0; t < 2; ++t) {
+      ptx::mbar_init(q_full0 + 8 * t, 1);
+      ptx::mbar_init(q_empty0 + 8 * t, 1);
+      ptx::mbar_init(s_full0 + 8 * t, 1);
+      ptx::mbar_init(p_full0 + 8 * t, kGroupWarps);
+      ptx::mbar_init(o_done0 + 8 * t, 1);
+      ptx::mbar_init(o_free0 + 8 * t, kGroupWarps);
+    }
+    ptx::mbar_init(x_full, kGroupWarps);
+    ptx::mbar_init(x_empty, kGroupWarps);
+    ptx::mbar_init(drain, 1);
+    for (int s = 0; s < kSegRing; ++s) {
+      ptx::mbar_init(seg_full0 + 8 * s, 1);
+      ptx::mbar_init(seg_empty0 + 8 * s, 1 + 2 * kGroupWarps);
+    }
+    ptx::fence_barrier_init();
+    ptx::prefetch_tmap(&tmap_q);
+    ptx::prefetch_tmap(&tmap_k);
+    ptx::prefetch_tmap(&tmap_v);
+  }
+  if (warp == 1) {
+    tc::tmem_alloc(ptx::smem_u32(&sc.tmem), kTmemCols);
+    tc::tmem_relinquish();
+  }
+  // ---- this block's range of the flat list of tiles
+  auto load = [&](int b, int& lo, int& n, int& past) -> int {  // tiles of one unit of sequence b
+    load_rows(p, b, lo, n, past);
+    return n > 0 && n <= p.thin_max ? (past + n + kKT - 1) / kKT : 0;
+  };
+  long long* scan = reinterpret_cast<long long*>(&sc.part[0][0][0]);
+  const int per_thread = (p.batch + kExtendThinThreads - 1) / kExtendThinThreads;
+  const int b_lo = min(tid * per_thread, p.batch), b_hi = min(b_lo + per_thread, p.batch);
+  long long mine = 0;
+  for (int b = b_lo; b < b_hi; ++b) {
+    int lo, n, past;
+    mine += (long long)p.n_units * load(b, lo, n, past);
+  }
+  long long incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += y;
+  }
+  if (lane == 31) scan[warp] = incl;
+  tc::fence_before_sync();
+  __syncthreads();
+  tc::fence_after_sync();
+  const uint32_t tmem = sc.tmem;
+  long long before = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kExtendThinThreads / 32; ++w) {
+    if (w < warp) before += scan[w];
+    total += scan[w];
+  }
+  const long long w0 = share_start(total, blockIdx.x, gridDim.x), w1 = share_start(total, blockIdx.x + 1, gridDim.x);
+  {
+    long long at = before + incl - mine;
+    if (w0 < w1 && at <= w0 && w0 < at + mine)
+      for (int b = b_lo; b < b_hi; ++b) {
+        int lo, n, past;
+        const long long c = (long long)p.n_units * load(b, lo, n, past);
+        if (w0 < at + c) {
+          sc.seek_b = b;
+          sc.seek_lo = at;
+          break;
+        }
+        at += c;
+      }
+  }
+  if (blockIdx.x == 0 && tid == 0) *p.list.total = total;
+  __syncthreads();
+
+  if (warp == 0) {
+    // ------------------------------------------------------------------ TMA producer
+    const int boxes_part = kKT / p.box_tok;
+    const int my_part = lane / kHalvesMax, my_half = lane % kHalvesMax;
+    const bool has_box = lane < kHalvesMax * boxes_part;
+    const uint32_t my_off = my_half * (kKT * 128) + my_part * (p.box_tok * 128);
+    const uint32_t ring = ptx::smem_u32(ring_s), q_u32 = ptx::smem_u32(q_s);
+    int ks = 0, vs = 0, k_count = 0, v_count = 0, segs = 0;  // ring places and tiles requested so far
+    uint32_t kph = 0, vph = 0;
+    bool ok = true, cut = false;
+    ExtendMeta m = {};
+    auto hand_out = [&](const ThinSegment& d) -> bool {
+      const int s = segs % kSegRing;
+      if (!wait_warp(seg_empty0 + 8 * s, ((segs / kSegRing) & 1) ^ 1, abort_flag)) return false;
+      if (lane == 0) {
+        sc.seg[s] = d;
+        ptx::mbar_arrive(seg_full0 + 8 * s);
+      }
+      __syncwarp();
+      return true;
+    };
+    int b = sc.seek_b, lo = 0, n = 0, past = 0, nt = 0, u = 0;
+    long long item_lo = sc.seek_lo;
+    if (w0 < w1) {
+      nt = load(b, lo, n, past);
+      const long long in = w0 - item_lo;
+      u = in < (1ll << 31) ? (int)((uint32_t)in / (uint32_t)nt) : (int)(in / nt);
+      item_lo += (long long)u * nt;
+    } else {
+      b = p.batch;
+    }
+    while (ok && b < p.batch && item_lo < w1) {
+      const int ta = w0 > item_lo ? (int)(w0 - item_lo) : 0;
+      const int tb = w1 - item_lo < nt ? (int)(w1 - item_lo) : nt;
+      const int kv_len = past + n;
+      const int head0 = u * p.parts * p.G;
+      const int hk0 = head0 / p.heads_per_k, hv0 = head0 / p.heads_per_v;  // Eq. (idx)
+      if (ta == 0 && tb < nt) {
+        cut = true;
+        m.valid = 1; m.row_lo = lo; m.rows = p.parts * n * p.G; m.part_rows = n * p.G; m.head0 = head0;
+        m.cost = 1; m.nt = nt; m.member = 0; m.lo = item_lo;
+      }
+      if (!hand_out({lo, n, past, head0, ta, tb, v_count, (ta == 0 ? kSegFirst : 0) | (ta == 0 && tb == nt ? kSegWhole : 0)})) {
+        ok = false;
+        break;
+      }
+      auto fetch = [&](int tile) -> int {  // page of this lane's box (fetched two tiles ahead)
+        if (!p.page_table) return b;
+        const int tok = tile * kKT + my_part * p.box_tok;
+        if (tile >= tb || !has_box || tok >= kv_len) return 0;
+        return p.page_table[(long long)b * p.max_pages_per_seq + tok / p.page_size];
+      };
+      // the tiles of the K heads (is_k) or of the V heads of token tile `tile`, whose page is `page`
+      auto request = [&](bool is_k, int tile, int page) {
+        const int tok = tile * kKT;
+        const int parts_valid = min(boxes_part, (kv_len - tok + p.box_tok - 1) / p.box_tok);
+        const int halves = is_k ? kHalvesK : kHalves, count = is_k ? p.k_parts : p.v_parts, head = is_k ? hk0 : hv0;
+        const bool here = has_box && my_part < parts_valid && my_half < halves;
+        if (here && (page < 0 || page >= p.num_blocks)) {  // never read outside the pool: flag it, read block 0 instead
+          report(p.dev_status, DIFFQKV_ERR_INDEX);
+          page = 0;
+        }
+        const int first = tok + my_part * p.box_tok;
+        const int slot_tok = p.page_table ? first % p.page_size : first;
+        for (int x = 0; x < count; ++x) {
+          const int slot = is_k ? ks : p.k_ring + vs;
+          if (!wait_warp(empty0 + 8 * slot, (is_k ? kph : vph) ^ 1, abort_flag)) { ok = false; return; }
+          const uint32_t bar = full0 + 8 * slot;
+          if (lane == 0) ptx::mbar_arrive_expect_tx(bar, (uint32_t)(parts_valid * p.box_tok * halves) * 128u);
+          __syncwarp();
+          if (here) ptx::tma_load_5d(ring + slot * kSlotBytes + my_off, is_k ? &tmap_k : &tmap_v, bar, 0, slot_tok, my_half, head + x, page);
+          if (is_k) {
+            ++k_count;
+            if (++ks == p.k_ring) { ks = 0; kph ^= 1; }
+          } else {
+            ++v_count;
+            if (++vs == p.v_ring) { vs = 0; vph ^= 1; }
+          }
+        }
+      };
+      // K runs a tile ahead of V: a V tile waits for the softmax of its scores anyway, and what waits holds a place
+      int page0 = fetch(ta), page1 = fetch(ta + 1);
+      request(true, ta, page0);
+      if (!ok) break;
+      // the segment's Q: rows of every head group behind one another, thin_max tokens each
+      const int qb = segs & 1;
+      if (!wait_warp(q_empty0 + 8 * qb, ((segs >> 1) & 1) ^ 1, abort_flag)) { ok = false; break; }
+      if (lane == 0) {
+        ptx::mbar_arrive_expect_tx(q_full0 + 8 * qb, (uint32_t)(p.parts * kHalvesK * p.G * p.thin_max) * 128u);
+        for (int g = 0; g < p.parts; ++g)
+#pragma unroll
+          for (int h = 0; h < kHalvesK; ++h)
+            ptx::tma_load_4d(q_u32 + qb * 16384 + h * (kThinCols * 128) + g * p.region * 128, &tmap_q, q_full0 + 8 * qb, 0,
+                             head0 + g * p.G, lo, h);
+      }
+      __syncwarp();
+      for (int tile = ta; tile < tb && ok; ++tile) {
+        const int page2 = fetch(tile + 2);
+        if (tile + 1 < tb) request(true, tile + 1, page1);
+        if (ok) request(false, tile, page0);
+        page0 = page1;
+        page1 = page2;
+      }
+      if (!ok) break;
+      ++segs;
+      item_lo += nt;
+      if (++u == p.n_units) {
+        u = 0;
+        do {
+          if (++b >= p.batch) break;
+          nt = load(b, lo, n, past);
+        } while (nt == 0);
+      }
+    }
+    if (ok) ok = hand_out({0, 0, 0, 0, 0, 0, 0, kSegEnd});
+    if (lane == 0) {
+      if (!cut) m.valid = 0;
+      p.list.meta[blockIdx.x] = m;
+    }
+    if (!ok) {
+      report(p.dev_status, DIFFQKV_ERR_TIMEOUT);
+      // give copies in flight a bounded chance to land before the block's shared memory is released
+      for (int s = 0; s < min(k_count, p.k_ring); ++s)
+        ptx::mbar_wait(full0 + 8 * s, (uint32_t)((k_count - s + p.k_ring - 1) / p.k_ring - 1) & 1u, nullptr);
+      for (int s = 0; s < min(v_count, p.v_ring); ++s)
+        ptx::mbar_wait(full0 + 8 * (p.k_ring + s), (uint32_t)((v_count - s + p.v_ring - 1) / p.v_ring - 1) & 1u, nullptr);
+      for (int s = max(0, segs - 1); s <= segs; ++s) ptx::mbar_wait(q_full0 + 8 * (s & 1), (uint32_t)(s >> 1) & 1u, nullptr);
+    }
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ MMA issuer (one thread)
+    constexpr uint32_t hi = tc::smem_desc_hi_sw128(1024);
+    if (lane == 0) {
+      const uint32_t q_lo = tc::smem_desc_lo(ptx::smem_u32(q_s), 16), r_lo = tc::smem_desc_lo(ptx::smem_u32(ring_s), 16);
+      // V^T: the two 64-channel chunks of M are half a tile apart.  With 64 channels they are the tiles of two V heads,
+      // neighbours in the ring of V (whose length is even then, so that a pair never wraps), or the same
+      // tile twice: lanes 0 .. 63 of the accumulator belong to even heads, 64 .. 127 to odd ones or to nobody.  A
+      // product of 128 x N x 16 takes about 100 cycles whatever N is (its A operand comes from shared memory).
+      const int v_step = kHalves == 1 && p.v_parts % 2 == 0 ? 2 : 1;
+      const uint32_t v_lo = tc::smem_desc_lo(ptx::smem_u32(ring_s), kHalves == 2 || v_step == 2 ? kKT * 128 : 0);
+      const uint32_t p_lo = tc::smem_desc_lo(ptx::smem_u32(p_s), 16);
+      bool ok = true;
+      int ks = 0, vs = 0, segs = 0;  // ring slots of the next K tile to score and the next V tile to use
+      uint32_t kph = 0, vph = 0, tp0 = 0, tp1 = 0, of0 = 1, of1 = 1;
+      auto step = [](int& s, uint32_t& ph, int by, int ring) { s += by; if (s >= ring) { s -= ring; ph ^= 1; } };
+      for (;; ++segs) {
+        const int sl = segs % kSegRing;
+        if (!ptx::mbar_wait(seg_full0 + 8 * sl, (segs / kSegRing) & 1, abort_flag)) { ok = false; break; }
+        const int flags = sc.seg[sl].flags, tiles = sc.seg[sl].tb - sc.seg[sl].ta, n = sc.seg[sl].n;
+        ptx::mbar_arrive(seg_empty0 + 8 * sl);
+        if (flags & kSegEnd) break;
+        const int qb = segs & 1;
+        const uint32_t cols = (uint32_t)((n * p.G + 15) & ~15);        // of a head group
+        const uint32_t all = (uint32_t)((p.parts - 1) * p.region) + cols;
+        // S^T: K and Q both K-major; O^T: V is M-major, P^T N-major
+        const uint32_t id_s = tc::idesc_bf16_f32(kKT, 0, 0, 0) | ((p.k_parts > 1 ? cols : all) >> 3 << 17);
+        const uint32_t id_o = tc::idesc_bf16_f32(128, 0, 1, 1) |
+                              ((p.v_parts == 1 ? all : v_step == 2 ? p.region + cols : cols) >> 3 << 17);
+        if (!ptx::mbar_wait(q_full0 + 8 * qb, (segs >> 1) & 1, abort_flag)) { ok = false; break; }
+        // step i: the scores of tile i + 1, then the product with tile i's weights; tile i belongs to group i & 1
+        for (int i = -1; i < tiles && ok; ++i) {
+          if (i + 1 < tiles) {
+            const uint32_t d = tmem + ((i + 1) & 1) * 128;  // free: the group's last weights have been announced
+            for (int x = 0; x < p.k_parts; ++x) {
+              if (!ptx::mbar_wait(full0 + 8 * ks, kph, abort_flag)) { ok = false; break; }
+              tc::fence_after_sync();
+              const uint32_t ka = r_lo + ks * (kSlotBytes >> 4);
+              const uint32_t qa = q_lo + ((qb * 16384 + x * p.region * 128) >> 4);
+              tc::mma_ss_halves<false>(d + x * p.region, ka, hi, qa, hi, id_s);
+#pragma unroll
+              for (int k = 1; k < kDQK / 16; ++k)
+                tc::mma_ss_halves<true>(d + x * p.region, ka + (((k / 4) * (kKT * 128) + (k % 4) * 32) >> 4), hi,
+                                        qa + (((k / 4) * (kThinCols * 128) + (k % 4) * 32) >> 4), hi, id_s);
+              tc::commit(empty0 + 8 * ks);
+              step(ks, kph, 1, p.k_ring);
+            }
+            if (!ok) break;
+            tc::commit(s_full0 + 8 * ((i + 1) & 1));
+            if (i + 2 == tiles) tc::commit(q_empty0 + 8 * qb);
+          }
+          if (i < 0) continue;
+          const int t = i & 1;
+          if (i < 2) {  // the accumulator of the segment before has been read out
+            if (!ptx::mbar_wait(o_free0 + 8 * t, t == 0 ? of0 : of1, abort_flag)) { ok = false; break; }
+            if (t == 0) of0 ^= 1; else of1 ^= 1;
+          }
+          if (!ptx::mbar_wait(p_full0 + 8 * t, t == 0 ? tp0 : tp1, abort_flag)) { ok = false; break; }
+          if (t == 0) tp0 ^= 1; else tp1 ^= 1;
+          const uint32_t d = tmem + 256 + t * kThinCols;
+          for (int x = 0; x < p.v_parts; x += v_step) {
+            for (int y = 0; y < v_step && ok; ++y) ok = ptx::mbar_wait(full0 + 8 * (p.k_ring + vs + y), vph, abort_flag);
+            if (!ok) break;
+            tc::fence_after_sync();
+            const uint32_t va = v_lo + (p.k_ring + vs) * (kSlotBytes >> 4);
+            const uint32_t pa = p_lo + ((t * 16384 + x * p.region * 2) >> 4);
+#pragma unroll
+            for (int k = 0; k < kKT / 16; ++k) {  // 16 tokens: 2048 bytes of V and of P^T
+              if (k == 0 && i < 2) tc::mma_ss_halves<false>(d + x * p.region, va, hi, pa, hi, id_o);
+              else tc::mma_ss_halves<true>(d + x * p.region, va + ((k * 2048) >> 4), hi, pa + ((k * 2048) >> 4), hi, id_o);
+            }
+            for (int y = 0; y < v_step; ++y) tc::commit(empty0 + 8 * (p.k_ring + vs + y));
+            step(vs, vph, v_step, p.v_ring);
+          }
+          if (!ok) break;
+          tc::commit(o_done0 + 8 * t);
+        }
+        if (!ok) break;
+      }
+      if (!ok) report(p.dev_status, DIFFQKV_ERR_TIMEOUT);
+      tc::commit(drain);
+    }
+    __syncwarp();
+  } else {
+    // ------------------------------------------------------------------ softmax groups
+    // Eight warps each: four for the token quarters of a tile, twice, for the lower and the upper 32 columns.  The four
+    // warps of a (group, half) decide together, so they meet at a hardware barrier; they leave together as well (a warp
+    // whose wait ran out says so at the next barrier), so none is left waiting there.
+    const int t = (warp - kSoftmaxWarp0) >> 3;
+    const int half = ((warp - kSoftmaxWarp0) >> 2) & 1;
+    const int quarter = warp & 3;          // tensor-memory lanes this warp may touch
+    const int wq = (warp - kSoftmaxWarp0) & 3;
+    const int r = quarter * 32 + lane;     // token of a tile; channel of the accumulator
+    const int c0 = half * kHalfCols;       // first column of this warp
+    const int bar_id = 1 + t * 2 + half;
+    const uint32_t s_taddr = tmem + ((uint32_t)(quarter * 32) << 16) + t * 128 + c0;
+    const uint32_t o_taddr = tmem + ((uint32_t)(quarter * 32) << 16) + 256 + c0;
+    unsigned char* p_row = p_s + t * 16384 + r * 128;
+    float* m = sc.m[t] + c0;
+    uint32_t par = 0, xpar = 0;
+    int other = 0;  // tiles of the other group in earlier segments
+    bool ok = true;
+    for (uint32_t segs = 0;; ++segs) {
+      const ThinSegment& w = sc.seg[segs % kSegRing];
+      ok = wait_warp(seg_full0 + 8 * (segs % kSegRing), (segs / kSegRing) & 1, abort_flag);
+      // Group 1 hands its sums and maxima over at a segment's end: it may write there again once they have been read.
+      if (ok && t == 1 && !(w.flags & kSegEnd) && w.tb - w.ta > 1) ok = wait_warp(x_empty, xpar ^ 1, abort_flag);
+      if (group_any(bar_id, !ok)) { ok = false; break; }
+      if (w.flags & kSegEnd) break;
+      const int tiles = w.tb - w.ta;
+      const int used = w.n * p.G;  // columns of a head group in use
+      uint32_t mask = 0;           // groups of eight columns of this half that hold some
+#pragma unroll
+      for (int q = 0; q < kHalfCols / 8; ++q)
+        if ((c0 + q * 8) / p.region < p.parts && ((c0 + q * 8) & (p.region - 1)) < used) mask |= 1u << q;
+      float l[kHalfCols];
+#pragma unroll
+      for (int c = 0; c < kHalfCols; ++c) l[c] = 0.f;
+      bool later = false;  // not the segment's first tile of this group
+#pragma unroll 1
+      for (int i = t; i < tiles; i += 2, par ^= 1, later = true) {
+        ok = wait_warp(s_full0 + 8 * t, par, abort_flag) && ok;
+        tc::fence_after_sync();
+        float x[kHalfCols];
+#pragma unroll
+        for (int q = 0; q < kHalfCols / 8; ++q)
+          if (mask >> q & 1) tc::ld_32x32b_x8(s_taddr + q * 8, *reinterpret_cast<uint32_t(*)[8]>(&x[q * 8]));
+        tc::wait_ld();
+        const int k0 = (w.ta + i) * kKT;
+        if (k0 + kKT > w.past + 1) {  // the tile reaches past some row's position
+          const bool ragged = k0 + kKT > w.past + w.n;
+          // (ragged) The tile before, the other group's, may still wait for its V, in the place that this one's V will
+          // have: until its product is done a wait for this V could take the phase before for its own.
+          if (ragged && i > 0) ok = wait_warp(o_done0 + 8 * (1 - t), (other + ((i - 1) >> 1)) & 1, abort_flag) && ok;
+          if (ragged && half == 0 && r >= w.past + w.n - k0) {
+            // V rows past the sequence end hold whatever followed in memory: zero them (0 * NaN would poison the product)
+            for (int y = 0; y < p.v_parts; ++y) {
+              const int at = w.v0 + i * p.v_parts + y, slot = p.k_ring + at % p.v_ring;
+              ok = ok && ptx::mbar_wait(full0 + 8 * slot, (at / p.v_ring) & 1, abort_flag);
+#pragma unroll
+              for (int h = 0; h < kHalves; ++h) {
+                uint4* dst = reinterpret_cast<uint4*>(ring_s + slot * kSlotBytes + h * (kKT * 128) + r * 128);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) dst[e] = make_uint4(0, 0, 0, 0);
+              }
+            }
+          }
+          __syncwarp();
+          const int hidden = (k0 + r - w.past) * p.G;  // columns of a group below this belong to rows before the token
+#pragma unroll
+          for (int c = 0; c < kHalfCols; ++c)
+            if (((c0 + c) & (p.region - 1)) < hidden) x[c] = -INFINITY;
+        }
+        // ---- scores on the scale of base 2, from the reference; does some score exceed it by 2^8?
+        bool over = !ok || !later;
+        if (later) {
+#pragma unroll
+          for (int q = 0; q < kHalfCols / 8; ++q)
+            if (mask >> q & 1) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const int c = q * 8 + e;
+                x[c] = fmaf(x[c], p.scale_log2, -m[c]);
+                over |= x[c] > kRescaleThreshold && ((c0 + c) & (p.region - 1)) < used;
+              }
+            }
+        } else {
+#pragma unroll
+          for (int c = 0; c < kHalfCols; ++c) x[c] *= p.scale_log2;
+        }
+        if (group_any(bar_id, over)) {
+          // ---- largest score of every column in this tile; the reference goes up where it is passed by 2^8
+          float y[kHalfCols / 2];  // over the lanes, half of the columns in every step; lane c ends with column c
+#pragma unroll
+          for (int c = 0; c < 16; ++c) {
+            const float give = lane & 16 ? x[c] : x[c + 16], keep = lane & 16 ? x[c + 16] : x[c];
+            y[c] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, give, 16));
+          }
+#pragma unroll
+          for (int o = 8; o > 0; o >>= 1) {
+#pragma unroll
+            for (int c = 0; c < o; ++c) {
+              const float give = lane & o ? y[c] : y[c + o], keep = lane & o ? y[c + o] : y[c];
+              y[c] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, give, o));
+            }
+          }
+          const float top = y[0];
+          sc.part[t][wq][c0 + lane] = top;
+          if (later) ok = wait_warp(o_done0 + 8 * t, par ^ 1, abort_flag) && ok;
+          if (group_any(bar_id, !ok)) { ok = false; break; }
+          if (wq == 0) {  // a lane per column
+            float up = fmaxf(fmaxf(top, sc.part[t][1][c0 + lane]), fmaxf(sc.part[t][2][c0 + lane], sc.part[t][3][c0 + lane]));
+            // x is relative to the reference; a row that sees no token yet keeps the reference 0 (weights 0)
+            if (later) up = up > kRescaleThreshold ? up : 0.f;
+            else if (up == -INFINITY) up = 0.f;
+            sc.part[t][0][c0 + lane] = up;
+            m[lane] = later ? m[lane] + up : up;
+          }
+          group_sync(bar_id);
+          const float* rise = &sc.part[t][0][c0];
+          tc::fence_after_sync();
+#pragma unroll
+          for (int q = 0; q < kHalfCols / 8; ++q) {
+            if (!(mask >> q & 1)) continue;
+            uint32_t o[8];
+            if (later) {
+              tc::ld_32x32b_x8(o_taddr + t * kThinCols + q * 8, o);
+              tc::wait_ld();
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const float up = rise[q * 8 + e];
+              x[q * 8 + e] -= up;
+              if (later) {
+                const float alpha = ex2(-up);
+                l[q * 8 + e] *= alpha;
+                o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
+              }
+            }
+            if (later) tc::st_32x32b_x8(o_taddr + t * kThinCols + q * 8, o);
+          }
+          if (later) tc::wait_st();
+        } else {  // the last product of this group has read its P^T
+          ok = wait_warp(o_done0 + 8 * t, par ^ 1, abort_flag) && ok;
+        }
+        // ---- P^T = 2^x as packed bf16, one row of 128 bytes per token, 16-byte chunks exclusive-ored with the row
+#pragma unroll
+        for (int q = 0; q < kHalfCols / 8; ++q)
+          if (mask >> q & 1) {
+            uint32_t y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float p0 = ex2(x[q * 8 + 2 * e]), p1 = ex2(x[q * 8 + 2 * e + 1]);
+              l[q * 8 + 2 * e] += p0;
+              l[q * 8 + 2 * e + 1] += p1;
+              y[e] = pack2(p0, p1);
+            }
+            *reinterpret_cast<uint4*>(p_row + (((half * 4 + q) ^ (r & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
+          }
+        ptx::fence_proxy_async();
+        tc::fence_before_sync();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(p_full0 + 8 * t);
+      }
+      // ---- the segment's result: sums over the lanes (every lane ends up with one column), then over the warps
+      if (t < tiles) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+#pragma unroll
+          for (int c = 0; c < o; ++c) {
+            const bool up = lane & o;
+            const float give = up ? l[c] : l[c + o], keep = up ? l[c + o] : l[c];
+            l[c] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+          }
+        }
+        ok = wait_warp(o_done0 + 8 * t, par ^ 1, abort_flag) && ok;
+        if (group_any(bar_id, !ok)) { ok = false; break; }  // also: the last raise has read its maxima
+        tc::fence_after_sync();
+        sc.part[t][wq][c0 + lane] = l[0];
+      }
+      other += t == 0 ? tiles >> 1 : (tiles + 1) >> 1;
+      const bool join = tiles > 1;
+      if (t == 1) {
+        tc::fence_before_sync();
+        __syncwarp();
+        if (lane == 0) {
+          if (join) ptx::mbar_arrive(x_full);
+          ptx::mbar_arrive(seg_empty0 + 8 * (segs % kSegRing));
+        }
+        if (join) xpar ^= 1;
+        continue;
+      }
+      if (join) {
+        ok = wait_warp(x_full, xpar, abort_flag);
+        xpar ^= 1;
+        tc::fence_after_sync();
+      }
+      if (group_any(bar_id, !ok)) { ok = false; break; }
+      const bool whole = w.flags & kSegWhole;
+      const long long prow0 = (2LL * blockIdx.x + ((w.flags & kSegFirst) ? 1 : 0)) * p.list.slot_rows;
+      if (wq == 0) {  // a lane per column: the two groups' weights in the result, the log-sum-exp
+        const int c = c0 + lane, g = c / p.region, lc = c & (p.region - 1);
+        const float l0 = sc.part[0][0][c] + sc.part[0][1][c] + sc.part[0][2][c] + sc.part[0][3][c];
+        const float l1 = join ? sc.part[1][0][c] + sc.part[1][1][c] + sc.part[1][2][c] + sc.part[1][3][c] : 0.f;
+        const float m0 = l0 > 0.f ? sc.m[0][c] : -INFINITY, m1 = l1 > 0.f ? sc.m[1][c] : -INFINITY;
+        const float top = fmaxf(m0, m1);
+        const float e0 = l0 > 0.f ? exp2f(m0 - top) : 0.f, e1 = l1 > 0.f ? exp2f(m1 - top) : 0.f;
+        const float sum = l0 * e0 + l1 * e1, inv = sum > 0.f ? 1.f / sum : 0.f;
+        sc.m[0][c] = e0 * inv;
+        if (join) sc.m[1][c] = e1 * inv;
+        if (g < p.parts && lc < used) {
+          const float lse2 = sum > 0.f ? top + log2f(sum) : -INFINITY;
+          const int token = lc / p.G;
+          if (!whole) p.list.part_lse[prow0 + g * used + lc] = lse2;
+          else if (p.lse) p.lse[(long long)(w.row_lo + token) * p.n_q + w.head0 + g * p.G + lc - token * p.G] = lse2 * kLn2;
+        }
+      }
+      group_sync(bar_id);
+#pragma unroll 1
+      for (int q = 0; q < kHalfCols / 8; ++q) {
+        if (!(mask >> q & 1)) continue;
+        uint32_t o0[8], o1[8];
+        tc::ld_32x32b_x8(o_taddr + q * 8, o0);
+        if (join) tc::ld_32x32b_x8(o_taddr + kThinCols + q * 8, o1);
+        tc::wait_ld();
+        const int c = c0 + q * 8, g = c / p.region, lc = c & (p.region - 1);
+        // the lanes that hold this head group's channels
+        const bool mine = kHalves == 2 || (r < 64) == (p.v_parts % 2 != 0 || g % 2 == 0);
+        const int ch = r & (kD - 1);
+        int token = lc / p.G, h = lc - token * p.G;
+        long long at = whole ? ((long long)(w.row_lo + token) * p.n_q + w.head0 + g * p.G + h) * kD + ch
+                             : (prow0 + g * used + lc) * kD + ch;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float y = __uint_as_float(o0[e]) * sc.m[0][c + e];
+          if (join) y = fmaf(__uint_as_float(o1[e]), sc.m[1][c + e], y);
+          if (lc + e < used && mine) {
+            if (!whole) p.list.part_o[at] = y;
+            else if (p.out_is_f32) reinterpret_cast<float*>(p.out)[at] = y;
+            else reinterpret_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(y);
+          }
+          at += kD;
+          if (whole && ++h == p.G) {  // the next token's first head
+            h = 0;
+            at += (long long)(p.n_q - p.G) * kD;
+          }
+        }
+      }
+      group_sync(bar_id);  // the weights have been read
+      tc::fence_before_sync();
+      __syncwarp();
+      if (lane == 0) {
+        ptx::mbar_arrive(o_free0);
+        if (join) {
+          ptx::mbar_arrive(o_free0 + 8);
+          ptx::mbar_arrive(x_empty);
+        }
+        ptx::mbar_arrive(seg_empty0 + 8 * (segs % kSegRing));
+      }
+    }
+    if (!ok) report(p.dev_status, DIFFQKV_ERR_TIMEOUT);
+  }
+
+  // ---- teardown: all products this block issued must be done before its tensor memory is released
+  tc::fence_before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    ptx::mbar_wait(drain, 0, nullptr);
+    tc::fence_after_sync();
+    tc::tmem_dealloc(tmem, kTmemCols);
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_extend_thin(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const ExtendParams& p,
+                               int d_qk, int d_v, int blocks, cudaStream_t stream) {
+  using Fn = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const ExtendParams);
+  const Fn fn = d_v == 64 ? extend_thin_kernel<64, 64> : (d_qk == 128 ? extend_thin_kernel<128, 128> : extend_thin_kernel<64, 128>);
+  const cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kThinSmem);
+  if (err != cudaSuccess) return err;
+  fn<<<blocks, kExtendThinThreads, kThinSmem, stream>>>(mq, mk, mv, p);
+  count_launch();
+  return cudaGetLastError();
+}
+
+}  // namespace diffqkv
