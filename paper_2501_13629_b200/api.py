@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 from typing import Optional, Tuple
 
@@ -611,30 +612,88 @@ def diffqkv_decode_topk(q: torch.Tensor, cache: KVCache, n_k: int, n_v: int, sca
 
 
 # ---- ragged batches over the cache: a step's new rows of sequence b are rows cu_q[b] .. cu_q[b + 1] - 1 of every ragged
-# tensor, cache.seqlens[b] is the number of tokens cached before the step (the caller adds the chunk lengths after it)
+# tensor, cache.seqlens[b] is the number of tokens cached before the step (the caller adds the chunk lengths after it).
+#
+# These calls take a few microseconds on the GPU when the step is small, so their marshalling is kept short: the argument
+# structs are packed into bytes (fields as in the ctypes structures above), and addresses go over as plain integers.
 
-def _on_device(*tensors: Optional[torch.Tensor]) -> None:
-    """The launch goes to the current device: every tensor has to be there."""
+_raw = C.CDLL(LIB_PATH)
+_B, _V, _I, _L = C.c_char_p, C.c_void_p, C.c_int32, C.c_int64
+for _name, _args in (
+        ("diffqkv_extend", [_V, _V, _I, _B, _B, _V, C.c_size_t, _V, _V, _V, _V]),
+        ("diffqkv_rope_append", [_V, _V, _V, _V, _I, _L, _L, _L, _B, _B, _B, _V, _V, _V]),
+        ("diffqkv_pages_free", [_V, _V, _I, _B, _V, _V]),
+        ("diffqkv_pages_fork", [_V, _V, _I, _B, _V, C.c_size_t, _V, _V]),
+        ("diffqkv_pages_reserve", [_V, _B, _B, _B, _V, _V, C.c_size_t, _V, _V]),
+        ("diffqkv_pages_copy", [_V, _V, _I, _B, _B, _B, _V, _V]),
+        ("diffqkv_pages_compact", [_B, _B, _B, _V, _V, _V, _V, C.c_size_t, _V, _V])):
+    getattr(_raw, _name).restype = C.c_int
+    getattr(_raw, _name).argtypes = _args
+for _name, _args in (("diffqkv_extend_workspace_bytes", [_B, _I]), ("diffqkv_pages_fork_workspace_bytes", [_B, _I]),
+                     ("diffqkv_pages_reserve_workspace_bytes", [_B]), ("diffqkv_pages_compact_workspace_bytes", [_B])):
+    getattr(_raw, _name).restype = C.c_size_t
+    getattr(_raw, _name).argtypes = _args
+_pack_cache = struct.Struct("@PP6qPP4i").pack
+_pack_shape = struct.Struct("@8if").pack
+_pack_rope = struct.Struct("@PP2if4x").pack
+_pack_pages = struct.Struct("@PPP4i").pack
+_DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _device_of(*tensors: Optional[torch.Tensor]) -> int:
+    """The launch goes to the current device: every tensor (or None) has to be there."""
+    dev = tensors[0].get_device()
     for t in tensors:
-        if t is not None and t.get_device() < 0:
-            raise ValueError(f"expected a CUDA tensor, got one on {t.device}")
-    current = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != current:
-            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{current}")
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"tensors on {tensors[0].device} and {t.device}")
+    if dev < 0:
+        raise ValueError(f"expected CUDA tensors, got some on {tensors[0].device}")
+    if dev != _current_device():
+        raise ValueError(f"tensors on cuda:{dev}, but the current device is cuda:{_current_device()}")
+    return dev
 
 
-def _on_device_cache(cache: KVCache, *tensors: Optional[torch.Tensor]) -> None:
-    _on_device(cache.k, cache.v, cache.seqlens, cache.page_table, *tensors)
+def _stream_on(stream: Optional[torch.cuda.Stream], dev: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
-def _cu_q(cu_q: torch.Tensor, batch: int) -> C.c_void_p:
-    assert cu_q.dtype == torch.int32 and cu_q.is_contiguous() and cu_q.numel() == batch + 1
-    return _p(cu_q)
+def _addr(t: Optional[torch.Tensor]) -> Optional[int]:
+    return None if t is None else t.data_ptr()
+
+
+def _ints(t: Optional[torch.Tensor], n: Optional[int] = None) -> Optional[int]:
+    """Address of a dense int32 tensor (of n elements) or None."""
+    if t is None:
+        return None
+    assert t.dtype == torch.int32 and t.is_contiguous() and (n is None or t.numel() == n)
+    return t.data_ptr()
+
+
+def _cache_bytes(cache: KVCache) -> bytes:
+    k, v, pt = cache.k, cache.v, cache.page_table
+    ks, vs = cache.k_strides or k.stride(), cache.v_strides or v.stride()
+    pages = 0
+    if pt is not None:
+        assert pt.dtype == torch.int32 and pt.is_contiguous() and pt.dim() == 2
+        pages = pt.shape[1]
+    nb = cache.num_blocks
+    return _pack_cache(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], _ints(cache.seqlens),
+                       0 if pt is None else pt.data_ptr(), cache.page_size, pages, k.shape[0] if nb is None else nb,
+                       cache.max_seqlen)
 
 
 def _workspace(workspace: Optional[torch.Tensor], nbytes: int, device) -> torch.Tensor:
-    return torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=device) if workspace is None else workspace
+    return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device) if workspace is None else workspace
+
+
+def _size(workspace: torch.Tensor) -> int:
+    return workspace.numel() * workspace.element_size()
+
+
+def _check_status(st: int, where: str) -> None:
+    if st != OK:
+        raise DiffQKVError(st, where)
 
 
 def diffqkv_extend_workspace_bytes(shape: ShapeStruct, total_q: int) -> int:
@@ -650,20 +709,21 @@ def diffqkv_extend(q: torch.Tensor, cu_q: torch.Tensor, cache: KVCache, n_k: int
     anything there)."""
     total_q, n_q, d_qk = q.shape
     d_v = cache.v.shape[-1]
-    batch = cache.seqlens.numel()
-    _on_device_cache(cache, q, cu_q, workspace, out, lse, dev_status)
-    assert cache.k.dtype == q.dtype and cache.v.dtype == q.dtype
-    assert q.is_contiguous() and (out is None or out.is_contiguous()) and (lse is None or lse.is_contiguous())
-    out_dtype = out_dtype or (out.dtype if out is not None else q.dtype)
-    shape = make_shape(batch, n_q, n_k, n_v, d_qk, d_v, q.dtype, out_dtype, scale)
-    workspace = _workspace(workspace, _lib.diffqkv_extend_workspace_bytes(C.byref(shape), total_q), q.device)
+    batch = cache.seqlens.shape[0]
+    dev = _device_of(q, cu_q, cache.k, cache.v, cache.seqlens, cache.page_table, out, lse, workspace, dev_status)
+    dtype = q.dtype
+    assert cache.k.dtype == dtype and cache.v.dtype == dtype and q.is_contiguous()
+    out_dtype = out_dtype or (dtype if out is None else out.dtype)
     if out is None:
         out = torch.empty((total_q, n_q, d_v), dtype=out_dtype, device=q.device)
-    cs = cache.c_struct()
-    st = _lib.diffqkv_extend(_p(q), _cu_q(cu_q, batch), total_q, C.byref(cs), C.byref(shape), _p(workspace),
-                             workspace.numel(), _p(out), _p(lse), _p(dev_status), _stream_ptr(stream))
-    if st != OK:
-        raise DiffQKVError(st, "diffqkv_extend")
+    assert out.is_contiguous() and out.numel() == total_q * n_q * d_v and out.dtype == out_dtype
+    assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == total_q * n_q)
+    shape = _pack_shape(batch, n_q, n_k, n_v, d_qk, d_v, _DTYPES[dtype], _DTYPES[out_dtype], scale)
+    if workspace is None:
+        workspace = _workspace(None, _raw.diffqkv_extend_workspace_bytes(shape, total_q), q.device)
+    _check_status(_raw.diffqkv_extend(q.data_ptr(), _ints(cu_q, batch + 1), total_q, _cache_bytes(cache), shape,
+                                      workspace.data_ptr(), _size(workspace), out.data_ptr(), _addr(lse),
+                                      _addr(dev_status), _stream_on(stream, dev)), "diffqkv_extend")
     return out
 
 
@@ -676,17 +736,16 @@ def rope_frequencies(rot_dim: int, theta: float, scaling: str = "plain", factor:
     """The table of inverse frequencies (float64 [rot_dim / 2], on ``device``) and the magnitude that goes with it."""
     table = (C.c_double * max(rot_dim // 2, 1))()
     magnitude = C.c_float()
-    st = _lib.diffqkv_rope_frequencies(rot_dim, theta, ROPE_SCALINGS[scaling], factor, original_length, fast, slow, table,
-                                       C.byref(magnitude))
-    if st != OK:
-        raise DiffQKVError(st, "diffqkv_rope_frequencies")
+    _check_status(_lib.diffqkv_rope_frequencies(rot_dim, theta, ROPE_SCALINGS[scaling], factor, original_length, fast,
+                                                slow, table, C.byref(magnitude)), "diffqkv_rope_frequencies")
     return torch.tensor(list(table), dtype=torch.float64, device=device), float(magnitude.value)
 
 
-def _row_stride(x: torch.Tensor) -> int:
+def _row_stride(x: torch.Tensor, rows: int, d: int) -> int:
     """Elements between the rows of x [rows, heads, d] whose heads are dense (a slice of a fused projection, say)."""
-    assert x.dim() == 3 and x.stride(2) == 1 and (x.shape[1] == 1 or x.stride(1) == x.shape[2])
-    return int(x.stride(0)) if x.shape[0] > 1 else 0
+    st = x.stride()
+    assert len(st) == 3 and x.shape[0] == rows and st[2] == 1 and (x.shape[1] == 1 or st[1] == d)
+    return st[0] if rows > 1 else 0
 
 
 def diffqkv_rope_append(q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: torch.Tensor, cu_q: torch.Tensor,
@@ -698,113 +757,101 @@ def diffqkv_rope_append(q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: t
     positions seqlens[b] + i; returns the rotated q (q_out may be q).  ``inv_freq`` float64 [rot_dim / 2], None for no
     rotation; ``positions`` int32 [total_q] replaces the rotation's position seqlens[b] + i."""
     total_q, n_k, d_qk = k_new.shape
-    n_v, d_v = v_new.shape[1], v_new.shape[2]
-    batch = cache.seqlens.numel()
-    n_q = n_k * n_v if q is None else q.shape[1]  # without queries any count both head counts divide does
-    _on_device_cache(cache, q, k_new, v_new, cu_q, inv_freq, positions, q_out, dev_status)
-    assert cache.k.dtype == k_new.dtype and cache.v.dtype == k_new.dtype
-    assert v_new.shape[0] == total_q and (q is None or (q.shape[0] == total_q and q.shape[2] == d_qk))
-    assert v_new.dtype == k_new.dtype and (q is None or q.dtype == k_new.dtype)
-    assert inv_freq is None or (inv_freq.dtype == torch.float64 and inv_freq.is_contiguous())
-    assert positions is None or (positions.dtype == torch.int32 and positions.is_contiguous() and
-                                 positions.numel() == total_q)
-    if q is not None and q_out is None:
-        q_out = torch.empty((total_q, n_q, d_qk), dtype=q.dtype, device=q.device)
-    assert q_out is None or q_out.is_contiguous()
-    shape = make_shape(batch, n_q, n_k, n_v, d_qk, d_v, k_new.dtype, k_new.dtype, 1.0)
-    rope = RopeStruct(None if inv_freq is None else inv_freq.data_ptr(), None if positions is None else positions.data_ptr(),
-                      0 if inv_freq is None else 2 * inv_freq.numel(), int(bool(interleaved)), float(magnitude))
-    cs = cache.c_struct()
-    st = _lib.diffqkv_rope_append(_p(q), _p(k_new), _p(v_new), _cu_q(cu_q, batch), total_q,
-                                  0 if q is None else _row_stride(q), _row_stride(k_new), _row_stride(v_new),
-                                  C.byref(rope), C.byref(cs), C.byref(shape), _p(q_out), _p(dev_status),
-                                  _stream_ptr(stream))
-    if st != OK:
-        raise DiffQKVError(st, "diffqkv_rope_append")
+    _, n_v, d_v = v_new.shape
+    batch = cache.seqlens.shape[0]
+    dev = _device_of(k_new, q, v_new, cu_q, cache.k, cache.v, cache.seqlens, cache.page_table, inv_freq, positions, q_out,
+                     dev_status)
+    dtype = k_new.dtype
+    assert v_new.dtype == dtype and cache.k.dtype == dtype and cache.v.dtype == dtype
+    n_q, q_stride = n_k * n_v, 0  # without queries any count both head counts divide does
+    if q is not None:
+        n_q, q_stride = q.shape[1], _row_stride(q, total_q, d_qk)
+        assert q.dtype == dtype and q.shape[2] == d_qk
+        if q_out is None:
+            q_out = torch.empty((total_q, n_q, d_qk), dtype=dtype, device=q.device)
+        assert q_out.is_contiguous() and q_out.dtype == dtype and q_out.numel() == total_q * n_q * d_qk
+    freqs, rot = 0, 0
+    if inv_freq is not None:
+        assert inv_freq.dtype == torch.float64 and inv_freq.is_contiguous()
+        freqs, rot = inv_freq.data_ptr(), 2 * inv_freq.numel()
+    rope = _pack_rope(freqs, _ints(positions, total_q) or 0, rot, bool(interleaved), magnitude)
+    code = _DTYPES[dtype]
+    _check_status(_raw.diffqkv_rope_append(
+        _addr(q), k_new.data_ptr(), v_new.data_ptr(), _ints(cu_q, batch + 1), total_q, q_stride,
+        _row_stride(k_new, total_q, d_qk), _row_stride(v_new, total_q, d_v), rope, _cache_bytes(cache),
+        _pack_shape(batch, n_q, n_k, n_v, d_qk, d_v, code, code, 1.0), _addr(q_out), _addr(dev_status),
+        _stream_on(stream, dev)), "diffqkv_rope_append")
     return q_out
 
 
 # ---- upkeep of the pages: cache.page_table [num_seqs, max_pages_per_seq], cache.seqlens and ref_counts [num_pages] are
 # written by these calls
 
-def _ints(t: Optional[torch.Tensor], n: Optional[int] = None):
-    assert t is None or (t.dtype == torch.int32 and t.is_contiguous() and (n is None or t.numel() == n))
-    return _p(t)
-
-
-def _pages(cache: KVCache, ref_counts: torch.Tensor) -> PagesStruct:
+def _pages_bytes(cache: KVCache, ref_counts: torch.Tensor) -> bytes:
     pt = cache.page_table
     assert pt is not None and pt.dtype == torch.int32 and pt.is_contiguous() and pt.dim() == 2
-    assert cache.seqlens.dtype == torch.int32 and cache.seqlens.is_contiguous() and cache.seqlens.numel() == pt.shape[0]
-    assert ref_counts.dtype == torch.int32 and ref_counts.is_contiguous()
-    return PagesStruct(pt.data_ptr(), cache.seqlens.data_ptr(), ref_counts.data_ptr(), pt.shape[0], pt.shape[1],
-                       ref_counts.numel(), int(cache.page_size))
+    seqs, row = pt.shape
+    return _pack_pages(pt.data_ptr(), _ints(cache.seqlens, seqs), _ints(ref_counts), seqs, row, ref_counts.numel(),
+                       cache.page_size)
 
 
-def _pool_shape(cache: KVCache, n_k: int, n_v: int) -> ShapeStruct:
-    assert cache.k.dtype == cache.v.dtype
-    return make_shape(1, n_k * n_v, n_k, n_v, cache.k.shape[-1], cache.v.shape[-1], cache.k.dtype, cache.k.dtype, 1.0)
+def _pools_bytes(cache: KVCache, n_k: int, n_v: int) -> bytes:
+    code = _DTYPES[cache.k.dtype]
+    assert cache.v.dtype == cache.k.dtype
+    return _pack_shape(1, n_k * n_v, n_k, n_v, cache.k.shape[-1], cache.v.shape[-1], code, code, 1.0)
 
 
 def diffqkv_pages_free(seq_ids: torch.Tensor, cache: KVCache, ref_counts: torch.Tensor,
                        keep_tokens: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
                        stream: Optional[torch.cuda.Stream] = None) -> None:
     """Give back the pages of the sequences ``seq_ids`` (int32 [n]) behind their first ``keep_tokens`` tokens."""
-    _on_device_cache(cache, seq_ids, keep_tokens, ref_counts, dev_status)
-    g = _pages(cache, ref_counts)
+    dev = _device_of(seq_ids, cache.page_table, cache.seqlens, ref_counts, keep_tokens, dev_status)
     n = seq_ids.numel()
-    st = _lib.diffqkv_pages_free(_ints(seq_ids), _ints(keep_tokens, n), n, C.byref(g), _p(dev_status), _stream_ptr(stream))
-    if st != OK:
-        raise DiffQKVError(st, "diffqkv_pages_free")
+    _check_status(_raw.diffqkv_pages_free(_ints(seq_ids), _ints(keep_tokens, n), n, _pages_bytes(cache, ref_counts),
+                                          _addr(dev_status), _stream_on(stream, dev)), "diffqkv_pages_free")
 
 
 def diffqkv_pages_fork(parents: torch.Tensor, children: torch.Tensor, cache: KVCache, ref_counts: torch.Tensor,
                        workspace: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
                        stream: Optional[torch.cuda.Stream] = None) -> None:
     """Sequence children[i] becomes a copy of sequence parents[i] that shares its pages."""
-    _on_device_cache(cache, parents, children, ref_counts, workspace, dev_status)
-    g = _pages(cache, ref_counts)
+    dev = _device_of(parents, children, cache.page_table, cache.seqlens, ref_counts, workspace, dev_status)
+    g = _pages_bytes(cache, ref_counts)
     n = children.numel()
-    workspace = _workspace(workspace, _lib.diffqkv_pages_fork_workspace_bytes(C.byref(g), n), ref_counts.device)
-    st = _lib.diffqkv_pages_fork(_ints(parents, n), _ints(children), n, C.byref(g), _p(workspace), workspace.numel(),
-                                 _p(dev_status), _stream_ptr(stream))
-    if st != OK:
-        raise DiffQKVError(st, "diffqkv_pages_fork")
+    if workspace is None:
+        workspace = _workspace(None, _raw.diffqkv_pages_fork_workspace_bytes(g, n), ref_counts.device)
+    _check_status(_raw.diffqkv_pages_fork(_ints(parents, n), _ints(children), n, g, workspace.data_ptr(), _size(workspace),
+                                          _addr(dev_status), _stream_on(stream, dev)), "diffqkv_pages_fork")
 
 
 def diffqkv_pages_reserve(cu_q: torch.Tensor, cache: KVCache, ref_counts: torch.Tensor, n_k: int, n_v: int,
                           granted: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
                           dev_status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> None:
     """Give every sequence pages of its own for its next cu_q[b + 1] - cu_q[b] tokens (copy on write)."""
-    _on_device_cache(cache, cu_q, ref_counts, granted, workspace, dev_status)
-    g = _pages(cache, ref_counts)
-    shape = _pool_shape(cache, n_k, n_v)
-    cs = cache.c_struct()
-    workspace = _workspace(workspace, _lib.diffqkv_pages_reserve_workspace_bytes(C.byref(g)), ref_counts.device)
-    st = _lib.diffqkv_pages_reserve(_cu_q(cu_q, g.num_seqs), C.byref(g), C.byref(cs), C.byref(shape),
-                                    _ints(granted, g.num_seqs), _p(workspace), workspace.numel(), _p(dev_status),
-                                    _stream_ptr(stream))
-    if st != OK:
-        raise DiffQKVError(st, "diffqkv_pages_reserve")
+    dev = _device_of(cu_q, cache.k, cache.v, cache.page_table, cache.seqlens, ref_counts, granted, workspace, dev_status)
+    g = _pages_bytes(cache, ref_counts)
+    seqs = cache.page_table.shape[0]
+    if workspace is None:
+        workspace = _workspace(None, _raw.diffqkv_pages_reserve_workspace_bytes(g), ref_counts.device)
+    _check_status(_raw.diffqkv_pages_reserve(_ints(cu_q, seqs + 1), g, _cache_bytes(cache), _pools_bytes(cache, n_k, n_v),
+                                             _ints(granted, seqs), workspace.data_ptr(), _size(workspace),
+                                             _addr(dev_status), _stream_on(stream, dev)), "diffqkv_pages_reserve")
 
 
 def diffqkv_pages_copy(src_ids: torch.Tensor, dst_ids: torch.Tensor, cache: KVCache, n_k: int, n_v: int,
                        dst_cache: Optional[KVCache] = None, dev_status: Optional[torch.Tensor] = None,
                        stream: Optional[torch.cuda.Stream] = None) -> None:
     """Pages src_ids[i] of ``cache`` become pages dst_ids[i] of ``dst_cache`` (default: of the same cache)."""
-    _on_device(cache.k, cache.v, src_ids, dst_ids, dev_status)
+    dev = _device_of(src_ids, dst_ids, cache.k, cache.v, dev_status)
+    src = dst = _cache_bytes(cache)
     if dst_cache is not None:
-        _on_device(dst_cache.k, dst_cache.v)
+        _device_of(src_ids, dst_cache.k, dst_cache.v)
         assert dst_cache.k.dtype == cache.k.dtype and dst_cache.v.dtype == cache.v.dtype
         assert dst_cache.k.shape[-1] == cache.k.shape[-1] and dst_cache.v.shape[-1] == cache.v.shape[-1]
-    shape = _pool_shape(cache, n_k, n_v)
-    src = cache.c_struct()
-    dst = src if dst_cache is None else dst_cache.c_struct()
+        dst = _cache_bytes(dst_cache)
     n = src_ids.numel()
-    st = _lib.diffqkv_pages_copy(_ints(src_ids), _ints(dst_ids, n), n, C.byref(src), C.byref(dst), C.byref(shape),
-                                 _p(dev_status), _stream_ptr(stream))
-    if st != OK:
-        raise DiffQKVError(st, "diffqkv_pages_copy")
+    _check_status(_raw.diffqkv_pages_copy(_ints(src_ids), _ints(dst_ids, n), n, src, dst, _pools_bytes(cache, n_k, n_v),
+                                          _addr(dev_status), _stream_on(stream, dev)), "diffqkv_pages_copy")
 
 
 def diffqkv_pages_compact(cache: KVCache, ref_counts: torch.Tensor, n_k: int, n_v: int,
@@ -813,16 +860,15 @@ def diffqkv_pages_compact(cache: KVCache, ref_counts: torch.Tensor, n_k: int, n_
                           dev_status: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """Move the pages in use to the front of the pool; returns the new (page table, counts), which are the cache's own
     tensors changed in place unless others are passed."""
-    _on_device_cache(cache, ref_counts, table_out, refs_out, live, workspace, dev_status)
-    g = _pages(cache, ref_counts)
-    shape = _pool_shape(cache, n_k, n_v)
-    cs = cache.c_struct()
+    dev = _device_of(ref_counts, cache.k, cache.v, cache.page_table, cache.seqlens, table_out, refs_out, live, workspace,
+                     dev_status)
+    g = _pages_bytes(cache, ref_counts)
     table_out = cache.page_table if table_out is None else table_out
     refs_out = ref_counts if refs_out is None else refs_out
-    workspace = _workspace(workspace, _lib.diffqkv_pages_compact_workspace_bytes(C.byref(g)), ref_counts.device)
-    st = _lib.diffqkv_pages_compact(C.byref(g), C.byref(cs), C.byref(shape), _ints(table_out, cache.page_table.numel()),
-                                    _ints(refs_out, ref_counts.numel()), _ints(live, 1), _p(workspace),
-                                    workspace.numel(), _p(dev_status), _stream_ptr(stream))
-    if st != OK:
-        raise DiffQKVError(st, "diffqkv_pages_compact")
+    if workspace is None:
+        workspace = _workspace(None, _raw.diffqkv_pages_compact_workspace_bytes(g), ref_counts.device)
+    _check_status(_raw.diffqkv_pages_compact(g, _cache_bytes(cache), _pools_bytes(cache, n_k, n_v),
+                                             _ints(table_out, cache.page_table.numel()), _ints(refs_out, ref_counts.numel()),
+                                             _ints(live, 1), workspace.data_ptr(), _size(workspace), _addr(dev_status),
+                                             _stream_on(stream, dev)), "diffqkv_pages_compact")
     return table_out, refs_out

@@ -771,7 +771,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
 // Joins the partial rows of the items that were cut: blocks x = 0 .. take the items that the blocks of the first kernel
 // began, then those of the second's; the rows of an item are dealt to gridDim.y blocks, and there to groups of kD / 4
 // lanes with four channels each.
-constexpr int kCombineThreads = 256;
+constexpr int kCombineThreads = 256, kMany = 4;
 
 template <int kD>
 __global__ void __launch_bounds__(kCombineThreads) extend_combine_kernel(const ExtendParams p, const ExtendList thin,
@@ -790,53 +790,77 @@ __global__ void __launch_bounds__(kCombineThreads) extend_combine_kernel(const E
   const long long total = *list.total;
   __syncthreads();
   // the teams that own tiles of the item, from the first on (in order: sums do not depend on timing)
-  const int k = first + threadIdx.x;
-  if (k < list.n_teams) {
-    const long long a = share_start(total, k, list.n_teams), z = share_start(total, k + 1, list.n_teams);
-    int slot = -1;
-    if (a < m.lo + (long long)m.cost * m.nt) {
-      const int ta = a <= m.lo ? 0 : (int)(((uint32_t)(a - m.lo) + m.cost - 1) / (uint32_t)m.cost);
-      const int tb = z - m.lo >= (long long)m.cost * m.nt ? m.nt : (int)(((uint32_t)(z - m.lo) + m.cost - 1) / (uint32_t)m.cost);
-      if (ta < tb) slot = 2 * (k * list.team + m.member) + (ta == 0);
-      atomicMax(&count_s, k - first + 1);
+  if (m.chunks > 0) {
+    if ((int)threadIdx.x < m.chunks) slots[threadIdx.x] = 2 * (block + threadIdx.x) + (threadIdx.x == 0);
+    if (threadIdx.x == 0) count_s = m.chunks;
+  } else {
+    const int k = first + threadIdx.x;
+    if (k < list.n_teams) {
+      const long long a = share_start(total, k, list.n_teams), z = share_start(total, k + 1, list.n_teams);
+      int slot = -1;
+      if (a < m.lo + (long long)m.cost * m.nt) {
+        const int ta = a <= m.lo ? 0 : (int)(((uint32_t)(a - m.lo) + m.cost - 1) / (uint32_t)m.cost);
+        const int tb = z - m.lo >= (long long)m.cost * m.nt ? m.nt : (int)(((uint32_t)(z - m.lo) + m.cost - 1) / (uint32_t)m.cost);
+        if (ta < tb) slot = 2 * (k * list.team + m.member) + (ta == 0);
+        atomicMax(&count_s, k - first + 1);
+      }
+      slots[threadIdx.x] = slot;
     }
-    slots[threadIdx.x] = slot;
   }
   __syncthreads();
   const int n = count_s, lane = threadIdx.x % kLanes;
-  for (int r = blockIdx.y * kGroups + threadIdx.x / kLanes; r < m.rows; r += gridDim.y * kGroups) {
-    float top = -INFINITY;
-#pragma unroll 4
-    for (int i = 0; i < n; ++i)
-      if (slots[i] >= 0) top = fmaxf(top, list.part_lse[(long long)slots[i] * list.slot_rows + r]);
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
-#pragma unroll 4
+  // kMany rows at a time, so that their loads are in flight together
+  for (int r0 = blockIdx.y * kGroups + threadIdx.x / kLanes; r0 < m.rows; r0 += gridDim.y * kGroups * kMany) {
+    float top[kMany], sum[kMany];
+    float4 acc[kMany];
+    const int step = gridDim.y * kGroups;
+#pragma unroll
+    for (int y = 0; y < kMany; ++y) {
+      top[y] = -INFINITY;
+      sum[y] = 0.f;
+      acc[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
     for (int i = 0; i < n; ++i) {
       const int slot = slots[i];
       if (slot < 0) continue;
-      const long long at = (long long)slot * list.slot_rows + r;
-      const float ls = list.part_lse[at];
-      const float4 o = *reinterpret_cast<const float4*>(list.part_o + at * kD + lane * 4);
-      if (ls == -INFINITY) continue;  // the part saw no token of this row (and wrote no values)
-      const float f = exp2f(ls - top);
-      sum += f;
-      acc.x = fmaf(f, o.x, acc.x);
-      acc.y = fmaf(f, o.y, acc.y);
-      acc.z = fmaf(f, o.z, acc.z);
-      acc.w = fmaf(f, o.w, acc.w);
+      const long long at = (long long)slot * list.slot_rows;
+      float ls[kMany];
+      float4 o[kMany];
+#pragma unroll
+      for (int y = 0; y < kMany; ++y) {
+        const int r = min(r0 + y * step, m.rows - 1);
+        ls[y] = list.part_lse[at + r];
+        o[y] = *reinterpret_cast<const float4*>(list.part_o + (at + r) * kD + lane * 4);
+      }
+#pragma unroll
+      for (int y = 0; y < kMany; ++y) {
+        if (ls[y] == -INFINITY) continue;  // the part saw no token of this row (and may have left no values)
+        const float up = fmaxf(top[y], ls[y]);
+        const float was = exp2f(top[y] - up), f = exp2f(ls[y] - up);
+        top[y] = up;
+        sum[y] = sum[y] * was + f;
+        acc[y].x = fmaf(f, o[y].x, acc[y].x * was);
+        acc[y].y = fmaf(f, o[y].y, acc[y].y * was);
+        acc[y].z = fmaf(f, o[y].z, acc[y].z * was);
+        acc[y].w = fmaf(f, o[y].w, acc[y].w * was);
+      }
     }
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
-    const int g = r / m.part_rows, lr = r - g * m.part_rows, tok = lr / p.G;
-    const long long row = (long long)(m.row_lo + tok) * p.n_q + m.head0 + g * p.G + (lr - tok * p.G);
-    if (p.out_is_f32) {
-      *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + row * kD + lane * 4) =
-          make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-    } else {
-      *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(p.out) + row * kD + lane * 4) =
-          make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
+#pragma unroll
+    for (int y = 0; y < kMany; ++y) {
+      const int r = r0 + y * step;
+      if (r >= m.rows) break;
+      const float inv = sum[y] > 0.f ? 1.f / sum[y] : 0.f;
+      const int g = r / m.part_rows, lr = r - g * m.part_rows, tok = lr / p.G;
+      const long long row = (long long)(m.row_lo + tok) * p.n_q + m.head0 + g * p.G + (lr - tok * p.G);
+      if (p.out_is_f32) {
+        *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + row * kD + lane * 4) =
+            make_float4(acc[y].x * inv, acc[y].y * inv, acc[y].z * inv, acc[y].w * inv);
+      } else {
+        *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(p.out) + row * kD + lane * 4) =
+            make_uint2(pack2(acc[y].x * inv, acc[y].y * inv), pack2(acc[y].z * inv, acc[y].w * inv));
+      }
+      if (p.lse && lane == 0) p.lse[row] = sum[y] > 0.f ? (top[y] + log2f(sum[y])) * kLn2 : -INFINITY;
     }
-    if (p.lse && lane == 0) p.lse[row] = sum > 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
   }
 }
 
@@ -847,6 +871,21 @@ bool make_cache_map(CUtensorMap* map, const void* base, int d, long long tok_ext
   const cuuint64_t dims[5] = {64, (cuuint64_t)tok_extent, (cuuint64_t)(d / 64), (cuuint64_t)heads, (cuuint64_t)blocks};
   const cuuint64_t strides[4] = {(cuuint64_t)st_tok * 2, 128, (cuuint64_t)st_head * 2, (cuuint64_t)st_blk * 2};
   const cuuint32_t box[5] = {64, (cuuint32_t)box_tok, 1, 1, 1};
+  return make_tmap_bf16_sw128(map, base, 5, dims, strides, box);
+}
+
+// The same for a pool whose heads lie behind one another in a block (stride_head = tokens * stride_tok) and whose rows
+// have 128 channels: dims (64 channels, 8 tokens, channel half, group of 8 tokens of any head, block), so that one box
+// brings whole rows, half as many boxes per tile (16-token pages were bound by the rate of boxes: 235 -> 190 us for 16
+// sequences of 4k-32k tokens, 5 new rows each, 32/4/8 heads).
+bool make_row_map(CUtensorMap* map, const void* base, int d, long long tok_extent, int heads, long long blocks,
+                  long long st_tok, long long st_head, long long st_blk, int box_tok) {
+  if (d != 128 || tok_extent % 8 != 0 || (heads > 1 && st_head != tok_extent * st_tok)) return false;
+  const long long groups = tok_extent / 8 * heads;
+  if (groups > 0x7fffffffLL) return false;
+  const cuuint64_t dims[5] = {64, 8, 2, (cuuint64_t)groups, (cuuint64_t)blocks};
+  const cuuint64_t strides[4] = {(cuuint64_t)st_tok * 2, 128, (cuuint64_t)st_tok * 16, (cuuint64_t)st_blk * 2};
+  const cuuint32_t box[5] = {64, 8, 2, (cuuint32_t)(box_tok / 8), 1};
   return make_tmap_bf16_sw128(map, base, 5, dims, strides, box);
 }
 
@@ -993,8 +1032,14 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
   // the first has, and takes the SMs that the first leaves (an SM has room for one block of either).
   cudaError_t err;
   if (thin_blocks > 0) {
+    CUtensorMap mk_rows, mv_rows;
     p.list = thin;
-    err = launch_extend_thin(mq_thin, mk, mv, p, s.d_qk, s.d_v, thin_blocks, stream);
+    p.head_groups = (int)(tok_extent / 8);
+    p.k_rows = make_row_map(&mk_rows, c.k_cache, s.d_qk, tok_extent, s.n_k, c.num_blocks, c.k_stride_tok, c.k_stride_head,
+                            c.k_stride_blk, box_tok);
+    p.v_rows = make_row_map(&mv_rows, c.v_cache, s.d_v, tok_extent, s.n_v, c.num_blocks, c.v_stride_tok, c.v_stride_head,
+                            c.v_stride_blk, box_tok);
+    err = launch_extend_thin(mq_thin, p.k_rows ? mk_rows : mk, p.v_rows ? mv_rows : mv, p, s.d_qk, s.d_v, thin_blocks, stream);
     if (err != cudaSuccess) return err;
   }
   p.list = wide;
@@ -1017,7 +1062,7 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
   if (err != cudaSuccess) return err;
   count_launch();
   const int rows = pl.slot_rows > pl.thin_rows ? pl.slot_rows : pl.thin_rows;
-  const int per = kCombineThreads / (s.d_v / 4) * 2;  // rows of a block: two per group of lanes
+  const int per = kCombineThreads / (s.d_v / 4) * kMany;  // rows of a block
   cfg.gridDim = dim3((unsigned)(thin_blocks + blocks), (unsigned)((rows + per - 1) / per));
   cfg.blockDim = dim3(kCombineThreads);
   cfg.dynamicSmemBytes = 0;

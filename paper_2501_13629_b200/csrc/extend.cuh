@@ -19,6 +19,7 @@ constexpr int kMaxBlocks = 256;
 struct ExtendMeta {  // an item that is cut, left by the block that has its first tile
   int valid, row_lo, rows, head0, cost, nt, member, part_rows;  // part_rows: rows of a head group (thin), else all
   long long lo;  // place of the item in the flat list
+  int chunks;    // (thin) 0, or the blocks from the first on that have a chunk of the item each
 };
 
 // One of the two flat lists of work, and where its cut items go.
@@ -43,7 +44,9 @@ struct ExtendParams {
   int region;          // columns of a head group of a thin sequence
   int k_parts, v_parts;  // K heads and V heads of a unit: (1, parts), (parts, 1) or (1, 1)
   int heads_per_k, heads_per_v;
-  int k_ring, v_ring;  // K and V tiles in the thin kernel's rings
+  // the thin kernel's K and V tiles: ring lengths; whether a TMA box brings whole rows, and then the groups of eight
+  // tokens from one head of a page to the next
+  int k_ring, v_ring, k_rows, v_rows, head_groups;
   int box_tok;         // tokens per TMA box of the cache maps
   float scale_log2;
   void* out;

@@ -10,10 +10,11 @@
 // exponentials each, row sums kept per thread until the end of the segment.  P^T goes to the tensor core through shared
 // memory (its B operand), 128 bytes per token, channels of V straight from their token-major tile (M-major A operand).
 //
-// The reference maximum of a column has to be one for all four warps of a softmax group (their tokens meet in one
-// accumulator): each tile's scores are compared with it, the four warps agree through one barrier whether some score
-// exceeds it by 2^8, and only then (and on a segment's first tile) the maxima are taken, lanes by shuffles that halve the
-// columns in every step, warps through shared memory.
+// The reference of a column (what its scores are taken from before the exponential) has to be one for all four warps of
+// a softmax group, whose tokens meet in one accumulator.  It starts as the score of the segment's first token, which
+// needs no search, and is raised to a tile's maximum when some score exceeds it by 2^24; the warps agree on that
+// through one hardware barrier per tile.  Weights of up to 2^24 are harmless: bf16 and fp32 have the range, the
+// relative precision of either does not depend on the magnitude, and the quotient takes the factor out again.
 //
 // Work: one flat list of (sequence, unit of heads, 128-token tile), divided evenly over one persistent block per SM, whose
 // two softmax groups take alternate tiles and are joined at the end of a segment; cut items leave partial rows as in
@@ -31,6 +32,7 @@ namespace {
 
 constexpr int kSoftmaxWarp0 = 2, kGroupWarps = 8;
 constexpr int kHalfCols = kThinCols / 2;
+constexpr float kThinThreshold = 24.f;  // log2 domain
 constexpr int kQRegion = 4 * 16384;  // two Q buffers and two P^T buffers of 16 KB
 
 struct ThinSegment {
@@ -134,38 +136,78 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     load_rows(p, b, lo, n, past);
     return n > 0 && n <= p.thin_max ? (past + n + kKT - 1) / kKT : 0;
   };
-  long long* scan = reinterpret_cast<long long*>(&sc.part[0][0][0]);
+  long long* scan = reinterpret_cast<long long*>(&sc.part[0][0][0]);  // tiles, then chunks, of every warp's sequences
+  int* scan_items = reinterpret_cast<int*>(scan + kExtendThinThreads / 32);
   const int per_thread = (p.batch + kExtendThinThreads - 1) / kExtendThinThreads;
   const int b_lo = min(tid * per_thread, p.batch), b_hi = min(b_lo + per_thread, p.batch);
   long long mine = 0;
+  int items = 0;
   for (int b = b_lo; b < b_hi; ++b) {
     int lo, n, past;
-    mine += (long long)p.n_units * load(b, lo, n, past);
+    const int nt = load(b, lo, n, past);
+    mine += (long long)p.n_units * nt;
+    items += nt > 0 ? p.n_units : 0;
   }
-  long long incl = mine;
+  auto warp_scan = [&](long long x) -> long long {  // inclusive
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += y;
-  }
-  if (lane == 31) scan[warp] = incl;
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    return x;
+  };
+  long long incl = warp_scan(mine);
+  items = __reduce_add_sync(0xffffffffu, items);
+  if (lane == 31) { scan[warp] = incl; scan_items[warp] = items; }
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
   const uint32_t tmem = sc.tmem;
   long long before = 0, total = 0;
+  items = 0;
 #pragma unroll
   for (int w = 0; w < kExtendThinThreads / 32; ++w) {
     if (w < warp) before += scan[w];
     total += scan[w];
+    items += scan_items[w];
   }
-  const long long w0 = share_start(total, blockIdx.x, gridDim.x), w1 = share_start(total, blockIdx.x + 1, gridDim.x);
+  // Equal shares of the list, cut wherever they end; or, where that costs no block more than four tiles, equal chunks
+  // that begin with their item: sum ceil(nt / chunk) <= total / chunk + items <= blocks, so every block has one
+  // segment at most.  (A segment costs about as much as five tiles next to its tiles, and short lists would give most
+  // blocks two: 8 x ~700 tokens, 32/4/16 heads of 64, 31 -> 22 us.)
+  int chunk = 0;
+  if (items < (int)gridDim.x && total < (1ll << 22)) {
+    chunk = (int)(((uint32_t)total + gridDim.x - items - 1) / (gridDim.x - items));
+    if (chunk > (int)((uint32_t)total / gridDim.x) + 4) chunk = 0;
+  }
+  long long w0 = share_start(total, blockIdx.x, gridDim.x), w1 = share_start(total, blockIdx.x + 1, gridDim.x);
+  if (chunk > 0) {
+    __syncthreads();  // everybody has read the sums
+    mine = 0;
+    for (int b = b_lo; b < b_hi; ++b) {
+      int lo, n, past;
+      mine += (long long)p.n_units * ((load(b, lo, n, past) + chunk - 1) / chunk);
+    }
+    incl = warp_scan(mine);
+    if (lane == 31) scan[warp] = incl;
+    __syncthreads();
+    before = 0;
+    long long chunks = 0;
+#pragma unroll
+    for (int w = 0; w < kExtendThinThreads / 32; ++w) {
+      if (w < warp) before += scan[w];
+      chunks += scan[w];
+    }
+    w0 = blockIdx.x;
+    w1 = w0 < chunks ? w0 + 1 : w0;
+  }
   {
     long long at = before + incl - mine;
     if (w0 < w1 && at <= w0 && w0 < at + mine)
       for (int b = b_lo; b < b_hi; ++b) {
         int lo, n, past;
-        const long long c = (long long)p.n_units * load(b, lo, n, past);
+        const int nt = load(b, lo, n, past);
+        const long long c = (long long)p.n_units * (chunk > 0 ? (nt + chunk - 1) / chunk : nt);
         if (w0 < at + c) {
           sc.seek_b = b;
           sc.seek_lo = at;
@@ -182,7 +224,6 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     const int boxes_part = kKT / p.box_tok;
     const int my_part = lane / kHalvesMax, my_half = lane % kHalvesMax;
     const bool has_box = lane < kHalvesMax * boxes_part;
-    const uint32_t my_off = my_half * (kKT * 128) + my_part * (p.box_tok * 128);
     const uint32_t ring = ptx::smem_u32(ring_s), q_u32 = ptx::smem_u32(q_s);
     int ks = 0, vs = 0, k_count = 0, v_count = 0, segs = 0;  // ring places and tiles requested so far
     uint32_t kph = 0, vph = 0;
@@ -203,8 +244,16 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     if (w0 < w1) {
       nt = load(b, lo, n, past);
       const long long in = w0 - item_lo;
-      u = in < (1ll << 31) ? (int)((uint32_t)in / (uint32_t)nt) : (int)(in / nt);
-      item_lo += (long long)u * nt;
+      if (chunk > 0) {  // chunk `in` of the sequence: a range of one item, counted from the item's start
+        const int per = (nt + chunk - 1) / chunk;
+        u = (int)in / per;
+        w0 = ((int)in - u * per) * chunk;
+        w1 = w0 + chunk < nt ? w0 + chunk : nt;
+        item_lo = 0;
+      } else {
+        u = in < (1ll << 31) ? (int)((uint32_t)in / (uint32_t)nt) : (int)(in / nt);
+        item_lo += (long long)u * nt;
+      }
     } else {
       b = p.batch;
     }
@@ -217,7 +266,7 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       if (ta == 0 && tb < nt) {
         cut = true;
         m.valid = 1; m.row_lo = lo; m.rows = p.parts * n * p.G; m.part_rows = n * p.G; m.head0 = head0;
-        m.cost = 1; m.nt = nt; m.member = 0; m.lo = item_lo;
+        m.cost = 1; m.nt = nt; m.member = 0; m.lo = item_lo; m.chunks = chunk > 0 ? (nt + chunk - 1) / chunk : 0;
       }
       if (!hand_out({lo, n, past, head0, ta, tb, v_count, (ta == 0 ? kSegFirst : 0) | (ta == 0 && tb == nt ? kSegWhole : 0)})) {
         ok = false;
@@ -234,20 +283,26 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         const int tok = tile * kKT;
         const int parts_valid = min(boxes_part, (kv_len - tok + p.box_tok - 1) / p.box_tok);
         const int halves = is_k ? kHalvesK : kHalves, count = is_k ? p.k_parts : p.v_parts, head = is_k ? hk0 : hv0;
-        const bool here = has_box && my_part < parts_valid && my_half < halves;
+        const bool whole_rows = is_k ? p.k_rows : p.v_rows;  // a box brings all channels of its tokens
+        const bool here = has_box && my_part < parts_valid && my_half < (whole_rows ? 1 : halves);
         if (here && (page < 0 || page >= p.num_blocks)) {  // never read outside the pool: flag it, read block 0 instead
           report(p.dev_status, DIFFQKV_ERR_INDEX);
           page = 0;
         }
         const int first = tok + my_part * p.box_tok;
         const int slot_tok = p.page_table ? first % p.page_size : first;
+        const uint32_t off = whole_rows ? my_part * (p.box_tok * 256) : my_half * (kKT * 128) + my_part * (p.box_tok * 128);
+        const CUtensorMap* map = is_k ? &tmap_k : &tmap_v;
         for (int x = 0; x < count; ++x) {
           const int slot = is_k ? ks : p.k_ring + vs;
           if (!wait_warp(empty0 + 8 * slot, (is_k ? kph : vph) ^ 1, abort_flag)) { ok = false; return; }
           const uint32_t bar = full0 + 8 * slot;
           if (lane == 0) ptx::mbar_arrive_expect_tx(bar, (uint32_t)(parts_valid * p.box_tok * halves) * 128u);
           __syncwarp();
-          if (here) ptx::tma_load_5d(ring + slot * kSlotBytes + my_off, is_k ? &tmap_k : &tmap_v, bar, 0, slot_tok, my_half, head + x, page);
+          if (here) {
+            if (whole_rows) ptx::tma_load_5d(ring + slot * kSlotBytes + off, map, bar, 0, 0, 0, (head + x) * p.head_groups + slot_tok / 8, page);
+            else ptx::tma_load_5d(ring + slot * kSlotBytes + off, map, bar, 0, slot_tok, my_half, head + x, page);
+          }
           if (is_k) {
             ++k_count;
             if (++ks == p.k_ring) { ks = 0; kph ^= 1; }
@@ -315,7 +370,11 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       // tile twice: lanes 0 .. 63 of the accumulator belong to even heads, 64 .. 127 to odd ones or to nobody.  A
       // product of 128 x N x 16 takes about 100 cycles whatever N is (its A operand comes from shared memory).
       const int v_step = kHalves == 1 && p.v_parts % 2 == 0 ? 2 : 1;
-      const uint32_t v_lo = tc::smem_desc_lo(ptx::smem_u32(ring_s), kHalves == 2 || v_step == 2 ? kKT * 128 : 0);
+      // A tile is [half][128 tokens][128 B], or, where boxes bring whole rows, [16 groups of 8 tokens][half][8][128 B].
+      const uint32_t v_lo = tc::smem_desc_lo(ptx::smem_u32(ring_s), p.v_rows ? 1024 : kHalves == 2 || v_step == 2 ? kKT * 128 : 0);
+      const uint32_t k_hi = tc::smem_desc_hi_sw128(p.k_rows ? 2048 : 1024), v_hi = tc::smem_desc_hi_sw128(p.v_rows ? 2048 : 1024);
+      const uint32_t k_half = (p.k_rows ? 1024 : kKT * 128) >> 4;  // from the first 64 channels of K to the others
+      const uint32_t v_16 = (p.v_rows ? 4096 : 2048) >> 4;         // 16 tokens of V
       const uint32_t p_lo = tc::smem_desc_lo(ptx::smem_u32(p_s), 16);
       bool ok = true;
       int ks = 0, vs = 0, segs = 0;  // ring slots of the next K tile to score and the next V tile to use
@@ -344,10 +403,10 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
               tc::fence_after_sync();
               const uint32_t ka = r_lo + ks * (kSlotBytes >> 4);
               const uint32_t qa = q_lo + ((qb * 16384 + x * p.region * 128) >> 4);
-              tc::mma_ss_halves<false>(d + x * p.region, ka, hi, qa, hi, id_s);
+              tc::mma_ss_halves<false>(d + x * p.region, ka, k_hi, qa, hi, id_s);
 #pragma unroll
               for (int k = 1; k < kDQK / 16; ++k)
-                tc::mma_ss_halves<true>(d + x * p.region, ka + (((k / 4) * (kKT * 128) + (k % 4) * 32) >> 4), hi,
+                tc::mma_ss_halves<true>(d + x * p.region, ka + (k / 4) * k_half + (((k % 4) * 32) >> 4), k_hi,
                                         qa + (((k / 4) * (kThinCols * 128) + (k % 4) * 32) >> 4), hi, id_s);
               tc::commit(empty0 + 8 * ks);
               step(ks, kph, 1, p.k_ring);
@@ -372,9 +431,9 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
             const uint32_t va = v_lo + (p.k_ring + vs) * (kSlotBytes >> 4);
             const uint32_t pa = p_lo + ((t * 16384 + x * p.region * 2) >> 4);
 #pragma unroll
-            for (int k = 0; k < kKT / 16; ++k) {  // 16 tokens: 2048 bytes of V and of P^T
-              if (k == 0 && i < 2) tc::mma_ss_halves<false>(d + x * p.region, va, hi, pa, hi, id_o);
-              else tc::mma_ss_halves<true>(d + x * p.region, va + ((k * 2048) >> 4), hi, pa + ((k * 2048) >> 4), hi, id_o);
+            for (int k = 0; k < kKT / 16; ++k) {  // 16 tokens at a time: 2048 bytes of P^T
+              if (k == 0 && i < 2) tc::mma_ss_halves<false>(d + x * p.region, va, v_hi, pa, hi, id_o);
+              else tc::mma_ss_halves<true>(d + x * p.region, va + k * v_16, v_hi, pa + ((k * 2048) >> 4), hi, id_o);
             }
             for (int y = 0; y < v_step; ++y) tc::commit(empty0 + 8 * (p.k_ring + vs + y));
             step(vs, vph, v_step, p.v_ring);
@@ -446,7 +505,8 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
               ok = ok && ptx::mbar_wait(full0 + 8 * slot, (at / p.v_ring) & 1, abort_flag);
 #pragma unroll
               for (int h = 0; h < kHalves; ++h) {
-                uint4* dst = reinterpret_cast<uint4*>(ring_s + slot * kSlotBytes + h * (kKT * 128) + r * 128);
+                uint4* dst = reinterpret_cast<uint4*>(ring_s + slot * kSlotBytes +
+                                                      (p.v_rows ? (r / 8) * 2048 + h * 1024 + (r % 8) * 128 : h * (kKT * 128) + r * 128));
 #pragma unroll
                 for (int e = 0; e < 8; ++e) dst[e] = make_uint4(0, 0, 0, 0);
               }
@@ -458,25 +518,33 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
           for (int c = 0; c < kHalfCols; ++c)
             if (((c0 + c) & (p.region - 1)) < hidden) x[c] = -INFINITY;
         }
-        // ---- scores on the scale of base 2, from the reference; does some score exceed it by 2^8?
-        bool over = !ok || !later;
-        if (later) {
-#pragma unroll
-          for (int q = 0; q < kHalfCols / 8; ++q)
-            if (mask >> q & 1) {
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const int c = q * 8 + e;
-                x[c] = fmaf(x[c], p.scale_log2, -m[c]);
-                over |= x[c] > kRescaleThreshold && ((c0 + c) & (p.region - 1)) < used;
-              }
-            }
-        } else {
+        // ---- scores on the scale of base 2, from the reference: the score of the segment's first token of this group to
+        // begin with (a row that does not see it sees none of the tile: reference 0, weights 0)
+        if (!later) {
 #pragma unroll
           for (int c = 0; c < kHalfCols; ++c) x[c] *= p.scale_log2;
+          if (quarter == 0 && lane == 0) {
+#pragma unroll
+            for (int c = 0; c < kHalfCols; c += 4)
+              *reinterpret_cast<float4*>(m + c) = make_float4(x[c] == -INFINITY ? 0.f : x[c], x[c + 1] == -INFINITY ? 0.f : x[c + 1],
+                                                              x[c + 2] == -INFINITY ? 0.f : x[c + 2], x[c + 3] == -INFINITY ? 0.f : x[c + 3]);
+          }
+          group_sync(bar_id);
         }
+        bool over = !ok;
+        const float f = later ? p.scale_log2 : 1.f;
+#pragma unroll
+        for (int q = 0; q < kHalfCols / 8; ++q)
+          if (mask >> q & 1) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int c = q * 8 + e;
+              x[c] = fmaf(x[c], f, -m[c]);
+              over |= x[c] > kThinThreshold && ((c0 + c) & (p.region - 1)) < used;
+            }
+          }
         if (group_any(bar_id, over)) {
-          // ---- largest score of every column in this tile; the reference goes up where it is passed by 2^8
+          // ---- largest score of every column in this tile; the reference goes up where it is passed
           float y[kHalfCols / 2];  // over the lanes, half of the columns in every step; lane c ends with column c
 #pragma unroll
           for (int c = 0; c < 16; ++c) {
@@ -497,11 +565,9 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
           if (group_any(bar_id, !ok)) { ok = false; break; }
           if (wq == 0) {  // a lane per column
             float up = fmaxf(fmaxf(top, sc.part[t][1][c0 + lane]), fmaxf(sc.part[t][2][c0 + lane], sc.part[t][3][c0 + lane]));
-            // x is relative to the reference; a row that sees no token yet keeps the reference 0 (weights 0)
-            if (later) up = up > kRescaleThreshold ? up : 0.f;
-            else if (up == -INFINITY) up = 0.f;
+            up = up > kThinThreshold ? up : 0.f;  // x is relative to the reference
             sc.part[t][0][c0 + lane] = up;
-            m[lane] = later ? m[lane] + up : up;
+            m[lane] += up;
           }
           group_sync(bar_id);
           const float* rise = &sc.part[t][0][c0];
@@ -527,7 +593,7 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
             if (later) tc::st_32x32b_x8(o_taddr + t * kThinCols + q * 8, o);
           }
           if (later) tc::wait_st();
-        } else {  // the last product of this group has read its P^T
+        } else if (later) {  // the last product of this group has read its P^T
           ok = wait_warp(o_done0 + 8 * t, par ^ 1, abort_flag) && ok;
         }
         // ---- P^T = 2^x as packed bf16, one row of 128 bytes per token, 16-byte chunks exclusive-ored with the row

@@ -312,11 +312,7 @@ def test_captured_upkeep(api):
     dev = Device(api, host)
     dev.reserve([20, 40, 0, 0])
     gone, parents, children, cu = ints([2, 3]), ints([0, 1]), ints([2, 3]), ints([0, 1, 2, 3, 4])
-    pages = api._pages(dev.cache, dev.refs)
-    import ctypes as C
-    ws = [torch.empty(max(256, n), dtype=torch.uint8, device="cuda") for n in
-          (api._lib.diffqkv_pages_fork_workspace_bytes(C.byref(pages), 2),
-           api._lib.diffqkv_pages_reserve_workspace_bytes(C.byref(pages)))]
+    ws = [torch.empty(1 << 16, dtype=torch.uint8, device="cuda") for _ in range(2)]
 
     def step():
         api.diffqkv_pages_free(gone, dev.cache, dev.refs)
