@@ -43,7 +43,10 @@ constexpr int kExtendThreads = 384;
 constexpr int kSoftmaxWarp0 = 4;
 // Shared memory: two Q tiles, the rings of K and V tiles, the exchange of the two softmax groups, barriers.
 constexpr int kExtendSmem = 1024 + 2 * (kRows * kDMax * 2) + kRingBytes + 1024 + 320;
-constexpr int kWideCost = 2, kNarrowCost = 1;  // of a K/V tile, in the division of the work
+// In the division of the work: a K/V tile of a wide and of a narrow item, and what an item costs next to its tiles (its
+// rows are written out and the pipeline fills again).  Measured on prompts of 1.5k-2k rows over 1k-5k tokens: 2.35 us a
+// tile, 5.8 us an item; without the last, blocks with many short items ended 13 % late.
+constexpr int kWideCost = 2, kNarrowCost = 1, kItemCost = 5;
 
 // A segment as the producer hands it to the other roles, through a ring in shared memory.
 struct Segment {
@@ -57,8 +60,10 @@ struct Segment {
 constexpr int kSegRing = 4;
 constexpr int kSegEnd = 1, kSegWide = 2, kSegWhole = 4, kSegFirst = 8;  // first: holds the item's first tile
 
-// sum of floor((a x + b) / m) for x = 0 .. n - 1, all arguments >= 0, m > 0: the Euclid-like recursion on (m, a).
-__device__ long long floor_sum(long long n, long long m, long long a, long long b) {
+// sum of floor((a x + b) / m) for x = 0 .. n - 1 with a, b >= 0, m > 0: the Euclid-like recursion on (m, a).  Not inlined:
+// the code that a block runs once at its start is fetched from the second-level cache line by line, which is what it
+// costs (with every quotient inlined a block began its first loads 16 us after its start).
+__device__ __noinline__ long long floor_sum(long long n, long long m, long long a, long long b) {
   long long ans = 0;
   while (n > 0) {
     if (a >= m) { ans += (n - 1) * n / 2 * (a / m); a %= m; }
@@ -71,7 +76,17 @@ __device__ long long floor_sum(long long n, long long m, long long a, long long 
   }
   return ans;
 }
-
+// The same with m = 128 and a = 2^s: for a >= 128 every term is floor(b / 128) + x a / 128, else with r = 128 / a terms in
+// a turn and e = floor(b / a) the sum of floor((e + x) / r), a difference of sums from 0.
+__device__ __forceinline__ long long floor_sum_128(int n, int s, int b) {
+  if (s >= 7) return (long long)n * (b >> 7) + (((long long)n * (n - 1) / 2) << (s - 7));
+  const int h = 7 - s, e = b >> s;
+  auto upto = [&](int t) -> long long {  // sum of y >> h for y < t
+    const int q = t >> h;
+    return ((long long)q * (q - 1) / 2 << h) + (long long)q * (t - (q << h));
+  };
+  return upto(e + n) - upto(e);
+}
 // One sequence of the step.
 struct Seq {
   int lo, n, past, items;  // first row, rows (0: not in this list), tokens cached before, items per head group
@@ -83,7 +98,9 @@ struct Seq {
   }
   // cost of the first i items, i < items
   __device__ long long cost_before(const ExtendParams& p, int i) const {
-    return kWideCost * floor_sum(i, kKT, 2 * p.T, (long long)past + 2 * p.T + kKT - 1);
+    const int b = past + 2 * p.T + kKT - 1;
+    const long long tiles = p.t_log2 >= 0 ? floor_sum_128(i, p.t_log2 + 1, b) : floor_sum(i, kKT, 2 * p.T, b);
+    return kWideCost * tiles + (long long)kItemCost * i;
   }
   __device__ bool wide(const ExtendParams& p, int i) const { return n - i * 2 * p.T > p.T; }
   __device__ int tiles(const ExtendParams& p, int i) const {  // K/V tiles of item i
@@ -91,7 +108,7 @@ struct Seq {
   }
   __device__ long long cost(const ExtendParams& p) const {  // of one head group
     if (n == 0) return 0;
-    return cost_before(p, items - 1) + (wide(p, items - 1) ? kWideCost : kNarrowCost) * (long long)tiles(p, items - 1);
+    return cost_before(p, items - 1) + kItemCost + (wide(p, items - 1) ? kWideCost : kNarrowCost) * (long long)tiles(p, items - 1);
   }
 };
 
@@ -111,7 +128,7 @@ struct Walk {
     if (w0 >= w1) { item_lo = w1; b = p.batch; return; }
     seq.load(p, b);
     const long long per = seq.cost(p);
-    u = (int)((w0 - lo) / per);
+    u = (int)quotient(w0 - lo, per);
     const long long r = (w0 - lo) - u * per;
     int a = 0, z = seq.items;  // largest item whose start is not behind r
     while (z - a > 1) {
@@ -126,9 +143,8 @@ struct Walk {
       wide = seq.wide(p, item);
       nt = seq.tiles(p, item);
       const int cost = wide ? kWideCost : kNarrowCost;
-      const long long size = (long long)cost * nt;
-      ta = item_lo >= begin ? 0 : (int)((begin - item_lo + cost - 1) / cost);
-      tb = end - item_lo >= size ? nt : (int)((end - item_lo + cost - 1) / cost);
+      ta = item_tile(begin - item_lo, cost, nt, kItemCost);
+      tb = item_tile(end - item_lo, cost, nt, kItemCost);
       if (ta < tb) {
         if (wide) {
           const int nt0 = (seq.past + item * 2 * p.T + p.T + kKT - 1) / kKT;  // tiles that the first row tile sees
@@ -143,7 +159,7 @@ struct Walk {
     return false;
   }
   __device__ void advance(const ExtendParams& p) {
-    item_lo += (long long)(seq.wide(p, item) ? kWideCost : kNarrowCost) * seq.tiles(p, item);
+    item_lo += kItemCost + (long long)(seq.wide(p, item) ? kWideCost : kNarrowCost) * seq.tiles(p, item);
     if (++item < seq.items) return;
     item = 0;
     if (++u < p.n_units) return;
@@ -155,6 +171,28 @@ struct Walk {
   }
   __device__ int tok0(const ExtendParams& p) const { return item * 2 * p.T; }
 };
+
+// The 4 x 4 matrix of 16-byte pieces that four neighbouring lanes hold, a row each, transposed: piece y of a lane becomes
+// its own piece of lane y.
+__device__ __forceinline__ void transpose4(uint4 (&v)[4], int lane) {
+  auto swap = [](uint4& a, uint4& b, bool yes) {
+    const uint4 x = a;
+    a = yes ? b : a;
+    b = yes ? x : b;
+  };
+  auto pass = [](uint4& a, int by) {
+    a.x = __shfl_xor_sync(0xffffffffu, a.x, by);
+    a.y = __shfl_xor_sync(0xffffffffu, a.y, by);
+    a.z = __shfl_xor_sync(0xffffffffu, a.z, by);
+    a.w = __shfl_xor_sync(0xffffffffu, a.w, by);
+  };
+  swap(v[0], v[1], lane & 1); swap(v[2], v[3], lane & 1);
+  pass(v[1], 1); pass(v[3], 1);
+  swap(v[0], v[1], lane & 1); swap(v[2], v[3], lane & 1);
+  swap(v[0], v[2], lane & 2); swap(v[1], v[3], lane & 2);
+  pass(v[2], 2); pass(v[3], 2);
+  swap(v[0], v[2], lane & 2); swap(v[1], v[3], lane & 2);
+}
 
 template <int kDQK, int kD>  // channels per head of Q/K and of V: (128, 128), (64, 64) or (64, 128)
 __global__ void __launch_bounds__(kExtendThreads, 1)
@@ -191,6 +229,9 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   __shared__ int seek_b_s;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  // The kernel for thin sequences works on other rows; whichever of the two comes second may take the SMs that the
+  // first one's blocks leave.  The joining kernel depends on the second alone, which therefore ends behind the first.
+  if (p.first) ptx::grid_launch_dependents();
   {  // a step of thin sequences alone (decode): nothing to do here
     bool any = false;
     for (int b = tid; b < p.batch; b += kExtendThreads) {
@@ -199,10 +240,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       any |= s.n > 0 || s.bad;
     }
     if (!__syncthreads_or(any)) {
-      if (tid == 0) {
-        p.list.meta[blockIdx.x].valid = 0;
-        if (blockIdx.x == 0) *p.list.total = 0;
-      }
+      if (tid == 0) p.list.meta[blockIdx.x].rows = 0;
       ptx::grid_dependency_wait();
       return;
     }
@@ -272,7 +310,12 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     total += scan_s[w + 1];
   }
   const int team = (int)blockIdx.x / p.list.team, member = (int)blockIdx.x - team * p.list.team;
-  const long long w0 = share_start(total, team, p.list.n_teams), w1 = share_start(total, team + 1, p.list.n_teams);
+  const int n_teams = shares(total, p.list.n_teams, kItemCost + kWideCost);  // that take part
+  long long w0 = total, w1 = total;
+  if (team < n_teams) {
+    w0 = share_start(total, team, n_teams);
+    w1 = share_start(total, team + 1, n_teams);
+  }
   {
     long long at = before + incl - mine;
     if (w0 < w1 && at <= w0 && w0 < at + mine)
@@ -288,7 +331,6 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         at += c;
       }
   }
-  if (blockIdx.x == 0 && tid == 0) *p.list.total = total;
   __syncthreads();
   const uint32_t q_u32 = ptx::smem_u32(q_s), k_u32 = ptx::smem_u32(k_s), v_u32 = ptx::smem_u32(v_s);
 
@@ -303,7 +345,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     const int my_part = lane / kHalvesMax, my_half = lane % kHalvesMax;
     const uint32_t my_off = my_half * (kKT * 128) + my_part * (p.box_tok * 128);
     int kc = 0, vc = 0, segs = 0;  // K tiles, V tiles, Q loads requested so far
-    bool ok = true, cut = false;
+    bool ok = true;
     ExtendMeta m = {};
     Walk w;
     w.start(p, w0, w1, seek_b_s, seek_lo_s);
@@ -324,9 +366,9 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       const int hk = head0 / p.heads_per_k, hv = head0 / p.heads_per_v;  // Eq. (idx)
       const int tok0 = w.tok0(p);
       if (w.ta == 0 && w.tb < w.nt) {
-        cut = true;
-        m.valid = 1; m.row_lo = w.seq.lo + tok0; m.rows = min(w.seq.n - tok0, 2 * p.T) * p.G; m.part_rows = m.rows; m.head0 = head0;
-        m.cost = w.wide ? kWideCost : kNarrowCost; m.nt = w.nt; m.member = member; m.lo = w.item_lo;
+        m.rows = m.part_rows = min(w.seq.n - tok0, 2 * p.T) * p.G; m.row_lo = w.seq.lo + tok0; m.head0 = head0;
+        m.member = member;
+        m.parts = share_of(w.item_lo + last_tile(w.wide ? kWideCost : kNarrowCost, w.nt, kItemCost), total, n_teams) - team + 1;
       }
       if (!hand_out({w.seq.lo, w.seq.n, w.seq.past, tok0, head0, w.ta, w.tb, w.nst0, vc,
                      (w.wide ? kSegWide : 0) | (w.ta == 0 ? kSegFirst : 0) |
@@ -402,11 +444,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       if (!ok) break;
     }
     if (ok) ok = hand_out({0, 0, 0, 0, 0, 0, 0, 0, 0, kSegEnd});
-    if (lane == 0) {
-      if (!cut) m.valid = 0;
-      p.list.meta[blockIdx.x] = m;
-    }
-    ptx::grid_launch_dependents();
+    if (lane == 0) p.list.meta[blockIdx.x] = m;
     if (!ok) {
       report(p.dev_status, DIFFQKV_ERR_TIMEOUT);
       // give copies in flight a bounded chance to land before the block's shared memory is released (a Q request is
@@ -701,13 +739,24 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       if (busy) {
         const bool store = r < rows_of(w);
         const bool whole = w.flags & kSegWhole;
-        const int row_tok = r / p.G;
-        const long long row = (long long)(w.row_lo + tok0_of(w) + row_tok) * p.n_q + w.head0 + (r - row_tok * p.G);
-        const long long prow = (2LL * blockIdx.x + ((w.flags & kSegFirst) ? 1 : 0)) * p.list.slot_rows + (wide ? t * p.T * p.G : 0) + r;
-        const bool as_f32 = !whole || p.out_is_f32;
-        float* dst32 = whole ? reinterpret_cast<float*>(p.out) + row * kD : p.list.part_o + prow * kD;
-        __nv_bfloat16* dst16 = reinterpret_cast<__nv_bfloat16*>(p.out) + row * kD;
+        auto out_row = [&](int y) -> long long {  // row y of this tile in q and out
+          const int tok = y / p.G;
+          return (long long)(w.row_lo + tok0_of(w) + tok) * p.n_q + w.head0 + (y - tok * p.G);
+        };
+        const long long row = out_row(r);
+        const long long prow0 = (2LL * blockIdx.x + ((w.flags & kSegFirst) ? 1 : 0)) * p.list.slot_rows + (wide ? t * p.T * p.G : 0);
+        const long long prow = prow0 + r;
         if (n > 0) {
+          // Four lanes exchange their rows' 16-byte pieces, so that a store covers 64 consecutive bytes of eight rows and
+          // not 16 of 32 (which took 4 of the 7 thousand cycles between an item's last product and the next one's).
+          const int r4 = quarter * 32 + (lane & ~3), piece = lane & 3;
+          long long at[4];
+#pragma unroll
+          for (int y = 0; y < 4; ++y) at[y] = (whole ? out_row(r4 + y) : prow0 + r4 + y) * kD;
+          const int rows = rows_of(w);
+          const bool as_f32 = !whole || p.out_is_f32;
+          float* dst32 = whole ? reinterpret_cast<float*>(p.out) : p.list.part_o;
+          __nv_bfloat16* dst16 = reinterpret_cast<__nv_bfloat16*>(p.out);
 #pragma unroll 1
           for (int x = 0; x < kD / 32; ++x) {
             uint32_t o[32], o1[32];
@@ -720,21 +769,34 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
               if (join) y = fmaf(__uint_as_float(o1[e]), weight1, y);
               o[e] = __float_as_uint(y);
             }
-            if (!store) continue;
             if (as_f32) {
-              uint4* dst = reinterpret_cast<uint4*>(dst32 + x * 32);
 #pragma unroll
-              for (int e = 0; e < 8; ++e) dst[e] = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+              for (int h = 0; h < 2; ++h) {
+                uint4 v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const int z = h * 16 + e * 4;
+                  v[e] = make_uint4(o[z], o[z + 1], o[z + 2], o[z + 3]);
+                }
+                transpose4(v, lane);
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                  if (r4 + y < rows) *reinterpret_cast<uint4*>(dst32 + at[y] + x * 32 + h * 16 + piece * 4) = v[y];
+              }
             } else {
-              uint4* dst = reinterpret_cast<uint4*>(dst16 + x * 32);
+              uint4 v[4];
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
                 uint32_t y[4];
 #pragma unroll
                 for (int z = 0; z < 4; ++z)
                   y[z] = pack2(__uint_as_float(o[8 * e + 2 * z]), __uint_as_float(o[8 * e + 2 * z + 1]));
-                dst[e] = make_uint4(y[0], y[1], y[2], y[3]);
+                v[e] = make_uint4(y[0], y[1], y[2], y[3]);
               }
+              transpose4(v, lane);
+#pragma unroll
+              for (int y = 0; y < 4; ++y)
+                if (r4 + y < rows) *reinterpret_cast<uint4*>(dst16 + at[y] + x * 32 + piece * 8) = v[y];
             }
           }
         }
@@ -763,103 +825,125 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     tc::fence_after_sync();
     tc::tmem_dealloc(tmem_base, kTmemCols);
   }
-  // The kernel for thin sequences was launched before this one and runs beside it; the joining kernel, which depends on
-  // this one alone, may only follow when both are over.
   ptx::grid_dependency_wait();
 }
 
-// Joins the partial rows of the items that were cut: blocks x = 0 .. take the items that the blocks of the first kernel
-// began, then those of the second's; the rows of an item are dealt to gridDim.y blocks, and there to groups of kD / 4
-// lanes with four channels each.
-constexpr int kCombineThreads = 256, kMany = 4;
+// Joins the partial rows of the items that were cut, left by the blocks of both kernels: all rows of all such items in one
+// list, dealt to the groups of kD / 4 lanes (four channels each) of as many blocks as are resident at once.  Bound by the
+// latency of its few dependent loads: a group takes up to four rows of an item, two at a time with four parts
+// each in flight.
+constexpr int kCombineThreads = 256, kCombineBlocks = 3;  // per SM
 
 template <int kD>
-__global__ void __launch_bounds__(kCombineThreads) extend_combine_kernel(const ExtendParams p, const ExtendList thin,
-                                                                       const int thin_blocks) {
-  constexpr int kLanes = kD / 4, kGroups = kCombineThreads / kLanes;
-  __shared__ int slots[kMaxBlocks];
-  __shared__ int count_s;
-  const bool first_list = (int)blockIdx.x < thin_blocks;
-  const ExtendList& list = first_list ? thin : p.list;
-  const int block = first_list ? blockIdx.x : blockIdx.x - thin_blocks;
-  const int first = block / list.team;
-  if (threadIdx.x == 0) count_s = 0;
+__global__ void __launch_bounds__(kCombineThreads, kCombineBlocks)
+extend_combine_kernel(const ExtendParams p, const ExtendList thin, const int thin_blocks, const int wide_blocks) {
+  constexpr int kLanes = kD / 4, kGroups = kCombineThreads / kLanes, kItems = 2 * kMaxBlocks;
+  constexpr int kPerLane = kItems / 32;
+  __shared__ int start_s[kItems + 1];  // bundles of rows in the items before this one
+  __shared__ int bundle_s;
+  const int lane = threadIdx.x % kLanes;
   ptx::grid_dependency_wait();
-  const ExtendMeta m = list.meta[block];
-  if (!m.valid || (int)blockIdx.y * kGroups >= m.rows) return;
-  const long long total = *list.total;
+  const int items = thin_blocks + wide_blocks;
+  auto meta_of = [&](int x) { return x < thin_blocks ? thin.meta + x : p.list.meta + (x - thin_blocks); };
+  for (int x = threadIdx.x; x < kItems; x += kCombineThreads) {
+    const ExtendMeta* m = meta_of(x);
+    start_s[x + 1] = x < items ? m->rows : 0;
+  }
   __syncthreads();
-  // the teams that own tiles of the item, from the first on (in order: sums do not depend on timing)
-  if (m.chunks > 0) {
-    if ((int)threadIdx.x < m.chunks) slots[threadIdx.x] = 2 * (block + threadIdx.x) + (threadIdx.x == 0);
-    if (threadIdx.x == 0) count_s = m.chunks;
-  } else {
-    const int k = first + threadIdx.x;
-    if (k < list.n_teams) {
-      const long long a = share_start(total, k, list.n_teams), z = share_start(total, k + 1, list.n_teams);
-      int slot = -1;
-      if (a < m.lo + (long long)m.cost * m.nt) {
-        const int ta = a <= m.lo ? 0 : (int)(((uint32_t)(a - m.lo) + m.cost - 1) / (uint32_t)m.cost);
-        const int tb = z - m.lo >= (long long)m.cost * m.nt ? m.nt : (int)(((uint32_t)(z - m.lo) + m.cost - 1) / (uint32_t)m.cost);
-        if (ta < tb) slot = 2 * (k * list.team + m.member) + (ta == 0);
-        atomicMax(&count_s, k - first + 1);
-      }
-      slots[threadIdx.x] = slot;
+  if (threadIdx.x < 32) {
+    int* mine = start_s + 1 + threadIdx.x * kPerLane;
+    int sum = 0;
+    for (int i = 0; i < kPerLane; ++i) sum += mine[i];
+    // four rows a bundle where there are many (one search for all, loads in flight together), else one
+    const int bundle = (int)__reduce_add_sync(0xffffffffu, sum) > 2 * (int)gridDim.x * kGroups ? 4 : 1;
+    sum = 0;
+    for (int i = 0; i < kPerLane; ++i) sum += (mine[i] + bundle - 1) / bundle;
+    int at = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, at, o);
+      if ((int)threadIdx.x >= o) at += y;
+    }
+    at -= sum;
+    if (threadIdx.x == 0) {
+      start_s[0] = 0;
+      bundle_s = bundle;
+    }
+    for (int i = 0; i < kPerLane; ++i) {
+      at += (mine[i] + bundle - 1) / bundle;
+      mine[i] = at;
     }
   }
   __syncthreads();
-  const int n = count_s, lane = threadIdx.x % kLanes;
-  // kMany rows at a time, so that their loads are in flight together
-  for (int r0 = blockIdx.y * kGroups + threadIdx.x / kLanes; r0 < m.rows; r0 += gridDim.y * kGroups * kMany) {
-    float top[kMany], sum[kMany];
-    float4 acc[kMany];
-    const int step = gridDim.y * kGroups;
-#pragma unroll
-    for (int y = 0; y < kMany; ++y) {
-      top[y] = -INFINITY;
-      sum[y] = 0.f;
-      acc[y] = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int bundle = bundle_s;
+  const int bundles = start_s[kItems];
+  for (int g = blockIdx.x * kGroups + threadIdx.x / kLanes; g < bundles; g += gridDim.x * kGroups) {
+    int x = 0, z = kItems;  // the item: the last that begins at or before bundle g
+    while (z - x > 1) {
+      const int mid = (x + z) >> 1;
+      if (start_s[mid] <= g) x = mid; else z = mid;
     }
-    for (int i = 0; i < n; ++i) {
-      const int slot = slots[i];
-      if (slot < 0) continue;
-      const long long at = (long long)slot * list.slot_rows;
-      float ls[kMany];
-      float4 o[kMany];
+    const bool first_list = x < thin_blocks;
+    const ExtendList& list = first_list ? thin : p.list;
+    const ExtendMeta m = *meta_of(x);
+    const int block = first_list ? x : x - thin_blocks;
+    // the parts lie one team apart, the first in its block's second slot, the others in the first: in order, so that sums
+    // do not depend on timing
+    const long long slot0 = 2LL * block + 1, step = 2LL * list.team;  // part i > 0: slot0 - 1 + i step
+    const int r0 = bundle * (g - start_s[x]), last = min(r0 + bundle, m.rows) - 1;
+#pragma unroll 1
+    for (int r = r0; r <= last; r += 2) {  // two rows at a time
+      float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
+      float4 acc[2];
+      acc[0] = acc[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int i = 0; i < m.parts; i += 4) {
+        float ls[4][2];
+        float4 o[4][2];
 #pragma unroll
-      for (int y = 0; y < kMany; ++y) {
-        const int r = min(r0 + y * step, m.rows - 1);
-        ls[y] = list.part_lse[at + r];
-        o[y] = *reinterpret_cast<const float4*>(list.part_o + (at + r) * kD + lane * 4);
+        for (int y = 0; y < 4; ++y) {
+          if (i + y < m.parts) {
+            const long long at = (i + y == 0 ? slot0 : slot0 - 1 + (i + y) * step) * list.slot_rows;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const int row = min(r + h, last);
+              ls[y][h] = list.part_lse[at + row];
+              o[y][h] = *reinterpret_cast<const float4*>(list.part_o + (at + row) * kD + lane * 4);
+            }
+          } else {
+            ls[y][0] = ls[y][1] = -INFINITY;
+          }
+        }
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            if (ls[y][h] == -INFINITY) continue;  // the part saw no token of this row (and may have left no values)
+            const float up = fmaxf(top[h], ls[y][h]);
+            const float was = exp2f(top[h] - up), f = exp2f(ls[y][h] - up);
+            top[h] = up;
+            sum[h] = sum[h] * was + f;
+            acc[h].x = fmaf(f, o[y][h].x, acc[h].x * was);
+            acc[h].y = fmaf(f, o[y][h].y, acc[h].y * was);
+            acc[h].z = fmaf(f, o[y][h].z, acc[h].z * was);
+            acc[h].w = fmaf(f, o[y][h].w, acc[h].w * was);
+          }
+        }
       }
 #pragma unroll
-      for (int y = 0; y < kMany; ++y) {
-        if (ls[y] == -INFINITY) continue;  // the part saw no token of this row (and may have left no values)
-        const float up = fmaxf(top[y], ls[y]);
-        const float was = exp2f(top[y] - up), f = exp2f(ls[y] - up);
-        top[y] = up;
-        sum[y] = sum[y] * was + f;
-        acc[y].x = fmaf(f, o[y].x, acc[y].x * was);
-        acc[y].y = fmaf(f, o[y].y, acc[y].y * was);
-        acc[y].z = fmaf(f, o[y].z, acc[y].z * was);
-        acc[y].w = fmaf(f, o[y].w, acc[y].w * was);
+      for (int h = 0; h < 2; ++h) {
+        if (r + h > last) break;
+        const float inv = sum[h] > 0.f ? 1.f / sum[h] : 0.f;
+        const int part = (r + h) / m.part_rows, lr = r + h - part * m.part_rows, tok = lr / p.G;
+        const long long row = (long long)(m.row_lo + tok) * p.n_q + m.head0 + part * p.G + (lr - tok * p.G);
+        if (p.out_is_f32) {
+          *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + row * kD + lane * 4) =
+              make_float4(acc[h].x * inv, acc[h].y * inv, acc[h].z * inv, acc[h].w * inv);
+        } else {
+          *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(p.out) + row * kD + lane * 4) =
+              make_uint2(pack2(acc[h].x * inv, acc[h].y * inv), pack2(acc[h].z * inv, acc[h].w * inv));
+        }
+        if (p.lse && lane == 0) p.lse[row] = sum[h] > 0.f ? (top[h] + log2f(sum[h])) * kLn2 : -INFINITY;
       }
-    }
-#pragma unroll
-    for (int y = 0; y < kMany; ++y) {
-      const int r = r0 + y * step;
-      if (r >= m.rows) break;
-      const float inv = sum[y] > 0.f ? 1.f / sum[y] : 0.f;
-      const int g = r / m.part_rows, lr = r - g * m.part_rows, tok = lr / p.G;
-      const long long row = (long long)(m.row_lo + tok) * p.n_q + m.head0 + g * p.G + (lr - tok * p.G);
-      if (p.out_is_f32) {
-        *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + row * kD + lane * 4) =
-            make_float4(acc[y].x * inv, acc[y].y * inv, acc[y].z * inv, acc[y].w * inv);
-      } else {
-        *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(p.out) + row * kD + lane * 4) =
-            make_uint2(pack2(acc[y].x * inv, acc[y].y * inv), pack2(acc[y].z * inv, acc[y].w * inv));
-      }
-      if (p.lse && lane == 0) p.lse[row] = sum[y] > 0.f ? (top[y] + log2f(sum[y])) * kLn2 : -INFINITY;
     }
   }
 }
@@ -953,7 +1037,6 @@ size_t place(const Plan& pl, int d_v, char* base, ExtendList* wide, ExtendList* 
   ExtendList* lists[2] = {wide, thin};
   for (int i = 0; i < 2; ++i) {
     ExtendList l = {};
-    l.total = reinterpret_cast<long long*>(take(8));
     l.meta = reinterpret_cast<ExtendMeta*>(take(sizeof(ExtendMeta) * kMaxBlocks));
     l.part_lse = reinterpret_cast<float*>(take(2 * sizeof(float) * (size_t)blocks[i] * rows[i]));
     l.part_o = reinterpret_cast<float*>(take(2 * sizeof(float) * (size_t)blocks[i] * rows[i] * d_v));
@@ -1010,7 +1093,10 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
   p.cu_q = cu_q; p.seqlens = c.seqlens; p.page_table = c.page_table;
   p.page_size = c.page_size; p.max_pages_per_seq = c.max_pages_per_seq; p.num_blocks = c.num_blocks; p.max_seqlen = c.max_seqlen;
   p.batch = s.batch; p.total_q = total_q; p.n_q = s.n_q;
-  p.G = pl.G; p.T = pl.T; p.parts = pl.parts; p.n_units = pl.groups / pl.parts;
+  p.G = pl.G; p.T = pl.T; p.t_log2 = -1;
+  for (int x = 0; x <= 7; ++x)
+    if (pl.T == 1 << x) p.t_log2 = x;
+  p.parts = pl.parts; p.n_units = pl.groups / pl.parts;
   p.thin_max = pl.thin_max; p.region = pl.region;
   p.heads_per_k = s.n_q / s.n_k; p.heads_per_v = s.n_q / s.n_v;
   p.k_parts = p.heads_per_k < p.heads_per_v ? pl.parts : 1;
@@ -1029,24 +1115,13 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
   const int thin_blocks = pl.thin_max > 0 ? pl.blocks : 0, blocks = pl.n_teams * pl.parts;
 
   // Which sequences are thin is known on the device alone, so both kernels are launched; the second may start as soon as
-  // the first has, and takes the SMs that the first leaves (an SM has room for one block of either).
-  cudaError_t err;
-  if (thin_blocks > 0) {
-    CUtensorMap mk_rows, mv_rows;
-    p.list = thin;
-    p.head_groups = (int)(tok_extent / 8);
-    p.k_rows = make_row_map(&mk_rows, c.k_cache, s.d_qk, tok_extent, s.n_k, c.num_blocks, c.k_stride_tok, c.k_stride_head,
-                            c.k_stride_blk, box_tok);
-    p.v_rows = make_row_map(&mv_rows, c.v_cache, s.d_v, tok_extent, s.n_v, c.num_blocks, c.v_stride_tok, c.v_stride_head,
-                            c.v_stride_blk, box_tok);
-    err = launch_extend_thin(mq_thin, p.k_rows ? mk_rows : mk, p.v_rows ? mv_rows : mv, p, s.d_qk, s.d_v, thin_blocks, stream);
-    if (err != cudaSuccess) return err;
-  }
-  p.list = wide;
+  // the first has, and takes the SMs that the first leaves (an SM has room for one block of either).  First comes the one
+  // that has the more work if the rows are spread evenly: behind the other it starts on SMs in another order, away from
+  // its team (prompts 578 instead of 507 us), and a step of thin sequences would wait for two launches (32, not 28 us).
   using ExtendFn = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const ExtendParams);
   const ExtendFn fn = s.d_v == 64 ? extend_attn_kernel<64, 64>
                                   : (s.d_qk == 128 ? extend_attn_kernel<128, 128> : extend_attn_kernel<64, 128>);
-  err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kExtendSmem);
+  cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kExtendSmem);
   if (err != cudaSuccess) return err;
   cudaLaunchConfig_t cfg = {};
   cfg.stream = stream;
@@ -1054,21 +1129,40 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
-  cfg.gridDim = dim3((unsigned)blocks);
-  cfg.blockDim = dim3(kExtendThreads);
-  cfg.dynamicSmemBytes = kExtendSmem;
-  cfg.numAttrs = thin_blocks > 0 ? 1 : 0;
-  err = cudaLaunchKernelEx(&cfg, fn, mq, mk, mv, p);
-  if (err != cudaSuccess) return err;
-  count_launch();
-  const int rows = pl.slot_rows > pl.thin_rows ? pl.slot_rows : pl.thin_rows;
-  const int per = kCombineThreads / (s.d_v / 4) * kMany;  // rows of a block
-  cfg.gridDim = dim3((unsigned)(thin_blocks + blocks), (unsigned)((rows + per - 1) / per));
+  const bool wide_first = thin_blocks == 0 || total_q > (long long)s.batch * pl.thin_max;
+  auto launch_wide = [&]() -> cudaError_t {
+    p.list = wide;
+    p.first = wide_first;
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(kExtendThreads);
+    cfg.dynamicSmemBytes = kExtendSmem;
+    cfg.numAttrs = wide_first ? 0 : 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, fn, mq, mk, mv, p);
+    if (e == cudaSuccess) count_launch();
+    return e;
+  };
+  auto launch_thin = [&]() -> cudaError_t {
+    if (thin_blocks == 0) return cudaSuccess;
+    CUtensorMap mk_rows, mv_rows;
+    p.list = thin;
+    p.first = !wide_first;
+    p.head_groups = (int)(tok_extent / 8);
+    p.k_rows = make_row_map(&mk_rows, c.k_cache, s.d_qk, tok_extent, s.n_k, c.num_blocks, c.k_stride_tok, c.k_stride_head,
+                            c.k_stride_blk, box_tok);
+    p.v_rows = make_row_map(&mv_rows, c.v_cache, s.d_v, tok_extent, s.n_v, c.num_blocks, c.v_stride_tok, c.v_stride_head,
+                            c.v_stride_blk, box_tok);
+    return launch_extend_thin(mq_thin, p.k_rows ? mk_rows : mk, p.v_rows ? mv_rows : mv, p, s.d_qk, s.d_v, thin_blocks,
+                              wide_first, stream);
+  };
+  if ((err = wide_first ? launch_wide() : launch_thin()) != cudaSuccess) return err;
+  if ((err = wide_first ? launch_thin() : launch_wide()) != cudaSuccess) return err;
+  p.list = wide;
+  cfg.gridDim = dim3((unsigned)(sm_count() * kCombineBlocks));
   cfg.blockDim = dim3(kCombineThreads);
   cfg.dynamicSmemBytes = 0;
   cfg.numAttrs = 1;
   err = cudaLaunchKernelEx(&cfg, s.d_v == 64 ? extend_combine_kernel<64> : extend_combine_kernel<128>,
-                           p, thin, thin_blocks);
+                           p, thin, thin_blocks, blocks);
   if (err != cudaSuccess) return err;
   count_launch();
   return cudaGetLastError();

@@ -98,7 +98,20 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     if (tid == 0) report(p.dev_status, DIFFQKV_ERR_ALIGNMENT);
     return;
   }
-  ptx::grid_launch_dependents();  // the kernel for longer chunks works on other rows: it may take SMs as they fall free
+  if (p.first) ptx::grid_launch_dependents();
+  {  // a step without thin sequences (prompts): nothing to do here
+    bool any = false;
+    for (int b = tid; b < p.batch; b += kExtendThinThreads) {
+      int lo, n, past;
+      load_rows(p, b, lo, n, past);
+      any |= n > 0 && n <= p.thin_max;
+    }
+    if (!__syncthreads_or(any)) {
+      if (tid == 0) p.list.meta[blockIdx.x].rows = 0;
+      ptx::grid_dependency_wait();
+      return;
+    }
+  }
   if (tid == 0) {
     sc.abort = 0;
     sc.seek_b = p.batch;
@@ -145,8 +158,10 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   for (int b = b_lo; b < b_hi; ++b) {
     int lo, n, past;
     const int nt = load(b, lo, n, past);
-    mine += (long long)p.n_units * nt;
-    items += nt > 0 ? p.n_units : 0;
+    if (nt > 0) {
+      mine += (long long)p.n_units * (nt + kThinItemCost);
+      items += p.n_units;
+    }
   }
   auto warp_scan = [&](long long x) -> long long {  // inclusive
 #pragma unroll
@@ -176,11 +191,17 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   // segment at most.  (A segment costs about as much as five tiles next to its tiles, and short lists would give most
   // blocks two: 8 x ~700 tokens, 32/4/16 heads of 64, 31 -> 22 us.)
   int chunk = 0;
-  if (items < (int)gridDim.x && total < (1ll << 22)) {
-    chunk = (int)(((uint32_t)total + gridDim.x - items - 1) / (gridDim.x - items));
-    if (chunk > (int)((uint32_t)total / gridDim.x) + 4) chunk = 0;
+  if (items > 0 && items < (int)gridDim.x && total < (1ll << 22)) {
+    const uint32_t tiles = (uint32_t)total - items * kThinItemCost;
+    chunk = (int)((tiles + gridDim.x - items - 1) / (gridDim.x - items));
+    if (chunk > (int)(tiles / gridDim.x) + 4) chunk = 0;
   }
-  long long w0 = share_start(total, blockIdx.x, gridDim.x), w1 = share_start(total, blockIdx.x + 1, gridDim.x);
+  const int blocks = shares(total, gridDim.x, kThinItemCost + 1);  // that take part
+  long long w0 = total, w1 = total;
+  if ((int)blockIdx.x < blocks) {
+    w0 = share_start(total, blockIdx.x, blocks);
+    w1 = share_start(total, blockIdx.x + 1, blocks);
+  }
   if (chunk > 0) {
     __syncthreads();  // everybody has read the sums
     mine = 0;
@@ -207,7 +228,7 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       for (int b = b_lo; b < b_hi; ++b) {
         int lo, n, past;
         const int nt = load(b, lo, n, past);
-        const long long c = (long long)p.n_units * (chunk > 0 ? (nt + chunk - 1) / chunk : nt);
+        const long long c = nt == 0 ? 0 : (long long)p.n_units * (chunk > 0 ? (nt + chunk - 1) / chunk : nt + kThinItemCost);
         if (w0 < at + c) {
           sc.seek_b = b;
           sc.seek_lo = at;
@@ -216,7 +237,6 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         at += c;
       }
   }
-  if (blockIdx.x == 0 && tid == 0) *p.list.total = total;
   __syncthreads();
 
   if (warp == 0) {
@@ -227,7 +247,7 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     const uint32_t ring = ptx::smem_u32(ring_s), q_u32 = ptx::smem_u32(q_s);
     int ks = 0, vs = 0, k_count = 0, v_count = 0, segs = 0;  // ring places and tiles requested so far
     uint32_t kph = 0, vph = 0;
-    bool ok = true, cut = false;
+    bool ok = true;
     ExtendMeta m = {};
     auto hand_out = [&](const ThinSegment& d) -> bool {
       const int s = segs % kSegRing;
@@ -239,6 +259,7 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       __syncwarp();
       return true;
     };
+    int chunk_lo = 0;
     int b = sc.seek_b, lo = 0, n = 0, past = 0, nt = 0, u = 0;
     long long item_lo = sc.seek_lo;
     if (w0 < w1) {
@@ -247,26 +268,44 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       if (chunk > 0) {  // chunk `in` of the sequence: a range of one item, counted from the item's start
         const int per = (nt + chunk - 1) / chunk;
         u = (int)in / per;
-        w0 = ((int)in - u * per) * chunk;
-        w1 = w0 + chunk < nt ? w0 + chunk : nt;
-        item_lo = 0;
+        chunk_lo = ((int)in - u * per) * chunk;
       } else {
-        u = in < (1ll << 31) ? (int)((uint32_t)in / (uint32_t)nt) : (int)(in / nt);
-        item_lo += (long long)u * nt;
+        const int size = nt + kThinItemCost;
+        u = in < (1ll << 31) ? (int)((uint32_t)in / (uint32_t)size) : (int)(in / size);
+        item_lo += (long long)u * size;
       }
     } else {
       b = p.batch;
     }
+    auto next_item = [&] {
+      item_lo += nt + kThinItemCost;
+      if (++u < p.n_units) return;
+      u = 0;
+      do {
+        if (++b >= p.batch) return;
+        nt = load(b, lo, n, past);
+      } while (nt == 0);
+    };
     while (ok && b < p.batch && item_lo < w1) {
-      const int ta = w0 > item_lo ? (int)(w0 - item_lo) : 0;
-      const int tb = w1 - item_lo < nt ? (int)(w1 - item_lo) : nt;
+      int ta, tb;
+      if (chunk > 0) {
+        ta = chunk_lo;
+        tb = min(nt, chunk_lo + chunk);
+      } else {
+        ta = item_tile(w0 - item_lo, 1, nt, kThinItemCost);
+        tb = item_tile(w1 - item_lo, 1, nt, kThinItemCost);
+      }
       const int kv_len = past + n;
       const int head0 = u * p.parts * p.G;
       const int hk0 = head0 / p.heads_per_k, hv0 = head0 / p.heads_per_v;  // Eq. (idx)
+      if (ta >= tb) {  // the share ends within the item's own cost
+        next_item();
+        continue;
+      }
       if (ta == 0 && tb < nt) {
-        cut = true;
-        m.valid = 1; m.row_lo = lo; m.rows = p.parts * n * p.G; m.part_rows = n * p.G; m.head0 = head0;
-        m.cost = 1; m.nt = nt; m.member = 0; m.lo = item_lo; m.chunks = chunk > 0 ? (nt + chunk - 1) / chunk : 0;
+        m.rows = p.parts * n * p.G; m.part_rows = n * p.G; m.row_lo = lo; m.head0 = head0;
+        m.parts = chunk > 0 ? (nt + chunk - 1) / chunk
+                            : share_of(item_lo + last_tile(1, nt, kThinItemCost), total, blocks) - (int)blockIdx.x + 1;
       }
       if (!hand_out({lo, n, past, head0, ta, tb, v_count, (ta == 0 ? kSegFirst : 0) | (ta == 0 && tb == nt ? kSegWhole : 0)})) {
         ok = false;
@@ -337,20 +376,11 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       }
       if (!ok) break;
       ++segs;
-      item_lo += nt;
-      if (++u == p.n_units) {
-        u = 0;
-        do {
-          if (++b >= p.batch) break;
-          nt = load(b, lo, n, past);
-        } while (nt == 0);
-      }
+      if (chunk > 0) break;
+      next_item();
     }
     if (ok) ok = hand_out({0, 0, 0, 0, 0, 0, 0, kSegEnd});
-    if (lane == 0) {
-      if (!cut) m.valid = 0;
-      p.list.meta[blockIdx.x] = m;
-    }
+    if (lane == 0) p.list.meta[blockIdx.x] = m;
     if (!ok) {
       report(p.dev_status, DIFFQKV_ERR_TIMEOUT);
       // give copies in flight a bounded chance to land before the block's shared memory is released
@@ -394,28 +424,34 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         const uint32_t id_o = tc::idesc_bf16_f32(128, 0, 1, 1) |
                               ((p.v_parts == 1 ? all : v_step == 2 ? p.region + cols : cols) >> 3 << 17);
         if (!ptx::mbar_wait(q_full0 + 8 * qb, (segs >> 1) & 1, abort_flag)) { ok = false; break; }
-        // step i: the scores of tile i + 1, then the product with tile i's weights; tile i belongs to group i & 1
-        for (int i = -1; i < tiles && ok; ++i) {
-          if (i + 1 < tiles) {
-            const uint32_t d = tmem + ((i + 1) & 1) * 128;  // free: the group's last weights have been announced
-            for (int x = 0; x < p.k_parts; ++x) {
-              if (!ptx::mbar_wait(full0 + 8 * ks, kph, abort_flag)) { ok = false; break; }
-              tc::fence_after_sync();
-              const uint32_t ka = r_lo + ks * (kSlotBytes >> 4);
-              const uint32_t qa = q_lo + ((qb * 16384 + x * p.region * 128) >> 4);
-              tc::mma_ss_halves<false>(d + x * p.region, ka, k_hi, qa, hi, id_s);
+        auto scores = [&](int i) {  // S^T of tile i, for group i & 1
+          const uint32_t d = tmem + (i & 1) * 128;  // free: the group's last weights have been announced
+          for (int x = 0; x < p.k_parts; ++x) {
+            if (!ptx::mbar_wait(full0 + 8 * ks, kph, abort_flag)) { ok = false; return; }
+            tc::fence_after_sync();
+            const uint32_t ka = r_lo + ks * (kSlotBytes >> 4);
+            const uint32_t qa = q_lo + ((qb * 16384 + x * p.region * 128) >> 4);
+            tc::mma_ss_halves<false>(d + x * p.region, ka, k_hi, qa, hi, id_s);
 #pragma unroll
-              for (int k = 1; k < kDQK / 16; ++k)
-                tc::mma_ss_halves<true>(d + x * p.region, ka + (k / 4) * k_half + (((k % 4) * 32) >> 4), k_hi,
-                                        qa + (((k / 4) * (kThinCols * 128) + (k % 4) * 32) >> 4), hi, id_s);
-              tc::commit(empty0 + 8 * ks);
-              step(ks, kph, 1, p.k_ring);
-            }
-            if (!ok) break;
-            tc::commit(s_full0 + 8 * ((i + 1) & 1));
-            if (i + 2 == tiles) tc::commit(q_empty0 + 8 * qb);
+            for (int k = 1; k < kDQK / 16; ++k)
+              tc::mma_ss_halves<true>(d + x * p.region, ka + (k / 4) * k_half + (((k % 4) * 32) >> 4), k_hi,
+                                      qa + (((k / 4) * (kThinCols * 128) + (k % 4) * 32) >> 4), hi, id_s);
+            tc::commit(empty0 + 8 * ks);
+            step(ks, kph, 1, p.k_ring);
           }
-          if (i < 0) continue;
+          tc::commit(s_full0 + 8 * (i & 1));
+          if (i + 1 == tiles) tc::commit(q_empty0 + 8 * qb);
+        };
+        scores(0);
+        for (int i = 0; i < tiles && ok; ++i) {
+          // The scores of tile i + 1 go first when its K is there, else behind the product with tile i's weights, which
+          // gives its V places back.
+          bool ahead = i + 1 < tiles;
+          if (ahead && ptx::mbar_try_wait(full0 + 8 * ks, kph)) {
+            scores(i + 1);
+            ahead = false;
+            if (!ok) break;
+          }
           const int t = i & 1;
           if (i < 2) {  // the accumulator of the segment before has been read out
             if (!ptx::mbar_wait(o_free0 + 8 * t, t == 0 ? of0 : of1, abort_flag)) { ok = false; break; }
@@ -440,6 +476,7 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
           }
           if (!ok) break;
           tc::commit(o_done0 + 8 * t);
+          if (ahead) scores(i + 1);
         }
         if (!ok) break;
       }
@@ -722,19 +759,30 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     tc::fence_after_sync();
     tc::tmem_dealloc(tmem, kTmemCols);
   }
+  ptx::grid_dependency_wait();  // see the kernel for longer chunks
 }
 
 }  // namespace
 
 cudaError_t launch_extend_thin(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const ExtendParams& p,
-                               int d_qk, int d_v, int blocks, cudaStream_t stream) {
+                               int d_qk, int d_v, int blocks, bool second, cudaStream_t stream) {
   using Fn = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const ExtendParams);
   const Fn fn = d_v == 64 ? extend_thin_kernel<64, 64> : (d_qk == 128 ? extend_thin_kernel<128, 128> : extend_thin_kernel<64, 128>);
   const cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kThinSmem);
   if (err != cudaSuccess) return err;
-  fn<<<blocks, kExtendThinThreads, kThinSmem, stream>>>(mq, mk, mv, p);
-  count_launch();
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3(kExtendThinThreads);
+  cfg.dynamicSmemBytes = kThinSmem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = second ? 1 : 0;
+  const cudaError_t launched = cudaLaunchKernelEx(&cfg, fn, mq, mk, mv, p);
+  if (launched == cudaSuccess) count_launch();
+  return launched;
 }
 
 }  // namespace diffqkv
