@@ -83,6 +83,14 @@ void diffqkv_debug_decode_cluster(int32_t mode);
  */
 void diffqkv_debug_decode_timeout(int64_t wait_limit_ns, int64_t skip_tile);
 
+/*
+ * Test hook (process-wide host state): which kernel diffqkv_extend takes, 0 = the fastest that applies (default), 1 = the
+ * one with a block per row and query head, 2 = tiles on FMAs (where it does not apply, 1).  All compute the same thing.
+ * diffqkv_last_extend_kernel: what the most recent call took, 0 none yet, 1 and 2 as above, 3 the tensor cores.
+ */
+void diffqkv_debug_extend_kernel(int32_t choice);
+int32_t diffqkv_last_extend_kernel(void);
+
 #ifdef __cplusplus
 }
 #endif

@@ -38,7 +38,7 @@ EXPORTS = (
     "diffqkv_extend", "diffqkv_extend_workspace_bytes", "diffqkv_rope_append", "diffqkv_rope_frequencies",
     "diffqkv_pages_free", "diffqkv_pages_fork", "diffqkv_pages_fork_workspace_bytes", "diffqkv_pages_reserve",
     "diffqkv_pages_reserve_workspace_bytes", "diffqkv_pages_copy", "diffqkv_pages_compact",
-    "diffqkv_pages_compact_workspace_bytes",
+    "diffqkv_pages_compact_workspace_bytes", "diffqkv_debug_extend_kernel", "diffqkv_last_extend_kernel",
 )
 
 
@@ -725,6 +725,16 @@ def diffqkv_extend(q: torch.Tensor, cu_q: torch.Tensor, cache: KVCache, n_k: int
                                       workspace.data_ptr(), _size(workspace), out.data_ptr(), _addr(lse),
                                       _addr(dev_status), _stream_on(stream, dev)), "diffqkv_extend")
     return out
+
+
+def extend_kernel(choice: int) -> None:
+    """Test hook: the kernel diffqkv_extend takes (0 automatic, 1 a block per row, 2 tiles on FMAs)."""
+    _lib.diffqkv_debug_extend_kernel(C.c_int32(choice))
+
+
+def last_extend_kernel() -> int:
+    """0 none yet, 1 a block per row, 2 tiles on FMAs, 3 tensor cores (most recent diffqkv_extend call)."""
+    return int(_lib.diffqkv_last_extend_kernel())
 
 
 ROPE_SCALINGS = {"plain": 0, "linear": 1, "ntk": 2, "yarn": 3, "bands": 4}

@@ -440,6 +440,12 @@ diffqkv_status diffqkv_decode_topk(const void* q, const diffqkv_cache* cache, co
   return diffqkv_decode_topk_ids(q, cache, shape, topk, workspace, workspace_bytes, out, lse, nullptr, dev_status, stream);
 }
 
+static std::atomic<int> g_extend_choice{0}, g_last_extend_kernel{0};  // test hooks, see diffqkv_debug.h
+
+void diffqkv_debug_extend_kernel(int32_t choice) { g_extend_choice = choice; }
+
+int32_t diffqkv_last_extend_kernel(void) { return g_last_extend_kernel; }
+
 size_t diffqkv_extend_workspace_bytes(const diffqkv_shape* shape, int32_t total_q) {
   if (check_shape(shape) != DIFFQKV_OK || total_q < 0) return 0;
   return extend_workspace_bytes(*shape, total_q);
@@ -459,8 +465,13 @@ diffqkv_status diffqkv_extend(const void* q, const int32_t* cu_q, int32_t total_
   if (!workspace || workspace_bytes < extend_workspace_bytes(*shape, total_q)) return DIFFQKV_ERR_WORKSPACE;
   if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return DIFFQKV_ERR_ALIGNMENT;
   cudaStream_t st_ = static_cast<cudaStream_t>(stream);
-  cudaError_t err = launch_extend(q, cu_q, total_q, *cache, *shape, workspace, out, lse, dev_status, st_);
-  if (err != cudaErrorNotSupported) return err == cudaSuccess ? DIFFQKV_OK : DIFFQKV_ERR_CUDA;
+  const int choice = g_extend_choice;
+  cudaError_t err = cudaErrorNotSupported;
+  if (choice == 0) err = launch_extend(q, cu_q, total_q, *cache, *shape, workspace, out, lse, dev_status, st_);
+  if (err != cudaErrorNotSupported) {
+    g_last_extend_kernel = 3;
+    return err == cudaSuccess ? DIFFQKV_OK : DIFFQKV_ERR_CUDA;
+  }
   DecodeParams p;
   p.q = q;
   p.cache = view_of(cache);
@@ -470,7 +481,10 @@ diffqkv_status diffqkv_extend(const void* q, const int32_t* cu_q, int32_t total_
   p.chunk = 0; p.splits = 1;
   p.o_partial = nullptr; p.lse_partial = nullptr;
   p.dev_status = dev_status;
-  err = launch_extend_generic(p, shape->dtype, cu_q, total_q, out, shape->out_dtype == DIFFQKV_F32, lse, st_);
+  if (choice != 1) err = launch_extend_simt(p, *shape, cu_q, total_q, workspace, out, lse, st_);
+  g_last_extend_kernel = err == cudaErrorNotSupported ? 1 : 2;
+  if (err == cudaErrorNotSupported)
+    err = launch_extend_generic(p, shape->dtype, cu_q, total_q, out, shape->out_dtype == DIFFQKV_F32, lse, st_);
   if (err == cudaErrorNotSupported) return DIFFQKV_ERR_UNSUPPORTED;
   return err == cudaSuccess ? DIFFQKV_OK : DIFFQKV_ERR_CUDA;
 }

@@ -140,10 +140,14 @@ cudaError_t launch_rope_append(const void* q, const void* k_new, const void* v_n
                                cudaStream_t stream);
 bool rope_frequencies(int rot_dim, double theta, int scaling, double s, double L, double fast, double slow,
                       double* inv_freq, float* magnitude);
-// Chunk attention: tensor cores (extend.cu; cudaErrorNotSupported where it does not apply), one block per (row, query head) on plain FMAs (decode_generic.cu).
+// Chunk attention: tensor cores (extend.cu, extend_thin.cu), tiles on FMAs (extend_simt.cu), one block per (row, query
+// head) on FMAs (decode_generic.cu); each of the first two answers cudaErrorNotSupported where it does not apply.
 size_t extend_workspace_bytes(const diffqkv_shape& s, int total_q);
 cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const diffqkv_cache& c, const diffqkv_shape& s,
                           void* workspace, void* out, float* lse, int* dev_status, cudaStream_t stream);
+size_t extend_simt_workspace_bytes(const diffqkv_shape& s, int total_q);
+cudaError_t launch_extend_simt(const DecodeParams& d, const diffqkv_shape& s, const int* cu_q, int total_q, void* workspace,
+                               void* out, float* lse, cudaStream_t stream);
 cudaError_t launch_extend_generic(const DecodeParams& p, diffqkv_dtype dtype, const int* cu_q, int total_q, void* out,
                                   int out_is_f32, float* lse, cudaStream_t stream);
 // Page upkeep (pages.cu).

@@ -1056,7 +1056,9 @@ bool dims_supported(const diffqkv_shape& s) {
 }  // namespace
 
 size_t extend_workspace_bytes(const diffqkv_shape& s, int total_q) {
-  return dims_supported(s) ? place(make_plan(s, total_q), s.d_v, nullptr, nullptr, nullptr) : 256;
+  const size_t simt = extend_simt_workspace_bytes(s, total_q);  // a cache may turn out to have no tensor map
+  const size_t need = dims_supported(s) ? place(make_plan(s, total_q), s.d_v, nullptr, nullptr, nullptr) : 256;
+  return need > simt ? need : simt;
 }
 
 // cudaErrorNotSupported, with nothing launched, where the plain kernel has to take the call.

@@ -98,6 +98,31 @@ def test_rising_scores_raise_the_maximum_in_every_tile(api):
     run(api, step.fill())
 
 
+@pytest.mark.parametrize("choice", [1, 2])
+@pytest.mark.parametrize("heads", ["32/4/8", "6/2/3", "16/1/1", "8/4/2"])
+@pytest.mark.parametrize("dims", [(128, 128), (64, 64), (64, 128), (128, 64)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_kernels_on_fmas(api, choice, heads, dims, dtype):
+    """The kernels that take what the tensor cores do not, on the same steps: many rows, and few over a long cache."""
+    api.extend_kernel(choice)
+    try:
+        run(api, Step(api, [0, 5, 130, 700, 0], [1, 4, 33, 129, 0], *HEADS[heads], *dims, dtype=dtype, seed=21).fill())
+        assert api.last_extend_kernel() == choice
+        run(api, Step(api, [3000, 90, 1024], [2, 1, 1], *HEADS[heads], *dims, dtype=dtype, seed=22, pad=2).fill())
+    finally:
+        api.extend_kernel(0)
+
+
+def test_which_kernel(api):
+    for kw, kernel in ((dict(), 3), (dict(dtype=F32), 2), (dict(page=24), 2), (dict(page=64), 3), (dict(layout="flat"), 3)):
+        run(api, Step(api, [30, 9], [5, 40], 8, 2, 4, 64, 64, seed=23, **kw).fill())
+        assert api.last_extend_kernel() == kernel, kw
+    run(api, Step(api, [30, 9], [5, 40], 8, 2, 4, 64, 64, seed=23).fill(), scale=-0.1)
+    assert api.last_extend_kernel() == 2
+    run(api, Step(api, [30, 9], [5, 40], 8, 2, 4, 96, 64, seed=23).fill())
+    assert api.last_extend_kernel() == 1
+
+
 def test_nothing_to_do(api):
     step = Step(api, [3, 9], [0, 0], 4, 2, 2, 64, 64, pad=5).fill()
     run(api, step)
