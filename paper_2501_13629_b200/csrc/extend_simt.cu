@@ -50,31 +50,41 @@ __device__ __forceinline__ bool rows_of(const SimtParams& p, int b, int& lo, int
   return true;
 }
 
-// Copies tokens k0 .. k0 + 127 (those below end) of one head into [128][D + 4] floats.
-template <typename T, int D>
-__device__ __forceinline__ void copy_tile(const SimtParams& p, float* dst, const void* pool, long long s_blk, long long s_tok,
-                                          long long head_off, int b, int k0, int end) {
-  constexpr int kPer = 16 / sizeof(T), kVecs = D / kPer;
-  for (int e = threadIdx.x; e < kTok * kVecs; e += kThreads) {
-    const int t = e / kVecs, c = (e - t * kVecs) * kPer;
-    float* to = dst + t * (D + 4) + c;
-    const int tok = k0 + t;
-    bool there = tok < end;
-    long long blk = b, slot = tok;
-    if (there && p.cache.page_table) {
-      blk = p.cache.page_table[(long long)b * p.cache.max_pages_per_seq + tok / p.cache.page_size];
-      slot = tok % p.cache.page_size;
-      if (blk < 0 || blk >= p.cache.num_blocks) {
-        there = false;
+// Where tokens k0 .. k0 + 127 lie: block and slot of each (block -1: not there), a thread per token.
+__device__ __forceinline__ void place_tile(const SimtParams& p, int2* place, int b, int k0, int end) {
+  if (threadIdx.x >= kTok) return;
+  const int tok = k0 + threadIdx.x;
+  int2 at = make_int2(-1, 0);
+  if (tok < end) {
+    at = make_int2(b, tok);
+    if (p.cache.page_table) {
+      at.x = p.cache.page_table[(long long)b * p.cache.max_pages_per_seq + tok / p.cache.page_size];
+      at.y = tok % p.cache.page_size;
+      if (at.x < 0 || at.x >= p.cache.num_blocks) {
+        at.x = -1;
         report(p.dev_status, DIFFQKV_ERR_INDEX);
       }
     }
-    if (!there) {  // zeros: a weight of zero must not meet what lies behind the sequence
+  }
+  place[threadIdx.x] = at;
+}
+
+// Copies the tokens of a tile, one head, into [128][D + 4] floats.
+template <typename T, int D>
+__device__ __forceinline__ void copy_tile(float* dst, const void* pool, long long s_blk, long long s_tok, long long head_off,
+                                          const int2* place) {
+  constexpr int kPer = 16 / sizeof(T), kVecs = D / kPer;
+#pragma unroll 4
+  for (int e = threadIdx.x; e < kTok * kVecs; e += kThreads) {
+    const int t = e / kVecs, c = (e - t * kVecs) * kPer;
+    float* to = dst + t * (D + 4) + c;
+    const int2 at = place[t];
+    if (at.x < 0) {  // zeros: a weight of zero must not meet what lies behind the sequence
 #pragma unroll
       for (int i = 0; i < kPer; i += 4) *reinterpret_cast<float4*>(to + i) = make_float4(0.f, 0.f, 0.f, 0.f);
       continue;
     }
-    const T* from = reinterpret_cast<const T*>(pool) + blk * s_blk + head_off + slot * s_tok + c;
+    const T* from = reinterpret_cast<const T*>(pool) + at.x * s_blk + head_off + at.y * s_tok + c;
     if (sizeof(T) == 4) {
       ptx::cp_async_16(ptx::smem_u32(to), from);
     } else {
@@ -98,6 +108,7 @@ __global__ void __launch_bounds__(kThreads) extend_simt_kernel(const SimtParams 
   float* v_s = k_s + kTok * (DQ + 4);                // [128][DV + 4]
   float* p_s = v_s + kTok * (DV + 4);                // [32][128]
   __shared__ int seq_s, tile_s, scan_s[kThreads / 32];
+  __shared__ int2 place_s[2][kTok];  // of this tile's and of the next one's tokens
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   // ---- block x takes the x-th row tile of all sequences
@@ -169,14 +180,18 @@ __global__ void __launch_bounds__(kThreads) extend_simt_kernel(const SimtParams 
   }
   const CacheView& cv = p.cache;
   const long long k_head = (long long)hk * cv.k_sh, v_head = (long long)hv * cv.v_sh;
+  int turn = 0;
   if (t0 < t1) {
-    copy_tile<T, DQ>(p, k_s, cv.k, cv.k_sb, cv.k_st, k_head, b, t0, t1);
+    place_tile(p, place_s[0], b, t0, t1);
+    __syncthreads();
+    copy_tile<T, DQ>(k_s, cv.k, cv.k_sb, cv.k_st, k_head, place_s[0]);
     ptx::cp_async_commit();
   }
   const float* q_w = q_s + warp * 4 * DQ;
   float* p_w = p_s + warp * 4 * kTok;
-  for (int k0 = t0; k0 < t1; k0 += kTok) {
-    copy_tile<T, DV>(p, v_s, cv.v, cv.v_sb, cv.v_st, v_head, b, k0, t1);
+  for (int k0 = t0; k0 < t1; k0 += kTok, turn ^= 1) {
+    copy_tile<T, DV>(v_s, cv.v, cv.v_sb, cv.v_st, v_head, place_s[turn]);
+    if (k0 + kTok < t1) place_tile(p, place_s[turn ^ 1], b, k0 + kTok, t1);
     ptx::cp_async_commit();
     ptx::cp_async_wait<1>();  // K of this tile
     __syncthreads();
@@ -231,7 +246,7 @@ __global__ void __launch_bounds__(kThreads) extend_simt_kernel(const SimtParams 
     ptx::cp_async_wait<0>();  // V of this tile
     __syncthreads();          // everybody is through with K
     if (k0 + kTok < t1) {
-      copy_tile<T, DQ>(p, k_s, cv.k, cv.k_sb, cv.k_st, k_head, b, k0 + kTok, t1);
+      copy_tile<T, DQ>(k_s, cv.k, cv.k_sb, cv.k_st, k_head, place_s[turn ^ 1]);
       ptx::cp_async_commit();
     }
     // ---- O += P V: channels lane * kC ..
@@ -337,15 +352,18 @@ int heads_per_tile(const diffqkv_shape& s) {
 
 bool dims_ok(const diffqkv_shape& s) { return (s.d_qk == 64 || s.d_qk == 128) && (s.d_v == 64 || s.d_v == 128); }
 
-// Splits along the tokens: enough blocks for two a SM, of at least 512 tokens each.  At most 2048 rows times heads need
-// any (more fill the SMs without).
+// Splits along the tokens: enough blocks for two a SM, of at least 256 tokens each; the partial rows of all splits stay
+// within 32768.
+int most_splits(const diffqkv_shape& s, int total_q) {
+  const long long most = 32768 / ((long long)total_q * s.n_q);
+  return most > kMaxSplits ? kMaxSplits : (int)most;
+}
 int split_count(const diffqkv_shape& s, int max_seqlen, int total_q) {
-  const long long rows = (long long)total_q * s.n_q;
-  if (rows > 2048 || max_seqlen < 1024) return 1;
-  const long long blocks = (rows + kRows - 1) / kRows;
+  const long long blocks = ((long long)total_q * s.n_q + kRows - 1) / kRows;
   long long want = (296 + blocks - 1) / blocks;
-  if (want > max_seqlen / 512) want = max_seqlen / 512;
-  return want < 1 ? 1 : want > kMaxSplits ? kMaxSplits : (int)want;
+  if (want > max_seqlen / 256) want = max_seqlen / 256;
+  if (want > most_splits(s, total_q)) want = most_splits(s, total_q);
+  return want < 1 ? 1 : (int)want;
 }
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
@@ -354,9 +372,9 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 // The capacity of the cache is not known when the workspace is sized: room for the most splits.
 size_t extend_simt_workspace_bytes(const diffqkv_shape& s, int total_q) {
-  const size_t rows = (size_t)total_q * s.n_q;
-  if (!dims_ok(s) || rows > 2048) return 0;
-  return up256(rows * kMaxSplits * sizeof(float)) + up256(rows * kMaxSplits * s.d_v * sizeof(float));
+  if (!dims_ok(s) || total_q == 0 || most_splits(s, total_q) < 2) return 0;
+  const size_t parts = (size_t)total_q * s.n_q * most_splits(s, total_q);
+  return up256(parts * sizeof(float)) + up256(parts * s.d_v * sizeof(float));
 }
 
 cudaError_t launch_extend_simt(const DecodeParams& d, const diffqkv_shape& s, const int* cu_q, int total_q, void* workspace,
@@ -371,9 +389,9 @@ cudaError_t launch_extend_simt(const DecodeParams& d, const diffqkv_shape& s, co
   p.splits = split_count(s, d.cache.max_seqlen, total_q);
   p.split_tokens = ((d.cache.max_seqlen + p.splits - 1) / p.splits + kTok - 1) / kTok * kTok;
   p.out = out; p.out_is_f32 = s.out_dtype == DIFFQKV_F32; p.lse = lse;
-  const size_t rows = (size_t)total_q * s.n_q;
   p.part_lse = static_cast<float*>(workspace);
-  p.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + up256(rows * kMaxSplits * sizeof(float)));
+  p.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) +
+                                      up256((size_t)total_q * s.n_q * p.splits * sizeof(float)));
   p.dev_status = d.dev_status;
   const long long tiles = (long long)total_q / p.T + s.batch;
   const dim3 grid((unsigned)(tiles < total_q ? tiles : total_q), (unsigned)(s.n_q / p.G), (unsigned)p.splits);
