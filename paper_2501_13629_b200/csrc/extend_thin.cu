@@ -22,6 +22,8 @@
 // share of the bandwidth; its products take about 0.6 us and its softmax less.
 // Warp 0 TMA producer, one thread of warp 1 issues the products, warps 2-9 and 10-17 the softmax groups.  Every wait is
 // bounded.
+#include <type_traits>
+
 #include "attn_math.cuh"
 #include "extend.cuh"
 #include "ptx.cuh"
@@ -75,7 +77,6 @@ __global__ void __launch_bounds__(kExtendThinThreads, 1)
 extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                    const __grid_constant__ CUtensorMap tmap_v, const ExtendParams p) {
   constexpr int kHalvesK = kDQK / 64, kHalves = kD / 64;
-  constexpr int kHalvesMax = kHalvesK > kHalves ? kHalvesK : kHalves;
   constexpr int kKBytes = kKT * kDQK * 2, kVBytes = kKT * kD * 2;
   constexpr int kSlotBytes = kKBytes > kVBytes ? kKBytes : kVBytes;
   constexpr int kSlots = kRingBytes / kSlotBytes;  // 5 tiles of 32 KB or 10 of 16 KB: a ring of K, then one of V
@@ -241,9 +242,16 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
 
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer
+    // Lanes: token part of a tile, then channel half (where a box does not bring whole rows), then head.  As many heads as
+    // fit are requested together: a request by the whole warp costs some 900 cycles, however many boxes it has.
     const int boxes_part = kKT / p.box_tok;
-    const int my_part = lane / kHalvesMax, my_half = lane % kHalvesMax;
-    const bool has_box = lane < kHalvesMax * boxes_part;
+    const int my_part = lane % boxes_part;
+    const int k_halves = p.k_rows ? 1 : kHalvesK, v_halves = p.v_rows ? 1 : kHalves;
+    const int my_rest = lane / boxes_part;
+    const int k_half = my_rest % k_halves, k_head = my_rest / k_halves, k_heads = 32 / (boxes_part * k_halves);
+    const int v_half = my_rest % v_halves, v_head = my_rest / v_halves, v_heads = 32 / (boxes_part * v_halves);
+    const uint32_t k_off = p.k_rows ? my_part * (p.box_tok * 256) : k_half * (kKT * 128) + my_part * (p.box_tok * 128);
+    const uint32_t v_off = p.v_rows ? my_part * (p.box_tok * 256) : v_half * (kKT * 128) + my_part * (p.box_tok * 128);
     const uint32_t ring = ptx::smem_u32(ring_s), q_u32 = ptx::smem_u32(q_s);
     int ks = 0, vs = 0, k_count = 0, v_count = 0, segs = 0;  // ring places and tiles requested so far
     uint32_t kph = 0, vph = 0;
@@ -314,46 +322,54 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       auto fetch = [&](int tile) -> int {  // page of this lane's box (fetched two tiles ahead)
         if (!p.page_table) return b;
         const int tok = tile * kKT + my_part * p.box_tok;
-        if (tile >= tb || !has_box || tok >= kv_len) return 0;
+        if (tile >= tb || tok >= kv_len) return 0;
         return p.page_table[(long long)b * p.max_pages_per_seq + tok / p.page_size];
       };
-      // the tiles of the K heads (is_k) or of the V heads of token tile `tile`, whose page is `page`
-      auto request = [&](bool is_k, int tile, int page) {
+      // The tiles of the K heads (is_k) or of the V heads of token tile `tile`, whose page is `page`.
+      auto request = [&](auto is_k, int tile, int page) __attribute__((always_inline)) {
+        constexpr bool kIsK = decltype(is_k)::value;
         const int tok = tile * kKT;
         const int parts_valid = min(boxes_part, (kv_len - tok + p.box_tok - 1) / p.box_tok);
-        const int halves = is_k ? kHalvesK : kHalves, count = is_k ? p.k_parts : p.v_parts, head = is_k ? hk0 : hv0;
-        const bool whole_rows = is_k ? p.k_rows : p.v_rows;  // a box brings all channels of its tokens
-        const bool here = has_box && my_part < parts_valid && my_half < (whole_rows ? 1 : halves);
-        if (here && (page < 0 || page >= p.num_blocks)) {  // never read outside the pool: flag it, read block 0 instead
+        if (my_part < parts_valid && (page < 0 || page >= p.num_blocks)) {  // never read outside the pool: flag it, block 0 instead
           report(p.dev_status, DIFFQKV_ERR_INDEX);
           page = 0;
         }
         const int first = tok + my_part * p.box_tok;
         const int slot_tok = p.page_table ? first % p.page_size : first;
-        const uint32_t off = whole_rows ? my_part * (p.box_tok * 256) : my_half * (kKT * 128) + my_part * (p.box_tok * 128);
-        const CUtensorMap* map = is_k ? &tmap_k : &tmap_v;
-        for (int x = 0; x < count; ++x) {
-          const int slot = is_k ? ks : p.k_ring + vs;
-          if (!wait_warp(empty0 + 8 * slot, (is_k ? kph : vph) ^ 1, abort_flag)) { ok = false; return; }
-          const uint32_t bar = full0 + 8 * slot;
-          if (lane == 0) ptx::mbar_arrive_expect_tx(bar, (uint32_t)(parts_valid * p.box_tok * halves) * 128u);
-          __syncwarp();
-          if (here) {
-            if (whole_rows) ptx::tma_load_5d(ring + slot * kSlotBytes + off, map, bar, 0, 0, 0, (head + x) * p.head_groups + slot_tok / 8, page);
-            else ptx::tma_load_5d(ring + slot * kSlotBytes + off, map, bar, 0, slot_tok, my_half, head + x, page);
+        const int count = kIsK ? p.k_parts : p.v_parts, together = kIsK ? k_heads : v_heads;
+        const int ring_size = kIsK ? p.k_ring : p.v_ring, mine = kIsK ? k_head : v_head;
+        const uint32_t bytes = (uint32_t)(parts_valid * p.box_tok * (kIsK ? kHalvesK : kHalves)) * 128u;
+        int& pos = kIsK ? ks : vs;
+        uint32_t& ph = kIsK ? kph : vph;
+        for (int x0 = 0; x0 < count; x0 += together) {
+          const int now = min(together, count - x0);  // heads of this request
+          int place = pos + mine;
+          uint32_t parity = ph;
+          if (place >= ring_size) { place -= ring_size; parity ^= 1; }
+          const int slot = (kIsK ? 0 : p.k_ring) + place;
+          const bool here = mine < now;
+          // every head as soon as its own place is free (the bytes are announced by one lane, in any order with the copies:
+          // the barrier cannot complete before)
+          const bool fine = !here || ptx::mbar_wait(empty0 + 8 * slot, parity ^ 1, abort_flag);
+          if (here && fine) {
+            const uint32_t bar = full0 + 8 * slot, dst = ring + slot * kSlotBytes + (kIsK ? k_off : v_off);
+            if (lane == mine * boxes_part * (kIsK ? k_halves : v_halves)) ptx::mbar_arrive_expect_tx(bar, bytes);
+            if (my_part < parts_valid) {
+              const int head = (kIsK ? hk0 : hv0) + x0 + mine;
+              const CUtensorMap* map = kIsK ? &tmap_k : &tmap_v;
+              if (kIsK ? p.k_rows : p.v_rows) ptx::tma_load_5d(dst, map, bar, 0, 0, 0, head * p.head_groups + slot_tok / 8, page);
+              else ptx::tma_load_5d(dst, map, bar, 0, slot_tok, kIsK ? k_half : v_half, head, page);
+            }
           }
-          if (is_k) {
-            ++k_count;
-            if (++ks == p.k_ring) { ks = 0; kph ^= 1; }
-          } else {
-            ++v_count;
-            if (++vs == p.v_ring) { vs = 0; vph ^= 1; }
-          }
+          if (!__all_sync(0xffffffffu, fine)) { ok = false; return; }
+          pos += now;
+          if (pos >= ring_size) { pos -= ring_size; ph ^= 1; }
+          (kIsK ? k_count : v_count) += now;
         }
       };
       // K runs a tile ahead of V: a V tile waits for the softmax of its scores anyway, and what waits holds a place
       int page0 = fetch(ta), page1 = fetch(ta + 1);
-      request(true, ta, page0);
+      request(std::true_type{}, ta, page0);
       if (!ok) break;
       // the segment's Q: rows of every head group behind one another, thin_max tokens each
       const int qb = segs & 1;
@@ -369,8 +385,8 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       __syncwarp();
       for (int tile = ta; tile < tb && ok; ++tile) {
         const int page2 = fetch(tile + 2);
-        if (tile + 1 < tb) request(true, tile + 1, page1);
-        if (ok) request(false, tile, page0);
+        if (tile + 1 < tb) request(std::true_type{}, tile + 1, page1);
+        if (ok) request(std::false_type{}, tile, page0);
         page0 = page1;
         page1 = page2;
       }
@@ -444,15 +460,19 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         };
         scores(0);
         for (int i = 0; i < tiles && ok; ++i) {
-          // The scores of tile i + 1 go first when its K is there, else behind the product with tile i's weights, which
-          // gives its V places back.
+          // Whichever is there first: K of tile i + 1, for its scores, or the weights of tile i, for the product with its V
+          // (which gives the places back).
+          const int t = i & 1;
           bool ahead = i + 1 < tiles;
-          if (ahead && ptx::mbar_try_wait(full0 + 8 * ks, kph)) {
-            scores(i + 1);
-            ahead = false;
+          if (ahead) {
+            const int which = ptx::mbar_wait_either(full0 + 8 * ks, kph, p_full0 + 8 * t, t == 0 ? tp0 : tp1, abort_flag);
+            if (which == 1) {
+              scores(i + 1);
+              ahead = false;
+            }
+            ok = ok && which != 0;
             if (!ok) break;
           }
-          const int t = i & 1;
           if (i < 2) {  // the accumulator of the segment before has been read out
             if (!ptx::mbar_wait(o_free0 + 8 * t, t == 0 ? of0 : of1, abort_flag)) { ok = false; break; }
             if (t == 0) of0 ^= 1; else of1 ^= 1;

@@ -37,6 +37,18 @@ __device__ __forceinline__ bool mbar_try_wait(uint32_t bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
+// The same without the pause that a try_wait may take.
+__device__ __forceinline__ bool mbar_test_wait(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 __device__ __forceinline__ uint64_t globaltimer_ns() {
   uint64_t t;
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
@@ -56,6 +68,25 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
       if (globaltimer_ns() - t0 > limit_ns) {
         if (abort_flag) *abort_flag = 1;
         return false;
+      }
+    }
+  }
+}
+
+// Bounded wait for whichever of two barriers completes first: 1, 2, or 0 when neither has (see mbar_wait).
+__device__ __forceinline__ int mbar_wait_either(uint32_t bar1, uint32_t parity1, uint32_t bar2, uint32_t parity2,
+                                                volatile int* abort_flag, uint64_t limit_ns = kWaitLimitNs) {
+  uint64_t t0 = 0;
+  for (uint32_t it = 1;; ++it) {
+    if (mbar_test_wait(bar1, parity1)) return 1;
+    if (mbar_test_wait(bar2, parity2)) return 2;
+    if ((it & 63u) == 0) {
+      if (abort_flag && *abort_flag) return 0;
+      const uint64_t now = globaltimer_ns();
+      if (t0 == 0) t0 = now;
+      if (now - t0 > limit_ns) {
+        if (abort_flag) *abort_flag = 1;
+        return 0;
       }
     }
   }
