@@ -100,13 +100,21 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     return;
   }
   if (p.first) ptx::grid_launch_dependents();
+  auto load = [&](int b, int& lo, int& n, int& past) -> int {  // tiles of one unit of sequence b
+    load_rows(p, b, lo, n, past);
+    return n > 0 && n <= p.thin_max ? (past + n + kKT - 1) / kKT : 0;
+  };
+  const int per_thread = (p.batch + kExtendThinThreads - 1) / kExtendThinThreads;
+  const int b_lo = min(tid * per_thread, p.batch), b_hi = min(b_lo + per_thread, p.batch);
+  int my_lo = 0, my_n = 0, my_past = 0;  // of the thread's first sequence: there is seldom another
+  const int my_nt = b_lo < b_hi ? load(b_lo, my_lo, my_n, my_past) : 0;
+  auto tiles_of = [&](int b) -> int {
+    int lo, n, past;
+    return b == b_lo ? my_nt : load(b, lo, n, past);
+  };
   {  // a step without thin sequences (prompts): nothing to do here
-    bool any = false;
-    for (int b = tid; b < p.batch; b += kExtendThinThreads) {
-      int lo, n, past;
-      load_rows(p, b, lo, n, past);
-      any |= n > 0 && n <= p.thin_max;
-    }
+    bool any = my_nt > 0;
+    for (int b = b_lo + 1; b < b_hi; ++b) any |= tiles_of(b) > 0;
     if (!__syncthreads_or(any)) {
       if (tid == 0) p.list.meta[blockIdx.x].rows = 0;
       ptx::grid_dependency_wait();
@@ -146,19 +154,12 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     tc::tmem_relinquish();
   }
   // ---- this block's range of the flat list of tiles
-  auto load = [&](int b, int& lo, int& n, int& past) -> int {  // tiles of one unit of sequence b
-    load_rows(p, b, lo, n, past);
-    return n > 0 && n <= p.thin_max ? (past + n + kKT - 1) / kKT : 0;
-  };
   long long* scan = reinterpret_cast<long long*>(&sc.part[0][0][0]);  // tiles, then chunks, of every warp's sequences
   int* scan_items = reinterpret_cast<int*>(scan + kExtendThinThreads / 32);
-  const int per_thread = (p.batch + kExtendThinThreads - 1) / kExtendThinThreads;
-  const int b_lo = min(tid * per_thread, p.batch), b_hi = min(b_lo + per_thread, p.batch);
   long long mine = 0;
   int items = 0;
   for (int b = b_lo; b < b_hi; ++b) {
-    int lo, n, past;
-    const int nt = load(b, lo, n, past);
+    const int nt = tiles_of(b);
     if (nt > 0) {
       mine += (long long)p.n_units * (nt + kThinItemCost);
       items += p.n_units;
@@ -206,10 +207,7 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   if (chunk > 0) {
     __syncthreads();  // everybody has read the sums
     mine = 0;
-    for (int b = b_lo; b < b_hi; ++b) {
-      int lo, n, past;
-      mine += (long long)p.n_units * ((load(b, lo, n, past) + chunk - 1) / chunk);
-    }
+    for (int b = b_lo; b < b_hi; ++b) mine += (long long)p.n_units * ((tiles_of(b) + chunk - 1) / chunk);
     incl = warp_scan(mine);
     if (lane == 31) scan[warp] = incl;
     __syncthreads();
@@ -227,8 +225,7 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     long long at = before + incl - mine;
     if (w0 < w1 && at <= w0 && w0 < at + mine)
       for (int b = b_lo; b < b_hi; ++b) {
-        int lo, n, past;
-        const int nt = load(b, lo, n, past);
+        const int nt = tiles_of(b);
         const long long c = nt == 0 ? 0 : (long long)p.n_units * (chunk > 0 ? (nt + chunk - 1) / chunk : nt + kThinItemCost);
         if (w0 < at + c) {
           sc.seek_b = b;
@@ -551,25 +548,6 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         tc::wait_ld();
         const int k0 = (w.ta + i) * kKT;
         if (k0 + kKT > w.past + 1) {  // the tile reaches past some row's position
-          const bool ragged = k0 + kKT > w.past + w.n;
-          // (ragged) The tile before, the other group's, may still wait for its V, in the place that this one's V will
-          // have: until its product is done a wait for this V could take the phase before for its own.
-          if (ragged && i > 0) ok = wait_warp(o_done0 + 8 * (1 - t), (other + ((i - 1) >> 1)) & 1, abort_flag) && ok;
-          if (ragged && half == 0 && r >= w.past + w.n - k0) {
-            // V rows past the sequence end hold whatever followed in memory: zero them (0 * NaN would poison the product)
-            for (int y = 0; y < p.v_parts; ++y) {
-              const int at = w.v0 + i * p.v_parts + y, slot = p.k_ring + at % p.v_ring;
-              ok = ok && ptx::mbar_wait(full0 + 8 * slot, (at / p.v_ring) & 1, abort_flag);
-#pragma unroll
-              for (int h = 0; h < kHalves; ++h) {
-                uint4* dst = reinterpret_cast<uint4*>(ring_s + slot * kSlotBytes +
-                                                      (p.v_rows ? (r / 8) * 2048 + h * 1024 + (r % 8) * 128 : h * (kKT * 128) + r * 128));
-#pragma unroll
-                for (int e = 0; e < 8; ++e) dst[e] = make_uint4(0, 0, 0, 0);
-              }
-            }
-          }
-          __syncwarp();
           const int hidden = (k0 + r - w.past) * p.G;  // columns of a group below this belong to rows before the token
 #pragma unroll
           for (int c = 0; c < kHalfCols; ++c)
@@ -667,6 +645,25 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
             }
             *reinterpret_cast<uint4*>(p_row + (((half * 4 + q) ^ (r & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
           }
+        if (k0 + kKT > w.past + w.n) {
+          // V rows past the sequence end hold whatever followed in memory: zero them (0 * NaN would poison the product).
+          // The tile before, the other group's, may still wait for its V, in the place that this one's V will have: until
+          // its product is done a wait for this V could take the phase before for its own.
+          if (i > 0) ok = wait_warp(o_done0 + 8 * (1 - t), (other + ((i - 1) >> 1)) & 1, abort_flag) && ok;
+          if (half == 0 && r >= w.past + w.n - k0) {
+            for (int y = 0; y < p.v_parts; ++y) {
+              const int at = w.v0 + i * p.v_parts + y, slot = p.k_ring + at % p.v_ring;
+              ok = ok && ptx::mbar_wait(full0 + 8 * slot, (at / p.v_ring) & 1, abort_flag);
+#pragma unroll
+              for (int h = 0; h < kHalves; ++h) {
+                uint4* dst = reinterpret_cast<uint4*>(ring_s + slot * kSlotBytes +
+                                                      (p.v_rows ? (r / 8) * 2048 + h * 1024 + (r % 8) * 128 : h * (kKT * 128) + r * 128));
+#pragma unroll
+                for (int e = 0; e < 8; ++e) dst[e] = make_uint4(0, 0, 0, 0);
+              }
+            }
+          }
+        }
         ptx::fence_proxy_async();
         tc::fence_before_sync();
         __syncwarp();
