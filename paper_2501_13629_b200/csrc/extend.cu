@@ -43,11 +43,6 @@ constexpr int kExtendThreads = 384;
 constexpr int kSoftmaxWarp0 = 4;
 // Shared memory: two Q tiles, the rings of K and V tiles, the exchange of the two softmax groups, barriers.
 constexpr int kExtendSmem = 1024 + 2 * (kRows * kDMax * 2) + kRingBytes + 1024 + 320;
-// In the division of the work: a K/V tile of a wide and of a narrow item, and what an item costs next to its tiles (its
-// rows are written out and the pipeline fills again).  Measured on prompts of 1.5k-2k rows over 1k-5k tokens: 2.35 us a
-// tile, 5.8 us an item; without the last, blocks with many short items ended 13 % late.
-constexpr int kWideCost = 2, kNarrowCost = 1, kItemCost = 5;
-
 // A segment as the producer hands it to the other roles, through a ring in shared memory.
 struct Segment {
   int row_lo, n, past;  // the sequence: first row, rows, tokens cached before
@@ -59,58 +54,6 @@ struct Segment {
 };
 constexpr int kSegRing = 4;
 constexpr int kSegEnd = 1, kSegWide = 2, kSegWhole = 4, kSegFirst = 8;  // first: holds the item's first tile
-
-// sum of floor((a x + b) / m) for x = 0 .. n - 1 with a, b >= 0, m > 0: the Euclid-like recursion on (m, a).  Not inlined:
-// the code that a block runs once at its start is fetched from the second-level cache line by line, which is what it
-// costs (with every quotient inlined a block began its first loads 16 us after its start).
-__device__ __noinline__ long long floor_sum(long long n, long long m, long long a, long long b) {
-  long long ans = 0;
-  while (n > 0) {
-    if (a >= m) { ans += (n - 1) * n / 2 * (a / m); a %= m; }
-    if (b >= m) { ans += n * (b / m); b %= m; }
-    const long long y = a * n + b;
-    if (y < m) break;
-    n = y / m;
-    b = y % m;
-    const long long t = m; m = a; a = t;
-  }
-  return ans;
-}
-// The same with m = 128 and a = 2^s: for a >= 128 every term is floor(b / 128) + x a / 128, else with r = 128 / a terms in
-// a turn and e = floor(b / a) the sum of floor((e + x) / r), a difference of sums from 0.
-__device__ __forceinline__ long long floor_sum_128(int n, int s, int b) {
-  if (s >= 7) return (long long)n * (b >> 7) + (((long long)n * (n - 1) / 2) << (s - 7));
-  const int h = 7 - s, e = b >> s;
-  auto upto = [&](int t) -> long long {  // sum of y >> h for y < t
-    const int q = t >> h;
-    return ((long long)q * (q - 1) / 2 << h) + (long long)q * (t - (q << h));
-  };
-  return upto(e + n) - upto(e);
-}
-// One sequence of the step.
-struct Seq {
-  int lo, n, past, items;  // first row, rows (0: not in this list), tokens cached before, items per head group
-  bool bad;                // does not fit
-  __device__ void load(const ExtendParams& p, int b) {
-    bad = !load_rows(p, b, lo, n, past);
-    if (n <= p.thin_max) n = 0;
-    items = (n + 2 * p.T - 1) / (2 * p.T);
-  }
-  // cost of the first i items, i < items
-  __device__ long long cost_before(const ExtendParams& p, int i) const {
-    const int b = past + 2 * p.T + kKT - 1;
-    const long long tiles = p.t_log2 >= 0 ? floor_sum_128(i, p.t_log2 + 1, b) : floor_sum(i, kKT, 2 * p.T, b);
-    return kWideCost * tiles + (long long)kItemCost * i;
-  }
-  __device__ bool wide(const ExtendParams& p, int i) const { return n - i * 2 * p.T > p.T; }
-  __device__ int tiles(const ExtendParams& p, int i) const {  // K/V tiles of item i
-    return (past + min(n, (i + 1) * 2 * p.T) + kKT - 1) / kKT;
-  }
-  __device__ long long cost(const ExtendParams& p) const {  // of one head group
-    if (n == 0) return 0;
-    return cost_before(p, items - 1) + kItemCost + (wide(p, items - 1) ? kWideCost : kNarrowCost) * (long long)tiles(p, items - 1);
-  }
-};
 
 // The segments of one block, in order.
 struct Walk {
@@ -224,7 +167,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 + 2 * kKSlots + 2 * kVSlots + 14 + 2 * kSegRing);
   volatile int* abort_flag = reinterpret_cast<int*>(tmem_slot + 1);
   __shared__ Segment seg_s[kSegRing];
-  __shared__ long long scan_s[kExtendThreads / 32 + 1];
+  __shared__ long long scan_s[kExtendThreads / 32], others_s[kExtendThreads / 32];
   __shared__ long long seek_lo_s;
   __shared__ int seek_b_s;
 
@@ -232,9 +175,13 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   // The kernel for thin sequences works on other rows; whichever of the two comes second may take the SMs that the
   // first one's blocks leave.  The joining kernel depends on the second alone, which therefore ends behind the first.
   if (p.first) ptx::grid_launch_dependents();
+  const int per_thread = (p.batch + kExtendThreads - 1) / kExtendThreads;
+  const int b_lo = min(tid * per_thread, p.batch), b_hi = min(b_lo + per_thread, p.batch);
+  Seq my = {};  // the thread's first sequence: there is seldom another
+  if (b_lo < b_hi) my.load(p, b_lo);
   {  // a step of thin sequences alone (decode): nothing to do here
-    bool any = false;
-    for (int b = tid; b < p.batch; b += kExtendThreads) {
+    bool any = my.n > 0 || my.bad;
+    for (int b = b_lo + 1; b < b_hi; ++b) {
       Seq s;
       s.load(p, b);
       any |= s.n > 0 || s.bad;
@@ -283,14 +230,13 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     tc::tmem_relinquish();
   }
   // ---- this block's range of the flat list: every thread sums the cost of its share of the sequences
-  const int per_thread = (p.batch + kExtendThreads - 1) / kExtendThreads;
-  const int b_lo = min(tid * per_thread, p.batch), b_hi = min(b_lo + per_thread, p.batch);
-  long long mine = 0;
+  long long mine = 0, others = 0;
   for (int b = b_lo; b < b_hi; ++b) {
-    Seq s;
-    s.load(p, b);
+    Seq s = my;
+    if (b > b_lo) s.load(p, b);
     if (s.bad && blockIdx.x == 0) report(p.dev_status, DIFFQKV_ERR_INDEX);
     mine += p.n_units * s.cost(p);
+    if (s.thin_tiles > 0) others += (long long)p.n_units * (s.thin_tiles + kThinItemCost);
   }
   long long incl = mine;
 #pragma unroll
@@ -298,30 +244,41 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     const long long y = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += y;
   }
-  if (lane == 31) scan_s[warp + 1] = incl;
+  if (__any_sync(0xffffffffu, others > 0)) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) others += __shfl_xor_sync(0xffffffffu, others, o);
+  }
+  if (lane == 31) {
+    scan_s[warp] = incl;
+    others_s[warp] = others;
+  }
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
   long long before = 0, total = 0;
+  others = 0;
 #pragma unroll
   for (int w = 0; w < kExtendThreads / 32; ++w) {
-    if (w < warp) before += scan_s[w + 1];
-    total += scan_s[w + 1];
+    if (w < warp) before += scan_s[w];
+    total += scan_s[w];
+    others += others_s[w];
   }
   const int team = (int)blockIdx.x / p.list.team, member = (int)blockIdx.x - team * p.list.team;
-  const int n_teams = shares(total, p.list.n_teams, kItemCost + kWideCost);  // that take part
-  long long w0 = total, w1 = total;
-  if (team < n_teams) {
-    w0 = share_start(total, team, n_teams);
-    w1 = share_start(total, team + 1, n_teams);
+  const int n_teams = wide_teams(p, total, others);  // that take part
+  if (team >= n_teams) {
+    if (tid == 0) p.list.meta[blockIdx.x].rows = 0;
+    if (warp == 1) tc::tmem_dealloc(tmem_base, kTmemCols);
+    ptx::grid_dependency_wait();
+    return;
   }
+  const long long w0 = share_start(total, team, n_teams), w1 = share_start(total, team + 1, n_teams);
   {
     long long at = before + incl - mine;
     if (w0 < w1 && at <= w0 && w0 < at + mine)
       for (int b = b_lo; b < b_hi; ++b) {
-        Seq s;
-        s.load(p, b);
+        Seq s = my;
+        if (b > b_lo) s.load(p, b);
         const long long c = p.n_units * s.cost(p);
         if (w0 < at + c) {
           seek_b_s = b;
@@ -1042,7 +999,6 @@ size_t place(const Plan& pl, int d_v, char* base, ExtendList* wide, ExtendList* 
     l.part_o = reinterpret_cast<float*>(take(2 * sizeof(float) * (size_t)blocks[i] * rows[i] * d_v));
     l.slot_rows = rows[i];
     l.team = i == 0 ? pl.parts : 1;
-    l.n_teams = i == 0 ? pl.n_teams : pl.blocks;
     if (lists[i]) *lists[i] = l;
   }
   return at;
@@ -1100,9 +1056,11 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
     if (pl.T == 1 << x) p.t_log2 = x;
   p.parts = pl.parts; p.n_units = pl.groups / pl.parts;
   p.thin_max = pl.thin_max; p.region = pl.region;
+  p.blocks = pl.blocks; p.n_teams = pl.n_teams; p.team = pl.parts;
   p.heads_per_k = s.n_q / s.n_k; p.heads_per_v = s.n_q / s.n_v;
   p.k_parts = p.heads_per_k < p.heads_per_v ? pl.parts : 1;
   p.v_parts = p.heads_per_v < p.heads_per_k ? pl.parts : 1;
+  p.thin_weight = 0.3f + 0.48f * (p.k_parts + p.v_parts);
   {  // 160 KB of tiles: K of two token tiles where there is room, the rest V; an even number where V tiles go in pairs
     const int slots = kRingBytes / (kKT * 2 * (s.d_qk > s.d_v ? s.d_qk : s.d_v));
     p.k_ring = 2 * p.k_parts < slots - p.v_parts ? 2 * p.k_parts : slots - p.v_parts;

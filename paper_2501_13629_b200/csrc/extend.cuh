@@ -30,7 +30,7 @@ struct ExtendList {
   float* part_lse;     // [2 blocks][slot_rows] base-2 log-sum-exp
   ExtendMeta* meta;    // [blocks]
   int slot_rows;
-  int team, n_teams;   // blocks = n_teams * team
+  int team;            // blocks that share an item's K or V head, next to each other
 };
 
 struct ExtendParams {
@@ -43,6 +43,9 @@ struct ExtendParams {
   int n_units, parts;  // head groups = n_units * parts: the groups of a unit share their K head or their V head
   int thin_max;        // sequences of at most this many rows are thin
   int region;          // columns of a head group of a thin sequence
+  // SMs; teams of the list of long chunks and blocks in one; cost of a tile of a thin sequence in that list's units
+  int blocks, n_teams, team;
+  float thin_weight;
   int k_parts, v_parts;  // K heads and V heads of a unit: (1, parts), (parts, 1) or (1, 1)
   int heads_per_k, heads_per_v;
   // the thin kernel's K and V tiles: ring lengths; whether a TMA box brings whole rows, and then the groups of eight
@@ -106,6 +109,87 @@ __device__ __forceinline__ long long last_tile(int cost, int nt, int extra) {
 }
 // Likewise for thin items, in tiles: a block's second item costs it about as much as five more tiles.
 constexpr int kThinItemCost = 5;
+// In the division of the work: a K/V tile of a wide and of a narrow item, and what an item costs next to its tiles (its
+// rows are written out and the pipeline fills again).  Measured on prompts of 1.5k-2k rows over 1k-5k tokens: 2.35 us a
+// tile, 5.8 us an item; without the last, blocks with many short items ended 13 % late.
+constexpr int kWideCost = 2, kNarrowCost = 1, kItemCost = 5;
+
+// sum of floor((a x + b) / m) for x = 0 .. n - 1 with a, b >= 0, m > 0: the Euclid-like recursion on (m, a).  Not inlined:
+// the code that a block runs once at its start is fetched from the second-level cache line by line, which is what it
+// costs (with every quotient inlined a block began its first loads 16 us after its start).
+static __device__ __noinline__ long long floor_sum(long long n, long long m, long long a, long long b) {
+  long long ans = 0;
+  while (n > 0) {
+    if (a >= m) { ans += (n - 1) * n / 2 * (a / m); a %= m; }
+    if (b >= m) { ans += n * (b / m); b %= m; }
+    const long long y = a * n + b;
+    if (y < m) break;
+    n = y / m;
+    b = y % m;
+    const long long t = m; m = a; a = t;
+  }
+  return ans;
+}
+// The same with m = 128 and a = 2^s: for a >= 128 every term is floor(b / 128) + x a / 128, else with r = 128 / a terms in
+// a turn and e = floor(b / a) the sum of floor((e + x) / r), a difference of sums from 0.
+__device__ __forceinline__ long long floor_sum_128(int n, int s, int b) {
+  if (s >= 7) return (long long)n * (b >> 7) + (((long long)n * (n - 1) / 2) << (s - 7));
+  const int h = 7 - s, e = b >> s;
+  auto upto = [&](int t) -> long long {  // sum of y >> h for y < t
+    const int q = t >> h;
+    return ((long long)q * (q - 1) / 2 << h) + (long long)q * (t - (q << h));
+  };
+  return upto(e + n) - upto(e);
+}
+// One sequence of the step as the list of long chunks has it.
+struct Seq {
+  int lo, n, past, items;  // first row, rows (0: not in this list), tokens cached before, items per head group
+  int thin_tiles;          // tiles of one unit of the other list (0: not in that one)
+  bool bad;                // does not fit
+  __device__ void load(const ExtendParams& p, int b) {
+    bad = !load_rows(p, b, lo, n, past);
+    thin_tiles = items = 0;
+    if (n > p.thin_max) {
+      items = (n + 2 * p.T - 1) / (2 * p.T);
+    } else {
+      thin_tiles = n > 0 ? (past + n + kKT - 1) / kKT : 0;
+      n = 0;
+    }
+  }
+  // cost of the first i items, i < items
+  __device__ long long cost_before(const ExtendParams& p, int i) const {
+    const int b = past + 2 * p.T + kKT - 1;
+    const long long tiles = p.t_log2 >= 0 ? floor_sum_128(i, p.t_log2 + 1, b) : floor_sum(i, kKT, 2 * p.T, b);
+    return kWideCost * tiles + (long long)kItemCost * i;
+  }
+  __device__ bool wide(const ExtendParams& p, int i) const { return n - i * 2 * p.T > p.T; }
+  __device__ int tiles(const ExtendParams& p, int i) const {  // K/V tiles of item i
+    return (past + min(n, (i + 1) * 2 * p.T) + kKT - 1) / kKT;
+  }
+  __device__ long long cost(const ExtendParams& p) const {  // of one head group
+    if (n == 0) return 0;
+    return cost_before(p, items - 1) + kItemCost + (wide(p, items - 1) ? kWideCost : kNarrowCost) * (long long)tiles(p, items - 1);
+  }
+};
+
+// Teams that the list of long chunks is divided over; the thin sequences have the other SMs, so that neither kernel waits
+// for the other (one thread block of either fits an SM): what a step of both kinds saves is one start, one end and one
+// uneven finish (a chunk of 512 rows next to 15 single ones over 0.5k-4k tokens, 16/2/4 heads: 74 -> 65 us).  The weight
+// of a thin tile, 0.3 + 0.48 units for each of its K and V tiles, is the middle of what was fastest for seven mixtures of
+// 64 and 128 channels; a third more or less costs up to a tenth, far too little or too much twice the time.
+__device__ __forceinline__ int wide_teams(const ExtendParams& p, long long wide, long long thin) {
+  if (wide == 0) return 0;
+  int n = p.n_teams;
+  if (thin > 0 && n > 1) {
+    const float w = (float)wide * p.team, t = (float)thin * p.thin_weight;
+    n = min(max((int)(n * (w / (w + t)) + 0.5f), 1), n - 1);
+  }
+  return shares(wide, n, kItemCost + kWideCost);
+}
+__device__ __forceinline__ int thin_blocks_left(const ExtendParams& p, int wide_teams) {
+  const int left = p.blocks - wide_teams * p.team;
+  return left > 0 ? left : p.blocks;  // one team alone: the lists one after the other
+}
 constexpr int kExtendThinThreads = 576;
 cudaError_t launch_extend_thin(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const ExtendParams& p,
                                int d_qk, int d_v, int blocks, bool second, cudaStream_t stream);

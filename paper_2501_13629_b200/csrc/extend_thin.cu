@@ -100,20 +100,17 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     return;
   }
   if (p.first) ptx::grid_launch_dependents();
-  auto load = [&](int b, int& lo, int& n, int& past) -> int {  // tiles of one unit of sequence b
-    load_rows(p, b, lo, n, past);
-    return n > 0 && n <= p.thin_max ? (past + n + kKT - 1) / kKT : 0;
-  };
   const int per_thread = (p.batch + kExtendThinThreads - 1) / kExtendThinThreads;
   const int b_lo = min(tid * per_thread, p.batch), b_hi = min(b_lo + per_thread, p.batch);
-  int my_lo = 0, my_n = 0, my_past = 0;  // of the thread's first sequence: there is seldom another
-  const int my_nt = b_lo < b_hi ? load(b_lo, my_lo, my_n, my_past) : 0;
+  Seq my = {};  // the thread's first sequence: there is seldom another
+  if (b_lo < b_hi) my.load(p, b_lo);
   auto tiles_of = [&](int b) -> int {
-    int lo, n, past;
-    return b == b_lo ? my_nt : load(b, lo, n, past);
+    Seq s = my;
+    if (b > b_lo) s.load(p, b);
+    return s.thin_tiles;
   };
   {  // a step without thin sequences (prompts): nothing to do here
-    bool any = my_nt > 0;
+    bool any = my.thin_tiles > 0;
     for (int b = b_lo + 1; b < b_hi; ++b) any |= tiles_of(b) > 0;
     if (!__syncthreads_or(any)) {
       if (tid == 0) p.list.meta[blockIdx.x].rows = 0;
@@ -156,14 +153,17 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   // ---- this block's range of the flat list of tiles
   long long* scan = reinterpret_cast<long long*>(&sc.part[0][0][0]);  // tiles, then chunks, of every warp's sequences
   int* scan_items = reinterpret_cast<int*>(scan + kExtendThinThreads / 32);
-  long long mine = 0;
+  long long* scan_others = reinterpret_cast<long long*>(scan_items + kExtendThinThreads / 32);
+  long long mine = 0, others = 0;  // others: the list of long chunks
   int items = 0;
   for (int b = b_lo; b < b_hi; ++b) {
-    const int nt = tiles_of(b);
-    if (nt > 0) {
-      mine += (long long)p.n_units * (nt + kThinItemCost);
+    Seq s = my;
+    if (b > b_lo) s.load(p, b);
+    if (s.thin_tiles > 0) {
+      mine += (long long)p.n_units * (s.thin_tiles + kThinItemCost);
       items += p.n_units;
     }
+    if (s.n > 0) others += p.n_units * s.cost(p);
   }
   auto warp_scan = [&](long long x) -> long long {  // inclusive
 #pragma unroll
@@ -175,30 +175,43 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   };
   long long incl = warp_scan(mine);
   items = __reduce_add_sync(0xffffffffu, items);
-  if (lane == 31) { scan[warp] = incl; scan_items[warp] = items; }
+  if (__any_sync(0xffffffffu, others > 0)) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) others += __shfl_xor_sync(0xffffffffu, others, o);
+  }
+  if (lane == 31) { scan[warp] = incl; scan_items[warp] = items; scan_others[warp] = others; }
   tc::fence_before_sync();
   __syncthreads();
   tc::fence_after_sync();
   const uint32_t tmem = sc.tmem;
   long long before = 0, total = 0;
   items = 0;
+  others = 0;
 #pragma unroll
   for (int w = 0; w < kExtendThinThreads / 32; ++w) {
     if (w < warp) before += scan[w];
     total += scan[w];
     items += scan_items[w];
+    others += scan_others[w];
+  }
+  const int grid = others > 0 ? thin_blocks_left(p, wide_teams(p, others, total)) : p.blocks;  // the other kernel leaves
+  if ((int)blockIdx.x >= grid) {
+    if (tid == 0) p.list.meta[blockIdx.x].rows = 0;
+    if (warp == 1) tc::tmem_dealloc(tmem, kTmemCols);
+    ptx::grid_dependency_wait();
+    return;
   }
   // Equal shares of the list, cut wherever they end; or, where that costs no block more than four tiles, equal chunks
   // that begin with their item: sum ceil(nt / chunk) <= total / chunk + items <= blocks, so every block has one
   // segment at most.  (A segment costs about as much as five tiles next to its tiles, and short lists would give most
   // blocks two: 8 x ~700 tokens, 32/4/16 heads of 64, 31 -> 22 us.)
   int chunk = 0;
-  if (items > 0 && items < (int)gridDim.x && total < (1ll << 22)) {
+  if (items > 0 && items < grid && total < (1ll << 22)) {
     const uint32_t tiles = (uint32_t)total - items * kThinItemCost;
-    chunk = (int)((tiles + gridDim.x - items - 1) / (gridDim.x - items));
-    if (chunk > (int)(tiles / gridDim.x) + 4) chunk = 0;
+    chunk = (int)((tiles + grid - items - 1) / (grid - items));
+    if (chunk > (int)(tiles / grid) + 4) chunk = 0;
   }
-  const int blocks = shares(total, gridDim.x, kThinItemCost + 1);  // that take part
+  const int blocks = shares(total, grid, kThinItemCost + 1);  // that take part
   long long w0 = total, w1 = total;
   if ((int)blockIdx.x < blocks) {
     w0 = share_start(total, blockIdx.x, blocks);
@@ -254,6 +267,10 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     uint32_t kph = 0, vph = 0;
     bool ok = true;
     ExtendMeta m = {};
+    auto load = [&](int b, int& lo, int& n, int& past) -> int {  // tiles of one unit of sequence b
+      load_rows(p, b, lo, n, past);
+      return n > 0 && n <= p.thin_max ? (past + n + kKT - 1) / kKT : 0;
+    };
     auto hand_out = [&](const ThinSegment& d) -> bool {
       const int s = segs % kSegRing;
       if (!wait_warp(seg_empty0 + 8 * s, ((segs / kSegRing) & 1) ^ 1, abort_flag)) return false;
