@@ -794,45 +794,43 @@ constexpr int kCombineThreads = 256, kCombineBlocks = 3;  // per SM
 template <int kD>
 __global__ void __launch_bounds__(kCombineThreads, kCombineBlocks)
 extend_combine_kernel(const ExtendParams p, const ExtendList thin, const int thin_blocks, const int wide_blocks) {
-  constexpr int kLanes = kD / 4, kGroups = kCombineThreads / kLanes, kItems = 2 * kMaxBlocks;
-  constexpr int kPerLane = kItems / 32;
+  constexpr int kLanes = kD / 8, kGroups = kCombineThreads / kLanes, kItems = 2 * kMaxBlocks;
   __shared__ int start_s[kItems + 1];  // bundles of rows in the items before this one
-  __shared__ int bundle_s;
+  __shared__ uint64_t scan_s[kCombineThreads / 32];
   const int lane = threadIdx.x % kLanes;
   ptx::grid_dependency_wait();
   const int items = thin_blocks + wide_blocks;
   auto meta_of = [&](int x) { return x < thin_blocks ? thin.meta + x : p.list.meta + (x - thin_blocks); };
-  for (int x = threadIdx.x; x < kItems; x += kCombineThreads) {
-    const ExtendMeta* m = meta_of(x);
-    start_s[x + 1] = x < items ? m->rows : 0;
-  }
-  __syncthreads();
-  if (threadIdx.x < 32) {
-    int* mine = start_s + 1 + threadIdx.x * kPerLane;
-    int sum = 0;
-    for (int i = 0; i < kPerLane; ++i) sum += mine[i];
-    // four rows a bundle where there are many (one search for all, loads in flight together), else one
-    const int bundle = (int)__reduce_add_sync(0xffffffffu, sum) > 2 * (int)gridDim.x * kGroups ? 4 : 1;
-    sum = 0;
-    for (int i = 0; i < kPerLane; ++i) sum += (mine[i] + bundle - 1) / bundle;
-    int at = sum;
+  // four rows a bundle where there are many (one search for all, loads in flight together), else one: both counts in a scan
+  static_assert(kItems == 2 * kCombineThreads, "two items a thread");
+  uint64_t sum = 0;
+  int rows[2];
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, at, o);
-      if ((int)threadIdx.x >= o) at += y;
-    }
-    at -= sum;
-    if (threadIdx.x == 0) {
-      start_s[0] = 0;
-      bundle_s = bundle;
-    }
-    for (int i = 0; i < kPerLane; ++i) {
-      at += (mine[i] + bundle - 1) / bundle;
-      mine[i] = at;
-    }
+  for (int y = 0; y < 2; ++y) {
+    const int x = 2 * threadIdx.x + y;
+    rows[y] = x < items ? meta_of(x)->rows : 0;
+    sum += (uint64_t)rows[y] << 32 | (uint32_t)((rows[y] + 3) >> 2);
   }
+  const uint64_t mine = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint64_t y = __shfl_up_sync(0xffffffffu, sum, o);
+    if ((int)(threadIdx.x % 32) >= o) sum += y;
+  }
+  if (threadIdx.x % 32 == 31) scan_s[threadIdx.x / 32] = sum;
   __syncthreads();
-  const int bundle = bundle_s;
+  uint64_t total = 0;
+  sum -= mine;
+#pragma unroll
+  for (int w = 0; w < kCombineThreads / 32; ++w) {
+    if (w < (int)threadIdx.x / 32) sum += scan_s[w];
+    total += scan_s[w];
+  }
+  const int bundle = (int)(total >> 32) > 2 * (int)gridDim.x * kGroups ? 4 : 1;
+  start_s[2 * threadIdx.x] = (int)(bundle == 4 ? sum : sum >> 32);
+  start_s[2 * threadIdx.x + 1] = start_s[2 * threadIdx.x] + (bundle == 4 ? (rows[0] + 3) >> 2 : rows[0]);
+  if (threadIdx.x == 0) start_s[kItems] = (int)(bundle == 4 ? total : total >> 32);
+  __syncthreads();
   const int bundles = start_s[kItems];
   for (int g = blockIdx.x * kGroups + threadIdx.x / kLanes; g < bundles; g += gridDim.x * kGroups) {
     int x = 0, z = kItems;  // the item: the last that begins at or before bundle g
@@ -843,63 +841,87 @@ extend_combine_kernel(const ExtendParams p, const ExtendList thin, const int thi
     const bool first_list = x < thin_blocks;
     const ExtendList& list = first_list ? thin : p.list;
     const ExtendMeta m = *meta_of(x);
-    const int block = first_list ? x : x - thin_blocks;
     // the parts lie one team apart, the first in its block's second slot, the others in the first: in order, so that sums
-    // do not depend on timing
-    const long long slot0 = 2LL * block + 1, step = 2LL * list.team;  // part i > 0: slot0 - 1 + i step
-    const int r0 = bundle * (g - start_s[x]), last = min(r0 + bundle, m.rows) - 1;
+    // do not depend on timing.  A slot's number, and any row's, fits 32 bits: 2 kMaxBlocks slots of at most 2 kRows rows.
+    const uint32_t slot0 = 2 * (first_list ? x : x - thin_blocks), step = 2 * list.team * list.slot_rows;
+    const int r0 = bundle * (g - start_s[x]), end = min(r0 + bundle, m.rows);
+    int part = r0 / m.part_rows, lr = r0 - part * m.part_rows, tok = lr / p.G, head = lr - tok * p.G;
 #pragma unroll 1
-    for (int r = r0; r <= last; r += 2) {  // two rows at a time
+    for (int r = r0; r < end; r += 2) {  // two rows at a time
+      const int second = r + 1 < end;
+      const uint32_t at1 = slot0 * list.slot_rows + r, at0 = at1 + list.slot_rows;  // first part's, and before the others'
       float top[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f};
-      float4 acc[2];
-      acc[0] = acc[1] = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int i = 0; i < m.parts; i += 4) {
-        float ls[4][2];
-        float4 o[4][2];
+      float4 acc[2][2];
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
+      for (int h = 0; h < 2; ++h) acc[h][0] = acc[h][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+      for (int i = 0; i < m.parts; i += 2) {
+        float ls[2][2];
+        float4 o[2][2][2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          ls[y][0] = ls[y][1] = -INFINITY;
           if (i + y < m.parts) {
-            const long long at = (i + y == 0 ? slot0 : slot0 - 1 + (i + y) * step) * list.slot_rows;
+            const uint32_t at = i + y == 0 ? at0 : at1 + (i + y) * step;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-              const int row = min(r + h, last);
-              ls[y][h] = list.part_lse[at + row];
-              o[y][h] = *reinterpret_cast<const float4*>(list.part_o + (at + row) * kD + lane * 4);
+              const uint32_t row = at + (h == 0 ? 0 : second);
+              ls[y][h] = list.part_lse[row];
+              const float4* src = reinterpret_cast<const float4*>(list.part_o + (size_t)row * kD) + lane * 2;
+              o[y][h][0] = src[0];
+              o[y][h][1] = src[1];
             }
-          } else {
-            ls[y][0] = ls[y][1] = -INFINITY;
           }
         }
 #pragma unroll
-        for (int y = 0; y < 4; ++y) {
+        for (int y = 0; y < 2; ++y) {
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             if (ls[y][h] == -INFINITY) continue;  // the part saw no token of this row (and may have left no values)
             const float up = fmaxf(top[h], ls[y][h]);
-            const float was = exp2f(top[h] - up), f = exp2f(ls[y][h] - up);
+            const float was = ex2(top[h] - up), f = ex2(ls[y][h] - up);
             top[h] = up;
-            sum[h] = sum[h] * was + f;
-            acc[h].x = fmaf(f, o[y][h].x, acc[h].x * was);
-            acc[h].y = fmaf(f, o[y][h].y, acc[h].y * was);
-            acc[h].z = fmaf(f, o[y][h].z, acc[h].z * was);
-            acc[h].w = fmaf(f, o[y][h].w, acc[h].w * was);
+            sum[h] = fmaf(sum[h], was, f);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              acc[h][e].x = fmaf(f, o[y][h][e].x, acc[h][e].x * was);
+              acc[h][e].y = fmaf(f, o[y][h][e].y, acc[h][e].y * was);
+              acc[h][e].z = fmaf(f, o[y][h][e].z, acc[h][e].z * was);
+              acc[h][e].w = fmaf(f, o[y][h][e].w, acc[h][e].w * was);
+            }
           }
         }
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        if (r + h > last) break;
+        if (h == 1 && !second) break;
         const float inv = sum[h] > 0.f ? 1.f / sum[h] : 0.f;
-        const int part = (r + h) / m.part_rows, lr = r + h - part * m.part_rows, tok = lr / p.G;
-        const long long row = (long long)(m.row_lo + tok) * p.n_q + m.head0 + part * p.G + (lr - tok * p.G);
+        const long long row = (long long)(m.row_lo + tok) * p.n_q + m.head0 + part * p.G + head;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          acc[h][e].x *= inv;
+          acc[h][e].y *= inv;
+          acc[h][e].z *= inv;
+          acc[h][e].w *= inv;
+        }
         if (p.out_is_f32) {
-          *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + row * kD + lane * 4) =
-              make_float4(acc[h].x * inv, acc[h].y * inv, acc[h].z * inv, acc[h].w * inv);
+          float4* dst = reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + row * kD) + lane * 2;
+          dst[0] = acc[h][0];
+          dst[1] = acc[h][1];
         } else {
-          *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(p.out) + row * kD + lane * 4) =
-              make_uint2(pack2(acc[h].x * inv, acc[h].y * inv), pack2(acc[h].z * inv, acc[h].w * inv));
+          reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.out) + row * kD)[lane] =
+              make_uint4(pack2(acc[h][0].x, acc[h][0].y), pack2(acc[h][0].z, acc[h][0].w), pack2(acc[h][1].x, acc[h][1].y),
+                         pack2(acc[h][1].z, acc[h][1].w));
         }
         if (p.lse && lane == 0) p.lse[row] = sum[h] > 0.f ? (top[h] + log2f(sum[h])) * kLn2 : -INFINITY;
+        if (++head == p.G) {
+          head = 0;
+          ++tok;
+        }
+        if (++lr == m.part_rows) {  // the next head group of the item
+          lr = tok = head = 0;
+          ++part;
+        }
       }
     }
   }
