@@ -102,6 +102,14 @@ def test_pairs_and_parts_of_the_head(api, dtype, interleaved, d_qk, rot):
     run(api, step.fill(whole=False), rot, interleaved, magnitude=1.0 if rot != 64 else 1.2079)
 
 
+@pytest.mark.parametrize("dtype,d_qk,rot", [(F32, 2048, 2048), (BF16, 4096, 512), (F32, 1100, 1096), (BF16, 8192, 8192)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_heads_of_very_many_channels(api, dtype, d_qk, rot, interleaved):
+    """More vectors to a head than a block has threads."""
+    step = Step(api, [2, 0], [3, 2], 2, 1, 2, d_qk, 512, dtype=dtype, pad=1, seed=rot)
+    run(api, step.fill(whole=False), rot, interleaved)
+
+
 @pytest.mark.parametrize("layout,page", [("paged", 16), ("token", 16), ("flat", 16), ("paged", 24), ("paged", 1),
                                          ("paged", 256)])
 def test_layouts(api, layout, page):
