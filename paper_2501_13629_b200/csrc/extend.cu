@@ -418,7 +418,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     constexpr uint32_t idesc = tc::idesc_bf16_f32(kRows, kKT, 0, 0);    // S: Q and K both K-major, N = 128 tokens
     constexpr uint32_t idesc_pv = tc::idesc_bf16_f32(kRows, kD, 0, 1);  // O: V is N-major, N = kD channels
     constexpr uint32_t hi = tc::smem_desc_hi_sw128(1024);
-    if (lane == 0) {
+    if (ptx::elect_one()) {
       bool ok = true;
       const uint32_t q_lo = tc::smem_desc_lo(q_u32, 16), k_lo = tc::smem_desc_lo(k_u32, 16);
       const uint32_t v_lo = tc::smem_desc_lo(v_u32, kKT * 128);  // 64-channel chunks of V are one half tile apart

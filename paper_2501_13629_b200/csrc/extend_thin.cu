@@ -423,7 +423,7 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer (one thread)
     constexpr uint32_t hi = tc::smem_desc_hi_sw128(1024);
-    if (lane == 0) {
+    if (ptx::elect_one()) {
       const uint32_t q_lo = tc::smem_desc_lo(ptx::smem_u32(q_s), 16), r_lo = tc::smem_desc_lo(ptx::smem_u32(ring_s), 16);
       // V^T: the two 64-channel chunks of M are half a tile apart.  With 64 channels they are the tiles of two V heads,
       // neighbours in the ring of V (whose length is even then, so that a pair never wraps), or the same
