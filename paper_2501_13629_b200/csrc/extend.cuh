@@ -144,11 +144,12 @@ __device__ __forceinline__ long long floor_sum_128(int n, int s, int b) {
 // One sequence of the step as the list of long chunks has it.
 struct Seq {
   int lo, n, past, items;  // first row, rows (0: not in this list), tokens cached before, items per head group
-  int thin_tiles;          // tiles of one unit of the other list (0: not in that one)
+  int rows, thin_tiles;    // rows in either list; tiles of one unit of the other list (0: not in that one)
   bool bad;                // does not fit
   __device__ void load(const ExtendParams& p, int b) {
     bad = !load_rows(p, b, lo, n, past);
     thin_tiles = items = 0;
+    rows = n;
     if (n > p.thin_max) {
       items = (n + 2 * p.T - 1) / (2 * p.T);
     } else {

@@ -52,7 +52,7 @@ struct Scratch {
   uint64_t bars[42];
   ThinSegment seg[kSegRing];
   long long seek_lo;
-  int seek_b;
+  int seek_b, seek_row, seek_n, seek_past;  // the sequence that this block begins with
   uint32_t tmem;
   int abort;
 };
@@ -211,12 +211,8 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     chunk = (int)((tiles + grid - items - 1) / (grid - items));
     if (chunk > (int)(tiles / grid) + 4) chunk = 0;
   }
-  const int blocks = shares(total, grid, kThinItemCost + 1);  // that take part
+  int blocks = 0;  // that take part
   long long w0 = total, w1 = total;
-  if ((int)blockIdx.x < blocks) {
-    w0 = share_start(total, blockIdx.x, blocks);
-    w1 = share_start(total, blockIdx.x + 1, blocks);
-  }
   if (chunk > 0) {
     __syncthreads();  // everybody has read the sums
     mine = 0;
@@ -233,15 +229,26 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     }
     w0 = blockIdx.x;
     w1 = w0 < chunks ? w0 + 1 : w0;
+  } else {
+    blocks = shares(total, grid, kThinItemCost + 1);
+    if ((int)blockIdx.x < blocks) {
+      w0 = share_start(total, blockIdx.x, blocks);
+      w1 = share_start(total, blockIdx.x + 1, blocks);
+    }
   }
   {
     long long at = before + incl - mine;
     if (w0 < w1 && at <= w0 && w0 < at + mine)
       for (int b = b_lo; b < b_hi; ++b) {
-        const int nt = tiles_of(b);
+        Seq s = my;
+        if (b > b_lo) s.load(p, b);
+        const int nt = s.thin_tiles;
         const long long c = nt == 0 ? 0 : (long long)p.n_units * (chunk > 0 ? (nt + chunk - 1) / chunk : nt + kThinItemCost);
         if (w0 < at + c) {
           sc.seek_b = b;
+          sc.seek_row = s.lo;
+          sc.seek_n = s.rows;
+          sc.seek_past = s.past;
           sc.seek_lo = at;
           break;
         }
@@ -282,10 +289,10 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       return true;
     };
     int chunk_lo = 0;
-    int b = sc.seek_b, lo = 0, n = 0, past = 0, nt = 0, u = 0;
+    int b = sc.seek_b, lo = sc.seek_row, n = sc.seek_n, past = sc.seek_past, nt = 0, u = 0;
     long long item_lo = sc.seek_lo;
     if (w0 < w1) {
-      nt = load(b, lo, n, past);
+      nt = (past + n + kKT - 1) / kKT;
       const long long in = w0 - item_lo;
       if (chunk > 0) {  // chunk `in` of the sequence: a range of one item, counted from the item's start
         const int per = (nt + chunk - 1) / chunk;
@@ -293,7 +300,7 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         chunk_lo = ((int)in - u * per) * chunk;
       } else {
         const int size = nt + kThinItemCost;
-        u = in < (1ll << 31) ? (int)((uint32_t)in / (uint32_t)size) : (int)(in / size);
+        u = (int)quotient(in, size);
         item_lo += (long long)u * size;
       }
     } else {
