@@ -182,9 +182,9 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   {  // a step of thin sequences alone (decode): nothing to do here
     bool any = my.n > 0 || my.bad;
     for (int b = b_lo + 1; b < b_hi; ++b) {
-      Seq s;
-      s.load(p, b);
-      any |= s.n > 0 || s.bad;
+      Seq x;
+      x.load(p, b);
+      any |= x.n > 0 || x.bad;
     }
     if (!__syncthreads_or(any)) {
       if (tid == 0) p.list.meta[blockIdx.x].rows = 0;
@@ -230,40 +230,24 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     tc::tmem_relinquish();
   }
   // ---- this block's range of the flat list: every thread sums the cost of its share of the sequences
-  long long mine = 0, others = 0;
-  for (int b = b_lo; b < b_hi; ++b) {
-    Seq s = my;
-    if (b > b_lo) s.load(p, b);
+  long long mine = 0, others = 0, total;
+  bool any_thin = false;
+  Seq s = my;
+  for (int b = b_lo; b < b_hi;) {
     if (s.bad && blockIdx.x == 0) report(p.dev_status, DIFFQKV_ERR_INDEX);
-    mine += p.n_units * s.cost(p);
-    if (s.thin_tiles > 0) others += (long long)p.n_units * (s.thin_tiles + kThinItemCost);
-  }
-  long long incl = mine;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += y;
-  }
-  if (__any_sync(0xffffffffu, others > 0)) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) others += __shfl_xor_sync(0xffffffffu, others, o);
-  }
-  if (lane == 31) {
-    scan_s[warp] = incl;
-    others_s[warp] = others;
+    if (s.n > 0) mine += p.n_units * s.cost(p);
+    if (s.thin_tiles > 0) {
+      others += (long long)p.n_units * (s.thin_tiles + kThinItemCost);
+      any_thin = true;
+    }
+    if (++b < b_hi) s.load(p, b);
   }
   tc::fence_before_sync();
-  __syncthreads();
+  any_thin = __syncthreads_or(any_thin);
+  long long before = block_scan<kExtendThreads / 32>(mine, scan_s, total);
   tc::fence_after_sync();
   const uint32_t tmem_base = *tmem_slot;
-  long long before = 0, total = 0;
-  others = 0;
-#pragma unroll
-  for (int w = 0; w < kExtendThreads / 32; ++w) {
-    if (w < warp) before += scan_s[w];
-    total += scan_s[w];
-    others += others_s[w];
-  }
+  if (any_thin) block_scan<kExtendThreads / 32>(others, others_s, others);
   const int team = (int)blockIdx.x / p.list.team, member = (int)blockIdx.x - team * p.list.team;
   const int n_teams = wide_teams(p, total, others);  // that take part
   if (team >= n_teams) {
@@ -273,20 +257,19 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     return;
   }
   const long long w0 = share_start(total, team, n_teams), w1 = share_start(total, team + 1, n_teams);
-  {
-    long long at = before + incl - mine;
-    if (w0 < w1 && at <= w0 && w0 < at + mine)
-      for (int b = b_lo; b < b_hi; ++b) {
-        Seq s = my;
-        if (b > b_lo) s.load(p, b);
-        const long long c = p.n_units * s.cost(p);
-        if (w0 < at + c) {
-          seek_b_s = b;
-          seek_lo_s = at;
-          break;
-        }
-        at += c;
+  if (w0 < w1 && before <= w0 && w0 < before + mine) {
+    s = my;
+    for (int b = b_lo;;) {
+      const long long c = p.n_units * s.cost(p);
+      if (w0 < before + c) {
+        seek_b_s = b;
+        seek_lo_s = before;
+        break;
       }
+      before += c;
+      if (++b >= b_hi) break;
+      s.load(p, b);
+    }
   }
   __syncthreads();
   const uint32_t q_u32 = ptx::smem_u32(q_s), k_u32 = ptx::smem_u32(k_s), v_u32 = ptx::smem_u32(v_s);

@@ -141,6 +141,28 @@ __device__ __forceinline__ long long floor_sum_128(int n, int s, int b) {
   };
   return upto(e + n) - upto(e);
 }
+// Inclusive sum over the lanes.  Not inlined either.
+static __device__ __noinline__ long long warp_scan(long long x) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  return x;
+}
+// Sum over the threads before this one, and over all, of a block of at most 32 warps; a word per warp in s, which a
+// barrier of the caller's separates from the call before.  Holds a barrier.
+template <int kWarps>
+__device__ __forceinline__ long long block_scan(long long mine, long long* s, long long& total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const long long incl = warp_scan(mine);
+  if (lane == 31) s[warp] = incl;
+  __syncthreads();
+  const long long x = lane < kWarps ? s[lane] : 0, all = warp_scan(x);
+  total = __shfl_sync(0xffffffffu, all, 31);
+  return incl - mine + __shfl_sync(0xffffffffu, all - x, warp);
+}
 // One sequence of the step as the list of long chunks has it.
 struct Seq {
   int lo, n, past, items;  // first row, rows (0: not in this list), tokens cached before, items per head group

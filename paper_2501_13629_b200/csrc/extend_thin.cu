@@ -104,19 +104,17 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   const int b_lo = min(tid * per_thread, p.batch), b_hi = min(b_lo + per_thread, p.batch);
   Seq my = {};  // the thread's first sequence: there is seldom another
   if (b_lo < b_hi) my.load(p, b_lo);
-  auto tiles_of = [&](int b) -> int {
-    Seq s = my;
-    if (b > b_lo) s.load(p, b);
-    return s.thin_tiles;
-  };
-  {  // a step without thin sequences (prompts): nothing to do here
-    bool any = my.thin_tiles > 0;
-    for (int b = b_lo + 1; b < b_hi; ++b) any |= tiles_of(b) > 0;
-    if (!__syncthreads_or(any)) {
-      if (tid == 0) p.list.meta[blockIdx.x].rows = 0;
-      ptx::grid_dependency_wait();
-      return;
-    }
+  bool any = my.thin_tiles > 0;
+  for (int b = b_lo + 1; b < b_hi; ++b) {
+    Seq s;
+    s.load(p, b);
+    any |= s.thin_tiles > 0;
+  }
+  const int busy_threads = __syncthreads_count(any);
+  if (busy_threads == 0) {  // a step without thin sequences (prompts): nothing to do here
+    if (tid == 0) p.list.meta[blockIdx.x].rows = 0;
+    ptx::grid_dependency_wait();
+    return;
   }
   if (tid == 0) {
     sc.abort = 0;
@@ -151,50 +149,25 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     tc::tmem_relinquish();
   }
   // ---- this block's range of the flat list of tiles
-  long long* scan = reinterpret_cast<long long*>(&sc.part[0][0][0]);  // tiles, then chunks, of every warp's sequences
-  int* scan_items = reinterpret_cast<int*>(scan + kExtendThinThreads / 32);
-  long long* scan_others = reinterpret_cast<long long*>(scan_items + kExtendThinThreads / 32);
-  long long mine = 0, others = 0;  // others: the list of long chunks
-  int items = 0;
-  for (int b = b_lo; b < b_hi; ++b) {
-    Seq s = my;
-    if (b > b_lo) s.load(p, b);
-    if (s.thin_tiles > 0) {
-      mine += (long long)p.n_units * (s.thin_tiles + kThinItemCost);
-      items += p.n_units;
+  long long* scan = reinterpret_cast<long long*>(&sc.part[0][0][0]);  // per warp: tiles, the other list's, chunks
+  long long mine = 0, others = 0, total;  // others: the list of long chunks
+  bool any_long = false;
+  Seq s = my;
+  for (int b = b_lo; b < b_hi;) {
+    if (s.thin_tiles > 0) mine += (long long)p.n_units * (s.thin_tiles + kThinItemCost);
+    if (s.n > 0) {
+      others += p.n_units * s.cost(p);
+      any_long = true;
     }
-    if (s.n > 0) others += p.n_units * s.cost(p);
+    if (++b < b_hi) s.load(p, b);
   }
-  auto warp_scan = [&](long long x) -> long long {  // inclusive
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
-    }
-    return x;
-  };
-  long long incl = warp_scan(mine);
-  items = __reduce_add_sync(0xffffffffu, items);
-  if (__any_sync(0xffffffffu, others > 0)) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) others += __shfl_xor_sync(0xffffffffu, others, o);
-  }
-  if (lane == 31) { scan[warp] = incl; scan_items[warp] = items; scan_others[warp] = others; }
   tc::fence_before_sync();
-  __syncthreads();
+  any_long = __syncthreads_or(any_long);
+  long long before = block_scan<kExtendThinThreads / 32>(mine, scan, total);
   tc::fence_after_sync();
   const uint32_t tmem = sc.tmem;
-  long long before = 0, total = 0;
-  items = 0;
-  others = 0;
-#pragma unroll
-  for (int w = 0; w < kExtendThinThreads / 32; ++w) {
-    if (w < warp) before += scan[w];
-    total += scan[w];
-    items += scan_items[w];
-    others += scan_others[w];
-  }
-  const int grid = others > 0 ? thin_blocks_left(p, wide_teams(p, others, total)) : p.blocks;  // the other kernel leaves
+  if (any_long) block_scan<kExtendThinThreads / 32>(others, scan + 32, others);
+  const int grid = any_long ? thin_blocks_left(p, wide_teams(p, others, total)) : p.blocks;  // the other kernel leaves
   if ((int)blockIdx.x >= grid) {
     if (tid == 0) p.list.meta[blockIdx.x].rows = 0;
     if (warp == 1) tc::tmem_dealloc(tmem, kTmemCols);
@@ -206,7 +179,8 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   // segment at most.  (A segment costs about as much as five tiles next to its tiles, and short lists would give most
   // blocks two: 8 x ~700 tokens, 32/4/16 heads of 64, 31 -> 22 us.)
   int chunk = 0;
-  if (items > 0 && items < grid && total < (1ll << 22)) {
+  const int items = per_thread == 1 ? min(busy_threads * p.n_units, grid) : grid;
+  if (items < grid && total < (1ll << 22)) {
     const uint32_t tiles = (uint32_t)total - items * kThinItemCost;
     chunk = (int)((tiles + grid - items - 1) / (grid - items));
     if (chunk > (int)(tiles / grid) + 4) chunk = 0;
@@ -214,19 +188,9 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   int blocks = 0;  // that take part
   long long w0 = total, w1 = total;
   if (chunk > 0) {
-    __syncthreads();  // everybody has read the sums
-    mine = 0;
-    for (int b = b_lo; b < b_hi; ++b) mine += (long long)p.n_units * ((tiles_of(b) + chunk - 1) / chunk);
-    incl = warp_scan(mine);
-    if (lane == 31) scan[warp] = incl;
-    __syncthreads();
-    before = 0;
-    long long chunks = 0;
-#pragma unroll
-    for (int w = 0; w < kExtendThinThreads / 32; ++w) {
-      if (w < warp) before += scan[w];
-      chunks += scan[w];
-    }
+    long long chunks;
+    mine = (long long)p.n_units * ((my.thin_tiles + chunk - 1) / chunk);
+    before = block_scan<kExtendThinThreads / 32>(mine, scan + 64, chunks);
     w0 = blockIdx.x;
     w1 = w0 < chunks ? w0 + 1 : w0;
   } else {
@@ -236,24 +200,23 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       w1 = share_start(total, blockIdx.x + 1, blocks);
     }
   }
-  {
-    long long at = before + incl - mine;
-    if (w0 < w1 && at <= w0 && w0 < at + mine)
-      for (int b = b_lo; b < b_hi; ++b) {
-        Seq s = my;
-        if (b > b_lo) s.load(p, b);
-        const int nt = s.thin_tiles;
-        const long long c = nt == 0 ? 0 : (long long)p.n_units * (chunk > 0 ? (nt + chunk - 1) / chunk : nt + kThinItemCost);
-        if (w0 < at + c) {
-          sc.seek_b = b;
-          sc.seek_row = s.lo;
-          sc.seek_n = s.rows;
-          sc.seek_past = s.past;
-          sc.seek_lo = at;
-          break;
-        }
-        at += c;
+  if (w0 < w1 && before <= w0 && w0 < before + mine) {
+    s = my;
+    for (int b = b_lo;;) {
+      const int nt = s.thin_tiles;
+      const long long c = nt == 0 ? 0 : (long long)p.n_units * (chunk > 0 ? (nt + chunk - 1) / chunk : nt + kThinItemCost);
+      if (w0 < before + c) {
+        sc.seek_b = b;
+        sc.seek_row = s.lo;
+        sc.seek_n = s.rows;
+        sc.seek_past = s.past;
+        sc.seek_lo = before;
+        break;
       }
+      before += c;
+      if (++b >= b_hi) break;
+      s.load(p, b);
+    }
   }
   __syncthreads();
 
