@@ -11,9 +11,10 @@
 // per element the fp64 steps and the sincos would cost more than the traffic).  Its threads move 16-byte vectors, for
 // rotate-half pairs the two that hold a channel and its partner; a thread keeps its channels, so that their turns stay in
 // registers, and goes from head to head.  The first vectors are read before the row's sequence is known.
-// 11.8k rows of 32/4/8 heads of 128 channels, 64 of them turned, bf16 (245 MB): 52 us, 4.7 TB/s; 56 us without the reads
-// ahead and with a quotient for every vector, 60 us with several rows to a block one after the other.  16 rows: 3.4 us,
-// of which a launch is most.
+// 10.9k rows of 32/4/8 heads of 128 channels, 64 of them turned, bf16 (245 MB): 42 us, 5.9 TB/s.  256 threads took 52 us
+// (half the vectors for the same addresses to work out, 3.2 instructions a cycle), without the reads ahead and with a
+// quotient for every vector it was 56 us, with several rows to a block one after the other 60.  16 rows: 3.3 us, of which
+// a launch is most.
 #include <cmath>
 
 #include "common.cuh"
@@ -21,7 +22,7 @@
 namespace diffqkv {
 namespace {
 
-constexpr int kRopeThreads = 256;
+constexpr int kRopeThreads = 128;
 
 struct RopeParams {
   const void* q;
@@ -84,10 +85,10 @@ __device__ __forceinline__ float reduced_angle(int pos, double f) {
 
 // kPairs: rotate-half, a vector and the one half a rotation further on together.
 template <typename T, bool kPairs>
-__global__ void __launch_bounds__(kRopeThreads, kPairs ? 4 : 5) rope_append_kernel(const RopeParams p) {
+__global__ void __launch_bounds__(kRopeThreads, kPairs ? 6 : 8) rope_append_kernel(const RopeParams p) {
   constexpr int N = Pack<T>::N;
   constexpr int kVec = kPairs ? 2 : 1;       // vectors of a task
-  constexpr int kAhead = kPairs ? 2 : 3;     // tasks read together
+  constexpr int kAhead = kPairs ? 3 : 5;     // tasks read together
   constexpr int kTurns = kPairs ? N : N / 2;
   extern __shared__ float2 turn_s[];  // [rot / 2] (cos, sin) * magnitude
   const int tid = threadIdx.x;
