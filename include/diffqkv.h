@@ -354,10 +354,11 @@ diffqkv_status diffqkv_decode_topk_ids(const void *q, const diffqkv_cache *cache
  *   workspace  diffqkv_extend_workspace_bytes(shape, total_q) bytes, 256-byte aligned; contents on entry are ignored.
  *              Two calls that may run at the same time (streams without an order, graphs replayed side by side) need
  *              a workspace each.
- * bf16 with (d_qk, d_v) = (128, 128), (64, 64) or (64, 128), a positive scale, up to 128 query heads per (K head,
- * V head) pair and pages of 8 to 64 tokens (a power of two) or a multiple of 128 runs on the tensor cores; everything
- * else diffqkv_decode accepts runs on fp32 FMAs.  Results do not depend on how sequences are batched beyond fp32
- * summation order, and are bitwise reproducible from call to call.
+ * bf16 with (d_qk, d_v) = (128, 128), (64, 64) or (64, 128), a positive scale and pages of 8 to 64 tokens (a power of
+ * two) or a multiple of 128 runs on the tensor cores, chunks of a few rows and long ones on a kernel each; everything else
+ * diffqkv_decode accepts runs on fp32 FMAs.  Results do not depend on how sequences are batched beyond rounding (fp32
+ * sums in another order, weights rounded to bf16 relative to another reference), and are bitwise reproducible from call
+ * to call.
  * As in any tensor-core attention a weight of zero multiplies the V rows of later tokens of the same chunk; those rows
  * must be finite.  What lies behind the last cached token in its page may hold anything.
  */
@@ -461,7 +462,8 @@ diffqkv_status diffqkv_pages_fork(const int32_t *parents, const int32_t *childre
  * (count > 1 at the start of the call) are replaced, and where past_b lies inside such a page its contents are copied
  * to the new one (copy on write).  If all holders of a page write in the same call each gets a copy.
  * A sequence gets all it needs or nothing: b is denied when the demands of sequences 0 .. b together exceed the free
- * pages (DIFFQKV_ERR_PAGES) or its row is too short (DIFFQKV_ERR_INDEX).
+ * pages (DIFFQKV_ERR_PAGES) or its row is too short (DIFFQKV_ERR_INDEX).  The rows of a denied sequence must not be
+ * written in this step: pages of its that others share are as they were, and missing ones are missing.
  *   cache, shape  the pools (pointers, strides, num_blocks = pages->num_pages); shape gives n_k, n_v, d_qk, d_v, dtype;
  *                 cache->page_table and cache->seqlens are not used
  *   granted       [num_seqs] int32: 1 = its rows may be written, 0 = denied; or NULL

@@ -11,21 +11,32 @@
 // rows holds T = 128 / G tokens of the chunk times G heads (row = token * G + head): one token of 32/4/8 heads already
 // fills four rows, and K and V are staged once for all of them.
 //
-// Work.  A chunk is cut into items of 2 T tokens.  An item of more than T tokens ("wide") has two row tiles that share
-// every 128-token K/V tile; one of at most T tokens ("narrow": decode rows, short chunks, the end of a long one) has a
-// single row tile, which is given to both softmax groups: one takes the even K/V tiles, the other the odd ones, and the
-// first joins the two results at the end (softmax does not care which tokens it has seen).  All (sequence, head group,
-// item, K/V tile) form one flat list, wide tiles counting twice, that is divided evenly over the persistent blocks, so
-// that a single row over a long cache and a thousand short chunks both fill the SMs.  A block's run inside an item is
-// a segment; an item that is cut leaves normalised partial rows in the workspace, which extend_combine_kernel joins.
-// Lengths are known on the device alone: each block finds its place by a closed-form sum (floor_sum) and walks from there.
+// Work.  Sequences of a few rows are left to extend_thin.cu.  A longer chunk is cut into items of 2 T tokens.  An item of
+// more than T tokens ("wide") has two row tiles that share every 128-token K/V tile; one of at most T tokens ("narrow":
+// the end of a chunk) has a single row tile, which is given to both softmax groups: one takes the even K/V tiles, the
+// other the odd ones, and the first joins the two results at the end (softmax does not care which tokens it has seen).
+// All (sequence, head group, item, K/V tile) form one flat list, in which an item costs something next to its tiles, that
+// is divided evenly over the persistent blocks, so that one long chunk and a hundred short ones both fill the SMs.  A
+// block's run inside an item is a segment; an item that is cut leaves normalised partial rows in the workspace, which
+// extend_combine_kernel joins in a fixed order.  Lengths are known on the device alone: each block finds its place by a
+// closed-form sum (floor_sum) and walks from there.
 // Head groups that differ only in their V head (or only in their K head) are given to a team of neighbouring blocks
 // that walk the same tiles at the same time, so that the shared K (V) tiles come out of the second-level cache.
 //
 // Roles of the twelve warps, as in prefill.cu: warp 0 TMA producer, one thread of warp 1 issues the products, warps 4-7
 // and 8-11 are the two softmax groups (one thread per row).  The producer walks the segments and hands them to the other
-// roles through a small ring; the roles meet only at mbarriers, so the next segment's K, V and Q are on their way while the last one is being written out.  Every wait is
-// bounded; on expiry the block reports DIFFQKV_ERR_TIMEOUT, drains and frees its tensor memory.
+// roles through a small ring; the roles meet only at mbarriers, so the next segment's K, V and Q are on their way while
+// the last one is being written out.  Every wait is bounded; on expiry the block reports DIFFQKV_ERR_TIMEOUT, drains and
+// frees its tensor memory.
+//
+// Bound by the chain score product -> softmax -> value product of each of the two row tiles, one of which computes while
+// the other's products run.  Chunks of 1.5k-2k rows over 0-6k cached tokens, four sequences, 32/4/8 heads of 128: 430 us,
+// 1065 TFLOP/s of causal work (0.62 of a large matrix product), a pair of row tiles in 3460 cycles: 2200 of softmax, of
+// which 1024 are exponentials at the rate of the special-function unit when both groups are at it, and 1260 from the last
+// weight to the next score, 768 of them products.  The tensor pipe is active 55 % of the time, the special-function unit
+// 55 %.  What did not help: exponentials by polynomial for an eighth to a half of the scores (the registers it takes cost
+// more, 415-850 us), announcing 96 or 112 instead of 64 tokens' weights first (436), waiting for the next K before the
+// last weights (450-470).
 #include <atomic>
 #include <numeric>
 
@@ -922,7 +933,7 @@ bool make_cache_map(CUtensorMap* map, const void* base, int d, long long tok_ext
 
 // The same for a pool whose heads lie behind one another in a block (stride_head = tokens * stride_tok) and whose rows
 // have 128 channels: dims (64 channels, 8 tokens, channel half, group of 8 tokens of any head, block), so that one box
-// brings whole rows, half as many boxes per tile (16-token pages were bound by the rate of boxes: 235 -> 190 us for 16
+// brings whole rows, half as many boxes per tile (16-token pages were bound by the rate of boxes: 242 -> 190 us for 16
 // sequences of 4k-32k tokens, 5 new rows each, 32/4/8 heads).
 bool make_row_map(CUtensorMap* map, const void* base, int d, long long tok_extent, int heads, long long blocks,
                   long long st_tok, long long st_head, long long st_blk, int box_tok) {
@@ -1082,7 +1093,7 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
   // Which sequences are thin is known on the device alone, so both kernels are launched; the second may start as soon as
   // the first has, and takes the SMs that the first leaves (an SM has room for one block of either).  First comes the one
   // that has the more work if the rows are spread evenly: behind the other it starts on SMs in another order, away from
-  // its team (prompts 578 instead of 507 us), and a step of thin sequences would wait for two launches (32, not 28 us).
+  // its team (prompts 447 instead of 434 us), and a step of thin sequences would wait for two launches (198, not 190 us).
   using ExtendFn = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const ExtendParams);
   const ExtendFn fn = s.d_v == 64 ? extend_attn_kernel<64, 64>
                                   : (s.d_qk == 128 ? extend_attn_kernel<128, 128> : extend_attn_kernel<64, 128>);

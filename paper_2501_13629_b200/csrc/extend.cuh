@@ -110,8 +110,8 @@ __device__ __forceinline__ long long last_tile(int cost, int nt, int extra) {
 // Likewise for thin items, in tiles: a block's second item costs it about as much as five more tiles.
 constexpr int kThinItemCost = 5;
 // In the division of the work: a K/V tile of a wide and of a narrow item, and what an item costs next to its tiles (its
-// rows are written out and the pipeline fills again).  Measured on prompts of 1.5k-2k rows over 1k-5k tokens: 2.35 us a
-// tile, 5.8 us an item; without the last, blocks with many short items ended 13 % late.
+// rows are written out and the pipeline fills again).  Measured on prompts of 1.5k-2k rows over 0-6k tokens: 1.85 us a
+// tile, 4-5 us an item; without the last, blocks with many short items ended 13 % late, 4 to 7 makes 1 %.
 constexpr int kWideCost = 2, kNarrowCost = 1, kItemCost = 5;
 
 // sum of floor((a x + b) / m) for x = 0 .. n - 1 with a, b >= 0, m > 0: the Euclid-like recursion on (m, a).  Not inlined:
@@ -197,7 +197,7 @@ struct Seq {
 
 // Teams that the list of long chunks is divided over; the thin sequences have the other SMs, so that neither kernel waits
 // for the other (one thread block of either fits an SM): what a step of both kinds saves is one start, one end and one
-// uneven finish (a chunk of 512 rows next to 15 single ones over 0.5k-4k tokens, 16/2/4 heads: 74 -> 65 us).  The weight
+// uneven finish (a chunk of 512 rows next to 15 single ones over 0.5k-4k tokens, 16/2/4 heads: 72 -> 64 us).  The weight
 // of a thin tile, 0.3 + 0.48 units for each of its K and V tiles, is the middle of what was fastest for seven mixtures of
 // 64 and 128 channels; a third more or less costs up to a tenth, far too little or too much twice the time.
 __device__ __forceinline__ int wide_teams(const ExtendParams& p, long long wide, long long thin) {

@@ -16,10 +16,16 @@
 // through one hardware barrier per tile.  Weights of up to 2^24 are harmless: bf16 and fp32 have the range, the
 // relative precision of either does not depend on the magnitude, and the quotient takes the factor out again.
 //
-// Work: one flat list of (sequence, unit of heads, 128-token tile), divided evenly over one persistent block per SM, whose
-// two softmax groups take alternate tiles and are joined at the end of a segment; cut items leave partial rows as in
-// extend.cu.  Bound by memory: a tile of a unit with one K and two V heads of 128 channels is 96 KB, 2.2 us at an SM's
-// share of the bandwidth; its products take about 0.6 us and its softmax less.
+// Work: one flat list of (sequence, unit of heads, 128-token tile), divided evenly over one persistent block per SM (or
+// over those that a step's long chunks leave), whose two softmax groups take alternate tiles and are joined at the end of a
+// segment; cut items leave partial rows as in extend.cu.  A unit has up to four head groups that share their K or V head:
+// one head group at a time, 16 sequences of 4k-32k tokens with 2-5 rows, 32/4/8 heads of 128, take 284 us instead of 190.
+//
+// Bound by memory where caches are long: those sequences (983 MB) take 186 us here, 5.3 TB/s (0.82 of a copy), plus the
+// joining kernel; with row tiles as in extend.cu it was 300 us.  Short steps are bound by the chain of a block's start
+// (8 thousand cycles to the first request: lengths, place in the list, page), its first tile (the code of every role comes
+// from the second-level cache once: a warp's first tile takes 6 thousand cycles, later ones 1.5) and the joining kernel:
+// 8 sequences of up to 2k tokens, 1-3 rows, 32/4/16 heads of 64, 26 us, of which 13 MB of cache are 2.
 // Warp 0 TMA producer, one thread of warp 1 issues the products, warps 2-9 and 10-17 the softmax groups.  Every wait is
 // bounded.
 #include <type_traits>
@@ -177,7 +183,7 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   // Equal shares of the list, cut wherever they end; or, where that costs no block more than four tiles, equal chunks
   // that begin with their item: sum ceil(nt / chunk) <= total / chunk + items <= blocks, so every block has one
   // segment at most.  (A segment costs about as much as five tiles next to its tiles, and short lists would give most
-  // blocks two: 8 x ~700 tokens, 32/4/16 heads of 64, 31 -> 22 us.)
+  // blocks two: 8 sequences of up to 2k tokens, 32/4/16 heads of 64, 36 -> 26 us.)
   int chunk = 0;
   const int items = per_thread == 1 ? min(busy_threads * p.n_units, grid) : grid;
   if (items < grid && total < (1ll << 22)) {

@@ -10,6 +10,12 @@
 // a megabyte of counts (262 144 pages, 12.9 GB of 16-token pages) in about a microsecond, and barrier.cluster costs less
 // than a second launch.  Pages themselves are moved by a second kernel over all SMs, from a list the first one leaves
 // in the workspace; it is bound by memory (each moved page is read once and written once).
+//
+// Measured, 32/4/8 heads of 128 in bf16 (49 KB a 16-token page): 4096 pages copied in 68 us, 5.9 TB/s; a pool of 49 152
+// with 29 491 in use compacted in 203 us, 11 800 moves of 1.16 GB in all at 5.7 TB/s behind 10 us of search and mapping; 24
+// pages 2.3 us.  Giving back 24 of 64 sequences, forking 24 others and reserving the next page for all, copies of
+// half-filled pages included (98 304 pages): 22 us in five launches of dependent reads, 0.9 us of traffic.  In a loop without
+// a graph the host needs longer to issue them (36 us).
 #include "common.cuh"
 #include "ptx.cuh"
 
