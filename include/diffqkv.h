@@ -338,8 +338,8 @@ diffqkv_status diffqkv_decode_topk_ids(const void *q, const diffqkv_cache *cache
  * diffqkv_decode's), so that one pair of arrays serves every layer:
  *     diffqkv_pages_reserve -> per layer: diffqkv_rope_append, diffqkv_extend -> the caller adds n_b to seqlens[b]
  *   cu_q     [batch + 1] int32, cu_q[0] = 0, not decreasing, cu_q[batch] <= total_q
- *   total_q  rows the ragged tensors hold; rows from cu_q[batch] on are neither read nor written, so a step of fixed
- *            capacity can be captured into a graph and replayed with other lengths
+ *   total_q  rows the ragged tensors hold; rows from cu_q[batch] on are not written and what they hold does not matter,
+ *            so a step of fixed capacity can be captured into a graph and replayed with other lengths
  * A sequence whose rows do not fit (past_b + n_b > max_seqlen, or cu_q out of order or beyond total_q) is reported as
  * DIFFQKV_ERR_INDEX in *dev_status and skipped; its rows stay as they were.
  * ------------------------------------------------------------------------------------------------------------------ */
@@ -486,7 +486,8 @@ diffqkv_status diffqkv_pages_copy(const int32_t *src_ids, const int32_t *dst_ids
 /*
  * diffqkv_pages_compact -- moves the pages in use to the front of the pool: with `live` of them in use, the i-th lowest
  * page in use with an id >= live moves to the i-th lowest free id below live; everything else stays.  Afterwards
- * exactly the ids 0 .. live - 1 are in use.
+ * exactly the ids 0 .. live - 1 are in use.  Only the page table is told: a page held by a pin alone moves too, so a prefix
+ * that is kept for later should be kept as a sequence (diffqkv_pages_fork to a spare row) where pools are compacted.
  *   table_out, refs_out  the new page table and counts; may be pages->page_table / ref_counts themselves.  Where they
  *                        are other buffers the old ones stay valid for readers already enqueued: a moved page keeps
  *                        its contents at its old id until that id is handed out again

@@ -511,7 +511,8 @@ __global__ void __launch_bounds__(kThreads) extend_generic_kernel(DecodeParams p
   __syncthreads();
   float m_run, l_run, acc[kMaxAccPerThread];
   attend_range<T>(p, b, h, 0, past + (t - lo) + 1, q_s, sm, m_run, l_run, acc);
-  const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
+  // every row sees itself: a sum of zero means that no score was a number above -inf, and the result is none either
+  const float inv = 1.f / l_run;
 #pragma unroll
   for (int e = 0; e < kMaxAccPerThread; ++e) {
     const int ch = tid + e * kThreads;
@@ -520,7 +521,7 @@ __global__ void __launch_bounds__(kThreads) extend_generic_kernel(DecodeParams p
       else reinterpret_cast<__nv_bfloat16*>(out)[row * p.d_v + ch] = __float2bfloat16_rn(acc[e] * inv);
     }
   }
-  if (lse && tid == 0) lse[row] = l_run > 0.f ? (m_run + log2f(l_run)) * kLn2 : -INFINITY;
+  if (lse && tid == 0) lse[row] = l_run != 0.f ? (m_run + log2f(l_run)) * kLn2 : __int_as_float(0x7fffffff);
 }
 
 }  // namespace

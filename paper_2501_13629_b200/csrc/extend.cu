@@ -658,7 +658,8 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         if (!wait_warp(gbar + kODone, par ^ 1, abort_flag)) { ok = false; break; }
         tc::fence_after_sync();
       }
-      float weight = l > 0.f ? 1.f / l : 0.f, weight1 = 0.f, lse2 = l > 0.f ? m_ref + log2f(l) : -INFINITY;
+      // a sum of zero: the row sees no token of the segment; a NaN stays one
+      float weight = l != 0.f ? 1.f / l : 0.f, weight1 = 0.f, lse2 = l != 0.f ? m_ref + log2f(l) : -INFINITY;
       const bool join = !wide && w.tb - w.ta > 1;
       if (join && t == 1) {  // hand over to the first group, which reads both accumulators
         xch_s[r] = make_float2(m_ref, l);
@@ -680,12 +681,12 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         ++joins;
         tc::fence_after_sync();
         const float2 o = xch_s[r];
-        const float top = fmaxf(l > 0.f ? m_ref : -INFINITY, o.y > 0.f ? o.x : -INFINITY);
-        const float e0 = l > 0.f ? exp2f(m_ref - top) : 0.f, e1 = o.y > 0.f ? exp2f(o.x - top) : 0.f;
+        const float top = fmaxf(l != 0.f ? m_ref : -INFINITY, o.y != 0.f ? o.x : -INFINITY);
+        const float e0 = l != 0.f ? exp2f(m_ref - top) : 0.f, e1 = o.y != 0.f ? exp2f(o.x - top) : 0.f;
         const float sum = l * e0 + o.y * e1;
-        weight = sum > 0.f ? e0 / sum : 0.f;
-        weight1 = sum > 0.f ? e1 / sum : 0.f;
-        lse2 = sum > 0.f ? top + log2f(sum) : -INFINITY;
+        weight = sum != 0.f ? e0 / sum : 0.f;
+        weight1 = sum != 0.f ? e1 / sum : 0.f;
+        lse2 = sum != 0.f ? top + log2f(sum) : -INFINITY;
       }
       if (busy) {
         const bool store = r < rows_of(w);
@@ -889,7 +890,7 @@ extend_combine_kernel(const ExtendParams p, const ExtendList thin, const int thi
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         if (h == 1 && !second) break;
-        const float inv = sum[h] > 0.f ? 1.f / sum[h] : 0.f;
+        const float inv = sum[h] != 0.f ? 1.f / sum[h] : 0.f;
         const long long row = (long long)(m.row_lo + tok) * p.n_q + m.head0 + part * p.G + head;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -907,7 +908,7 @@ extend_combine_kernel(const ExtendParams p, const ExtendList thin, const int thi
               make_uint4(pack2(acc[h][0].x, acc[h][0].y), pack2(acc[h][0].z, acc[h][0].w), pack2(acc[h][1].x, acc[h][1].y),
                          pack2(acc[h][1].z, acc[h][1].w));
         }
-        if (p.lse && lane == 0) p.lse[row] = sum[h] > 0.f ? (top[h] + log2f(sum[h])) * kLn2 : -INFINITY;
+        if (p.lse && lane == 0) p.lse[row] = sum[h] != 0.f ? (top[h] + log2f(sum[h])) * kLn2 : -INFINITY;
         if (++head == p.G) {
           head = 0;
           ++tok;

@@ -285,10 +285,10 @@ __global__ void __launch_bounds__(kThreads) extend_simt_kernel(const SimtParams 
     float sum = l[i];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
     const int tok = r / p.G;
     const long long row = (long long)(row_lo + tok0 + tok) * p.n_q + head0 + (r - tok * p.G);
-    const float lse2 = sum > 0.f ? m[i] + log2f(sum) : -INFINITY;
+    const float lse2 = sum != 0.f ? m[i] + log2f(sum) : -INFINITY;
     if (p.splits > 1) {
       const long long at = row * p.splits + blockIdx.z;
 #pragma unroll
@@ -332,13 +332,13 @@ __global__ void __launch_bounds__(256) extend_join_kernel(const SimtParams p) {
 #pragma unroll
     for (int c = 0; c < kC; ++c) acc[c] = fmaf(f, p.part_o[(row * p.splits + i) * DV + lane * kC + c], acc[c]);
   }
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  const float inv = sum != 0.f ? 1.f / sum : 0.f;
 #pragma unroll
   for (int c = 0; c < kC; ++c) {
     if (p.out_is_f32) reinterpret_cast<float*>(p.out)[row * DV + lane * kC + c] = acc[c] * inv;
     else store_out(reinterpret_cast<__nv_bfloat16*>(p.out) + row * DV + lane * kC + c, acc[c] * inv);
   }
-  if (p.lse && lane == 0) p.lse[row] = sum > 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+  if (p.lse && lane == 0) p.lse[row] = sum != 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
 }
 
 int heads_per_tile(const diffqkv_shape& s) {

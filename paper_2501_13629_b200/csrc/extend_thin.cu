@@ -702,14 +702,14 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         const int c = c0 + lane, g = c / p.region, lc = c & (p.region - 1);
         const float l0 = sc.part[0][0][c] + sc.part[0][1][c] + sc.part[0][2][c] + sc.part[0][3][c];
         const float l1 = join ? sc.part[1][0][c] + sc.part[1][1][c] + sc.part[1][2][c] + sc.part[1][3][c] : 0.f;
-        const float m0 = l0 > 0.f ? sc.m[0][c] : -INFINITY, m1 = l1 > 0.f ? sc.m[1][c] : -INFINITY;
+        const float m0 = l0 != 0.f ? sc.m[0][c] : -INFINITY, m1 = l1 != 0.f ? sc.m[1][c] : -INFINITY;
         const float top = fmaxf(m0, m1);
-        const float e0 = l0 > 0.f ? exp2f(m0 - top) : 0.f, e1 = l1 > 0.f ? exp2f(m1 - top) : 0.f;
-        const float sum = l0 * e0 + l1 * e1, inv = sum > 0.f ? 1.f / sum : 0.f;
+        const float e0 = l0 != 0.f ? exp2f(m0 - top) : 0.f, e1 = l1 != 0.f ? exp2f(m1 - top) : 0.f;
+        const float sum = l0 * e0 + l1 * e1, inv = sum != 0.f ? 1.f / sum : 0.f;
         sc.m[0][c] = e0 * inv;
         if (join) sc.m[1][c] = e1 * inv;
         if (g < p.parts && lc < used) {
-          const float lse2 = sum > 0.f ? top + log2f(sum) : -INFINITY;
+          const float lse2 = sum != 0.f ? top + log2f(sum) : -INFINITY;
           const int token = lc / p.G;
           if (!whole) p.list.part_lse[prow0 + g * used + lc] = lse2;
           else if (p.lse) p.lse[(long long)(w.row_lo + token) * p.n_q + w.head0 + g * p.G + lc - token * p.G] = lse2 * kLn2;

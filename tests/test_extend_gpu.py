@@ -138,6 +138,42 @@ def test_many_sequences(api):
     run(api, Step(api, past, new, 8, 2, 4, 64, 64, seed=6).fill())
 
 
+def test_many_sequences_of_both_kinds(api):
+    """Several sequences to a thread in both lists, sequences of either kind anywhere among the others."""
+    r = random.Random(2)
+    past = [r.randint(0, 60) for _ in range(1900)]
+    new = [r.choice([0, 1, 1, 2, 3, 40, 130]) if i % 5 == 0 else r.choice([0, 0, 1]) for i in range(1900)]
+    run(api, Step(api, past, new, 8, 2, 4, 64, 64, seed=9, pad=3).fill())
+
+
+@pytest.mark.parametrize("heads", ["32/4/8", "16/2/4", "6/2/3", "16/1/1", "32/4/16"])
+@pytest.mark.parametrize("load", ["one chunk", "one token", "even", "short caches"])
+def test_long_chunks_beside_single_rows(api, heads, load):
+    """The two kinds divide the SMs: nearly all of the work of one kind, of the other, of both, and too little for all."""
+    past, new = {"one chunk": ([2000] + [3] * 2, [600] + [1] * 2), "one token": ([20] + [4000] * 12, [70] + [2] * 12),
+                 "even": ([900, 1500] + [2500] * 10, [200, 100] + [1, 2, 3, 1, 1] * 2),
+                 "short caches": ([0, 1, 2, 3], [65, 1, 1, 66])}[load]
+    run(api, Step(api, past, new, *HEADS[heads], 128, 128, seed=len(load), pad=2).fill())
+
+
+@pytest.mark.parametrize("dtype,dims", [(BF16, (128, 128)), (BF16, (64, 64)), (F32, (64, 64)), (F32, (96, 80))])
+@pytest.mark.parametrize("past", [40, 500, 9000])
+def test_a_row_that_is_not_finite_stays_alone(api, dtype, dims, past):
+    """NaN and infinity in one query row reach its own results, all of them, in chunks of either kind."""
+    for new, bad in (([3, 2], 1), ([200, 3], 77), ([200, 3], 201)):
+        step = Step(api, [past, 40], new, 8, 2, 4, *dims, dtype=dtype, seed=11).fill()
+        clean, clean_lse = run(api, step)
+        for x in (math.nan, math.inf):
+            q = step.q.clone()
+            q[bad, 3] = x
+            lse = torch.empty_like(clean_lse)
+            out = api.diffqkv_extend(q, step.cu, step.cache, 2, 4, step.d_qk ** -0.5, lse=lse)
+            torch.cuda.synchronize()
+            assert not bool(torch.isfinite(out[bad, 3]).any()) and bool(lse[bad, 3].isnan())
+            out[bad, 3], lse[bad, 3] = clean[bad, 3], clean_lse[bad, 3]
+            assert torch.equal(out, clean) and torch.equal(lse, clean_lse)
+
+
 @pytest.mark.parametrize("seed", range(12))
 def test_random_steps(api, seed):
     r = random.Random(seed)
