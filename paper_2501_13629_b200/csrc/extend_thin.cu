@@ -640,9 +640,11 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
           }
         if (k0 + kKT > w.past + w.n) {
           // V rows past the sequence end hold whatever followed in memory: zero them (0 * NaN would poison the product).
-          // The tile before, the other group's, may still wait for its V, in the place that this one's V will have: until
-          // its product is done a wait for this V could take the phase before for its own.
-          if (i > 0) ok = wait_warp(o_done0 + 8 * (1 - t), (other + ((i - 1) >> 1)) & 1, abort_flag) && ok;
+          // Where the ring has room for one tile's V the tile before, the other group's, may still wait for its own, in the
+          // place that this one's will have: until its product is done a wait for this V could take the phase before for
+          // its own.  (In a longer ring that place was the tile's before, whose product this group has waited for, or an
+          // earlier segment's, whose products had all been issued.)
+          if (i > 0 && p.v_ring < 2 * p.v_parts) ok = wait_warp(o_done0 + 8 * (1 - t), (other + ((i - 1) >> 1)) & 1, abort_flag) && ok;
           if (half == 0 && r >= w.past + w.n - k0) {
             for (int y = 0; y < p.v_parts; ++y) {
               const int at = w.v0 + i * p.v_parts + y, slot = p.k_ring + at % p.v_ring;
