@@ -358,7 +358,8 @@ diffqkv_status diffqkv_decode_topk_ids(const void *q, const diffqkv_cache *cache
  * two) or a multiple of 128 runs on the tensor cores, chunks of a few rows and long ones on a kernel each; everything else
  * diffqkv_decode accepts runs on fp32 FMAs.  Results do not depend on how sequences are batched beyond rounding (fp32
  * sums in another order, weights rounded to bf16 relative to another reference), and are bitwise reproducible from call
- * to call.
+ * to call.  Three launches, whatever the step holds; a step known to have one row for every sequence is faster through
+ * diffqkv_decode (whose seqlens count the new token).
  * As in any tensor-core attention a weight of zero multiplies the V rows of later tokens of the same chunk; those rows
  * must be finite.  What lies behind the last cached token in its page may hold anything.
  */
