@@ -430,6 +430,7 @@ diffqkv_status diffqkv_rope_append(const void *q, const void *k_new, const void 
  * may also be raised by the caller (a prefix that is kept pinned).  No call synchronises or tells the host anything:
  * a serving loop can run them inside a captured step.
  * Sequence ids outside [0, num_seqs) and page ids outside [0, num_pages) are reported as DIFFQKV_ERR_INDEX, skipped.
+ * At most 65535 sequences and 2^20 pages; more are refused with DIFFQKV_ERR_UNSUPPORTED.
  */
 typedef struct {
   int32_t *page_table; /* [num_seqs, max_pages_per_seq]                              */
