@@ -543,20 +543,29 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         if (k0 + kKT > w.past + 1) {  // the tile reaches past some row's position
           const int hidden = (k0 + r - w.past) * p.G;  // columns of a group below this belong to rows before the token
 #pragma unroll
-          for (int c = 0; c < kHalfCols; ++c)
-            if (((c0 + c) & (p.region - 1)) < hidden) x[c] = -INFINITY;
+          for (int q = 0; q < kHalfCols / 8; ++q)
+            if (mask >> q & 1) {
+              const int first = hidden - ((c0 + q * 8) & (p.region - 1));
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                if (e < first) x[q * 8 + e] = -INFINITY;
+            }
         }
         // ---- scores on the scale of base 2, from the reference: the score of the segment's first token of this group to
         // begin with (a row that does not see it sees none of the tile: reference 0, weights 0)
         if (!later) {
 #pragma unroll
-          for (int c = 0; c < kHalfCols; ++c) x[c] *= p.scale_log2;
-          if (quarter == 0 && lane == 0) {
+          for (int q = 0; q < kHalfCols / 8; ++q)
+            if (mask >> q & 1) {
 #pragma unroll
-            for (int c = 0; c < kHalfCols; c += 4)
-              *reinterpret_cast<float4*>(m + c) = make_float4(x[c] == -INFINITY ? 0.f : x[c], x[c + 1] == -INFINITY ? 0.f : x[c + 1],
-                                                              x[c + 2] == -INFINITY ? 0.f : x[c + 2], x[c + 3] == -INFINITY ? 0.f : x[c + 3]);
-          }
+              for (int e = 0; e < 8; ++e) x[q * 8 + e] *= p.scale_log2;
+              if (quarter == 0 && lane == 0) {
+#pragma unroll
+                for (int c = q * 8; c < q * 8 + 8; c += 4)
+                  *reinterpret_cast<float4*>(m + c) = make_float4(x[c] == -INFINITY ? 0.f : x[c], x[c + 1] == -INFINITY ? 0.f : x[c + 1],
+                                                                  x[c + 2] == -INFINITY ? 0.f : x[c + 2], x[c + 3] == -INFINITY ? 0.f : x[c + 3]);
+              }
+            }
           group_sync(bar_id);
         }
         bool over = !ok;
@@ -564,11 +573,12 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
 #pragma unroll
         for (int q = 0; q < kHalfCols / 8; ++q)
           if (mask >> q & 1) {
+            const int end = used - ((c0 + q * 8) & (p.region - 1));
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               const int c = q * 8 + e;
               x[c] = fmaf(x[c], f, -m[c]);
-              over |= x[c] > kThinThreshold && ((c0 + c) & (p.region - 1)) < used;
+              over |= x[c] > kThinThreshold && e < end;
             }
           }
         if (group_any(bar_id, over)) {
