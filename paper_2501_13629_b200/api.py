@@ -683,8 +683,16 @@ def _cache_bytes(cache: KVCache) -> bytes:
                        cache.max_seqlen)
 
 
-def _workspace(workspace: Optional[torch.Tensor], nbytes: int, device) -> torch.Tensor:
-    return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device) if workspace is None else workspace
+def _fresh(shape, dtype: torch.dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    """Memory of the stream the launch goes to: it is handed out again (a workspace is, at once) behind the launch."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _workspace(nbytes: int, device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
+    return _fresh(max(nbytes, 256), torch.uint8, device, stream)
 
 
 def _size(workspace: torch.Tensor) -> int:
@@ -715,12 +723,12 @@ def diffqkv_extend(q: torch.Tensor, cu_q: torch.Tensor, cache: KVCache, n_k: int
     assert cache.k.dtype == dtype and cache.v.dtype == dtype and q.is_contiguous()
     out_dtype = out_dtype or (dtype if out is None else out.dtype)
     if out is None:
-        out = torch.empty((total_q, n_q, d_v), dtype=out_dtype, device=q.device)
+        out = _fresh((total_q, n_q, d_v), out_dtype, q.device, stream)
     assert out.is_contiguous() and out.numel() == total_q * n_q * d_v and out.dtype == out_dtype
     assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == total_q * n_q)
     shape = _pack_shape(batch, n_q, n_k, n_v, d_qk, d_v, _DTYPES[dtype], _DTYPES[out_dtype], scale)
     if workspace is None:
-        workspace = _workspace(None, _raw.diffqkv_extend_workspace_bytes(shape, total_q), q.device)
+        workspace = _workspace(_raw.diffqkv_extend_workspace_bytes(shape, total_q), q.device, stream)
     _check_status(_raw.diffqkv_extend(q.data_ptr(), _ints(cu_q, batch + 1), total_q, _cache_bytes(cache), shape,
                                       workspace.data_ptr(), _size(workspace), out.data_ptr(), _addr(lse),
                                       _addr(dev_status), _stream_on(stream, dev)), "diffqkv_extend")
@@ -778,7 +786,7 @@ def diffqkv_rope_append(q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: t
         n_q, q_stride = q.shape[1], _row_stride(q, total_q, d_qk)
         assert q.dtype == dtype and q.shape[2] == d_qk
         if q_out is None:
-            q_out = torch.empty((total_q, n_q, d_qk), dtype=dtype, device=q.device)
+            q_out = _fresh((total_q, n_q, d_qk), dtype, q.device, stream)
         assert q_out.is_contiguous() and q_out.dtype == dtype and q_out.numel() == total_q * n_q * d_qk
     freqs, rot = 0, 0
     if inv_freq is not None:
@@ -829,7 +837,7 @@ def diffqkv_pages_fork(parents: torch.Tensor, children: torch.Tensor, cache: KVC
     g = _pages_bytes(cache, ref_counts)
     n = children.numel()
     if workspace is None:
-        workspace = _workspace(None, _raw.diffqkv_pages_fork_workspace_bytes(g, n), ref_counts.device)
+        workspace = _workspace(_raw.diffqkv_pages_fork_workspace_bytes(g, n), ref_counts.device, stream)
     _check_status(_raw.diffqkv_pages_fork(_ints(parents, n), _ints(children), n, g, workspace.data_ptr(), _size(workspace),
                                           _addr(dev_status), _stream_on(stream, dev)), "diffqkv_pages_fork")
 
@@ -842,7 +850,7 @@ def diffqkv_pages_reserve(cu_q: torch.Tensor, cache: KVCache, ref_counts: torch.
     g = _pages_bytes(cache, ref_counts)
     seqs = cache.page_table.shape[0]
     if workspace is None:
-        workspace = _workspace(None, _raw.diffqkv_pages_reserve_workspace_bytes(g), ref_counts.device)
+        workspace = _workspace(_raw.diffqkv_pages_reserve_workspace_bytes(g), ref_counts.device, stream)
     _check_status(_raw.diffqkv_pages_reserve(_ints(cu_q, seqs + 1), g, _cache_bytes(cache), _pools_bytes(cache, n_k, n_v),
                                              _ints(granted, seqs), workspace.data_ptr(), _size(workspace),
                                              _addr(dev_status), _stream_on(stream, dev)), "diffqkv_pages_reserve")
@@ -876,7 +884,7 @@ def diffqkv_pages_compact(cache: KVCache, ref_counts: torch.Tensor, n_k: int, n_
     table_out = cache.page_table if table_out is None else table_out
     refs_out = ref_counts if refs_out is None else refs_out
     if workspace is None:
-        workspace = _workspace(None, _raw.diffqkv_pages_compact_workspace_bytes(g), ref_counts.device)
+        workspace = _workspace(_raw.diffqkv_pages_compact_workspace_bytes(g), ref_counts.device, stream)
     _check_status(_raw.diffqkv_pages_compact(g, _cache_bytes(cache), _pools_bytes(cache, n_k, n_v),
                                              _ints(table_out, cache.page_table.numel()), _ints(refs_out, ref_counts.numel()),
                                              _ints(live, 1), workspace.data_ptr(), _size(workspace), _addr(dev_status),

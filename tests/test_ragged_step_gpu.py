@@ -6,7 +6,7 @@ import random
 import pytest
 import torch
 
-from ragged import BF16, F32, HALF_STEP, attend64, ints
+from ragged import BF16, F32, HALF_STEP, Step, attend64, ints
 
 pytestmark = pytest.mark.gpu
 
@@ -188,3 +188,34 @@ def test_two_captured_loops_side_by_side(api):
                 g.replay()
         for loop in loops:
             loop.check()
+
+
+def test_memory_of_a_call_belongs_to_its_stream(api, monkeypatch):
+    """A workspace that a call on another stream brings itself must not be handed out on the current one while the call may
+    still be waiting to run."""
+    step = Step(api, [900, 40, 3], [2, 70, 1], 8, 2, 4, 64, 64, seed=1).fill()
+    refs = torch.ones(step.k.shape[0], dtype=torch.int32, device="cuda")
+    side, taken = torch.cuda.Stream(), []
+    place = {"diffqkv_extend": 5, "diffqkv_pages_fork": 4, "diffqkv_pages_reserve": 5, "diffqkv_pages_compact": 6}
+    for name, at in place.items():
+        def spy(*args, call=getattr(api._raw, name), at=at):
+            taken.append((args[at], args[at + 1]))
+            return call(*args)
+        monkeypatch.setattr(api._raw, name, spy)
+    ids, none = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    k_new, v_new = step.q[:, :2].contiguous(), step.q[:, :4].contiguous()
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    out = api.diffqkv_extend(step.q, step.cu, step.cache, 2, 4, 0.125, stream=side)
+    api.diffqkv_pages_fork(ids, ids, step.cache, refs, stream=side)
+    api.diffqkv_pages_reserve(none, step.cache, refs, 2, 4, stream=side)
+    api.diffqkv_pages_compact(step.cache, refs, 2, 4, stream=side)
+    turned = api.diffqkv_rope_append(step.q, k_new, v_new, step.cu, step.cache, None, stream=side)
+    assert len(taken) == 4
+    kept = [torch.empty(n, dtype=torch.uint8, device="cuda") for _, n in taken for _ in range(3)]
+    kept += [torch.empty_like(out), torch.empty_like(turned)]
+    spans = [(p, p + n) for p, n in taken]
+    for x in kept:
+        lo, hi = x.data_ptr(), x.data_ptr() + x.numel() * x.element_size()
+        assert all(hi <= a or b <= lo for a, b in spans)
+    torch.cuda.synchronize()
