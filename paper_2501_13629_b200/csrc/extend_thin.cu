@@ -24,8 +24,8 @@
 // Bound by memory where caches are long: those sequences (983 MB) take 186 us here, 5.3 TB/s (0.82 of a copy), plus the
 // joining kernel; with row tiles as in extend.cu it was 300 us.  Short steps are bound by the chain of a block's start
 // (8 thousand cycles to the first request: lengths, place in the list, page), its first tile (the code of every role comes
-// from the second-level cache once: a warp's first tile takes 6 thousand cycles, later ones 1.5) and the joining kernel:
-// 8 sequences of up to 2k tokens, 1-3 rows, 32/4/16 heads of 64, 26 us, of which 13 MB of cache are 2.
+// from the second-level cache once: a warp's first tile takes 4-9 thousand cycles, later ones 2.2) and the joining kernel:
+// 8 sequences of up to 2k tokens, 1-3 rows, 32/4/16 heads of 64, 25 us, of which 13 MB of cache are 2.
 // Warp 0 TMA producer, one thread of warp 1 issues the products, warps 2-9 and 10-17 the softmax groups.  Every wait is
 // bounded.
 #include <type_traits>
