@@ -107,12 +107,12 @@ __device__ __forceinline__ int item_tile(long long at, int cost, int nt, int ext
 __device__ __forceinline__ long long last_tile(int cost, int nt, int extra) {
   return nt == 1 ? 0 : extra + (long long)cost * (nt - 1);
 }
-// Likewise for thin items, in tiles: a block's second item costs it about as much as five more tiles.
-constexpr int kThinItemCost = 5;
 // In the division of the work: a K/V tile of a wide and of a narrow item, and what an item costs next to its tiles (its
 // rows are written out and the pipeline fills again).  Measured on prompts of 1.5k-2k rows over 0-6k tokens: 1.85 us a
 // tile, 4-5 us an item; without the last, blocks with many short items ended 13 % late, 4 to 7 makes 1 %.
 constexpr int kWideCost = 2, kNarrowCost = 1, kItemCost = 5;
+// Likewise for thin items, in tiles: a block's second item costs it about as much as five more tiles.
+constexpr int kThinItemCost = 5;
 
 // sum of floor((a x + b) / m) for x = 0 .. n - 1 with a, b >= 0, m > 0: the Euclid-like recursion on (m, a).  Not inlined:
 // the code that a block runs once at its start is fetched from the second-level cache line by line, which is what it
@@ -200,6 +200,7 @@ struct Seq {
 // uneven finish (a chunk of 512 rows next to 15 single ones over 0.5k-4k tokens, 16/2/4 heads: 72 -> 64 us).  The weight
 // of a thin tile, 0.3 + 0.48 units for each of its K and V tiles, is the middle of what was fastest for seven mixtures of
 // 64 and 128 channels; a third more or less costs up to a tenth, far too little or too much twice the time.
+// (The two kernels need not agree to the last block: each divides its own list, whatever the other takes.)
 __device__ __forceinline__ int wide_teams(const ExtendParams& p, long long wide, long long thin) {
   if (wide == 0) return 0;
   int n = p.n_teams;
