@@ -1134,7 +1134,8 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
   if ((err = wide_first ? launch_wide() : launch_thin()) != cudaSuccess) return err;
   if ((err = wide_first ? launch_thin() : launch_wide()) != cudaSuccess) return err;
   p.list = wide;
-  cfg.gridDim = dim3((unsigned)(sm_count() * kCombineBlocks));
+  const long long groups = kCombineThreads / (s.d_v / 8), rows = (long long)total_q * s.n_q, fill = sm_count() * kCombineBlocks;
+  cfg.gridDim = dim3((unsigned)((rows + groups - 1) / groups < fill ? (rows + groups - 1) / groups : fill));
   cfg.blockDim = dim3(kCombineThreads);
   cfg.dynamicSmemBytes = 0;
   cfg.numAttrs = 1;
