@@ -796,7 +796,8 @@ extend_combine_kernel(const ExtendParams p, const ExtendList thin, const int thi
   ptx::grid_dependency_wait();
   const int items = thin_blocks + wide_blocks;
   auto meta_of = [&](int x) { return x < thin_blocks ? thin.meta + x : p.list.meta + (x - thin_blocks); };
-  // four rows a bundle where there are many (one search for all, loads in flight together), else one: both counts in a scan
+  // Rows go in bundles: one each while that keeps no group waiting, two (read together) up to twice as many, else four (one
+  // search for all).  The three counts, at most 2^17 each, in one scan.
   static_assert(kItems == 2 * kCombineThreads, "two items a thread");
   uint64_t sum = 0;
   int rows[2];
@@ -804,7 +805,7 @@ extend_combine_kernel(const ExtendParams p, const ExtendList thin, const int thi
   for (int y = 0; y < 2; ++y) {
     const int x = 2 * threadIdx.x + y;
     rows[y] = x < items ? meta_of(x)->rows : 0;
-    sum += (uint64_t)rows[y] << 32 | (uint32_t)((rows[y] + 3) >> 2);
+    sum += (uint64_t)rows[y] | (uint64_t)((rows[y] + 1) >> 1) << 21 | (uint64_t)((rows[y] + 3) >> 2) << 42;
   }
   const uint64_t mine = sum;
 #pragma unroll
@@ -821,10 +822,16 @@ extend_combine_kernel(const ExtendParams p, const ExtendList thin, const int thi
     if (w < (int)threadIdx.x / 32) sum += scan_s[w];
     total += scan_s[w];
   }
-  const int bundle = (int)(total >> 32) > 2 * (int)gridDim.x * kGroups ? 4 : 1;
-  start_s[2 * threadIdx.x] = (int)(bundle == 4 ? sum : sum >> 32);
-  start_s[2 * threadIdx.x + 1] = start_s[2 * threadIdx.x] + (bundle == 4 ? (rows[0] + 3) >> 2 : rows[0]);
-  if (threadIdx.x == 0) start_s[kItems] = (int)(bundle == 4 ? total : total >> 32);
+  const int all = (int)total & 0x1fffff, at_once = (int)gridDim.x * kGroups;
+  const int log = all > 2 * at_once ? 2 : all > at_once ? 1 : 0, bundle = 1 << log;
+  auto count = [&](uint64_t x) {
+    const int c0 = (int)x & 0x1fffff, c1 = (int)(x >> 21) & 0x1fffff, c2 = (int)(x >> 42);
+    return log == 0 ? c0 : log == 1 ? c1 : c2;
+  };
+  const int mine0 = count(sum);
+  start_s[2 * threadIdx.x] = mine0;
+  start_s[2 * threadIdx.x + 1] = mine0 + ((rows[0] + bundle - 1) >> log);
+  if (threadIdx.x == 0) start_s[kItems] = count(total);
   __syncthreads();
   const int bundles = start_s[kItems];
   for (int g = blockIdx.x * kGroups + threadIdx.x / kLanes; g < bundles; g += gridDim.x * kGroups) {
