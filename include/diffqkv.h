@@ -340,8 +340,10 @@ diffqkv_status diffqkv_decode_topk_ids(const void *q, const diffqkv_cache *cache
  *   cu_q     [batch + 1] int32, cu_q[0] = 0, not decreasing, cu_q[batch] <= total_q
  *   total_q  rows the ragged tensors hold; rows from cu_q[batch] on are not written and what they hold does not matter,
  *            so a step of fixed capacity can be captured into a graph and replayed with other lengths
- * A sequence whose rows do not fit (past_b + n_b > max_seqlen, or cu_q out of order or beyond total_q) is reported as
- * DIFFQKV_ERR_INDEX in *dev_status and skipped; its rows stay as they were.
+ * A sequence whose rows do not fit (past_b + n_b > max_seqlen, a negative past_b, rows beyond total_q, an end before its
+ * beginning) is reported as DIFFQKV_ERR_INDEX in *dev_status and skipped; rows and cache positions that are its alone stay
+ * as they were.  Once cu_q decreases, sequences that still fit may be left out as well, and a row or cache position that it
+ * gives to several holds any one's result.
  * ------------------------------------------------------------------------------------------------------------------ */
 
 /*

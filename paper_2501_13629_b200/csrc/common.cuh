@@ -52,6 +52,47 @@ __device__ __forceinline__ void report(int* dev_status, int code) {
   if (dev_status) atomicOr(dev_status, 1 << code);
 }
 
+// Ragged steps: rows of sequence b (first row, number) and tokens cached before; false, with none of either, when they do
+// not fit.
+__device__ __forceinline__ bool ragged_rows(const int* cu_q, const int* seqlens, int b, int total_q, int max_seqlen, int& lo,
+                                            int& n, int& past) {
+  lo = cu_q[b];
+  const int hi = cu_q[b + 1];
+  past = seqlens[b];
+  if (lo < 0 || hi < lo || hi > total_q || past < 0 || (long long)past + (hi - lo) > max_seqlen) {
+    n = 0;
+    past = 0;
+    return false;
+  }
+  n = hi - lo;
+  return true;
+}
+// The sequence that row t belongs to, with its rows, looked for by a block of kThreads threads: the first that fits and has
+// the row between its ends, whatever the order of the others' ends; -1 = none.  With `report_all` the sequences
+// that do not fit are reported (one block of a launch does this).  Holds a barrier.
+template <int kThreads>
+__device__ __forceinline__ int ragged_sequence_of(const int* cu_q, const int* seqlens, int batch, int total_q, int max_seqlen,
+                                                  int t, bool report_all, int* dev_status, int& lo, int& n, int& past) {
+  __shared__ unsigned found_s[kThreads / 32];
+  unsigned found = ~0u;
+  for (int b = threadIdx.x; b < batch; b += kThreads) {
+    const bool between = cu_q[b] <= t && t < cu_q[b + 1];
+    if (!between && !report_all) continue;
+    if (!ragged_rows(cu_q, seqlens, b, total_q, max_seqlen, lo, n, past)) {
+      if (report_all) report(dev_status, DIFFQKV_ERR_INDEX);
+    } else if (between && found == ~0u) {
+      found = b;
+    }
+  }
+  found = __reduce_min_sync(0xffffffffu, found);
+  if ((threadIdx.x & 31) == 0) found_s[threadIdx.x >> 5] = found;
+  __syncthreads();
+  for (int w = 0; w < kThreads / 32; ++w) found = min(found, found_s[w]);
+  if (found == ~0u) return -1;
+  ragged_rows(cu_q, seqlens, (int)found, total_q, max_seqlen, lo, n, past);
+  return (int)found;
+}
+
 // Launchers (defined next to their kernels).
 cudaError_t launch_decode_generic(const DecodeParams& p, diffqkv_dtype dtype, cudaStream_t stream);
 cudaError_t launch_prefill_generic(const DecodeParams& p, diffqkv_dtype dtype, int q_len, void* out, int out_is_f32,

@@ -485,8 +485,8 @@ __global__ void __launch_bounds__(kThreads) prefill_generic_kernel(DecodeParams 
   if (lse && tid == 0) lse[row] = l_run > 0.f ? (m_run + log2f(l_run)) * kLn2 : -INFINITY;
 }
 
-// Attention of ragged chunks, one block per (row, query head): the row's sequence is the number of chunk ends at or
-// below it.  Rows that belong to no chunk, and chunks that do not fit the cache, are left alone.
+// Attention of ragged chunks, one block per (row, query head).  Rows that belong to no chunk, and chunks that do not fit the
+// cache, are left alone.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) extend_generic_kernel(DecodeParams p, const int* cu_q, int total_q, void* out,
                                                                  int out_is_f32, float* lse) {
@@ -494,17 +494,10 @@ __global__ void __launch_bounds__(kThreads) extend_generic_kernel(DecodeParams p
   __shared__ GenericSmem sm;
   const int t = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
   const CacheView& c = p.cache;
-  int count = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += kThreads) {
-    const int b = b0 + tid;
-    count += __syncthreads_count(b < p.batch && cu_q[b + 1] <= t);
-  }
-  if (count >= p.batch) return;
-  const int b = count, lo = cu_q[b], hi = cu_q[b + 1], past = c.seqlens[b];
-  if (lo < 0 || t < lo || t >= hi || hi > total_q || past < 0 || (long long)past + (hi - lo) > c.max_seqlen) {
-    if (tid == 0) report(p.dev_status, DIFFQKV_ERR_INDEX);
-    return;
-  }
+  int lo, n, past;
+  const int b = ragged_sequence_of<kThreads>(cu_q, c.seqlens, p.batch, total_q, c.max_seqlen, t, t == 0 && h == 0,
+                                             p.dev_status, lo, n, past);
+  if (b < 0) return;
   const long long row = (long long)t * p.n_q + h;
   const T* q = reinterpret_cast<const T*>(p.q) + row * p.d_qk;
   for (int e = tid; e < p.d_qk; e += kThreads) q_s[e] = to_float(q[e]) * p.scale_log2;

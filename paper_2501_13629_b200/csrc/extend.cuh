@@ -63,16 +63,7 @@ struct ExtendParams {
 
 // Rows of sequence b: first row, number, tokens cached before; false when they do not fit.
 __device__ __forceinline__ bool load_rows(const ExtendParams& p, int b, int& lo, int& n, int& past) {
-  lo = p.cu_q[b];
-  const int hi = p.cu_q[b + 1];
-  past = p.seqlens[b];
-  n = hi - lo;
-  if (lo < 0 || n < 0 || hi > p.total_q || past < 0 || (long long)past + n > p.max_seqlen) {
-    n = 0;
-    past = 0;
-    return false;
-  }
-  return true;
+  return ragged_rows(p.cu_q, p.seqlens, b, p.total_q, p.max_seqlen, lo, n, past);
 }
 
 // Shares are at least as long as the longest way between the starts of two tiles of an item (see item_tile), so that of

@@ -41,15 +41,7 @@ struct SimtParams {
 };
 
 __device__ __forceinline__ bool rows_of(const SimtParams& p, int b, int& lo, int& n, int& past) {
-  lo = p.cu_q[b];
-  const int hi = p.cu_q[b + 1];
-  past = p.cache.seqlens[b];
-  n = hi - lo;
-  if (lo < 0 || n < 0 || hi > p.total_q || past < 0 || (long long)past + n > p.cache.max_seqlen) {
-    n = 0;
-    return false;
-  }
-  return true;
+  return ragged_rows(p.cu_q, p.cache.seqlens, b, p.total_q, p.cache.max_seqlen, lo, n, past);
 }
 
 // Where tokens k0 .. k0 + 127 lie: block and slot of each (block -1: not there), a thread per token.
@@ -312,14 +304,11 @@ __global__ void __launch_bounds__(256) extend_join_kernel(const SimtParams p) {
   constexpr int kC = DV / 32;
   const int lane = threadIdx.x & 31;
   const int t = blockIdx.x, h = blockIdx.y * 8 + (threadIdx.x >> 5);
-  int count = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += 256) {
-    const int b = b0 + threadIdx.x;
-    count += __syncthreads_count(b < p.batch && p.cu_q[b + 1] <= t);
-  }
-  if (count >= p.batch || h >= p.n_q) return;
   int lo, n, past;
-  if (!rows_of(p, count, lo, n, past) || t < lo || t >= lo + n) return;
+  if (ragged_sequence_of<256>(p.cu_q, p.cache.seqlens, p.batch, p.total_q, p.cache.max_seqlen, t, false, p.dev_status, lo, n,
+                              past) < 0 ||
+      h >= p.n_q)
+    return;
   const long long row = (long long)t * p.n_q + h;
   float top = -INFINITY, sum = 0.f, acc[kC];
 #pragma unroll

@@ -123,15 +123,11 @@ __global__ void __launch_bounds__(kRopeThreads, kPairs ? 6 : 8) rope_append_kern
     if (first + y * heads_at_once < heads) read(first + y * heads_at_once, ahead[y]);
   if (v_first < v_heads) v_ahead = *reinterpret_cast<const uint4*>(v_row + v_first * p.d_v);
 
-  // ---- the row's sequence: the number of ends cu_q[1 ..] at or below the row, counted by the whole block
-  int b = 0;
-  for (int b0 = 0; b0 < p.batch; b0 += kRopeThreads) b += __syncthreads_count(b0 + tid < p.batch && p.cu_q[b0 + tid + 1] <= t);
-  if (b >= p.batch) return;  // behind the last sequence
-  const int lo = p.cu_q[b], hi = p.cu_q[b + 1], past = p.cache.seqlens[b];
-  if (lo < 0 || t < lo || hi > p.total_q || past < 0 || (long long)past + (hi - lo) > p.cache.max_seqlen) {
-    if (tid == 0) report(p.dev_status, DIFFQKV_ERR_INDEX);
-    return;
-  }
+  // ---- the row's sequence
+  int lo, n, past;
+  const int b = ragged_sequence_of<kRopeThreads>(p.cu_q, p.cache.seqlens, p.batch, p.total_q, p.cache.max_seqlen, t, t == 0,
+                                                 p.dev_status, lo, n, past);
+  if (b < 0) return;  // behind the last sequence, or of one that does not fit
   const int tok = past + (t - lo);
   long long blk = b, slot = tok;
   bool place_ok = true;
