@@ -108,11 +108,11 @@ __global__ void __launch_bounds__(kThreads) extend_simt_kernel(const SimtParams 
   // ---- block x takes the x-th row tile of all sequences
   if (tid == 0) seq_s = -1;
   int before = 0;
+  const bool reports = blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0;  // the sequences that do not fit: sees them all
   for (int b0 = 0; b0 < p.batch; b0 += kThreads) {
     int lo, n = 0, past;
     const int b = b0 + tid;
-    if (b < p.batch && !rows_of(p, b, lo, n, past) && blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0)
-      report(p.dev_status, DIFFQKV_ERR_INDEX);
+    if (b < p.batch && !rows_of(p, b, lo, n, past) && reports) report(p.dev_status, DIFFQKV_ERR_INDEX);
     const int mine = b < p.batch ? (n + p.T - 1) / p.T : 0;
     int incl = mine;
 #pragma unroll
@@ -134,7 +134,7 @@ __global__ void __launch_bounds__(kThreads) extend_simt_kernel(const SimtParams 
       tile_s = blockIdx.x - at;
     }
     before += all;
-    if ((int)blockIdx.x < before) break;
+    if ((int)blockIdx.x < before && !reports) break;
   }
   __syncthreads();
   const int b = seq_s;

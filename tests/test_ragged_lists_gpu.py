@@ -150,3 +150,20 @@ def test_joined_splits(api):
     assert int(status.item()) == 1 << api.ERR_INDEX
     assert bool((out[:3] == 7.0).all()) and bool((lse[:3] == 7.0).all())
     check_extend(step, out[3:], lse[3:], 0.125)
+
+
+@pytest.mark.parametrize("choice,dtype,d_qk", [(0, BF16, 64), (0, F32, 64), (1, F32, 64)])
+def test_the_last_of_many_sequences_is_reported(api, choice, dtype, d_qk):
+    step = Step(api, [3] * 600, [1] * 600, 4, 2, 2, d_qk, 64, dtype=dtype, seed=6).fill()
+    step.lens[599] = step.max_seqlen
+    out, status = torch.full((600, 4, 64), 7.0, dtype=dtype, device="cuda"), ints([0])
+    api.extend_kernel(choice)
+    try:
+        api.diffqkv_extend(step.q, step.cu, step.cache, 2, 2, 0.125, out=out, dev_status=status)
+    finally:
+        api.extend_kernel(0)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 1 << api.ERR_INDEX
+    assert bool((out[599] == 7.0).all())
+    step.new[599] = 0
+    check_extend(step, out, None, 0.125)
