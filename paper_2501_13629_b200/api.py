@@ -763,7 +763,11 @@ def _row_stride(x: torch.Tensor, rows: int, d: int) -> int:
     """Elements between the rows of x [rows, heads, d] whose heads are dense (a slice of a fused projection, say)."""
     st = x.stride()
     assert len(st) == 3 and x.shape[0] == rows and st[2] == 1 and (x.shape[1] == 1 or st[1] == d)
-    return st[0] if rows > 1 else 0
+    if rows <= 1:
+        return 0
+    if st[0] < x.shape[1] * d:  # one row expanded to many has stride 0, which the library takes for dense
+        raise ValueError(f"rows of {x.shape[1]} x {d} elements, but a row stride of {st[0]}")
+    return st[0]
 
 
 def diffqkv_rope_append(q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: torch.Tensor, cu_q: torch.Tensor,
