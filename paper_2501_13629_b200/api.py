@@ -662,6 +662,14 @@ def _addr(t: Optional[torch.Tensor]) -> Optional[int]:
     return None if t is None else t.data_ptr()
 
 
+def _status(t: Optional[torch.Tensor]) -> Optional[int]:
+    """Address of the status word, or None."""
+    if t is None:
+        return None
+    assert t.dtype == torch.int32 and t.numel() > 0
+    return t.data_ptr()
+
+
 def _ints(t: Optional[torch.Tensor], n: Optional[int] = None) -> Optional[int]:
     """Address of a dense int32 tensor (of n elements) or None."""
     if t is None:
@@ -670,17 +678,41 @@ def _ints(t: Optional[torch.Tensor], n: Optional[int] = None) -> Optional[int]:
     return t.data_ptr()
 
 
-def _cache_bytes(cache: KVCache) -> bytes:
-    k, v, pt = cache.k, cache.v, cache.page_table
-    ks, vs = cache.k_strides or k.stride(), cache.v_strides or v.stride()
+def _pool_strides(name: str, pool: torch.Tensor, strides: Optional[Tuple[int, int, int]], blocks: int, heads: int,
+                  tokens: int, d: int, whole: bool):
+    """Strides of a pool that holds ``blocks`` blocks of ``tokens`` tokens for ``heads`` heads of ``d`` channels; with
+    ``whole`` these are all of its heads."""
+    if strides is None:
+        b, h, t, c = pool.shape
+        sb, sh, st, one = pool.stride()
+        if c != d or one != 1 or h < heads or (whole and h != heads) or t < tokens or b < blocks:
+            raise ValueError(f"{name} {tuple(pool.shape)} does not hold {blocks} blocks x {heads} heads x {tokens} tokens x "
+                             f"{d} channels")
+        return sb, sh, st
+    end = (blocks - 1) * strides[0] + (heads - 1) * strides[1] + (tokens - 1) * strides[2] + d
+    if blocks > 0 and tokens > 0 and (
+            end > pool.untyped_storage().nbytes() // pool.element_size() - pool.storage_offset()):
+        raise ValueError(f"{name} with strides {tuple(strides)} does not hold {blocks} blocks x {heads} heads x {tokens} "
+                         f"tokens x {d} channels")
+    return strides
+
+
+def _cache_bytes(cache: KVCache, n_k: int, n_v: int, d_qk: int, d_v: int, whole: bool = False) -> bytes:
+    """The packed cache, once its pools are known to hold these heads and channels and its table every sequence."""
+    k, v, pt, lens, nb = cache.k, cache.v, cache.page_table, cache.seqlens, cache.num_blocks
+    if nb is None:
+        nb = k.shape[0]
     pages = 0
     if pt is not None:
         assert pt.dtype == torch.int32 and pt.is_contiguous() and pt.dim() == 2
-        pages = pt.shape[1]
-    nb = cache.num_blocks
-    return _pack_cache(k.data_ptr(), v.data_ptr(), ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], _ints(cache.seqlens),
-                       0 if pt is None else pt.data_ptr(), cache.page_size, pages, k.shape[0] if nb is None else nb,
-                       cache.max_seqlen)
+        rows, pages = pt.shape
+        if rows < lens.numel():
+            raise ValueError(f"a page table of {rows} rows for {lens.numel()} sequences")
+    tokens = cache.max_seqlen if pt is None and not whole else cache.page_size
+    ks = _pool_strides("cache.k", k, cache.k_strides, nb, n_k, tokens, d_qk, whole)
+    vs = _pool_strides("cache.v", v, cache.v_strides, nb, n_v, tokens, d_v, whole)
+    return _pack_cache(k.data_ptr(), v.data_ptr(), *ks, *vs, _ints(lens),
+                       0 if pt is None else pt.data_ptr(), cache.page_size, pages, nb, cache.max_seqlen)
 
 
 def _fresh(shape, dtype: torch.dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
@@ -729,9 +761,10 @@ def diffqkv_extend(q: torch.Tensor, cu_q: torch.Tensor, cache: KVCache, n_k: int
     shape = _pack_shape(batch, n_q, n_k, n_v, d_qk, d_v, _DTYPES[dtype], _DTYPES[out_dtype], scale)
     if workspace is None:
         workspace = _workspace(_raw.diffqkv_extend_workspace_bytes(shape, total_q), q.device, stream)
-    _check_status(_raw.diffqkv_extend(q.data_ptr(), _ints(cu_q, batch + 1), total_q, _cache_bytes(cache), shape,
-                                      workspace.data_ptr(), _size(workspace), out.data_ptr(), _addr(lse),
-                                      _addr(dev_status), _stream_on(stream, dev)), "diffqkv_extend")
+    _check_status(_raw.diffqkv_extend(q.data_ptr(), _ints(cu_q, batch + 1), total_q,
+                                      _cache_bytes(cache, n_k, n_v, d_qk, d_v), shape, workspace.data_ptr(),
+                                      _size(workspace), out.data_ptr(), _addr(lse), _status(dev_status),
+                                      _stream_on(stream, dev)), "diffqkv_extend")
     return out
 
 
@@ -761,13 +794,14 @@ def rope_frequencies(rot_dim: int, theta: float, scaling: str = "plain", factor:
 
 def _row_stride(x: torch.Tensor, rows: int, d: int) -> int:
     """Elements between the rows of x [rows, heads, d] whose heads are dense (a slice of a fused projection, say)."""
-    st = x.stride()
-    assert len(st) == 3 and x.shape[0] == rows and st[2] == 1 and (x.shape[1] == 1 or st[1] == d)
+    n, heads, _ = x.shape
+    row, head, one = x.stride()
+    assert n == rows and one == 1 and (heads == 1 or head == d)
     if rows <= 1:
         return 0
-    if st[0] < x.shape[1] * d:  # one row expanded to many has stride 0, which the library takes for dense
-        raise ValueError(f"rows of {x.shape[1]} x {d} elements, but a row stride of {st[0]}")
-    return st[0]
+    if row < heads * d:  # one row expanded to many has stride 0, which the library takes for dense
+        raise ValueError(f"rows of {heads} x {d} elements, but a row stride of {row}")
+    return row
 
 
 def diffqkv_rope_append(q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: torch.Tensor, cu_q: torch.Tensor,
@@ -800,9 +834,9 @@ def diffqkv_rope_append(q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: t
     code = _DTYPES[dtype]
     _check_status(_raw.diffqkv_rope_append(
         _addr(q), k_new.data_ptr(), v_new.data_ptr(), _ints(cu_q, batch + 1), total_q, q_stride,
-        _row_stride(k_new, total_q, d_qk), _row_stride(v_new, total_q, d_v), rope, _cache_bytes(cache),
-        _pack_shape(batch, n_q, n_k, n_v, d_qk, d_v, code, code, 1.0), _addr(q_out), _addr(dev_status),
-        _stream_on(stream, dev)), "diffqkv_rope_append")
+        _row_stride(k_new, total_q, d_qk), _row_stride(v_new, total_q, d_v), rope,
+        _cache_bytes(cache, n_k, n_v, d_qk, d_v), _pack_shape(batch, n_q, n_k, n_v, d_qk, d_v, code, code, 1.0),
+        _addr(q_out), _status(dev_status), _stream_on(stream, dev)), "diffqkv_rope_append")
     return q_out
 
 
@@ -817,10 +851,13 @@ def _pages_bytes(cache: KVCache, ref_counts: torch.Tensor) -> bytes:
                        cache.page_size)
 
 
-def _pools_bytes(cache: KVCache, n_k: int, n_v: int) -> bytes:
+def _pools_bytes(cache: KVCache, n_k: int, n_v: int) -> Tuple[bytes, bytes]:
+    """The packed cache and a shape for calls that move whole pages: all heads of both pools."""
     code = _DTYPES[cache.k.dtype]
     assert cache.v.dtype == cache.k.dtype
-    return _pack_shape(1, n_k * n_v, n_k, n_v, cache.k.shape[-1], cache.v.shape[-1], code, code, 1.0)
+    d_qk, d_v = cache.k.shape[-1], cache.v.shape[-1]
+    return (_cache_bytes(cache, n_k, n_v, d_qk, d_v, True),
+            _pack_shape(1, n_k * n_v, n_k, n_v, d_qk, d_v, code, code, 1.0))
 
 
 def diffqkv_pages_free(seq_ids: torch.Tensor, cache: KVCache, ref_counts: torch.Tensor,
@@ -830,7 +867,7 @@ def diffqkv_pages_free(seq_ids: torch.Tensor, cache: KVCache, ref_counts: torch.
     dev = _device_of(seq_ids, cache.page_table, cache.seqlens, ref_counts, keep_tokens, dev_status)
     n = seq_ids.numel()
     _check_status(_raw.diffqkv_pages_free(_ints(seq_ids), _ints(keep_tokens, n), n, _pages_bytes(cache, ref_counts),
-                                          _addr(dev_status), _stream_on(stream, dev)), "diffqkv_pages_free")
+                                          _status(dev_status), _stream_on(stream, dev)), "diffqkv_pages_free")
 
 
 def diffqkv_pages_fork(parents: torch.Tensor, children: torch.Tensor, cache: KVCache, ref_counts: torch.Tensor,
@@ -843,7 +880,7 @@ def diffqkv_pages_fork(parents: torch.Tensor, children: torch.Tensor, cache: KVC
     if workspace is None:
         workspace = _workspace(_raw.diffqkv_pages_fork_workspace_bytes(g, n), ref_counts.device, stream)
     _check_status(_raw.diffqkv_pages_fork(_ints(parents, n), _ints(children), n, g, workspace.data_ptr(), _size(workspace),
-                                          _addr(dev_status), _stream_on(stream, dev)), "diffqkv_pages_fork")
+                                          _status(dev_status), _stream_on(stream, dev)), "diffqkv_pages_fork")
 
 
 def diffqkv_pages_reserve(cu_q: torch.Tensor, cache: KVCache, ref_counts: torch.Tensor, n_k: int, n_v: int,
@@ -855,9 +892,9 @@ def diffqkv_pages_reserve(cu_q: torch.Tensor, cache: KVCache, ref_counts: torch.
     seqs = cache.page_table.shape[0]
     if workspace is None:
         workspace = _workspace(_raw.diffqkv_pages_reserve_workspace_bytes(g), ref_counts.device, stream)
-    _check_status(_raw.diffqkv_pages_reserve(_ints(cu_q, seqs + 1), g, _cache_bytes(cache), _pools_bytes(cache, n_k, n_v),
+    _check_status(_raw.diffqkv_pages_reserve(_ints(cu_q, seqs + 1), g, *_pools_bytes(cache, n_k, n_v),
                                              _ints(granted, seqs), workspace.data_ptr(), _size(workspace),
-                                             _addr(dev_status), _stream_on(stream, dev)), "diffqkv_pages_reserve")
+                                             _status(dev_status), _stream_on(stream, dev)), "diffqkv_pages_reserve")
 
 
 def diffqkv_pages_copy(src_ids: torch.Tensor, dst_ids: torch.Tensor, cache: KVCache, n_k: int, n_v: int,
@@ -865,15 +902,16 @@ def diffqkv_pages_copy(src_ids: torch.Tensor, dst_ids: torch.Tensor, cache: KVCa
                        stream: Optional[torch.cuda.Stream] = None) -> None:
     """Pages src_ids[i] of ``cache`` become pages dst_ids[i] of ``dst_cache`` (default: of the same cache)."""
     dev = _device_of(src_ids, dst_ids, cache.k, cache.v, dev_status)
-    src = dst = _cache_bytes(cache)
+    src, shape = _pools_bytes(cache, n_k, n_v)
+    dst = src
     if dst_cache is not None:
         _device_of(src_ids, dst_cache.k, dst_cache.v)
         assert dst_cache.k.dtype == cache.k.dtype and dst_cache.v.dtype == cache.v.dtype
         assert dst_cache.k.shape[-1] == cache.k.shape[-1] and dst_cache.v.shape[-1] == cache.v.shape[-1]
-        dst = _cache_bytes(dst_cache)
+        dst, _ = _pools_bytes(dst_cache, n_k, n_v)
     n = src_ids.numel()
-    _check_status(_raw.diffqkv_pages_copy(_ints(src_ids), _ints(dst_ids, n), n, src, dst, _pools_bytes(cache, n_k, n_v),
-                                          _addr(dev_status), _stream_on(stream, dev)), "diffqkv_pages_copy")
+    _check_status(_raw.diffqkv_pages_copy(_ints(src_ids), _ints(dst_ids, n), n, src, dst, shape, _status(dev_status),
+                                          _stream_on(stream, dev)), "diffqkv_pages_copy")
 
 
 def diffqkv_pages_compact(cache: KVCache, ref_counts: torch.Tensor, n_k: int, n_v: int,
@@ -889,8 +927,8 @@ def diffqkv_pages_compact(cache: KVCache, ref_counts: torch.Tensor, n_k: int, n_
     refs_out = ref_counts if refs_out is None else refs_out
     if workspace is None:
         workspace = _workspace(_raw.diffqkv_pages_compact_workspace_bytes(g), ref_counts.device, stream)
-    _check_status(_raw.diffqkv_pages_compact(g, _cache_bytes(cache), _pools_bytes(cache, n_k, n_v),
+    _check_status(_raw.diffqkv_pages_compact(g, *_pools_bytes(cache, n_k, n_v),
                                              _ints(table_out, cache.page_table.numel()), _ints(refs_out, ref_counts.numel()),
-                                             _ints(live, 1), workspace.data_ptr(), _size(workspace), _addr(dev_status),
+                                             _ints(live, 1), workspace.data_ptr(), _size(workspace), _status(dev_status),
                                              _stream_on(stream, dev)), "diffqkv_pages_compact")
     return table_out, refs_out

@@ -74,3 +74,55 @@ def test_broadcast_rows_are_refused(api):
     assert args[5:8] == (896, 896, 896)
     one = lambda h: z(1, h, 64).expand(1, h, 64)  # noqa: E731
     assert made(api, lambda: rope(api, q=one(8), k=one(2), v=one(4)))[5:8] == (0, 0, 0)
+
+
+def extend(api, c=None, q=None, n_k=2, n_v=4, **kw):
+    q = z(5, 8, 64) if q is None else q
+    return api.diffqkv_extend(q, ints(3), c or cache(api), n_k, n_v, 0.125, stream=STREAM, **kw)
+
+
+def test_heads_and_channels_are_the_pools(api):
+    """More heads than a pool has would be written behind a page; keys of another width are other keys."""
+    made(api, lambda: rope(api))
+    refused(api, lambda: rope(api, k=z(5, 4, 64)))
+    refused(api, lambda: rope(api, v=z(5, 8, 64)))
+    refused(api, lambda: rope(api, q=z(5, 8, 32), k=z(5, 2, 32)))
+    refused(api, lambda: rope(api, v=z(5, 4, 32)))
+    made(api, lambda: extend(api))
+    refused(api, lambda: extend(api, q=z(5, 8, 32)))
+    refused(api, lambda: extend(api, n_k=4))
+    refused(api, lambda: extend(api, n_v=8))
+    for heads in (dict(n_k=1, n_v=4), dict(n_k=4, n_v=4), dict(n_k=2, n_v=2), dict(n_k=2, n_v=8)):
+        refused(api, lambda: api.diffqkv_pages_reserve(ints(3), cache(api), ints(6), stream=STREAM, **heads))
+        refused(api, lambda: api.diffqkv_pages_copy(ints(2), ints(2), cache(api), stream=STREAM, **heads))
+        refused(api, lambda: api.diffqkv_pages_compact(cache(api), ints(6), stream=STREAM, **heads))
+    made(api, lambda: api.diffqkv_pages_reserve(ints(3), cache(api), ints(6), 2, 4, stream=STREAM))
+    made(api, lambda: api.diffqkv_pages_copy(ints(2), ints(2), cache(api, page_table=None), 2, 4, stream=STREAM))
+    made(api, lambda: api.diffqkv_pages_compact(cache(api), ints(6), 2, 4, stream=STREAM))
+    refused(api, lambda: api.diffqkv_pages_copy(ints(2), ints(2), cache(api), 2, 4, stream=STREAM,
+                                                dst_cache=cache(api, k=z(6, 1, 16, 64))))
+
+
+def test_the_pools_hold_what_the_cache_says(api):
+    for kw in (dict(num_blocks=7), dict(page_size=32, max_seqlen=96), dict(k=z(6, 2, 64, 16).transpose(2, 3)),
+               dict(page_table=ints(1, 3)), dict(page_table=None, page_size=0, max_seqlen=17)):
+        refused(api, lambda: extend(api, c=cache(api, **kw)))
+        refused(api, lambda: rope(api, c=cache(api, **kw)))
+    made(api, lambda: extend(api, c=cache(api, num_blocks=5)))
+    made(api, lambda: extend(api, c=cache(api, page_table=None, page_size=0, max_seqlen=16)))
+    # pools of any shape with strides beside them: up to their last element, and not behind it
+    flat = dict(k=z(6 * 16 * 2 * 64).view(-1, 64), v=z(6 * 16 * 4 * 64).view(-1, 64), k_strides=(2048, 64, 128),
+                v_strides=(4096, 64, 256), num_blocks=6)
+    made(api, lambda: extend(api, c=cache(api, **flat)))
+    refused(api, lambda: extend(api, c=cache(api, **dict(flat, num_blocks=7))))
+    refused(api, lambda: extend(api, c=cache(api, **dict(flat, k_strides=(2048, 64, 136)))))
+    refused(api, lambda: extend(api, c=cache(api, **dict(flat, v=flat["v"][1:]))))
+
+
+def test_the_status_word_is_an_int32(api):
+    made(api, lambda: extend(api, dev_status=ints(1)))
+    made(api, lambda: extend(api, dev_status=ints(4)[2:]))
+    for bad in (z(1), torch.zeros(1, dtype=torch.uint8), ints(0)):
+        refused(api, lambda: extend(api, dev_status=bad))
+        refused(api, lambda: rope(api, dev_status=bad))
+        refused(api, lambda: api.diffqkv_pages_free(ints(1), cache(api), ints(6), dev_status=bad, stream=STREAM))
