@@ -641,14 +641,14 @@ _DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _device_of(*tensors: Optional[torch.Tensor]) -> int:
+def _device_of(first: torch.Tensor, *others: Optional[torch.Tensor]) -> int:
     """The launch goes to the current device: every tensor (or None) has to be there."""
-    dev = tensors[0].get_device()
-    for t in tensors:
+    dev = first.get_device()
+    for t in others:
         if t is not None and t.get_device() != dev:
-            raise ValueError(f"tensors on {tensors[0].device} and {t.device}")
+            raise ValueError(f"tensors on {first.device} and {t.device}")
     if dev < 0:
-        raise ValueError(f"expected CUDA tensors, got some on {tensors[0].device}")
+        raise ValueError(f"expected CUDA tensors, got some on {first.device}")
     if dev != _current_device():
         raise ValueError(f"tensors on cuda:{dev}, but the current device is cuda:{_current_device()}")
     return dev
@@ -679,40 +679,40 @@ def _ints(t: Optional[torch.Tensor], n: Optional[int] = None) -> Optional[int]:
 
 
 def _pool_strides(name: str, pool: torch.Tensor, strides: Optional[Tuple[int, int, int]], blocks: int, heads: int,
-                  tokens: int, d: int, whole: bool):
-    """Strides of a pool that holds ``blocks`` blocks of ``tokens`` tokens for ``heads`` heads of ``d`` channels; with
-    ``whole`` these are all of its heads."""
+                  tokens: int, d: int):
+    """Strides of a pool that holds ``blocks`` blocks of ``tokens`` tokens for ``heads`` heads of ``d`` channels.  d = 0: the
+    pool's own channels, and all of its heads."""
     if strides is None:
         b, h, t, c = pool.shape
         sb, sh, st, one = pool.stride()
-        if c != d or one != 1 or h < heads or (whole and h != heads) or t < tokens or b < blocks:
-            raise ValueError(f"{name} {tuple(pool.shape)} does not hold {blocks} blocks x {heads} heads x {tokens} tokens x "
-                             f"{d} channels")
-        return sb, sh, st
-    end = (blocks - 1) * strides[0] + (heads - 1) * strides[1] + (tokens - 1) * strides[2] + d
-    if blocks > 0 and tokens > 0 and (
-            end > pool.untyped_storage().nbytes() // pool.element_size() - pool.storage_offset()):
-        raise ValueError(f"{name} with strides {tuple(strides)} does not hold {blocks} blocks x {heads} heads x {tokens} "
-                         f"tokens x {d} channels")
-    return strides
+        if c == d and one == 1 and h >= heads and t >= tokens and b >= blocks or (
+                d == 0 and one == 1 and h == heads and t >= tokens and b >= blocks):
+            return sb, sh, st
+    else:
+        sb, sh, st = strides
+        end = (blocks - 1) * sb + (heads - 1) * sh + (tokens - 1) * st + (d or pool.shape[-1])
+        if blocks <= 0 or tokens <= 0 or (
+                end <= pool.untyped_storage().nbytes() // pool.element_size() - pool.storage_offset()):
+            return strides
+    raise ValueError(f"{name} {tuple(pool.shape)} with strides {tuple(strides or pool.stride())} does not hold {blocks} blocks x "
+                     f"{heads} heads x {tokens} tokens x {d or pool.shape[-1]} channels")
 
 
-def _cache_bytes(cache: KVCache, n_k: int, n_v: int, d_qk: int, d_v: int, whole: bool = False) -> bytes:
+def _cache_bytes(cache: KVCache, n_k: int, n_v: int, d_qk: int, d_v: int) -> bytes:
     """The packed cache, once its pools are known to hold these heads and channels and its table every sequence."""
     k, v, pt, lens, nb = cache.k, cache.v, cache.page_table, cache.seqlens, cache.num_blocks
     if nb is None:
-        nb = k.shape[0]
-    pages = 0
+        nb = k.size(0)
+    tokens, pages, table = cache.max_seqlen, 0, 0
     if pt is not None:
-        assert pt.dtype == torch.int32 and pt.is_contiguous() and pt.dim() == 2
+        assert pt.dtype == torch.int32 and pt.is_contiguous()
         rows, pages = pt.shape
         if rows < lens.numel():
             raise ValueError(f"a page table of {rows} rows for {lens.numel()} sequences")
-    tokens = cache.max_seqlen if pt is None and not whole else cache.page_size
-    ks = _pool_strides("cache.k", k, cache.k_strides, nb, n_k, tokens, d_qk, whole)
-    vs = _pool_strides("cache.v", v, cache.v_strides, nb, n_v, tokens, d_v, whole)
-    return _pack_cache(k.data_ptr(), v.data_ptr(), *ks, *vs, _ints(lens),
-                       0 if pt is None else pt.data_ptr(), cache.page_size, pages, nb, cache.max_seqlen)
+        tokens, table = cache.page_size, pt.data_ptr()
+    return _pack_cache(k.data_ptr(), v.data_ptr(), *_pool_strides("cache.k", k, cache.k_strides, nb, n_k, tokens, d_qk),
+                       *_pool_strides("cache.v", v, cache.v_strides, nb, n_v, tokens, d_v), _ints(lens), table,
+                       cache.page_size, pages, nb, cache.max_seqlen)
 
 
 def _fresh(shape, dtype: torch.dtype, device, stream: Optional[torch.cuda.Stream]) -> torch.Tensor:
@@ -852,12 +852,17 @@ def _pages_bytes(cache: KVCache, ref_counts: torch.Tensor) -> bytes:
 
 
 def _pools_bytes(cache: KVCache, n_k: int, n_v: int) -> Tuple[bytes, bytes]:
-    """The packed cache and a shape for calls that move whole pages: all heads of both pools."""
-    code = _DTYPES[cache.k.dtype]
-    assert cache.v.dtype == cache.k.dtype
-    d_qk, d_v = cache.k.shape[-1], cache.v.shape[-1]
-    return (_cache_bytes(cache, n_k, n_v, d_qk, d_v, True),
-            _pack_shape(1, n_k * n_v, n_k, n_v, d_qk, d_v, code, code, 1.0))
+    """The packed cache, as far as calls that move whole pages need it, and a shape: all heads of both pools."""
+    k, v, nb, page = cache.k, cache.v, cache.num_blocks, cache.page_size
+    dtype = k.dtype
+    assert v.dtype == dtype
+    if nb is None:
+        nb = k.size(0)
+    code = _DTYPES[dtype]
+    return (_pack_cache(k.data_ptr(), v.data_ptr(), *_pool_strides("cache.k", k, cache.k_strides, nb, n_k, page, 0),
+                        *_pool_strides("cache.v", v, cache.v_strides, nb, n_v, page, 0), 0, 0, page, 0, nb,
+                        cache.max_seqlen),
+            _pack_shape(1, n_k * n_v, n_k, n_v, k.size(-1), v.size(-1), code, code, 1.0))
 
 
 def diffqkv_pages_free(seq_ids: torch.Tensor, cache: KVCache, ref_counts: torch.Tensor,
