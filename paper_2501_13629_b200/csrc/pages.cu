@@ -291,6 +291,7 @@ struct MoveParams {
   const int* dst;
   const int* count;  // device count of entries, or NULL: n
   int n;
+  int gaps;          // a source of -1: nothing to move for the entry (reserve's lists, an entry per sequence)
   int from_blocks, to_blocks;
   PoolView pool[2];
   int tasks[2];  // tasks of kTaskVecs vectors per page
@@ -324,7 +325,7 @@ __global__ void __launch_bounds__(kCopyThreads) pages_move_kernel(const MovePara
     const int i = (int)(t / per);
     int part = (int)(t - (long long)i * per);
     const int src = p.src[i], dst = p.dst[i];
-    if (src == -1 && dst == -1) continue;  // nothing to move for this entry
+    if (p.gaps && src == -1) continue;
     if (src < 0 || src >= p.from_blocks || dst < 0 || dst >= p.to_blocks) {
       if (threadIdx.x == 0) report(p.dev_status, DIFFQKV_ERR_INDEX);
       continue;
@@ -525,7 +526,7 @@ cudaError_t launch_pages_reserve(const int* cu_q, const diffqkv_pages& g, const 
   const cudaError_t err = cudaGetLastError();
   if (err != cudaSuccess) return err;
   MoveParams m;
-  m.src = ws.src; m.dst = ws.dst; m.count = nullptr; m.n = g.num_seqs;
+  m.src = ws.src; m.dst = ws.dst; m.count = nullptr; m.n = g.num_seqs; m.gaps = 1;
   m.dev_status = dev_status;
   set_pools(&m, c, c, s);
   return launch_move(m, g.num_seqs, true, stream);
@@ -534,7 +535,7 @@ cudaError_t launch_pages_reserve(const int* cu_q, const diffqkv_pages& g, const 
 cudaError_t launch_pages_copy(const int* src_ids, const int* dst_ids, int n, const diffqkv_cache& from,
                               const diffqkv_cache& to, const diffqkv_shape& s, int* dev_status, cudaStream_t stream) {
   MoveParams m;
-  m.src = src_ids; m.dst = dst_ids; m.count = nullptr; m.n = n;
+  m.src = src_ids; m.dst = dst_ids; m.count = nullptr; m.n = n; m.gaps = 0;
   m.dev_status = dev_status;
   set_pools(&m, from, to, s);
   return launch_move(m, n, false, stream);
@@ -560,7 +561,7 @@ cudaError_t launch_pages_compact(const diffqkv_pages& g, const diffqkv_cache& c,
   const cudaError_t err = cudaGetLastError();
   if (err != cudaSuccess) return err;
   MoveParams m;
-  m.src = ws.src; m.dst = ws.dst; m.count = ws.count; m.n = 0;
+  m.src = ws.src; m.dst = ws.dst; m.count = ws.count; m.n = 0; m.gaps = 0;
   m.dev_status = dev_status;
   set_pools(&m, c, c, s);
   m.map = ws.map; m.table = g.page_table; m.table_out = table_out;

@@ -167,3 +167,15 @@ def test_the_last_of_many_sequences_is_reported(api, choice, dtype, d_qk):
     assert bool((out[599] == 7.0).all())
     step.new[599] = 0
     check_extend(step, out, None, 0.125)
+
+
+@pytest.mark.parametrize("src,dst", [(-1, -1), (-1, 2), (1, -1), (-2 ** 31, -2 ** 31), (6, 6)])
+def test_a_copy_without_pages_is_reported(api, src, dst):
+    k, v = (torch.randn((6, 2, 16, 64), device="cuda").to(BF16) for _ in range(2))
+    cache = api.KVCache(k, v, ints([0]), 16, page_table=ints([[0]]), page_size=16)
+    want_k, want_v, status = k.clone(), v.clone(), ints([0])
+    want_k[5], want_v[5] = k[4], v[4]
+    api.diffqkv_pages_copy(ints([src, 4]), ints([dst, 5]), cache, 2, 2, dev_status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 1 << api.ERR_INDEX
+    assert torch.equal(k, want_k) and torch.equal(v, want_v)
