@@ -362,6 +362,8 @@ diffqkv_status diffqkv_decode_topk_ids(const void *q, const diffqkv_cache *cache
  * sums in another order, weights rounded to bf16 relative to another reference), and are bitwise reproducible from call
  * to call.  Three launches, whatever the step holds; a step known to have one row for every sequence is faster through
  * diffqkv_decode (whose seqlens count the new token).
+ * Scores are formed in fp32 in units of log 2, so that one of more than 2.35e38 counts as infinite.  A row whose scores are
+ * all -inf has out = 0 and lse = -inf; a NaN or +inf among them makes both NaN.
  * As in any tensor-core attention a weight of zero multiplies the V rows of later tokens of the same chunk; those rows
  * must be finite.  What lies behind the last cached token in its page may hold anything.
  */

@@ -60,8 +60,9 @@ struct GenericSmem {
 
 // Attention of query head h of sequence b over cached tokens [t0, t1), t0 < t1: running maximum and sum (base-2
 // domain) and the un-normalised output channels tid, tid + kThreads, ... of this thread.  q_s holds the query times
-// scale * log2(e).  All threads of the block call it.
-template <typename T>
+// scale * log2(e).  All threads of the block call it.  kKeepNan: a score that is NaN makes the sum NaN even where no other
+// score is a number above -inf (otherwise it counts as -inf there).
+template <typename T, bool kKeepNan = false>
 __device__ void attend_range(const DecodeParams& p, int b, int h, int t0, int t1, const float* q_s, GenericSmem& sm,
                              float& m_run, float& l_run, float (&acc)[kMaxAccPerThread]) {
   const int tid = threadIdx.x;
@@ -110,6 +111,8 @@ __device__ void attend_range(const DecodeParams& p, int b, int h, int t0, int t1
     if (m_new != -INFINITY) {  // all tokens of the tile may have been rejected
       alpha = exp2f(m_run - m_new);
       pj = exp2f(sc - m_new);
+    } else if (kKeepNan && sc != sc) {
+      pj = sc;
     }
     sm.p_s[tid] = pj;
     sm.vrow_s[tid] = vrow;
@@ -503,9 +506,8 @@ __global__ void __launch_bounds__(kThreads) extend_generic_kernel(DecodeParams p
   for (int e = tid; e < p.d_qk; e += kThreads) q_s[e] = to_float(q[e]) * p.scale_log2;
   __syncthreads();
   float m_run, l_run, acc[kMaxAccPerThread];
-  attend_range<T>(p, b, h, 0, past + (t - lo) + 1, q_s, sm, m_run, l_run, acc);
-  // every row sees itself: a sum of zero means that no score was a number above -inf, and the result is none either
-  const float inv = 1.f / l_run;
+  attend_range<T, true>(p, b, h, 0, past + (t - lo) + 1, q_s, sm, m_run, l_run, acc);
+  const float inv = l_run != 0.f ? 1.f / l_run : 0.f;  // zero: all scores are -inf
 #pragma unroll
   for (int e = 0; e < kMaxAccPerThread; ++e) {
     const int ch = tid + e * kThreads;
@@ -514,7 +516,7 @@ __global__ void __launch_bounds__(kThreads) extend_generic_kernel(DecodeParams p
       else reinterpret_cast<__nv_bfloat16*>(out)[row * p.d_v + ch] = __float2bfloat16_rn(acc[e] * inv);
     }
   }
-  if (lse && tid == 0) lse[row] = l_run != 0.f ? (m_run + log2f(l_run)) * kLn2 : __int_as_float(0x7fffffff);
+  if (lse && tid == 0) lse[row] = l_run != 0.f ? (m_run + log2f(l_run)) * kLn2 : -INFINITY;
 }
 
 }  // namespace

@@ -1,0 +1,77 @@
+"""diffqkv_extend on scores at the edges of their type: first tokens far below all others or at -inf, scores that are all far
+from zero, and maxima that rise from tile to tile; against the definition in float64."""
+import math
+
+import pytest
+import torch
+
+from ragged import BF16, F32, HALF_STEP, Step
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def api():
+    from paper_2501_13629_b200 import api as _api
+    return _api
+
+
+def check(step, out, lse, scale):
+    """Bounds as in ragged.check_extend, with the size of the scores taken per row over the tokens whose weight is at least
+    1e-30: the others' weights are zero or add less than t 1e-30 to the result, whatever their scores are off by (scores
+    below -10^4 are off by less than a thousandth of themselves)."""
+    assert bool(torch.isfinite(out).all()) and not bool(torch.isnan(lse).any())
+    for b, (past, n) in enumerate(zip(step.past, step.new)):
+        lo, t = step.cu_host[b], step.total[b]
+        q = step.q[lo:lo + n].double()
+        k = step.k_tok[b].double().repeat_interleave(step.n_q // step.n_k, 1)
+        v = step.v_tok[b].double().repeat_interleave(step.n_q // step.n_v, 1)
+        x = torch.einsum("ihd,jhd->ihj", q, k) * scale
+        hidden = torch.arange(t, device="cuda")[None] > past + torch.arange(n, device="cuda")[:, None]
+        x = torch.where(x * math.log2(math.e) < -torch.finfo(F32).max, -math.inf, x)  # beyond fp32 in units of log 2
+        x = x.masked_fill(hidden[:, None], -math.inf)
+        ref_lse = torch.logsumexp(x, 2)
+        none = ref_lse == -math.inf  # such a row has nothing
+        assert bool((out[lo:lo + n][none] == 0).all()) and bool((lse[lo:lo + n][none] == -math.inf).all())
+        ref_lse = ref_lse.masked_fill(none, 0.0)
+        p = torch.exp(x - ref_lse[..., None])
+        size = torch.einsum("ihd,jhd->ihj", q.abs(), k.abs()) * scale
+        big = torch.where(p >= 1e-30, size, 0.0).amax(2).clamp(min=1.0)
+        ref, mean_abs = torch.einsum("ihj,jhd->ihd", p, v), torch.einsum("ihj,jhd->ihd", p, v.abs())
+        score = (step.d_qk + 16) * 2.0 ** -24 * big
+        weight = (2 * score + (t + 16) * 2.0 ** -24 + (HALF_STEP[BF16] if step.dtype == BF16 else 0.0))[..., None]
+        bound = weight * mean_abs * (1 + weight) + 1e-25
+        bound = bound + HALF_STEP[out.dtype] * (ref.abs() + bound)
+        err = (out[lo:lo + n].double() - ref).abs()
+        assert bool((err <= bound).all()), f"sequence {b}: {float((err / bound).max()):.2f} times the bound"
+        bound = score + (t + 16) * 2.0 ** -24 + 2.0 ** -22 * ref_lse.abs()
+        err = (lse[lo:lo + n].double().masked_fill(none, 0.0) - ref_lse).abs()
+        assert bool((err <= bound).all()), f"sequence {b}: lse {float((err / bound).max()):.2f} times the bound"
+
+
+def made(api, past, new, heads, dims, dtype, level, seed):
+    """Scores of about one in size around level(token numbers): the first channel of every query is 1."""
+    step = Step(api, past, new, *heads, *dims, dtype=dtype, seed=seed)
+    spread = dims[0] ** -0.25
+    step.q = (step.q.float() * spread).to(dtype)
+    step.q[..., 0] = 1.0
+    for b, t in enumerate(step.total):
+        step.k_tok[b] = (step.k_tok[b].float() * spread).to(dtype)
+        step.k_tok[b][:, :, 0] = level(torch.arange(t, device="cuda")).to(dtype)[:, None]
+    return step.fill()
+
+
+@pytest.mark.parametrize("dims,dtype", [((128, 128), BF16), ((64, 64), BF16), ((64, 64), F32), ((96, 64), F32), ((96, 64), BF16)])
+@pytest.mark.parametrize("bad", [-math.inf, math.nan, math.inf])
+def test_keys_that_are_not_finite(api, dims, dtype, bad):
+    """All visible keys at -inf: nothing; at NaN or +inf: NaN; rows that see numbers beside -inf: the numbers."""
+    for new in ([1, 2], [4, 150]):
+        step = made(api, [140, 0], new, (8, 2, 4), dims, dtype, lambda j: torch.where(j < 142, bad, 1.0), 4)
+        out = torch.empty((step.total_q, 8, step.d_v), dtype=F32, device="cuda")
+        lse = torch.empty((step.total_q, 8), dtype=F32, device="cuda")
+        api.diffqkv_extend(step.q, step.cu, step.cache, 2, 4, 1.0, out=out, lse=lse)
+        torch.cuda.synchronize()
+        if bad == -math.inf:
+            check(step, out, lse, 1.0)
+        else:
+            assert bool(out.isnan().all()) and bool(lse.isnan().all())
