@@ -13,7 +13,8 @@
 // The reference of a column (what its scores are taken from before the exponential) has to be one for all four warps of
 // a softmax group, whose tokens meet in one accumulator.  It starts as the score of the segment's first token, which
 // needs no search, and is raised to a tile's maximum when some score exceeds it by 2^24; the warps agree on that
-// through one hardware barrier per tile.  Weights of up to 2^24 are harmless: bf16 and fp32 have the range, the
+// through one hardware barrier per tile.  That first score may be any number, or -inf, which counts as the lowest
+// number: a raised column is formed from its scores again, not from distances to a reference far below.  Weights of up to 2^24 are harmless: bf16 and fp32 have the range, the
 // relative precision of either does not depend on the magnitude, and the quotient takes the factor out again.
 //
 // Work: one flat list of (sequence, unit of heads, 128-token tile), divided evenly over one persistent block per SM (or
@@ -41,6 +42,7 @@ namespace {
 constexpr int kSoftmaxWarp0 = 2, kGroupWarps = 8;
 constexpr int kHalfCols = kThinCols / 2;
 constexpr float kThinThreshold = 24.f;  // log2 domain
+constexpr float kLowest = -3.402823466e38f;
 constexpr int kQRegion = 4 * 16384;  // two Q buffers and two P^T buffers of 16 KB
 
 struct ThinSegment {
@@ -535,41 +537,42 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         ok = wait_warp(s_full0 + 8 * t, par, abort_flag) && ok;
         tc::fence_after_sync();
         float x[kHalfCols];
-#pragma unroll
-        for (int q = 0; q < kHalfCols / 8; ++q)
-          if (mask >> q & 1) tc::ld_32x32b_x8(s_taddr + q * 8, *reinterpret_cast<uint32_t(*)[8]>(&x[q * 8]));
-        tc::wait_ld();
         const int k0 = (w.ta + i) * kKT;
-        if (k0 + kKT > w.past + 1) {  // the tile reaches past some row's position
-          const int hidden = (k0 + r - w.past) * p.G;  // columns of a group below this belong to rows before the token
+        auto load_scores = [&] {  // they stay in tensor memory until this tile's weights are announced
 #pragma unroll
           for (int q = 0; q < kHalfCols / 8; ++q)
-            if (mask >> q & 1) {
-              const int first = hidden - ((c0 + q * 8) & (p.region - 1));
+            if (mask >> q & 1) tc::ld_32x32b_x8(s_taddr + q * 8, *reinterpret_cast<uint32_t(*)[8]>(&x[q * 8]));
+          tc::wait_ld();
+          if (k0 + kKT > w.past + 1) {  // the tile reaches past some row's position
+            const int hidden = (k0 + r - w.past) * p.G;  // columns of a group below this belong to rows before the token
 #pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (e < first) x[q * 8 + e] = -INFINITY;
-            }
-        }
+            for (int q = 0; q < kHalfCols / 8; ++q)
+              if (mask >> q & 1) {
+                const int first = hidden - ((c0 + q * 8) & (p.region - 1));
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                  if (e < first) x[q * 8 + e] = -INFINITY;
+              }
+          }
+        };
+        load_scores();
         // ---- scores on the scale of base 2, from the reference: the score of the segment's first token of this group to
-        // begin with (a row that does not see it sees none of the tile: reference 0, weights 0)
+        // begin with (a row that does not see it sees none of the tile)
         if (!later) {
+          if (quarter == 0 && lane == 0) {
+            // -inf counts as the lowest number, which any other raises
+            auto start = [&](float y) { y *= p.scale_log2; return y == -INFINITY ? kLowest : y; };
 #pragma unroll
-          for (int q = 0; q < kHalfCols / 8; ++q)
-            if (mask >> q & 1) {
-#pragma unroll
-              for (int e = 0; e < 8; ++e) x[q * 8 + e] *= p.scale_log2;
-              if (quarter == 0 && lane == 0) {
+            for (int q = 0; q < kHalfCols / 8; ++q)
+              if (mask >> q & 1) {
 #pragma unroll
                 for (int c = q * 8; c < q * 8 + 8; c += 4)
-                  *reinterpret_cast<float4*>(m + c) = make_float4(x[c] == -INFINITY ? 0.f : x[c], x[c + 1] == -INFINITY ? 0.f : x[c + 1],
-                                                                  x[c + 2] == -INFINITY ? 0.f : x[c + 2], x[c + 3] == -INFINITY ? 0.f : x[c + 3]);
+                  *reinterpret_cast<float4*>(m + c) = make_float4(start(x[c]), start(x[c + 1]), start(x[c + 2]), start(x[c + 3]));
               }
-            }
+          }
           group_sync(bar_id);
         }
         bool over = !ok;
-        const float f = later ? p.scale_log2 : 1.f;
 #pragma unroll
         for (int q = 0; q < kHalfCols / 8; ++q)
           if (mask >> q & 1) {
@@ -577,12 +580,13 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               const int c = q * 8 + e;
-              x[c] = fmaf(x[c], f, -m[c]);
+              x[c] = fmaf(x[c], p.scale_log2, -m[c]);
               over |= x[c] > kThinThreshold && e < end;
             }
           }
         if (group_any(bar_id, over)) {
           // ---- largest score of every column in this tile; the reference goes up where it is passed
+          load_scores();
           float y[kHalfCols / 2];  // over the lanes, half of the columns in every step; lane c ends with column c
 #pragma unroll
           for (int c = 0; c < 16; ++c) {
@@ -602,13 +606,14 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
           if (later) ok = wait_warp(o_done0 + 8 * t, par ^ 1, abort_flag) && ok;
           if (group_any(bar_id, !ok)) { ok = false; break; }
           if (wq == 0) {  // a lane per column
-            float up = fmaxf(fmaxf(top, sc.part[t][1][c0 + lane]), fmaxf(sc.part[t][2][c0 + lane], sc.part[t][3][c0 + lane]));
-            up = up > kThinThreshold ? up : 0.f;  // x is relative to the reference
-            sc.part[t][0][c0 + lane] = up;
-            m[lane] += up;
+            const float largest = p.scale_log2 * fmaxf(fmaxf(top, sc.part[t][1][c0 + lane]),
+                                                       fmaxf(sc.part[t][2][c0 + lane], sc.part[t][3][c0 + lane]));
+            const float was = m[lane], now = largest - was > kThinThreshold ? largest : was;
+            sc.part[t][0][c0 + lane] = now != was ? ex2(was - now) : 1.f;
+            m[lane] = now;
           }
           group_sync(bar_id);
-          const float* rise = &sc.part[t][0][c0];
+          const float* alphas = &sc.part[t][0][c0];
           tc::fence_after_sync();
 #pragma unroll
           for (int q = 0; q < kHalfCols / 8; ++q) {
@@ -620,10 +625,9 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              const float up = rise[q * 8 + e];
-              x[q * 8 + e] -= up;
+              x[q * 8 + e] = fmaf(x[q * 8 + e], p.scale_log2, -m[q * 8 + e]);
               if (later) {
-                const float alpha = ex2(-up);
+                const float alpha = alphas[q * 8 + e];
                 l[q * 8 + e] *= alpha;
                 o[e] = __float_as_uint(__uint_as_float(o[e]) * alpha);
               }

@@ -9,6 +9,8 @@ from ragged import BF16, F32, HALF_STEP, Step
 
 pytestmark = pytest.mark.gpu
 
+TILE = 128  # tokens
+
 
 @pytest.fixture(scope="module")
 def api():
@@ -49,6 +51,16 @@ def check(step, out, lse, scale):
         assert bool((err <= bound).all()), f"sequence {b}: lse {float((err / bound).max()):.2f} times the bound"
 
 
+def run(api, step, scale=1.0):
+    out = torch.empty((step.total_q, step.n_q, step.d_v), dtype=F32, device="cuda")
+    lse = torch.empty((step.total_q, step.n_q), dtype=F32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    api.diffqkv_extend(step.q, step.cu, step.cache, step.n_k, step.n_v, scale, out=out, lse=lse, dev_status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    check(step, out, lse, scale)
+
+
 def made(api, past, new, heads, dims, dtype, level, seed):
     """Scores of about one in size around level(token numbers): the first channel of every query is 1."""
     step = Step(api, past, new, *heads, *dims, dtype=dtype, seed=seed)
@@ -59,6 +71,34 @@ def made(api, past, new, heads, dims, dtype, level, seed):
         step.k_tok[b] = (step.k_tok[b].float() * spread).to(dtype)
         step.k_tok[b][:, :, 0] = level(torch.arange(t, device="cuda")).to(dtype)[:, None]
     return step.fill()
+
+
+STEPS = {"one token": ([5], [1]), "a few": ([126, 700], [3, 1]), "long caches": ([3000, 20, 9000], [2, 5, 1]),
+         "long chunks": ([0, 300], [140, 70])}
+
+
+@pytest.mark.parametrize("low", [-math.inf, -3.38e38, -1e7, -1e5, -3e4, -1e3])
+@pytest.mark.parametrize("others", [0.0, -300.0])
+@pytest.mark.parametrize("step", STEPS)
+@pytest.mark.parametrize("dims,dtype", [((128, 128), BF16), ((64, 64), BF16), ((64, 128), BF16), ((64, 64), F32), ((96, 64), F32)])
+def test_first_tokens_far_below(api, low, others, step, dims, dtype):
+    """The first token of every tile has a score of -inf or far below all others' (and no weight worth a number)."""
+    level = lambda j: torch.where(j % TILE == 0, low, others)  # noqa: E731
+    run(api, made(api, *STEPS[step], (16, 2, 4), dims, dtype, level, 1))
+
+
+@pytest.mark.parametrize("rise", [20.0, 60.0, 2000.0, -60.0])
+@pytest.mark.parametrize("step", STEPS)
+@pytest.mark.parametrize("dims,dtype", [((128, 128), BF16), ((64, 64), BF16), ((64, 64), F32)])
+def test_maxima_move_from_tile_to_tile(api, rise, step, dims, dtype):
+    level = lambda j: -800.0 + rise * (j // TILE)  # noqa: E731
+    run(api, made(api, *STEPS[step], (32, 4, 8), dims, dtype, level, 2))
+
+
+@pytest.mark.parametrize("level", [-1e4, 1e4])
+@pytest.mark.parametrize("step", STEPS)
+def test_scores_far_from_zero(api, level, step):
+    run(api, made(api, *STEPS[step], (8, 4, 2), (128, 128), BF16, lambda j: torch.full_like(j, level, dtype=F32), 3))
 
 
 @pytest.mark.parametrize("dims,dtype", [((128, 128), BF16), ((64, 64), BF16), ((64, 64), F32), ((96, 64), F32), ((96, 64), BF16)])
