@@ -468,10 +468,12 @@ diffqkv_status diffqkv_pages_fork(const int32_t *parents, const int32_t *childre
  * (count > 1 at the start of the call) are replaced, and where past_b lies inside such a page its contents are copied
  * to the new one (copy on write).  If all holders of a page write in the same call each gets a copy.
  * A sequence gets all it needs or nothing: b is denied when the demands of sequences 0 .. b together exceed the free
- * pages (DIFFQKV_ERR_PAGES) or its row is too short (DIFFQKV_ERR_INDEX).  The rows of a denied sequence must not be
- * written in this step: pages of its that others share are as they were, and missing ones are missing.
+ * pages (DIFFQKV_ERR_PAGES), or its rows do not fit or its table row is too short (DIFFQKV_ERR_INDEX).  The rows of a
+ * denied sequence must not be written in this step: pages of its that others share are as they were, and missing ones are
+ * missing.
  *   cache, shape  the pools (pointers, strides, num_blocks = pages->num_pages); shape gives n_k, n_v, d_qk, d_v, dtype;
- *                 cache->page_table and cache->seqlens are not used
+ *                 cache->page_table and cache->seqlens are not used; max_seqlen that of the calls which write the rows
+ *                 (0 = the table rows' length alone).  total_q is not known here: rows beyond it are theirs to skip
  *   granted       [num_seqs] int32: 1 = its rows may be written, 0 = denied; or NULL
  *   workspace     diffqkv_pages_reserve_workspace_bytes(pages) bytes, 256-byte aligned
  */

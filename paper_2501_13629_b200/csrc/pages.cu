@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(256) pages_fork_write_kernel(const int* childr
 // ---------------------------------------------------------------------------------------------------------- reserve
 
 struct ReserveWs {
-  int* demand;     // [num_seqs] pages the sequence asks for; -1 = its row is too short (or cu_q out of order)
+  int* demand;     // [num_seqs] pages the sequence asks for; -1 = its rows do not fit
   int* base;       // [num_seqs] rank of its first page among all handed out, -1 = denied
   int* free_count; // [kClusterBlocks] free pages in each block's share of the counts
   int* fresh;      // [num_pages] the free ids, lowest first
@@ -169,14 +169,18 @@ __device__ __forceinline__ int for_needed(const diffqkv_pages& g, int first, int
   return found;
 }
 
-// The entries of sequence s that the step writes: [first, end); false when its row is too short.
-__device__ __forceinline__ bool write_range(const diffqkv_pages& g, const int* cu_q, int s, int& len, int& first, int& end) {
-  len = max(g.seqlens[s], 0);
+// The entries of sequence s that the step writes: [first, end); false when its rows do not fit, as the calls that write them
+// have it (max_seqlen > 0), or its row of the table is too short.
+__device__ __forceinline__ bool write_range(const diffqkv_pages& g, const int* cu_q, int max_seqlen, int s, int& len,
+                                            int& first, int& end) {
+  const int held = g.seqlens[s];
+  len = max(held, 0);
   const long long n = (long long)cu_q[s + 1] - cu_q[s];
   first = len / g.page_size;
   end = first;
   if (n < 0) return false;  // cu_q out of order
   if (n == 0) return true;
+  if (held < 0 || cu_q[s] < 0 || (max_seqlen > 0 && held + n > max_seqlen)) return false;
   const long long need = (len + n + g.page_size - 1) / g.page_size;
   if (need > g.max_pages_per_seq) return false;
   end = (int)need;
@@ -184,7 +188,7 @@ __device__ __forceinline__ bool write_range(const diffqkv_pages& g, const int* c
 }
 
 __global__ void __cluster_dims__(kClusterBlocks, 1, 1) __launch_bounds__(kScanThreads)
-pages_reserve_kernel(const int* cu_q, diffqkv_pages g, ReserveWs ws, int* granted, int* dev_status) {
+pages_reserve_kernel(const int* cu_q, diffqkv_pages g, int max_seqlen, ReserveWs ws, int* granted, int* dev_status) {
   __shared__ int red[33];
   const int rank = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
   const int warp_all = rank * (kScanThreads / 32) + (tid >> 5), warps_all = kClusterBlocks * (kScanThreads / 32);
@@ -195,7 +199,7 @@ pages_reserve_kernel(const int* cu_q, diffqkv_pages g, ReserveWs ws, int* grante
   // ---- what every sequence asks for, and how many pages are free
   for (int s = warp_all; s < g.num_seqs; s += warps_all) {
     int len, first, end;
-    const bool fits = write_range(g, cu_q, s, len, first, end);
+    const bool fits = write_range(g, cu_q, max_seqlen, s, len, first, end);
     const int* row = g.page_table + (long long)s * g.max_pages_per_seq;
     const int n = fits ? for_needed(g, first, end, row, [](int, int, int) {}) : -1;
     if (lane == 0) ws.demand[s] = n;
@@ -253,7 +257,7 @@ pages_reserve_kernel(const int* cu_q, diffqkv_pages g, ReserveWs ws, int* grante
     int src = -1, dst = -1;
     if (base >= 0) {
       int len, first, end;
-      write_range(g, cu_q, s, len, first, end);
+      write_range(g, cu_q, max_seqlen, s, len, first, end);
       int* row = g.page_table + (long long)s * g.max_pages_per_seq;
       for_needed(g, first, end, row, [&](int e, int id, int k) {
         const int now = ws.fresh[base + k];
@@ -521,7 +525,8 @@ cudaError_t launch_pages_reserve(const int* cu_q, const diffqkv_pages& g, const 
   ws.dst = take(sizeof(int) * (size_t)g.num_seqs);
   ws.fresh = take(sizeof(int) * (size_t)g.num_pages);
   ws.old = take(sizeof(int) * (size_t)g.num_pages);
-  pages_reserve_kernel<<<kClusterBlocks, kScanThreads, 0, stream>>>(cu_q, g, ws, granted, dev_status);
+  pages_reserve_kernel<<<kClusterBlocks, kScanThreads, 0, stream>>>(cu_q, g, c.max_seqlen, ws, granted,
+                                                                      dev_status);
   count_launch();
   const cudaError_t err = cudaGetLastError();
   if (err != cudaSuccess) return err;

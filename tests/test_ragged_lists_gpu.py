@@ -179,3 +179,30 @@ def test_a_copy_without_pages_is_reported(api, src, dst):
     torch.cuda.synchronize()
     assert int(status.item()) == 1 << api.ERR_INDEX
     assert torch.equal(k, want_k) and torch.equal(v, want_v)
+
+
+@pytest.mark.parametrize("cu,past,fits", [
+    ([0, 10, 20, 30, 44], [55, 54, 10, 51], [0, 1, 1, 0]),                  # past + n up to the capacity, and one more
+    ([0, 10, 20, 30, 44], [2 ** 31 - 1, -1, 54, -2 ** 31], [0, 0, 1, 0]),
+    ([-3, 20, 24, 30, 44], [10, 20, 58, 1], [0, 1, 1, 1]),
+    ([0, 20, 19, 30, 30], [10, 20, 40, 50], [1, 0, 1, 1]),
+    ([0, 0, 0, 0, 1], [-1, 65, 64, 64], [1, 1, 1, 0]),                      # nothing to write fits anywhere
+])
+def test_reserve_grants_what_the_other_calls_write(api, cu, past, fits):
+    """A table row has room for 72 tokens, a sequence for 64."""
+    k, v, _ = pools(2, 2, 64, 64, BF16, True, 7)
+    table, refs = torch.full((4, ROW), -1, dtype=torch.int32, device="cuda"), torch.zeros(5 * ROW, dtype=torch.int32, device="cuda")
+    granted, status = ints([9] * 4), ints([0])
+    cache = api.KVCache(k, v, ints(past), CAP, page_table=table, page_size=PAGE)
+    api.diffqkv_pages_reserve(ints(cu), cache, refs, 2, 2, granted=granted, dev_status=status)
+    torch.cuda.synchronize()
+    assert granted.tolist() == fits
+    assert int(status.item()) == 1 << api.ERR_INDEX
+    want, used = [[-1] * ROW for _ in range(4)], 0
+    for b, ok in enumerate(fits):
+        lo, hi = cu[b], cu[b + 1]
+        if ok and hi > lo:
+            for e in range(past[b] // PAGE, -(-(past[b] + hi - lo) // PAGE)):
+                want[b][e], used = used, used + 1
+    assert table.tolist() == want
+    assert refs.tolist() == [1] * used + [0] * (5 * ROW - used)
