@@ -470,7 +470,8 @@ diffqkv_status diffqkv_pages_fork(const int32_t *parents, const int32_t *childre
  * A sequence gets all it needs or nothing: b is denied when the demands of sequences 0 .. b together exceed the free
  * pages (DIFFQKV_ERR_PAGES), or its rows do not fit or its table row is too short (DIFFQKV_ERR_INDEX).  The rows of a
  * denied sequence must not be written in this step: pages of its that others share are as they were, and missing ones are
- * missing.
+ * missing.  A step that cannot ask the host (a captured one) gives diffqkv_rope_append and diffqkv_extend a seqlens array of
+ * its own with -1 where granted is 0: they skip such a sequence and report it.
  *   cache, shape  the pools (pointers, strides, num_blocks = pages->num_pages); shape gives n_k, n_v, d_qk, d_v, dtype;
  *                 cache->page_table and cache->seqlens are not used; max_seqlen that of the calls which write the rows
  *                 (0 = the table rows' length alone).  total_q is not known here: rows beyond it are theirs to skip

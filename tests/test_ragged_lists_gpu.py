@@ -206,3 +206,51 @@ def test_reserve_grants_what_the_other_calls_write(api, cu, past, fits):
                 want[b][e], used = used, used + 1
     assert table.tolist() == want
     assert refs.tolist() == [1] * used + [0] * (5 * ROW - used)
+
+
+def test_denied_sequences_are_left_out_of_a_captured_step(api):
+    """reserve -> lengths of the granted ones -> rope_append -> extend, captured.  Sequence 1 shares a half-filled page with
+    sequence 0 and gets no page of its own once the pool has run out: sequence 0's tokens stay what they were."""
+    n_q, n_k, n_v, d, page, n_pages = 4, 2, 2, 64, 16, 4
+    g = torch.Generator("cuda").manual_seed(8)
+    rand = lambda *s: torch.randn(s, generator=g, device="cuda").to(BF16)  # noqa: E731
+    k, v = rand(n_pages, n_k, page, d), rand(n_pages, n_v, page, d)
+    table, refs, lens = ints([[0, -1], [0, -1], [1, -1]]), ints([2, 1, 0, 0]), ints([5, 5, 9])
+    cu, granted, status, seen = ints([0, 1, 2, 3]), ints([0] * 3), ints([0]), ints([0] * 3)
+    q, k_new, v_new = rand(3, n_q, d), rand(3, n_k, d), rand(3, n_v, d)
+    out = torch.zeros((3, n_q, d), dtype=BF16, device="cuda")
+    cache = api.KVCache(k, v, lens, 2 * page, page_table=table, page_size=page)
+    writes = api.KVCache(k, v, seen, 2 * page, page_table=table, page_size=page)
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+
+    def step():
+        api.diffqkv_pages_reserve(cu, cache, refs, n_k, n_v, granted=granted, workspace=ws, dev_status=status)
+        seen.copy_(torch.where(granted > 0, lens, -1))
+        api.diffqkv_rope_append(q, k_new, v_new, cu, writes, None, q_out=q, dev_status=status)
+        api.diffqkv_extend(q, cu, writes, n_k, n_v, 0.125, out=out, workspace=ws, dev_status=status)
+
+    state = [x.clone() for x in (k, v, table, refs, lens)]
+    step()  # two free pages: 0 and 1 write, each gets a copy
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0 and granted.tolist() == [1, 1, 1] and table.tolist() == [[2, -1], [3, -1], [1, -1]]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for x, y in zip((k, v, table, refs, lens), state):
+        x.copy_(y)
+    refs.copy_(ints([2, 1, 1, 0]))  # one free page
+    status.zero_(), out.fill_(3.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert granted.tolist() == [1, 0, 1] and int(status.item()) == (1 << api.ERR_PAGES) | (1 << api.ERR_INDEX)
+    assert table.tolist() == [[3, -1], [0, -1], [1, -1]] and refs.tolist() == [1, 1, 1, 1]
+    want_k, want_v = state[0].clone(), state[1].clone()
+    for pool, new in ((want_k, k_new), (want_v, v_new)):
+        pool[3] = pool[0]  # sequence 0's copy
+        pool[3, :, 5], pool[1, :, 9] = new[0], new[2]
+    assert torch.equal(k, want_k) and torch.equal(v, want_v)
+    assert bool((out[1] == 3.0).all())
+    for b, (blk, n) in ((0, (3, 6)), (2, (1, 10))):
+        ref, _, _, _ = attend64(q[b:b + 1], k[blk, :, :n].transpose(0, 1), v[blk, :, :n].transpose(0, 1), 0.125, n - 1)
+        # a weight is off by half a step of bf16 and little besides, the result by another
+        assert bool(((out[b:b + 1].double() - ref).abs() <= 3 * 2.0 ** -8 * v[blk, :, :n].double().abs().amax()).all())
