@@ -148,30 +148,31 @@ _lib.diffqkv_profile_split_events.restype = None
 _lib.diffqkv_profile_split_events.argtypes = [C.c_void_p, C.c_void_p]
 
 
-_SHAPE, _CACHE, _PAGES = C.POINTER(ShapeStruct), C.POINTER(CacheStruct), C.POINTER(PagesStruct)
+# The ragged calls.  They take a few microseconds on the GPU when the step is small, so their wrappers pack the argument
+# structs into bytes (fields as in the ctypes structures above) and hand addresses over as plain integers; an argument
+# that points to a struct takes such bytes as well as C.byref of a structure.
+_raw = _lib
+_S, _V, _I, _L, _Z = C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
 for _name, _res, _args in (
-        ("diffqkv_extend_workspace_bytes", C.c_size_t, [_SHAPE, C.c_int32]),
-        ("diffqkv_extend", C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, _CACHE, _SHAPE, C.c_void_p, C.c_size_t,
-                                     C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
-        ("diffqkv_rope_frequencies", C.c_int, [C.c_int32, C.c_double, C.c_int, C.c_double, C.c_double, C.c_double,
-                                               C.c_double, C.POINTER(C.c_double), C.POINTER(C.c_float)]),
-        ("diffqkv_rope_append", C.c_int, [C.c_void_p] * 4 + [C.c_int32, C.c_int64, C.c_int64, C.c_int64,
-                                                             C.POINTER(RopeStruct), _CACHE, _SHAPE, C.c_void_p,
-                                                             C.c_void_p, C.c_void_p]),
-        ("diffqkv_pages_free", C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, _PAGES, C.c_void_p, C.c_void_p]),
-        ("diffqkv_pages_fork_workspace_bytes", C.c_size_t, [_PAGES, C.c_int32]),
-        ("diffqkv_pages_fork", C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, _PAGES, C.c_void_p, C.c_size_t, C.c_void_p,
-                                         C.c_void_p]),
-        ("diffqkv_pages_reserve_workspace_bytes", C.c_size_t, [_PAGES]),
-        ("diffqkv_pages_reserve", C.c_int, [C.c_void_p, _PAGES, _CACHE, _SHAPE, C.c_void_p, C.c_void_p, C.c_size_t,
-                                            C.c_void_p, C.c_void_p]),
-        ("diffqkv_pages_copy", C.c_int, [C.c_void_p, C.c_void_p, C.c_int32, _CACHE, _CACHE, _SHAPE, C.c_void_p,
-                                         C.c_void_p]),
-        ("diffqkv_pages_compact_workspace_bytes", C.c_size_t, [_PAGES]),
-        ("diffqkv_pages_compact", C.c_int, [_PAGES, _CACHE, _SHAPE, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
-                                            C.c_size_t, C.c_void_p, C.c_void_p])):
-    getattr(_lib, _name).restype = _res
-    getattr(_lib, _name).argtypes = _args
+        ("diffqkv_extend_workspace_bytes", _Z, [_S, _I]),
+        ("diffqkv_extend", C.c_int, [_V, _V, _I, _S, _S, _V, _Z, _V, _V, _V, _V]),
+        ("diffqkv_rope_frequencies", C.c_int, [_I, C.c_double, C.c_int, C.c_double, C.c_double, C.c_double, C.c_double,
+                                               C.POINTER(C.c_double), C.POINTER(C.c_float)]),
+        ("diffqkv_rope_append", C.c_int, [_V, _V, _V, _V, _I, _L, _L, _L, _S, _S, _S, _V, _V, _V]),
+        ("diffqkv_pages_free", C.c_int, [_V, _V, _I, _S, _V, _V]),
+        ("diffqkv_pages_fork_workspace_bytes", _Z, [_S, _I]),
+        ("diffqkv_pages_fork", C.c_int, [_V, _V, _I, _S, _V, _Z, _V, _V]),
+        ("diffqkv_pages_reserve_workspace_bytes", _Z, [_S]),
+        ("diffqkv_pages_reserve", C.c_int, [_V, _S, _S, _S, _V, _V, _Z, _V, _V]),
+        ("diffqkv_pages_copy", C.c_int, [_V, _V, _I, _S, _S, _S, _V, _V]),
+        ("diffqkv_pages_compact_workspace_bytes", _Z, [_S]),
+        ("diffqkv_pages_compact", C.c_int, [_S, _S, _S, _V, _V, _V, _V, _Z, _V, _V])):
+    getattr(_raw, _name).restype = _res
+    getattr(_raw, _name).argtypes = _args
+_pack_cache = struct.Struct("@PP6qPP4i").pack
+_pack_shape = struct.Struct("@8if").pack
+_pack_rope = struct.Struct("@PP2if4x").pack
+_pack_pages = struct.Struct("@PPP4i").pack
 
 
 class DiffQKVError(RuntimeError):
@@ -613,30 +614,7 @@ def diffqkv_decode_topk(q: torch.Tensor, cache: KVCache, n_k: int, n_v: int, sca
 
 # ---- ragged batches over the cache: a step's new rows of sequence b are rows cu_q[b] .. cu_q[b + 1] - 1 of every ragged
 # tensor, cache.seqlens[b] is the number of tokens cached before the step (the caller adds the chunk lengths after it).
-#
-# These calls take a few microseconds on the GPU when the step is small, so their marshalling is kept short: the argument
-# structs are packed into bytes (fields as in the ctypes structures above), and addresses go over as plain integers.
 
-_raw = C.CDLL(LIB_PATH)
-_B, _V, _I, _L = C.c_char_p, C.c_void_p, C.c_int32, C.c_int64
-for _name, _args in (
-        ("diffqkv_extend", [_V, _V, _I, _B, _B, _V, C.c_size_t, _V, _V, _V, _V]),
-        ("diffqkv_rope_append", [_V, _V, _V, _V, _I, _L, _L, _L, _B, _B, _B, _V, _V, _V]),
-        ("diffqkv_pages_free", [_V, _V, _I, _B, _V, _V]),
-        ("diffqkv_pages_fork", [_V, _V, _I, _B, _V, C.c_size_t, _V, _V]),
-        ("diffqkv_pages_reserve", [_V, _B, _B, _B, _V, _V, C.c_size_t, _V, _V]),
-        ("diffqkv_pages_copy", [_V, _V, _I, _B, _B, _B, _V, _V]),
-        ("diffqkv_pages_compact", [_B, _B, _B, _V, _V, _V, _V, C.c_size_t, _V, _V])):
-    getattr(_raw, _name).restype = C.c_int
-    getattr(_raw, _name).argtypes = _args
-for _name, _args in (("diffqkv_extend_workspace_bytes", [_B, _I]), ("diffqkv_pages_fork_workspace_bytes", [_B, _I]),
-                     ("diffqkv_pages_reserve_workspace_bytes", [_B]), ("diffqkv_pages_compact_workspace_bytes", [_B])):
-    getattr(_raw, _name).restype = C.c_size_t
-    getattr(_raw, _name).argtypes = _args
-_pack_cache = struct.Struct("@PP6qPP4i").pack
-_pack_shape = struct.Struct("@8if").pack
-_pack_rope = struct.Struct("@PP2if4x").pack
-_pack_pages = struct.Struct("@PPP4i").pack
 _DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 

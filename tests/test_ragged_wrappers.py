@@ -126,3 +126,12 @@ def test_the_status_word_is_an_int32(api):
         refused(api, lambda: extend(api, dev_status=bad))
         refused(api, lambda: rope(api, dev_status=bad))
         refused(api, lambda: api.diffqkv_pages_free(ints(1), cache(api), ints(6), dev_status=bad, stream=STREAM))
+
+
+def test_packed_structs_are_the_structures(api):
+    """The bytes that the wrappers pack are what the ctypes structures hold."""
+    cache_values = [16, 32, 1 << 40, -2, 3, 4, 5, 6, 48, 64, 7, 8, 9, 10]
+    assert api._pack_cache(*cache_values) == bytes(api.CacheStruct(*cache_values))
+    assert api._pack_shape(1, 2, 3, 4, 5, 6, 1, 0, 0.5) == bytes(api.ShapeStruct(1, 2, 3, 4, 5, 6, 1, 0, 0.5))
+    assert api._pack_rope(16, 32, 64, 1, 1.5) == bytes(api.RopeStruct(16, 32, 64, 1, 1.5))
+    assert api._pack_pages(16, 32, 48, 1, 2, 3, 4) == bytes(api.PagesStruct(16, 32, 48, 1, 2, 3, 4))
