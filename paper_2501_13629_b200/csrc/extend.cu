@@ -318,7 +318,6 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       const int tok0 = w.tok0(p);
       if (w.ta == 0 && w.tb < w.nt) {
         m.rows = m.part_rows = min(w.seq.n - tok0, 2 * p.T) * p.G; m.row_lo = w.seq.lo + tok0; m.head0 = head0;
-        m.member = member;
         m.parts = share_of(w.item_lo + last_tile(w.wide ? kWideCost : kNarrowCost, w.nt, kItemCost), total, n_teams) - team + 1;
       }
       if (!hand_out({w.seq.lo, w.seq.n, w.seq.past, tok0, head0, w.ta, w.tb, w.nst0, vc,

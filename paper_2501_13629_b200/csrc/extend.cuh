@@ -20,7 +20,6 @@ struct ExtendMeta {  // an item that is cut, left by the block that has its firs
   int rows;          // 0: no such item; of the item, and of a head group of it (thin), else all
   int part_rows;
   int row_lo, head0; // first row in q, first head
-  int member;        // place of the block in its team
   int parts;         // the teams from this block's on that have some of its tiles each
 };
 
