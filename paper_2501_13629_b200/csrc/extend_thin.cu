@@ -104,7 +104,11 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if ((ptx::smem_u32(smem) & 1023u) != 0) {  // swizzled tiles start on multiples of 1024 bytes
-    if (tid == 0) report(p.dev_status, DIFFQKV_ERR_ALIGNMENT);
+    if (tid == 0) {
+      report(p.dev_status, DIFFQKV_ERR_ALIGNMENT);
+      p.list.meta[blockIdx.x].rows = 0;
+    }
+    ptx::grid_dependency_wait();
     return;
   }
   if (p.first) ptx::grid_launch_dependents();
