@@ -67,30 +67,42 @@ __device__ __forceinline__ bool ragged_rows(const int* cu_q, const int* seqlens,
   n = hi - lo;
   return true;
 }
-// The sequence that row t belongs to, with its rows, looked for by a block of kThreads threads: the first that fits and has
-// the row between its ends, whatever the order of the others' ends; -1 = none.  With `report_all` the sequences
-// that do not fit are reported (one block of a launch does this).  Holds a barrier.
-template <int kThreads>
-__device__ __forceinline__ int ragged_sequence_of(const int* cu_q, const int* seqlens, int batch, int total_q, int max_seqlen,
-                                                  int t, bool report_all, int* dev_status, int& lo, int& n, int& past) {
-  __shared__ unsigned found_s[kThreads / 32];
-  unsigned found = ~0u;
-  for (int b = threadIdx.x; b < batch; b += kThreads) {
-    const bool between = cu_q[b] <= t && t < cu_q[b + 1];
-    if (!between && !report_all) continue;
-    if (!ragged_rows(cu_q, seqlens, b, total_q, max_seqlen, lo, n, past)) {
-      if (report_all) report(dev_status, DIFFQKV_ERR_INDEX);
-    } else if (between && found == ~0u) {
-      found = b;
-    }
-  }
-  found = __reduce_min_sync(0xffffffffu, found);
-  if ((threadIdx.x & 31) == 0) found_s[threadIdx.x >> 5] = found;
+// The first sequence that fits and has row t between its ends, looked for by the whole block; -1 = none.  With `report_all`
+// those that do not fit are reported.  Not inlined: it is seldom called, and its registers are the caller's otherwise.
+static __device__ __noinline__ int ragged_search(const int* cu_q, const int* seqlens, int batch, int total_q, int max_seqlen,
+                                                 int t, bool report_all, int* dev_status) {
+  __shared__ int found_s;
+  if (threadIdx.x == 0) found_s = batch;
   __syncthreads();
-  for (int w = 0; w < kThreads / 32; ++w) found = min(found, found_s[w]);
-  if (found == ~0u) return -1;
-  ragged_rows(cu_q, seqlens, (int)found, total_q, max_seqlen, lo, n, past);
-  return (int)found;
+  for (int x = threadIdx.x; x < batch; x += blockDim.x) {
+    int lo, n, past;
+    const bool fits = ragged_rows(cu_q, seqlens, x, total_q, max_seqlen, lo, n, past);
+    if (fits && lo <= t && t < lo + n) atomicMin(&found_s, x);
+    if (!fits && report_all) report(dev_status, DIFFQKV_ERR_INDEX);
+  }
+  __syncthreads();
+  return found_s < batch ? found_s : -1;
+}
+// The sequence that row t belongs to, with its rows, for a block of kThreads threads; -1 = none that fits.  With ends in order
+// it is the number of ends at or below the row; only where that one does not have the row are all looked at, and `again` is
+// called (for values of the caller's that then need not be kept meanwhile).  One block of a launch reports the sequences
+// that do not fit (`report_all`).  Holds barriers.
+template <int kThreads, typename F>
+__device__ __forceinline__ int ragged_sequence_of(const int* cu_q, const int* seqlens, int batch, int total_q, int max_seqlen,
+                                                  int t, bool report_all, int* dev_status, int& lo, int& n, int& past,
+                                                  F again) {
+  int b = 0;
+  for (int b0 = 0; b0 < batch; b0 += kThreads) {
+    const int x = b0 + (int)threadIdx.x;
+    b += __syncthreads_count(x < batch && cu_q[x + 1] <= t);
+  }
+  if (b >= batch || report_all || !ragged_rows(cu_q, seqlens, b, total_q, max_seqlen, lo, n, past) || t < lo || t >= lo + n) {
+    b = ragged_search(cu_q, seqlens, batch, total_q, max_seqlen, t, report_all, dev_status);
+    if (b < 0) return -1;
+    ragged_rows(cu_q, seqlens, b, total_q, max_seqlen, lo, n, past);
+    again();
+  }
+  return b;
 }
 
 // Launchers (defined next to their kernels).

@@ -499,7 +499,7 @@ __global__ void __launch_bounds__(kThreads) extend_generic_kernel(DecodeParams p
   const CacheView& c = p.cache;
   int lo, n, past;
   const int b = ragged_sequence_of<kThreads>(cu_q, c.seqlens, p.batch, total_q, c.max_seqlen, t, t == 0 && h == 0,
-                                             p.dev_status, lo, n, past);
+                                             p.dev_status, lo, n, past, [] {});
   if (b < 0) return;
   const long long row = (long long)t * p.n_q + h;
   const T* q = reinterpret_cast<const T*>(p.q) + row * p.d_qk;

@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(256) extend_join_kernel(const SimtParams p) {
   const int t = blockIdx.x, h = blockIdx.y * 8 + (threadIdx.x >> 5);
   int lo, n, past;
   if (ragged_sequence_of<256>(p.cu_q, p.cache.seqlens, p.batch, p.total_q, p.cache.max_seqlen, t, false, p.dev_status, lo, n,
-                              past) < 0 ||
+                              past, [] {}) < 0 ||
       h >= p.n_q)
     return;
   const long long row = (long long)t * p.n_q + h;

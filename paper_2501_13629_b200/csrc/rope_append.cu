@@ -118,15 +118,18 @@ __global__ void __launch_bounds__(kRopeThreads, kPairs ? 6 : 8) rope_append_kern
   // The first vectors are on their way while the row's sequence, place and angles are found (reads that depend on one
   // another): they are rows of the caller's whether or not the step has a use for them.
   uint4 ahead[kAhead][kVec], v_ahead;
+  auto read_ahead = [&] {
 #pragma unroll
-  for (int y = 0; y < kAhead; ++y)
-    if (first + y * heads_at_once < heads) read(first + y * heads_at_once, ahead[y]);
-  if (v_first < v_heads) v_ahead = *reinterpret_cast<const uint4*>(v_row + v_first * p.d_v);
+    for (int y = 0; y < kAhead; ++y)
+      if (first + y * heads_at_once < heads) read(first + y * heads_at_once, ahead[y]);
+    if (v_first < v_heads) v_ahead = *reinterpret_cast<const uint4*>(v_row + v_first * p.d_v);
+  };
+  read_ahead();
 
   // ---- the row's sequence
   int lo, n, past;
   const int b = ragged_sequence_of<kRopeThreads>(p.cu_q, p.cache.seqlens, p.batch, p.total_q, p.cache.max_seqlen, t, t == 0,
-                                                 p.dev_status, lo, n, past);
+                                                 p.dev_status, lo, n, past, read_ahead);
   if (b < 0) return;  // behind the last sequence, or of one that does not fit
   const int tok = past + (t - lo);
   long long blk = b, slot = tok;
