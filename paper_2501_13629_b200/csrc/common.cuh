@@ -67,18 +67,16 @@ __device__ __forceinline__ bool ragged_rows(const int* cu_q, const int* seqlens,
   n = hi - lo;
   return true;
 }
-// The first sequence that fits and has row t between its ends, looked for by the whole block; -1 = none.  With `report_all`
-// those that do not fit are reported.  Not inlined: it is seldom called, and its registers are the caller's otherwise.
+// The first sequence that fits and has row t between its ends, looked for by the whole block; -1 = none.  Not inlined: it is
+// seldom called, and its registers are the caller's otherwise.
 static __device__ __noinline__ int ragged_search(const int* cu_q, const int* seqlens, int batch, int total_q, int max_seqlen,
-                                                 int t, bool report_all, int* dev_status) {
+                                                 int t) {
   __shared__ int found_s;
   if (threadIdx.x == 0) found_s = batch;
   __syncthreads();
   for (int x = threadIdx.x; x < batch; x += blockDim.x) {
     int lo, n, past;
-    const bool fits = ragged_rows(cu_q, seqlens, x, total_q, max_seqlen, lo, n, past);
-    if (fits && lo <= t && t < lo + n) atomicMin(&found_s, x);
-    if (!fits && report_all) report(dev_status, DIFFQKV_ERR_INDEX);
+    if (ragged_rows(cu_q, seqlens, x, total_q, max_seqlen, lo, n, past) && lo <= t && t < lo + n) atomicMin(&found_s, x);
   }
   __syncthreads();
   return found_s < batch ? found_s : -1;
@@ -94,10 +92,12 @@ __device__ __forceinline__ int ragged_sequence_of(const int* cu_q, const int* se
   int b = 0;
   for (int b0 = 0; b0 < batch; b0 += kThreads) {
     const int x = b0 + (int)threadIdx.x;
+    if (report_all && x < batch && !ragged_rows(cu_q, seqlens, x, total_q, max_seqlen, lo, n, past))
+      report(dev_status, DIFFQKV_ERR_INDEX);
     b += __syncthreads_count(x < batch && cu_q[x + 1] <= t);
   }
-  if (b >= batch || report_all || !ragged_rows(cu_q, seqlens, b, total_q, max_seqlen, lo, n, past) || t < lo || t >= lo + n) {
-    b = ragged_search(cu_q, seqlens, batch, total_q, max_seqlen, t, report_all, dev_status);
+  if (b >= batch || !ragged_rows(cu_q, seqlens, b, total_q, max_seqlen, lo, n, past) || t < lo || t >= lo + n) {
+    b = ragged_search(cu_q, seqlens, batch, total_q, max_seqlen, t);
     if (b < 0) return -1;
     ragged_rows(cu_q, seqlens, b, total_q, max_seqlen, lo, n, past);
     again();

@@ -254,3 +254,24 @@ def test_denied_sequences_are_left_out_of_a_captured_step(api):
         ref, _, _, _ = attend64(q[b:b + 1], k[blk, :, :n].transpose(0, 1), v[blk, :, :n].transpose(0, 1), 0.125, n - 1)
         # a weight is off by half a step of bf16 and little besides, the result by another
         assert bool(((out[b:b + 1].double() - ref).abs() <= 3 * 2.0 ** -8 * v[blk, :, :n].double().abs().amax()).all())
+
+
+def test_rope_append_of_many_sequences_one_out_of_order(api):
+    """More sequences than a block has threads; one end far ahead moves the count of ends for every row before it."""
+    n = 600
+    k, v = (torch.zeros((n, 2, 4, 64), dtype=BF16, device="cuda") for _ in range(2))
+    cu = list(range(n + 1))
+    cu[301] = 590  # sequence 300 gets 290 rows and does not fit, 301 ends before it begins, the others have their row
+    lens = [i % 4 for i in range(n)]
+    lens[599] = 4  # full
+    g = torch.Generator("cuda").manual_seed(9)
+    q, k_new, v_new = (torch.randn((n, h, 64), generator=g, device="cuda").to(BF16) for h in (4, 2, 2))
+    out, status = torch.full((n, 4, 64), 5.0, dtype=BF16, device="cuda"), ints([0])
+    api.diffqkv_rope_append(q, k_new, v_new, ints(cu), api.KVCache(k, v, ints(lens), 4), None, q_out=out, dev_status=status)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 1 << api.ERR_INDEX
+    want_k, want_v, want_q = torch.zeros_like(k), torch.zeros_like(v), torch.full_like(out, 5.0)
+    for b in range(n):
+        if b not in (300, 301, 599):
+            want_k[b, :, lens[b]], want_v[b, :, lens[b]], want_q[b] = k_new[b], v_new[b], q[b]
+    assert torch.equal(k, want_k) and torch.equal(v, want_v) and torch.equal(out, want_q)
