@@ -86,7 +86,8 @@ __global__ void __launch_bounds__(256) pages_free_kernel(const int* seq_ids, con
 
 // ------------------------------------------------------------------------------------------------------------- fork
 
-// Whether pair i stands: valid ids, and no earlier pair with a valid parent names the same child.
+// Whether pair i stands: valid ids, and no earlier pair with a valid parent names the same child.  Each pair looks through
+// all before it, 256 at a time: 1024 pairs take 21 us, 4096 27, 32 000 266.
 __device__ __forceinline__ bool fork_stands(const int* parents, const int* children, int i, const diffqkv_pages& g) {
   const int child = children[i], parent = parents[i];
   const bool valid = child >= 0 && child < g.num_seqs && parent >= 0 && parent < g.num_seqs;
@@ -192,8 +193,7 @@ pages_reserve_kernel(const int* cu_q, diffqkv_pages g, int max_seqlen, ReserveWs
   __shared__ int red[33];
   const int rank = blockIdx.x, tid = threadIdx.x, lane = tid & 31;
   const int warp_all = rank * (kScanThreads / 32) + (tid >> 5), warps_all = kClusterBlocks * (kScanThreads / 32);
-  // share of the counts: a multiple of 4 pages per thread row
-  const int share = ((g.num_pages + kClusterBlocks - 1) / kClusterBlocks + 3) & ~3;
+  const int share = (g.num_pages + kClusterBlocks - 1) / kClusterBlocks;  // of the counts
   const int lo = min(rank * share, g.num_pages), hi = min(lo + share, g.num_pages);
 
   // ---- what every sequence asks for, and how many pages are free
@@ -386,7 +386,8 @@ void set_pools(MoveParams* m, const diffqkv_cache& from, const diffqkv_cache& to
   m->map = nullptr; m->table = nullptr; m->table_out = nullptr; m->entries = 0; m->num_pages = 0;
 }
 
-// Behind another kernel of the same call (`dependent`): launched while that one is finishing.
+// Behind another kernel of the same call (`dependent`): its launch is prepared while that one runs, its blocks start when that
+// one has ended (neither search lets them in earlier).
 cudaError_t launch_move(const MoveParams& m, long long most_pages, bool dependent, cudaStream_t stream) {
   long long blocks = most_pages * (m.tasks[0] + m.tasks[1]);
   const long long table_blocks = (m.entries + kCopyThreads * 4 - 1) / (kCopyThreads * 4);
