@@ -360,8 +360,9 @@ diffqkv_status diffqkv_decode_topk_ids(const void *q, const diffqkv_cache *cache
  * two) or a multiple of 128 runs on the tensor cores, chunks of a few rows and long ones on a kernel each; everything else
  * diffqkv_decode accepts runs on fp32 FMAs.  Results do not depend on how sequences are batched beyond rounding (fp32
  * sums in another order, weights rounded to bf16 relative to another reference), and are bitwise reproducible from call
- * to call.  Three launches, whatever the step holds; a step known to have one row for every sequence is faster through
- * diffqkv_decode (whose seqlens count the new token).
+ * to call.  The launches do not depend on what the step holds: three on the tensor cores (two where so many query heads
+ * share both heads that no chunk is short), one or two on FMAs.  A step known to have one row for every sequence is
+ * faster through diffqkv_decode (whose seqlens count the new token).
  * Scores are formed in fp32 in units of log 2, so that one of more than 2.35e38 counts as infinite.  A row whose scores are
  * all -inf has out = 0 and lse = -inf; a NaN or +inf among them makes both NaN.
  * As in any tensor-core attention a weight of zero multiplies the V rows of later tokens of the same chunk; those rows
@@ -429,7 +430,7 @@ diffqkv_status diffqkv_rope_append(const void *q, const void *k_new, const void 
 /*
  * Upkeep of the pages.  A page is a block of both pools (one id for K and V, as in diffqkv_cache).  The state is three
  * device arrays of the caller: the page table, the lengths, and the number of table entries that name each page.
- * Entry -1 means no page; a sequence's pages fill its row from the front.  A page whose count is 0 is free, and free
+ * Entry -1 (or any negative one) means no page; a sequence's pages fill its row from the front.  A page whose count is 0 is free, and free
  * pages are always handed out lowest id first, in the order of the sequences, so every call is deterministic.  Counts
  * may also be raised by the caller (a prefix that is kept pinned).  No call synchronises or tells the host anything:
  * a serving loop can run them inside a captured step.

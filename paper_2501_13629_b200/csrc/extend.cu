@@ -30,13 +30,16 @@
 // frees its tensor memory.
 //
 // Bound by the chain score product -> softmax -> value product of each of the two row tiles, one of which computes while
-// the other's products run.  Chunks of 1.5k-2k rows over 0-6k cached tokens, four sequences, 32/4/8 heads of 128: 430 us,
-// 1065 TFLOP/s of causal work (0.62 of a large matrix product), a pair of row tiles in 3460 cycles: 2200 of softmax, of
-// which 1024 are exponentials at the rate of the special-function unit when both groups are at it, and 1260 from the last
-// weight to the next score, 768 of them products.  The tensor pipe is active 55 % of the time, the special-function unit
-// 55 %.  What did not help: exponentials by polynomial for an eighth to a half of the scores (the registers it takes cost
-// more, 415-850 us), announcing 96 or 112 instead of 64 tokens' weights first (436), waiting for the next K before the
-// last weights (450-470).
+// the other's products run.  Chunks of 1.5k-2k rows over 0-6k cached tokens, four sequences, 32/4/8 heads of 128: 430 us
+// while the SMs run at 1965 MHz, 1065 TFLOP/s of causal work (0.62 of a large matrix product in a burst); calls without a
+// pause run into the power limit and settle at 1730 MHz and 490 us, the same number of cycles.  A pair of row tiles takes
+// 3460 cycles: 2200 of softmax, of which 1024 are exponentials at the rate of the special-function unit when both groups
+// are at it, and 1260 from the last weight to the next score, 768 of them products.  The tensor pipe is active 55 % of the
+// time, the special-function unit 55 %.  What did not help: announcing 96 or 112 instead of 64 tokens' weights first
+// (436 us), waiting for the next K before the last weights (450-470).  Not settled: exponentials by polynomial for a part
+// of the scores.  Earlier forms of this kernel took 415 to 850 us with them for an eighth to a half of the scores.
+// Heads of 64 channels (32/4/16), the same chunks: 396 us without a pause, 580 TFLOP/s; 64-channel keys with 128-channel
+// values 471 us, 730 TFLOP/s (half the products, as many exponentials).
 #include <atomic>
 #include <numeric>
 

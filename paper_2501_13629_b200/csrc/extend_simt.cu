@@ -9,8 +9,9 @@
 // Bound by shared-memory reads next to the FMAs: in the first product 64 FMAs a lane need four K vectors (rows padded by
 // 16 bytes, no conflicts) and four broadcast Q vectors, 20 cycles of shared memory to 16 of FMA.
 // V of a tile is copied (cp.async) while its scores are computed, K of the next tile during the second product.
-// A long cache under few rows is cut into splits along the tokens (the host knows the cache's capacity and the number of
-// rows), joined by a second kernel.  Four sequences of 17-100 rows over up to 1k tokens, 16/2/4 heads of 64, fp32: 41 us and
+// A long cache under few rows is cut into splits along the tokens, joined by a second kernel.  The host knows the cache's
+// capacity and the number of rows, not the lengths: sequences that fill a small part of their capacity leave most of the
+// splits, and of the blocks, without work.  Four sequences of 17-100 rows over up to 1k tokens, 16/2/4 heads of 64, fp32: 41 us and
 // 4 us for the join (0.58 GFLOP, 8 us at the FMAs' rate; 2.2 instructions a cycle and SM); splits half as long 52 us, eight
 // rows to each of four warps 46 us, packed FMAs in the first product no change.
 #include <numeric>

@@ -14,15 +14,17 @@
 // a softmax group, whose tokens meet in one accumulator.  It starts as the score of the segment's first token, which
 // needs no search, and is raised to a tile's maximum when some score exceeds it by 2^24; the warps agree on that
 // through one hardware barrier per tile.  That first score may be any number, or -inf, which counts as the lowest
-// number: a raised column is formed from its scores again, not from distances to a reference far below.  Weights of up to 2^24 are harmless: bf16 and fp32 have the range, the
-// relative precision of either does not depend on the magnitude, and the quotient takes the factor out again.
+// number: a raised column is formed from its scores again, not from distances to a reference far below.  Weights of up
+// to 2^24 are harmless: bf16 and fp32 have the range, the relative precision of either does not depend on the magnitude,
+// and the quotient takes the factor out again.
 //
 // Work: one flat list of (sequence, unit of heads, 128-token tile), divided evenly over one persistent block per SM (or
 // over those that a step's long chunks leave), whose two softmax groups take alternate tiles and are joined at the end of a
 // segment; cut items leave partial rows as in extend.cu.  A unit has up to four head groups that share their K or V head:
-// one head group at a time, 16 sequences of 4k-32k tokens with 2-5 rows, 32/4/8 heads of 128, take 284 us instead of 190.
+// one head group at a time, 16 sequences of 4k-32k tokens with 2-5 rows, 32/4/8 heads of 128, take 284 us instead of 190
+// (187 since the scores' distances are formed in one step).
 //
-// Bound by memory where caches are long: those sequences (983 MB) take 186 us here, 5.3 TB/s (0.82 of a copy), plus the
+// Bound by memory where caches are long: those sequences (983 MB) take 182 us here, 5.4 TB/s (0.84 of a copy), plus the
 // joining kernel; with row tiles as in extend.cu it was 300 us.  Short steps are bound by the chain of a block's start
 // (8 thousand cycles to the first request: lengths, place in the list, page), its first tile (the code of every role comes
 // from the second-level cache once: a warp's first tile takes 4-9 thousand cycles, later ones 2.2) and the joining kernel:
