@@ -7,6 +7,7 @@ module loads the library and raises if it has not been built -- there is no fall
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 import struct
 from dataclasses import dataclass
@@ -797,7 +798,7 @@ def diffqkv_rope_append(q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: t
                      dev_status)
     dtype = k_new.dtype
     assert v_new.dtype == dtype and cache.k.dtype == dtype and cache.v.dtype == dtype
-    n_q, q_stride = n_k * n_v, 0  # without queries any count both head counts divide does
+    n_q, q_stride = math.lcm(n_k, n_v), 0  # without queries any count both head counts divide does
     if q is not None:
         n_q, q_stride = q.shape[1], _row_stride(q, total_q, d_qk)
         assert q.dtype == dtype and q.shape[2] == d_qk
@@ -840,7 +841,7 @@ def _pools_bytes(cache: KVCache, n_k: int, n_v: int) -> Tuple[bytes, bytes]:
     return (_pack_cache(k.data_ptr(), v.data_ptr(), *_pool_strides("cache.k", k, cache.k_strides, nb, n_k, page, 0),
                         *_pool_strides("cache.v", v, cache.v_strides, nb, n_v, page, 0), 0, 0, page, 0, nb,
                         cache.max_seqlen),
-            _pack_shape(1, n_k * n_v, n_k, n_v, k.size(-1), v.size(-1), code, code, 1.0))
+            _pack_shape(1, math.lcm(n_k, n_v), n_k, n_v, k.size(-1), v.size(-1), code, code, 1.0))
 
 
 def diffqkv_pages_free(seq_ids: torch.Tensor, cache: KVCache, ref_counts: torch.Tensor,

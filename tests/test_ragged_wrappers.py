@@ -1,5 +1,6 @@
 """What the Python forms of the ragged-batch calls refuse before the library is called (no GPU: the tensors lie on the host,
 and a call that gets as far as the library is recorded, not made)."""
+import ctypes as C
 import types
 
 import pytest
@@ -135,3 +136,18 @@ def test_packed_structs_are_the_structures(api):
     assert api._pack_shape(1, 2, 3, 4, 5, 6, 1, 0, 0.5) == bytes(api.ShapeStruct(1, 2, 3, 4, 5, 6, 1, 0, 0.5))
     assert api._pack_rope(16, 32, 64, 1, 1.5) == bytes(api.RopeStruct(16, 32, 64, 1, 1.5))
     assert api._pack_pages(16, 32, 48, 1, 2, 3, 4) == bytes(api.PagesStruct(16, 32, 48, 1, 2, 3, 4))
+
+
+def test_pools_of_all_layers_heads(api):
+    """Page calls take pools with the heads of every layer: the number of query heads that the shape needs is the least that
+    both divide, since more than 65535 are refused."""
+    for n_k, n_v, want in ((256, 256, 256), (128, 512, 512), (104, 416, 416), (2, 3, 6)):
+        c = cache(api, k=z(2, n_k, 16, 8), v=z(2, n_v, 16, 8), page_table=ints(2, 3))
+        for call in (lambda: api.diffqkv_pages_reserve(ints(3), c, ints(2), n_k, n_v, stream=STREAM),
+                     lambda: api.diffqkv_pages_copy(ints(2), ints(2), c, n_k, n_v, stream=STREAM),
+                     lambda: api.diffqkv_pages_compact(c, ints(2), n_k, n_v, stream=STREAM),
+                     lambda: api.diffqkv_rope_append(None, z(5, n_k, 8), z(5, n_v, 8), ints(3), c, None, stream=STREAM)):
+            shapes = [api.ShapeStruct.from_buffer_copy(a) for a in made(api, call)
+                      if isinstance(a, bytes) and len(a) == C.sizeof(api.ShapeStruct)]
+            assert (want, n_k, n_v) in [(s.n_q, s.n_k, s.n_v) for s in shapes]
+            assert want <= 65535
