@@ -96,3 +96,41 @@ def test_pages(api, kind):
     torch.cuda.synchronize()
     assert int(live.item()) == n - 2 and table.tolist() == [[1, -1], [0, -1]]
     assert same(0, 3.5, 4.5) and same(1, 3.5, 4.5) and same(2, 0, 0) and int(status.item()) == 0
+
+
+@pytest.mark.parametrize("n,choice", [(130, 0), (2, 0), (2, 2)])
+def test_rows_behind_2_to_31_elements(api, n, choice):
+    """Queries and results of more than 2^31 elements: sequences of n rows, the last ones checked."""
+    n_q, n_k, n_v, d = 128, 8, 8, 128
+    batch = FAR // (n_q * d * n) + 3
+    if batch > 65535:
+        batch, n = 65535, 3
+    rows = batch * n
+    assert rows * n_q * d > FAR
+    g = torch.Generator("cuda").manual_seed(2)
+    k, v = (torch.randn((1, h, 256, d), generator=g, device="cuda").to(BF16) for h in (n_k, n_v))
+    table, cu = torch.zeros((batch, 1), dtype=torch.int32, device="cuda"), ints([i * n for i in range(batch + 1)])
+    lens = torch.full((batch,), 60, dtype=torch.int32, device="cuda")
+    cache, status = api.KVCache(k, v, lens, 256, page_table=table, page_size=256), ints([0])
+    q = torch.zeros((rows, n_q, d), dtype=BF16, device="cuda")
+    q[-2 * n:] = torch.randn((2 * n, n_q, d), generator=g, device="cuda").to(BF16)
+    kept = q[-2 * n:].clone()
+    k_new, v_new = torch.zeros((rows, n_k, d), dtype=BF16, device="cuda"), torch.zeros((rows, n_v, d), dtype=BF16, device="cuda")
+    for i, x in ((0, k_new), (1, v_new)):  # all sequences share the page and write the same
+        x.view(batch, n, 8, d)[:] = torch.randn((n, 8, d), generator=g, device="cuda").to(BF16)
+    api.diffqkv_rope_append(q, k_new, v_new, cu, cache, None, q_out=q, dev_status=status)
+    assert torch.equal(q[-2 * n:], kept)
+    assert torch.equal(k[0, :, 60:60 + n].transpose(0, 1), k_new[-n:]) and torch.equal(v[0, :, 60:60 + n].transpose(0, 1), v_new[-n:])
+    out = torch.zeros((rows, n_q, d), dtype=BF16, device="cuda")
+    lse = torch.zeros((rows, n_q), dtype=F32, device="cuda")
+    api.extend_kernel(choice)
+    try:
+        api.diffqkv_extend(q, cu, cache, n_k, n_v, d ** -0.5, out=out, lse=lse, dev_status=status)
+    finally:
+        api.extend_kernel(0)
+    torch.cuda.synchronize()
+    assert int(status.item()) == 0
+    s = Step.__new__(Step)
+    s.past, s.new, s.total, s.cu_host, s.q, s.d_qk, s.dtype = [60, 60], [n, n], [60 + n, 60 + n], [0, n], kept, d, BF16
+    s.k_tok, s.v_tok = [k[0, :, :60 + n].transpose(0, 1)] * 2, [v[0, :, :60 + n].transpose(0, 1)] * 2
+    check_extend(s, out[-2 * n:], lse[-2 * n:], d ** -0.5)
