@@ -115,3 +115,18 @@ def test_keys_that_are_not_finite(api, dims, dtype, bad):
             check(step, out, lse, 1.0)
         else:
             assert bool(out.isnan().all()) and bool(lse.isnan().all())
+
+
+@pytest.mark.parametrize("seed", range(10))
+@pytest.mark.parametrize("spread", [10.0, 300.0])
+def test_heavy_tails(api, seed, spread):
+    """Tokens' levels drawn from a Cauchy distribution: maxima jump anywhere, by anything, up and not at all."""
+    g = torch.Generator("cuda").manual_seed(seed)
+
+    def level(j):
+        u = torch.rand(j.shape, generator=g, device="cuda", dtype=torch.float64)
+        return (spread * torch.tan(math.pi * (u - 0.5))).clamp(-1e6, 1e4)
+
+    heads = [(32, 4, 8), (16, 8, 2), (12, 2, 6), (16, 1, 1), (32, 4, 16)][seed % 5]
+    dims = [(128, 128), (64, 64), (64, 128)][seed % 3]
+    run(api, made(api, [2000, 40, 300, 5000, 0, 129], [1, 3, 2, 1, 4, 150 if seed % 2 else 2], heads, dims, BF16, level, seed))
