@@ -96,7 +96,8 @@ __device__ __forceinline__ int ragged_sequence_of(const int* cu_q, const int* se
       report(dev_status, DIFFQKV_ERR_INDEX);
     b += __syncthreads_count(x < batch && cu_q[x + 1] <= t);
   }
-  if (b >= batch || !ragged_rows(cu_q, seqlens, b, total_q, max_seqlen, lo, n, past) || t < lo || t >= lo + n) {
+  if (b >= batch) return -1;  // every end is at or below the row
+  if (!ragged_rows(cu_q, seqlens, b, total_q, max_seqlen, lo, n, past) || t < lo || t >= lo + n) {
     b = ragged_search(cu_q, seqlens, batch, total_q, max_seqlen, t);
     if (b < 0) return -1;
     ragged_rows(cu_q, seqlens, b, total_q, max_seqlen, lo, n, past);

@@ -11,10 +11,10 @@
 // per element the fp64 steps and the sincos would cost more than the traffic).  Its threads move 16-byte vectors, for
 // rotate-half pairs the two that hold a channel and its partner; a thread keeps its channels, so that their turns stay in
 // registers, and goes from head to head.  The first vectors are read before the row's sequence is known.
-// 10.9k rows of 32/4/8 heads of 128 channels, 64 of them turned, bf16 (245 MB): 42 us, 5.9 TB/s.  256 threads took 52 us
-// (half the vectors for the same addresses to work out, 3.2 instructions a cycle), without the reads ahead and with a
-// quotient for every vector it was 56 us, with several rows to a block one after the other 60.  16 rows: 3.3 us, of which
-// a launch is most.
+// 10.9k rows of 32/4/8 heads of 128 channels, 64 of them turned, neighbouring pairs, bf16 (245 MB): 41 us, 6.0 TB/s;
+// rotate-half 56 (over all channels 48).  256 threads took 52 us instead of 42 (half the vectors for the same addresses to
+// work out, 3.2 instructions a cycle), without the reads ahead and with a quotient for every vector it was 56 us, with
+// several rows to a block one after the other 60.  16 rows: 3.6 us, of which a launch is most.
 #include <cmath>
 
 #include "common.cuh"
