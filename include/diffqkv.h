@@ -374,6 +374,50 @@ diffqkv_status diffqkv_extend(const void *q, const int32_t *cu_q, int32_t total_
                               int32_t *dev_status, void *stream);
 
 /*
+ * diffqkv_extend_window -- diffqkv_extend for a layer with a sliding window and a few first tokens that stay visible: row i
+ * of sequence b, at position p = past_b + i, sees the tokens j <= p with j > p - window or j < sinks.
+ *   window  >= 1: tokens of the window, the row's own among them       sinks  >= 0: first tokens that every row sees
+ * Everything else, the workspace and its size included, as diffqkv_extend.  Work and traffic go by the tokens seen, not by
+ * the tokens cached.  Pages that hold no token which a row of the step sees are not read: they may have been given back, and
+ * their table entries may be -1.  (Positions go on counting; diffqkv_pages_free gives back ends, not middles, so a caller who
+ * frees pages behind the window lowers their counts and sets their entries itself.)  A weight of zero multiplies the V rows
+ * of tokens that another row of the same chunk sees; those must be finite, all others may hold anything.
+ * A window that reaches back over the whole cache (window + sinks >= max_seqlen) is diffqkv_extend itself.
+ */
+diffqkv_status diffqkv_extend_window(const void *q, const int32_t *cu_q, int32_t total_q, int32_t window, int32_t sinks,
+                                     const diffqkv_cache *cache, const diffqkv_shape *shape, void *workspace,
+                                     size_t workspace_bytes, void *out, float *lse, int32_t *dev_status, void *stream);
+
+/*
+ * diffqkv_extend_shared -- diffqkv_extend for sequences that share their first tokens (samples of one prompt, requests behind
+ * one instruction; diffqkv_pages_fork makes such sequences): the K and V of a shared prefix are read once for the rows of all
+ * sequences of its group and joined with what each sequence has behind it,
+ *     out = (2^a o_prefix + 2^b o_own) / (2^a + 2^b),   a, b the base-2 log-sum-exps of the two parts.
+ * The result is that of diffqkv_extend beyond rounding.  The sequences of a group are neighbours in the batch.
+ */
+typedef struct {
+  const int32_t *cu_seqs; /* [num_groups + 1] device, not decreasing: group g is the sequences cu_seqs[g] .. cu_seqs[g + 1] - 1 */
+  const int32_t *lens;    /* [num_groups] device: tokens that the sequences of group g share, any number from 0 on               */
+  int32_t num_groups;     /* at most 65535; sequences in front of the first group and behind the last share nothing              */
+} diffqkv_prefixes;
+/*
+ *   prefixes   every sequence of a group that has rows in the step has at least lens[g] tokens cached.  The first lens[g]
+ *              tokens are read from the pages (or, without pages, the slab) of the group's FIRST sequence, which may have no
+ *              rows itself; those of the others are taken to be the same.  A sequence whose group does not fit
+ *              it (a prefix longer than its cache or than max_seqlen, or negative, an end of the group outside the batch, rows
+ *              outside the group's) is reported as DIFFQKV_ERR_INDEX and skipped.
+ *   workspace  diffqkv_extend_shared_workspace_bytes(shape, total_q) bytes, 256-byte aligned (it holds both parts of every
+ *              row in fp32)
+ * Everything else as diffqkv_extend.  Four launches on the tensor cores; where diffqkv_extend runs on
+ * FMAs, which bound it and not the cache, every sequence reads all of its own tokens instead.  Two calls that may run at the
+ * same time need a workspace each.
+ */
+size_t diffqkv_extend_shared_workspace_bytes(const diffqkv_shape *shape, int32_t total_q);
+diffqkv_status diffqkv_extend_shared(const void *q, const int32_t *cu_q, int32_t total_q, const diffqkv_prefixes *prefixes,
+                                     const diffqkv_cache *cache, const diffqkv_shape *shape, void *workspace,
+                                     size_t workspace_bytes, void *out, float *lse, int32_t *dev_status, void *stream);
+
+/*
  * Rotary positions.  Channel pairs of the first rot_dim channels of every q and k head are turned by the angle
  * pos * inv_freq[i]; the other channels pass through:
  *     (y_a, y_b) = magnitude * (x_a cos - x_b sin, x_b cos + x_a sin),   pair i = (i, i + rot_dim / 2), or
@@ -426,6 +470,27 @@ diffqkv_status diffqkv_rope_append(const void *q, const void *k_new, const void 
                                    int32_t total_q, int64_t q_stride_tok, int64_t k_stride_tok, int64_t v_stride_tok,
                                    const diffqkv_rope *rope, const diffqkv_cache *cache, const diffqkv_shape *shape,
                                    void *q_out, int32_t *dev_status, void *stream);
+
+/*
+ * diffqkv_norm_rope_append -- diffqkv_rope_append behind a root-mean-square norm of every q and k head, in the same launch:
+ *     x <- x / sqrt(mean_c x_c^2 + eps) * (weight_offset + w_c)      over the d_qk channels of a head
+ * and then the rotation, all in fp32, rounded once.  (Squares are summed in fp32, so channels have to stay below 1e18.)
+ *   q_weight, k_weight   [d_qk], or one for each head ([n_q, d_qk], [n_k, d_qk]) with a head stride of d_qk; NULL = all zero
+ *                        where weight_offset is not 0, all one where it is
+ *   *_head_stride        elements between the weights of two heads: 0 (one for all heads) or a multiple of 16 bytes, >= d_qk
+ * Everything else as diffqkv_rope_append (rot_dim 0 = norm and cache write alone).
+ */
+typedef struct {
+  const void *q_weight, *k_weight;          /* device, 16-byte aligned                                     */
+  int64_t q_head_stride, k_head_stride;
+  diffqkv_dtype weight_dtype;               /* shape.dtype, or DIFFQKV_F32                                 */
+  float eps;                                /* >= 0                                                        */
+  float weight_offset;                      /* 0, or 1 for weights that are stored as their difference to 1 */
+} diffqkv_qk_norm;
+diffqkv_status diffqkv_norm_rope_append(const void *q, const void *k_new, const void *v_new, const int32_t *cu_q,
+                                        int32_t total_q, int64_t q_stride_tok, int64_t k_stride_tok, int64_t v_stride_tok,
+                                        const diffqkv_qk_norm *norm, const diffqkv_rope *rope, const diffqkv_cache *cache,
+                                        const diffqkv_shape *shape, void *q_out, int32_t *dev_status, void *stream);
 
 /*
  * Upkeep of the pages.  A page is a block of both pools (one id for K and V, as in diffqkv_cache).  The state is three

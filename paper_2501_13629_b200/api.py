@@ -40,6 +40,7 @@ EXPORTS = (
     "diffqkv_pages_free", "diffqkv_pages_fork", "diffqkv_pages_fork_workspace_bytes", "diffqkv_pages_reserve",
     "diffqkv_pages_reserve_workspace_bytes", "diffqkv_pages_copy", "diffqkv_pages_compact",
     "diffqkv_pages_compact_workspace_bytes", "diffqkv_debug_extend_kernel", "diffqkv_last_extend_kernel",
+    "diffqkv_extend_window", "diffqkv_extend_shared", "diffqkv_extend_shared_workspace_bytes", "diffqkv_norm_rope_append",
 )
 
 
@@ -65,6 +66,15 @@ class ShapeStruct(C.Structure):
 class RopeStruct(C.Structure):
     _fields_ = [("inv_freq", C.c_void_p), ("positions", C.c_void_p), ("rot_dim", C.c_int32), ("interleaved", C.c_int32),
                 ("magnitude", C.c_float)]
+
+
+class PrefixesStruct(C.Structure):
+    _fields_ = [("cu_seqs", C.c_void_p), ("lens", C.c_void_p), ("num_groups", C.c_int32)]
+
+
+class QkNormStruct(C.Structure):
+    _fields_ = [("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("q_head_stride", C.c_int64),
+                ("k_head_stride", C.c_int64), ("weight_dtype", C.c_int), ("eps", C.c_float), ("weight_offset", C.c_float)]
 
 
 class PagesStruct(C.Structure):
@@ -157,6 +167,10 @@ _S, _V, _I, _L, _Z = C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
 for _name, _res, _args in (
         ("diffqkv_extend_workspace_bytes", _Z, [_S, _I]),
         ("diffqkv_extend", C.c_int, [_V, _V, _I, _S, _S, _V, _Z, _V, _V, _V, _V]),
+        ("diffqkv_extend_window", C.c_int, [_V, _V, _I, _I, _I, _S, _S, _V, _Z, _V, _V, _V, _V]),
+        ("diffqkv_extend_shared_workspace_bytes", _Z, [_S, _I]),
+        ("diffqkv_extend_shared", C.c_int, [_V, _V, _I, _S, _S, _S, _V, _Z, _V, _V, _V, _V]),
+        ("diffqkv_norm_rope_append", C.c_int, [_V, _V, _V, _V, _I, _L, _L, _L, _S, _S, _S, _S, _V, _V, _V]),
         ("diffqkv_rope_frequencies", C.c_int, [_I, C.c_double, C.c_int, C.c_double, C.c_double, C.c_double, C.c_double,
                                                C.POINTER(C.c_double), C.POINTER(C.c_float)]),
         ("diffqkv_rope_append", C.c_int, [_V, _V, _V, _V, _I, _L, _L, _L, _S, _S, _S, _V, _V, _V]),
@@ -174,6 +188,8 @@ _pack_cache = struct.Struct("@PP6qPP4i").pack
 _pack_shape = struct.Struct("@8if").pack
 _pack_rope = struct.Struct("@PP2if4x").pack
 _pack_pages = struct.Struct("@PPP4i").pack
+_pack_prefixes = struct.Struct("@PPi4x").pack
+_pack_norm = struct.Struct("@PP2qi2f4x").pack
 
 
 class DiffQKVError(RuntimeError):
@@ -719,17 +735,14 @@ def diffqkv_extend_workspace_bytes(shape: ShapeStruct, total_q: int) -> int:
     return int(_lib.diffqkv_extend_workspace_bytes(C.byref(shape), int(total_q)))
 
 
-def diffqkv_extend(q: torch.Tensor, cu_q: torch.Tensor, cache: KVCache, n_k: int, n_v: int, scale: float,
-                   workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
-                   lse: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
-                   out_dtype: Optional[torch.dtype] = None, stream: Optional[torch.cuda.Stream] = None):
-    """Causal attention of ragged chunks: q [total_q, n_q, d_qk] against the cache, which holds the chunks' own rows
-    already; returns out [total_q, n_q, d_v].  Rows behind the last chunk stay as they are (a fresh out holds
-    anything there)."""
+def _extend(name: str, middle: tuple, workspace_bytes, q, cu_q, cache: KVCache, n_k, n_v, scale, workspace, out, lse,
+            dev_status, out_dtype, stream, *tensors):
+    """diffqkv_extend and its relatives: ``middle`` is what the entry point ``name`` takes between total_q and the cache,
+    ``tensors`` what of that is on the device."""
     total_q, n_q, d_qk = q.shape
     d_v = cache.v.shape[-1]
     batch = cache.seqlens.shape[0]
-    dev = _device_of(q, cu_q, cache.k, cache.v, cache.seqlens, cache.page_table, out, lse, workspace, dev_status)
+    dev = _device_of(q, cu_q, cache.k, cache.v, cache.seqlens, cache.page_table, out, lse, workspace, dev_status, *tensors)
     dtype = q.dtype
     assert cache.k.dtype == dtype and cache.v.dtype == dtype and q.is_contiguous()
     out_dtype = out_dtype or (dtype if out is None else out.dtype)
@@ -739,12 +752,51 @@ def diffqkv_extend(q: torch.Tensor, cu_q: torch.Tensor, cache: KVCache, n_k: int
     assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.numel() == total_q * n_q)
     shape = _pack_shape(batch, n_q, n_k, n_v, d_qk, d_v, _DTYPES[dtype], _DTYPES[out_dtype], scale)
     if workspace is None:
-        workspace = _workspace(_raw.diffqkv_extend_workspace_bytes(shape, total_q), q.device, stream)
-    _check_status(_raw.diffqkv_extend(q.data_ptr(), _ints(cu_q, batch + 1), total_q,
+        workspace = _workspace(workspace_bytes(shape, total_q), q.device, stream)
+    _check_status(getattr(_raw, name)(q.data_ptr(), _ints(cu_q, batch + 1), total_q, *middle,
                                       _cache_bytes(cache, n_k, n_v, d_qk, d_v), shape, workspace.data_ptr(),
                                       _size(workspace), out.data_ptr(), _addr(lse), _status(dev_status),
-                                      _stream_on(stream, dev)), "diffqkv_extend")
+                                      _stream_on(stream, dev)), name)
     return out
+
+
+def diffqkv_extend(q: torch.Tensor, cu_q: torch.Tensor, cache: KVCache, n_k: int, n_v: int, scale: float,
+                   workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                   lse: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
+                   out_dtype: Optional[torch.dtype] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Causal attention of ragged chunks: q [total_q, n_q, d_qk] against the cache, which holds the chunks' own rows
+    already; returns out [total_q, n_q, d_v].  Rows behind the last chunk stay as they are (a fresh out holds
+    anything there)."""
+    return _extend("diffqkv_extend", (), _raw.diffqkv_extend_workspace_bytes, q, cu_q, cache, n_k, n_v, scale, workspace,
+                   out, lse, dev_status, out_dtype, stream)
+
+
+def diffqkv_extend_window(q: torch.Tensor, cu_q: torch.Tensor, cache: KVCache, n_k: int, n_v: int, scale: float,
+                          window: int, sinks: int = 0, workspace: Optional[torch.Tensor] = None,
+                          out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                          dev_status: Optional[torch.Tensor] = None, out_dtype: Optional[torch.dtype] = None,
+                          stream: Optional[torch.cuda.Stream] = None):
+    """diffqkv_extend in which a row sees the last ``window`` tokens up to its own and the first ``sinks`` ones.  Pages
+    that hold no token which a row sees need not exist (entry -1)."""
+    return _extend("diffqkv_extend_window", (window, sinks), _raw.diffqkv_extend_workspace_bytes, q, cu_q, cache, n_k, n_v,
+                   scale, workspace, out, lse, dev_status, out_dtype, stream)
+
+
+def diffqkv_extend_shared_workspace_bytes(shape: ShapeStruct, total_q: int) -> int:
+    return int(_lib.diffqkv_extend_shared_workspace_bytes(C.byref(shape), int(total_q)))
+
+
+def diffqkv_extend_shared(q: torch.Tensor, cu_q: torch.Tensor, cache: KVCache, cu_groups: torch.Tensor,
+                          prefix_lens: torch.Tensor, n_k: int, n_v: int, scale: float,
+                          workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                          lse: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
+                          out_dtype: Optional[torch.dtype] = None, stream: Optional[torch.cuda.Stream] = None):
+    """diffqkv_extend for a batch in which the sequences cu_groups[g] .. cu_groups[g + 1] - 1 (int32 [groups + 1]) hold the
+    same first prefix_lens[g] tokens (int32 [groups]): these are read once, from the pages of the group's first sequence."""
+    groups = prefix_lens.numel()
+    return _extend("diffqkv_extend_shared", (_pack_prefixes(_ints(cu_groups, groups + 1), _ints(prefix_lens), groups),),
+                   _raw.diffqkv_extend_shared_workspace_bytes, q, cu_q, cache, n_k, n_v, scale, workspace, out, lse,
+                   dev_status, out_dtype, stream, cu_groups, prefix_lens)
 
 
 def extend_kernel(choice: int) -> None:
@@ -791,11 +843,51 @@ def diffqkv_rope_append(q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: t
     """Rotate q [total_q, n_q, d_qk] and k_new [total_q, n_k, d_qk] and write k_new / v_new [total_q, n_v, d_v] to cache
     positions seqlens[b] + i; returns the rotated q (q_out may be q).  ``inv_freq`` float64 [rot_dim / 2], None for no
     rotation; ``positions`` int32 [total_q] replaces the rotation's position seqlens[b] + i."""
+    return _rope_append("diffqkv_rope_append", (), q, k_new, v_new, cu_q, cache, inv_freq, interleaved, magnitude,
+                        positions, q_out, dev_status, stream)
+
+
+def _head_weight(name: str, w: Optional[torch.Tensor], heads: int, d: int, dtype: torch.dtype) -> Tuple[int, int]:
+    """Address and head stride of a norm's weight: [d], or [heads, d]."""
+    if w is None:
+        return 0, 0
+    assert w.dtype == dtype and w.stride(-1) == 1
+    if w.shape == (d,):
+        return w.data_ptr(), 0
+    if w.shape != (heads, d):
+        raise ValueError(f"{name} {tuple(w.shape)} for {heads} heads of {d} channels")
+    if heads > 1 and 0 < w.stride(0) < d:
+        raise ValueError(f"{name} with strides {tuple(w.stride())} for heads of {d} channels")
+    return w.data_ptr(), w.stride(0) if heads > 1 else 0
+
+
+def diffqkv_norm_rope_append(q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: torch.Tensor, cu_q: torch.Tensor,
+                             cache: KVCache, inv_freq: Optional[torch.Tensor], q_weight: Optional[torch.Tensor],
+                             k_weight: Optional[torch.Tensor], eps: float, weight_offset: float = 0.0,
+                             interleaved: bool = False, magnitude: float = 1.0, positions: Optional[torch.Tensor] = None,
+                             q_out: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
+                             stream: Optional[torch.cuda.Stream] = None):
+    """diffqkv_rope_append behind a root-mean-square norm of every q and k head: x / sqrt(mean x^2 + eps) * (weight_offset +
+    weight).  Weights are [d_qk] or one for each head ([n_q, d_qk], [n_k, d_qk]), of q's type or both float32; None =
+    nothing but the norm."""
+    n_k, d_qk = k_new.shape[1:]
+    given = k_weight if k_weight is not None else q_weight
+    dtype = k_new.dtype if given is None else given.dtype
+    kw, k_stride = _head_weight("k_weight", k_weight, n_k, d_qk, dtype)
+    qw, q_stride = _head_weight("q_weight", q_weight, 0 if q is None else q.shape[1], d_qk, dtype)
+    norm = _pack_norm(qw, kw, q_stride, k_stride, _DTYPES[dtype], eps, weight_offset)
+    return _rope_append("diffqkv_norm_rope_append", (norm,), q, k_new, v_new, cu_q, cache, inv_freq, interleaved, magnitude,
+                        positions, q_out, dev_status, stream, q_weight, k_weight)
+
+
+def _rope_append(name: str, middle: tuple, q, k_new, v_new, cu_q, cache: KVCache, inv_freq, interleaved, magnitude, positions,
+                 q_out, dev_status, stream, *tensors):
+    """diffqkv_rope_append and its relative: ``middle`` is what the entry point ``name`` takes in front of the rotation."""
     total_q, n_k, d_qk = k_new.shape
     _, n_v, d_v = v_new.shape
     batch = cache.seqlens.shape[0]
     dev = _device_of(k_new, q, v_new, cu_q, cache.k, cache.v, cache.seqlens, cache.page_table, inv_freq, positions, q_out,
-                     dev_status)
+                     dev_status, *tensors)
     dtype = k_new.dtype
     assert v_new.dtype == dtype and cache.k.dtype == dtype and cache.v.dtype == dtype
     n_q, q_stride = math.lcm(n_k, n_v), 0  # without queries any count both head counts divide does
@@ -811,11 +903,11 @@ def diffqkv_rope_append(q: Optional[torch.Tensor], k_new: torch.Tensor, v_new: t
         freqs, rot = inv_freq.data_ptr(), 2 * inv_freq.numel()
     rope = _pack_rope(freqs, _ints(positions, total_q) or 0, rot, bool(interleaved), magnitude)
     code = _DTYPES[dtype]
-    _check_status(_raw.diffqkv_rope_append(
+    _check_status(getattr(_raw, name)(
         _addr(q), k_new.data_ptr(), v_new.data_ptr(), _ints(cu_q, batch + 1), total_q, q_stride,
-        _row_stride(k_new, total_q, d_qk), _row_stride(v_new, total_q, d_v), rope,
+        _row_stride(k_new, total_q, d_qk), _row_stride(v_new, total_q, d_v), *middle, rope,
         _cache_bytes(cache, n_k, n_v, d_qk, d_v), _pack_shape(batch, n_q, n_k, n_v, d_qk, d_v, code, code, 1.0),
-        _addr(q_out), _status(dev_status), _stream_on(stream, dev)), "diffqkv_rope_append")
+        _addr(q_out), _status(dev_status), _stream_on(stream, dev)), name)
     return q_out
 
 

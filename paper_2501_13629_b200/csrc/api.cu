@@ -451,9 +451,14 @@ size_t diffqkv_extend_workspace_bytes(const diffqkv_shape* shape, int32_t total_
   return extend_workspace_bytes(*shape, total_q);
 }
 
-diffqkv_status diffqkv_extend(const void* q, const int32_t* cu_q, int32_t total_q, const diffqkv_cache* cache,
-                              const diffqkv_shape* shape, void* workspace, size_t workspace_bytes, void* out, float* lse,
-                              int32_t* dev_status, void* stream) {
+static size_t extend_need(const diffqkv_shape& s, int32_t total_q, const ExtendRange* range) {
+  return extend_workspace_bytes(s, total_q) + (range && range->groups > 0 ? extend_groups_workspace_bytes(s, total_q) : 0);
+}
+
+// diffqkv_extend and its ranged forms.
+static diffqkv_status extend_impl(const void* q, const int32_t* cu_q, int32_t total_q, const diffqkv_cache* cache,
+                                  const diffqkv_shape* shape, const ExtendRange* range, void* workspace,
+                                  size_t workspace_bytes, void* out, float* lse, int32_t* dev_status, cudaStream_t stream) {
   diffqkv_status st = check_shape(shape);
   if (st != DIFFQKV_OK) return st;
   if (total_q < 0) return DIFFQKV_ERR_INVALID_ARG;
@@ -462,12 +467,13 @@ diffqkv_status diffqkv_extend(const void* q, const int32_t* cu_q, int32_t total_
   st = check_cache(cache, shape);
   if (st != DIFFQKV_OK) return st;
   if (!aligned16(q) || !aligned16(out)) return DIFFQKV_ERR_ALIGNMENT;
-  if (!workspace || workspace_bytes < extend_workspace_bytes(*shape, total_q)) return DIFFQKV_ERR_WORKSPACE;
+  if (!workspace || workspace_bytes < extend_need(*shape, total_q, range)) return DIFFQKV_ERR_WORKSPACE;
   if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return DIFFQKV_ERR_ALIGNMENT;
-  cudaStream_t st_ = static_cast<cudaStream_t>(stream);
+  // a window that hides no token of the longest sequence
+  if (range && range->groups == 0 && (long long)range->window + range->sinks >= cache->max_seqlen) range = nullptr;
   const int choice = g_extend_choice;
   cudaError_t err = cudaErrorNotSupported;
-  if (choice == 0) err = launch_extend(q, cu_q, total_q, *cache, *shape, workspace, out, lse, dev_status, st_);
+  if (choice == 0) err = launch_extend(q, cu_q, total_q, *cache, *shape, range, workspace, out, lse, dev_status, stream);
   if (err != cudaErrorNotSupported) {
     g_last_extend_kernel = 3;
     return err == cudaSuccess ? DIFFQKV_OK : DIFFQKV_ERR_CUDA;
@@ -481,12 +487,63 @@ diffqkv_status diffqkv_extend(const void* q, const int32_t* cu_q, int32_t total_
   p.chunk = 0; p.splits = 1;
   p.o_partial = nullptr; p.lse_partial = nullptr;
   p.dev_status = dev_status;
-  if (choice != 1) err = launch_extend_simt(p, *shape, cu_q, total_q, workspace, out, lse, st_);
+  if (range && range->groups > 0) {  // FMAs bound these kernels, not the cache: every sequence reads all of its own
+    int* lengths = reinterpret_cast<int*>(static_cast<char*>(workspace) + extend_workspace_bytes(*shape, total_q));
+    if (launch_extend_lengths(cu_q, total_q, *cache, shape->batch, *range, lengths, stream) != cudaSuccess) return DIFFQKV_ERR_CUDA;
+    p.cache.seqlens = lengths;
+    range = nullptr;
+  }
+  if (choice != 1) err = launch_extend_simt(p, *shape, cu_q, total_q, range, workspace, out, lse, stream);
   g_last_extend_kernel = err == cudaErrorNotSupported ? 1 : 2;
   if (err == cudaErrorNotSupported)
-    err = launch_extend_generic(p, shape->dtype, cu_q, total_q, out, shape->out_dtype == DIFFQKV_F32, lse, st_);
+    err = launch_extend_generic(p, shape->dtype, cu_q, total_q, range, out, shape->out_dtype == DIFFQKV_F32, lse, stream);
   if (err == cudaErrorNotSupported) return DIFFQKV_ERR_UNSUPPORTED;
   return err == cudaSuccess ? DIFFQKV_OK : DIFFQKV_ERR_CUDA;
+}
+
+diffqkv_status diffqkv_extend(const void* q, const int32_t* cu_q, int32_t total_q, const diffqkv_cache* cache,
+                              const diffqkv_shape* shape, void* workspace, size_t workspace_bytes, void* out, float* lse,
+                              int32_t* dev_status, void* stream) {
+  return extend_impl(q, cu_q, total_q, cache, shape, nullptr, workspace, workspace_bytes, out, lse, dev_status,
+                     static_cast<cudaStream_t>(stream));
+}
+
+diffqkv_status diffqkv_extend_window(const void* q, const int32_t* cu_q, int32_t total_q, int32_t window, int32_t sinks,
+                                     const diffqkv_cache* cache, const diffqkv_shape* shape, void* workspace,
+                                     size_t workspace_bytes, void* out, float* lse, int32_t* dev_status, void* stream) {
+  if (window < 1 || sinks < 0) return DIFFQKV_ERR_INVALID_ARG;
+  ExtendRange range = {};
+  range.window = window;
+  range.sinks = sinks;
+  return extend_impl(q, cu_q, total_q, cache, shape, &range, workspace, workspace_bytes, out, lse, dev_status,
+                     static_cast<cudaStream_t>(stream));
+}
+
+static diffqkv_status range_of(const diffqkv_prefixes* prefixes, ExtendRange* range) {
+  if (!prefixes || prefixes->num_groups < 0) return DIFFQKV_ERR_INVALID_ARG;
+  if (prefixes->num_groups > 0 && (!prefixes->cu_seqs || !prefixes->lens)) return DIFFQKV_ERR_INVALID_ARG;
+  if (prefixes->num_groups > 65535) return DIFFQKV_ERR_UNSUPPORTED;
+  *range = {};
+  range->window = 0x7fffffff;  // none
+  range->groups = prefixes->num_groups;
+  range->cu_groups = prefixes->cu_seqs;
+  range->prefix_lens = prefixes->lens;
+  return DIFFQKV_OK;
+}
+
+size_t diffqkv_extend_shared_workspace_bytes(const diffqkv_shape* shape, int32_t total_q) {
+  if (check_shape(shape) != DIFFQKV_OK || total_q < 0) return 0;
+  return extend_workspace_bytes(*shape, total_q) + extend_groups_workspace_bytes(*shape, total_q);
+}
+
+diffqkv_status diffqkv_extend_shared(const void* q, const int32_t* cu_q, int32_t total_q, const diffqkv_prefixes* prefixes,
+                                     const diffqkv_cache* cache, const diffqkv_shape* shape, void* workspace,
+                                     size_t workspace_bytes, void* out, float* lse, int32_t* dev_status, void* stream) {
+  ExtendRange range;
+  const diffqkv_status st = range_of(prefixes, &range);
+  if (st != DIFFQKV_OK) return st;
+  return extend_impl(q, cu_q, total_q, cache, shape, range.groups > 0 ? &range : nullptr, workspace, workspace_bytes, out, lse,
+                     dev_status, static_cast<cudaStream_t>(stream));
 }
 
 diffqkv_status diffqkv_rope_frequencies(int32_t rot_dim, double theta, diffqkv_rope_scaling scaling, double factor,
@@ -497,16 +554,12 @@ diffqkv_status diffqkv_rope_frequencies(int32_t rot_dim, double theta, diffqkv_r
              : DIFFQKV_ERR_INVALID_ARG;
 }
 
-diffqkv_status diffqkv_rope_append(const void* q, const void* k_new, const void* v_new, const int32_t* cu_q,
-                                   int32_t total_q, int64_t q_stride_tok, int64_t k_stride_tok, int64_t v_stride_tok,
-                                   const diffqkv_rope* rope, const diffqkv_cache* cache, const diffqkv_shape* shape,
-                                   void* q_out, int32_t* dev_status, void* stream) {
-  diffqkv_status st = check_shape(shape);
-  if (st != DIFFQKV_OK) return st;
-  if (!rope || total_q < 0) return DIFFQKV_ERR_INVALID_ARG;
-  if (shape->batch == 0 || total_q == 0) return DIFFQKV_OK;
+static diffqkv_status check_rope_append(const void* q, const void* k_new, const void* v_new, const int32_t* cu_q,
+                                        int64_t q_stride_tok, int64_t k_stride_tok, int64_t v_stride_tok,
+                                        const diffqkv_rope* rope, const diffqkv_cache* cache, const diffqkv_shape* shape,
+                                        const void* q_out) {
   if (!k_new || !v_new || !cu_q || (q && !q_out)) return DIFFQKV_ERR_INVALID_ARG;
-  st = check_cache(cache, shape);
+  const diffqkv_status st = check_cache(cache, shape);
   if (st != DIFFQKV_OK) return st;
   const int vec = shape->dtype == DIFFQKV_BF16 ? 8 : 4;
   if (rope->rot_dim < 0 || rope->rot_dim > shape->d_qk || (rope->rot_dim > 0 && !rope->inv_freq))
@@ -524,9 +577,47 @@ diffqkv_status diffqkv_rope_append(const void* q, const void* k_new, const void*
     if (strides[i] % vec != 0) return DIFFQKV_ERR_ALIGNMENT;
   }
   if (q && q == q_out && q_stride_tok != 0 && q_stride_tok != widths[0]) return DIFFQKV_ERR_INVALID_ARG;
+  return DIFFQKV_OK;
+}
+
+diffqkv_status diffqkv_rope_append(const void* q, const void* k_new, const void* v_new, const int32_t* cu_q,
+                                   int32_t total_q, int64_t q_stride_tok, int64_t k_stride_tok, int64_t v_stride_tok,
+                                   const diffqkv_rope* rope, const diffqkv_cache* cache, const diffqkv_shape* shape,
+                                   void* q_out, int32_t* dev_status, void* stream) {
+  diffqkv_status st = check_shape(shape);
+  if (st != DIFFQKV_OK) return st;
+  if (!rope || total_q < 0) return DIFFQKV_ERR_INVALID_ARG;
+  if (shape->batch == 0 || total_q == 0) return DIFFQKV_OK;
+  st = check_rope_append(q, k_new, v_new, cu_q, q_stride_tok, k_stride_tok, v_stride_tok, rope, cache, shape, q_out);
+  if (st != DIFFQKV_OK) return st;
   const cudaError_t err = launch_rope_append(q, k_new, v_new, cu_q, total_q, q_stride_tok, k_stride_tok, v_stride_tok,
                                              *rope, view_of(cache), *shape, q_out, dev_status,
                                              static_cast<cudaStream_t>(stream));
+  return err == cudaSuccess ? DIFFQKV_OK : DIFFQKV_ERR_CUDA;
+}
+
+diffqkv_status diffqkv_norm_rope_append(const void* q, const void* k_new, const void* v_new, const int32_t* cu_q,
+                                        int32_t total_q, int64_t q_stride_tok, int64_t k_stride_tok, int64_t v_stride_tok,
+                                        const diffqkv_qk_norm* norm, const diffqkv_rope* rope, const diffqkv_cache* cache,
+                                        const diffqkv_shape* shape, void* q_out, int32_t* dev_status, void* stream) {
+  diffqkv_status st = check_shape(shape);
+  if (st != DIFFQKV_OK) return st;
+  if (!rope || !norm || total_q < 0) return DIFFQKV_ERR_INVALID_ARG;
+  if (norm->weight_dtype != DIFFQKV_BF16 && norm->weight_dtype != DIFFQKV_F32) return DIFFQKV_ERR_INVALID_ARG;
+  if (!(norm->eps >= 0.f) || !(norm->weight_offset == norm->weight_offset)) return DIFFQKV_ERR_INVALID_ARG;
+  if (norm->weight_dtype != shape->dtype && norm->weight_dtype != DIFFQKV_F32) return DIFFQKV_ERR_UNSUPPORTED;
+  if (shape->batch == 0 || total_q == 0) return DIFFQKV_OK;
+  st = check_rope_append(q, k_new, v_new, cu_q, q_stride_tok, k_stride_tok, v_stride_tok, rope, cache, shape, q_out);
+  if (st != DIFFQKV_OK) return st;
+  if (!aligned16(norm->q_weight) || !aligned16(norm->k_weight)) return DIFFQKV_ERR_ALIGNMENT;
+  const int64_t strides[2] = {norm->q_head_stride, norm->k_head_stride};
+  for (int64_t x : strides) {
+    if (x != 0 && x < shape->d_qk) return DIFFQKV_ERR_INVALID_ARG;
+    if (x % (norm->weight_dtype == DIFFQKV_BF16 ? 8 : 4) != 0) return DIFFQKV_ERR_ALIGNMENT;
+  }
+  const cudaError_t err = launch_norm_rope_append(q, k_new, v_new, cu_q, total_q, q_stride_tok, k_stride_tok, v_stride_tok,
+                                                  *norm, *rope, view_of(cache), *shape, q_out, dev_status,
+                                                  static_cast<cudaStream_t>(stream));
   return err == cudaSuccess ? DIFFQKV_OK : DIFFQKV_ERR_CUDA;
 }
 

@@ -192,18 +192,36 @@ cudaError_t launch_rope_append(const void* q, const void* k_new, const void* v_n
                                long long q_st, long long k_st, long long v_st, const diffqkv_rope& rope,
                                const CacheView& cache, const diffqkv_shape& s, void* q_out, int* dev_status,
                                cudaStream_t stream);
+// norm_rope.cu: the same behind a norm of every head.
+cudaError_t launch_norm_rope_append(const void* q, const void* k_new, const void* v_new, const int* cu_q, int total_q,
+                                    long long q_st, long long k_st, long long v_st, const diffqkv_qk_norm& norm,
+                                    const diffqkv_rope& rope, const CacheView& cache, const diffqkv_shape& s, void* q_out,
+                                    int* dev_status, cudaStream_t stream);
 bool rope_frequencies(int rot_dim, double theta, int scaling, double s, double L, double fast, double slow,
                       double* inv_freq, float* magnitude);
 // Chunk attention: tensor cores (extend.cu, extend_thin.cu), tiles on FMAs (extend_simt.cu), one block per (row, query
 // head) on FMAs (decode_generic.cu); each of the first two answers cudaErrorNotSupported where it does not apply.
+// `range` (or null): rows that do not see all tokens before them.
+struct ExtendRange {
+  int window, sinks;  // a row sees tokens before `sinks` and those less than `window` before its own
+  int groups;         // of sequences that share their first tokens; the window does not apply to these
+  const int* cu_groups;
+  const int* prefix_lens;
+};
 size_t extend_workspace_bytes(const diffqkv_shape& s, int total_q);
+size_t extend_groups_workspace_bytes(const diffqkv_shape& s, int total_q);  // on top of that
 cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const diffqkv_cache& c, const diffqkv_shape& s,
-                          void* workspace, void* out, float* lse, int* dev_status, cudaStream_t stream);
+                          const ExtendRange* range, void* workspace, void* out, float* lse, int* dev_status,
+                          cudaStream_t stream);
 size_t extend_simt_workspace_bytes(const diffqkv_shape& s, int total_q);
-cudaError_t launch_extend_simt(const DecodeParams& d, const diffqkv_shape& s, const int* cu_q, int total_q, void* workspace,
-                               void* out, float* lse, cudaStream_t stream);
-cudaError_t launch_extend_generic(const DecodeParams& p, diffqkv_dtype dtype, const int* cu_q, int total_q, void* out,
-                                  int out_is_f32, float* lse, cudaStream_t stream);
+// These two take a window (range->groups = 0); a step with groups goes through them as one without, whose lengths
+// launch_extend_lengths has set to -1 for the sequences that do not fit their group.
+cudaError_t launch_extend_simt(const DecodeParams& d, const diffqkv_shape& s, const int* cu_q, int total_q,
+                               const ExtendRange* range, void* workspace, void* out, float* lse, cudaStream_t stream);
+cudaError_t launch_extend_generic(const DecodeParams& p, diffqkv_dtype dtype, const int* cu_q, int total_q,
+                                  const ExtendRange* range, void* out, int out_is_f32, float* lse, cudaStream_t stream);
+cudaError_t launch_extend_lengths(const int* cu_q, int total_q, const diffqkv_cache& c, int batch, const ExtendRange& range,
+                                  int* seqlens, cudaStream_t stream);
 // Page upkeep (pages.cu).
 cudaError_t launch_pages_free(const int* seq_ids, const int* keep_tokens, int n, const diffqkv_pages& g, int* dev_status,
                               cudaStream_t stream);

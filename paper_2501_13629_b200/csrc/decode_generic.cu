@@ -61,10 +61,10 @@ struct GenericSmem {
 // Attention of query head h of sequence b over cached tokens [t0, t1), t0 < t1: running maximum and sum (base-2
 // domain) and the un-normalised output channels tid, tid + kThreads, ... of this thread.  q_s holds the query times
 // scale * log2(e).  All threads of the block call it.  kKeepNan: a score that is NaN makes the sum NaN even where no other
-// score is a number above -inf (otherwise it counts as -inf there).
-template <typename T, bool kKeepNan = false>
+// score is a number above -inf (otherwise it counts as -inf there).  kGap: tokens from gap_at on are `gap` further on.
+template <typename T, bool kKeepNan = false, bool kGap = false>
 __device__ void attend_range(const DecodeParams& p, int b, int h, int t0, int t1, const float* q_s, GenericSmem& sm,
-                             float& m_run, float& l_run, float (&acc)[kMaxAccPerThread]) {
+                             float& m_run, float& l_run, float (&acc)[kMaxAccPerThread], int gap_at = 0, int gap = 0) {
   const int tid = threadIdx.x;
   const CacheView& c = p.cache;
   const int hk = (int)(((long long)h * p.n_k) / p.n_q);  // Eq. (idx)
@@ -77,10 +77,11 @@ __device__ void attend_range(const DecodeParams& p, int b, int h, int t0, int t1
   for (int i = 0; i < kMaxAccPerThread; ++i) acc[i] = 0.f;
 
   for (int base = t0; base < t1; base += kThreads) {
-    const int j = base + tid;
+    int j = base + tid;
     float sc = -INFINITY;
     long long vrow = -1;
     if (j < t1) {
+      if (kGap && j >= gap_at) j += gap;
       long long blk = b, slot = j;
       bool ok = true;
       if (c.page_table) {
@@ -490,9 +491,9 @@ __global__ void __launch_bounds__(kThreads) prefill_generic_kernel(DecodeParams 
 
 // Attention of ragged chunks, one block per (row, query head).  Rows that belong to no chunk, and chunks that do not fit the
 // cache, are left alone.
-template <typename T>
-__global__ void __launch_bounds__(kThreads) extend_generic_kernel(DecodeParams p, const int* cu_q, int total_q, void* out,
-                                                                 int out_is_f32, float* lse) {
+template <typename T, bool kWindow>
+__global__ void __launch_bounds__(kThreads) extend_generic_kernel(DecodeParams p, const int* cu_q, int total_q, int window,
+                                                                 int sinks, void* out, int out_is_f32, float* lse) {
   extern __shared__ float q_s[];  // [d_qk]
   __shared__ GenericSmem sm;
   const int t = blockIdx.x, h = blockIdx.y, tid = threadIdx.x;
@@ -506,7 +507,13 @@ __global__ void __launch_bounds__(kThreads) extend_generic_kernel(DecodeParams p
   for (int e = tid; e < p.d_qk; e += kThreads) q_s[e] = to_float(q[e]) * p.scale_log2;
   __syncthreads();
   float m_run, l_run, acc[kMaxAccPerThread];
-  attend_range<T, true>(p, b, h, 0, past + (t - lo) + 1, q_s, sm, m_run, l_run, acc);
+  const int end = past + (t - lo) + 1;
+  if constexpr (kWindow) {
+    const int gap = max(end - window - sinks, 0);  // tokens between the first ones and the window
+    attend_range<T, true, true>(p, b, h, 0, end - gap, q_s, sm, m_run, l_run, acc, sinks, gap);
+  } else {
+    attend_range<T, true>(p, b, h, 0, end, q_s, sm, m_run, l_run, acc);
+  }
   const float inv = l_run != 0.f ? 1.f / l_run : 0.f;  // zero: all scores are -inf
 #pragma unroll
   for (int e = 0; e < kMaxAccPerThread; ++e) {
@@ -583,14 +590,15 @@ cudaError_t launch_prefill_generic(const DecodeParams& p, diffqkv_dtype dtype, i
   return cudaGetLastError();
 }
 
-cudaError_t launch_extend_generic(const DecodeParams& p, diffqkv_dtype dtype, const int* cu_q, int total_q, void* out,
-                                  int out_is_f32, float* lse, cudaStream_t stream) {
+cudaError_t launch_extend_generic(const DecodeParams& p, diffqkv_dtype dtype, const int* cu_q, int total_q,
+                                  const ExtendRange* range, void* out, int out_is_f32, float* lse, cudaStream_t stream) {
   const dim3 grid(total_q, p.n_q);
   const size_t smem = sizeof(float) * p.d_qk;
-  if (dtype == DIFFQKV_F32)
-    extend_generic_kernel<float><<<grid, kThreads, smem, stream>>>(p, cu_q, total_q, out, out_is_f32, lse);
-  else
-    extend_generic_kernel<__nv_bfloat16><<<grid, kThreads, smem, stream>>>(p, cu_q, total_q, out, out_is_f32, lse);
+  using Fn = void (*)(DecodeParams, const int*, int, int, int, void*, int, float*);
+  constexpr Fn fns[2][2] = {{extend_generic_kernel<__nv_bfloat16, false>, extend_generic_kernel<__nv_bfloat16, true>},
+                            {extend_generic_kernel<float, false>, extend_generic_kernel<float, true>}};
+  fns[dtype == DIFFQKV_F32][range != nullptr]<<<grid, kThreads, smem, stream>>>(
+      p, cu_q, total_q, range ? range->window : 0, range ? range->sinks : 0, out, out_is_f32, lse);
   count_launch();
   return cudaGetLastError();
 }

@@ -42,6 +42,7 @@
 // values 471 us, 730 TFLOP/s (half the products, as many exponentials).
 #include <atomic>
 #include <numeric>
+#include <type_traits>
 
 #include "attn_math.cuh"
 #include "common.cuh"
@@ -66,14 +67,20 @@ struct Segment {
   int v0;               // V tiles requested before the segment (the ring's position)
   int flags;
 };
+struct RangedSegment : Segment {
+  int end, start;  // the entry's tokens
+  int low, skip;   // first token behind the sinks that some row of the item sees; tiles skipped
+  int dst;
+};
 constexpr int kSegRing = 4;
 constexpr int kSegEnd = 1, kSegWide = 2, kSegWhole = 4, kSegFirst = 8;  // first: holds the item's first tile
 
 // The segments of one block, in order.
+template <bool kRanged>
 struct Walk {
   int b, u, item;
   long long item_lo, end, begin;
-  Seq seq;
+  SeqOf<kRanged> seq;
   // of the current segment
   bool wide;
   int nt, ta, tb, nst0;
@@ -82,7 +89,7 @@ struct Walk {
   __device__ void start(const ExtendParams& p, long long w0, long long w1, int b0, long long lo) {
     begin = w0; end = w1;
     b = b0;
-    if (w0 >= w1) { item_lo = w1; b = p.batch; return; }
+    if (w0 >= w1) { item_lo = w1; b = entries_of<kRanged>(p); return; }
     seq.load(p, b);
     const long long per = seq.cost(p);
     u = (int)quotient(w0 - lo, per);
@@ -96,7 +103,7 @@ struct Walk {
     item_lo = lo + u * per + seq.cost_before(p, item);
   }
   __device__ bool next(const ExtendParams& p) {  // false: no more segments
-    while (b < p.batch && item_lo < end) {
+    while (b < entries_of<kRanged>(p) && item_lo < end) {
       wide = seq.wide(p, item);
       nt = seq.tiles(p, item);
       const int cost = wide ? kWideCost : kNarrowCost;
@@ -104,7 +111,9 @@ struct Walk {
       tb = item_tile(end - item_lo, cost, nt, kItemCost);
       if (ta < tb) {
         if (wide) {
-          const int nt0 = (seq.past + item * 2 * p.T + p.T + kKT - 1) / kKT;  // tiles that the first row tile sees
+          int nt0;  // tiles that the first row tile sees
+          if constexpr (kRanged) nt0 = seq.reach(p, item * 2 * p.T + p.T) - seq.skip(p, item * 2 * p.T);
+          else nt0 = (seq.past + item * 2 * p.T + p.T + kKT - 1) / kKT;
           nst0 = max(0, min(tb, nt0) - ta);
         } else {
           nst0 = (tb - ta + 1) / 2;
@@ -122,7 +131,7 @@ struct Walk {
     if (++u < p.n_units) return;
     u = 0;
     do {
-      if (++b >= p.batch) return;
+      if (++b >= entries_of<kRanged>(p)) return;
       seq.load(p, b);
     } while (seq.n == 0);
   }
@@ -151,7 +160,9 @@ __device__ __forceinline__ void transpose4(uint4 (&v)[4], int lane) {
   swap(v[0], v[2], lane & 2); swap(v[1], v[3], lane & 2);
 }
 
-template <int kDQK, int kD>  // channels per head of Q/K and of V: (128, 128), (64, 64) or (64, 128)
+// kDQK, kD: channels per head of Q/K and of V: (128, 128), (64, 64) or (64, 128).  kRanged: rows do not see all tokens before
+// them; the tiles that no row of an item sees are left out of the list, boxes of pages that none sees are not read.
+template <int kDQK, int kD, bool kRanged>
 __global__ void __launch_bounds__(kExtendThreads, 1)
 extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                    const __grid_constant__ CUtensorMap tmap_v, const ExtendParams p) {
@@ -180,7 +191,8 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   const uint32_t seg_full0 = drain + 8, seg_empty0 = seg_full0 + 8 * kSegRing;
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 + 2 * kKSlots + 2 * kVSlots + 14 + 2 * kSegRing);
   volatile int* abort_flag = reinterpret_cast<int*>(tmem_slot + 1);
-  __shared__ Segment seg_s[kSegRing];
+  using Seg = typename std::conditional<kRanged, RangedSegment, Segment>::type;
+  __shared__ Seg seg_s[kSegRing];
   __shared__ long long scan_s[kExtendThreads / 32], others_s[kExtendThreads / 32];
   __shared__ long long seek_lo_s;
   __shared__ int seek_b_s;
@@ -189,8 +201,10 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   // The kernel for thin sequences works on other rows; whichever of the two comes second may take the SMs that the
   // first one's blocks leave.  The joining kernel depends on the second alone, which therefore ends behind the first.
   if (p.first) ptx::grid_launch_dependents();
-  const int per_thread = (p.batch + kExtendThreads - 1) / kExtendThreads;
-  const int b_lo = min(tid * per_thread, p.batch), b_hi = min(b_lo + per_thread, p.batch);
+  using Seq = SeqOf<kRanged>;
+  const int entries = entries_of<kRanged>(p);
+  const int per_thread = (entries + kExtendThreads - 1) / kExtendThreads;
+  const int b_lo = min(tid * per_thread, entries), b_hi = min(b_lo + per_thread, entries);
   Seq my = {};  // the thread's first sequence: there is seldom another
   if (b_lo < b_hi) my.load(p, b_lo);
   {  // a step of thin sequences alone (decode): nothing to do here
@@ -208,7 +222,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   }
   if (tid == 0) {
     *abort_flag = 0;
-    seek_b_s = p.batch;
+    seek_b_s = entries;
     seek_lo_s = 0;
     ptx::mbar_init(q_full, 1);
     ptx::mbar_init(q_empty, 1);
@@ -301,9 +315,9 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     int kc = 0, vc = 0, segs = 0;  // K tiles, V tiles, Q loads requested so far
     bool ok = true;
     ExtendMeta m = {};
-    Walk w;
+    Walk<kRanged> w;
     w.start(p, w0, w1, seek_b_s, seek_lo_s);
-    auto hand_out = [&](const Segment& d) -> bool {
+    auto hand_out = [&](const Seg& d) -> bool {
       const int s = segs % kSegRing;
       if (!wait_warp(seg_empty0 + 8 * s, ((segs / kSegRing) & 1) ^ 1, abort_flag)) return false;
       if (lane == 0) {
@@ -314,7 +328,13 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       return true;
     };
     for (; ok && w.next(p); w.advance(p), ++segs) {
-      const int kv_len = w.seq.past + w.seq.n;
+      int kv_len = w.seq.past + w.seq.n, tab = w.b, low = 0, skip = 0;
+      if constexpr (kRanged) {
+        kv_len = w.seq.end;
+        tab = w.seq.tab;
+        low = w.seq.low(p, w.tok0(p));
+        skip = w.seq.skip(p, w.tok0(p));
+      }
       const int g = w.u * p.list.team + member;
       const int head0 = g * p.G;
       const int hk = head0 / p.heads_per_k, hv = head0 / p.heads_per_v;  // Eq. (idx)
@@ -322,20 +342,31 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       if (w.ta == 0 && w.tb < w.nt) {
         m.rows = m.part_rows = min(w.seq.n - tok0, 2 * p.T) * p.G; m.row_lo = w.seq.lo + tok0; m.head0 = head0;
         m.parts = share_of(w.item_lo + last_tile(w.wide ? kWideCost : kNarrowCost, w.nt, kItemCost), total, n_teams) - team + 1;
+        if constexpr (kRanged) m.dst = w.seq.dst;
       }
-      if (!hand_out({w.seq.lo, w.seq.n, w.seq.past, tok0, head0, w.ta, w.tb, w.nst0, vc,
-                     (w.wide ? kSegWide : 0) | (w.ta == 0 ? kSegFirst : 0) |
-                         (w.ta == 0 && w.tb == w.nt ? kSegWhole : 0)})) {
+      Seg seg;
+      static_cast<Segment&>(seg) = {w.seq.lo, w.seq.n, w.seq.past, tok0, head0, w.ta, w.tb, w.nst0, vc,
+                                    (w.wide ? kSegWide : 0) | (w.ta == 0 ? kSegFirst : 0) |
+                                        (w.ta == 0 && w.tb == w.nt ? kSegWhole : 0)};
+      if constexpr (kRanged) {
+        seg.end = kv_len; seg.start = w.seq.start; seg.low = low; seg.skip = skip; seg.dst = w.seq.dst;
+      }
+      if (!hand_out(seg)) {
         ok = false;
         break;
       }
+      // first token of tile `tile`, and whether this lane's box of it has a token that is wanted
+      auto token_of = [&](int tile) -> int {
+        return (kRanged && tile >= p.sink_tiles ? tile + skip : tile) * kKT;
+      };
+      auto wanted = [&](int tok) -> bool { return !kRanged || tok < p.sinks || tok + p.box_tok > low; };
       const int per_step = w.wide ? 1 : 2;
       // page of this lane's box of a tile (fetched a step ahead)
       auto fetch = [&](int tile) -> int {
-        if (!p.page_table) return w.b;
-        const int tok = tile * kKT + my_part * p.box_tok;
-        if (tile >= w.tb || lane >= boxes || tok >= kv_len) return 0;
-        return p.page_table[(long long)w.b * p.max_pages_per_seq + tok / p.page_size];
+        if (!p.page_table) return tab;
+        const int tok = token_of(tile) + my_part * p.box_tok;
+        if (tile >= w.tb || lane >= boxes || tok >= kv_len || !wanted(tok)) return 0;
+        return p.page_table[(long long)tab * p.max_pages_per_seq + tok / p.page_size];
       };
       int blk[2];
 #pragma unroll
@@ -346,7 +377,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
           now[x] = blk[x];
-          if (x < count && lane < boxes && tile * kKT + my_part * p.box_tok < kv_len &&
+          if (x < count && lane < boxes && token_of(tile + x) + my_part * p.box_tok < kv_len &&
               (now[x] < 0 || now[x] >= p.num_blocks)) {  // never read outside the pool: flag it, read block 0 instead
             report(p.dev_status, DIFFQKV_ERR_INDEX);
             now[x] = 0;
@@ -357,11 +388,12 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             if (x >= count || !ok) continue;
-            const int tok = (tile + x) * kKT;
-            const int parts_valid = min(parts, (kv_len - tok + p.box_tok - 1) / p.box_tok);
+            const int tok = token_of(tile + x);
+            int parts_valid = min(parts, (kv_len - tok + p.box_tok - 1) / p.box_tok);
             const int first = tok + my_part * p.box_tok;
             const int slot_tok = p.page_table ? first % p.page_size : first;
-            const bool here = lane < boxes && my_part < parts_valid;
+            const bool here = lane < boxes && my_part < parts_valid && wanted(first);
+            if constexpr (kRanged) parts_valid = __popc(__ballot_sync(0xffffffffu, here && my_half == 0));
             if (kv == 0) {
               const int s = kc % kKSlots;
               if (!wait_warp(k_empty0 + 8 * s, ((kc / kKSlots) & 1) ^ 1, abort_flag)) { ok = false; continue; }
@@ -396,7 +428,9 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       }
       if (!ok) break;
     }
-    if (ok) ok = hand_out({0, 0, 0, 0, 0, 0, 0, 0, 0, kSegEnd});
+    Seg last = {};
+    last.flags = kSegEnd;
+    if (ok) ok = hand_out(last);
     if (lane == 0) p.list.meta[blockIdx.x] = m;
     if (!ok) {
       report(p.dev_status, DIFFQKV_ERR_TIMEOUT);
@@ -525,17 +559,27 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     uint32_t joins = 0;  // narrow segments in which both groups had tiles
     bool ok = true;
     // first token of this group's rows within the chunk, and the rows in use
-    auto tok0_of = [&](const Segment& w) { return w.tok0 + ((w.flags & kSegWide) ? t * p.T : 0); };
-    auto rows_of = [&](const Segment& w) { return min(p.T, w.n - tok0_of(w)) * p.G; };
+    auto tok0_of = [&](const Seg& w) { return w.tok0 + ((w.flags & kSegWide) ? t * p.T : 0); };
+    auto rows_of = [&](const Seg& w) { return min(p.T, w.n - tok0_of(w)) * p.G; };
     for (uint32_t segs = 0;; ++segs) {
-      const Segment& w = seg_s[segs % kSegRing];  // released at the end of the segment
+      const Seg& w = seg_s[segs % kSegRing];  // released at the end of the segment
       if (!wait_warp(seg_full0 + 8 * (segs % kSegRing), (segs / kSegRing) & 1, abort_flag)) { ok = false; break; }
       if (w.flags & kSegEnd) break;
       const bool wide = w.flags & kSegWide;
       const int n = t == 0 ? w.nst0 : (wide ? w.tb - w.ta : w.tb - w.ta - w.nst0);  // tiles of this group
       const bool busy = quarter * 32 < rows_of(w);                                 // some row of this warp is in use
       // tiles from here on reach past some row's position (a ragged last tile is one of them)
-      const int j_diag = (w.past + tok0_of(w) + 1) / kKT;
+      int j_diag = (w.past + tok0_of(w) + 1) / kKT;
+      // ranged: first token of tile j; the first token behind the sinks that the last of the group's rows sees
+      auto token_of = [&](int j) -> int {
+        if constexpr (kRanged) return (j >= p.sink_tiles ? j + w.skip : j) * kKT;
+        else return j * kKT;
+      };
+      int low_last = 0;
+      if constexpr (kRanged) {
+        j_diag = min(w.past + tok0_of(w) + 1, w.end) / kKT;
+        low_last = max(w.start, w.past + tok0_of(w) + p.T - p.window);
+      }
       float m_ref = -INFINITY, l = 0.f;
       int j = w.ta + (wide ? 0 : t);
       const int j_end = j + (wide ? n : 2 * n);
@@ -544,12 +588,27 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       for (; j < j_end; j += wide ? 1 : 2, par ^= 1, later = true) {
         if (!wait_warp(gbar, par, abort_flag)) { ok = false; break; }
         tc::fence_after_sync();
-        if (j >= j_diag && j * kKT + kKT > w.past + w.n) {
+        bool clear;
+        if constexpr (kRanged) {
+          const int k0 = token_of(j);
+          clear = k0 + kKT > w.end || (k0 < w.low && k0 + kKT > p.sinks);
+        } else {
+          clear = j >= j_diag && j * kKT + kKT > w.past + w.n;
+        }
+        if (clear) {
           // ragged last tile: V rows past the sequence end hold whatever followed in memory; zero them before any
-          // product reads the tile (0 * NaN would poison it).  Both groups may do this; they write the same zeros.
+          // product reads the tile (0 * NaN would poison it).  Both groups may do this; they write the same zeros.  Ranged:
+          // likewise tokens that no row of the item sees, whose boxes may not have been read.
           const int idx = w.v0 + j - w.ta, vslot = idx % kVSlots;
           if (!wait_warp(v_full0 + 8 * vslot, (idx / kVSlots) & 1, abort_flag)) { ok = false; break; }
-          if (r >= w.past + w.n - j * kKT) {
+          bool zero;
+          if constexpr (kRanged) {
+            const int token = token_of(j) + r;
+            zero = token >= w.end || (token < w.low && token >= p.sinks);
+          } else {
+            zero = r >= w.past + w.n - j * kKT;
+          }
+          if (zero) {
 #pragma unroll
             for (int half = 0; half < kHalves; ++half) {
               uint4* dst = reinterpret_cast<uint4*>(v_s + vslot * kTBytes + half * (kKT * 128) + r * 128);
@@ -582,7 +641,21 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
           __syncwarp();
           if (lane == 0) ptx::mbar_arrive(gbar + kSFree);
         }
-        if (j >= j_diag) {
+        if constexpr (kRanged) {
+          const int k0 = token_of(j);
+          if (k0 / kKT >= j_diag) {
+            const int sees = min(w.past + tok0_of(w) + r / p.G, w.end - 1) - k0;
+#pragma unroll
+            for (int e = 0; e < 128; ++e)
+              if (e > sees) s[e] = 0xff800000u;  // -inf
+          }
+          if (k0 < low_last && k0 + kKT > p.sinks) {
+            const int low = max(w.start, w.past + tok0_of(w) + r / p.G + 1 - p.window) - k0, sinks = p.sinks - k0;
+#pragma unroll
+            for (int e = 0; e < 128; ++e)
+              if (e < low && e >= sinks) s[e] = 0xff800000u;
+          }
+        } else if (j >= j_diag) {
           const int sees = min(w.past + tok0_of(w) + r / p.G, w.past + w.n - 1) - j * kKT;  // last column the row sees
 #pragma unroll
           for (int e = 0; e < 128; ++e)
@@ -708,8 +781,14 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
 #pragma unroll
           for (int y = 0; y < 4; ++y) at[y] = (whole ? out_row(r4 + y) : prow0 + r4 + y) * kD;
           const int rows = rows_of(w);
-          const bool as_f32 = !whole || p.out_is_f32;
+          bool as_f32 = !whole || p.out_is_f32;
           float* dst32 = whole ? reinterpret_cast<float*>(p.out) : p.list.part_o;
+          if constexpr (kRanged) {
+            if (whole && w.dst != kDstOut) {
+              as_f32 = true;
+              dst32 = p.buffer[w.dst - 1].o;
+            }
+          }
           __nv_bfloat16* dst16 = reinterpret_cast<__nv_bfloat16*>(p.out);
 #pragma unroll 1
           for (int x = 0; x < kD / 32; ++x) {
@@ -755,8 +834,13 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
           }
         }
         if (store) {
+          bool done = false;
+          if constexpr (kRanged) {
+            done = whole && w.dst != kDstOut;
+            if (done) p.buffer[w.dst - 1].lse[row] = lse2;
+          }
           if (!whole) p.list.part_lse[prow] = lse2;
-          else if (p.lse) p.lse[row] = lse2 * kLn2;
+          else if (!done && p.lse) p.lse[row] = lse2 * kLn2;
         }
       }
       // the accumulators may be overwritten
@@ -788,7 +872,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
 // each in flight.
 constexpr int kCombineThreads = 256, kCombineBlocks = 3;  // per SM
 
-template <int kD>
+template <int kD, bool kRanged>
 __global__ void __launch_bounds__(kCombineThreads, kCombineBlocks)
 extend_combine_kernel(const ExtendParams p, const ExtendList thin, const int thin_blocks, const int wide_blocks) {
   constexpr int kLanes = kD / 8, kGroups = kCombineThreads / kLanes, kItems = 2 * kMaxBlocks;
@@ -908,8 +992,9 @@ extend_combine_kernel(const ExtendParams p, const ExtendList thin, const int thi
           acc[h][e].z *= inv;
           acc[h][e].w *= inv;
         }
-        if (p.out_is_f32) {
-          float4* dst = reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + row * kD) + lane * 2;
+        const bool to_out = !kRanged || m.dst == kDstOut;
+        if (!to_out || p.out_is_f32) {
+          float4* dst = reinterpret_cast<float4*>((to_out ? reinterpret_cast<float*>(p.out) : p.buffer[m.dst - 1].o) + row * kD) + lane * 2;
           dst[0] = acc[h][0];
           dst[1] = acc[h][1];
         } else {
@@ -917,7 +1002,8 @@ extend_combine_kernel(const ExtendParams p, const ExtendList thin, const int thi
               make_uint4(pack2(acc[h][0].x, acc[h][0].y), pack2(acc[h][0].z, acc[h][0].w), pack2(acc[h][1].x, acc[h][1].y),
                          pack2(acc[h][1].z, acc[h][1].w));
         }
-        if (p.lse && lane == 0) p.lse[row] = sum[h] != 0.f ? (top[h] + log2f(sum[h])) * kLn2 : -INFINITY;
+        float* const lse = to_out ? p.lse : p.buffer[m.dst - 1].lse;
+        if (lse && lane == 0) lse[row] = sum[h] != 0.f ? (top[h] + log2f(sum[h])) * (to_out ? kLn2 : 1.f) : -INFINITY;
         if (++head == p.G) {
           head = 0;
           ++tok;
@@ -929,6 +1015,63 @@ extend_combine_kernel(const ExtendParams p, const ExtendList thin, const int thi
       }
     }
   }
+}
+
+// A row with two entries, its group's prefix and its own tokens: out = sum of the two parts weighted by 2^lse, a block a row.
+// Rows of sequences without a prefix, or that do not fit, are not touched.
+constexpr int kMergeThreads = 256;
+
+template <int kD>
+__global__ void __launch_bounds__(kMergeThreads) extend_merge_kernel(const ExtendParams p) {
+  const int t = blockIdx.x;
+  int lo, n, past;
+  const int b = ragged_sequence_of<kMergeThreads>(p.cu_q, p.seqlens, p.batch, p.total_q, p.max_seqlen, t, false, p.dev_status,
+                                                  lo, n, past, [] {});
+  const int prefix = b < 0 ? 0 : group_prefix(p, b, lo, n, past);
+  ptx::grid_dependency_wait();
+  if (prefix <= 0) return;
+  constexpr int kLanes = kD / 4;
+  const int lane = threadIdx.x % kLanes;
+  for (int h = threadIdx.x / kLanes; h < p.n_q; h += kMergeThreads / kLanes) {
+    const long long row = (long long)t * p.n_q + h;
+    float l[2];
+    float4 o[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      l[i] = p.buffer[i].lse[row];
+      o[i] = reinterpret_cast<const float4*>(p.buffer[i].o + row * kD)[lane];
+    }
+    const float top = fmaxf(l[0], l[1]);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (l[i] == -INFINITY) continue;
+      const float f = ex2(l[i] - top);
+      sum += f;
+      acc.x = fmaf(f, o[i].x, acc.x);
+      acc.y = fmaf(f, o[i].y, acc.y);
+      acc.z = fmaf(f, o[i].z, acc.z);
+      acc.w = fmaf(f, o[i].w, acc.w);
+    }
+    const float inv = sum != 0.f ? 1.f / sum : 0.f;
+    if (p.out_is_f32)
+      reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + row * kD)[lane] =
+          make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    else
+      reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(p.out) + row * kD)[lane] =
+          make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
+    if (p.lse && lane == 0) p.lse[row] = sum != 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
+  }
+}
+
+// Lengths for the kernels that know no groups: -1, which they skip and report, where a sequence does not fit its group.
+__global__ void extend_lengths_kernel(const ExtendParams p, int* seqlens) {
+  const int b = blockIdx.x * blockDim.x + threadIdx.x;
+  if (b >= p.batch) return;
+  int lo, n, past;
+  const bool fits = load_rows(p, b, lo, n, past) && (n == 0 || group_prefix(p, b, lo, n, past) >= 0);
+  seqlens[b] = fits ? past : -1;
 }
 
 // Tensor map over one cache pool: dims (64 channels, token slot, channel half, head, block); a box brings box_tok tokens
@@ -1030,6 +1173,17 @@ size_t place(const Plan& pl, int d_v, char* base, ExtendList* wide, ExtendList* 
   return at;
 }
 
+// Behind them, for a step with groups, the rows' two parts.
+size_t place_buffers(const diffqkv_shape& s, int total_q, char* base, RowBuffer* buffers) {
+  const size_t rows = (size_t)total_q * s.n_q;
+  const size_t lse = up256(rows * sizeof(float)), o = up256(rows * s.d_v * sizeof(float));
+  for (int i = 0; i < 2 && buffers; ++i) {
+    buffers[i].lse = reinterpret_cast<float*>(base + i * (lse + o));
+    buffers[i].o = reinterpret_cast<float*>(base + i * (lse + o) + lse);
+  }
+  return 2 * (lse + o);
+}
+
 bool dims_supported(const diffqkv_shape& s) {
   if (s.dtype != DIFFQKV_BF16 || !(s.scale > 0.f)) return false;
   return (s.d_qk == 128 && s.d_v == 128) || (s.d_qk == 64 && s.d_v == 64) || (s.d_qk == 64 && s.d_v == 128);
@@ -1043,9 +1197,27 @@ size_t extend_workspace_bytes(const diffqkv_shape& s, int total_q) {
   return need > simt ? need : simt;
 }
 
+size_t extend_groups_workspace_bytes(const diffqkv_shape& s, int total_q) {
+  const size_t lengths = up256(sizeof(int) * (size_t)s.batch);  // see launch_extend_lengths
+  const size_t need = dims_supported(s) ? place_buffers(s, total_q, nullptr, nullptr) : 0;
+  return need > lengths ? need : lengths;
+}
+
+cudaError_t launch_extend_lengths(const int* cu_q, int total_q, const diffqkv_cache& c, int batch, const ExtendRange& range,
+                                  int* seqlens, cudaStream_t stream) {
+  ExtendParams p = {};
+  p.cu_q = cu_q; p.seqlens = c.seqlens; p.max_seqlen = c.max_seqlen;
+  p.batch = batch; p.total_q = total_q;
+  p.groups = range.groups; p.cu_groups = range.cu_groups; p.prefix_lens = range.prefix_lens;
+  extend_lengths_kernel<<<(unsigned)((batch + 127) / 128), 128, 0, stream>>>(p, seqlens);
+  count_launch();
+  return cudaGetLastError();
+}
+
 // cudaErrorNotSupported, with nothing launched, where the plain kernel has to take the call.
 cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const diffqkv_cache& c, const diffqkv_shape& s,
-                          void* workspace, void* out, float* lse, int* dev_status, cudaStream_t stream) {
+                          const ExtendRange* range, void* workspace, void* out, float* lse, int* dev_status,
+                          cudaStream_t stream) {
   if (!dims_supported(s) || c.max_seqlen < 1 || c.max_seqlen > 0x7ffffe00 || c.num_blocks < 1) return cudaErrorNotSupported;
   int box_tok = kKT;
   if (c.page_table) {
@@ -1098,6 +1270,13 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
   p.out = out; p.out_is_f32 = s.out_dtype == DIFFQKV_F32; p.lse = lse; p.dev_status = dev_status;
   ExtendList wide, thin;
   place(pl, s.d_v, static_cast<char*>(workspace), &wide, &thin);
+  if (range) {
+    p.window = range->window;
+    p.sinks = range->sinks; p.sink_tiles = (range->sinks + kKT - 1) / kKT;
+    p.groups = range->groups; p.entries = range->groups + s.batch;
+    p.cu_groups = range->cu_groups; p.prefix_lens = range->prefix_lens;
+    if (p.groups > 0) place_buffers(s, total_q, static_cast<char*>(workspace) + extend_workspace_bytes(s, total_q), p.buffer);
+  }
   const int thin_blocks = pl.thin_max > 0 ? pl.blocks : 0, blocks = pl.n_teams * pl.parts;
 
   // Which sequences are thin is known on the device alone, so both kernels are launched; the second may start as soon as
@@ -1105,8 +1284,11 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
   // that has the more work if the rows are spread evenly: behind the other it starts on SMs in another order, away from
   // its team (prompts 447 instead of 434 us), and a step of thin sequences would wait for two launches (198, not 190 us).
   using ExtendFn = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const ExtendParams);
-  const ExtendFn fn = s.d_v == 64 ? extend_attn_kernel<64, 64>
-                                  : (s.d_qk == 128 ? extend_attn_kernel<128, 128> : extend_attn_kernel<64, 128>);
+  const int dims = s.d_v == 64 ? 0 : s.d_qk == 128 ? 1 : 2;
+  constexpr ExtendFn fns[2][3] = {
+      {extend_attn_kernel<64, 64, false>, extend_attn_kernel<128, 128, false>, extend_attn_kernel<64, 128, false>},
+      {extend_attn_kernel<64, 64, true>, extend_attn_kernel<128, 128, true>, extend_attn_kernel<64, 128, true>}};
+  const ExtendFn fn = fns[range != nullptr][dims];
   cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kExtendSmem);
   if (err != cudaSuccess) return err;
   cudaLaunchConfig_t cfg = {};
@@ -1138,7 +1320,7 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
     p.v_rows = make_row_map(&mv_rows, c.v_cache, s.d_v, tok_extent, s.n_v, c.num_blocks, c.v_stride_tok, c.v_stride_head,
                             c.v_stride_blk, box_tok);
     return launch_extend_thin(mq_thin, p.k_rows ? mk_rows : mk, p.v_rows ? mv_rows : mv, p, s.d_qk, s.d_v, thin_blocks,
-                              wide_first, stream);
+                              wide_first, range != nullptr, stream);
   };
   if ((err = wide_first ? launch_wide() : launch_thin()) != cudaSuccess) return err;
   if ((err = wide_first ? launch_thin() : launch_wide()) != cudaSuccess) return err;
@@ -1148,10 +1330,19 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
   cfg.blockDim = dim3(kCombineThreads);
   cfg.dynamicSmemBytes = 0;
   cfg.numAttrs = 1;
-  err = cudaLaunchKernelEx(&cfg, s.d_v == 64 ? extend_combine_kernel<64> : extend_combine_kernel<128>,
-                           p, thin, thin_blocks, blocks);
+  using CombineFn = void (*)(const ExtendParams, const ExtendList, const int, const int);
+  constexpr CombineFn joins[2][2] = {{extend_combine_kernel<64, false>, extend_combine_kernel<128, false>},
+                                     {extend_combine_kernel<64, true>, extend_combine_kernel<128, true>}};
+  err = cudaLaunchKernelEx(&cfg, joins[range != nullptr][s.d_v == 128], p, thin, thin_blocks, blocks);
   if (err != cudaSuccess) return err;
   count_launch();
+  if (p.groups > 0) {
+    cfg.gridDim = dim3((unsigned)total_q);
+    cfg.blockDim = dim3(kMergeThreads);
+    err = cudaLaunchKernelEx(&cfg, s.d_v == 64 ? extend_merge_kernel<64> : extend_merge_kernel<128>, p);
+    if (err != cudaSuccess) return err;
+    count_launch();
+  }
   return cudaGetLastError();
 }
 

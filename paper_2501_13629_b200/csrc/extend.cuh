@@ -1,4 +1,5 @@
-// What the two kernels of diffqkv_extend share (extend.cu: chunks of many rows; extend_thin.cu: a few rows a sequence).
+// What the two kernels of diffqkv_extend share (extend.cu: chunks of many rows; extend_thin.cu: a few rows a sequence), and
+// their ranged forms (diffqkv_extend_window, diffqkv_extend_shared), in which a row does not see all tokens before it.
 #pragma once
 
 #include <cuda.h>
@@ -21,6 +22,16 @@ struct ExtendMeta {  // an item that is cut, left by the block that has its firs
   int part_rows;
   int row_lo, head0; // first row in q, first head
   int parts;         // the teams from this block's on that have some of its tiles each
+  int dst;           // ranged: where its rows go (kDst...)
+};
+
+constexpr int kNoWindow = 0x7fffffff;
+// Where the rows of an entry of a ranged step go: to the result, or, where a row has two entries (the prefix of its group and
+// its own tokens), to a buffer for each, which extend_merge_kernel joins.
+constexpr int kDstOut = 0, kDstPrefix = 1, kDstOwn = 2;
+struct RowBuffer {
+  float* o;    // [total_q n_q][d_v]
+  float* lse;  // [total_q n_q] base 2
 };
 
 // One of the two flat lists of work, and where its cut items go.
@@ -58,6 +69,14 @@ struct ExtendParams {
   float* lse;
   int* dev_status;
   ExtendList list;     // of the kernel that gets these parameters
+  // ranged: row i of a sequence sees, of its tokens from `start` on, those before `sinks` and those less than `window` before
+  // its own position.  The first `groups` entries of the list are the prefixes of groups of sequences, the others, up to
+  // `entries`, the sequences, whose own tokens begin behind their group's prefix.
+  int window, sinks, sink_tiles;
+  int groups, entries;
+  const int* cu_groups;
+  const int* prefix_lens;
+  RowBuffer buffer[2];  // kDstPrefix - 1, kDstOwn - 1
 };
 
 // Rows of sequence b: first row, number, tokens cached before; false when they do not fit.
@@ -153,8 +172,37 @@ __device__ __forceinline__ long long block_scan(long long mine, long long* s, lo
   total = __shfl_sync(0xffffffffu, all, 31);
   return incl - mine + __shfl_sync(0xffffffffu, all - x, warp);
 }
+// The rows of group g and the tokens that its sequences share; false when they do not fit.
+__device__ __forceinline__ bool group_rows(const ExtendParams& p, int g, int& lo, int& hi, int& first, int& prefix) {
+  first = p.cu_groups[g];
+  const int end = p.cu_groups[g + 1];
+  prefix = p.prefix_lens[g];
+  if (first < 0 || end < first || end > p.batch || prefix < 0 || prefix > p.max_seqlen) return false;
+  lo = p.cu_q[first];
+  hi = p.cu_q[end];
+  return lo >= 0 && hi >= lo && hi <= p.total_q && prefix <= 0x7ffffe00 - (hi - lo);  // positions stay within 32 bits
+}
+// Tokens of sequence b, whose rows are lo .. lo + n - 1 behind `past` tokens, that its group has for it (0 outside of all
+// groups); -1 when the group's rows or tokens do not hold those of the sequence.
+__device__ __forceinline__ int group_prefix(const ExtendParams& p, int b, int lo, int n, int past) {
+  int g = 0, z = p.groups;  // the last group that begins at or before b
+  if (z == 0) return 0;
+  while (z - g > 1) {
+    const int mid = (g + z) >> 1;
+    if (p.cu_groups[mid] <= b) g = mid; else z = mid;
+  }
+  if (b < p.cu_groups[g] || b >= p.cu_groups[g + 1]) return 0;
+  int g_lo, g_hi, first, prefix;
+  if (!group_rows(p, g, g_lo, g_hi, first, prefix) || prefix > past || lo < g_lo || lo + n > g_hi) return -1;
+  return prefix;
+}
+
 // One sequence of the step as the list of long chunks has it.
-struct Seq {
+template <bool kRanged>
+struct SeqOf;
+using Seq = SeqOf<false>;
+template <>
+struct SeqOf<false> {
   int lo, n, past, items;  // first row, rows (0: not in this list), tokens cached before, items per head group
   int rows, thin_tiles;    // rows in either list; tiles of one unit of the other list (0: not in that one)
   bool bad;                // does not fit
@@ -185,6 +233,84 @@ struct Seq {
   }
 };
 
+// An entry of a ranged step.  Its K/V tiles are numbered without those that no row of the item sees: tile v of an item is the
+// tile v of the cache in front of `sink_tiles`, and `skip` tiles further on behind them.
+template <>
+struct SeqOf<true> {
+  int lo, n, past, items;
+  int rows, thin_tiles;
+  int end, start;  // its tokens: from start (or the first) on, below end
+  int tab, dst;    // row of the page table, kDst...
+  bool bad;
+  __device__ void load(const ExtendParams& p, int x) {
+    start = 0;
+    dst = kDstOut;
+    if (x < p.groups) {  // every row of the group sees the whole prefix: as if it were cached before any of them
+      int hi;
+      bad = false;  // of a group that does not fit every sequence with rows says so
+      n = group_rows(p, x, lo, hi, tab, past) && past > 0 ? hi - lo : 0;
+      if (n == 0) past = 0;
+      end = past;
+      dst = kDstPrefix;
+    } else {
+      tab = x - p.groups;
+      bad = !load_rows(p, tab, lo, n, past);
+      if (!bad && n > 0) {
+        start = group_prefix(p, tab, lo, n, past);
+        if (start < 0) {
+          bad = true;
+          n = start = past = 0;
+        }
+        if (start > 0) dst = kDstOwn;
+      }
+      end = past + n;
+    }
+    thin_tiles = items = 0;
+    rows = n;
+    if (n > p.thin_max) {
+      items = (n + 2 * p.T - 1) / (2 * p.T);
+    } else {
+      thin_tiles = n > 0 ? (end + kKT - 1) / kKT - skip(p, 0) : 0;
+      n = 0;
+    }
+  }
+  // first token behind the sinks that the chunk's row `tok` sees
+  __device__ int low(const ExtendParams& p, int tok) const { return max(start, past + tok + 1 - p.window); }
+  // tiles behind the sinks that no row from `tok` on sees
+  __device__ int skip(const ExtendParams& p, int tok) const { return max(low(p, tok) / kKT - p.sink_tiles, 0); }
+  // tiles of the cache up to the last one that rows before `tok` see
+  __device__ int reach(const ExtendParams& p, int tok) const { return (min(past + tok, end) + kKT - 1) / kKT; }
+  // cost of the first i items, i < items
+  __device__ long long cost_before(const ExtendParams& p, int i) const {
+    if (i == 0) return 0;
+    auto sum = [&](int count, int b) -> long long {
+      return p.t_log2 >= 0 ? floor_sum_128(count, p.t_log2 + 1, b) : floor_sum(count, kKT, 2 * p.T, b);
+    };
+    long long tiles = dst == kDstPrefix ? (long long)i * ((end + kKT - 1) / kKT) : sum(i, past + 2 * p.T + kKT - 1);
+    if (p.window == kNoWindow) {
+      tiles -= (long long)i * (start / kKT);
+    } else {  // item x skips max(0, floor((c + 2 T x) / 128)) tiles
+      int c = past + 1 - p.window - p.sink_tiles * kKT, x0 = 0;
+      if (c < 0) {
+        x0 = (2 * p.T - 1 - c) / (2 * p.T);
+        c += (long long)x0 * 2 * p.T;
+      }
+      if (i > x0) tiles -= sum(i - x0, c);
+    }
+    return kWideCost * tiles + (long long)kItemCost * i;
+  }
+  __device__ bool wide(const ExtendParams& p, int i) const { return n - i * 2 * p.T > p.T; }
+  __device__ int tiles(const ExtendParams& p, int i) const {  // K/V tiles of item i
+    return reach(p, min(n, (i + 1) * 2 * p.T)) - skip(p, i * 2 * p.T);
+  }
+  __device__ long long cost(const ExtendParams& p) const {  // of one head group
+    if (n == 0) return 0;
+    return cost_before(p, items - 1) + kItemCost + (wide(p, items - 1) ? kWideCost : kNarrowCost) * (long long)tiles(p, items - 1);
+  }
+};
+template <bool kRanged>
+__device__ __forceinline__ int entries_of(const ExtendParams& p) { return kRanged ? p.entries : p.batch; }
+
 // Teams that the list of long chunks is divided over; the thin sequences have the other SMs, so that neither kernel waits
 // for the other (one thread block of either fits an SM): what a step of both kinds saves is one start, one end and one
 // uneven finish (a chunk of 512 rows next to 15 single ones over 0.5k-4k tokens, 16/2/4 heads: 72 -> 64 us).  The weight
@@ -206,6 +332,6 @@ __device__ __forceinline__ int thin_blocks_left(const ExtendParams& p, int wide_
 }
 constexpr int kExtendThinThreads = 576;
 cudaError_t launch_extend_thin(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const ExtendParams& p,
-                               int d_qk, int d_v, int blocks, bool second, cudaStream_t stream);
+                               int d_qk, int d_v, int blocks, bool second, bool ranged, cudaStream_t stream);
 
 }  // namespace diffqkv

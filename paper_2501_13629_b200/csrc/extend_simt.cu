@@ -32,6 +32,7 @@ struct SimtParams {
   int batch, total_q, n_q, G, T;
   int heads_per_k, heads_per_v;
   float scale_log2;
+  int window, sinks;         // with a window: see ExtendRange
   int splits, split_tokens;  // tokens per split, a multiple of kTok
   void* out;
   int out_is_f32;
@@ -45,12 +46,14 @@ __device__ __forceinline__ bool rows_of(const SimtParams& p, int b, int& lo, int
   return ragged_rows(p.cu_q, p.cache.seqlens, b, p.total_q, p.cache.max_seqlen, lo, n, past);
 }
 
-// Where tokens k0 .. k0 + 127 lie: block and slot of each (block -1: not there), a thread per token.
-__device__ __forceinline__ void place_tile(const SimtParams& p, int2* place, int b, int k0, int end) {
+// Where tokens k0 .. k0 + 127 lie: block and slot of each (block -1: not there), a thread per token.  Tokens that no row of
+// the tile sees are left out: those from `gap_at` on are `gap` further on in the cache.
+__device__ __forceinline__ void place_tile(const SimtParams& p, int2* place, int b, int k0, int end, int gap_at, int gap) {
   if (threadIdx.x >= kTok) return;
-  const int tok = k0 + threadIdx.x;
+  int tok = k0 + threadIdx.x;
   int2 at = make_int2(-1, 0);
   if (tok < end) {
+    if (tok >= gap_at) tok += gap;
     at = make_int2(b, tok);
     if (p.cache.page_table) {
       at.x = p.cache.page_table[(long long)b * p.cache.max_pages_per_seq + tok / p.cache.page_size];
@@ -94,7 +97,7 @@ __device__ __forceinline__ void copy_tile(float* dst, const void* pool, long lon
   }
 }
 
-template <typename T, int DQ, int DV>
+template <typename T, int DQ, int DV, bool kWindow>
 __global__ void __launch_bounds__(kThreads) extend_simt_kernel(const SimtParams p) {
   constexpr int kC = DV / 32;  // channels of V per lane
   extern __shared__ float4 smem4[];
@@ -145,7 +148,12 @@ __global__ void __launch_bounds__(kThreads) extend_simt_kernel(const SimtParams 
   const int tok0 = tile_s * p.T, head0 = blockIdx.y * p.G;
   const int rows = min(p.T, n - tok0) * p.G;
   const int hk = head0 / p.heads_per_k, hv = head0 / p.heads_per_v;  // Eq. (idx)
-  const int last = past + min(n, tok0 + p.T);                        // tokens that the tile's last row sees
+  int last = past + min(n, tok0 + p.T);  // tokens that the tile's last row sees
+  int gap = 0;                           // tokens between the first ones and the window of the tile's first row
+  if constexpr (kWindow) {
+    gap = max(past + tok0 + 1 - p.window - p.sinks, 0);
+    last -= gap;
+  }
   const int t0 = blockIdx.z * p.split_tokens;
   const int t1 = p.splits > 1 ? min(last, t0 + p.split_tokens) : last;
 
@@ -177,7 +185,7 @@ __global__ void __launch_bounds__(kThreads) extend_simt_kernel(const SimtParams 
   const long long k_head = (long long)hk * cv.k_sh, v_head = (long long)hv * cv.v_sh;
   int turn = 0;
   if (t0 < t1) {
-    place_tile(p, place_s[0], b, t0, t1);
+    place_tile(p, place_s[0], b, t0, t1, p.sinks, gap);
     __syncthreads();
     copy_tile<T, DQ>(k_s, cv.k, cv.k_sb, cv.k_st, k_head, place_s[0]);
     ptx::cp_async_commit();
@@ -186,7 +194,7 @@ __global__ void __launch_bounds__(kThreads) extend_simt_kernel(const SimtParams 
   float* p_w = p_s + warp * 4 * kTok;
   for (int k0 = t0; k0 < t1; k0 += kTok, turn ^= 1) {
     copy_tile<T, DV>(v_s, cv.v, cv.v_sb, cv.v_st, v_head, place_s[turn]);
-    if (k0 + kTok < t1) place_tile(p, place_s[turn ^ 1], b, k0 + kTok, t1);
+    if (k0 + kTok < t1) place_tile(p, place_s[turn ^ 1], b, k0 + kTok, t1, p.sinks, gap);
     ptx::cp_async_commit();
     ptx::cp_async_wait<1>();  // K of this tile
     __syncthreads();
@@ -218,8 +226,15 @@ __global__ void __launch_bounds__(kThreads) extend_simt_kernel(const SimtParams 
       float top = -INFINITY;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int tok = k0 + lane + 32 * j;
-        if (tok > pos[i] || tok >= t1) s[i][j] = -INFINITY;
+        int tok = k0 + lane + 32 * j;
+        bool hidden = tok >= t1;
+        if constexpr (kWindow) {
+          if (tok >= p.sinks) {
+            tok += gap;
+            hidden |= tok <= pos[i] - p.window;
+          }
+        }
+        if (hidden || tok > pos[i]) s[i][j] = -INFINITY;
         top = fmaxf(top, s[i][j]);
       }
 #pragma unroll
@@ -369,8 +384,8 @@ size_t extend_simt_workspace_bytes(const diffqkv_shape& s, int total_q) {
   return up256(parts * sizeof(float)) + up256(parts * s.d_v * sizeof(float));
 }
 
-cudaError_t launch_extend_simt(const DecodeParams& d, const diffqkv_shape& s, const int* cu_q, int total_q, void* workspace,
-                               void* out, float* lse, cudaStream_t stream) {
+cudaError_t launch_extend_simt(const DecodeParams& d, const diffqkv_shape& s, const int* cu_q, int total_q,
+                               const ExtendRange* range, void* workspace, void* out, float* lse, cudaStream_t stream) {
   if (!dims_ok(s)) return cudaErrorNotSupported;
   SimtParams p;
   p.q = d.q; p.cache = d.cache; p.cu_q = cu_q;
@@ -378,8 +393,11 @@ cudaError_t launch_extend_simt(const DecodeParams& d, const diffqkv_shape& s, co
   p.G = heads_per_tile(s); p.T = kRows / p.G;
   p.heads_per_k = s.n_q / s.n_k; p.heads_per_v = s.n_q / s.n_v;
   p.scale_log2 = d.scale_log2;
-  p.splits = split_count(s, d.cache.max_seqlen, total_q);
-  p.split_tokens = ((d.cache.max_seqlen + p.splits - 1) / p.splits + kTok - 1) / kTok * kTok;
+  p.window = range ? range->window : 0; p.sinks = range ? range->sinks : 0;
+  long long most = d.cache.max_seqlen;  // tokens that the rows of a tile see
+  if (range && (long long)range->window + range->sinks + p.T - 1 < most) most = (long long)range->window + range->sinks + p.T - 1;
+  p.splits = split_count(s, (int)most, total_q);
+  p.split_tokens = (int)(((most + p.splits - 1) / p.splits + kTok - 1) / kTok * kTok);
   p.out = out; p.out_is_f32 = s.out_dtype == DIFFQKV_F32; p.lse = lse;
   p.part_lse = static_cast<float*>(workspace);
   p.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) +
@@ -389,9 +407,11 @@ cudaError_t launch_extend_simt(const DecodeParams& d, const diffqkv_shape& s, co
   const dim3 grid((unsigned)(tiles < total_q ? tiles : total_q), (unsigned)(s.n_q / p.G), (unsigned)p.splits);
   const size_t smem = sizeof(float) * ((size_t)kRows * s.d_qk + kTok * (s.d_qk + 4) + kTok * (s.d_v + 4) + kRows * kTok);
   void (*fn)(const SimtParams) = nullptr;
-#define DIFFQKV_SIMT_CASE(DQ, DV)     \
-  if (s.d_qk == DQ && s.d_v == DV)    \
-    fn = s.dtype == DIFFQKV_F32 ? extend_simt_kernel<float, DQ, DV> : extend_simt_kernel<__nv_bfloat16, DQ, DV>;
+#define DIFFQKV_SIMT_CASE(DQ, DV)                                                                                   \
+  if (s.d_qk == DQ && s.d_v == DV)                                                                                  \
+    fn = s.dtype == DIFFQKV_F32                                                                                     \
+             ? (range ? extend_simt_kernel<float, DQ, DV, true> : extend_simt_kernel<float, DQ, DV, false>)         \
+             : (range ? extend_simt_kernel<__nv_bfloat16, DQ, DV, true> : extend_simt_kernel<__nv_bfloat16, DQ, DV, false>);
   DIFFQKV_SIMT_CASE(64, 64) DIFFQKV_SIMT_CASE(64, 128) DIFFQKV_SIMT_CASE(128, 64) DIFFQKV_SIMT_CASE(128, 128)
 #undef DIFFQKV_SIMT_CASE
   cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
