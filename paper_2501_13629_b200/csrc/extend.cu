@@ -265,7 +265,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     if (s.bad && blockIdx.x == 0) report(p.dev_status, DIFFQKV_ERR_INDEX);
     if (s.n > 0) mine += p.n_units * s.cost(p);
     if (s.thin_tiles > 0) {
-      others += (long long)p.n_units * (s.thin_tiles + kThinItemCost);
+      others += (long long)p.n_units * (s.thin_tiles + (kRanged ? kFewItemCost : kThinItemCost));
       any_thin = true;
     }
     if (++b < b_hi) s.load(p, b);
@@ -1084,6 +1084,15 @@ bool make_cache_map(CUtensorMap* map, const void* base, int d, long long tok_ext
   return make_tmap_bf16_sw128(map, base, 5, dims, strides, box);
 }
 
+// The same with boxes of whole rows: [channel half][box_tok tokens][64 channels].
+bool make_pool_map(CUtensorMap* map, const void* base, int d, long long tok_extent, int heads, long long blocks,
+                   long long st_tok, long long st_head, long long st_blk, int box_tok) {
+  const cuuint64_t dims[5] = {64, (cuuint64_t)tok_extent, (cuuint64_t)(d / 64), (cuuint64_t)heads, (cuuint64_t)blocks};
+  const cuuint64_t strides[4] = {(cuuint64_t)st_tok * 2, 128, (cuuint64_t)st_head * 2, (cuuint64_t)st_blk * 2};
+  const cuuint32_t box[5] = {64, (cuuint32_t)box_tok, (cuuint32_t)(d / 64), 1, 1};
+  return make_tmap_bf16_sw128(map, base, 5, dims, strides, box);
+}
+
 // The same for a pool whose heads lie behind one another in a block (stride_head = tokens * stride_tok) and whose rows
 // have 128 channels: dims (64 channels, 8 tokens, channel half, group of 8 tokens of any head, block), so that one box
 // brings whole rows, half as many boxes per tile (16-token pages were bound by the rate of boxes: 242 -> 190 us for 16
@@ -1244,6 +1253,12 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
       !make_cache_map(&mv, c.v_cache, s.d_v, tok_extent, s.n_v, c.num_blocks, c.v_stride_tok, c.v_stride_head,
                       c.v_stride_blk, box_tok))
     return cudaErrorNotSupported;
+  CUtensorMap mk_few, mv_few;
+  if (range && (!make_pool_map(&mk_few, c.k_cache, s.d_qk, tok_extent, s.n_k, c.num_blocks, c.k_stride_tok, c.k_stride_head,
+                               c.k_stride_blk, box_tok < kFewT ? box_tok : kFewT) ||
+                !make_pool_map(&mv_few, c.v_cache, s.d_v, tok_extent, s.n_v, c.num_blocks, c.v_stride_tok, c.v_stride_head,
+                               c.v_stride_blk, box_tok < kFewT ? box_tok : kFewT)))
+    return cudaErrorNotSupported;
 
   ExtendParams p = {};
   p.cu_q = cu_q; p.seqlens = c.seqlens; p.page_table = c.page_table;
@@ -1271,8 +1286,11 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
   ExtendList wide, thin;
   place(pl, s.d_v, static_cast<char*>(workspace), &wide, &thin);
   if (range) {
+    p.thin_weight *= 0.5f;  // extend_few.cu's tiles have half the tokens
     p.window = range->window;
-    p.sinks = range->sinks; p.sink_tiles = (range->sinks + kKT - 1) / kKT;
+    p.sinks = range->sinks;
+    p.sink_tiles = (int)(((long long)range->sinks + kKT - 1) / kKT);
+    p.sink_few = (int)(((long long)range->sinks + kFewT - 1) / kFewT);
     p.groups = range->groups; p.entries = range->groups + s.batch;
     p.cu_groups = range->cu_groups; p.prefix_lens = range->prefix_lens;
     if (p.groups > 0) place_buffers(s, total_q, static_cast<char*>(workspace) + extend_workspace_bytes(s, total_q), p.buffer);
@@ -1314,13 +1332,14 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
     CUtensorMap mk_rows, mv_rows;
     p.list = thin;
     p.first = !wide_first;
+    if (range) return launch_extend_few(mk_few, mv_few, q, p, s.d_qk, s.d_v, thin_blocks, wide_first, stream);
     p.head_groups = (int)(tok_extent / 8);
     p.k_rows = make_row_map(&mk_rows, c.k_cache, s.d_qk, tok_extent, s.n_k, c.num_blocks, c.k_stride_tok, c.k_stride_head,
                             c.k_stride_blk, box_tok);
     p.v_rows = make_row_map(&mv_rows, c.v_cache, s.d_v, tok_extent, s.n_v, c.num_blocks, c.v_stride_tok, c.v_stride_head,
                             c.v_stride_blk, box_tok);
     return launch_extend_thin(mq_thin, p.k_rows ? mk_rows : mk, p.v_rows ? mv_rows : mv, p, s.d_qk, s.d_v, thin_blocks,
-                              wide_first, range != nullptr, stream);
+                              wide_first, stream);
   };
   if ((err = wide_first ? launch_wide() : launch_thin()) != cudaSuccess) return err;
   if ((err = wide_first ? launch_thin() : launch_wide()) != cudaSuccess) return err;

@@ -1,5 +1,6 @@
 // What the two kernels of diffqkv_extend share (extend.cu: chunks of many rows; extend_thin.cu: a few rows a sequence), and
-// their ranged forms (diffqkv_extend_window, diffqkv_extend_shared), in which a row does not see all tokens before it.
+// those of its ranged forms (diffqkv_extend_window, diffqkv_extend_shared), in which a row does not see all tokens before it
+// (extend.cu again, and extend_few.cu).
 #pragma once
 
 #include <cuda.h>
@@ -72,7 +73,8 @@ struct ExtendParams {
   // ranged: row i of a sequence sees, of its tokens from `start` on, those before `sinks` and those less than `window` before
   // its own position.  The first `groups` entries of the list are the prefixes of groups of sequences, the others, up to
   // `entries`, the sequences, whose own tokens begin behind their group's prefix.
-  int window, sinks, sink_tiles;
+  int window, sinks, sink_tiles, sink_few;  // the sinks in tiles of this kernel and of extend_few.cu
+  int few_stages;
   int groups, entries;
   const int* cu_groups;
   const int* prefix_lens;
@@ -122,6 +124,8 @@ __device__ __forceinline__ long long last_tile(int cost, int nt, int extra) {
 constexpr int kWideCost = 2, kNarrowCost = 1, kItemCost = 5;
 // Likewise for thin items, in tiles: a block's second item costs it about as much as five more tiles.
 constexpr int kThinItemCost = 5;
+// The ranged steps' few rows go by tiles of 64 tokens; an item costs about two of them more.
+constexpr int kFewT = 64, kFewItemCost = 2;
 
 // sum of floor((a x + b) / m) for x = 0 .. n - 1 with a, b >= 0, m > 0: the Euclid-like recursion on (m, a).  Not inlined:
 // the code that a block runs once at its start is fetched from the second-level cache line by line, which is what it
@@ -270,10 +274,12 @@ struct SeqOf<true> {
     if (n > p.thin_max) {
       items = (n + 2 * p.T - 1) / (2 * p.T);
     } else {
-      thin_tiles = n > 0 ? (end + kKT - 1) / kKT - skip(p, 0) : 0;
+      thin_tiles = n > 0 ? (end + kFewT - 1) / kFewT - skip_few(p) : 0;
       n = 0;
     }
   }
+  // of extend_few.cu's tiles, behind the sinks, those that no row sees
+  __device__ int skip_few(const ExtendParams& p) const { return max(low(p, 0) / kFewT - p.sink_few, 0); }
   // first token behind the sinks that the chunk's row `tok` sees
   __device__ int low(const ExtendParams& p, int tok) const { return max(start, past + tok + 1 - p.window); }
   // tiles behind the sinks that no row from `tok` on sees
@@ -332,6 +338,9 @@ __device__ __forceinline__ int thin_blocks_left(const ExtendParams& p, int wide_
 }
 constexpr int kExtendThinThreads = 576;
 cudaError_t launch_extend_thin(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const ExtendParams& p,
-                               int d_qk, int d_v, int blocks, bool second, bool ranged, cudaStream_t stream);
+                               int d_qk, int d_v, int blocks, bool second, cudaStream_t stream);
+// The K and V boxes bring box_tok (at most 64) tokens, all channels of one head.
+cudaError_t launch_extend_few(const CUtensorMap& mk, const CUtensorMap& mv, const void* q, ExtendParams p, int d_qk, int d_v,
+                              int blocks, bool second, cudaStream_t stream);
 
 }  // namespace diffqkv

@@ -1,0 +1,597 @@
+// Sequences with a few new rows, and prefixes shared by a few rows, of the ranged steps (diffqkv_extend_window,
+// diffqkv_extend_shared): the other half of extend.cu, which has the mathematics and takes the longer chunks.
+//
+// Such steps are short: a window of 4k tokens, the tokens behind a shared prefix.  extend_thin.cu's way, which plain steps
+// take, costs 18 us of starts, first tiles and ends however little there is to do, because every role's straight code is
+// fetched once (about 10 cycles an instruction); 16 sequences with a window of 1k tokens took it 24 us, of which the cache is
+// 4.  So here all warps but one run the same short loop, on warp-level products, which have rate enough: with 64 columns a
+// 64-token tile of three heads takes a third of the time that memory needs for it.
+//
+// Work: one flat list of (entry, unit of heads, 64-token tile), where the tiles that no row sees are left out, divided over
+// one persistent block an SM, or over those that the step's long chunks leave; cut items leave partial rows as in extend.cu.
+// A unit's K and V heads (one of either kind, up to four of the other) pass an SM once for all of its query heads.
+//
+// Per block: warp 8 requests whole tiles by TMA into a ring of stages.  The other eight share a tile's (16 rows of one
+// head group) x (tokens): with up to four such row groups, each has 8, 4 or 2 warps, which take 16 or 32 tokens of a tile
+// each (with 8, every other tile) and are joined through shared memory at the end of a segment.  A warp holds its rows'
+// queries and their accumulator in registers,
+//     S[16 rows x 16 tokens] = Q K^T,   O[16 x d_v] += P V        (P from registers, K and V by ldmatrix)
+// with the running reference of a row raised only when passed by 2^8, as in extend.cu; statistics and sums are fp32, the
+// weights are rounded to bf16 for the second product.  V rows that no row of the sequence sees are cleared first: their
+// boxes may not have been read.
+#include "attn_math.cuh"
+#include "extend.cuh"
+#include "ptx.cuh"
+
+namespace diffqkv {
+namespace {
+
+constexpr int kWarps = 8, kThreads = (kWarps + 1) * 32;
+constexpr int kMaxStages = 8;
+constexpr int kCached = 32;  // entries of a block's share kept in shared memory
+constexpr float kFewThreshold = 8.f;  // log2 domain
+constexpr int kMaxSmem = 232448;
+
+struct FewEntry {
+  int lo, n, past, end, start, tab, dst, nt;
+};
+struct FewSegment {  // as the producer hands it to the other warps, through a ring in shared memory
+  int lo, n, past, end, start;  // see SeqOf
+  int low, skip;                // first token behind the sinks that the first row sees; tiles skipped in front of it
+  int unit, ta, tb, dst, flags;
+};
+constexpr int kSegRing = 4;
+constexpr int kSegEnd = 1, kSegWhole = 2, kSegFirst = 4;
+template <int kD>
+struct Scratch {
+  float4 o[4][kD / 8][32];  // accumulators handed from warp to warp, a register of all lanes behind one another
+  float2 ml[4][16];         // their rows' reference and sum
+  FewEntry entry[kCached];  // from the share's first entry on
+  long long total[2][kWarps + 1];
+  int busy[kWarps + 1], longs[kWarps + 1];
+  uint64_t full[kMaxStages], empty[kMaxStages], seg_full[kSegRing], seg_empty[kSegRing];
+  FewSegment seg[kSegRing];
+  long long seek_lo;
+  int seek_e;
+  int abort;
+};
+
+template <int kDQK, int kD>
+__global__ void __launch_bounds__(kThreads, 1)
+extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
+                  const __nv_bfloat16* __restrict__ q, const ExtendParams p) {
+  constexpr int HK = kDQK / 64, HV = kD / 64;
+  constexpr int kKBytes = kFewT * kDQK * 2, kVBytes = kFewT * kD * 2;
+  constexpr int kItem = kFewItemCost;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  const uint32_t stage_bytes = p.k_parts * kKBytes + p.v_parts * kVBytes;
+  Scratch<kD>& sc = *reinterpret_cast<Scratch<kD>*>(smem + p.few_stages * stage_bytes);
+  const uint32_t ring = ptx::smem_u32(smem), full0 = ptx::smem_u32(sc.full), empty0 = ptx::smem_u32(sc.empty);
+  const uint32_t seg_full0 = ptx::smem_u32(sc.seg_full), seg_empty0 = ptx::smem_u32(sc.seg_empty);
+  volatile int* abort_flag = &sc.abort;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  if ((ring & 1023u) != 0) {  // swizzled tiles start on multiples of 1024 bytes
+    if (tid == 0) {
+      report(p.dev_status, DIFFQKV_ERR_ALIGNMENT);
+      p.list.meta[blockIdx.x].rows = 0;
+    }
+    ptx::grid_dependency_wait();
+    return;
+  }
+  if (p.first) ptx::grid_launch_dependents();
+  using Seq = SeqOf<true>;
+  // ---- this block's share of the list: every thread sums up the tiles of its entries
+  const int per_thread = (p.entries + kThreads - 1) / kThreads;
+  const int e_lo = min(tid * per_thread, p.entries), e_hi = min(e_lo + per_thread, p.entries);
+  Seq my = {};  // the thread's first entry: there is seldom another
+  long long mine = 0, others = 0;  // others: the list of long chunks
+  bool any_long = false;
+  {
+    Seq s;
+    for (int e = e_lo; e < e_hi; ++e) {
+      s.load(p, e);
+      if (e == e_lo) my = s;
+      if (s.thin_tiles > 0) mine += (long long)p.n_units * (s.thin_tiles + kItem);
+      if (s.n > 0) {
+        others += p.n_units * s.cost(p);
+        any_long = true;
+      }
+    }
+  }
+  if (tid < kMaxStages + kSegRing) {  // full and empty, of the stages and behind them of the segments
+    const bool seg = tid >= kMaxStages;
+    ptx::mbar_init(seg ? seg_full0 + 8 * (tid - kMaxStages) : full0 + 8 * tid, 1);
+    ptx::mbar_init(seg ? seg_empty0 + 8 * (tid - kMaxStages) : empty0 + 8 * tid, kWarps);
+    ptx::fence_barrier_init();
+  }
+  if (tid == 0) {
+    sc.abort = 0;
+    ptx::prefetch_tmap(&tmap_k);
+    ptx::prefetch_tmap(&tmap_v);
+  }
+  auto scan = [&](long long x, int which) -> long long {  // inclusive over the warp; the warp's sum to shared memory
+#pragma unroll 1
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, x, o);
+      if (lane >= o) x += y;
+    }
+    if (lane == 31) sc.total[which][warp] = x;
+    return x;
+  };
+  auto before_warp = [&](int which, long long& all) -> long long {
+    long long before = 0;
+    all = 0;
+#pragma unroll 1
+    for (int w = 0; w <= kWarps; ++w) {
+      if (w < warp) before += sc.total[which][w];
+      all += sc.total[which][w];
+    }
+    return before;
+  };
+  long long before = scan(mine, 0) - mine, total;
+  {
+    const int busy = __popc(__ballot_sync(0xffffffffu, mine > 0)), longs = __any_sync(0xffffffffu, any_long);
+    if (lane == 0) {
+      sc.busy[warp] = busy;
+      sc.longs[warp] = longs;
+    }
+  }
+  __syncthreads();
+  before += before_warp(0, total);
+  int busy = 0, longs = 0;
+#pragma unroll 1
+  for (int w = 0; w <= kWarps; ++w) {
+    busy += sc.busy[w];
+    longs |= sc.longs[w];
+  }
+  int grid = p.blocks;
+  if (longs) {
+    scan(others, 1);
+    __syncthreads();
+    before_warp(1, others);
+    __syncthreads();
+    grid = thin_blocks_left(p, wide_teams(p, others, total));  // what the other kernel leaves
+  }
+  // Equal shares of the list, cut wherever they end; or, where that costs no block more than six tiles, equal chunks that
+  // begin with their item (see extend_thin.cu), so that every block has one segment at most.
+  int chunk = 0;
+  const int items = per_thread == 1 ? min(busy * p.n_units, grid) : grid;
+  if (items < grid && total < (1ll << 22)) {
+    const uint32_t tiles = (uint32_t)total - items * kItem;
+    chunk = (int)((tiles + grid - items - 1) / (grid - items));
+    if (chunk > (int)(tiles / grid) + 6) chunk = 0;
+  }
+  int blocks = 0;  // that take part
+  long long w0 = total, w1 = total;
+  if (total > 0 && (int)blockIdx.x < grid) {
+    if (chunk > 0) {
+      long long chunks;
+      mine = (long long)p.n_units * ((my.thin_tiles + chunk - 1) / chunk);
+      before = scan(mine, 1) - mine;
+      __syncthreads();
+      before += before_warp(1, chunks);
+      w0 = blockIdx.x;
+      w1 = w0 < chunks ? w0 + 1 : w0;
+    } else {
+      blocks = shares(total, grid, kItem + 1);
+      if ((int)blockIdx.x < blocks) {
+        w0 = share_start(total, blockIdx.x, blocks);
+        w1 = share_start(total, blockIdx.x + 1, blocks);
+      }
+    }
+  }
+  if (w0 >= w1) {  // nothing to do: a step of long chunks, or fewer tiles than blocks
+    if (tid == 0) p.list.meta[blockIdx.x].rows = 0;
+    ptx::grid_dependency_wait();
+    return;
+  }
+  auto pack = [](const Seq& s) -> FewEntry { return {s.lo, s.rows, s.past, s.end, s.start, s.tab, s.dst, s.thin_tiles}; };
+  if (before <= w0 && w0 < before + mine) {
+    Seq s = my;
+    for (int e = e_lo;;) {
+      const int nt = s.thin_tiles;
+      const long long c = nt == 0 ? 0 : (long long)p.n_units * (chunk > 0 ? (nt + chunk - 1) / chunk : nt + kItem);
+      if (w0 < before + c) {
+        sc.seek_e = e;
+        sc.seek_lo = before;
+        sc.entry[0] = pack(s);
+        break;
+      }
+      before += c;
+      s.load(p, ++e);
+    }
+  }
+  __syncthreads();
+  if (chunk == 0) {
+    const int e0 = sc.seek_e;
+    for (int e = max(e_lo, e0 + 1); e < min(e_hi, e0 + kCached); ++e) {
+      if (e != e_lo) my.load(p, e);
+      sc.entry[e - e0] = pack(my);
+    }
+    __syncthreads();
+  }
+
+  const int bt_shift = 31 - __clz(p.box_tok);
+  int stage = 0;
+  uint32_t phase = 0;
+  auto step = [&]() {
+    if (++stage == p.few_stages) {
+      stage = 0;
+      phase ^= 1;
+    }
+  };
+
+  if (warp == kWarps) {
+    // ------------------------------------------------------------------ TMA producer
+    // Lane: token part of a tile, then head; a box brings all channels of a part.
+    const int parts = kFewT >> bt_shift, my_part = lane & (parts - 1), my_head = lane / parts, together = 32 / parts;
+    const int heads = p.k_parts + p.v_parts;
+    const uint32_t part_bytes = p.box_tok * 128u;
+    int count = 0, segs = 0;
+    bool ok = true;
+    ExtendMeta m = {};
+    int e = sc.seek_e, u, chunk_lo = 0;
+    FewEntry x = sc.entry[0];
+    long long item_lo = sc.seek_lo;
+    if (chunk > 0) {
+      const int per = (x.nt + chunk - 1) / chunk, in = (int)(w0 - item_lo);
+      u = (int)((uint32_t)in / (uint32_t)per);
+      chunk_lo = (in - u * per) * chunk;
+    } else {
+      u = (int)quotient(w0 - item_lo, x.nt + kItem);
+      item_lo += (long long)u * (x.nt + kItem);
+    }
+    auto next_item = [&]() {
+      item_lo += x.nt + kItem;
+      if (++u < p.n_units) return;
+      u = 0;
+      do {
+        if (++e >= p.entries) return;
+        const int at = e - sc.seek_e;
+        if (at < kCached) {
+          x = sc.entry[at];
+        } else {
+          Seq s;
+          s.load(p, e);
+          x = pack(s);
+        }
+      } while (x.nt == 0);
+    };
+    auto hand_out = [&](const FewSegment& d, volatile int* abort) -> bool {
+      const int at = segs % kSegRing;
+      if (!wait_warp(seg_empty0 + 8 * at, ((segs / kSegRing) & 1) ^ 1, abort)) return false;
+      if (lane == 0) {
+        sc.seg[at] = d;
+        ptx::mbar_arrive(seg_full0 + 8 * at);  // releases the stores above
+      }
+      __syncwarp();
+      ++segs;
+      return true;
+    };
+    while (ok && e < p.entries && item_lo < w1) {
+      int ta, tb;
+      if (chunk > 0) {
+        ta = chunk_lo;
+        tb = min(x.nt, chunk_lo + chunk);
+      } else {
+        ta = item_tile(w0 - item_lo, 1, x.nt, kItem);
+        tb = item_tile(w1 - item_lo, 1, x.nt, kItem);
+        if (ta >= tb) {  // the share begins, or ends, within the item's own cost
+          next_item();
+          continue;
+        }
+      }
+      const int low = max(x.start, x.past + 1 - p.window), skip = max(low / kFewT - p.sink_few, 0);
+      const int head0 = u * p.parts * p.G, hk0 = head0 / p.heads_per_k, hv0 = head0 / p.heads_per_v;  // Eq. (idx)
+      if (!hand_out({x.lo, x.n, x.past, x.end, x.start, low, skip, u, ta, tb, x.dst,
+                     (ta == 0 ? kSegFirst : 0) | (ta == 0 && tb == x.nt ? kSegWhole : 0)}, abort_flag)) {
+        ok = false;
+        break;
+      }
+      if (ta == 0 && tb < x.nt) {
+        m.rows = p.parts * x.n * p.G; m.part_rows = x.n * p.G; m.row_lo = x.lo; m.head0 = head0; m.dst = x.dst;
+        m.parts = chunk > 0 ? (x.nt + chunk - 1) / chunk
+                            : share_of(item_lo + last_tile(1, x.nt, kItem), total, blocks) - (int)blockIdx.x + 1;
+      }
+      auto token_of = [&](int tile) -> int { return ((tile >= p.sink_few ? tile + skip : tile) << 6) + my_part * p.box_tok; };
+      auto wanted = [&](int tok) -> bool { return tok < x.end && (tok < p.sinks || tok + p.box_tok > low); };
+      auto fetch = [&](int tile) -> int {  // page of this lane's box
+        if (!p.page_table) return x.tab;
+        const int tok = token_of(tile);
+        if (tile >= tb || !wanted(tok)) return 0;
+        return p.page_table[(long long)x.tab * p.max_pages_per_seq + tok / p.page_size];
+      };
+      int page = fetch(ta);
+      for (int tile = ta; tile < tb; ++tile) {
+        const int page_next = fetch(tile + 1);
+        const int tok = token_of(tile);
+        const bool reads = wanted(tok);
+        if (reads && (page < 0 || page >= p.num_blocks)) {  // never read outside the pool: flag it, block 0 instead
+          report(p.dev_status, DIFFQKV_ERR_INDEX);
+          page = 0;
+        }
+        const int slot = p.page_table ? tok % p.page_size : tok;
+        const int valid = __popc(__ballot_sync(0xffffffffu, reads && my_head == 0));
+        if (!wait_warp(empty0 + 8 * stage, phase ^ 1, abort_flag)) { ok = false; break; }
+        const uint32_t bar = full0 + 8 * stage;
+        if (lane == 0) ptx::mbar_arrive_expect_tx(bar, valid * part_bytes * (p.k_parts * HK + p.v_parts * HV));
+        __syncwarp();
+        if (reads) {
+          const uint32_t dst = ring + stage * stage_bytes;
+          for (int h = my_head; h < heads; h += together) {
+            const int v = h - p.k_parts;
+            if (v < 0) ptx::tma_load_5d(dst + h * kKBytes + my_part * (part_bytes * HK), &tmap_k, bar, 0, slot, 0, hk0 + h, page);
+            else ptx::tma_load_5d(dst + p.k_parts * kKBytes + v * kVBytes + my_part * (part_bytes * HV), &tmap_v, bar, 0, slot, 0, hv0 + v, page);
+          }
+        }
+        page = page_next;
+        ++count;
+        step();
+      }
+      if (!ok || chunk > 0) break;
+      next_item();
+    }
+    FewSegment end = {};
+    end.flags = kSegEnd;
+    if (!hand_out(end, nullptr)) ok = false;  // in any case: the other warps leave together
+    if (lane == 0) p.list.meta[blockIdx.x] = m;
+    if (!ok) {
+      report(p.dev_status, DIFFQKV_ERR_TIMEOUT);
+      // give copies in flight a bounded chance to land before the block's shared memory is released
+      for (int s = 0; s < min(count, p.few_stages); ++s)
+        ptx::mbar_wait(full0 + 8 * s, (uint32_t)((count - s + p.few_stages - 1) / p.few_stages - 1) & 1u, nullptr);
+    }
+  } else {
+    // ------------------------------------------------------------------ products and softmax
+    const int g8 = lane >> 2, t4 = lane & 3;  // row and column pair of the fragments
+    const int bt_mask = p.box_tok - 1;
+    bool dead = false;  // a wait for tiles ran out: go on without waiting, so that all warps meet at the barriers below
+    for (uint32_t segs = 0;; ++segs) {
+      const FewSegment& w = sc.seg[segs % kSegRing];  // released at the end of the segment
+      // the producer hands an end out even where it gives up, long before this limit, so that all warps take the same way
+      if (!__all_sync(0xffffffffu, ptx::mbar_wait(seg_full0 + 8 * (segs % kSegRing), (segs / kSegRing) & 1, nullptr,
+                                                  8 * ptx::kWaitLimitNs))) {
+        dead = true;
+        break;
+      }
+      if (w.flags & kSegEnd) break;
+      const int used = w.n * p.G;                                            // rows of a head group
+      const int blocks16 = (used + 15) >> 4, all16 = p.parts * blocks16;     // at most 4
+      const int mshift = all16 > 2 ? 2 : all16 - 1, slices = kWarps >> mshift;
+      const int mt = warp & ((1 << mshift) - 1), slice = warp >> mshift;
+      const int group = mt / blocks16, r0 = (mt - group * blocks16) << 4;
+      const bool active = mt < all16;
+      // ---- the warp's rows r0 + g8 and r0 + g8 + 8 of the head group: queries, the tokens that they see
+      auto out_row = [&](int r) -> long long {
+        const int tok = r / p.G;
+        return (long long)(w.lo + tok) * p.n_q + (w.unit * p.parts + group) * p.G + (r - tok * p.G);
+      };
+      uint32_t qf[kDQK / 16][4];
+      int last[2], first[2];  // up to last, from first on (and the sinks)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int r = r0 + g8 + 8 * y, tok = r / p.G;
+        const bool here = active && r < used;
+        last[y] = min(w.past + tok, w.end - 1);
+        first[y] = max(w.start, w.past + tok + 1 - p.window);
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(q + (here ? out_row(r) : 0) * kDQK) + t4;
+#pragma unroll
+        for (int ks = 0; ks < kDQK / 16; ++ks) {
+          qf[ks][y] = here ? src[ks * 8] : 0u;
+          qf[ks][y + 2] = here ? src[ks * 8 + 4] : 0u;
+        }
+      }
+      float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+      float acc[kD / 8][4];
+#pragma unroll
+      for (int c = 0; c < kD / 8; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[c][e] = 0.f;
+      const uint32_t k_off = (p.k_parts > 1 ? group : 0) * kKBytes;
+      const uint32_t v_off = p.k_parts * kKBytes + (p.v_parts > 1 ? group : 0) * kVBytes;
+      const int low = w.low, end = w.end, tb = w.tb;
+      // The slices of a row group: two take the halves of a tile each, four or eight every second or fourth tile.
+      const int r = (slice & 1) * 32, turn = slice >> 1, turns = (slices >> 1) - 1;
+#pragma unroll 1
+      for (int i = w.ta; i < tb; ++i) {
+        if (!dead && !wait_warp(full0 + 8 * stage, phase, abort_flag)) dead = true;
+        const int t0 = ((i >= p.sink_few ? i + w.skip : i) << 6) + r;  // first of the warp's 32 tokens
+        const uint32_t base = ring + stage * stage_bytes;
+        const bool edge = t0 + 32 > end || (t0 < low && t0 + 32 > p.sinks);  // some are seen by no row
+        if (active && !dead && ((i - w.ta) & turns) == turn && t0 < end && (t0 + 32 > low || t0 < p.sinks)) {
+          // ---- scores
+          float s[4][4];
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[e >> 2][e & 3] = 0.f;
+          {
+            const int row = r + (lane & 7) + 8 * (lane >> 4), half = (lane >> 3) & 1;
+            // 16 tokens further on: another box, or further down in the same one
+            const uint32_t at = base + k_off + ((((row >> bt_shift) * HK << bt_shift) + (row & bt_mask)) << 7);
+            const uint32_t at2 = base + k_off + (((((row + 16) >> bt_shift) * HK << bt_shift) + ((row + 16) & bt_mask)) << 7);
+#pragma unroll
+            for (int ks = 0; ks < kDQK / 16; ++ks) {
+              const uint32_t off = (((uint32_t)(ks / 4) << bt_shift) << 7) + ((((ks % 4) * 2 + half) ^ (row & 7)) << 4);
+              uint32_t b[4], d[4];
+              ptx::ldmatrix_x4(at + off, b);
+              ptx::ldmatrix_x4(at2 + off, d);
+              ptx::mma_bf16_16816(s[0], qf[ks], b[0], b[1]);
+              ptx::mma_bf16_16816(s[1], qf[ks], b[2], b[3]);
+              ptx::mma_bf16_16816(s[2], qf[ks], d[0], d[1]);
+              ptx::mma_bf16_16816(s[3], qf[ks], d[2], d[3]);
+            }
+          }
+          if (t0 + 31 > min(last[0], last[1]) || (t0 < max(first[0], first[1]) && t0 + 32 > p.sinks)) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int tok = t0 + (e >> 2) * 8 + 2 * t4 + (e & 1), y = (e >> 1) & 1;
+              if (tok > last[y] || (tok < first[y] && tok >= p.sinks)) s[e >> 2][e & 3] = -INFINITY;
+            }
+          }
+          // ---- softmax over the 32 tokens: four lanes a row
+          float alpha[2];
+          bool raise = false;
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            float mx = fmaxf(s[0][2 * y], s[0][2 * y + 1]);
+#pragma unroll
+            for (int h = 1; h < 4; ++h) mx = max3(mx, s[h][2 * y], s[h][2 * y + 1]);
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+            mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2)) * p.scale_log2;
+            const bool up = mx > m[y] + kFewThreshold;
+            alpha[y] = up ? ex2(m[y] - mx) : 1.f;
+            if (up) m[y] = mx;
+            raise |= up;
+          }
+          if (__any_sync(0xffffffffu, raise)) {
+            l[0] *= alpha[0];
+            l[1] *= alpha[1];
+#pragma unroll
+            for (int c = 0; c < kD / 8; ++c) {
+              acc[c][0] *= alpha[0]; acc[c][1] *= alpha[0];
+              acc[c][2] *= alpha[1]; acc[c][3] *= alpha[1];
+            }
+          }
+          uint32_t pf[2][4];
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const float neg = m[y] == -INFINITY ? 0.f : -m[y];
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+              const float a = ex2(fmaf(s[h][2 * y], p.scale_log2, neg)), b = ex2(fmaf(s[h][2 * y + 1], p.scale_log2, neg));
+              l[y] += a + b;
+              pf[h >> 1][2 * (h & 1) + y] = pack2(a, b);
+            }
+          }
+          // ---- V rows that no row sees hold anything: 0 * NaN would poison the product
+          if (edge) {
+            const int row = r + lane, tok = t0 + lane;
+            if (tok >= end || (tok < low && tok >= p.sinks)) {
+              unsigned char* dst = smem + stage * stage_bytes + v_off + ((((row >> bt_shift) * HV << bt_shift) + (row & bt_mask)) << 7);
+#pragma unroll 1
+              for (int c = 0; c < HV * 8; ++c)
+                *reinterpret_cast<uint4*>(dst + (((uint32_t)(c >> 3) << bt_shift) << 7) + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
+            }
+            ptx::fence_proxy_async();  // before the next TMA write
+            __syncwarp();
+          }
+          // ---- O += P V, 16 tokens at a time
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int row = r + h * 16 + (lane & 15), half = lane >> 4;
+            const uint32_t at = base + v_off + ((((row >> bt_shift) * HV << bt_shift) + (row & bt_mask)) << 7);
+#pragma unroll
+            for (int c = 0; c < kD / 16; ++c) {
+              uint32_t b[4];
+              ptx::ldmatrix_x4_trans(at + (((uint32_t)(c / 4) << bt_shift) << 7) + ((((c % 4) * 2 + half) ^ (row & 7)) << 4), b);
+              ptx::mma_bf16_16816(acc[2 * c], pf[h], b[0], b[1]);
+              ptx::mma_bf16_16816(acc[2 * c + 1], pf[h], b[2], b[3]);
+            }
+          }
+        }
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(empty0 + 8 * stage);
+        step();
+      }
+      // ---- the segment's result: sums over the four lanes of a row, then the slices pairwise, the upper half to the lower
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        l[y] += __shfl_xor_sync(0xffffffffu, l[y], 1);
+        l[y] += __shfl_xor_sync(0xffffffffu, l[y], 2);
+      }
+#pragma unroll 1
+      for (int h = slices >> 1; h > 0; h >>= 1) {
+        const int at = ((slice & (h - 1)) << mshift) | mt;
+        if (slice >= h && slice < 2 * h) {
+#pragma unroll
+          for (int c = 0; c < kD / 8; ++c) sc.o[at][c][lane] = make_float4(acc[c][0], acc[c][1], acc[c][2], acc[c][3]);
+          if (t4 == 0) {
+            sc.ml[at][g8] = make_float2(m[0], l[0]);
+            sc.ml[at][g8 + 8] = make_float2(m[1], l[1]);
+          }
+        }
+        ptx::named_barrier_sync(1, kWarps * 32);
+        if (slice < h) {
+          float wa[2], wb[2];
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            const float2 o = sc.ml[at][g8 + 8 * y];
+            const float top = fmaxf(m[y], o.x), ref = top == -INFINITY ? 0.f : top;
+            wa[y] = ex2(m[y] - ref);
+            wb[y] = ex2(o.x - ref);
+            l[y] = l[y] * wa[y] + o.y * wb[y];
+            m[y] = top;
+          }
+#pragma unroll
+          for (int c = 0; c < kD / 8; ++c) {
+            const float4 o = sc.o[at][c][lane];
+            acc[c][0] = fmaf(o.x, wb[0], acc[c][0] * wa[0]);
+            acc[c][1] = fmaf(o.y, wb[0], acc[c][1] * wa[0]);
+            acc[c][2] = fmaf(o.z, wb[1], acc[c][2] * wa[1]);
+            acc[c][3] = fmaf(o.w, wb[1], acc[c][3] * wa[1]);
+          }
+        }
+        ptx::named_barrier_sync(1, kWarps * 32);
+      }
+      if (slice == 0) {
+        const bool whole = w.flags & kSegWhole, to_out = whole && w.dst == kDstOut;
+        const bool as_f32 = !to_out || p.out_is_f32;
+        float* dst32 = to_out ? reinterpret_cast<float*>(p.out) : whole ? p.buffer[w.dst - 1].o : p.list.part_o;
+        const long long prow = (2LL * blockIdx.x + ((w.flags & kSegFirst) ? 1 : 0)) * p.list.slot_rows + group * used;
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const int lr = r0 + g8 + 8 * y;
+          if (!active || lr >= used) continue;
+          const float inv = l[y] != 0.f ? 1.f / l[y] : 0.f, lse2 = l[y] != 0.f ? m[y] + log2f(l[y]) : -INFINITY;
+          const long long row = whole ? out_row(lr) : prow + lr;
+          if (t4 == 0) {
+            if (!whole) p.list.part_lse[row] = lse2;
+            else if (!to_out) p.buffer[w.dst - 1].lse[row] = lse2;
+            else if (p.lse) p.lse[row] = lse2 * kLn2;
+          }
+#pragma unroll
+          for (int c = 0; c < kD / 8; ++c) {
+            const float a = acc[c][2 * y] * inv, b = acc[c][2 * y + 1] * inv;
+            if (as_f32) *reinterpret_cast<float2*>(dst32 + row * kD + c * 8 + 2 * t4) = make_float2(a, b);
+            else *reinterpret_cast<uint32_t*>(reinterpret_cast<__nv_bfloat16*>(p.out) + row * kD + c * 8 + 2 * t4) = pack2(a, b);
+          }
+        }
+      }
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(seg_empty0 + 8 * (segs % kSegRing));
+    }
+    if (dead) report(p.dev_status, DIFFQKV_ERR_TIMEOUT);
+  }
+  ptx::grid_dependency_wait();  // see extend.cu: the second of the two kernels ends behind the first
+}
+
+}  // namespace
+
+cudaError_t launch_extend_few(const CUtensorMap& mk, const CUtensorMap& mv, const void* q, ExtendParams p, int d_qk, int d_v,
+                              int blocks, bool second, cudaStream_t stream) {
+  using Fn = void (*)(const CUtensorMap, const CUtensorMap, const __nv_bfloat16*, const ExtendParams);
+  const Fn fn = d_v == 64 ? extend_few_kernel<64, 64> : d_qk == 128 ? extend_few_kernel<128, 128> : extend_few_kernel<64, 128>;
+  if (p.box_tok > kFewT) p.box_tok = kFewT;
+  const int stage = kFewT * 2 * (p.k_parts * d_qk + p.v_parts * d_v);
+  const int scratch = d_v == 64 ? (int)sizeof(Scratch<64>) : (int)sizeof(Scratch<128>);
+  p.few_stages = (kMaxSmem - scratch) / stage;
+  if (p.few_stages > kMaxStages) p.few_stages = kMaxStages;
+  const int smem = p.few_stages * stage + scratch;
+  const cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (err != cudaSuccess) return err;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)blocks);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = (size_t)smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = second ? 1 : 0;
+  const cudaError_t launched = cudaLaunchKernelEx(&cfg, fn, mk, mv, static_cast<const __nv_bfloat16*>(q), p);
+  if (launched == cudaSuccess) count_launch();
+  return launched;
+}
+
+}  // namespace diffqkv

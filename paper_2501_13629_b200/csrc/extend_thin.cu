@@ -53,29 +53,21 @@ struct ThinSegment {
   int v0;                      // V tiles requested before the segment (the ring's position)
   int flags;
 };
-struct RangedThinSegment : ThinSegment {
-  int end, start;  // the entry's tokens
-  int low, skip;   // first token behind the sinks that the chunk's first row sees; tiles skipped
-  int dst;
-};
 constexpr int kSegRing = 2;
 constexpr int kSegEnd = 1, kSegWhole = 2, kSegFirst = 4;
 
-template <bool kRanged>
 struct Scratch {
   float m[2][kThinCols];        // reference maximum of every column, per softmax group; weights at a segment's end
   float part[2][4][kThinCols];  // per warp: maxima, or sums at a segment's end
   uint64_t bars[42];
-  typename std::conditional<kRanged, RangedThinSegment, ThinSegment>::type seg[kSegRing];
+  ThinSegment seg[kSegRing];
   long long seek_lo;
   int seek_b, seek_row, seek_n, seek_past;  // the sequence that this block begins with
   uint32_t tmem;
   int abort;
-  int seek_end, seek_start, seek_tab, seek_dst;  // ranged
 };
-template <bool kRanged>
-constexpr int kThinSmem = kQRegion + kRingBytes + (int)sizeof(Scratch<kRanged>);
-static_assert(kThinSmem<true> <= 232448, "shared memory of a block");
+constexpr int kThinSmem = kQRegion + kRingBytes + (int)sizeof(Scratch);
+static_assert(kThinSmem <= 232448, "shared memory of a block");
 
 // The four warps of a (softmax group, half of the columns): does the condition hold anywhere; and a plain barrier.
 __device__ __forceinline__ bool group_any(int id, bool x) {
@@ -90,7 +82,7 @@ __device__ __forceinline__ bool group_any(int id, bool x) {
 }
 __device__ __forceinline__ void group_sync(int id) { asm volatile("barrier.cta.sync %0, 128;" ::"r"(id) : "memory"); }
 
-template <int kDQK, int kD, bool kRanged>
+template <int kDQK, int kD>
 __global__ void __launch_bounds__(kExtendThinThreads, 1)
 extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k,
                    const __grid_constant__ CUtensorMap tmap_v, const ExtendParams p) {
@@ -102,7 +94,7 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   unsigned char* q_s = smem;                     // [buffer][half][64 columns][128 B]
   unsigned char* p_s = smem + 2 * 16384;         // [group][128 tokens][128 B]
   unsigned char* ring_s = smem + kQRegion;
-  Scratch<kRanged>& sc = *reinterpret_cast<Scratch<kRanged>*>(smem + kQRegion + kRingBytes);
+  Scratch& sc = *reinterpret_cast<Scratch*>(smem + kQRegion + kRingBytes);
   const uint32_t bar0 = ptx::smem_u32(sc.bars);
   const uint32_t full0 = bar0, empty0 = full0 + 8 * kSlots;
   const uint32_t q_full0 = empty0 + 8 * kSlots, q_empty0 = q_full0 + 16;
@@ -122,10 +114,8 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     return;
   }
   if (p.first) ptx::grid_launch_dependents();
-  using Seq = SeqOf<kRanged>;
-  const int entries = entries_of<kRanged>(p);
-  const int per_thread = (entries + kExtendThinThreads - 1) / kExtendThinThreads;
-  const int b_lo = min(tid * per_thread, entries), b_hi = min(b_lo + per_thread, entries);
+  const int per_thread = (p.batch + kExtendThinThreads - 1) / kExtendThinThreads;
+  const int b_lo = min(tid * per_thread, p.batch), b_hi = min(b_lo + per_thread, p.batch);
   Seq my = {};  // the thread's first sequence: there is seldom another
   if (b_lo < b_hi) my.load(p, b_lo);
   bool any = my.thin_tiles > 0;
@@ -142,7 +132,7 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   }
   if (tid == 0) {
     sc.abort = 0;
-    sc.seek_b = entries;
+    sc.seek_b = p.batch;
     sc.seek_lo = 0;
     for (int s = 0; s < kSlots; ++s) {
       ptx::mbar_init(full0 + 8 * s, 1);
@@ -234,12 +224,6 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         sc.seek_row = s.lo;
         sc.seek_n = s.rows;
         sc.seek_past = s.past;
-        if constexpr (kRanged) {
-          sc.seek_end = s.end;
-          sc.seek_start = s.start;
-          sc.seek_tab = s.tab;
-          sc.seek_dst = s.dst;
-        }
         sc.seek_lo = before;
         break;
       }
@@ -267,21 +251,11 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     uint32_t kph = 0, vph = 0;
     bool ok = true;
     ExtendMeta m = {};
-    [[maybe_unused]] Seq seq;  // ranged: the entry, as far as it is kept there (end, start, tab, dst)
     auto load = [&](int b, int& lo, int& n, int& past) -> int {  // tiles of one unit of sequence b
-      if constexpr (kRanged) {
-        seq.load(p, b);
-        lo = seq.lo;
-        n = seq.rows;
-        past = seq.past;
-        return seq.thin_tiles;
-      } else {
-        load_rows(p, b, lo, n, past);
-        return n > 0 && n <= p.thin_max ? (past + n + kKT - 1) / kKT : 0;
-      }
+      load_rows(p, b, lo, n, past);
+      return n > 0 && n <= p.thin_max ? (past + n + kKT - 1) / kKT : 0;
     };
-    using Seg = typename std::conditional<kRanged, RangedThinSegment, ThinSegment>::type;
-    auto hand_out = [&](const Seg& d) -> bool {
+    auto hand_out = [&](const ThinSegment& d) -> bool {
       const int s = segs % kSegRing;
       if (!wait_warp(seg_empty0 + 8 * s, ((segs / kSegRing) & 1) ^ 1, abort_flag)) return false;
       if (lane == 0) {
@@ -296,11 +270,6 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     long long item_lo = sc.seek_lo;
     if (w0 < w1) {
       nt = (past + n + kKT - 1) / kKT;
-      if constexpr (kRanged) {
-        seq.end = sc.seek_end; seq.start = sc.seek_start; seq.tab = sc.seek_tab; seq.dst = sc.seek_dst;
-        seq.past = past;
-        nt = (seq.end + kKT - 1) / kKT - seq.skip(p, 0);
-      }
       const long long in = w0 - item_lo;
       if (chunk > 0) {  // chunk `in` of the sequence: a range of one item, counted from the item's start
         const int per = (nt + chunk - 1) / chunk;
@@ -312,18 +281,18 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         item_lo += (long long)u * size;
       }
     } else {
-      b = entries;
+      b = p.batch;
     }
     auto next_item = [&] {
       item_lo += nt + kThinItemCost;
       if (++u < p.n_units) return;
       u = 0;
       do {
-        if (++b >= entries) return;
+        if (++b >= p.batch) return;
         nt = load(b, lo, n, past);
       } while (nt == 0);
     };
-    while (ok && b < entries && item_lo < w1) {
+    while (ok && b < p.batch && item_lo < w1) {
       int ta, tb;
       if (chunk > 0) {
         ta = chunk_lo;
@@ -332,13 +301,7 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         ta = item_tile(w0 - item_lo, 1, nt, kThinItemCost);
         tb = item_tile(w1 - item_lo, 1, nt, kThinItemCost);
       }
-      int kv_len = past + n, tab = b, low = 0, skip = 0;
-      if constexpr (kRanged) {
-        kv_len = seq.end;
-        tab = seq.tab;
-        low = seq.low(p, 0);
-        skip = seq.skip(p, 0);
-      }
+      const int kv_len = past + n;
       const int head0 = u * p.parts * p.G;
       const int hk0 = head0 / p.heads_per_k, hv0 = head0 / p.heads_per_v;  // Eq. (idx)
       if (ta >= tb) {  // the share ends within the item's own cost
@@ -349,35 +312,23 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         m.rows = p.parts * n * p.G; m.part_rows = n * p.G; m.row_lo = lo; m.head0 = head0;
         m.parts = chunk > 0 ? (nt + chunk - 1) / chunk
                             : share_of(item_lo + last_tile(1, nt, kThinItemCost), total, blocks) - (int)blockIdx.x + 1;
-        if constexpr (kRanged) m.dst = seq.dst;
       }
-      Seg seg;
-      static_cast<ThinSegment&>(seg) = {lo, n, past, head0, ta, tb, v_count, (ta == 0 ? kSegFirst : 0) | (ta == 0 && tb == nt ? kSegWhole : 0)};
-      if constexpr (kRanged) {
-        seg.end = kv_len; seg.start = seq.start; seg.low = low; seg.skip = skip; seg.dst = seq.dst;
-      }
-      if (!hand_out(seg)) {
+      if (!hand_out({lo, n, past, head0, ta, tb, v_count, (ta == 0 ? kSegFirst : 0) | (ta == 0 && tb == nt ? kSegWhole : 0)})) {
         ok = false;
         break;
       }
-      // first token of tile `tile`, and whether this lane's box of it has a token that is wanted
-      auto token_of = [&](int tile) -> int { return (kRanged && tile >= p.sink_tiles ? tile + skip : tile) * kKT; };
-      auto wanted = [&](int tok) -> bool { return !kRanged || tok < p.sinks || tok + p.box_tok > low; };
       auto fetch = [&](int tile) -> int {  // page of this lane's box (fetched two tiles ahead)
-        if (!p.page_table) return tab;
-        const int tok = token_of(tile) + my_part * p.box_tok;
-        if (tile >= tb || tok >= kv_len || !wanted(tok)) return 0;
-        return p.page_table[(long long)tab * p.max_pages_per_seq + tok / p.page_size];
+        if (!p.page_table) return b;
+        const int tok = tile * kKT + my_part * p.box_tok;
+        if (tile >= tb || tok >= kv_len) return 0;
+        return p.page_table[(long long)b * p.max_pages_per_seq + tok / p.page_size];
       };
       // The tiles of the K heads (is_k) or of the V heads of token tile `tile`, whose page is `page`.
       auto request = [&](auto is_k, int tile, int page) __attribute__((always_inline)) {
         constexpr bool kIsK = decltype(is_k)::value;
-        const int tok = token_of(tile);
-        int parts_valid = min(boxes_part, (kv_len - tok + p.box_tok - 1) / p.box_tok);  // of the tile that are read
-        const bool reads = my_part < parts_valid && wanted(tok + my_part * p.box_tok);
-        if constexpr (kRanged)
-          parts_valid = __popc(__ballot_sync(0xffffffffu, reads) & (uint32_t)((1ull << boxes_part) - 1));
-        if (reads && (page < 0 || page >= p.num_blocks)) {  // never read outside the pool: flag it, block 0 instead
+        const int tok = tile * kKT;
+        const int parts_valid = min(boxes_part, (kv_len - tok + p.box_tok - 1) / p.box_tok);
+        if (my_part < parts_valid && (page < 0 || page >= p.num_blocks)) {  // never read outside the pool: flag it, block 0 instead
           report(p.dev_status, DIFFQKV_ERR_INDEX);
           page = 0;
         }
@@ -401,7 +352,7 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
           if (here && fine) {
             const uint32_t bar = full0 + 8 * slot, dst = ring + slot * kSlotBytes + (kIsK ? k_off : v_off);
             if (lane == mine * boxes_part * (kIsK ? k_halves : v_halves)) ptx::mbar_arrive_expect_tx(bar, bytes);
-            if (reads) {
+            if (my_part < parts_valid) {
               const int head = (kIsK ? hk0 : hv0) + x0 + mine;
               const CUtensorMap* map = kIsK ? &tmap_k : &tmap_v;
               if (kIsK ? p.k_rows : p.v_rows) ptx::tma_load_5d(dst, map, bar, 0, 0, 0, head * p.head_groups + slot_tok / 8, page);
@@ -442,9 +393,7 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       if (chunk > 0) break;
       next_item();
     }
-    Seg last = {};
-    last.flags = kSegEnd;
-    if (ok) ok = hand_out(last);
+    if (ok) ok = hand_out({0, 0, 0, 0, 0, 0, 0, kSegEnd});
     if (lane == 0) p.list.meta[blockIdx.x] = m;
     if (!ok) {
       report(p.dev_status, DIFFQKV_ERR_TIMEOUT);
@@ -573,7 +522,7 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     int other = 0;  // tiles of the other group in earlier segments
     bool ok = true;
     for (uint32_t segs = 0;; ++segs) {
-      const auto& w = sc.seg[segs % kSegRing];
+      const ThinSegment& w = sc.seg[segs % kSegRing];
       ok = wait_warp(seg_full0 + 8 * (segs % kSegRing), (segs / kSegRing) & 1, abort_flag);
       // Group 1 hands its sums and maxima over at a segment's end: it may write there again once they have been read.
       if (ok && t == 1 && !(w.flags & kSegEnd) && w.tb - w.ta > 1) ok = wait_warp(x_empty, xpar ^ 1, abort_flag);
@@ -594,36 +543,13 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         ok = wait_warp(s_full0 + 8 * t, par, abort_flag) && ok;
         tc::fence_after_sync();
         float x[kHalfCols];
-        int k0 = (w.ta + i) * kKT;  // first token
-        if constexpr (kRanged) {
-          if (w.ta + i >= p.sink_tiles) k0 += w.skip * kKT;
-        }
+        const int k0 = (w.ta + i) * kKT;
         auto load_scores = [&] {  // they stay in tensor memory until this tile's weights are announced
 #pragma unroll
           for (int q = 0; q < kHalfCols / 8; ++q)
             if (mask >> q & 1) tc::ld_32x32b_x8(s_taddr + q * 8, *reinterpret_cast<uint32_t(*)[8]>(&x[q * 8]));
           tc::wait_ld();
-          if constexpr (kRanged) {
-            // columns of a group from `first` on and below `last` belong to rows that see this thread's token
-            const int token = k0 + r;
-            int first = 0, last = kThinCols;
-            if (token > w.past) first = token < w.end ? (token - w.past) * p.G : kThinCols;
-            else if (token >= w.end) first = kThinCols;  // a prefix, whose rows all come behind it
-            if (token >= p.sinks) {
-              if (token < w.start) last = 0;
-              else if (token - w.past < p.thin_max - p.window) last = max(token - w.past + p.window, 0) * p.G;
-            }
-            if (__any_sync(0xffffffffu, first > 0 || last < kThinCols)) {
-#pragma unroll
-              for (int q = 0; q < kHalfCols / 8; ++q)
-                if (mask >> q & 1) {
-                  const int lc = (c0 + q * 8) & (p.region - 1);
-#pragma unroll
-                  for (int e = 0; e < 8; ++e)
-                    if (lc + e < first || lc + e >= last) x[q * 8 + e] = -INFINITY;
-                }
-            }
-          } else if (k0 + kKT > w.past + 1) {  // the tile reaches past some row's position
+          if (k0 + kKT > w.past + 1) {  // the tile reaches past some row's position
             const int hidden = (k0 + r - w.past) * p.G;  // columns of a group below this belong to rows before the token
 #pragma unroll
             for (int q = 0; q < kHalfCols / 8; ++q)
@@ -639,11 +565,7 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         // ---- scores on the scale of base 2, from the reference: the score of the segment's first token of this group to
         // begin with (a row that does not see it sees none of the tile)
         if (!later) {
-          int from = 0;  // ranged: the first token that every row of the chunk sees, as far as its window goes
-          if constexpr (kRanged) {
-            if (k0 >= p.sinks) from = min(max(max(w.start, w.past + w.n - p.window) - k0, 0), kKT - 1);
-          }
-          if (r == from) {
+          if (quarter == 0 && lane == 0) {
             // -inf counts as the lowest number, which any other raises
             auto start = [&](float y) { y *= p.scale_log2; return y == -INFINITY ? kLowest : y; };
 #pragma unroll
@@ -736,20 +658,14 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
             }
             *reinterpret_cast<uint4*>(p_row + (((half * 4 + q) ^ (r & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
           }
-        bool clear;
-        if constexpr (kRanged) clear = k0 + kKT > w.end || (k0 < w.low && k0 + kKT > p.sinks);
-        else clear = k0 + kKT > w.past + w.n;
-        if (clear) {
+        if (k0 + kKT > w.past + w.n) {
           // V rows past the sequence end hold whatever followed in memory: zero them (0 * NaN would poison the product).
           // Where the ring has room for one tile's V the tile before, the other group's, may still wait for its own, in the
           // place that this one's will have: until its product is done a wait for this V could take the phase before for
           // its own.  (In a longer ring that place was the tile's before, whose product this group has waited for, or an
           // earlier segment's, whose products had all been issued.)
           if (i > 0 && p.v_ring < 2 * p.v_parts) ok = wait_warp(o_done0 + 8 * (1 - t), (other + ((i - 1) >> 1)) & 1, abort_flag) && ok;
-          bool zero;
-          if constexpr (kRanged) zero = k0 + r >= w.end || (k0 + r < w.low && k0 + r >= p.sinks);
-          else zero = r >= w.past + w.n - k0;
-          if (half == 0 && zero) {
+          if (half == 0 && r >= w.past + w.n - k0) {
             for (int y = 0; y < p.v_parts; ++y) {
               const int at = w.v0 + i * p.v_parts + y, slot = p.k_ring + at % p.v_ring;
               ok = ok && ptx::mbar_wait(full0 + 8 * slot, (at / p.v_ring) & 1, abort_flag);
@@ -817,21 +733,8 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         if (g < p.parts && lc < used) {
           const float lse2 = sum != 0.f ? top + log2f(sum) : -INFINITY;
           const int token = lc / p.G;
-          bool done = false;
-          if constexpr (kRanged) {
-            done = whole && w.dst != kDstOut;
-            if (done) p.buffer[w.dst - 1].lse[(long long)(w.row_lo + token) * p.n_q + w.head0 + g * p.G + lc - token * p.G] = lse2;
-          }
           if (!whole) p.list.part_lse[prow0 + g * used + lc] = lse2;
-          else if (!done && p.lse) p.lse[(long long)(w.row_lo + token) * p.n_q + w.head0 + g * p.G + lc - token * p.G] = lse2 * kLn2;
-        }
-      }
-      bool as_f32 = p.out_is_f32;
-      float* dst32 = reinterpret_cast<float*>(p.out);
-      if constexpr (kRanged) {
-        if (w.dst != kDstOut) {
-          as_f32 = true;
-          dst32 = p.buffer[w.dst - 1].o;
+          else if (p.lse) p.lse[(long long)(w.row_lo + token) * p.n_q + w.head0 + g * p.G + lc - token * p.G] = lse2 * kLn2;
         }
       }
       group_sync(bar_id);
@@ -855,7 +758,7 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
           if (join) y = fmaf(__uint_as_float(o1[e]), sc.m[1][c + e], y);
           if (lc + e < used && mine) {
             if (!whole) p.list.part_o[at] = y;
-            else if (as_f32) dst32[at] = y;
+            else if (p.out_is_f32) reinterpret_cast<float*>(p.out)[at] = y;
             else reinterpret_cast<__nv_bfloat16*>(p.out)[at] = __float2bfloat16_rn(y);
           }
           at += kD;
@@ -894,19 +797,15 @@ extend_thin_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
 }  // namespace
 
 cudaError_t launch_extend_thin(const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv, const ExtendParams& p,
-                               int d_qk, int d_v, int blocks, bool second, bool ranged, cudaStream_t stream) {
+                               int d_qk, int d_v, int blocks, bool second, cudaStream_t stream) {
   using Fn = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const ExtendParams);
-  constexpr Fn fns[2][3] = {
-      {extend_thin_kernel<64, 64, false>, extend_thin_kernel<128, 128, false>, extend_thin_kernel<64, 128, false>},
-      {extend_thin_kernel<64, 64, true>, extend_thin_kernel<128, 128, true>, extend_thin_kernel<64, 128, true>}};
-  const Fn fn = fns[ranged][d_v == 64 ? 0 : d_qk == 128 ? 1 : 2];
-  const int smem = ranged ? kThinSmem<true> : kThinSmem<false>;
-  const cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const Fn fn = d_v == 64 ? extend_thin_kernel<64, 64> : (d_qk == 128 ? extend_thin_kernel<128, 128> : extend_thin_kernel<64, 128>);
+  const cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kThinSmem);
   if (err != cudaSuccess) return err;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks);
   cfg.blockDim = dim3(kExtendThinThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = kThinSmem;
   cfg.stream = stream;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
