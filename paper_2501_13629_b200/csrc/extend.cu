@@ -85,6 +85,22 @@ struct Walk {
   bool wide;
   int nt, ta, tb, nst0;
 
+  // ranged: likewise, the sequence is loaded already
+  __device__ void start(const ExtendParams& p, uint32_t w0, uint32_t w1, int b0, uint32_t lo, const SeqOf<true>& s0) {
+    begin = w0; end = w1;
+    b = b0;
+    seq = s0;
+    const uint32_t per = seq.cost(p);
+    u = (int)((w0 - lo) / per);
+    const int r = (int)(w0 - lo - u * per);
+    int a = 0, z = seq.items;  // largest item whose start is not behind r
+    while (z - a > 1) {
+      const int mid = (a + z) >> 1;
+      if (seq.cost_before(p, mid) <= r) a = mid; else z = mid;
+    }
+    item = a;
+    item_lo = (long long)lo + u * per + seq.cost_before(p, item);
+  }
   // from the sequence b0 in which the block's range begins, whose flat place is lo
   __device__ void start(const ExtendParams& p, long long w0, long long w1, int b0, long long lo) {
     begin = w0; end = w1;
@@ -126,6 +142,7 @@ struct Walk {
   }
   __device__ void advance(const ExtendParams& p) {
     item_lo += kItemCost + (long long)(seq.wide(p, item) ? kWideCost : kNarrowCost) * seq.tiles(p, item);
+    if (kRanged && item_lo >= end) return;  // no reading on through entries of a few rows, 800 cycles each
     if (++item < seq.items) return;
     item = 0;
     if (++u < p.n_units) return;
@@ -194,6 +211,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   using Seg = typename std::conditional<kRanged, RangedSegment, Segment>::type;
   __shared__ Seg seg_s[kSegRing];
   __shared__ long long scan_s[kExtendThreads / 32], others_s[kExtendThreads / 32];
+  __shared__ RangedScan<kExtendThreads / 32> ranged_s;
   __shared__ long long seek_lo_s;
   __shared__ int seek_b_s;
 
@@ -201,102 +219,130 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   // The kernel for thin sequences works on other rows; whichever of the two comes second may take the SMs that the
   // first one's blocks leave.  The joining kernel depends on the second alone, which therefore ends behind the first.
   if (p.first) ptx::grid_launch_dependents();
-  using Seq = SeqOf<kRanged>;
-  const int entries = entries_of<kRanged>(p);
-  const int per_thread = (entries + kExtendThreads - 1) / kExtendThreads;
-  const int b_lo = min(tid * per_thread, entries), b_hi = min(b_lo + per_thread, entries);
-  Seq my = {};  // the thread's first sequence: there is seldom another
-  if (b_lo < b_hi) my.load(p, b_lo);
-  {  // a step of thin sequences alone (decode): nothing to do here
-    bool any = my.n > 0 || my.bad;
-    for (int b = b_lo + 1; b < b_hi; ++b) {
-      Seq x;
-      x.load(p, b);
-      any |= x.n > 0 || x.bad;
+  const int team = (int)blockIdx.x / p.list.team, member = (int)blockIdx.x - team * p.list.team;
+  long long total, w0, w1;  // of the flat list; this block's range of it
+  int n_teams;              // that take part
+  uint32_t tmem_base;
+  auto init = [&] {
+    if (tid == 0) {
+      *abort_flag = 0;
+      if constexpr (!kRanged) {
+        seek_b_s = p.batch;
+        seek_lo_s = 0;
+      }
+      ptx::mbar_init(q_full, 1);
+      ptx::mbar_init(q_empty, 1);
+      for (int s = 0; s < kKSlots; ++s) {
+        ptx::mbar_init(k_full0 + 8 * s, 1);
+        ptx::mbar_init(k_empty0 + 8 * s, 1);
+      }
+      for (int s = 0; s < kVSlots; ++s) {
+        ptx::mbar_init(v_full0 + 8 * s, 1);
+        ptx::mbar_init(v_empty0 + 8 * s, 1);
+      }
+      for (int t = 0; t < 2; ++t) {
+        ptx::mbar_init(s_full0 + 8 * t, 1);
+        ptx::mbar_init(p_half0 + 8 * t, 4);
+        ptx::mbar_init(p_full0 + 8 * t, 4);
+        ptx::mbar_init(o_done0 + 8 * t, 1);
+        ptx::mbar_init(o_free0 + 8 * t, 4);
+        ptx::mbar_init(s_free0 + 8 * t, 4);
+      }
+      ptx::mbar_init(x_full, 4);
+      for (int s = 0; s < kSegRing; ++s) {
+        ptx::mbar_init(seg_full0 + 8 * s, 1);
+        ptx::mbar_init(seg_empty0 + 8 * s, 9);  // the MMA thread and eight softmax warps
+      }
+      ptx::mbar_init(drain, 1);
+      ptx::fence_barrier_init();
+      ptx::prefetch_tmap(&tmap_q);
+      ptx::prefetch_tmap(&tmap_k);
+      ptx::prefetch_tmap(&tmap_v);
     }
-    if (!__syncthreads_or(any)) {
+    if (warp == 1) {
+      tc::tmem_alloc(ptx::smem_u32(tmem_slot), kTmemCols);
+      tc::tmem_relinquish();
+    }
+  };
+  if constexpr (kRanged) {
+    init();
+    tc::fence_before_sync();
+    SeqOf<true> my;
+    const RangedStart at = ranged_start(p, ranged_s, my, blockIdx.x == 0);
+    tc::fence_after_sync();
+    tmem_base = *tmem_slot;
+    total = at.wide;
+    n_teams = ranged_wide_teams(p, at.wide, at.few);
+    if (team >= n_teams) {  // no long chunks (decode), or fewer than blocks
       if (tid == 0) p.list.meta[blockIdx.x].rows = 0;
+      if (warp == 1) tc::tmem_dealloc(tmem_base, kTmemCols);
       ptx::grid_dependency_wait();
       return;
     }
-  }
-  if (tid == 0) {
-    *abort_flag = 0;
-    seek_b_s = entries;
-    seek_lo_s = 0;
-    ptx::mbar_init(q_full, 1);
-    ptx::mbar_init(q_empty, 1);
-    for (int s = 0; s < kKSlots; ++s) {
-      ptx::mbar_init(k_full0 + 8 * s, 1);
-      ptx::mbar_init(k_empty0 + 8 * s, 1);
-    }
-    for (int s = 0; s < kVSlots; ++s) {
-      ptx::mbar_init(v_full0 + 8 * s, 1);
-      ptx::mbar_init(v_empty0 + 8 * s, 1);
-    }
-    for (int t = 0; t < 2; ++t) {
-      ptx::mbar_init(s_full0 + 8 * t, 1);
-      ptx::mbar_init(p_half0 + 8 * t, 4);
-      ptx::mbar_init(p_full0 + 8 * t, 4);
-      ptx::mbar_init(o_done0 + 8 * t, 1);
-      ptx::mbar_init(o_free0 + 8 * t, 4);
-      ptx::mbar_init(s_free0 + 8 * t, 4);
-    }
-    ptx::mbar_init(x_full, 4);
-    for (int s = 0; s < kSegRing; ++s) {
-      ptx::mbar_init(seg_full0 + 8 * s, 1);
-      ptx::mbar_init(seg_empty0 + 8 * s, 9);  // the MMA thread and eight softmax warps
-    }
-    ptx::mbar_init(drain, 1);
-    ptx::fence_barrier_init();
-    ptx::prefetch_tmap(&tmap_q);
-    ptx::prefetch_tmap(&tmap_k);
-    ptx::prefetch_tmap(&tmap_v);
-  }
-  if (warp == 1) {
-    tc::tmem_alloc(ptx::smem_u32(tmem_slot), kTmemCols);
-    tc::tmem_relinquish();
-  }
-  // ---- this block's range of the flat list: every thread sums the cost of its share of the sequences
-  long long mine = 0, others = 0, total;
-  bool any_thin = false;
-  Seq s = my;
-  for (int b = b_lo; b < b_hi;) {
-    if (s.bad && blockIdx.x == 0) report(p.dev_status, DIFFQKV_ERR_INDEX);
-    if (s.n > 0) mine += p.n_units * s.cost(p);
-    if (s.thin_tiles > 0) {
-      others += (long long)p.n_units * (s.thin_tiles + (kRanged ? kFewItemCost : kThinItemCost));
-      any_thin = true;
-    }
-    if (++b < b_hi) s.load(p, b);
-  }
-  tc::fence_before_sync();
-  any_thin = __syncthreads_or(any_thin);
-  long long before = block_scan<kExtendThreads / 32>(mine, scan_s, total);
-  tc::fence_after_sync();
-  const uint32_t tmem_base = *tmem_slot;
-  if (any_thin) block_scan<kExtendThreads / 32>(others, others_s, others);
-  const int team = (int)blockIdx.x / p.list.team, member = (int)blockIdx.x - team * p.list.team;
-  const int n_teams = wide_teams(p, total, others);  // that take part
-  if (team >= n_teams) {
-    if (tid == 0) p.list.meta[blockIdx.x].rows = 0;
-    if (warp == 1) tc::tmem_dealloc(tmem_base, kTmemCols);
-    ptx::grid_dependency_wait();
-    return;
-  }
-  const long long w0 = share_start(total, team, n_teams), w1 = share_start(total, team + 1, n_teams);
-  if (w0 < w1 && before <= w0 && w0 < before + mine) {
-    s = my;
-    for (int b = b_lo;;) {
-      const long long c = p.n_units * s.cost(p);
-      if (w0 < before + c) {
-        seek_b_s = b;
-        seek_lo_s = before;
-        break;
+    w0 = ranged_share_start(at.wide, team, n_teams);
+    w1 = ranged_share_start(at.wide, team + 1, n_teams);
+    ranged_seek(p, ranged_s, at, my, (uint32_t)w0, at.before_wide,
+                [&](const SeqOf<true>& s) -> uint32_t { return s.n > 0 ? p.n_units * (uint32_t)s.cost(p) : 0u; });
+  } else {
+    const int per_thread = (p.batch + kExtendThreads - 1) / kExtendThreads;
+    const int b_lo = min(tid * per_thread, p.batch), b_hi = min(b_lo + per_thread, p.batch);
+    SeqOf<false> my = {};  // the thread's first sequence: there is seldom another
+    if (b_lo < b_hi) my.load(p, b_lo);
+    {  // a step of thin sequences alone (decode): nothing to do here
+      bool any = my.n > 0 || my.bad;
+      for (int b = b_lo + 1; b < b_hi; ++b) {
+        SeqOf<false> x;
+        x.load(p, b);
+        any |= x.n > 0 || x.bad;
       }
-      before += c;
-      if (++b >= b_hi) break;
-      s.load(p, b);
+      if (!__syncthreads_or(any)) {
+        if (tid == 0) p.list.meta[blockIdx.x].rows = 0;
+        ptx::grid_dependency_wait();
+        return;
+      }
+    }
+    init();
+    // ---- this block's range of the flat list: every thread sums the cost of its share of the sequences
+    long long mine = 0, others = 0;
+    bool any_thin = false;
+    SeqOf<false> s = my;
+    for (int b = b_lo; b < b_hi;) {
+      if (s.bad && blockIdx.x == 0) report(p.dev_status, DIFFQKV_ERR_INDEX);
+      if (s.n > 0) mine += p.n_units * s.cost(p);
+      if (s.thin_tiles > 0) {
+        others += (long long)p.n_units * (s.thin_tiles + kThinItemCost);
+        any_thin = true;
+      }
+      if (++b < b_hi) s.load(p, b);
+    }
+    tc::fence_before_sync();
+    any_thin = __syncthreads_or(any_thin);
+    long long before = block_scan<kExtendThreads / 32>(mine, scan_s, total);
+    tc::fence_after_sync();
+    tmem_base = *tmem_slot;
+    if (any_thin) block_scan<kExtendThreads / 32>(others, others_s, others);
+    n_teams = wide_teams(p, total, others);  // that take part
+    if (team >= n_teams) {
+      if (tid == 0) p.list.meta[blockIdx.x].rows = 0;
+      if (warp == 1) tc::tmem_dealloc(tmem_base, kTmemCols);
+      ptx::grid_dependency_wait();
+      return;
+    }
+    w0 = share_start(total, team, n_teams);
+    w1 = share_start(total, team + 1, n_teams);
+    if (w0 < w1 && before <= w0 && w0 < before + mine) {
+      s = my;
+      for (int b = b_lo;;) {
+        const long long c = p.n_units * s.cost(p);
+        if (w0 < before + c) {
+          seek_b_s = b;
+          seek_lo_s = before;
+          break;
+        }
+        before += c;
+        if (++b >= b_hi) break;
+        s.load(p, b);
+      }
     }
   }
   __syncthreads();
@@ -309,14 +355,21 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     // ------------------------------------------------------------------ TMA producer
     // One box per (token part, channel half) of a tile: lane x owns box x of every K tile and of every V tile.
     const int parts = kKT / p.box_tok;
-    const int boxes = kHalvesMax * parts;
-    const int my_part = lane / kHalvesMax, my_half = lane % kHalvesMax;
+    // Ranged: where the cache allows (see make_row_map) a box brings whole rows, half as many boxes: tiles of 16-token pages
+    // come at the rate of boxes (7.2 thousand cycles for a K and a V tile of 128 channels, not 3.5).
+    int box_halves = kHalvesMax;
+    if constexpr (kRanged) box_halves = (kHalvesK == 2 && !p.k_rows) || (kHalves == 2 && !p.v_rows) ? 2 : 1;
+    const int boxes = box_halves * parts;
+    const int my_part = lane / box_halves, my_half = lane % box_halves;
     const uint32_t my_off = my_half * (kKT * 128) + my_part * (p.box_tok * 128);
+    const bool k_here = kRanged && p.k_rows ? my_half == 0 : my_half < kHalvesK;
+    const bool v_here = kRanged && p.v_rows ? my_half == 0 : my_half < kHalves;
     int kc = 0, vc = 0, segs = 0;  // K tiles, V tiles, Q loads requested so far
     bool ok = true;
     ExtendMeta m = {};
     Walk<kRanged> w;
-    w.start(p, w0, w1, seek_b_s, seek_lo_s);
+    if constexpr (kRanged) w.start(p, (uint32_t)w0, (uint32_t)w1, ranged_s.e, ranged_s.lo, ranged_s.seq);
+    else w.start(p, w0, w1, seek_b_s, seek_lo_s);
     auto hand_out = [&](const Seg& d) -> bool {
       const int s = segs % kSegRing;
       if (!wait_warp(seg_empty0 + 8 * s, ((segs / kSegRing) & 1) ^ 1, abort_flag)) return false;
@@ -399,16 +452,26 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
               if (!wait_warp(k_empty0 + 8 * s, ((kc / kKSlots) & 1) ^ 1, abort_flag)) { ok = false; continue; }
               if (lane == 0) ptx::mbar_arrive_expect_tx(k_full0 + 8 * s, (uint32_t)parts_valid * p.box_tok * 128u * kHalvesK);
               __syncwarp();
-              if (here && my_half < kHalvesK)
-                ptx::tma_load_5d(k_u32 + s * kKBytes + my_off, &tmap_k, k_full0 + 8 * s, 0, slot_tok, my_half, hk, now[x]);
+              if (here && k_here) {
+                if (kRanged && p.k_rows)
+                  ptx::tma_load_5d(k_u32 + s * kKBytes + my_part * (p.box_tok * 256), &tmap_k, k_full0 + 8 * s, 0, 0, 0,
+                                   hk * p.head_groups + slot_tok / 8, now[x]);
+                else
+                  ptx::tma_load_5d(k_u32 + s * kKBytes + my_off, &tmap_k, k_full0 + 8 * s, 0, slot_tok, my_half, hk, now[x]);
+              }
               ++kc;
             } else {
               const int s = vc % kVSlots;
               if (!wait_warp(v_empty0 + 8 * s, ((vc / kVSlots) & 1) ^ 1, abort_flag)) { ok = false; continue; }
               if (lane == 0) ptx::mbar_arrive_expect_tx(v_full0 + 8 * s, (uint32_t)parts_valid * p.box_tok * 128u * kHalves);
               __syncwarp();
-              if (here && my_half < kHalves)
-                ptx::tma_load_5d(v_u32 + s * kTBytes + my_off, &tmap_v, v_full0 + 8 * s, 0, slot_tok, my_half, hv, now[x]);
+              if (here && v_here) {
+                if (kRanged && p.v_rows)
+                  ptx::tma_load_5d(v_u32 + s * kTBytes + my_part * (p.box_tok * 256), &tmap_v, v_full0 + 8 * s, 0, 0, 0,
+                                   hv * p.head_groups + slot_tok / 8, now[x]);
+                else
+                  ptx::tma_load_5d(v_u32 + s * kTBytes + my_off, &tmap_v, v_full0 + 8 * s, 0, slot_tok, my_half, hv, now[x]);
+              }
               ++vc;
             }
           }
@@ -451,15 +514,21 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     if (ptx::elect_one()) {
       bool ok = true;
       const uint32_t q_lo = tc::smem_desc_lo(q_u32, 16), k_lo = tc::smem_desc_lo(k_u32, 16);
-      const uint32_t v_lo = tc::smem_desc_lo(v_u32, kKT * 128);  // 64-channel chunks of V are one half tile apart
+      // 64-channel chunks of V are one half tile apart; or, where boxes bring whole rows, a tile is [16 groups of 8
+      // tokens][half][8][128 B]
+      const bool k_rows = kRanged && p.k_rows, v_rows = kRanged && p.v_rows;
+      const uint32_t v_lo = tc::smem_desc_lo(v_u32, v_rows ? 1024 : kKT * 128);
+      const uint32_t k_hi = k_rows ? tc::smem_desc_hi_sw128(2048) : hi, v_hi = v_rows ? tc::smem_desc_hi_sw128(2048) : hi;
+      const uint32_t k_half = (k_rows ? 1024 : 128 * 128) >> 4, v_16 = (v_rows ? 4096 : 16 * 128) >> 4;  // 16 tokens of V
       auto issue_s = [&](int t, int qt, int slot) {  // S_t = Q_qt . K^T
         const uint32_t qa = q_lo + qt * (kQBytes >> 4), ka = k_lo + slot * (kKBytes >> 4);
         const uint32_t d = tmem_base + t * 128;
-        tc::mma_ss_halves<false>(d, qa, hi, ka, hi, idesc);
+        tc::mma_ss_halves<false>(d, qa, hi, ka, k_hi, idesc);
 #pragma unroll
         for (int ks = 1; ks < kDQK / 16; ++ks) {
           const uint32_t step = ((ks / 4) * (128 * 128) + (ks % 4) * 32) >> 4;
-          tc::mma_ss_halves<true>(d, qa + step, hi, ka + step, hi, idesc);
+          const uint32_t k_step = (ks / 4) * k_half + (((ks % 4) * 32) >> 4);
+          tc::mma_ss_halves<true>(d, qa + step, hi, ka + k_step, k_hi, idesc);
         }
         tc::commit(s_full0 + 8 * t);
       };
@@ -468,14 +537,14 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         const uint32_t d = tmem_base + 256 + t * kD, pa = kSepP ? tmem_base + 384 + t * 64 : tmem_base + t * 128;
         constexpr int kSteps = kKT / 32;
         if (half == 0) {
-          if (first) tc::mma_ts_halves<false>(d, pa, va, hi, idesc_pv);
-          else tc::mma_ts_halves<true>(d, pa, va, hi, idesc_pv);
+          if (first) tc::mma_ts_halves<false>(d, pa, va, v_hi, idesc_pv);
+          else tc::mma_ts_halves<true>(d, pa, va, v_hi, idesc_pv);
 #pragma unroll
-          for (int k = 1; k < kSteps; ++k) tc::mma_ts_halves<true>(d, pa + k * 8, va + ((k * 16 * 128) >> 4), hi, idesc_pv);
+          for (int k = 1; k < kSteps; ++k) tc::mma_ts_halves<true>(d, pa + k * 8, va + k * v_16, v_hi, idesc_pv);
         } else {
 #pragma unroll
           for (int k = kSteps; k < 2 * kSteps; ++k)
-            tc::mma_ts_halves<true>(d, pa + k * 8, va + ((k * 16 * 128) >> 4), hi, idesc_pv);
+            tc::mma_ts_halves<true>(d, pa + k * 8, va + k * v_16, v_hi, idesc_pv);
           tc::commit(o_done0 + 8 * t);
         }
       };
@@ -611,7 +680,8 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
           if (zero) {
 #pragma unroll
             for (int half = 0; half < kHalves; ++half) {
-              uint4* dst = reinterpret_cast<uint4*>(v_s + vslot * kTBytes + half * (kKT * 128) + r * 128);
+              const int at = kRanged && p.v_rows ? (r / 8) * 2048 + half * 1024 + (r % 8) * 128 : half * (kKT * 128) + r * 128;
+              uint4* dst = reinterpret_cast<uint4*>(v_s + vslot * kTBytes + at);
 #pragma unroll
               for (int e = 0; e < 8; ++e) dst[e] = make_uint4(0, 0, 0, 0);
             }
@@ -1238,6 +1308,13 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
     }
   }
   const Plan pl = make_plan(s, total_q);
+  if (range) {  // both lists in 32 bits; see ranged_start
+    const long long entries = (long long)range->groups + s.batch, units = pl.groups / pl.parts;
+    const long long items = total_q / (2 * pl.T) * (range->groups > 0 ? 2LL : 1LL) + entries;
+    if (items * units * (kItemCost + kWideCost * (c.max_seqlen / kKT + 2LL)) > 0x7fffffffLL ||
+        entries * units * (kFewItemCost + c.max_seqlen / kFewT + 2LL) > 0x7fffffffLL)
+      return cudaErrorNotSupported;
+  }
   CUtensorMap mq, mq_thin, mk, mv;
   {
     const cuuint64_t dims[4] = {64, (cuuint64_t)s.n_q, (cuuint64_t)total_q, (cuuint64_t)(s.d_qk / 64)};
@@ -1315,7 +1392,13 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
-  const bool wide_first = thin_blocks == 0 || total_q > (long long)s.batch * pl.thin_max;
+  const bool wide_first = thin_blocks == 0 || total_q > (long long)s.batch * pl.thin_max || (range && range->groups > 0);
+  CUtensorMap mk_rows, mv_rows;  // of whole rows, for the kernels that take them
+  p.head_groups = (int)(tok_extent / 8);
+  p.k_rows = make_row_map(&mk_rows, c.k_cache, s.d_qk, tok_extent, s.n_k, c.num_blocks, c.k_stride_tok, c.k_stride_head,
+                          c.k_stride_blk, box_tok);
+  p.v_rows = make_row_map(&mv_rows, c.v_cache, s.d_v, tok_extent, s.n_v, c.num_blocks, c.v_stride_tok, c.v_stride_head,
+                          c.v_stride_blk, box_tok);
   auto launch_wide = [&]() -> cudaError_t {
     p.list = wide;
     p.first = wide_first;
@@ -1323,21 +1406,16 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
     cfg.blockDim = dim3(kExtendThreads);
     cfg.dynamicSmemBytes = kExtendSmem;
     cfg.numAttrs = wide_first ? 0 : 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, fn, mq, mk, mv, p);
+    const cudaError_t e = range ? cudaLaunchKernelEx(&cfg, fn, mq, p.k_rows ? mk_rows : mk, p.v_rows ? mv_rows : mv, p)
+                                : cudaLaunchKernelEx(&cfg, fn, mq, mk, mv, p);
     if (e == cudaSuccess) count_launch();
     return e;
   };
   auto launch_thin = [&]() -> cudaError_t {
     if (thin_blocks == 0) return cudaSuccess;
-    CUtensorMap mk_rows, mv_rows;
     p.list = thin;
     p.first = !wide_first;
     if (range) return launch_extend_few(mk_few, mv_few, q, p, s.d_qk, s.d_v, thin_blocks, wide_first, stream);
-    p.head_groups = (int)(tok_extent / 8);
-    p.k_rows = make_row_map(&mk_rows, c.k_cache, s.d_qk, tok_extent, s.n_k, c.num_blocks, c.k_stride_tok, c.k_stride_head,
-                            c.k_stride_blk, box_tok);
-    p.v_rows = make_row_map(&mv_rows, c.v_cache, s.d_v, tok_extent, s.n_v, c.num_blocks, c.v_stride_tok, c.v_stride_head,
-                            c.v_stride_blk, box_tok);
     return launch_extend_thin(mq_thin, p.k_rows ? mk_rows : mk, p.v_rows ? mv_rows : mv, p, s.d_qk, s.d_v, thin_blocks,
                               wide_first, stream);
   };

@@ -286,36 +286,139 @@ struct SeqOf<true> {
   __device__ int skip(const ExtendParams& p, int tok) const { return max(low(p, tok) / kKT - p.sink_tiles, 0); }
   // tiles of the cache up to the last one that rows before `tok` see
   __device__ int reach(const ExtendParams& p, int tok) const { return (min(past + tok, end) + kKT - 1) / kKT; }
+  // sum over x < count of floor((b + 2 T x) / 128), b >= 0
+  __device__ static int steps(const ExtendParams& p, int count, int b) {
+    const int whole = count * (b >> 7);
+    b &= kKT - 1;
+    if (p.t_log2 >= 0) return whole + (int)floor_sum_128(count, p.t_log2 + 1, b);
+    return whole + (int)floor_sum(count, kKT, 2 * p.T, b);
+  }
   // cost of the first i items, i < items
-  __device__ long long cost_before(const ExtendParams& p, int i) const {
+  __device__ int cost_before(const ExtendParams& p, int i) const {
     if (i == 0) return 0;
-    auto sum = [&](int count, int b) -> long long {
-      return p.t_log2 >= 0 ? floor_sum_128(count, p.t_log2 + 1, b) : floor_sum(count, kKT, 2 * p.T, b);
-    };
-    long long tiles = dst == kDstPrefix ? (long long)i * ((end + kKT - 1) / kKT) : sum(i, past + 2 * p.T + kKT - 1);
+    int tiles = dst == kDstPrefix ? i * ((end + kKT - 1) / kKT) : steps(p, i, past + 2 * p.T + kKT - 1);
     if (p.window == kNoWindow) {
-      tiles -= (long long)i * (start / kKT);
+      tiles -= i * (start / kKT);
     } else {  // item x skips max(0, floor((c + 2 T x) / 128)) tiles
       int c = past + 1 - p.window - p.sink_tiles * kKT, x0 = 0;
       if (c < 0) {
         x0 = (2 * p.T - 1 - c) / (2 * p.T);
-        c += (long long)x0 * 2 * p.T;
+        c += x0 * 2 * p.T;
       }
-      if (i > x0) tiles -= sum(i - x0, c);
+      if (i > x0) tiles -= steps(p, i - x0, c);
     }
-    return kWideCost * tiles + (long long)kItemCost * i;
+    return kWideCost * tiles + kItemCost * i;
   }
   __device__ bool wide(const ExtendParams& p, int i) const { return n - i * 2 * p.T > p.T; }
   __device__ int tiles(const ExtendParams& p, int i) const {  // K/V tiles of item i
     return reach(p, min(n, (i + 1) * 2 * p.T)) - skip(p, i * 2 * p.T);
   }
-  __device__ long long cost(const ExtendParams& p) const {  // of one head group
+  __device__ int cost(const ExtendParams& p) const {  // of one head group
     if (n == 0) return 0;
-    return cost_before(p, items - 1) + kItemCost + (wide(p, items - 1) ? kWideCost : kNarrowCost) * (long long)tiles(p, items - 1);
+    return cost_before(p, items - 1) + kItemCost + (wide(p, items - 1) ? kWideCost : kNarrowCost) * tiles(p, items - 1);
   }
 };
 template <bool kRanged>
 __device__ __forceinline__ int entries_of(const ExtendParams& p) { return kRanged ? p.entries : p.batch; }
+
+// Where a block of a ranged step begins.  What a block runs once at its start is fetched line by line, some 25 cycles an
+// instruction, so this is one short piece of code for both kernels, in 32-bit arithmetic (the host sees to it that both lists
+// stay below 2^31): with the plain steps' code a block of long chunks made its first request 16 us after its start.
+__device__ __forceinline__ uint32_t ranged_share_start(uint32_t total, uint32_t k, uint32_t n) {  // floor(total k / n)
+  const uint32_t q = total / n, r = total - q * n;
+  return q * k + r * k / n;
+}
+__device__ __forceinline__ int ranged_shares(uint32_t total, int n, int least) {  // see shares
+  return total >= (uint32_t)(n * least) ? n : max(1, (int)(total / (uint32_t)least));
+}
+__device__ __forceinline__ int ranged_wide_teams(const ExtendParams& p, uint32_t wide, uint32_t few) {  // see wide_teams
+  if (wide == 0) return 0;
+  int n = p.n_teams;
+  if (few > 0 && n > 1) {
+    const float w = (float)wide * p.team, f = (float)few * p.thin_weight;
+    n = min(max((int)(n * __fdividef(w, w + f) + 0.5f), 1), n - 1);
+  }
+  return ranged_shares(wide, n, kItemCost + kWideCost);
+}
+struct RangedStart {
+  uint32_t wide, few;        // lengths of the two lists
+  int first, busy;           // the thread's first entry and the threads that have few rows in theirs
+  bool single;               // no thread has more than one entry
+  uint32_t before_wide, before_few;  // of the lists, in front of the thread's entries
+};
+template <int kWarps>
+struct RangedScan {
+  unsigned long long sum[kWarps];
+  int busy[kWarps];
+  SeqOf<true> seq;  // of the block's first item: its entry, the entry's start in the list
+  int e;
+  uint32_t lo;
+};
+// Sums up both lists; `my` is the thread's first entry.  Holds a barrier, and report's that an entry does not fit.
+template <int kWarps>
+__device__ __forceinline__ RangedStart ranged_start(const ExtendParams& p, RangedScan<kWarps>& sc, SeqOf<true>& my, bool reports) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int per_thread = (p.entries + kWarps * 32 - 1) / (kWarps * 32);
+  RangedStart r;
+  r.single = per_thread == 1;
+  r.first = tid * per_thread;
+  uint32_t wide = 0, few = 0;
+  my.n = my.thin_tiles = 0;
+#pragma unroll 1
+  for (int i = per_thread - 1; i >= 0; --i) {
+    if (r.first + i >= p.entries) continue;
+    my.load(p, r.first + i);
+    if (my.bad && reports) report(p.dev_status, DIFFQKV_ERR_INDEX);
+    if (my.thin_tiles > 0) few += p.n_units * (my.thin_tiles + kFewItemCost);
+    if (my.n > 0) wide += p.n_units * (uint32_t)my.cost(p);
+  }
+  const unsigned long long mine = (unsigned long long)wide << 32 | few;
+  unsigned long long x = mine;
+#pragma unroll 1
+  for (int o = 1; o < 32; o <<= 1) {
+    const unsigned long long y = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += y;
+  }
+  const int busy = __popc(__ballot_sync(0xffffffffu, few > 0));
+  if (lane == 31) {
+    sc.sum[warp] = x;
+    sc.busy[warp] = busy;
+  }
+  __syncthreads();
+  unsigned long long before = x - mine, all = 0;
+  r.busy = 0;
+#pragma unroll 1
+  for (int w = 0; w < kWarps; ++w) {
+    if (w < warp) before += sc.sum[w];
+    all += sc.sum[w];
+    r.busy += sc.busy[w];
+  }
+  r.wide = (uint32_t)(all >> 32);
+  r.few = (uint32_t)all;
+  r.before_wide = (uint32_t)(before >> 32);
+  r.before_few = (uint32_t)before;
+  return r;
+}
+// The thread that has place w0 of a list among its entries, which begin at `before`, leaves the entry there.  cost: an entry's
+// length in the list.
+template <int kWarps, typename F>
+__device__ __forceinline__ void ranged_seek(const ExtendParams& p, RangedScan<kWarps>& sc, const RangedStart& r, SeqOf<true>& my,
+                                            uint32_t w0, uint32_t before, F cost) {
+  const int per_thread = (p.entries + kWarps * 32 - 1) / (kWarps * 32);
+#pragma unroll 1
+  for (int i = 0; i < per_thread && r.first + i < p.entries; ++i) {
+    if (before > w0) break;
+    if (!r.single) my.load(p, r.first + i);
+    const uint32_t c = cost(my);
+    if (before <= w0 && w0 - before < c) {
+      sc.seq = my;
+      sc.e = r.first + i;
+      sc.lo = before;
+      break;
+    }
+    before += c;
+  }
+}
 
 // Teams that the list of long chunks is divided over; the thin sequences have the other SMs, so that neither kernel waits
 // for the other (one thread block of either fits an SM): what a step of both kinds saves is one start, one end and one

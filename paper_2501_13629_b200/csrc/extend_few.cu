@@ -28,13 +28,9 @@ namespace {
 
 constexpr int kWarps = 8, kThreads = (kWarps + 1) * 32;
 constexpr int kMaxStages = 8;
-constexpr int kCached = 32;  // entries of a block's share kept in shared memory
 constexpr float kFewThreshold = 8.f;  // log2 domain
 constexpr int kMaxSmem = 232448;
 
-struct FewEntry {
-  int lo, n, past, end, start, tab, dst, nt;
-};
 struct FewSegment {  // as the producer hands it to the other warps, through a ring in shared memory
   int lo, n, past, end, start;  // see SeqOf
   int low, skip;                // first token behind the sinks that the first row sees; tiles skipped in front of it
@@ -46,13 +42,10 @@ template <int kD>
 struct Scratch {
   float4 o[4][kD / 8][32];  // accumulators handed from warp to warp, a register of all lanes behind one another
   float2 ml[4][16];         // their rows' reference and sum
-  FewEntry entry[kCached];  // from the share's first entry on
-  long long total[2][kWarps + 1];
-  int busy[kWarps + 1], longs[kWarps + 1];
+  RangedScan<kWarps + 1> scan;
+  uint32_t chunks[kWarps + 1];
   uint64_t full[kMaxStages], empty[kMaxStages], seg_full[kSegRing], seg_empty[kSegRing];
   FewSegment seg[kSegRing];
-  long long seek_lo;
-  int seek_e;
   int abort;
 };
 
@@ -80,25 +73,6 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     return;
   }
   if (p.first) ptx::grid_launch_dependents();
-  using Seq = SeqOf<true>;
-  // ---- this block's share of the list: every thread sums up the tiles of its entries
-  const int per_thread = (p.entries + kThreads - 1) / kThreads;
-  const int e_lo = min(tid * per_thread, p.entries), e_hi = min(e_lo + per_thread, p.entries);
-  Seq my = {};  // the thread's first entry: there is seldom another
-  long long mine = 0, others = 0;  // others: the list of long chunks
-  bool any_long = false;
-  {
-    Seq s;
-    for (int e = e_lo; e < e_hi; ++e) {
-      s.load(p, e);
-      if (e == e_lo) my = s;
-      if (s.thin_tiles > 0) mine += (long long)p.n_units * (s.thin_tiles + kItem);
-      if (s.n > 0) {
-        others += p.n_units * s.cost(p);
-        any_long = true;
-      }
-    }
-  }
   if (tid < kMaxStages + kSegRing) {  // full and empty, of the stages and behind them of the segments
     const bool seg = tid >= kMaxStages;
     ptx::mbar_init(seg ? seg_full0 + 8 * (tid - kMaxStages) : full0 + 8 * tid, 1);
@@ -110,74 +84,47 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     ptx::prefetch_tmap(&tmap_k);
     ptx::prefetch_tmap(&tmap_v);
   }
-  auto scan = [&](long long x, int which) -> long long {  // inclusive over the warp; the warp's sum to shared memory
-#pragma unroll 1
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long y = __shfl_up_sync(0xffffffffu, x, o);
-      if (lane >= o) x += y;
-    }
-    if (lane == 31) sc.total[which][warp] = x;
-    return x;
-  };
-  auto before_warp = [&](int which, long long& all) -> long long {
-    long long before = 0;
-    all = 0;
-#pragma unroll 1
-    for (int w = 0; w <= kWarps; ++w) {
-      if (w < warp) before += sc.total[which][w];
-      all += sc.total[which][w];
-    }
-    return before;
-  };
-  long long before = scan(mine, 0) - mine, total;
-  {
-    const int busy = __popc(__ballot_sync(0xffffffffu, mine > 0)), longs = __any_sync(0xffffffffu, any_long);
-    if (lane == 0) {
-      sc.busy[warp] = busy;
-      sc.longs[warp] = longs;
-    }
-  }
-  __syncthreads();
-  before += before_warp(0, total);
-  int busy = 0, longs = 0;
-#pragma unroll 1
-  for (int w = 0; w <= kWarps; ++w) {
-    busy += sc.busy[w];
-    longs |= sc.longs[w];
-  }
-  int grid = p.blocks;
-  if (longs) {
-    scan(others, 1);
-    __syncthreads();
-    before_warp(1, others);
-    __syncthreads();
-    grid = thin_blocks_left(p, wide_teams(p, others, total));  // what the other kernel leaves
-  }
+  // ---- this block's share of the list
+  using Seq = SeqOf<true>;
+  Seq my;
+  const RangedStart at = ranged_start(p, sc.scan, my, false);
+  const uint32_t total = at.few;
   // Equal shares of the list, cut wherever they end; or, where that costs no block more than six tiles, equal chunks that
   // begin with their item (see extend_thin.cu), so that every block has one segment at most.
-  int chunk = 0;
-  const int items = per_thread == 1 ? min(busy * p.n_units, grid) : grid;
-  if (items < grid && total < (1ll << 22)) {
-    const uint32_t tiles = (uint32_t)total - items * kItem;
-    chunk = (int)((tiles + grid - items - 1) / (grid - items));
-    if (chunk > (int)(tiles / grid) + 6) chunk = 0;
-  }
-  int blocks = 0;  // that take part
-  long long w0 = total, w1 = total;
+  const int grid = at.wide == 0 ? p.blocks : thin_blocks_left(p, ranged_wide_teams(p, at.wide, total));  // what the other kernel leaves
+  int chunk = 0, blocks = 0;  // blocks: that take part
+  uint32_t w0 = 0, w1 = 0, before = at.before_few;
   if (total > 0 && (int)blockIdx.x < grid) {
-    if (chunk > 0) {
-      long long chunks;
-      mine = (long long)p.n_units * ((my.thin_tiles + chunk - 1) / chunk);
-      before = scan(mine, 1) - mine;
+    const int items = at.single ? min(at.busy * p.n_units, grid) : grid;
+    if (items < grid) {
+      const uint32_t tiles = total - items * kItem;
+      chunk = (int)((tiles + grid - items - 1) / (uint32_t)(grid - items));
+      if (chunk > (int)(tiles / (uint32_t)grid) + 6) chunk = 0;
+    }
+    if (chunk > 0) {  // the list of chunks instead
+      uint32_t x = p.n_units * ((uint32_t)(my.thin_tiles + chunk - 1) / (uint32_t)chunk);
+      const uint32_t mine = x;
+#pragma unroll 1
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+      }
+      if (lane == 31) sc.chunks[warp] = x;
       __syncthreads();
-      before += before_warp(1, chunks);
+      uint32_t all = 0;
+      before = x - mine;
+#pragma unroll 1
+      for (int w = 0; w <= kWarps; ++w) {
+        if (w < warp) before += sc.chunks[w];
+        all += sc.chunks[w];
+      }
       w0 = blockIdx.x;
-      w1 = w0 < chunks ? w0 + 1 : w0;
+      w1 = w0 < all ? w0 + 1 : w0;
     } else {
-      blocks = shares(total, grid, kItem + 1);
+      blocks = ranged_shares(total, grid, kItem + 1);
       if ((int)blockIdx.x < blocks) {
-        w0 = share_start(total, blockIdx.x, blocks);
-        w1 = share_start(total, blockIdx.x + 1, blocks);
+        w0 = ranged_share_start(total, blockIdx.x, blocks);
+        w1 = ranged_share_start(total, blockIdx.x + 1, blocks);
       }
     }
   }
@@ -186,31 +133,11 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     ptx::grid_dependency_wait();
     return;
   }
-  auto pack = [](const Seq& s) -> FewEntry { return {s.lo, s.rows, s.past, s.end, s.start, s.tab, s.dst, s.thin_tiles}; };
-  if (before <= w0 && w0 < before + mine) {
-    Seq s = my;
-    for (int e = e_lo;;) {
-      const int nt = s.thin_tiles;
-      const long long c = nt == 0 ? 0 : (long long)p.n_units * (chunk > 0 ? (nt + chunk - 1) / chunk : nt + kItem);
-      if (w0 < before + c) {
-        sc.seek_e = e;
-        sc.seek_lo = before;
-        sc.entry[0] = pack(s);
-        break;
-      }
-      before += c;
-      s.load(p, ++e);
-    }
-  }
+  ranged_seek(p, sc.scan, at, my, w0, before, [&](const Seq& s) -> uint32_t {
+    if (s.thin_tiles == 0) return 0;
+    return p.n_units * (uint32_t)(chunk > 0 ? (s.thin_tiles + chunk - 1) / chunk : s.thin_tiles + kItem);
+  });
   __syncthreads();
-  if (chunk == 0) {
-    const int e0 = sc.seek_e;
-    for (int e = max(e_lo, e0 + 1); e < min(e_hi, e0 + kCached); ++e) {
-      if (e != e_lo) my.load(p, e);
-      sc.entry[e - e0] = pack(my);
-    }
-    __syncthreads();
-  }
 
   const int bt_shift = 31 - __clz(p.box_tok);
   int stage = 0;
@@ -231,32 +158,25 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     int count = 0, segs = 0;
     bool ok = true;
     ExtendMeta m = {};
-    int e = sc.seek_e, u, chunk_lo = 0;
-    FewEntry x = sc.entry[0];
-    long long item_lo = sc.seek_lo;
-    if (chunk > 0) {
-      const int per = (x.nt + chunk - 1) / chunk, in = (int)(w0 - item_lo);
-      u = (int)((uint32_t)in / (uint32_t)per);
-      chunk_lo = (in - u * per) * chunk;
-    } else {
-      u = (int)quotient(w0 - item_lo, x.nt + kItem);
-      item_lo += (long long)u * (x.nt + kItem);
+    int e = sc.scan.e, u, chunk_lo = 0;
+    Seq x = sc.scan.seq;
+    int nt = x.thin_tiles;
+    uint32_t item_lo = sc.scan.lo;
+    {
+      const uint32_t in = w0 - item_lo, per = chunk > 0 ? (nt + chunk - 1) / chunk : nt + kItem;
+      u = (int)(in / per);
+      if (chunk > 0) chunk_lo = (int)(in - u * per) * chunk;
+      else item_lo += u * per;
     }
     auto next_item = [&]() {
-      item_lo += x.nt + kItem;
-      if (++u < p.n_units) return;
+      item_lo += nt + kItem;
+      if (item_lo >= w1 || ++u < p.n_units) return;
       u = 0;
       do {
         if (++e >= p.entries) return;
-        const int at = e - sc.seek_e;
-        if (at < kCached) {
-          x = sc.entry[at];
-        } else {
-          Seq s;
-          s.load(p, e);
-          x = pack(s);
-        }
-      } while (x.nt == 0);
+        x.load(p, e);
+        nt = x.thin_tiles;
+      } while (nt == 0);
     };
     auto hand_out = [&](const FewSegment& d, volatile int* abort) -> bool {
       const int at = segs % kSegRing;
@@ -273,26 +193,26 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       int ta, tb;
       if (chunk > 0) {
         ta = chunk_lo;
-        tb = min(x.nt, chunk_lo + chunk);
+        tb = min(nt, chunk_lo + chunk);
       } else {
-        ta = item_tile(w0 - item_lo, 1, x.nt, kItem);
-        tb = item_tile(w1 - item_lo, 1, x.nt, kItem);
+        ta = w0 > item_lo ? item_tile(w0 - item_lo, 1, nt, kItem) : 0;
+        tb = item_tile(w1 - item_lo, 1, nt, kItem);
         if (ta >= tb) {  // the share begins, or ends, within the item's own cost
           next_item();
           continue;
         }
       }
-      const int low = max(x.start, x.past + 1 - p.window), skip = max(low / kFewT - p.sink_few, 0);
+      const int low = max(x.low(p, 0), 0), skip = x.skip_few(p);
       const int head0 = u * p.parts * p.G, hk0 = head0 / p.heads_per_k, hv0 = head0 / p.heads_per_v;  // Eq. (idx)
-      if (!hand_out({x.lo, x.n, x.past, x.end, x.start, low, skip, u, ta, tb, x.dst,
-                     (ta == 0 ? kSegFirst : 0) | (ta == 0 && tb == x.nt ? kSegWhole : 0)}, abort_flag)) {
+      if (!hand_out({x.lo, x.rows, x.past, x.end, x.start, low, skip, u, ta, tb, x.dst,
+                     (ta == 0 ? kSegFirst : 0) | (ta == 0 && tb == nt ? kSegWhole : 0)}, abort_flag)) {
         ok = false;
         break;
       }
-      if (ta == 0 && tb < x.nt) {
-        m.rows = p.parts * x.n * p.G; m.part_rows = x.n * p.G; m.row_lo = x.lo; m.head0 = head0; m.dst = x.dst;
-        m.parts = chunk > 0 ? (x.nt + chunk - 1) / chunk
-                            : share_of(item_lo + last_tile(1, x.nt, kItem), total, blocks) - (int)blockIdx.x + 1;
+      if (ta == 0 && tb < nt) {
+        m.rows = p.parts * x.rows * p.G; m.part_rows = x.rows * p.G; m.row_lo = x.lo; m.head0 = head0; m.dst = x.dst;
+        m.parts = chunk > 0 ? (nt + chunk - 1) / chunk
+                            : share_of((long long)item_lo + last_tile(1, nt, kItem), total, blocks) - (int)blockIdx.x + 1;
       }
       auto token_of = [&](int tile) -> int { return ((tile >= p.sink_few ? tile + skip : tile) << 6) + my_part * p.box_tok; };
       auto wanted = [&](int tok) -> bool { return tok < x.end && (tok < p.sinks || tok + p.box_tok > low); };
