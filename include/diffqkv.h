@@ -377,13 +377,15 @@ diffqkv_status diffqkv_extend(const void *q, const int32_t *cu_q, int32_t total_
  * diffqkv_extend_window -- diffqkv_extend for a layer with a sliding window and a few first tokens that stay visible: row i
  * of sequence b, at position p = past_b + i, sees the tokens j <= p with j > p - window or j < sinks.
  *   window  >= 1: tokens of the window, the row's own among them       sinks  >= 0: first tokens that every row sees
- * Everything else, the workspace and its size included, as diffqkv_extend.  Work and traffic go by the tokens seen, not by
+ *   workspace  diffqkv_extend_window_workspace_bytes(shape, total_q) bytes, 256-byte aligned
+ * Everything else as diffqkv_extend.  Work and traffic go by the tokens seen, not by
  * the tokens cached.  Pages that hold no token which a row of the step sees are not read: they may have been given back, and
  * their table entries may be -1.  (Positions go on counting; diffqkv_pages_free gives back ends, not middles, so a caller who
  * frees pages behind the window lowers their counts and sets their entries itself.)  A weight of zero multiplies the V rows
  * of tokens that another row of the same chunk sees; those must be finite, all others may hold anything.
  * A window that reaches back over the whole cache (window + sinks >= max_seqlen) is diffqkv_extend itself.
  */
+size_t diffqkv_extend_window_workspace_bytes(const diffqkv_shape *shape, int32_t total_q);
 diffqkv_status diffqkv_extend_window(const void *q, const int32_t *cu_q, int32_t total_q, int32_t window, int32_t sinks,
                                      const diffqkv_cache *cache, const diffqkv_shape *shape, void *workspace,
                                      size_t workspace_bytes, void *out, float *lse, int32_t *dev_status, void *stream);

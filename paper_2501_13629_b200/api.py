@@ -40,7 +40,7 @@ EXPORTS = (
     "diffqkv_pages_free", "diffqkv_pages_fork", "diffqkv_pages_fork_workspace_bytes", "diffqkv_pages_reserve",
     "diffqkv_pages_reserve_workspace_bytes", "diffqkv_pages_copy", "diffqkv_pages_compact",
     "diffqkv_pages_compact_workspace_bytes", "diffqkv_debug_extend_kernel", "diffqkv_last_extend_kernel",
-    "diffqkv_extend_window", "diffqkv_extend_shared", "diffqkv_extend_shared_workspace_bytes", "diffqkv_norm_rope_append",
+    "diffqkv_extend_window", "diffqkv_extend_window_workspace_bytes", "diffqkv_extend_shared", "diffqkv_extend_shared_workspace_bytes", "diffqkv_norm_rope_append",
 )
 
 
@@ -167,6 +167,7 @@ _S, _V, _I, _L, _Z = C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
 for _name, _res, _args in (
         ("diffqkv_extend_workspace_bytes", _Z, [_S, _I]),
         ("diffqkv_extend", C.c_int, [_V, _V, _I, _S, _S, _V, _Z, _V, _V, _V, _V]),
+        ("diffqkv_extend_window_workspace_bytes", _Z, [_S, _I]),
         ("diffqkv_extend_window", C.c_int, [_V, _V, _I, _I, _I, _S, _S, _V, _Z, _V, _V, _V, _V]),
         ("diffqkv_extend_shared_workspace_bytes", _Z, [_S, _I]),
         ("diffqkv_extend_shared", C.c_int, [_V, _V, _I, _S, _S, _S, _V, _Z, _V, _V, _V, _V]),
@@ -771,6 +772,10 @@ def diffqkv_extend(q: torch.Tensor, cu_q: torch.Tensor, cache: KVCache, n_k: int
                    out, lse, dev_status, out_dtype, stream)
 
 
+def diffqkv_extend_window_workspace_bytes(shape: ShapeStruct, total_q: int) -> int:
+    return int(_lib.diffqkv_extend_window_workspace_bytes(C.byref(shape), int(total_q)))
+
+
 def diffqkv_extend_window(q: torch.Tensor, cu_q: torch.Tensor, cache: KVCache, n_k: int, n_v: int, scale: float,
                           window: int, sinks: int = 0, workspace: Optional[torch.Tensor] = None,
                           out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
@@ -778,8 +783,8 @@ def diffqkv_extend_window(q: torch.Tensor, cu_q: torch.Tensor, cache: KVCache, n
                           stream: Optional[torch.cuda.Stream] = None):
     """diffqkv_extend in which a row sees the last ``window`` tokens up to its own and the first ``sinks`` ones.  Pages
     that hold no token which a row sees need not exist (entry -1)."""
-    return _extend("diffqkv_extend_window", (window, sinks), _raw.diffqkv_extend_workspace_bytes, q, cu_q, cache, n_k, n_v,
-                   scale, workspace, out, lse, dev_status, out_dtype, stream)
+    return _extend("diffqkv_extend_window", (window, sinks), _raw.diffqkv_extend_window_workspace_bytes, q, cu_q, cache, n_k,
+                   n_v, scale, workspace, out, lse, dev_status, out_dtype, stream)
 
 
 def diffqkv_extend_shared_workspace_bytes(shape: ShapeStruct, total_q: int) -> int:

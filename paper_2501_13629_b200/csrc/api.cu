@@ -448,11 +448,11 @@ int32_t diffqkv_last_extend_kernel(void) { return g_last_extend_kernel; }
 
 size_t diffqkv_extend_workspace_bytes(const diffqkv_shape* shape, int32_t total_q) {
   if (check_shape(shape) != DIFFQKV_OK || total_q < 0) return 0;
-  return extend_workspace_bytes(*shape, total_q);
+  return extend_workspace_bytes(*shape, total_q, false);
 }
 
 static size_t extend_need(const diffqkv_shape& s, int32_t total_q, const ExtendRange* range) {
-  return extend_workspace_bytes(s, total_q) + (range && range->groups > 0 ? extend_groups_workspace_bytes(s, total_q) : 0);
+  return extend_workspace_bytes(s, total_q, range != nullptr) + (range && range->groups > 0 ? extend_groups_workspace_bytes(s, total_q) : 0);
 }
 
 // diffqkv_extend and its ranged forms.
@@ -488,7 +488,7 @@ static diffqkv_status extend_impl(const void* q, const int32_t* cu_q, int32_t to
   p.o_partial = nullptr; p.lse_partial = nullptr;
   p.dev_status = dev_status;
   if (range && range->groups > 0) {  // FMAs bound these kernels, not the cache: every sequence reads all of its own
-    int* lengths = reinterpret_cast<int*>(static_cast<char*>(workspace) + extend_workspace_bytes(*shape, total_q));
+    int* lengths = reinterpret_cast<int*>(static_cast<char*>(workspace) + extend_workspace_bytes(*shape, total_q, true));
     if (launch_extend_lengths(cu_q, total_q, *cache, shape->batch, *range, lengths, stream) != cudaSuccess) return DIFFQKV_ERR_CUDA;
     p.cache.seqlens = lengths;
     range = nullptr;
@@ -506,6 +506,11 @@ diffqkv_status diffqkv_extend(const void* q, const int32_t* cu_q, int32_t total_
                               int32_t* dev_status, void* stream) {
   return extend_impl(q, cu_q, total_q, cache, shape, nullptr, workspace, workspace_bytes, out, lse, dev_status,
                      static_cast<cudaStream_t>(stream));
+}
+
+size_t diffqkv_extend_window_workspace_bytes(const diffqkv_shape* shape, int32_t total_q) {
+  if (check_shape(shape) != DIFFQKV_OK || total_q < 0) return 0;
+  return extend_workspace_bytes(*shape, total_q, true);
 }
 
 diffqkv_status diffqkv_extend_window(const void* q, const int32_t* cu_q, int32_t total_q, int32_t window, int32_t sinks,
@@ -533,7 +538,7 @@ static diffqkv_status range_of(const diffqkv_prefixes* prefixes, ExtendRange* ra
 
 size_t diffqkv_extend_shared_workspace_bytes(const diffqkv_shape* shape, int32_t total_q) {
   if (check_shape(shape) != DIFFQKV_OK || total_q < 0) return 0;
-  return extend_workspace_bytes(*shape, total_q) + extend_groups_workspace_bytes(*shape, total_q);
+  return extend_workspace_bytes(*shape, total_q, true) + extend_groups_workspace_bytes(*shape, total_q);
 }
 
 diffqkv_status diffqkv_extend_shared(const void* q, const int32_t* cu_q, int32_t total_q, const diffqkv_prefixes* prefixes,

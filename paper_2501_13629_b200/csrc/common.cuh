@@ -208,7 +208,7 @@ struct ExtendRange {
   const int* cu_groups;
   const int* prefix_lens;
 };
-size_t extend_workspace_bytes(const diffqkv_shape& s, int total_q);
+size_t extend_workspace_bytes(const diffqkv_shape& s, int total_q, bool ranged);
 size_t extend_groups_workspace_bytes(const diffqkv_shape& s, int total_q);  // on top of that
 cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const diffqkv_cache& c, const diffqkv_shape& s,
                           const ExtendRange* range, void* workspace, void* out, float* lse, int* dev_status,

@@ -265,6 +265,14 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
     }
   };
   if constexpr (kRanged) {
+    // a step of a few rows each (decode): most blocks leave here, in a third of the time that the sums below take
+    bool any = blockIdx.x == 0;  // which reports the entries that do not fit
+    for (int e = tid; e < p.entries; e += kExtendThreads) any |= long_entry(p, e);
+    if (!__syncthreads_or(any)) {
+      if (tid == 0) p.list.meta[blockIdx.x].rows = 0;
+      ptx::grid_dependency_wait();
+      return;
+    }
     init();
     tc::fence_before_sync();
     SeqOf<true> my;
@@ -1202,8 +1210,9 @@ int sm_count() {
 }
 
 // Head groups, rows per tile and teams; the same for the workspace's size and the launch.
-Plan make_plan(const diffqkv_shape& s, int total_q) {
+Plan make_plan(const diffqkv_shape& s, int total_q, bool ranged) {
   Plan pl;
+  const int columns = ranged ? kFewCols : kThinCols;
   const int per_k = s.n_q / s.n_k, per_v = s.n_q / s.n_v;
   int G = std::gcd(per_k, per_v);
   const bool nested = G == per_k || G == per_v;  // one kind of head groups lies within the other
@@ -1220,7 +1229,7 @@ Plan make_plan(const diffqkv_shape& s, int total_q) {
   int parts = share < 4 ? share : 4;
   while (share % parts != 0 || pl.groups % parts != 0) --parts;
   pl.parts = parts;
-  pl.region = parts == 1 ? kThinCols : (parts == 2 ? kThinCols / 2 : kThinCols / 4);
+  pl.region = parts == 1 ? columns : (parts == 2 ? columns / 2 : columns / 4);
   pl.thin_max = pl.region / G;
   pl.blocks = sm_count();
   pl.n_teams = pl.blocks / parts;
@@ -1270,9 +1279,9 @@ bool dims_supported(const diffqkv_shape& s) {
 
 }  // namespace
 
-size_t extend_workspace_bytes(const diffqkv_shape& s, int total_q) {
+size_t extend_workspace_bytes(const diffqkv_shape& s, int total_q, bool ranged) {
   const size_t simt = extend_simt_workspace_bytes(s, total_q);  // a cache may turn out to have no tensor map
-  const size_t need = dims_supported(s) ? place(make_plan(s, total_q), s.d_v, nullptr, nullptr, nullptr) : 256;
+  const size_t need = dims_supported(s) ? place(make_plan(s, total_q, ranged), s.d_v, nullptr, nullptr, nullptr) : 256;
   return need > simt ? need : simt;
 }
 
@@ -1307,7 +1316,7 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
       box_tok = c.page_size;
     }
   }
-  const Plan pl = make_plan(s, total_q);
+  const Plan pl = make_plan(s, total_q, range != nullptr);
   if (range) {  // both lists in 32 bits; see ranged_start
     const long long entries = (long long)range->groups + s.batch, units = pl.groups / pl.parts;
     const long long items = total_q / (2 * pl.T) * (range->groups > 0 ? 2LL : 1LL) + entries;
@@ -1322,14 +1331,16 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
     const cuuint32_t box[4] = {64, (cuuint32_t)pl.G, (cuuint32_t)pl.T, 1};
     const cuuint32_t thin[4] = {64, (cuuint32_t)pl.G, (cuuint32_t)pl.thin_max, 1};
     if (!make_tmap_bf16_sw128(&mq, q, 4, dims, strides, box)) return cudaErrorNotSupported;
-    if (pl.thin_max > 0 && !make_tmap_bf16_sw128(&mq_thin, q, 4, dims, strides, thin)) return cudaErrorNotSupported;
+    if (!range && pl.thin_max > 0 && !make_tmap_bf16_sw128(&mq_thin, q, 4, dims, strides, thin)) return cudaErrorNotSupported;
   }
   const long long tok_extent = c.page_table ? c.page_size : c.max_seqlen;
-  if (!make_cache_map(&mk, c.k_cache, s.d_qk, tok_extent, s.n_k, c.num_blocks, c.k_stride_tok, c.k_stride_head,
-                      c.k_stride_blk, box_tok) ||
-      !make_cache_map(&mv, c.v_cache, s.d_v, tok_extent, s.n_v, c.num_blocks, c.v_stride_tok, c.v_stride_head,
-                      c.v_stride_blk, box_tok))
-    return cudaErrorNotSupported;
+  auto cache_maps = [&]() -> bool {
+    return make_cache_map(&mk, c.k_cache, s.d_qk, tok_extent, s.n_k, c.num_blocks, c.k_stride_tok, c.k_stride_head,
+                          c.k_stride_blk, box_tok) &&
+           make_cache_map(&mv, c.v_cache, s.d_v, tok_extent, s.n_v, c.num_blocks, c.v_stride_tok, c.v_stride_head,
+                          c.v_stride_blk, box_tok);
+  };
+  if (!range && !cache_maps()) return cudaErrorNotSupported;
   CUtensorMap mk_few, mv_few;
   if (range && (!make_pool_map(&mk_few, c.k_cache, s.d_qk, tok_extent, s.n_k, c.num_blocks, c.k_stride_tok, c.k_stride_head,
                                c.k_stride_blk, box_tok < kFewT ? box_tok : kFewT) ||
@@ -1370,7 +1381,7 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
     p.sink_few = (int)(((long long)range->sinks + kFewT - 1) / kFewT);
     p.groups = range->groups; p.entries = range->groups + s.batch;
     p.cu_groups = range->cu_groups; p.prefix_lens = range->prefix_lens;
-    if (p.groups > 0) place_buffers(s, total_q, static_cast<char*>(workspace) + extend_workspace_bytes(s, total_q), p.buffer);
+    if (p.groups > 0) place_buffers(s, total_q, static_cast<char*>(workspace) + extend_workspace_bytes(s, total_q, true), p.buffer);
   }
   const int thin_blocks = pl.thin_max > 0 ? pl.blocks : 0, blocks = pl.n_teams * pl.parts;
 
@@ -1399,6 +1410,7 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
                           c.k_stride_blk, box_tok);
   p.v_rows = make_row_map(&mv_rows, c.v_cache, s.d_v, tok_extent, s.n_v, c.num_blocks, c.v_stride_tok, c.v_stride_head,
                           c.v_stride_blk, box_tok);
+  if (range && (!p.k_rows || !p.v_rows) && !cache_maps()) return cudaErrorNotSupported;
   auto launch_wide = [&]() -> cudaError_t {
     p.list = wide;
     p.first = wide_first;

@@ -126,6 +126,7 @@ constexpr int kWideCost = 2, kNarrowCost = 1, kItemCost = 5;
 constexpr int kThinItemCost = 5;
 // The ranged steps' few rows go by tiles of 64 tokens; an item costs about two of them more.
 constexpr int kFewT = 64, kFewItemCost = 2;
+constexpr int kFewCols = 128;  // as kThinCols
 
 // sum of floor((a x + b) / m) for x = 0 .. n - 1 with a, b >= 0, m > 0: the Euclid-like recursion on (m, a).  Not inlined:
 // the code that a block runs once at its start is fetched from the second-level cache line by line, which is what it
@@ -320,6 +321,16 @@ struct SeqOf<true> {
 };
 template <bool kRanged>
 __device__ __forceinline__ int entries_of(const ExtendParams& p) { return kRanged ? p.entries : p.batch; }
+
+// Whether an entry of a ranged step is for the kernel of long chunks, if it fits.
+__device__ __forceinline__ bool long_entry(const ExtendParams& p, int x) {
+  int lo, hi;
+  if (x < p.groups) {
+    int first, prefix;
+    return group_rows(p, x, lo, hi, first, prefix) && prefix > 0 && hi - lo > p.thin_max;
+  }
+  return p.cu_q[x - p.groups + 1] - p.cu_q[x - p.groups] > p.thin_max;
+}
 
 // Where a block of a ranged step begins.  What a block runs once at its start is fetched line by line, some 25 cycles an
 // instruction, so this is one short piece of code for both kernels, in 32-bit arithmetic (the host sees to it that both lists

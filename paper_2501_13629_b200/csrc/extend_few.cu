@@ -277,8 +277,8 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       }
       if (w.flags & kSegEnd) break;
       const int used = w.n * p.G;                                            // rows of a head group
-      const int blocks16 = (used + 15) >> 4, all16 = p.parts * blocks16;     // at most 4
-      const int mshift = all16 > 2 ? 2 : all16 - 1, slices = kWarps >> mshift;
+      const int blocks16 = (used + 15) >> 4, all16 = p.parts * blocks16;     // at most 8
+      const int mshift = all16 > 1 ? 32 - __clz(all16 - 1) : 0, slices = kWarps >> mshift;
       const int mt = warp & ((1 << mshift) - 1), slice = warp >> mshift;
       const int group = mt / blocks16, r0 = (mt - group * blocks16) << 4;
       const bool active = mt < all16;
@@ -311,15 +311,21 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       const uint32_t k_off = (p.k_parts > 1 ? group : 0) * kKBytes;
       const uint32_t v_off = p.k_parts * kKBytes + (p.v_parts > 1 ? group : 0) * kVBytes;
       const int low = w.low, end = w.end, tb = w.tb;
-      // The slices of a row group: two take the halves of a tile each, four or eight every second or fourth tile.
-      const int r = (slice & 1) * 32, turn = slice >> 1, turns = (slices >> 1) - 1;
+      // The slices of a row group: one takes both halves of a tile, two one each, four or eight those of every second or
+      // fourth tile.
+      const int half0 = (slice & 1) * 32, halves = slices == 1 ? 64 : half0 + 32;
+      const int turn = slice >> 1, turns = slices > 1 ? (slices >> 1) - 1 : 0;
 #pragma unroll 1
       for (int i = w.ta; i < tb; ++i) {
         if (!dead && !wait_warp(full0 + 8 * stage, phase, abort_flag)) dead = true;
-        const int t0 = ((i >= p.sink_few ? i + w.skip : i) << 6) + r;  // first of the warp's 32 tokens
+        const int k0 = (i >= p.sink_few ? i + w.skip : i) << 6;
         const uint32_t base = ring + stage * stage_bytes;
-        const bool edge = t0 + 32 > end || (t0 < low && t0 + 32 > p.sinks);  // some are seen by no row
-        if (active && !dead && ((i - w.ta) & turns) == turn && t0 < end && (t0 + 32 > low || t0 < p.sinks)) {
+        const bool mine = active && !dead && ((i - w.ta) & turns) == turn;
+#pragma unroll 1
+        for (int r = half0; r < halves; r += 32) {
+          const int t0 = k0 + r;  // first of 32 tokens
+          if (!mine || t0 >= end || (t0 + 32 <= low && t0 >= p.sinks)) continue;  // the same for the whole warp
+          const bool edge = t0 + 32 > end || (t0 < low && t0 + 32 > p.sinks);     // some are seen by no row
           // ---- scores
           float s[4][4];
 #pragma unroll

@@ -163,7 +163,7 @@ def test_nan_in_what_a_row_sees_stays_with_it(api):
 def test_repeats_bit_for_bit_and_with_any_workspace(api):
     step = forget(Step(api, [3000, 10, 700], [2, 1, 600], 32, 4, 8, 128, 128, seed=5).fill(), 900, 4)
     first, lse = run(api, step, 900, 4)
-    nbytes = api.diffqkv_extend_workspace_bytes(api.make_shape(3, 32, 4, 8, 128, 128, BF16, BF16, 1.0), step.total_q)
+    nbytes = api.diffqkv_extend_window_workspace_bytes(api.make_shape(3, 32, 4, 8, 128, 128, BF16, BF16, 1.0), step.total_q)
     for fill in (0, 255):
         ws = torch.full((nbytes,), fill, dtype=torch.uint8, device="cuda")
         again, lse2 = run(api, step, 900, 4, workspace=ws)
@@ -219,7 +219,7 @@ def test_a_captured_step_replays_with_other_lengths(api):
     table = torch.zeros((4, row), dtype=torch.int32, device="cuda")
     lens, cu, status = ints([0] * 4), ints([0] * 5), ints([0])
     cache = api.KVCache(k, v, lens, row * 16, page_table=table, page_size=16)
-    ws = torch.empty(api.diffqkv_extend_workspace_bytes(api.make_shape(4, 8, 2, 4, 64, 64, BF16, BF16, 1.0), cap),
+    ws = torch.empty(api.diffqkv_extend_window_workspace_bytes(api.make_shape(4, 8, 2, 4, 64, 64, BF16, BF16, 1.0), cap),
                      dtype=torch.uint8, device="cuda")
     call = lambda: api.diffqkv_extend_window(q, cu, cache, 2, 4, 0.1, 250, sinks=20, out=out, workspace=ws,  # noqa: E731
                                              dev_status=status)

@@ -56,8 +56,10 @@ def test_extend_window(api):
     assert call(window=0) == api.ERR_INVALID_ARG and call(window=-5) == api.ERR_INVALID_ARG
     assert call(sinks=-1) == api.ERR_INVALID_ARG
     assert call(window=0, total=0) == api.ERR_INVALID_ARG
-    need = api.diffqkv_extend_workspace_bytes(shape(api), 5)
-    assert call(ws_bytes=need - 1) == api.ERR_WORKSPACE
+    need = api.diffqkv_extend_window_workspace_bytes(shape(api), 5)
+    assert need >= 256 and need % 256 == 0 and call(ws_bytes=need - 1) == api.ERR_WORKSPACE
+    assert api.diffqkv_extend_window_workspace_bytes(shape(api, n_k=3), 5) == 0
+    assert api.diffqkv_extend_window_workspace_bytes(shape(api), -1) == 0
     assert api.launch_count() == before
 
 
@@ -76,7 +78,7 @@ def test_extend_shared(api):
     assert call(n=0, groups=None, lens=None, total=0) == api.OK
     assert api._lib.diffqkv_extend_shared(A, A, 5, None, C.byref(cache(api)), C.byref(shape(api)), A, 1 << 30, A, None, None,
                                           None) == bad
-    need, plain = api.diffqkv_extend_shared_workspace_bytes(shape(api), 5), api.diffqkv_extend_workspace_bytes(shape(api), 5)
+    need, plain = api.diffqkv_extend_shared_workspace_bytes(shape(api), 5), api.diffqkv_extend_window_workspace_bytes(shape(api), 5)
     assert need >= plain + 2 * 5 * 8 * (64 + 1) * 4 and need % 256 == 0
     assert call(ws_bytes=need - 1) == api.ERR_WORKSPACE
     # a step without tensor cores needs a length for every sequence
