@@ -265,7 +265,15 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
   } else {
     // ------------------------------------------------------------------ products and softmax
     const int g8 = lane >> 2, t4 = lane & 3;  // row and column pair of the fragments
-    const int bt_mask = p.box_tok - 1;
+    // Row r, 64-channel half h of a head tile lies at ((r / box_tok) H + h) box_tok + r % box_tok times 128 bytes, its 16-byte
+    // pieces exclusive-ored with r mod 8.  Of the rows that a lane addresses (ldmatrix) r mod 8 is lane mod 8 always, so
+    // that a step's addresses are a base and constants: rows 16 and 32 further down, the other half, and the pieces.
+    const int box = p.box_tok;
+    auto row_at = [&](int r, int H) -> uint32_t { return (uint32_t)(((r >> bt_shift) * H << bt_shift) + (r & (box - 1))) << 7; };
+    const uint32_t half_at = (uint32_t)box << 7;
+    const uint32_t k_lane = row_at((lane & 7) + 8 * (lane >> 4), HK) + ((((lane >> 3) & 1) ^ (lane & 7)) << 4);
+    const uint32_t v_lane = row_at(lane & 15, HV) + (((lane >> 4) ^ (lane & 7)) << 4);
+    const uint32_t k_16 = row_at(16, HK), k_32 = row_at(32, HK), v_16 = row_at(16, HV), v_32 = row_at(32, HV);
     bool dead = false;  // a wait for tiles ran out: go on without waiting, so that all warps meet at the barriers below
     for (uint32_t segs = 0;; ++segs) {
       const FewSegment& w = sc.seg[segs % kSegRing];  // released at the end of the segment
@@ -330,22 +338,17 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
           float s[4][4];
 #pragma unroll
           for (int e = 0; e < 16; ++e) s[e >> 2][e & 3] = 0.f;
-          {
-            const int row = r + (lane & 7) + 8 * (lane >> 4), half = (lane >> 3) & 1;
-            // 16 tokens further on: another box, or further down in the same one
-            const uint32_t at = base + k_off + ((((row >> bt_shift) * HK << bt_shift) + (row & bt_mask)) << 7);
-            const uint32_t at2 = base + k_off + (((((row + 16) >> bt_shift) * HK << bt_shift) + ((row + 16) & bt_mask)) << 7);
+          const uint32_t k_at = base + k_off + k_lane + (r ? k_32 : 0u);
 #pragma unroll
-            for (int ks = 0; ks < kDQK / 16; ++ks) {
-              const uint32_t off = (((uint32_t)(ks / 4) << bt_shift) << 7) + ((((ks % 4) * 2 + half) ^ (row & 7)) << 4);
-              uint32_t b[4], d[4];
-              ptx::ldmatrix_x4(at + off, b);
-              ptx::ldmatrix_x4(at2 + off, d);
-              ptx::mma_bf16_16816(s[0], qf[ks], b[0], b[1]);
-              ptx::mma_bf16_16816(s[1], qf[ks], b[2], b[3]);
-              ptx::mma_bf16_16816(s[2], qf[ks], d[0], d[1]);
-              ptx::mma_bf16_16816(s[3], qf[ks], d[2], d[3]);
-            }
+          for (int ks = 0; ks < kDQK / 16; ++ks) {
+            const uint32_t at = k_at + (ks / 4) * half_at;
+            uint32_t b[4], d[4];
+            ptx::ldmatrix_x4(at ^ ((ks % 4) << 5), b);
+            ptx::ldmatrix_x4((at + k_16) ^ ((ks % 4) << 5), d);
+            ptx::mma_bf16_16816(s[0], qf[ks], b[0], b[1]);
+            ptx::mma_bf16_16816(s[1], qf[ks], b[2], b[3]);
+            ptx::mma_bf16_16816(s[2], qf[ks], d[0], d[1]);
+            ptx::mma_bf16_16816(s[3], qf[ks], d[2], d[3]);
           }
           if (t0 + 31 > min(last[0], last[1]) || (t0 < max(first[0], first[1]) && t0 + 32 > p.sinks)) {
 #pragma unroll
@@ -391,25 +394,24 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
           }
           // ---- V rows that no row sees hold anything: 0 * NaN would poison the product
           if (edge) {
-            const int row = r + lane, tok = t0 + lane;
+            const int tok = t0 + lane;
             if (tok >= end || (tok < low && tok >= p.sinks)) {
-              unsigned char* dst = smem + stage * stage_bytes + v_off + ((((row >> bt_shift) * HV << bt_shift) + (row & bt_mask)) << 7);
+              unsigned char* dst = smem + stage * stage_bytes + v_off + row_at(r + lane, HV);
 #pragma unroll 1
               for (int c = 0; c < HV * 8; ++c)
-                *reinterpret_cast<uint4*>(dst + (((uint32_t)(c >> 3) << bt_shift) << 7) + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4*>(dst + (c >> 3) * half_at + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
             }
             ptx::fence_proxy_async();  // before the next TMA write
             __syncwarp();
           }
           // ---- O += P V, 16 tokens at a time
+          const uint32_t v_at = base + v_off + v_lane + (r ? v_32 : 0u);
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const int row = r + h * 16 + (lane & 15), half = lane >> 4;
-            const uint32_t at = base + v_off + ((((row >> bt_shift) * HV << bt_shift) + (row & bt_mask)) << 7);
 #pragma unroll
             for (int c = 0; c < kD / 16; ++c) {
               uint32_t b[4];
-              ptx::ldmatrix_x4_trans(at + (((uint32_t)(c / 4) << bt_shift) << 7) + ((((c % 4) * 2 + half) ^ (row & 7)) << 4), b);
+              ptx::ldmatrix_x4_trans((v_at + h * v_16 + (c / 4) * half_at) ^ ((c % 4) << 5), b);
               ptx::mma_bf16_16816(acc[2 * c], pf[h], b[0], b[1]);
               ptx::mma_bf16_16816(acc[2 * c + 1], pf[h], b[2], b[3]);
             }
