@@ -403,7 +403,10 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       if (w.ta == 0 && w.tb < w.nt) {
         m.rows = m.part_rows = min(w.seq.n - tok0, 2 * p.T) * p.G; m.row_lo = w.seq.lo + tok0; m.head0 = head0;
         m.parts = share_of(w.item_lo + last_tile(w.wide ? kWideCost : kNarrowCost, w.nt, kItemCost), total, n_teams) - team + 1;
-        if constexpr (kRanged) m.dst = w.seq.dst;
+      }
+      if constexpr (kRanged) {
+        if (w.ta == 0 && member == 0 && p.groups > 0 && lane == 0)
+          p.refs[((w.seq.dst == kDstPrefix ? 0LL : p.total_q) + w.seq.lo + tok0) * p.n_units + w.u] = {team, w.tb < w.nt ? -m.parts : -1};
       }
       Seg seg;
       static_cast<Segment&>(seg) = {w.seq.lo, w.seq.n, w.seq.past, tok0, head0, w.ta, w.tb, w.nst0, vc,
@@ -499,6 +502,9 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       }
       if (!ok) break;
     }
+    // Ranged: the joining kernel, which waits for the end of both, may take its place once the second one's last tiles are on
+    // their way (a launch and the search for a row's items are then no longer in its time).
+    if (kRanged && !p.first) ptx::grid_launch_dependents();
     Seg last = {};
     last.flags = kSegEnd;
     if (ok) ok = hand_out(last);
@@ -950,7 +956,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
 // each in flight.
 constexpr int kCombineThreads = 256, kCombineBlocks = 3;  // per SM
 
-template <int kD, bool kRanged>
+template <int kD>
 __global__ void __launch_bounds__(kCombineThreads, kCombineBlocks)
 extend_combine_kernel(const ExtendParams p, const ExtendList thin, const int thin_blocks, const int wide_blocks) {
   constexpr int kLanes = kD / 8, kGroups = kCombineThreads / kLanes, kItems = 2 * kMaxBlocks;
@@ -1070,9 +1076,8 @@ extend_combine_kernel(const ExtendParams p, const ExtendList thin, const int thi
           acc[h][e].z *= inv;
           acc[h][e].w *= inv;
         }
-        const bool to_out = !kRanged || m.dst == kDstOut;
-        if (!to_out || p.out_is_f32) {
-          float4* dst = reinterpret_cast<float4*>((to_out ? reinterpret_cast<float*>(p.out) : p.buffer[m.dst - 1].o) + row * kD) + lane * 2;
+        if (p.out_is_f32) {
+          float4* dst = reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + row * kD) + lane * 2;
           dst[0] = acc[h][0];
           dst[1] = acc[h][1];
         } else {
@@ -1080,8 +1085,7 @@ extend_combine_kernel(const ExtendParams p, const ExtendList thin, const int thi
               make_uint4(pack2(acc[h][0].x, acc[h][0].y), pack2(acc[h][0].z, acc[h][0].w), pack2(acc[h][1].x, acc[h][1].y),
                          pack2(acc[h][1].z, acc[h][1].w));
         }
-        float* const lse = to_out ? p.lse : p.buffer[m.dst - 1].lse;
-        if (lse && lane == 0) lse[row] = sum[h] != 0.f ? (top[h] + log2f(sum[h])) * (to_out ? kLn2 : 1.f) : -INFINITY;
+        if (p.lse && lane == 0) p.lse[row] = sum[h] != 0.f ? (top[h] + log2f(sum[h])) * kLn2 : -INFINITY;
         if (++head == p.G) {
           head = 0;
           ++tok;
@@ -1095,51 +1099,134 @@ extend_combine_kernel(const ExtendParams p, const ExtendList thin, const int thi
   }
 }
 
-// A row with two entries, its group's prefix and its own tokens: out = sum of the two parts weighted by 2^lse, a block a row.
-// Rows of sequences without a prefix, or that do not fit, are not touched.
-constexpr int kMergeThreads = 256;
+// The rows of a step with groups: a row's result is joined from the parts of its two items, that of its group's prefix and
+// that of its own tokens, whole or cut, in their order (out = sum of 2^lse o / sum of 2^lse).  Rows of sequences without a
+// prefix whose item is whole have their result already; those that do not fit are not touched.  A block first finds the items
+// of its rows, while the two kernels before still run, and reads where these items' parts are; then kD / 8 lanes take a head,
+// eight channels each, row after row, so that a row's parts are one read (of four at a time).
+constexpr int kMergeThreads = 256, kMergeBlocks = 3;  // per SM
+constexpr int kMergeRows = 16, kMergeRefs = 512;      // of a block, at most; row's units whose items fit shared memory
 
 template <int kD>
-__global__ void __launch_bounds__(kMergeThreads) extend_merge_kernel(const ExtendParams p) {
-  const int t = blockIdx.x;
-  int lo, n, past;
-  const int b = ragged_sequence_of<kMergeThreads>(p.cu_q, p.seqlens, p.batch, p.total_q, p.max_seqlen, t, false, p.dev_status,
-                                                  lo, n, past, [] {});
-  const int prefix = b < 0 ? 0 : group_prefix(p, b, lo, n, past);
+__global__ void __launch_bounds__(kMergeThreads, kMergeBlocks)
+extend_merge_kernel(const ExtendParams p, const ExtendList few, const int rows_each) {
+  constexpr int kLanes = kD / 8, kHeads = kMergeThreads / kLanes;
+  struct Row {
+    int has;       // 0: nothing to do here, 1: own tokens alone, 2: a prefix too
+    int first[2];  // first row of the item of either kind
+    int rows[2];   // of a head group, of an item of a few rows; 0: of long chunks
+  };
+  __shared__ Row row_s[kMergeRows];
+  __shared__ ItemRef ref_s[kMergeRefs][2];
+  const int t0 = blockIdx.x * rows_each, count = min(rows_each, p.total_q - t0);
+  {
+    int b = -1, lo = 0, n = 0, past, g_lo = 0, g_hi = 0, prefix = -1;
+    for (int r = 0; r < count; ++r) {
+      const int t = t0 + r;
+      if (b < 0 || t >= lo + n) {  // the next row's sequence
+        b = ragged_sequence_of<kMergeThreads>(p.cu_q, p.seqlens, p.batch, p.total_q, p.max_seqlen, t, false, p.dev_status, lo,
+                                              n, past, [] {});
+        prefix = b < 0 ? -1 : group_prefix(p, b, lo, n, past, g_lo, g_hi);
+      }
+      if (threadIdx.x < 2) {
+        const int k = threadIdx.x, first = k == 0 ? g_lo : lo, rows = k == 0 ? g_hi - g_lo : n;
+        const bool wide = rows > p.thin_max;
+        row_s[r].has = prefix < 0 ? 0 : prefix == 0 ? 1 : 2;
+        row_s[r].first[k] = wide ? first + (t - first) / (2 * p.T) * (2 * p.T) : first;
+        row_s[r].rows[k] = wide ? 0 : rows * p.G;
+      }
+    }
+  }
+  __syncthreads();
   ptx::grid_dependency_wait();
-  if (prefix <= 0) return;
-  constexpr int kLanes = kD / 4;
+  auto ref_of = [&](int r, int unit, int k) -> ItemRef {
+    const Row& w = row_s[r];
+    if (w.has < (k == 0 ? 2 : 1)) return {0, 0};
+    ItemRef x = p.refs[((size_t)k * p.total_q + w.first[k]) * p.n_units + unit];
+    const int most = w.rows[k] == 0 ? p.n_teams : p.blocks;
+    if (w.rows[k] == 0) x.parts = -x.parts;
+    // never read outside of the workspace: what a block that gave up did not leave is passed over
+    if (x.first < 0 || x.first >= most || x.parts < 0 || x.parts > most - x.first) x.parts = 0;
+    return x;
+  };
+  const bool cached = count * p.n_units <= kMergeRefs;
+  if (cached) {
+    for (int x = threadIdx.x; x < 2 * count * p.n_units; x += kMergeThreads)
+      ref_s[x >> 1][x & 1] = ref_of((x >> 1) / p.n_units, (x >> 1) % p.n_units, x & 1);
+    __syncthreads();
+  }
   const int lane = threadIdx.x % kLanes;
-  for (int h = threadIdx.x / kLanes; h < p.n_q; h += kMergeThreads / kLanes) {
-    const long long row = (long long)t * p.n_q + h;
-    float l[2];
-    float4 o[2];
+  for (int h = blockIdx.y * kHeads + threadIdx.x / kLanes; h < p.n_q; h += gridDim.y * kHeads) {
+    const int group = h / p.G, unit = group / p.parts, member = group - unit * p.parts, head = h - group * p.G;
+    for (int r = 0; r < count; ++r) {
+      const Row& w = row_s[r];
+      const ItemRef ref0 = cached ? ref_s[r * p.n_units + unit][0] : ref_of(r, unit, 0);
+      const ItemRef ref1 = cached ? ref_s[r * p.n_units + unit][1] : ref_of(r, unit, 1);
+      const int total = ref0.parts + ref1.parts;
+      if (w.has == 0 || (w.has == 1 && total <= 1)) continue;  // nothing to join
+      const size_t row = (size_t)(t0 + r) * p.n_q + h;
+      float top = -INFINITY, sum = 0.f;
+      float4 acc[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll 1
+      for (int x0 = 0; x0 < total; x0 += 4) {
+        float ls[4];
+        float4 v[4][2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      l[i] = p.buffer[i].lse[row];
-      o[i] = reinterpret_cast<const float4*>(p.buffer[i].o + row * kD)[lane];
-    }
-    const float top = fmaxf(l[0], l[1]);
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float sum = 0.f;
+        for (int x = 0; x < 4; ++x) {
+          ls[x] = -INFINITY;
+          if (x0 + x < total) {
+            const int k = x0 + x >= ref0.parts, part = k ? x0 + x - ref0.parts : x0 + x;
+            const ItemRef ref = k ? ref1 : ref0;
+            const float* lse = p.buffer[k].lse;
+            const float* o = p.buffer[k].o;
+            size_t at = row;
+            if (ref.parts > 1) {  // the first part lies in its block's second slot, the others in the first
+              const bool wide = w.rows[k] == 0;
+              const ExtendList& list = wide ? p.list : few;
+              const int block = (ref.first + part) * list.team + (wide ? member : 0);
+              at = (size_t)(2 * block + (part == 0)) * list.slot_rows + ((t0 + r - w.first[k]) * p.G + head + member * w.rows[k]);
+              lse = list.part_lse;
+              o = list.part_o;
+            }
+            ls[x] = lse[at];
+            const float4* from = reinterpret_cast<const float4*>(o + at * kD) + 2 * lane;
+            v[x][0] = from[0];
+            v[x][1] = from[1];
+          }
+        }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      if (l[i] == -INFINITY) continue;
-      const float f = ex2(l[i] - top);
-      sum += f;
-      acc.x = fmaf(f, o[i].x, acc.x);
-      acc.y = fmaf(f, o[i].y, acc.y);
-      acc.z = fmaf(f, o[i].z, acc.z);
-      acc.w = fmaf(f, o[i].w, acc.w);
+        for (int x = 0; x < 4; ++x) {
+          if (ls[x] == -INFINITY) continue;  // the part saw no token of this row (and may have left no values)
+          const float up = fmaxf(top, ls[x]), was = ex2(top - up), f = ex2(ls[x] - up);
+          top = up;
+          sum = fmaf(sum, was, f);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            acc[e].x = fmaf(f, v[x][e].x, acc[e].x * was);
+            acc[e].y = fmaf(f, v[x][e].y, acc[e].y * was);
+            acc[e].z = fmaf(f, v[x][e].z, acc[e].z * was);
+            acc[e].w = fmaf(f, v[x][e].w, acc[e].w * was);
+          }
+        }
+      }
+      const float inv = sum != 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        acc[e].x *= inv;
+        acc[e].y *= inv;
+        acc[e].z *= inv;
+        acc[e].w *= inv;
+      }
+      if (p.out_is_f32) {
+        float4* dst = reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + row * kD) + 2 * lane;
+        dst[0] = acc[0];
+        dst[1] = acc[1];
+      } else {
+        reinterpret_cast<uint4*>(reinterpret_cast<__nv_bfloat16*>(p.out) + row * kD)[lane] =
+            make_uint4(pack2(acc[0].x, acc[0].y), pack2(acc[0].z, acc[0].w), pack2(acc[1].x, acc[1].y), pack2(acc[1].z, acc[1].w));
+      }
+      if (p.lse && lane == 0) p.lse[row] = sum != 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
     }
-    const float inv = sum != 0.f ? 1.f / sum : 0.f;
-    if (p.out_is_f32)
-      reinterpret_cast<float4*>(reinterpret_cast<float*>(p.out) + row * kD)[lane] =
-          make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-    else
-      reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(p.out) + row * kD)[lane] =
-          make_uint2(pack2(acc.x * inv, acc.y * inv), pack2(acc.z * inv, acc.w * inv));
-    if (p.lse && lane == 0) p.lse[row] = sum != 0.f ? (top + log2f(sum)) * kLn2 : -INFINITY;
   }
 }
 
@@ -1148,7 +1235,8 @@ __global__ void extend_lengths_kernel(const ExtendParams p, int* seqlens) {
   const int b = blockIdx.x * blockDim.x + threadIdx.x;
   if (b >= p.batch) return;
   int lo, n, past;
-  const bool fits = load_rows(p, b, lo, n, past) && (n == 0 || group_prefix(p, b, lo, n, past) >= 0);
+  int g_lo, g_hi;
+  const bool fits = load_rows(p, b, lo, n, past) && (n == 0 || group_prefix(p, b, lo, n, past, g_lo, g_hi) >= 0);
   seqlens[b] = fits ? past : -1;
 }
 
@@ -1261,15 +1349,16 @@ size_t place(const Plan& pl, int d_v, char* base, ExtendList* wide, ExtendList* 
   return at;
 }
 
-// Behind them, for a step with groups, the rows' two parts.
-size_t place_buffers(const diffqkv_shape& s, int total_q, char* base, RowBuffer* buffers) {
+// Behind them, for a step with groups, the rows' two parts and where those are that were cut.
+size_t place_buffers(const diffqkv_shape& s, const Plan& pl, int total_q, char* base, ExtendParams* p) {
   const size_t rows = (size_t)total_q * s.n_q;
   const size_t lse = up256(rows * sizeof(float)), o = up256(rows * s.d_v * sizeof(float));
-  for (int i = 0; i < 2 && buffers; ++i) {
-    buffers[i].lse = reinterpret_cast<float*>(base + i * (lse + o));
-    buffers[i].o = reinterpret_cast<float*>(base + i * (lse + o) + lse);
+  for (int i = 0; i < 2 && p; ++i) {
+    p->buffer[i].lse = reinterpret_cast<float*>(base + i * (lse + o));
+    p->buffer[i].o = reinterpret_cast<float*>(base + i * (lse + o) + lse);
   }
-  return 2 * (lse + o);
+  if (p) p->refs = reinterpret_cast<ItemRef*>(base + 2 * (lse + o));
+  return 2 * (lse + o) + up256(2 * sizeof(ItemRef) * (size_t)total_q * (pl.groups / pl.parts));
 }
 
 bool dims_supported(const diffqkv_shape& s) {
@@ -1287,7 +1376,7 @@ size_t extend_workspace_bytes(const diffqkv_shape& s, int total_q, bool ranged) 
 
 size_t extend_groups_workspace_bytes(const diffqkv_shape& s, int total_q) {
   const size_t lengths = up256(sizeof(int) * (size_t)s.batch);  // see launch_extend_lengths
-  const size_t need = dims_supported(s) ? place_buffers(s, total_q, nullptr, nullptr) : 0;
+  const size_t need = dims_supported(s) ? place_buffers(s, make_plan(s, total_q, true), total_q, nullptr, nullptr) : 0;
   return need > lengths ? need : lengths;
 }
 
@@ -1381,7 +1470,7 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
     p.sink_few = (int)(((long long)range->sinks + kFewT - 1) / kFewT);
     p.groups = range->groups; p.entries = range->groups + s.batch;
     p.cu_groups = range->cu_groups; p.prefix_lens = range->prefix_lens;
-    if (p.groups > 0) place_buffers(s, total_q, static_cast<char*>(workspace) + extend_workspace_bytes(s, total_q, true), p.buffer);
+    if (p.groups > 0) place_buffers(s, pl, total_q, static_cast<char*>(workspace) + extend_workspace_bytes(s, total_q, true), &p);
   }
   const int thin_blocks = pl.thin_max > 0 ? pl.blocks : 0, blocks = pl.n_teams * pl.parts;
 
@@ -1434,24 +1523,23 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
   if ((err = wide_first ? launch_wide() : launch_thin()) != cudaSuccess) return err;
   if ((err = wide_first ? launch_thin() : launch_wide()) != cudaSuccess) return err;
   p.list = wide;
-  const long long groups = kCombineThreads / (s.d_v / 8), rows = (long long)total_q * s.n_q, fill = sm_count() * kCombineBlocks;
-  cfg.gridDim = dim3((unsigned)((rows + groups - 1) / groups < fill ? (rows + groups - 1) / groups : fill));
-  cfg.blockDim = dim3(kCombineThreads);
   cfg.dynamicSmemBytes = 0;
   cfg.numAttrs = 1;
-  using CombineFn = void (*)(const ExtendParams, const ExtendList, const int, const int);
-  constexpr CombineFn joins[2][2] = {{extend_combine_kernel<64, false>, extend_combine_kernel<128, false>},
-                                     {extend_combine_kernel<64, true>, extend_combine_kernel<128, true>}};
-  err = cudaLaunchKernelEx(&cfg, joins[range != nullptr][s.d_v == 128], p, thin, thin_blocks, blocks);
+  if (p.groups > 0) {
+    const int heads = kMergeThreads / (s.d_v / 8), across = (s.n_q + heads - 1) / heads, resident = kMergeBlocks * sm_count();
+    int rows_each = (int)(((long long)total_q * across + resident - 1) / resident);
+    if (rows_each > kMergeRows) rows_each = kMergeRows;
+    cfg.gridDim = dim3((unsigned)((total_q + rows_each - 1) / rows_each), (unsigned)across);
+    cfg.blockDim = dim3(kMergeThreads);
+    err = cudaLaunchKernelEx(&cfg, s.d_v == 64 ? extend_merge_kernel<64> : extend_merge_kernel<128>, p, thin, rows_each);
+  } else {
+    const long long groups = kCombineThreads / (s.d_v / 8), rows = (long long)total_q * s.n_q, fill = sm_count() * kCombineBlocks;
+    cfg.gridDim = dim3((unsigned)((rows + groups - 1) / groups < fill ? (rows + groups - 1) / groups : fill));
+    cfg.blockDim = dim3(kCombineThreads);
+    err = cudaLaunchKernelEx(&cfg, s.d_v == 64 ? extend_combine_kernel<64> : extend_combine_kernel<128>, p, thin, thin_blocks, blocks);
+  }
   if (err != cudaSuccess) return err;
   count_launch();
-  if (p.groups > 0) {
-    cfg.gridDim = dim3((unsigned)total_q);
-    cfg.blockDim = dim3(kMergeThreads);
-    err = cudaLaunchKernelEx(&cfg, s.d_v == 64 ? extend_merge_kernel<64> : extend_merge_kernel<128>, p);
-    if (err != cudaSuccess) return err;
-    count_launch();
-  }
   return cudaGetLastError();
 }
 

@@ -23,16 +23,21 @@ struct ExtendMeta {  // an item that is cut, left by the block that has its firs
   int part_rows;
   int row_lo, head0; // first row in q, first head
   int parts;         // the teams from this block's on that have some of its tiles each
-  int dst;           // ranged: where its rows go (kDst...)
 };
 
 constexpr int kNoWindow = 0x7fffffff;
 // Where the rows of an entry of a ranged step go: to the result, or, where a row has two entries (the prefix of its group and
-// its own tokens), to a buffer for each, which extend_merge_kernel joins.
+// its own tokens), to a buffer for each.
 constexpr int kDstOut = 0, kDstPrefix = 1, kDstOwn = 2;
 struct RowBuffer {
   float* o;    // [total_q n_q][d_v]
   float* lse;  // [total_q n_q] base 2
+};
+// Of a step with groups, where the parts of an item are, for extend_merge_kernel: left by the block that has its first tile,
+// at [kind of entry][first row of the item][unit].
+struct ItemRef {
+  int first;  // that block, or its team
+  int parts;  // negative in the list of long chunks; 1: the whole item, in its buffer or the result
 };
 
 // One of the two flat lists of work, and where its cut items go.
@@ -79,6 +84,7 @@ struct ExtendParams {
   const int* cu_groups;
   const int* prefix_lens;
   RowBuffer buffer[2];  // kDstPrefix - 1, kDstOwn - 1
+  ItemRef* refs;        // [2][total_q][n_units]
 };
 
 // Rows of sequence b: first row, number, tokens cached before; false when they do not fit.
@@ -188,8 +194,8 @@ __device__ __forceinline__ bool group_rows(const ExtendParams& p, int g, int& lo
   return lo >= 0 && hi >= lo && hi <= p.total_q && prefix <= 0x7ffffe00 - (hi - lo);  // positions stay within 32 bits
 }
 // Tokens of sequence b, whose rows are lo .. lo + n - 1 behind `past` tokens, that its group has for it (0 outside of all
-// groups); -1 when the group's rows or tokens do not hold those of the sequence.
-__device__ __forceinline__ int group_prefix(const ExtendParams& p, int b, int lo, int n, int past) {
+// groups); -1 when the group's rows or tokens do not hold those of the sequence.  The group's rows are g_lo .. g_hi - 1.
+__device__ __forceinline__ int group_prefix(const ExtendParams& p, int b, int lo, int n, int past, int& g_lo, int& g_hi) {
   int g = 0, z = p.groups;  // the last group that begins at or before b
   if (z == 0) return 0;
   while (z - g > 1) {
@@ -197,7 +203,7 @@ __device__ __forceinline__ int group_prefix(const ExtendParams& p, int b, int lo
     if (p.cu_groups[mid] <= b) g = mid; else z = mid;
   }
   if (b < p.cu_groups[g] || b >= p.cu_groups[g + 1]) return 0;
-  int g_lo, g_hi, first, prefix;
+  int first, prefix;
   if (!group_rows(p, g, g_lo, g_hi, first, prefix) || prefix > past || lo < g_lo || lo + n > g_hi) return -1;
   return prefix;
 }
@@ -261,7 +267,8 @@ struct SeqOf<true> {
       tab = x - p.groups;
       bad = !load_rows(p, tab, lo, n, past);
       if (!bad && n > 0) {
-        start = group_prefix(p, tab, lo, n, past);
+        int g_lo, g_hi;
+        start = group_prefix(p, tab, lo, n, past, g_lo, g_hi);
         if (start < 0) {
           bad = true;
           n = start = past = 0;

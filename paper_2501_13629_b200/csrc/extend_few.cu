@@ -210,10 +210,12 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         break;
       }
       if (ta == 0 && tb < nt) {
-        m.rows = p.parts * x.rows * p.G; m.part_rows = x.rows * p.G; m.row_lo = x.lo; m.head0 = head0; m.dst = x.dst;
+        m.rows = p.parts * x.rows * p.G; m.part_rows = x.rows * p.G; m.row_lo = x.lo; m.head0 = head0;
         m.parts = chunk > 0 ? (nt + chunk - 1) / chunk
                             : share_of((long long)item_lo + last_tile(1, nt, kItem), total, blocks) - (int)blockIdx.x + 1;
       }
+      if (ta == 0 && p.groups > 0 && lane == 0)
+        p.refs[((x.dst == kDstPrefix ? 0LL : p.total_q) + x.lo) * p.n_units + u] = {(int)blockIdx.x, tb < nt ? m.parts : 1};
       auto token_of = [&](int tile) -> int { return ((tile >= p.sink_few ? tile + skip : tile) << 6) + my_part * p.box_tok; };
       auto wanted = [&](int tok) -> bool { return tok < x.end && (tok < p.sinks || tok + p.box_tok > low); };
       auto fetch = [&](int tile) -> int {  // page of this lane's box
@@ -252,6 +254,7 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       if (!ok || chunk > 0) break;
       next_item();
     }
+    if (!p.first) ptx::grid_launch_dependents();  // see extend.cu
     FewSegment end = {};
     end.flags = kSegEnd;
     if (!hand_out(end, nullptr)) ok = false;  // in any case: the other warps leave together
