@@ -727,17 +727,20 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
         }
         if constexpr (kRanged) {
           const int k0 = token_of(j);
-          if (k0 / kKT >= j_diag) {
-            const int sees = min(w.past + tok0_of(w) + r / p.G, w.end - 1) - k0;
+          if (k0 / kKT >= j_diag || (k0 < low_last && k0 + kKT > p.sinks)) {
+            // a word of 32 columns at a time, most of which every row of the warp sees or none does
+            const int pos = w.past + tok0_of(w) + r / p.G;
+            const int sees = min(pos, w.end - 1) - k0, low = max(w.start, pos + 1 - p.window) - k0, sinks = p.sinks - k0;
+            auto below = [](int x) -> uint32_t { return x >= 32 ? ~0u : x <= 0 ? 0u : (1u << x) - 1; };  // columns before x
 #pragma unroll
-            for (int e = 0; e < 128; ++e)
-              if (e > sees) s[e] = 0xff800000u;  // -inf
-          }
-          if (k0 < low_last && k0 + kKT > p.sinks) {
-            const int low = max(w.start, w.past + tok0_of(w) + r / p.G + 1 - p.window) - k0, sinks = p.sinks - k0;
+            for (int c = 0; c < 128; c += 32) {
+              const uint32_t seen = below(sees + 1 - c) & (~below(low - c) | below(sinks - c));
+              if (__any_sync(0xffffffffu, seen != ~0u)) {
 #pragma unroll
-            for (int e = 0; e < 128; ++e)
-              if (e < low && e >= sinks) s[e] = 0xff800000u;
+                for (int e = 0; e < 32; ++e)
+                  if (!(seen >> e & 1)) s[c + e] = 0xff800000u;  // -inf
+              }
+            }
           }
         } else if (j >= j_diag) {
           const int sees = min(w.past + tok0_of(w) + r / p.G, w.past + w.n - 1) - j * kKT;  // last column the row sees
