@@ -3,12 +3,18 @@
 //
 // Mathematics: every head x of q and k becomes x * r * (offset + w), r = 1 / sqrt(mean x_c^2 + eps) over its d_qk channels,
 // and its first rot_dim channels are then turned as in rope_append.cu, all in fp32 (bf16 between the two would cost another
-// half step of 2^-8 of every channel), rounded once.
+// half step of 2^-8 of every channel), rounded once.  Weight and turn are one: with g = offset + w a pair (u, v) becomes
+//     (r u) g_u cos - (r v) g_v sin,   (r v) g_v cos + (r u) g_u sin,
+// four coefficients a pair, which the heads of a row share.
 //
 // Bound by memory like rope_append.cu, whose plan this follows: a block a row, its angles worked out once for all heads, first
 // vectors read before the row's place is known.  A head belongs to a group of lanes of one warp, two 16-byte vectors to a
 // lane (a channel and its partner; neighbours where pairs are neighbours or nothing turns), so that the sum of squares is
-// a few shuffles and the head never leaves its registers.  Heads of more than 64 vectors are read a second time.
+// a few shuffles and the head never leaves its registers; a lane keeps its channels from head to head, first q's, then
+// k's, and their coefficients in registers as packed pairs (with weight and turn applied one after the other to every head
+// the kernel was bound by instructions, 72 us where it now takes @@).  Weights of each head's own are combined per head.
+// Heads of more than 64 vectors are read a second time.
+#include "attn_math.cuh"
 #include "common.cuh"
 #include "rope.cuh"
 
@@ -36,25 +42,62 @@ __device__ __forceinline__ void open_weight(const W* w, float (&x)[Pack<T>::N]) 
   }
 }
 
-// kPairs: rotate-half.
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+// kPairs: rotate-half.  A task is two vectors of a head, seen as pairs: u from the first, v from the second; where neighbours
+// turn together, u the even and v the odd channels of both.
+template <typename T, bool kPairs>
+struct Task {
+  static constexpr int N = Pack<T>::N;
+  int c0, c1;  // first channels of its vectors; -1: none
+  bool rotated;
+  __device__ void open(const uint4 (&raw)[2], uint64_t (&u)[N / 2], uint64_t (&v)[N / 2]) const {
+    float a[2 * N];
+    Pack<T>::open(raw[0], *reinterpret_cast<float(*)[N]>(a));
+    Pack<T>::open(raw[1], *reinterpret_cast<float(*)[N]>(a + N));
+    split(a, u, v);
+  }
+  static __device__ void split(const float (&a)[2 * N], uint64_t (&u)[N / 2], uint64_t (&v)[N / 2]) {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      u[i] = kPairs ? pair(a[2 * i], a[2 * i + 1]) : pair(a[4 * i], a[4 * i + 2]);
+      v[i] = kPairs ? pair(a[N + 2 * i], a[N + 2 * i + 1]) : pair(a[4 * i + 1], a[4 * i + 3]);
+    }
+  }
+  static __device__ void join(const uint64_t (&u)[N / 2], const uint64_t (&v)[N / 2], uint4 (&raw)[2]) {
+    float a[2 * N];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      unpair(u[i], a[kPairs ? 2 * i : 4 * i], a[kPairs ? 2 * i + 1 : 4 * i + 2]);
+      unpair(v[i], a[kPairs ? N + 2 * i : 4 * i + 1], a[kPairs ? N + 2 * i + 1 : 4 * i + 3]);
+    }
+    raw[0] = Pack<T>::close(*reinterpret_cast<float(*)[N]>(a));
+    raw[1] = Pack<T>::close(*reinterpret_cast<float(*)[N]>(a + N));
+  }
+};
+
 template <typename T, typename W, bool kPairs>
-__global__ void __launch_bounds__(kRopeThreads, 5) norm_rope_kernel(const RopeParams p, const NormParams m) {
+__global__ void __launch_bounds__(kRopeThreads, 7) norm_rope_kernel(const RopeParams p, const NormParams m) {
   constexpr int N = Pack<T>::N;
   constexpr int kAhead = 3;  // heads read together
-  extern __shared__ float2 turn_s[];  // [rot / 2] (cos, sin) * magnitude
+  using Task = Task<T, kPairs>;
+  // (cos, sin) * magnitude [rot / 2], for heads of many tasks; or the coefficients of q's and of k's tasks, sixteen bytes of
+  // every task behind one another: [2][N][tasks][4]
+  extern __shared__ float4 smem4[];
+  float2* turn_s = reinterpret_cast<float2*>(smem4);
+  float* coef_s = reinterpret_cast<float*>(smem4);
   const int tid = threadIdx.x;
   const int t = blockIdx.x;  // row
 
-  // A task is two vectors of a head; lane x of a head's lanes has tasks x, x + lanes, ...
+  // lane x of a head's lanes has tasks x, x + lanes, ...
   const int half = p.rot >> 1;
   const int rot_tasks = p.rot / (2 * N), rest = (p.d_qk - p.rot) / N, tasks = rot_tasks + (rest + 1) / 2;
   const int lanes = m.lanes, heads_at_once = kRopeThreads / lanes, first = tid / lanes, lane = tid - first * lanes;
   const int q_heads = p.q ? p.n_q : 0, heads = q_heads + p.n_k;
-  const bool single = tasks <= lanes;
-  struct Task {
-    int c0, c1;  // first channels of its vectors; -1: none
-    bool rotated;
-  };
   auto task = [&](int x) -> Task {
     if (x < rot_tasks) return kPairs ? Task{x * N, x * N + half, true} : Task{2 * x * N, (2 * x + 1) * N, true};
     const int y = 2 * (x - rot_tasks);
@@ -95,11 +138,38 @@ __global__ void __launch_bounds__(kRopeThreads, 5) norm_rope_kernel(const RopePa
     place_ok = blk >= 0 && blk < p.cache.num_blocks;
     if (!place_ok && tid == 0) report(p.dev_status, DIFFQKV_ERR_INDEX);
   }
-  for (int i = tid; i < half; i += kRopeThreads) {
-    const int pos = p.positions ? p.positions[t] : tok;
+  const int pos = p.positions ? p.positions[t] : tok;
+  auto turn = [&](int i) -> float2 {
     float sn, cs;
     sincosf(reduced_angle(pos, p.inv_freq[i]), &sn, &cs);
-    turn_s[i] = make_float2(cs * p.magnitude, sn * p.magnitude);
+    return make_float2(cs * p.magnitude, sn * p.magnitude);
+  };
+  auto weights = [&](bool is_q) -> const W* { return reinterpret_cast<const W*>(is_q ? m.q_weight : m.k_weight); };
+  auto weight_head = [&](bool is_q) -> long long { return is_q ? m.q_wst : m.k_wst; };
+  const float no_weight = m.offset != 0.f ? m.offset : 1.f;
+  const bool single = tasks <= lanes;
+  if (single) {  // a thread a pair, of q's and of k's; weights that every head has its own of are left to the heads
+    for (int x = tid; x < 2 * tasks * N; x += kRopeThreads) {
+      const bool is_q = x < tasks * N;
+      const int j = is_q ? x : x - tasks * N, at = j / N, i = j - at * N;
+      const Task k = task(at);
+      const int cu = kPairs ? k.c0 + i : k.c0 + 2 * i, cv = kPairs ? k.c1 + i : cu + 1;
+      float gu = 1.f, gv = 1.f;
+      if (weight_head(is_q) == 0) {
+        const W* weight = weights(is_q);
+        gu = !weight ? no_weight : cu < p.d_qk ? to_float(weight[cu]) + m.offset : 0.f;  // (a last vector without a second)
+        gv = !weight ? no_weight : k.c1 >= 0 || (!kPairs && cv < p.d_qk) ? to_float(weight[cv]) + m.offset : 0.f;
+      }
+      const float2 w = k.rotated ? turn((kPairs ? k.c0 : k.c0 / 2) + i) : make_float2(1.f, 0.f);
+      float* dst = coef_s + (((is_q ? 0 : N) + i / 4) * tasks + at) * 4 + i % 4;
+      const int step = (N / 4) * tasks * 4;
+      dst[0] = gu * w.x;
+      dst[step] = gv * w.x;
+      dst[2 * step] = gu * w.y;
+      dst[3 * step] = -gv * w.y;
+    }
+  } else {
+    for (int i = tid; i < half; i += kRopeThreads) turn_s[i] = turn(i);
   }
   __syncthreads();
   if (place_ok) {
@@ -111,73 +181,87 @@ __global__ void __launch_bounds__(kRopeThreads, 5) norm_rope_kernel(const RopePa
   T* q_out = reinterpret_cast<T*>(p.q_out) + (long long)t * p.n_q * p.d_qk;
   T* k_out = reinterpret_cast<T*>(const_cast<void*>(p.cache.k)) + blk * p.cache.k_sb + slot * p.cache.k_st;
 
-  auto squares = [&](const uint4 (&raw)[2]) -> float {
-    float s = 0.f;
+  auto squares = [&](const uint64_t (&u)[N / 2], const uint64_t (&v)[N / 2]) -> float {
+    uint64_t s = 0;
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      float a[N];
-      Pack<T>::open(raw[y], a);
-#pragma unroll
-      for (int i = 0; i < N; ++i) s = fmaf(a[i], a[i], s);
-    }
-    return s;
+    for (int i = 0; i < N / 2; ++i) s = fma2(v[i], v[i], fma2(u[i], u[i], s));
+    float x, y;
+    unpair(s, x, y);
+    return x + y;
   };
   auto over_lanes = [&](float s) -> float {  // the head's factor; every lane of the warp calls it
     for (int o = lanes >> 1; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     return rsqrtf(fmaf(s, m.inv_d, m.eps));
   };
-  auto finish = [&](int h, const Task& k, const float2 (&turn)[N], float r, const uint4 (&raw)[2]) {
-    if (h >= heads || k.c0 < 0) return;
-    const bool is_q = h < q_heads;
-    if (!is_q && !place_ok) return;
-    T* dst = is_q ? q_out + h * p.d_qk : k_out + (h - q_heads) * p.cache.k_sh;
-    const W* weight = reinterpret_cast<const W*>(is_q ? m.q_weight : m.k_weight);
-    if (weight) weight += is_q ? h * m.q_wst : (h - q_heads) * m.k_wst;
-    float a[2][N];
+  auto own_weights = [&](const W* weight, const Task& k, uint64_t (&u)[N / 2], uint64_t (&v)[N / 2]) {  // of one head
+    float g[2 * N];
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      Pack<T>::open(raw[y], a[y]);
-      float w[N];
-      const int c = y == 0 ? k.c0 : k.c1;
-      if (weight && c >= 0) {
+    for (int i = 0; i < 2 * N; ++i) g[i] = no_weight;
+    if (weight) {
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        const int c = y == 0 ? k.c0 : k.c1;
+        if (c < 0) continue;
+        float w[N];
         open_weight<T, W>(weight + c, w);
 #pragma unroll
-        for (int i = 0; i < N; ++i) w[i] += m.offset;
-      } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) w[i] = m.offset != 0.f ? m.offset : 1.f;
-      }
-#pragma unroll
-      for (int i = 0; i < N; ++i) a[y][i] = a[y][i] * r * w[i];
-    }
-    if (k.rotated) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        float& u = kPairs ? a[0][i] : a[2 * i / N][2 * i % N];
-        float& v = kPairs ? a[1][i] : a[2 * i / N][2 * i % N + 1];
-        const float x = u, y = v;
-        u = x * turn[i].x - y * turn[i].y;
-        v = y * turn[i].x + x * turn[i].y;
+        for (int i = 0; i < N; ++i) g[y * N + i] = w[i] + m.offset;
       }
     }
-    *reinterpret_cast<uint4*>(dst + k.c0) = Pack<T>::close(a[0]);
-    if (k.c1 >= 0) *reinterpret_cast<uint4*>(dst + k.c1) = Pack<T>::close(a[1]);
-  };
-  auto turns_of = [&](const Task& k, float2 (&turn)[N]) {
-    if (!k.rotated) return;
+    uint64_t gu[N / 2], gv[N / 2];
+    Task::split(g, gu, gv);
 #pragma unroll
-    for (int i = 0; i < N; ++i) turn[i] = turn_s[(kPairs ? k.c0 : k.c0 / 2) + i];
+    for (int i = 0; i < N / 2; ++i) {
+      u[i] = mul2(u[i], gu[i]);
+      v[i] = mul2(v[i], gv[i]);
+    }
   };
-  float2 turn[N];
+  auto place_of = [&](int h) -> T* { return h < q_heads ? q_out + h * p.d_qk : k_out + (h - q_heads) * p.cache.k_sh; };
+  auto write = [&](int h, const Task& k, const uint64_t (&u)[N / 2], const uint64_t (&v)[N / 2]) {
+    uint4 raw[2];
+    Task::join(u, v, raw);
+    T* dst = place_of(h);
+    if (k.c0 >= 0) *reinterpret_cast<uint4*>(dst + k.c0) = raw[0];
+    if (k.c1 >= 0) *reinterpret_cast<uint4*>(dst + k.c1) = raw[1];
+  };
+
   if (single) {
-    turns_of(mine, turn);
     for (int h0 = 0;;) {  // the same for all threads: the warp's lanes meet in the sums
 #pragma unroll
-      for (int y = 0; y < kAhead; ++y)
-        if (h0 + y * heads_at_once < heads) {
-          const float r = over_lanes(squares(ahead[y]));
-          finish(h0 + y * heads_at_once + first, mine, turn, r, ahead[y]);
+      for (int y = 0; y < kAhead; ++y) {
+        if (h0 + y * heads_at_once >= heads) break;
+        const int h = h0 + y * heads_at_once + first;
+        uint64_t u[N / 2], v[N / 2];
+        mine.open(ahead[y], u, v);
+        const float r = over_lanes(squares(u, v));
+        if (h >= heads || (h >= q_heads && !place_ok) || mine.c0 < 0) continue;
+        const uint64_t r2 = pair(r, r);
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+          u[i] = mul2(u[i], r2);
+          v[i] = mul2(v[i], r2);
         }
+        const bool is_q = h < q_heads;
+        if (weight_head(is_q) != 0) own_weights(weights(is_q) + (is_q ? h : h - q_heads) * weight_head(is_q), mine, u, v);
+        const ulonglong2* f = reinterpret_cast<const ulonglong2*>(coef_s) + (is_q ? 0 : N * tasks) + lane;
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {  // two packed pairs of each coefficient
+          const ulonglong2 uc = f[i * tasks], vc2 = f[(N / 4 + i) * tasks];
+          const uint64_t a0 = u[2 * i], b0 = v[2 * i], a1 = u[2 * i + 1], b1 = v[2 * i + 1];
+          u[2 * i] = mul2(a0, uc.x);
+          v[2 * i] = mul2(b0, vc2.x);
+          u[2 * i + 1] = mul2(a1, uc.y);
+          v[2 * i + 1] = mul2(b1, vc2.y);
+          if (mine.rotated) {
+            const ulonglong2 us = f[(2 * (N / 4) + i) * tasks], vs = f[(3 * (N / 4) + i) * tasks];
+            u[2 * i] = fma2(b0, vs.x, u[2 * i]);
+            v[2 * i] = fma2(a0, us.x, v[2 * i]);
+            u[2 * i + 1] = fma2(b1, vs.y, u[2 * i + 1]);
+            v[2 * i + 1] = fma2(a1, us.y, v[2 * i + 1]);
+          }
+        }
+        write(h, mine, u, v);
+      }
       h0 += kAhead * heads_at_once;
       if (h0 >= heads) break;
 #pragma unroll
@@ -186,25 +270,51 @@ __global__ void __launch_bounds__(kRopeThreads, 5) norm_rope_kernel(const RopePa
     return;
   }
   for (int h0 = 0; h0 < heads; h0 += heads_at_once) {
+    const int h = h0 + first;
+    const bool is_q = h < q_heads;
     float s = 0.f;
     uint4 raw[2];
-    for (int x = lane; x < tasks; x += lanes) {
-      read(h0 + first, task(x), raw);
-      s += squares(raw);
-    }
-    const float r = over_lanes(s);
+    uint64_t u[N / 2], v[N / 2];
     for (int x = lane; x < tasks; x += lanes) {
       const Task k = task(x);
-      read(h0 + first, k, raw);
-      turns_of(k, turn);
-      finish(h0 + first, k, turn, r, raw);
+      read(h, k, raw);
+      k.open(raw, u, v);
+      s += squares(u, v);
+    }
+    const float r = over_lanes(s);
+    if (h >= heads || (!is_q && !place_ok)) continue;
+    const uint64_t r2 = pair(r, r);
+    const W* weight = weights(is_q);
+    if (weight) weight += (is_q ? h : h - q_heads) * weight_head(is_q);
+    for (int x = lane; x < tasks; x += lanes) {
+      const Task k = task(x);
+      read(h, k, raw);
+      k.open(raw, u, v);
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) {
+        u[i] = mul2(u[i], r2);
+        v[i] = mul2(v[i], r2);
+      }
+      own_weights(weight, k, u, v);
+      if (k.rotated) {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) {
+          const float2* w = turn_s + (kPairs ? k.c0 : k.c0 / 2) + 2 * i;
+          const float2 w0 = w[0], w1 = w[1];
+          const uint64_t a = u[i], b = v[i];
+          u[i] = fma2(b, pair(-w0.y, -w1.y), mul2(a, pair(w0.x, w1.x)));
+          v[i] = fma2(a, pair(w0.y, w1.y), mul2(b, pair(w0.x, w1.x)));
+        }
+      }
+      write(h, k, u, v);
     }
   }
 }
 
 template <typename T, typename W>
 cudaError_t launch(const RopeParams& p, const NormParams& m, cudaStream_t stream) {
-  const size_t smem = sizeof(float2) * (p.rot / 2 + 1);
+  const int n = Pack<T>::N, tasks = p.rot / (2 * n) + ((p.d_qk - p.rot) / n + 1) / 2;
+  const size_t smem = tasks <= m.lanes ? sizeof(float4) * 2 * n * tasks : sizeof(float2) * (p.rot / 2 + 1);
   if (p.interleaved) norm_rope_kernel<T, W, false><<<(unsigned)p.total_q, kRopeThreads, smem, stream>>>(p, m);
   else norm_rope_kernel<T, W, true><<<(unsigned)p.total_q, kRopeThreads, smem, stream>>>(p, m);
   count_launch();
