@@ -218,6 +218,8 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   // The kernel for thin sequences works on other rows; whichever of the two comes second may take the SMs that the
   // first one's blocks leave.  The joining kernel depends on the second alone, which therefore ends behind the first.
+  // Ranged, the first of the two is launched before the work in front of it has ended, for which it waits here.
+  if (kRanged && p.first) ptx::grid_dependency_wait();
   if (p.first) ptx::grid_launch_dependents();
   const int team = (int)blockIdx.x / p.list.team, member = (int)blockIdx.x - team * p.list.team;
   long long total, w0, w1;  // of the flat list; this block's range of it
@@ -1509,7 +1511,7 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3(kExtendThreads);
     cfg.dynamicSmemBytes = kExtendSmem;
-    cfg.numAttrs = wide_first ? 0 : 1;
+    cfg.numAttrs = wide_first && !range ? 0 : 1;
     const cudaError_t e = range ? cudaLaunchKernelEx(&cfg, fn, mq, p.k_rows ? mk_rows : mk, p.v_rows ? mv_rows : mv, p)
                                 : cudaLaunchKernelEx(&cfg, fn, mq, mk, mv, p);
     if (e == cudaSuccess) count_launch();
@@ -1519,7 +1521,7 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
     if (thin_blocks == 0) return cudaSuccess;
     p.list = thin;
     p.first = !wide_first;
-    if (range) return launch_extend_few(mk_few, mv_few, q, p, s.d_qk, s.d_v, thin_blocks, wide_first, stream);
+    if (range) return launch_extend_few(mk_few, mv_few, q, p, s.d_qk, s.d_v, thin_blocks, stream);
     return launch_extend_thin(mq_thin, p.k_rows ? mk_rows : mk, p.v_rows ? mv_rows : mv, p, s.d_qk, s.d_v, thin_blocks,
                               wide_first, stream);
   };

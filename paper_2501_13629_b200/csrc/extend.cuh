@@ -462,6 +462,6 @@ cudaError_t launch_extend_thin(const CUtensorMap& mq, const CUtensorMap& mk, con
                                int d_qk, int d_v, int blocks, bool second, cudaStream_t stream);
 // The K and V boxes bring box_tok (at most 64) tokens, all channels of one head.
 cudaError_t launch_extend_few(const CUtensorMap& mk, const CUtensorMap& mv, const void* q, ExtendParams p, int d_qk, int d_v,
-                              int blocks, bool second, cudaStream_t stream);
+                              int blocks, cudaStream_t stream);
 
 }  // namespace diffqkv

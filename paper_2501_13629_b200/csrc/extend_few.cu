@@ -72,7 +72,10 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     ptx::grid_dependency_wait();
     return;
   }
-  if (p.first) ptx::grid_launch_dependents();
+  if (p.first) {  // see extend.cu
+    ptx::grid_dependency_wait();
+    ptx::grid_launch_dependents();
+  }
   if (tid < kMaxStages + kSegRing) {  // full and empty, of the stages and behind them of the segments
     const bool seg = tid >= kMaxStages;
     ptx::mbar_init(seg ? seg_full0 + 8 * (tid - kMaxStages) : full0 + 8 * tid, 1);
@@ -499,7 +502,7 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
 }  // namespace
 
 cudaError_t launch_extend_few(const CUtensorMap& mk, const CUtensorMap& mv, const void* q, ExtendParams p, int d_qk, int d_v,
-                              int blocks, bool second, cudaStream_t stream) {
+                              int blocks, cudaStream_t stream) {
   using Fn = void (*)(const CUtensorMap, const CUtensorMap, const __nv_bfloat16*, const ExtendParams);
   const Fn fn = d_v == 64 ? extend_few_kernel<64, 64> : d_qk == 128 ? extend_few_kernel<128, 128> : extend_few_kernel<64, 128>;
   if (p.box_tok > kFewT) p.box_tok = kFewT;
@@ -519,7 +522,7 @@ cudaError_t launch_extend_few(const CUtensorMap& mk, const CUtensorMap& mv, cons
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
-  cfg.numAttrs = second ? 1 : 0;
+  cfg.numAttrs = 1;
   const cudaError_t launched = cudaLaunchKernelEx(&cfg, fn, mk, mv, static_cast<const __nv_bfloat16*>(q), p);
   if (launched == cudaSuccess) count_launch();
   return launched;

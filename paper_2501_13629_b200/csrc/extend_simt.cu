@@ -359,16 +359,17 @@ int heads_per_tile(const diffqkv_shape& s) {
 
 bool dims_ok(const diffqkv_shape& s) { return (s.d_qk == 64 || s.d_qk == 128) && (s.d_v == 64 || s.d_v == 128); }
 
-// Splits along the tokens: enough blocks for two a SM, of at least 256 tokens each; the partial rows of all splits stay
-// within 32768.
+// Splits along the tokens: enough blocks for two a SM, of at least `least` tokens each; the partial rows of all splits stay
+// within 32768.  Within a window, whose few tiles are what a block's time is, 128 (17-100 rows, window 300, 16/2/4 heads of
+// 64: 35 us with the join, 40 with 256).
 int most_splits(const diffqkv_shape& s, int total_q) {
   const long long most = 32768 / ((long long)total_q * s.n_q);
   return most > kMaxSplits ? kMaxSplits : (int)most;
 }
-int split_count(const diffqkv_shape& s, int max_seqlen, int total_q) {
+int split_count(const diffqkv_shape& s, int max_seqlen, int total_q, int least) {
   const long long blocks = ((long long)total_q * s.n_q + kRows - 1) / kRows;
   long long want = (296 + blocks - 1) / blocks;
-  if (want > max_seqlen / 256) want = max_seqlen / 256;
+  if (want > max_seqlen / least) want = max_seqlen / least;
   if (want > most_splits(s, total_q)) want = most_splits(s, total_q);
   return want < 1 ? 1 : (int)want;
 }
@@ -396,7 +397,7 @@ cudaError_t launch_extend_simt(const DecodeParams& d, const diffqkv_shape& s, co
   p.window = range ? range->window : 0; p.sinks = range ? range->sinks : 0;
   long long most = d.cache.max_seqlen;  // tokens that the rows of a tile see
   if (range && (long long)range->window + range->sinks + p.T - 1 < most) most = (long long)range->window + range->sinks + p.T - 1;
-  p.splits = split_count(s, (int)most, total_q);
+  p.splits = split_count(s, (int)most, total_q, range ? 128 : 256);
   p.split_tokens = (int)(((most + p.splits - 1) / p.splits + kTok - 1) / kTok * kTok);
   p.out = out; p.out_is_f32 = s.out_dtype == DIFFQKV_F32; p.lse = lse;
   p.part_lse = static_cast<float*>(workspace);

@@ -19,6 +19,7 @@
 // Heads of more than 64 vectors are read a second time.
 #include "attn_math.cuh"
 #include "common.cuh"
+#include "ptx.cuh"
 #include "rope.cuh"
 
 namespace diffqkv {
@@ -97,6 +98,8 @@ __global__ void __launch_bounds__(kRopeThreads, 8) norm_rope_kernel(const RopePa
   float* coef_s = reinterpret_cast<float*>(smem4);
   const int tid = threadIdx.x;
   const int t = blockIdx.x;  // row
+
+  ptx::grid_dependency_wait();  // launched before the work in front of it has ended
 
   // lane x of a head's lanes has tasks x, x + lanes, ...
   const int half = p.rot >> 1, rot_tasks = m.rot_tasks, rest = m.rest, tasks = m.tasks;
@@ -331,10 +334,19 @@ __global__ void __launch_bounds__(kRopeThreads, 8) norm_rope_kernel(const RopePa
 template <typename T, typename W>
 cudaError_t launch(const RopeParams& p, const NormParams& m, cudaStream_t stream) {
   const size_t smem = m.tasks <= m.lanes ? sizeof(float4) * 2 * Pack<T>::N * m.tasks : sizeof(float2) * (p.rot / 2 + 1);
-  if (p.interleaved) norm_rope_kernel<T, W, false><<<(unsigned)p.total_q, kRopeThreads, smem, stream>>>(p, m);
-  else norm_rope_kernel<T, W, true><<<(unsigned)p.total_q, kRopeThreads, smem, stream>>>(p, m);
-  count_launch();
-  return cudaGetLastError();
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)p.total_q);
+  cfg.blockDim = dim3(kRopeThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  const cudaError_t err = cudaLaunchKernelEx(&cfg, p.interleaved ? norm_rope_kernel<T, W, false> : norm_rope_kernel<T, W, true>, p, m);
+  if (err == cudaSuccess) count_launch();
+  return err;
 }
 
 }  // namespace
