@@ -1497,7 +1497,10 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
-  const bool wide_first = thin_blocks == 0 || total_q > (long long)s.batch * pl.thin_max || (range && range->groups > 0);
+  // Prefixes shared by many rows are long chunks: ranged steps with groups begin with these, whose start would otherwise
+  // fall into the other kernel's stream of tiles (64 single rows behind 16k tokens: 111 -> 100 us).
+  p.alone = range && total_q <= pl.thin_max;
+  const bool wide_first = !p.alone && (thin_blocks == 0 || total_q > (long long)s.batch * pl.thin_max || (range && range->groups > 0));
   CUtensorMap mk_rows, mv_rows;  // of whole rows, for the kernels that take them
   p.head_groups = (int)(tok_extent / 8);
   p.k_rows = make_row_map(&mk_rows, c.k_cache, s.d_qk, tok_extent, s.n_k, c.num_blocks, c.k_stride_tok, c.k_stride_head,
@@ -1525,8 +1528,12 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
     return launch_extend_thin(mq_thin, p.k_rows ? mk_rows : mk, p.v_rows ? mv_rows : mv, p, s.d_qk, s.d_v, thin_blocks,
                               wide_first, stream);
   };
-  if ((err = wide_first ? launch_wide() : launch_thin()) != cudaSuccess) return err;
-  if ((err = wide_first ? launch_thin() : launch_wide()) != cudaSuccess) return err;
+  if (p.alone) {
+    if ((err = launch_thin()) != cudaSuccess) return err;
+  } else {
+    if ((err = wide_first ? launch_wide() : launch_thin()) != cudaSuccess) return err;
+    if ((err = wide_first ? launch_thin() : launch_wide()) != cudaSuccess) return err;
+  }
   p.list = wide;
   cfg.dynamicSmemBytes = 0;
   cfg.numAttrs = 1;
@@ -1541,7 +1548,8 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
     const long long groups = kCombineThreads / (s.d_v / 8), rows = (long long)total_q * s.n_q, fill = sm_count() * kCombineBlocks;
     cfg.gridDim = dim3((unsigned)((rows + groups - 1) / groups < fill ? (rows + groups - 1) / groups : fill));
     cfg.blockDim = dim3(kCombineThreads);
-    err = cudaLaunchKernelEx(&cfg, s.d_v == 64 ? extend_combine_kernel<64> : extend_combine_kernel<128>, p, thin, thin_blocks, blocks);
+    err = cudaLaunchKernelEx(&cfg, s.d_v == 64 ? extend_combine_kernel<64> : extend_combine_kernel<128>, p, thin, thin_blocks,
+                             p.alone ? 0 : blocks);
   }
   if (err != cudaSuccess) return err;
   count_launch();

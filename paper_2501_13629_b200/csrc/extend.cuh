@@ -80,6 +80,7 @@ struct ExtendParams {
   // `entries`, the sequences, whose own tokens begin behind their group's prefix.
   int window, sinks, sink_tiles, sink_few;  // the sinks in tiles of this kernel and of extend_few.cu
   int few_stages;
+  int alone;  // the kernel of few rows comes without the other one: too few rows in all for a long chunk
   int groups, entries;
   const int* cu_groups;
   const int* prefix_lens;

@@ -90,7 +90,7 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
   // ---- this block's share of the list
   using Seq = SeqOf<true>;
   Seq my;
-  const RangedStart at = ranged_start(p, sc.scan, my, false);
+  const RangedStart at = ranged_start(p, sc.scan, my, p.alone && blockIdx.x == 0);
   const uint32_t total = at.few;
   // Equal shares of the list, cut wherever they end; or, where that costs no block more than six tiles, equal chunks that
   // begin with their item (see extend_thin.cu), so that every block has one segment at most.
