@@ -40,6 +40,7 @@
 // of the scores.  Earlier forms of this kernel took 415 to 850 us with them for an eighth to a half of the scores.
 // Heads of 64 channels (32/4/16), the same chunks: 396 us without a pause, 580 TFLOP/s; 64-channel keys with 128-channel
 // values 471 us, 730 TFLOP/s (half the products, as many exponentials).
+#include <algorithm>
 #include <atomic>
 #include <numeric>
 #include <type_traits>
@@ -1415,7 +1416,7 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
     const long long entries = (long long)range->groups + s.batch, units = pl.groups / pl.parts;
     const long long items = total_q / (2 * pl.T) * (range->groups > 0 ? 2LL : 1LL) + entries;
     if (items * units * (kItemCost + kWideCost * (c.max_seqlen / kKT + 2LL)) > 0x7fffffffLL ||
-        entries * units * (kFewItemCost + c.max_seqlen / kFewT + 2LL) > 0x7fffffffLL)
+        entries * units * (kFewItemCost + kFewMostCost * (c.max_seqlen / kFewT + 2LL)) > 0x7fffffffLL)
       return cudaErrorNotSupported;
   }
   CUtensorMap mq, mq_thin, mk, mv;
@@ -1468,7 +1469,14 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
   ExtendList wide, thin;
   place(pl, s.d_v, static_cast<char*>(workspace), &wide, &thin);
   if (range) {
-    p.thin_weight *= 0.5f;  // extend_few.cu's tiles have half the tokens
+    // A tile of a few rows takes as long as its bytes, 1.85 thousand cycles for 48 KB, or as its products: about 2.2 thousand
+    // cycles for four groups of 16 rows and 128 channels of either kind, that is four or five units, half of that for two
+    // groups and twice for eight.
+    const long long bytes = kFewT * 2LL * (p.k_parts * s.d_qk + p.v_parts * s.d_v);
+    const int memory = (int)((4 * bytes + 24576) / 49152), products[3] = {2, 5, 10}, d = s.d_qk + s.d_v;
+    for (int i = 0; i < 3; ++i)
+      p.few_cost[i] = std::min(std::max(std::max(memory, (products[i] * d + 128) / 256), 1), kFewMostCost);
+    p.thin_weight *= 0.5f / p.few_cost[0];  // tiles of half the tokens, in these units
     p.window = range->window;
     p.sinks = range->sinks;
     p.sink_tiles = (int)(((long long)range->sinks + kKT - 1) / kKT);

@@ -79,7 +79,7 @@ struct ExtendParams {
   // its own position.  The first `groups` entries of the list are the prefixes of groups of sequences, the others, up to
   // `entries`, the sequences, whose own tokens begin behind their group's prefix.
   int window, sinks, sink_tiles, sink_few;  // the sinks in tiles of this kernel and of extend_few.cu
-  int few_stages;
+  int few_stages, few_cost[3];
   int alone;  // the kernel of few rows comes without the other one: too few rows in all for a long chunk
   int groups, entries;
   const int* cu_groups;
@@ -131,8 +131,9 @@ __device__ __forceinline__ long long last_tile(int cost, int nt, int extra) {
 constexpr int kWideCost = 2, kNarrowCost = 1, kItemCost = 5;
 // Likewise for thin items, in tiles: a block's second item costs it about as much as five more tiles.
 constexpr int kThinItemCost = 5;
-// The ranged steps' few rows go by tiles of 64 tokens; an item costs about two of them more.
-constexpr int kFewT = 64, kFewItemCost = 2;
+// The ranged steps' few rows go by tiles of 64 tokens, whose cost is a quarter of what one of three 128-channel heads takes
+// when memory bounds it (see few_cost); an item costs about two such more.
+constexpr int kFewT = 64, kFewItemCost = 8, kFewMostCost = 16;
 constexpr int kFewCols = 128;  // as kThinCols
 
 // sum of floor((a x + b) / m) for x = 0 .. n - 1 with a, b >= 0, m > 0: the Euclid-like recursion on (m, a).  Not inlined:
@@ -287,6 +288,13 @@ struct SeqOf<true> {
       n = 0;
     }
   }
+  // cost of one of extend_few.cu's tiles, by its groups of 16 rows: up to two, up to four, more
+  __device__ int few_cost(const ExtendParams& p) const {
+    const int groups = p.parts * ((rows * p.G + 15) >> 4);
+    return p.few_cost[groups <= 2 ? 0 : groups <= 4 ? 1 : 2];
+  }
+  // and of a unit of it
+  __device__ int few_unit(const ExtendParams& p) const { return thin_tiles > 0 ? thin_tiles * few_cost(p) + kFewItemCost : 0; }
   // of extend_few.cu's tiles, behind the sinks, those that no row sees
   __device__ int skip_few(const ExtendParams& p) const { return max(low(p, 0) / kFewT - p.sink_few, 0); }
   // first token behind the sinks that the chunk's row `tok` sees
@@ -388,7 +396,7 @@ __device__ __forceinline__ RangedStart ranged_start(const ExtendParams& p, Range
     if (r.first + i >= p.entries) continue;
     my.load(p, r.first + i);
     if (my.bad && reports) report(p.dev_status, DIFFQKV_ERR_INDEX);
-    if (my.thin_tiles > 0) few += p.n_units * (my.thin_tiles + kFewItemCost);
+    few += p.n_units * my.few_unit(p);
     if (my.n > 0) wide += p.n_units * (uint32_t)my.cost(p);
   }
   const unsigned long long mine = (unsigned long long)wide << 32 | few;

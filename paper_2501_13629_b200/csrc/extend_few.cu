@@ -100,7 +100,7 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
   if (total > 0 && (int)blockIdx.x < grid) {
     const int items = at.single ? min(at.busy * p.n_units, grid) : grid;
     if (items < grid) {
-      const uint32_t tiles = total - items * kItem;
+      const uint32_t tiles = (total - items * kItem + p.few_cost[0] - 1) / (uint32_t)p.few_cost[0];  // or more
       chunk = (int)((tiles + grid - items - 1) / (uint32_t)(grid - items));
       if (chunk > (int)(tiles / (uint32_t)grid) + 6) chunk = 0;
     }
@@ -124,7 +124,7 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       w0 = blockIdx.x;
       w1 = w0 < all ? w0 + 1 : w0;
     } else {
-      blocks = ranged_shares(total, grid, kItem + 1);
+      blocks = ranged_shares(total, grid, kItem + kFewMostCost);
       if ((int)blockIdx.x < blocks) {
         w0 = ranged_share_start(total, blockIdx.x, blocks);
         w1 = ranged_share_start(total, blockIdx.x + 1, blocks);
@@ -137,8 +137,7 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     return;
   }
   ranged_seek(p, sc.scan, at, my, w0, before, [&](const Seq& s) -> uint32_t {
-    if (s.thin_tiles == 0) return 0;
-    return p.n_units * (uint32_t)(chunk > 0 ? (s.thin_tiles + chunk - 1) / chunk : s.thin_tiles + kItem);
+    return p.n_units * (uint32_t)(chunk > 0 ? (s.thin_tiles + chunk - 1) / chunk : s.few_unit(p));
   });
   __syncthreads();
 
@@ -163,22 +162,23 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     ExtendMeta m = {};
     int e = sc.scan.e, u, chunk_lo = 0;
     Seq x = sc.scan.seq;
-    int nt = x.thin_tiles;
+    int nt = x.thin_tiles, cost = x.few_cost(p);
     uint32_t item_lo = sc.scan.lo;
     {
-      const uint32_t in = w0 - item_lo, per = chunk > 0 ? (nt + chunk - 1) / chunk : nt + kItem;
+      const uint32_t in = w0 - item_lo, per = chunk > 0 ? (nt + chunk - 1) / chunk : cost * nt + kItem;
       u = (int)(in / per);
       if (chunk > 0) chunk_lo = (int)(in - u * per) * chunk;
       else item_lo += u * per;
     }
     auto next_item = [&]() {
-      item_lo += nt + kItem;
+      item_lo += cost * nt + kItem;
       if (item_lo >= w1 || ++u < p.n_units) return;
       u = 0;
       do {
         if (++e >= p.entries) return;
         x.load(p, e);
         nt = x.thin_tiles;
+        cost = x.few_cost(p);
       } while (nt == 0);
     };
     auto hand_out = [&](const FewSegment& d, volatile int* abort) -> bool {
@@ -198,8 +198,8 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         ta = chunk_lo;
         tb = min(nt, chunk_lo + chunk);
       } else {
-        ta = w0 > item_lo ? item_tile(w0 - item_lo, 1, nt, kItem) : 0;
-        tb = item_tile(w1 - item_lo, 1, nt, kItem);
+        ta = w0 > item_lo ? item_tile(w0 - item_lo, cost, nt, kItem) : 0;
+        tb = item_tile(w1 - item_lo, cost, nt, kItem);
         if (ta >= tb) {  // the share begins, or ends, within the item's own cost
           next_item();
           continue;
@@ -215,7 +215,7 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       if (ta == 0 && tb < nt) {
         m.rows = p.parts * x.rows * p.G; m.part_rows = x.rows * p.G; m.row_lo = x.lo; m.head0 = head0;
         m.parts = chunk > 0 ? (nt + chunk - 1) / chunk
-                            : share_of((long long)item_lo + last_tile(1, nt, kItem), total, blocks) - (int)blockIdx.x + 1;
+                            : share_of((long long)item_lo + last_tile(cost, nt, kItem), total, blocks) - (int)blockIdx.x + 1;
       }
       if (ta == 0 && p.groups > 0 && lane == 0)
         p.refs[((x.dst == kDstPrefix ? 0LL : p.total_q) + x.lo) * p.n_units + u] = {(int)blockIdx.x, tb < nt ? m.parts : 1};
