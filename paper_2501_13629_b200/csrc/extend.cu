@@ -1476,7 +1476,7 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
     const int memory = (int)((4 * bytes + 24576) / 49152), products[3] = {2, 5, 10}, d = s.d_qk + s.d_v;
     for (int i = 0; i < 3; ++i)
       p.few_cost[i] = std::min(std::max(std::max(memory, (products[i] * d + 128) / 256), 1), kFewMostCost);
-    p.thin_weight *= 0.5f / p.few_cost[0];  // tiles of half the tokens, in these units
+    p.thin_weight *= 0.42f / p.few_cost[0];  // tiles of half the tokens, in these units; the best of five for two mixtures
     p.window = range->window;
     p.sinks = range->sinks;
     p.sink_tiles = (int)(((long long)range->sinks + kKT - 1) / kKT);
