@@ -783,7 +783,8 @@ def diffqkv_extend_window(q: torch.Tensor, cu_q: torch.Tensor, cache: KVCache, n
                           stream: Optional[torch.cuda.Stream] = None):
     """diffqkv_extend in which a row sees the last ``window`` tokens up to its own and the first ``sinks`` ones.  Pages
     that hold no token which a row sees need not exist (entry -1)."""
-    return _extend("diffqkv_extend_window", (window, sinks), _raw.diffqkv_extend_window_workspace_bytes, q, cu_q, cache, n_k,
+    reach = tuple(max(-1, min(x, 2 ** 31 - 1)) for x in (window, sinks))  # the call takes 32 bits, which ctypes cuts to
+    return _extend("diffqkv_extend_window", reach, _raw.diffqkv_extend_window_workspace_bytes, q, cu_q, cache, n_k,
                    n_v, scale, workspace, out, lse, dev_status, out_dtype, stream)
 
 

@@ -1145,6 +1145,7 @@ extend_merge_kernel(const ExtendParams p, const ExtendList few, const int rows_e
   }
   __syncthreads();
   ptx::grid_dependency_wait();
+  if (p.refs[2LL * p.total_q * p.n_units].first) return;  // left out
   auto ref_of = [&](int r, int unit, int k) -> ItemRef {
     const Row& w = row_s[r];
     if (w.has < (k == 0 ? 2 : 1)) return {0, 0};
@@ -1364,7 +1365,7 @@ size_t place_buffers(const diffqkv_shape& s, const Plan& pl, int total_q, char* 
     p->buffer[i].o = reinterpret_cast<float*>(base + i * (lse + o) + lse);
   }
   if (p) p->refs = reinterpret_cast<ItemRef*>(base + 2 * (lse + o));
-  return 2 * (lse + o) + up256(2 * sizeof(ItemRef) * (size_t)total_q * (pl.groups / pl.parts));
+  return 2 * (lse + o) + up256(sizeof(ItemRef) * (2 * (size_t)total_q * (pl.groups / pl.parts) + 1));
 }
 
 bool dims_supported(const diffqkv_shape& s) {

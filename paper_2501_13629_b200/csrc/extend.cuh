@@ -85,7 +85,7 @@ struct ExtendParams {
   const int* cu_groups;
   const int* prefix_lens;
   RowBuffer buffer[2];  // kDstPrefix - 1, kDstOwn - 1
-  ItemRef* refs;        // [2][total_q][n_units]
+  ItemRef* refs;        // [2][total_q][n_units], and one whose `first` says that the step has been left out
 };
 
 // Rows of sequence b: first row, number, tokens cached before; false when they do not fit.
@@ -254,13 +254,14 @@ struct SeqOf<true> {
   int rows, thin_tiles;
   int end, start;  // its tokens: from start (or the first) on, below end
   int tab, dst;    // row of the page table, kDst...
-  bool bad;
+  bool bad, back;  // does not fit; ends in front of its beginning
   __device__ void load(const ExtendParams& p, int x) {
     start = 0;
     dst = kDstOut;
     if (x < p.groups) {  // every row of the group sees the whole prefix: as if it were cached before any of them
       int hi;
       bad = false;  // of a group that does not fit every sequence with rows says so
+      back = p.cu_groups[x + 1] < p.cu_groups[x];
       n = group_rows(p, x, lo, hi, tab, past) && past > 0 ? hi - lo : 0;
       if (n == 0) past = 0;
       end = past;
@@ -268,6 +269,7 @@ struct SeqOf<true> {
     } else {
       tab = x - p.groups;
       bad = !load_rows(p, tab, lo, n, past);
+      back = bad && p.cu_q[tab + 1] < lo;
       if (!bad && n > 0) {
         int g_lo, g_hi;
         start = group_prefix(p, tab, lo, n, past, g_lo, g_hi);
@@ -381,7 +383,8 @@ struct RangedScan {
   int e;
   uint32_t lo;
 };
-// Sums up both lists; `my` is the thread's first entry.  Holds a barrier, and report's that an entry does not fit.
+// Sums up both lists, which are empty where ends are out of order: rows may then be several entries' own, and the lists longer
+// than the host has counted.  `my` is the thread's first entry.  Holds a barrier, and report's that an entry does not fit.
 template <int kWarps>
 __device__ __forceinline__ RangedStart ranged_start(const ExtendParams& p, RangedScan<kWarps>& sc, SeqOf<true>& my, bool reports) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -390,12 +393,14 @@ __device__ __forceinline__ RangedStart ranged_start(const ExtendParams& p, Range
   r.single = per_thread == 1;
   r.first = tid * per_thread;
   uint32_t wide = 0, few = 0;
+  bool back = false;
   my.n = my.thin_tiles = 0;
 #pragma unroll 1
   for (int i = per_thread - 1; i >= 0; --i) {
     if (r.first + i >= p.entries) continue;
     my.load(p, r.first + i);
-    if (my.bad && reports) report(p.dev_status, DIFFQKV_ERR_INDEX);
+    if ((my.bad || my.back) && reports) report(p.dev_status, DIFFQKV_ERR_INDEX);
+    back |= my.back;
     few += p.n_units * my.few_unit(p);
     if (my.n > 0) wide += p.n_units * (uint32_t)my.cost(p);
   }
@@ -411,7 +416,8 @@ __device__ __forceinline__ RangedStart ranged_start(const ExtendParams& p, Range
     sc.sum[warp] = x;
     sc.busy[warp] = busy;
   }
-  __syncthreads();
+  back = __syncthreads_or(back);
+  if (reports && p.groups > 0 && tid == 0) p.refs[2LL * p.total_q * p.n_units].first = back;
   unsigned long long before = x - mine, all = 0;
   r.busy = 0;
 #pragma unroll 1
@@ -420,6 +426,7 @@ __device__ __forceinline__ RangedStart ranged_start(const ExtendParams& p, Range
     all += sc.sum[w];
     r.busy += sc.busy[w];
   }
+  if (back) all = 0;
   r.wide = (uint32_t)(all >> 32);
   r.few = (uint32_t)all;
   r.before_wide = (uint32_t)(before >> 32);

@@ -217,6 +217,54 @@ def test_sequences_that_do_not_fit(api, dtype, dims):
     call([0, 3, 5], [200, 1 << 30], bad=[3, 4])
 
 
+@pytest.mark.parametrize("bad", [None, 0, 2])
+def test_a_few_rows_in_all(api, bad):
+    """Steps that one kernel takes alone, with a sequence that does not fit among them."""
+    step = Step(api, [300, 310, 290, 50], [1, 0, 2, 1], 8, 2, 4, 128, 128, seed=7, pad=2)
+    share(step, [0, 3], [200])
+    if bad is not None:
+        step.lens[bad] = -1 if bad else 199
+    out, status = torch.full((step.total_q, 8, 128), 77.0, dtype=BF16, device="cuda"), ints([0])
+    api.diffqkv_extend_shared(step.q, step.cu, step.cache, ints([0, 3]), ints([200]), 2, 4, 0.1, out=out, dev_status=status)
+    assert int(status.item()) == (0 if bad is None else 1 << api.ERR_INDEX)
+    check(step, out, None, 0.1, joined=True, only=[b for b in range(4) if b != bad])
+    if bad is not None:
+        assert bool((out[step.cu_host[bad]:step.cu_host[bad + 1]] == 77.0).all())
+    assert bool((out[step.rows:] == 77.0).all())
+
+
+@pytest.mark.parametrize("groups,size", [(450, 2), (3, 300)])
+def test_more_entries_than_threads(api, groups, size):
+    r = random.Random(groups)
+    ends, prefix, past = [0], [], []
+    for _ in range(groups):
+        p = r.randint(0, 90)
+        past += [p + r.randint(0, 60) for _ in range(size)]
+        ends.append(ends[-1] + size)
+        prefix.append(p)
+    new = [r.choice([0, 1, 1, 2, 30]) for _ in past]
+    step = Step(api, past, new, 8, 2, 4, 64, 64, page=16, seed=groups, pad=2)
+    run(api, share(step, ends, prefix), ends, prefix)
+
+
+def test_groups_that_go_back(api):
+    """cu_seqs decreases, so that groups of rows overlap: reported, and the step is left out."""
+    step = Step(api, [300, 310, 290, 305, 20, 40], [3, 4, 2, 1, 5, 60], 8, 2, 4, 128, 128, seed=7, pad=4)
+    share(step, [0, 4], [200])
+    nbytes = api.diffqkv_extend_shared_workspace_bytes(api.make_shape(6, 8, 2, 4, 128, 128, BF16, BF16, 0.1), step.total_q)
+    ws = torch.zeros(nbytes, dtype=torch.uint8, device="cuda")
+    for groups, back in (([0, 4, 4, 4], False), ([0, 4, 2, 4], True), ([2, 4, 0, 4], True), ([0, 4, 4, 6], False)):
+        out, status = torch.full((step.total_q, 8, 128), 77.0, dtype=BF16, device="cuda"), ints([0])
+        api.diffqkv_extend_shared(step.q, step.cu, step.cache, ints(groups), ints([200, 200, 0]), 2, 4, 0.1, out=out,
+                                  workspace=ws, dev_status=status)
+        assert int(status.item()) == (1 << api.ERR_INDEX if back else 0)
+        if back:
+            assert bool((out == 77.0).all())
+        else:
+            check(step, out, None, 0.1, joined=True)
+        assert bool((out[step.rows:] == 77.0).all())
+
+
 def test_rows_out_of_order_are_not_written(api):
     """cu_q decreases inside a group: its sequences' rows are not the group's."""
     step = Step(api, [300, 310, 290], [3, 4, 2], 8, 2, 4, 128, 128, seed=7, pad=4)

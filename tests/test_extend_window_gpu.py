@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from ragged import BF16, F32, Step, ints
-from ranged import check, forget
+from ranged import HALF_STEP, attend64, check, forget
 
 pytestmark = pytest.mark.gpu
 
@@ -181,6 +181,64 @@ def test_sequences_that_do_not_fit(api):
         assert int(status.item()) == 1 << api.ERR_INDEX
         assert bool((out[3:43] == 77.0).all()) and bool((out[44:] == 77.0).all())
         check(step, out, None, 0.1, 128, 2, only=(0, 2))
+
+
+@pytest.mark.parametrize("new,bad,rows", [([1, 2, 1], 1, slice(1, 3)), ([1, 0, 1], 1, slice(0, 0)), ([2, 1, 1], 0, slice(0, 2))])
+def test_a_few_rows_in_all_that_do_not_fit(api, new, bad, rows):
+    """Steps that one kernel takes alone."""
+    step = Step(api, [300, 200, 400], new, 8, 2, 4, 128, 128, seed=7, pad=1).fill()
+    step.lens[bad] = step.max_seqlen + 1
+    out, status = torch.full((step.total_q, 8, 128), 77.0, dtype=BF16, device="cuda"), ints([0])
+    api.diffqkv_extend_window(step.q, step.cu, step.cache, 2, 4, 0.1, 128, sinks=2, out=out, dev_status=status)
+    assert int(status.item()) == 1 << api.ERR_INDEX
+    assert bool((out[rows] == 77.0).all()) and bool((out[step.rows:] == 77.0).all())
+    check(step, out, None, 0.1, 128, 2, only=[b for b in range(3) if b != bad])
+
+
+@pytest.mark.parametrize("batch", [300, 700, 1200])
+def test_more_sequences_than_threads(api, batch):
+    r = random.Random(batch)
+    past = [r.choice([0, r.randint(0, 300)]) for _ in range(batch)]
+    new = [r.choice([0, 1, 1, 2, 40]) if b % 9 else 1 for b in range(batch)]
+    step = Step(api, past, new, 8, 2, 4, 64, 64, seed=batch, pad=2).fill()
+    run(api, forget(step, 60, 3), 60, 3)
+
+
+def test_offsets_past_32_bits(api):
+    """A pool of more than 2^32 bytes and elements, of which a window lies at the end."""
+    past, n_k, d = 2_100_000, 16, 128
+    k, v = (torch.empty((1, n_k, past + 128, d), dtype=BF16, device="cuda") for _ in range(2))  # 4.3 G elements each
+    window, rows = 200, 3
+    for x in (k, v):
+        x[:, :, :4].normal_()
+        x[:, :, past - window:past + rows].normal_()
+    q = torch.randn((rows, n_k, d), device="cuda").to(BF16)
+    cache = api.KVCache(k, v, ints([past]), past + rows)
+    out = torch.empty_like(q)
+    api.diffqkv_extend_window(q, ints([0, rows]), cache, n_k, n_k, 0.1, window, sinks=4, out=out)
+    seen = torch.cat([torch.arange(4, device="cuda"), torch.arange(past - window + 1, past + rows, device="cuda")])
+    pos = past + torch.arange(rows, device="cuda")[:, None]
+    sees = (seen[None] <= pos) & ((seen[None] < 4) | (seen[None] > pos - window))
+    kd, vd = (x[0][:, seen].double().transpose(0, 1) for x in (k, v))
+    ref, _, mean_abs, big = attend64(q, kd, vd, 0.1, sees)
+    weight = 2 * (d + 16) * 2.0 ** -24 * max(big, 1.0) + (len(seen) + 16) * 2.0 ** -24 + HALF_STEP[BF16]
+    bound = weight * mean_abs * (1 + weight)
+    bound = bound + HALF_STEP[BF16] * (ref.abs() + bound)
+    assert bool(((out.double() - ref).abs() <= bound).all())
+
+
+def test_rows_given_to_many_sequences_at_once(api):
+    """cu_q goes back and forth, so that every other sequence has all rows: far more work than the step's rows can be.  It is
+    reported, and left out."""
+    n, pairs, tokens = 32768, 300, 1 << 20
+    q = torch.zeros((n, 8, 64), dtype=BF16, device="cuda")
+    pool = torch.zeros((2, 8, 16, 64), dtype=BF16, device="cuda")
+    table = torch.zeros((2 * pairs, tokens // 16), dtype=torch.int32, device="cuda")
+    cache = api.KVCache(pool, pool.clone(), ints([tokens - n] * (2 * pairs)), tokens, page_table=table, page_size=16)
+    status, out = ints([0]), torch.full((n, 8, 64), 77.0, dtype=BF16, device="cuda")
+    api.diffqkv_extend_window(q, ints([0, n] * pairs + [0]), cache, 8, 8, 0.1, tokens - 1, out=out, dev_status=status)
+    assert int(status.item()) == 1 << api.ERR_INDEX and api.last_extend_kernel() == 3
+    assert bool((out == 77.0).all())
 
 
 def test_a_missing_page_inside_the_window_is_reported(api):

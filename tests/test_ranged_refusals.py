@@ -165,6 +165,9 @@ def test_wrappers_of_the_attention_calls(api, recorded):
     window = lambda q=z(5, 8, 64), cu=ints(3), **kw: api.diffqkv_extend_window(  # noqa: E731
         q, cu, kv(api), 2, 4, 0.125, 16, sinks=2, stream=STREAM, **kw)
     assert made(recorded, window)[2:5] == (5, 16, 2)
+    far = lambda window, sinks: made(recorded, lambda: api.diffqkv_extend_window(  # noqa: E731
+        z(5, 8, 64), ints(3), kv(api), 2, 4, 0.125, window, sinks=sinks, stream=STREAM))[3:5]
+    assert far(2 ** 32 + 5, 2 ** 63 - 1) == (2 ** 31 - 1, 2 ** 31 - 1) and far(-2 ** 32 + 5, -2 ** 32) == (-1, -1)
     refused(recorded, lambda: window(q=z(5, 8, 32)))
     refused(recorded, lambda: window(q=z(5, 8, 64, dtype=F32)))
     refused(recorded, lambda: window(cu=ints(4)))
