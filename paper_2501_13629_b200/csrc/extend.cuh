@@ -79,7 +79,7 @@ struct ExtendParams {
   // its own position.  The first `groups` entries of the list are the prefixes of groups of sequences, the others, up to
   // `entries`, the sequences, whose own tokens begin behind their group's prefix.
   int window, sinks, sink_tiles, sink_few;  // the sinks in tiles of this kernel and of extend_few.cu
-  int few_stages, few_cost[3];
+  int few_stages, few_cost[3], item_cost;
   int alone;  // the kernel of few rows comes without the other one: too few rows in all for a long chunk
   int groups, entries;
   const int* cu_groups;
@@ -129,6 +129,16 @@ __device__ __forceinline__ long long last_tile(int cost, int nt, int extra) {
 // rows are written out and the pipeline fills again).  Measured on prompts of 1.5k-2k rows over 0-6k tokens: 1.85 us a
 // tile, 4-5 us an item; without the last, blocks with many short items ended 13 % late, 4 to 7 makes 1 %.
 constexpr int kWideCost = 2, kNarrowCost = 1, kItemCost = 5;
+// A step with groups has items of very different lengths, a prefix and a chunk's own few tiles, and rows that are written in
+// fp32: 6, 7, 9 and 11 for an item of chunks of 150-600 rows behind two prefixes of 3k-5k tokens (32/4/16 heads, 64 and 128
+// channels) make it 313, 304, 288 and 296 us, 5 makes it 330; 16 chunks of 100-300 rows behind 8k tokens 538, 515, 495, 496,
+// not 574.  Windows, whose items are alike, take 296 us with 5 and 299 with 9.
+constexpr int kSharedItemCost = 9;
+template <bool kRanged>
+__device__ __forceinline__ int item_cost(const ExtendParams& p) {
+  if constexpr (kRanged) return p.item_cost;
+  return kItemCost;
+}
 // Likewise for thin items, in tiles: a block's second item costs it about as much as five more tiles.
 constexpr int kThinItemCost = 5;
 // The ranged steps' few rows go by tiles of 64 tokens, whose cost is a quarter of what one of three 128-channel heads takes
@@ -326,7 +336,7 @@ struct SeqOf<true> {
       }
       if (i > x0) tiles -= steps(p, i - x0, c);
     }
-    return kWideCost * tiles + kItemCost * i;
+    return kWideCost * tiles + p.item_cost * i;
   }
   __device__ bool wide(const ExtendParams& p, int i) const { return n - i * 2 * p.T > p.T; }
   __device__ int tiles(const ExtendParams& p, int i) const {  // K/V tiles of item i
@@ -334,7 +344,7 @@ struct SeqOf<true> {
   }
   __device__ int cost(const ExtendParams& p) const {  // of one head group
     if (n == 0) return 0;
-    return cost_before(p, items - 1) + kItemCost + (wide(p, items - 1) ? kWideCost : kNarrowCost) * tiles(p, items - 1);
+    return cost_before(p, items - 1) + p.item_cost + (wide(p, items - 1) ? kWideCost : kNarrowCost) * tiles(p, items - 1);
   }
 };
 template <bool kRanged>
@@ -367,7 +377,7 @@ __device__ __forceinline__ int ranged_wide_teams(const ExtendParams& p, uint32_t
     const float w = (float)wide * p.team, f = (float)few * p.thin_weight;
     n = min(max((int)(n * __fdividef(w, w + f) + 0.5f), 1), n - 1);
   }
-  return ranged_shares(wide, n, kItemCost + kWideCost);
+  return ranged_shares(wide, n, p.item_cost + kWideCost);
 }
 struct RangedStart {
   uint32_t wide, few;        // lengths of the two lists
