@@ -700,7 +700,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
               const int at = kRanged && p.v_rows ? (r / 8) * 2048 + half * 1024 + (r % 8) * 128 : half * (kKT * 128) + r * 128;
               uint4* dst = reinterpret_cast<uint4*>(v_s + vslot * kTBytes + at);
 #pragma unroll
-              for (int e = 0; e < 8; ++e) dst[e] = make_uint4(0, 0, 0, 0);
+              for (int e = 0; e < 8; ++e) dst[e ^ (lane & 7)] = make_uint4(0, 0, 0, 0);  // every bank at once
             }
           }
           ptx::fence_proxy_async();

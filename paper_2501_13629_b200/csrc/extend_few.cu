@@ -405,7 +405,7 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
               unsigned char* dst = smem + stage * stage_bytes + v_off + row_at(r + lane, HV);
 #pragma unroll 1
               for (int c = 0; c < HV * 8; ++c)
-                *reinterpret_cast<uint4*>(dst + (c >> 3) * half_at + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
+                *reinterpret_cast<uint4*>(dst + (c >> 3) * half_at + (((c ^ lane) & 7) << 4)) = make_uint4(0, 0, 0, 0);
             }
             ptx::fence_proxy_async();  // before the next TMA write
             __syncwarp();
