@@ -169,37 +169,54 @@ def test_two_graphs_side_by_side(api):
 
 
 def test_pages_behind_the_window_given_up(api):
-    """A cache of windowed layers alone: pages that no later row sees lose their entries and are used again."""
+    """A cache of windowed layers alone: pages that no later row sees lose their entries and are used again.  A sequence with
+    such gaps is forked and freed like any other."""
     gen = torch.Generator("cuda").manual_seed(3)
     rnd = lambda *shape: torch.randn(shape, generator=gen, device="cuda").to(BF16)  # noqa: E731
-    pages = 9
-    k, v = torch.empty((pages, N_K, PAGE, D), dtype=BF16, device="cuda"), torch.empty((pages, N_V, PAGE, D), dtype=BF16, device="cuda")
-    table, lens, refs, status = torch.full((1, 30), -1, dtype=torch.int32, device="cuda"), ints([0]), ints([0] * pages), ints([0])
+    pages, nan = 9, float("nan")
+    k, v = (torch.full((pages, h, PAGE, D), nan, dtype=BF16, device="cuda") for h in (N_K, N_V))
+    table, lens, refs, status = torch.full((2, 30), -1, dtype=torch.int32, device="cuda"), ints([0, 0]), ints([0] * pages), ints([0])
     cache = api.KVCache(k, v, lens, 30 * PAGE, page_table=table, page_size=PAGE)
-    keys, values, length = [], [], 0
-    for n in [50, 1, 1, 30, 1, 40, 1, 1, 60, 1, 1, 55, 1]:
-        q, k_new, v_new, cu = rnd(n, N_Q, D), rnd(n, N_K, D), rnd(n, N_V, D), ints([0, n])
+    tokens = [([], []), ([], [])]
+    length = [0, 0]
+
+    def step(new):
+        n = sum(new)
+        q, k_new, v_new, cu = rnd(n, N_Q, D), rnd(n, N_K, D), rnd(n, N_V, D), ints([0, new[0], n])
         api.diffqkv_pages_reserve(cu, cache, refs, N_K, N_V, dev_status=status)
         turned = api.diffqkv_norm_rope_append(q, k_new, v_new, cu, cache, None, None, None, EPS, dev_status=status)
         out = api.diffqkv_extend_window(turned, cu, cache, N_K, N_V, SCALE, WINDOW, sinks=SINKS, dev_status=status)
         assert int(status.item()) == 0
-        keys.append((k_new.float() * torch.rsqrt(k_new.float().square().mean(-1, keepdim=True) + EPS)).to(BF16))
-        values.append(v_new)
-        kk, vv = torch.cat(keys), torch.cat(values)
-        ref, _, mean_abs, big = attend64(turned, kk, vv, SCALE, visible(length, n, len(kk), WINDOW, SINKS))
-        # keys that lie next to a rounding boundary may be rounded the other way here: a whole step instead of none
-        weight = 2 * (2 * HALF_STEP[BF16] * big + (D + 16) * 2.0 ** -24 * max(big, 1.0)) + HALF_STEP[BF16] + (len(kk) + 16) * 2.0 ** -24
-        bound = float(torch.tensor(weight).expm1()) * mean_abs
-        bound = bound + HALF_STEP[BF16] * (ref.abs() + bound)
-        assert bool(((out.double() - ref).abs() <= bound).all())
-        length += n
-        lens += n
-        # what the next row, at position `length`, no longer sees: every whole page behind the sinks' below its window
-        gone = range(-(-SINKS // PAGE), (length + 1 - WINDOW) // PAGE)
-        for j in gone:
-            page = int(table[0, j])
-            if page >= 0:
-                refs[page] -= 1
-                table[0, j] = -1
-                k[page] = float("nan")
-                v[page] = float("nan")
+        k_new = (k_new.float() * torch.rsqrt(k_new.float().square().mean(-1, keepdim=True) + EPS)).to(BF16)
+        for s, rows in enumerate((slice(0, new[0]), slice(new[0], n))):
+            if not new[s]:
+                continue
+            tokens[s][0].append(k_new[rows])
+            tokens[s][1].append(v_new[rows])
+            kk, vv = torch.cat(tokens[s][0]), torch.cat(tokens[s][1])
+            ref, _, mean_abs, big = attend64(turned[rows], kk, vv, SCALE, visible(length[s], new[s], len(kk), WINDOW, SINKS))
+            # keys that lie next to a rounding boundary may be rounded the other way here: a whole step instead of none
+            weight = 2 * (2 * HALF_STEP[BF16] * big + (D + 16) * 2.0 ** -24 * max(big, 1.0)) + HALF_STEP[BF16] + (len(kk) + 16) * 2.0 ** -24
+            bound = float(torch.tensor(weight).expm1()) * mean_abs
+            bound = bound + HALF_STEP[BF16] * (ref.abs() + bound)
+            assert bool(((out[rows].double() - ref).abs() <= bound).all())
+            length[s] += new[s]
+            lens[s] += new[s]
+            # what the next row, at position length, no longer sees: every whole page behind the sinks' below its window
+            for j in range(-(-SINKS // PAGE), (length[s] + 1 - WINDOW) // PAGE):
+                page = int(table[s, j])
+                if page >= 0:
+                    refs[page] -= 1
+                    table[s, j] = -1
+                    if int(refs[page]) == 0:
+                        k[page] = v[page] = nan
+
+    for n in [50, 1, 1, 30, 1, 40, 1, 1, 60, 1, 1, 55, 1]:
+        step([n, 0])
+    api.diffqkv_pages_fork(ints([0]), ints([1]), cache, refs, dev_status=status)
+    tokens[1] = tuple(list(x) for x in tokens[0])
+    length[1] = length[0]
+    for new in ([1, 1], [0, 9], [3, 1], [1, 1]):
+        step(new)
+    api.diffqkv_pages_free(ints([0, 1]), cache, refs, dev_status=status)
+    assert int(status.item()) == 0 and refs.tolist() == [0] * pages and bool((table == -1).all())
