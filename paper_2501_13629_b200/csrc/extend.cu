@@ -1122,7 +1122,7 @@ extend_merge_kernel(const ExtendParams p, const ExtendList few, const int rows_e
     int first[2];  // first row of the item of either kind
     int rows[2];   // of a head group, of an item of a few rows; 0: of long chunks
   };
-  __shared__ Row row_s[kMergeRows];
+  __shared__ Row row_s[2][kMergeRows];  // of a step with long chunks and of one whose rows are all few
   __shared__ ItemRef ref_s[kMergeRefs][2];
   const int t0 = blockIdx.x * rows_each, count = min(rows_each, p.total_q - t0);
   {
@@ -1135,19 +1135,28 @@ extend_merge_kernel(const ExtendParams p, const ExtendList few, const int rows_e
         prefix = b < 0 ? -1 : group_prefix(p, b, lo, n, past, g_lo, g_hi);
       }
       if (threadIdx.x < 2) {
-        const int k = threadIdx.x, first = k == 0 ? g_lo : lo, rows = k == 0 ? g_hi - g_lo : n;
+        const int k = threadIdx.x, first = k == 0 ? g_lo : lo, rows = k == 0 ? g_hi - g_lo : n, in = t - first;
         const bool wide = rows > p.thin_max;
-        row_s[r].has = prefix < 0 ? 0 : prefix == 0 ? 1 : 2;
-        row_s[r].first[k] = wide ? first + (t - first) / (2 * p.T) * (2 * p.T) : first;
-        row_s[r].rows[k] = wide ? 0 : rows * p.G;
+        row_s[0][r].has = row_s[1][r].has = prefix < 0 ? 0 : prefix == 0 ? 1 : 2;
+        row_s[0][r].first[k] = row_s[1][r].first[k] = first;
+        row_s[0][r].rows[k] = row_s[1][r].rows[k] = rows * p.G;
+        if (wide) {  // see SeqOf
+          const int blocks = min((rows + p.thin_max - 1) / max(p.thin_max, 1), kMidBlocks + 1), each = (rows + blocks - 1) / blocks;
+          row_s[0][r].first[k] += in / (2 * p.T) * (2 * p.T);
+          row_s[0][r].rows[k] = 0;
+          row_s[1][r].first[k] += in / each * each;
+          row_s[1][r].rows[k] = min(each, rows - in / each * each) * p.G;
+        }
       }
     }
   }
   __syncthreads();
   ptx::grid_dependency_wait();
-  if (p.refs[2LL * p.total_q * p.n_units].first) return;  // left out
+  const ItemRef step = p.refs[2LL * p.total_q * p.n_units];
+  if (step.first) return;  // left out
+  const Row* rows_s = row_s[step.parts != 0];
   auto ref_of = [&](int r, int unit, int k) -> ItemRef {
-    const Row& w = row_s[r];
+    const Row& w = rows_s[r];
     if (w.has < (k == 0 ? 2 : 1)) return {0, 0};
     ItemRef x = p.refs[((size_t)k * p.total_q + w.first[k]) * p.n_units + unit];
     const int most = w.rows[k] == 0 ? p.n_teams : p.blocks;
@@ -1166,7 +1175,7 @@ extend_merge_kernel(const ExtendParams p, const ExtendList few, const int rows_e
   for (int h = blockIdx.y * kHeads + threadIdx.x / kLanes; h < p.n_q; h += gridDim.y * kHeads) {
     const int group = h / p.G, unit = group / p.parts, member = group - unit * p.parts, head = h - group * p.G;
     for (int r = 0; r < count; ++r) {
-      const Row& w = row_s[r];
+      const Row& w = rows_s[r];
       const ItemRef ref0 = cached ? ref_s[r * p.n_units + unit][0] : ref_of(r, unit, 0);
       const ItemRef ref1 = cached ? ref_s[r * p.n_units + unit][1] : ref_of(r, unit, 1);
       const int total = ref0.parts + ref1.parts;
@@ -1479,6 +1488,7 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
       p.few_cost[i] = std::min(std::max(std::max(memory, (products[i] * d + 128) / 256), 1), kFewMostCost);
     p.thin_weight *= 0.42f / p.few_cost[0];  // tiles of half the tokens, in these units; the best of five for two mixtures
     p.item_cost = range->groups > 0 ? kSharedItemCost : kItemCost;
+    p.mid_most = std::min(kMidMost * pl.blocks, kMidLong - 1);
     p.window = range->window;
     p.sinks = range->sinks;
     p.sink_tiles = (int)(((long long)range->sinks + kKT - 1) / kKT);

@@ -79,13 +79,13 @@ struct ExtendParams {
   // its own position.  The first `groups` entries of the list are the prefixes of groups of sequences, the others, up to
   // `entries`, the sequences, whose own tokens begin behind their group's prefix.
   int window, sinks, sink_tiles, sink_few;  // the sinks in tiles of this kernel and of extend_few.cu
-  int few_stages, few_cost[3], item_cost;
+  int few_stages, few_cost[3], item_cost, mid_most;
   int alone;  // the kernel of few rows comes without the other one: too few rows in all for a long chunk
   int groups, entries;
   const int* cu_groups;
   const int* prefix_lens;
   RowBuffer buffer[2];  // kDstPrefix - 1, kDstOwn - 1
-  ItemRef* refs;        // [2][total_q][n_units], and one whose `first` says that the step has been left out
+  ItemRef* refs;        // [2][total_q][n_units], and one that says whether the step is left out, and whether its rows are all few
 };
 
 // Rows of sequence b: first row, number, tokens cached before; false when they do not fit.
@@ -145,6 +145,12 @@ constexpr int kThinItemCost = 5;
 // when memory bounds it (see few_cost); an item costs about two such more.
 constexpr int kFewT = 64, kFewItemCost = 8, kFewMostCost = 16;
 constexpr int kFewCols = 128;  // as kThinCols
+// A step whose long chunks are short in all goes to the kernel of few rows too, in blocks of rows that each read the chunk's
+// tokens: the kernel of long chunks takes 20 us for its start and its first tiles alone, this one three or four times as long
+// for what comes behind them.  Up to this many units of cost for an SM; a chunk of more blocks, or of more cost than
+// kMidLong, is too long by itself.  64 rows in three groups behind 30-60 tokens 31 -> 20 us, 143 rows behind 320-960 tokens
+// 41 -> 30, 540 rows in a window of 33 tokens 35 -> 24; with 24 units the last two stay as they were, with 84 nothing changes.
+constexpr int kMidMost = 44, kMidLong = 8192, kMidBlocks = 16;
 
 // sum of floor((a x + b) / m) for x = 0 .. n - 1 with a, b >= 0, m > 0: the Euclid-like recursion on (m, a).  Not inlined:
 // the code that a block runs once at its start is fetched from the second-level cache line by line, which is what it
@@ -262,6 +268,7 @@ template <>
 struct SeqOf<true> {
   int lo, n, past, items;
   int rows, thin_tiles;
+  int blocks, block_rows;  // of rows, for the kernel of few rows
   int end, start;  // its tokens: from start (or the first) on, below end
   int tab, dst;    // row of the page table, kDst...
   bool bad, back;  // does not fit; ends in front of its beginning
@@ -291,22 +298,38 @@ struct SeqOf<true> {
       }
       end = past + n;
     }
-    thin_tiles = items = 0;
-    rows = n;
+    items = 0;
+    rows = block_rows = n;
+    blocks = 1;
+    thin_tiles = n > 0 ? (end + kFewT - 1) / kFewT - skip_few(p) : 0;
     if (n > p.thin_max) {
       items = (n + 2 * p.T - 1) / (2 * p.T);
+      blocks = min((n + p.thin_max - 1) / max(p.thin_max, 1), kMidBlocks + 1);
+      block_rows = (n + blocks - 1) / blocks;
     } else {
-      thin_tiles = n > 0 ? (end + kFewT - 1) / kFewT - skip_few(p) : 0;
       n = 0;
     }
   }
+  // the list that it is in, which the step's length decides
+  __device__ void choose(bool all_few) {
+    if (all_few) n = 0;
+    else if (n > 0) thin_tiles = 0;
+  }
+  // the other kernel's cost of a long chunk
+  __device__ int mid(const ExtendParams& p) const {
+    if (n == 0) return 0;
+    if (p.thin_max == 0 || blocks > kMidBlocks || thin_tiles > kMidLong / kFewItemCost) return kMidLong;
+    return min(p.n_units * few_unit(p), kMidLong);
+  }
   // cost of one of extend_few.cu's tiles, by its groups of 16 rows: up to two, up to four, more
   __device__ int few_cost(const ExtendParams& p) const {
-    const int groups = p.parts * ((rows * p.G + 15) >> 4);
+    const int groups = p.parts * ((block_rows * p.G + 15) >> 4);
     return p.few_cost[groups <= 2 ? 0 : groups <= 4 ? 1 : 2];
   }
-  // and of a unit of it
-  __device__ int few_unit(const ExtendParams& p) const { return thin_tiles > 0 ? thin_tiles * few_cost(p) + kFewItemCost : 0; }
+  // and of a unit of it, all blocks of rows
+  __device__ int few_unit(const ExtendParams& p) const {
+    return thin_tiles > 0 ? blocks * (thin_tiles * few_cost(p) + kFewItemCost) : 0;
+  }
   // of extend_few.cu's tiles, behind the sinks, those that no row sees
   __device__ int skip_few(const ExtendParams& p) const { return max(low(p, 0) / kFewT - p.sink_few, 0); }
   // first token behind the sinks that the chunk's row `tok` sees
@@ -381,14 +404,15 @@ __device__ __forceinline__ int ranged_wide_teams(const ExtendParams& p, uint32_t
 }
 struct RangedStart {
   uint32_t wide, few;        // lengths of the two lists
-  int first, busy;           // the thread's first entry and the threads that have few rows in theirs
+  int first, busy;           // the thread's first entry; blocks of few rows, where no thread has more than one entry
   bool single;               // no thread has more than one entry
+  bool all_few;              // long chunks are in the list of few rows too
   uint32_t before_wide, before_few;  // of the lists, in front of the thread's entries
 };
 template <int kWarps>
 struct RangedScan {
   unsigned long long sum[kWarps];
-  int busy[kWarps];
+  uint32_t mid[kWarps], busy[kWarps];
   SeqOf<true> seq;  // of the block's first item: its entry, the entry's start in the list
   int e;
   uint32_t lo;
@@ -402,7 +426,7 @@ __device__ __forceinline__ RangedStart ranged_start(const ExtendParams& p, Range
   RangedStart r;
   r.single = per_thread == 1;
   r.first = tid * per_thread;
-  uint32_t wide = 0, few = 0;
+  uint32_t wide = 0, few = 0, mid = 0;
   bool back = false;
   my.n = my.thin_tiles = 0;
 #pragma unroll 1
@@ -411,36 +435,59 @@ __device__ __forceinline__ RangedStart ranged_start(const ExtendParams& p, Range
     my.load(p, r.first + i);
     if ((my.bad || my.back) && reports) report(p.dev_status, DIFFQKV_ERR_INDEX);
     back |= my.back;
-    few += p.n_units * my.few_unit(p);
-    if (my.n > 0) wide += p.n_units * (uint32_t)my.cost(p);
+    if (my.n > 0) {
+      wide += p.n_units * (uint32_t)my.cost(p);
+      mid += my.mid(p);
+    } else {
+      few += p.n_units * my.few_unit(p);
+    }
   }
   const unsigned long long mine = (unsigned long long)wide << 32 | few;
   unsigned long long x = mine;
+  uint32_t z = mid;
 #pragma unroll 1
   for (int o = 1; o < 32; o <<= 1) {
     const unsigned long long y = __shfl_up_sync(0xffffffffu, x, o);
-    if (lane >= o) x += y;
+    const uint32_t v = __shfl_up_sync(0xffffffffu, z, o);
+    if (lane >= o) {
+      x += y;
+      z += v;
+    }
   }
-  const int busy = __popc(__ballot_sync(0xffffffffu, few > 0));
+  const uint32_t busy = __reduce_add_sync(0xffffffffu, few > 0 ? 1 : mid > 0 ? my.blocks << 16 : 0);
   if (lane == 31) {
     sc.sum[warp] = x;
+    sc.mid[warp] = z;
     sc.busy[warp] = busy;
   }
   back = __syncthreads_or(back);
-  if (reports && p.groups > 0 && tid == 0) p.refs[2LL * p.total_q * p.n_units].first = back;
   unsigned long long before = x - mine, all = 0;
-  r.busy = 0;
+  uint32_t before_mid = z - mid, all_mid = 0, all_busy = 0;
 #pragma unroll 1
   for (int w = 0; w < kWarps; ++w) {
-    if (w < warp) before += sc.sum[w];
+    if (w < warp) {
+      before += sc.sum[w];
+      before_mid += sc.mid[w];
+    }
     all += sc.sum[w];
-    r.busy += sc.busy[w];
+    all_mid += sc.mid[w];
+    all_busy += sc.busy[w];
   }
-  if (back) all = 0;
+  if (back) all = all_mid = 0;
   r.wide = (uint32_t)(all >> 32);
   r.few = (uint32_t)all;
   r.before_wide = (uint32_t)(before >> 32);
   r.before_few = (uint32_t)before;
+  r.busy = all_busy & 0xffff;
+  r.all_few = all_mid <= (uint32_t)p.mid_most;
+  if (r.all_few) {
+    r.wide = 0;
+    r.few += all_mid;
+    r.before_few += before_mid;
+    r.busy += all_busy >> 16;
+  }
+  my.choose(r.all_few);
+  if (reports && p.groups > 0 && tid == 0) p.refs[2LL * p.total_q * p.n_units] = {back, r.all_few};
   return r;
 }
 // The thread that has place w0 of a list among its entries, which begin at `before`, leaves the entry there.  cost: an entry's
@@ -452,7 +499,10 @@ __device__ __forceinline__ void ranged_seek(const ExtendParams& p, RangedScan<kW
 #pragma unroll 1
   for (int i = 0; i < per_thread && r.first + i < p.entries; ++i) {
     if (before > w0) break;
-    if (!r.single) my.load(p, r.first + i);
+    if (!r.single) {
+      my.load(p, r.first + i);
+      my.choose(r.all_few);
+    }
     const uint32_t c = cost(my);
     if (before <= w0 && w0 - before < c) {
       sc.seq = my;

@@ -105,7 +105,7 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       if (chunk > (int)(tiles / (uint32_t)grid) + 6) chunk = 0;
     }
     if (chunk > 0) {  // the list of chunks instead
-      uint32_t x = p.n_units * ((uint32_t)(my.thin_tiles + chunk - 1) / (uint32_t)chunk);
+      uint32_t x = p.n_units * my.blocks * ((uint32_t)(my.thin_tiles + chunk - 1) / (uint32_t)chunk);
       const uint32_t mine = x;
 #pragma unroll 1
       for (int o = 1; o < 32; o <<= 1) {
@@ -137,7 +137,7 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     return;
   }
   ranged_seek(p, sc.scan, at, my, w0, before, [&](const Seq& s) -> uint32_t {
-    return p.n_units * (uint32_t)(chunk > 0 ? (s.thin_tiles + chunk - 1) / chunk : s.few_unit(p));
+    return p.n_units * (uint32_t)(chunk > 0 ? s.blocks * ((s.thin_tiles + chunk - 1) / chunk) : s.few_unit(p));
   });
   __syncthreads();
 
@@ -160,7 +160,7 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     int count = 0, segs = 0;
     bool ok = true;
     ExtendMeta m = {};
-    int e = sc.scan.e, u, chunk_lo = 0;
+    int e = sc.scan.e, u, chunk_lo = 0;  // u: unit, and block of rows n_units further on
     Seq x = sc.scan.seq;
     int nt = x.thin_tiles, cost = x.few_cost(p);
     uint32_t item_lo = sc.scan.lo;
@@ -172,11 +172,12 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     }
     auto next_item = [&]() {
       item_lo += cost * nt + kItem;
-      if (item_lo >= w1 || ++u < p.n_units) return;
+      if (item_lo >= w1 || ++u < p.n_units * x.blocks) return;
       u = 0;
       do {
         if (++e >= p.entries) return;
         x.load(p, e);
+        x.choose(at.all_few);
         nt = x.thin_tiles;
         cost = x.few_cost(p);
       } while (nt == 0);
@@ -206,19 +207,21 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
         }
       }
       const int low = max(x.low(p, 0), 0), skip = x.skip_few(p);
-      const int head0 = u * p.parts * p.G, hk0 = head0 / p.heads_per_k, hv0 = head0 / p.heads_per_v;  // Eq. (idx)
-      if (!hand_out({x.lo, x.rows, x.past, x.end, x.start, low, skip, u, ta, tb, x.dst,
+      const int block = u / p.n_units, unit = u - block * p.n_units, tok0 = block * x.block_rows;
+      const int lo = x.lo + tok0, rows = min(x.block_rows, x.rows - tok0);
+      const int head0 = unit * p.parts * p.G, hk0 = head0 / p.heads_per_k, hv0 = head0 / p.heads_per_v;  // Eq. (idx)
+      if (!hand_out({lo, rows, x.past + tok0, x.end, x.start, low, skip, unit, ta, tb, x.dst,
                      (ta == 0 ? kSegFirst : 0) | (ta == 0 && tb == nt ? kSegWhole : 0)}, abort_flag)) {
         ok = false;
         break;
       }
       if (ta == 0 && tb < nt) {
-        m.rows = p.parts * x.rows * p.G; m.part_rows = x.rows * p.G; m.row_lo = x.lo; m.head0 = head0;
+        m.rows = p.parts * rows * p.G; m.part_rows = rows * p.G; m.row_lo = lo; m.head0 = head0;
         m.parts = chunk > 0 ? (nt + chunk - 1) / chunk
                             : share_of((long long)item_lo + last_tile(cost, nt, kItem), total, blocks) - (int)blockIdx.x + 1;
       }
       if (ta == 0 && p.groups > 0 && lane == 0)
-        p.refs[((x.dst == kDstPrefix ? 0LL : p.total_q) + x.lo) * p.n_units + u] = {(int)blockIdx.x, tb < nt ? m.parts : 1};
+        p.refs[((x.dst == kDstPrefix ? 0LL : p.total_q) + lo) * p.n_units + unit] = {(int)blockIdx.x, tb < nt ? m.parts : 1};
       auto token_of = [&](int tile) -> int { return ((tile >= p.sink_few ? tile + skip : tile) << 6) + my_part * p.box_tok; };
       auto wanted = [&](int tok) -> bool { return tok < x.end && (tok < p.sinks || tok + p.box_tok > low); };
       auto fetch = [&](int tile) -> int {  // page of this lane's box

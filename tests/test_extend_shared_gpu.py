@@ -116,6 +116,15 @@ def test_other_head_dimensions(api, dims):
     run(api, share(step, [0, 2], [100]), [0, 2], [100])
 
 
+@pytest.mark.parametrize("heads", ["32/4/8", "6/2/3", "8/8/8", "16/1/1", "12/2/4"])
+@pytest.mark.parametrize("new", [[5, 5, 6], [16, 17, 1], [10, 11, 22], [33, 31, 64], [60, 65, 4], [1, 128, 130]])
+@pytest.mark.parametrize("prefix", [20, 150])
+def test_rows_around_what_is_few(api, heads, new, prefix):
+    """Rows of groups and of sequences that fill the blocks of the kernel of few rows, one less and one more."""
+    step = Step(api, [prefix + 7 * i for i in range(3)] + [40], new + [18], *HEADS[heads], 64, 128, page=32, seed=sum(new), pad=2)
+    run(api, share(step, [0, 3], [prefix]), [0, 3], [prefix])
+
+
 def test_the_prefix_is_read_from_the_first_sequence_alone(api):
     """The others' copies of it hold NaN."""
     step = Step(api, [500, 520, 600, 77], [1, 20, 100, 3], 16, 2, 4, 128, 128, seed=3)

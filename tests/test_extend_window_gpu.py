@@ -111,6 +111,15 @@ def test_long_chunks(api, heads, window, sinks):
     run(api, forget(step, window, sinks), window, sinks)
 
 
+@pytest.mark.parametrize("heads", ["32/4/8", "6/2/3", "8/8/8", "16/1/1", "12/2/4"])
+@pytest.mark.parametrize("window,sinks", [(7, 0), (100, 70), (400, 1)])
+@pytest.mark.parametrize("new", [[15, 16, 17], [31, 1, 33], [21, 22, 43, 2], [63, 64, 65], [127, 128, 129, 5], [160], [0, 255, 1]])
+def test_chunks_around_what_is_few(api, heads, window, sinks, new):
+    """Rows that fill the blocks of the kernel of few rows, one less and one more."""
+    step = Step(api, [50 + 90 * i for i in range(len(new))], new, *HEADS[heads], 64, 128, page=32, seed=sum(new), pad=2).fill()
+    run(api, forget(step, window, sinks), window, sinks)
+
+
 def test_a_window_over_the_whole_cache_is_extend(api):
     step = Step(api, PAST, NEW, 16, 2, 4, 128, 128, seed=8, pad=2).fill()
     out = torch.empty((step.total_q, 16, 128), dtype=BF16, device="cuda")
