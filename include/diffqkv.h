@@ -378,12 +378,15 @@ diffqkv_status diffqkv_extend(const void *q, const int32_t *cu_q, int32_t total_
  * of sequence b, at position p = past_b + i, sees the tokens j <= p with j > p - window or j < sinks.
  *   window  >= 1: tokens of the window, the row's own among them       sinks  >= 0: first tokens that every row sees
  *   workspace  diffqkv_extend_window_workspace_bytes(shape, total_q) bytes, 256-byte aligned
- * Everything else as diffqkv_extend.  Work and traffic go by the tokens seen, not by
- * the tokens cached.  Pages that hold no token which a row of the step sees are not read: they may have been given back, and
- * their table entries may be -1.  (Positions go on counting; diffqkv_pages_free gives back ends, not middles, so a caller who
- * frees pages behind the window lowers their counts and sets their entries itself.)  A weight of zero multiplies the V rows
- * of tokens that another row of the same chunk sees; those must be finite, all others may hold anything.
- * A window that reaches back over the whole cache (window + sinks >= max_seqlen) is diffqkv_extend itself.
+ * Everything else as diffqkv_extend.  Work and traffic go by the tokens seen, not by the tokens cached.  Three launches on
+ * the tensor cores, two where total_q is so small that no sequence can have many rows.  Pages that hold no token which a row
+ * of the step sees are not read: they may have been given back, and their table entries may be -1.  (Positions go on
+ * counting; diffqkv_pages_free gives back ends, not middles, so a caller who frees pages behind the window lowers their
+ * counts and sets their entries itself; such a sequence is forked, freed and compacted like any other.)  A weight of zero
+ * multiplies the V rows of tokens that another row of the same chunk sees; those must be finite, all others may hold
+ * anything.
+ * A window that reaches back over the whole cache (window + sinks >= max_seqlen) is diffqkv_extend itself.  With a cu_q that
+ * decreases anywhere the whole step may be left out.
  */
 size_t diffqkv_extend_window_workspace_bytes(const diffqkv_shape *shape, int32_t total_q);
 diffqkv_status diffqkv_extend_window(const void *q, const int32_t *cu_q, int32_t total_q, int32_t window, int32_t sinks,
@@ -410,9 +413,9 @@ typedef struct {
  *              outside the group's) is reported as DIFFQKV_ERR_INDEX and skipped.
  *   workspace  diffqkv_extend_shared_workspace_bytes(shape, total_q) bytes, 256-byte aligned (it holds both parts of every
  *              row in fp32)
- * Everything else as diffqkv_extend.  Four launches on the tensor cores; where diffqkv_extend runs on
- * FMAs, which bound it and not the cache, every sequence reads all of its own tokens instead.  Two calls that may run at the
- * same time need a workspace each.
+ * Everything else as diffqkv_extend.  Launches as diffqkv_extend_window; where diffqkv_extend runs on FMAs, which bound it and
+ * not the cache, every sequence reads all of its own tokens instead.  With a cu_q or a cu_seqs that decreases anywhere the
+ * whole step may be left out.  Two calls that may run at the same time need a workspace each.
  */
 size_t diffqkv_extend_shared_workspace_bytes(const diffqkv_shape *shape, int32_t total_q);
 diffqkv_status diffqkv_extend_shared(const void *q, const int32_t *cu_q, int32_t total_q, const diffqkv_prefixes *prefixes,

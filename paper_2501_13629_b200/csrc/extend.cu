@@ -40,6 +40,19 @@
 // of the scores.  Earlier forms of this kernel took 415 to 850 us with them for an eighth to a half of the scores.
 // Heads of 64 channels (32/4/16), the same chunks: 396 us without a pause, 580 TFLOP/s; 64-channel keys with 128-channel
 // values 471 us, 730 TFLOP/s (half the products, as many exponentials).
+//
+// Ranged steps (diffqkv_extend_window, diffqkv_extend_shared), whose sequences of a few rows are extend_few.cu's: the tiles
+// that no row of an item sees are left out of its list, so that an item's tiles are those of its first tokens and, `skip`
+// tiles further on, those of its window; a group's prefix is an entry in front of the sequences', whose own tokens begin
+// behind it, and extend_merge_kernel joins the two.  A step begins in one short piece of code in 32-bit arithmetic (see
+// ranged_start); a block's first request still goes out 16 thousand cycles, 9 us, after its start, nearly all of it code that
+// is fetched once, and an item costs 7-8 thousand cycles next to its tiles (2.5 of them the masks of its first and last tile).
+// The same four chunks in windows of 2k tokens: 284 us in a graph, 300 call by call, 750 TFLOP/s of what is seen; tensor pipe
+// 44 % active, special-function unit 45 %.  3k rows behind two prefixes of 3k-5k tokens, 64 and 128 channels: 288 us, 250 of
+// them here (power keeps the SMs at 1.4-1.6 GHz) and 36 of joining 98 MB of parts.
+// Tried and not kept: rows written 32 bytes a lane without the exchange of four lanes (329 -> 343 us: the same lines, and
+// none of it was instructions), a thread a barrier at the start (283 -> 289), two rows at a time in the join (36 -> 37), a way
+// of its own there for rows of whole items (36), four blocks of it an SM (34, but 4 x 4 single rows 24.2 -> 25.1).
 #include <algorithm>
 #include <atomic>
 #include <numeric>

@@ -4,21 +4,27 @@
 // Such steps are short: a window of 4k tokens, the tokens behind a shared prefix.  extend_thin.cu's way, which plain steps
 // take, costs 18 us of starts, first tiles and ends however little there is to do, because every role's straight code is
 // fetched once (about 10 cycles an instruction); 16 sequences with a window of 1k tokens took it 24 us, of which the cache is
-// 4.  So here all warps but one run the same short loop, on warp-level products, which have rate enough: with 64 columns a
-// 64-token tile of three heads takes a third of the time that memory needs for it.
+// 4.  So here all warps but one run the same short loop, on warp-level products, and the same step takes 13 us.
 //
-// Work: one flat list of (entry, unit of heads, 64-token tile), where the tiles that no row sees are left out, divided over
-// one persistent block an SM, or over those that the step's long chunks leave; cut items leave partial rows as in extend.cu.
-// A unit's K and V heads (one of either kind, up to four of the other) pass an SM once for all of its query heads.
+// Work: one flat list of (entry, block of rows, unit of heads, 64-token tile), where the tiles that no row sees are left out,
+// divided over one persistent block an SM, or over those that the step's long chunks leave; cut items leave partial rows as
+// in extend.cu.  An entry is one block of rows, or several that read the same tokens (see kMidMost).  A unit's K and V heads
+// (one of either kind, up to four of the other) pass an SM once for all of its query heads.
 //
-// Per block: warp 8 requests whole tiles by TMA into a ring of stages.  The other eight share a tile's (16 rows of one
-// head group) x (tokens): with up to four such row groups, each has 8, 4 or 2 warps, which take 16 or 32 tokens of a tile
-// each (with 8, every other tile) and are joined through shared memory at the end of a segment.  A warp holds its rows'
-// queries and their accumulator in registers,
-//     S[16 rows x 16 tokens] = Q K^T,   O[16 x d_v] += P V        (P from registers, K and V by ldmatrix)
+// Per block: warp 8 requests whole tiles by TMA into a ring of stages.  The other eight share a tile's 128 columns at most,
+// (16 rows of one head group) x (tokens): one, two, four or up to eight such row groups have 8, 4, 2 or one warp each, which
+// take 32 tokens of a tile, or both halves of it (with 4 or 8 warps to a row group those of every second or fourth tile), and
+// are joined through shared memory at the end of a segment.  A warp holds its rows' queries and their accumulator in
+// registers,
+//     S[16 rows x 32 tokens] = Q K^T,   O[16 x d_v] += P V        (P from registers, K and V by ldmatrix)
 // with the running reference of a row raised only when passed by 2^8, as in extend.cu; statistics and sums are fp32, the
 // weights are rounded to bf16 for the second product.  V rows that no row of the sequence sees are cleared first: their
 // boxes may not have been read.
+//
+// Bound, for up to two row groups, by memory (a 48 KB tile in 1.85 thousand cycles), for more by the warps' chain of products
+// and softmax (2.2 thousand for four, twice that for eight): 32 sequences of 2-5 rows of 32/4/8 heads behind windows of 4k
+// tokens (405 MB) take 80 us, 5.1 TB/s, the warp-level tensor pipe active 28 %.  Started, a
+// block has its first tile after 9 thousand cycles; the step of 16 rows has little else.
 #include "attn_math.cuh"
 #include "extend.cuh"
 #include "ptx.cuh"
