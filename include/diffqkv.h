@@ -385,8 +385,8 @@ diffqkv_status diffqkv_extend(const void *q, const int32_t *cu_q, int32_t total_
  * counts and sets their entries itself; such a sequence is forked, freed and compacted like any other.)  A weight of zero
  * multiplies the V rows of tokens that another row of the same chunk sees; those must be finite, all others may hold
  * anything.
- * A window that reaches back over the whole cache (window + sinks >= max_seqlen) is diffqkv_extend itself.  With a cu_q that
- * decreases anywhere the whole step may be left out.
+ * A window that reaches back over the whole cache (window + sinks >= max_seqlen) gives what diffqkv_extend gives beyond
+ * rounding.  With a cu_q that decreases anywhere the whole step may be left out.
  */
 size_t diffqkv_extend_window_workspace_bytes(const diffqkv_shape *shape, int32_t total_q);
 diffqkv_status diffqkv_extend_window(const void *q, const int32_t *cu_q, int32_t total_q, int32_t window, int32_t sinks,

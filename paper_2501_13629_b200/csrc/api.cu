@@ -469,8 +469,6 @@ static diffqkv_status extend_impl(const void* q, const int32_t* cu_q, int32_t to
   if (!aligned16(q) || !aligned16(out)) return DIFFQKV_ERR_ALIGNMENT;
   if (!workspace || workspace_bytes < extend_need(*shape, total_q, range)) return DIFFQKV_ERR_WORKSPACE;
   if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return DIFFQKV_ERR_ALIGNMENT;
-  // a window that hides no token of the longest sequence
-  if (range && range->groups == 0 && (long long)range->window + range->sinks >= cache->max_seqlen) range = nullptr;
   const int choice = g_extend_choice;
   cudaError_t err = cudaErrorNotSupported;
   if (choice == 0) err = launch_extend(q, cu_q, total_q, *cache, *shape, range, workspace, out, lse, dev_status, stream);
@@ -493,6 +491,7 @@ static diffqkv_status extend_impl(const void* q, const int32_t* cu_q, int32_t to
     p.cache.seqlens = lengths;
     range = nullptr;
   }
+  if (range && (long long)range->window + range->sinks >= cache->max_seqlen) range = nullptr;  // hides nothing
   if (choice != 1) err = launch_extend_simt(p, *shape, cu_q, total_q, range, workspace, out, lse, stream);
   g_last_extend_kernel = err == cudaErrorNotSupported ? 1 : 2;
   if (err == cudaErrorNotSupported)

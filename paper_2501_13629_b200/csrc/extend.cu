@@ -1434,7 +1434,15 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
       box_tok = c.page_size;
     }
   }
-  const Plan pl = make_plan(s, total_q, range != nullptr);
+  Plan pl = make_plan(s, total_q, range != nullptr);
+  // A window that hides nothing of the longest sequence: long chunks are the plain kernels' (1.5k-2k rows of 64-channel heads
+  // 473, not 529 us; of 128 channels 540, not 510; four of 300 rows 32, not 35), few rows stay here (16 single rows behind 32k
+  // tokens 247, not 269 us; 64 behind 1k-4k 95, not 120; four of 60 rows 19, not 31).
+  const bool hides = range && (long long)range->window + range->sinks < c.max_seqlen;
+  if (range && range->groups == 0 && !hides && total_q > (long long)s.batch * kMidBlocks * pl.thin_max) {
+    range = nullptr;
+    pl = make_plan(s, total_q, false);
+  }
   if (range) {  // both lists in 32 bits; see ranged_start
     const long long entries = (long long)range->groups + s.batch, units = pl.groups / pl.parts;
     const long long items = total_q / (2 * pl.T) * (range->groups > 0 ? 2LL : 1LL) + entries;
@@ -1502,10 +1510,10 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
     p.thin_weight *= 0.42f / p.few_cost[0];  // tiles of half the tokens, in these units; the best of five for two mixtures
     p.item_cost = range->groups > 0 ? kSharedItemCost : kItemCost;
     p.mid_most = std::min(kMidMost * pl.blocks, kMidLong - 1);
-    p.window = range->window;
-    p.sinks = range->sinks;
-    p.sink_tiles = (int)(((long long)range->sinks + kKT - 1) / kKT);
-    p.sink_few = (int)(((long long)range->sinks + kFewT - 1) / kFewT);
+    p.window = hides ? range->window : kNoWindow;  // window and sinks together stay within 32 bits
+    p.sinks = hides ? range->sinks : 0;
+    p.sink_tiles = (p.sinks + kKT - 1) / kKT;
+    p.sink_few = (p.sinks + kFewT - 1) / kFewT;
     p.groups = range->groups; p.entries = range->groups + s.batch;
     p.cu_groups = range->cu_groups; p.prefix_lens = range->prefix_lens;
     if (p.groups > 0) place_buffers(s, pl, total_q, static_cast<char*>(workspace) + extend_workspace_bytes(s, total_q, true), &p);
