@@ -1436,10 +1436,10 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
   }
   Plan pl = make_plan(s, total_q, range != nullptr);
   // A window that hides nothing of the longest sequence: long chunks are the plain kernels' (1.5k-2k rows of 64-channel heads
-  // 473, not 529 us; of 128 channels 540, not 510; four of 300 rows 32, not 35), few rows stay here (16 single rows behind 32k
+  // 473, not 529 us; of 128 channels 540, not 510; two of 240 rows 39, not 42), few rows stay here (16 single rows behind 32k
   // tokens 247, not 269 us; 64 behind 1k-4k 95, not 120; four of 60 rows 19, not 31).
   const bool hides = range && (long long)range->window + range->sinks < c.max_seqlen;
-  if (range && range->groups == 0 && !hides && total_q > (long long)s.batch * kMidBlocks * pl.thin_max) {
+  if (range && range->groups == 0 && !hides && total_q > (long long)s.batch * (kMidBlocks / 2) * pl.thin_max) {
     range = nullptr;
     pl = make_plan(s, total_q, false);
   }

@@ -99,10 +99,20 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
   const RangedStart at = ranged_start(p, sc.scan, my, p.alone && blockIdx.x == 0);
   const uint32_t total = at.few;
   // Equal shares of the list, cut wherever they end; or, where that costs no block more than six tiles, equal chunks that
-  // begin with their item (see extend_thin.cu), so that every block has one segment at most.
+  // begin with their item (see extend_thin.cu), so that every block has one segment at most.  A chunk is that many of the
+  // cheapest tiles, rounded up of others (42 rows in two groups, whose tiles cost more than twice their own tokens': 29 us,
+  // 36 with as many of either).
   const int grid = at.wide == 0 ? p.blocks : thin_blocks_left(p, ranged_wide_teams(p, at.wide, total));  // what the other kernel leaves
   int chunk = 0, blocks = 0;  // blocks: that take part
   uint32_t w0 = 0, w1 = 0, before = at.before_few;
+  auto chunk_of = [&](const Seq& s) -> int {
+    const int cost = s.few_cost(p);
+    return cost == p.few_cost[0] ? chunk : (chunk * p.few_cost[0] + cost - 1) / cost;
+  };
+  auto chunks_of = [&](const Seq& s) -> int {
+    const int each = chunk_of(s);
+    return s.blocks * ((s.thin_tiles + each - 1) / each);
+  };
   if (total > 0 && (int)blockIdx.x < grid) {
     const int items = at.single ? min(at.busy * p.n_units, grid) : grid;
     if (items < grid) {
@@ -111,7 +121,7 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
       if (chunk > (int)(tiles / (uint32_t)grid) + 6) chunk = 0;
     }
     if (chunk > 0) {  // the list of chunks instead
-      uint32_t x = p.n_units * my.blocks * ((uint32_t)(my.thin_tiles + chunk - 1) / (uint32_t)chunk);
+      uint32_t x = my.thin_tiles > 0 ? p.n_units * chunks_of(my) : 0;
       const uint32_t mine = x;
 #pragma unroll 1
       for (int o = 1; o < 32; o <<= 1) {
@@ -143,7 +153,7 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     return;
   }
   ranged_seek(p, sc.scan, at, my, w0, before, [&](const Seq& s) -> uint32_t {
-    return p.n_units * (uint32_t)(chunk > 0 ? s.blocks * ((s.thin_tiles + chunk - 1) / chunk) : s.few_unit(p));
+    return p.n_units * (uint32_t)(chunk > 0 ? (s.thin_tiles > 0 ? chunks_of(s) : 0) : s.few_unit(p));
   });
   __syncthreads();
 
@@ -170,6 +180,7 @@ extend_few_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_const
     Seq x = sc.scan.seq;
     int nt = x.thin_tiles, cost = x.few_cost(p);
     uint32_t item_lo = sc.scan.lo;
+    if (chunk > 0) chunk = chunk_of(x);  // of the block's one item
     {
       const uint32_t in = w0 - item_lo, per = chunk > 0 ? (nt + chunk - 1) / chunk : cost * nt + kItem;
       u = (int)(in / per);
