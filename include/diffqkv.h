@@ -406,11 +406,12 @@ typedef struct {
   int32_t num_groups;     /* at most 65535; sequences in front of the first group and behind the last share nothing              */
 } diffqkv_prefixes;
 /*
- *   prefixes   every sequence of a group that has rows in the step has at least lens[g] tokens cached.  The first lens[g]
- *              tokens are read from the pages (or, without pages, the slab) of the group's FIRST sequence, which may have no
- *              rows itself; those of the others are taken to be the same.  A sequence whose group does not fit
- *              it (a prefix longer than its cache or than max_seqlen, or negative, an end of the group outside the batch, rows
- *              outside the group's) is reported as DIFFQKV_ERR_INDEX and skipped.
+ *   prefixes   every sequence of a group that has rows in the step has at least lens[g] tokens cached, in its own pages (or
+ *              slab) as for diffqkv_extend; those of all sequences of a group are the same, usually the same pages.  A shared
+ *              prefix is read from the group's FIRST sequence, which may have no rows itself; where sharing would save
+ *              nothing (short prefixes, long chunks, a group of one) every sequence reads its own.  A sequence whose group
+ *              does not fit it (a prefix longer than its cache or than max_seqlen, or negative, an end of the group outside
+ *              the batch, rows outside the group's) is reported as DIFFQKV_ERR_INDEX and skipped.
  *   workspace  diffqkv_extend_shared_workspace_bytes(shape, total_q) bytes, 256-byte aligned (it holds both parts of every
  *              row in fp32)
  * Everything else as diffqkv_extend.  Launches as diffqkv_extend_window; where diffqkv_extend runs on FMAs, which bound it and

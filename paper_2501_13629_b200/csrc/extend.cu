@@ -137,8 +137,8 @@ struct Walk {
       wide = seq.wide(p, item);
       nt = seq.tiles(p, item);
       const int cost = wide ? kWideCost : kNarrowCost;
-      ta = item_tile(begin - item_lo, cost, nt, item_cost<kRanged>(p));
-      tb = item_tile(end - item_lo, cost, nt, item_cost<kRanged>(p));
+      ta = item_tile(begin - item_lo, cost, nt, item_cost<kRanged>);
+      tb = item_tile(end - item_lo, cost, nt, item_cost<kRanged>);
       if (ta < tb) {
         if (wide) {
           int nt0;  // tiles that the first row tile sees
@@ -155,7 +155,7 @@ struct Walk {
     return false;
   }
   __device__ void advance(const ExtendParams& p) {
-    item_lo += item_cost<kRanged>(p) + (long long)(seq.wide(p, item) ? kWideCost : kNarrowCost) * seq.tiles(p, item);
+    item_lo += item_cost<kRanged> + (long long)(seq.wide(p, item) ? kWideCost : kNarrowCost) * seq.tiles(p, item);
     if (kRanged && item_lo >= end) return;  // no reading on through entries of a few rows, 800 cycles each
     if (++item < seq.items) return;
     item = 0;
@@ -418,7 +418,7 @@ extend_attn_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_cons
       const int tok0 = w.tok0(p);
       if (w.ta == 0 && w.tb < w.nt) {
         m.rows = m.part_rows = min(w.seq.n - tok0, 2 * p.T) * p.G; m.row_lo = w.seq.lo + tok0; m.head0 = head0;
-        m.parts = share_of(w.item_lo + last_tile(w.wide ? kWideCost : kNarrowCost, w.nt, item_cost<kRanged>(p)), total, n_teams) - team + 1;
+        m.parts = share_of(w.item_lo + last_tile(w.wide ? kWideCost : kNarrowCost, w.nt, item_cost<kRanged>), total, n_teams) - team + 1;
       }
       if constexpr (kRanged) {
         if (w.ta == 0 && member == 0 && p.groups > 0 && lane == 0)
@@ -1446,7 +1446,7 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
   if (range) {  // both lists in 32 bits; see ranged_start
     const long long entries = (long long)range->groups + s.batch, units = pl.groups / pl.parts;
     const long long items = total_q / (2 * pl.T) * (range->groups > 0 ? 2LL : 1LL) + entries;
-    if (items * units * (kSharedItemCost + kWideCost * (c.max_seqlen / kKT + 2LL)) > 0x7fffffffLL ||
+    if (items * units * (kRangedItemCost + kWideCost * (c.max_seqlen / kKT + 2LL)) > 0x7fffffffLL ||
         entries * units * (kFewItemCost + kFewMostCost * (c.max_seqlen / kFewT + 2LL)) > 0x7fffffffLL)
       return cudaErrorNotSupported;
   }
@@ -1508,7 +1508,6 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
     for (int i = 0; i < 3; ++i)
       p.few_cost[i] = std::min(std::max(std::max(memory, (products[i] * d + 128) / 256), 1), kFewMostCost);
     p.thin_weight *= 0.42f / p.few_cost[0];  // tiles of half the tokens, in these units; the best of five for two mixtures
-    p.item_cost = range->groups > 0 ? kSharedItemCost : kItemCost;
     p.mid_most = std::min(kMidMost * pl.blocks, kMidLong - 1);
     p.window = hides ? range->window : kNoWindow;  // window and sinks together stay within 32 bits
     p.sinks = hides ? range->sinks : 0;

@@ -79,7 +79,7 @@ struct ExtendParams {
   // its own position.  The first `groups` entries of the list are the prefixes of groups of sequences, the others, up to
   // `entries`, the sequences, whose own tokens begin behind their group's prefix.
   int window, sinks, sink_tiles, sink_few;  // the sinks in tiles of this kernel and of extend_few.cu
-  int few_stages, few_cost[3], item_cost, mid_most;
+  int few_stages, few_cost[3], mid_most;
   int alone;  // the kernel of few rows comes without the other one: too few rows in all for a long chunk
   int groups, entries;
   const int* cu_groups;
@@ -129,16 +129,12 @@ __device__ __forceinline__ long long last_tile(int cost, int nt, int extra) {
 // rows are written out and the pipeline fills again).  Measured on prompts of 1.5k-2k rows over 0-6k tokens: 1.85 us a
 // tile, 4-5 us an item; without the last, blocks with many short items ended 13 % late, 4 to 7 makes 1 %.
 constexpr int kWideCost = 2, kNarrowCost = 1, kItemCost = 5;
-// A step with groups has items of very different lengths, a prefix and a chunk's own few tiles, and rows that are written in
-// fp32: 6, 7, 9 and 11 for an item of chunks of 150-600 rows behind two prefixes of 3k-5k tokens (32/4/16 heads, 64 and 128
-// channels) make it 313, 304, 288 and 296 us, 5 makes it 330; 16 chunks of 100-300 rows behind 8k tokens 538, 515, 495, 496,
-// not 574.  Windows, whose items are alike, take 296 us with 5 and 299 with 9.
-constexpr int kSharedItemCost = 9;
+// Ranged, an item costs more next to its tiles: the masks of its first and last tile, and the rows of a step with groups are
+// written in fp32.  5, 7 and 9: chunks of 150-600 rows of two groups (32/4/16 heads, 64 and 128 channels) 289, 284 and 284 us,
+// 16 chunks of 30-60 rows behind 4k tokens 97, 96 and 101, windows of 2k tokens 296, 296 and 299.
+constexpr int kRangedItemCost = 7;
 template <bool kRanged>
-__device__ __forceinline__ int item_cost(const ExtendParams& p) {
-  if constexpr (kRanged) return p.item_cost;
-  return kItemCost;
-}
+constexpr int item_cost = kRanged ? kRangedItemCost : kItemCost;
 // Likewise for thin items, in tiles: a block's second item costs it about as much as five more tiles.
 constexpr int kThinItemCost = 5;
 // The ranged steps' few rows go by tiles of 64 tokens, whose cost is a quarter of what one of three 128-channel heads takes
@@ -211,8 +207,20 @@ __device__ __forceinline__ bool group_rows(const ExtendParams& p, int g, int& lo
   hi = p.cu_q[end];
   return lo >= 0 && hi >= lo && hi <= p.total_q && prefix <= 0x7ffffe00 - (hi - lo);  // positions stay within 32 bits
 }
+// Whether a prefix of that many tokens is worth an entry of its own next to its sequences', which read it each otherwise.  It
+// costs items more, and two parts to every row that are joined.  With few rows to a sequence that is as much as reading some
+// hundred tokens more; long chunks are bound by their products, of which sharing saves the empty rows of their tiles alone.
+// Shared and not: 12 chunks of 96-192 rows of three groups behind 14-29 tokens 83, 58 us; 6 of 300-500 rows behind 2k tokens
+// 215, 201; 16 of 20-30 rows behind 1k 52, 46; 16 of 30-60 behind 4k 100, 112; 8 of 40-80 behind 16k 162, 239; two of 220
+// behind 8k 102, 122; single rows in pairs behind 400 tokens 22, 19, behind 1k 23, 25.
+constexpr int kShareTokens = 512, kShareLeast = 1024;
+constexpr float kShareLong = 1000.f;
+__device__ __forceinline__ bool worth_sharing(const ExtendParams& p, int rows, int seqs, int prefix) {
+  if (rows <= seqs * p.thin_max) return (float)prefix * (seqs - 1) >= (float)kShareTokens;
+  return (float)(prefix - kShareLeast) * p.T * seqs >= kShareLong * rows;
+}
 // Tokens of sequence b, whose rows are lo .. lo + n - 1 behind `past` tokens, that its group has for it (0 outside of all
-// groups); -1 when the group's rows or tokens do not hold those of the sequence.  The group's rows are g_lo .. g_hi - 1.
+// groups, and where they are not shared); -1 when the group's rows or tokens do not hold those of the sequence.  The group's rows are g_lo .. g_hi - 1.
 __device__ __forceinline__ int group_prefix(const ExtendParams& p, int b, int lo, int n, int past, int& g_lo, int& g_hi) {
   int g = 0, z = p.groups;  // the last group that begins at or before b
   if (z == 0) return 0;
@@ -223,7 +231,7 @@ __device__ __forceinline__ int group_prefix(const ExtendParams& p, int b, int lo
   if (b < p.cu_groups[g] || b >= p.cu_groups[g + 1]) return 0;
   int first, prefix;
   if (!group_rows(p, g, g_lo, g_hi, first, prefix) || prefix > past || lo < g_lo || lo + n > g_hi) return -1;
-  return prefix;
+  return worth_sharing(p, g_hi - g_lo, p.cu_groups[g + 1] - first, prefix) ? prefix : 0;
 }
 
 // One sequence of the step as the list of long chunks has it.
@@ -279,7 +287,7 @@ struct SeqOf<true> {
       int hi;
       bad = false;  // of a group that does not fit every sequence with rows says so
       back = p.cu_groups[x + 1] < p.cu_groups[x];
-      n = group_rows(p, x, lo, hi, tab, past) && past > 0 ? hi - lo : 0;
+      n = group_rows(p, x, lo, hi, tab, past) && past > 0 && worth_sharing(p, hi - lo, p.cu_groups[x + 1] - tab, past) ? hi - lo : 0;
       if (n == 0) past = 0;
       end = past;
       dst = kDstPrefix;
@@ -359,7 +367,7 @@ struct SeqOf<true> {
       }
       if (i > x0) tiles -= steps(p, i - x0, c);
     }
-    return kWideCost * tiles + p.item_cost * i;
+    return kWideCost * tiles + item_cost<true> * i;
   }
   __device__ bool wide(const ExtendParams& p, int i) const { return n - i * 2 * p.T > p.T; }
   __device__ int tiles(const ExtendParams& p, int i) const {  // K/V tiles of item i
@@ -367,7 +375,7 @@ struct SeqOf<true> {
   }
   __device__ int cost(const ExtendParams& p) const {  // of one head group
     if (n == 0) return 0;
-    return cost_before(p, items - 1) + p.item_cost + (wide(p, items - 1) ? kWideCost : kNarrowCost) * tiles(p, items - 1);
+    return cost_before(p, items - 1) + item_cost<true> + (wide(p, items - 1) ? kWideCost : kNarrowCost) * tiles(p, items - 1);
   }
 };
 template <bool kRanged>
@@ -378,7 +386,8 @@ __device__ __forceinline__ bool long_entry(const ExtendParams& p, int x) {
   int lo, hi;
   if (x < p.groups) {
     int first, prefix;
-    return group_rows(p, x, lo, hi, first, prefix) && prefix > 0 && hi - lo > p.thin_max;
+    return group_rows(p, x, lo, hi, first, prefix) && prefix > 0 && hi - lo > p.thin_max &&
+           worth_sharing(p, hi - lo, p.cu_groups[x + 1] - first, prefix);
   }
   return p.cu_q[x - p.groups + 1] - p.cu_q[x - p.groups] > p.thin_max;
 }
@@ -400,7 +409,7 @@ __device__ __forceinline__ int ranged_wide_teams(const ExtendParams& p, uint32_t
     const float w = (float)wide * p.team, f = (float)few * p.thin_weight;
     n = min(max((int)(n * __fdividef(w, w + f) + 0.5f), 1), n - 1);
   }
-  return ranged_shares(wide, n, p.item_cost + kWideCost);
+  return ranged_shares(wide, n, item_cost<true> + kWideCost);
 }
 struct RangedStart {
   uint32_t wide, few;        // lengths of the two lists

@@ -125,9 +125,9 @@ def test_rows_around_what_is_few(api, heads, new, prefix):
     run(api, share(step, [0, 3], [prefix]), [0, 3], [prefix])
 
 
-def test_the_prefix_is_read_from_the_first_sequence_alone(api):
-    """The others' copies of it hold NaN."""
-    step = Step(api, [500, 520, 600, 77], [1, 20, 100, 3], 16, 2, 4, 128, 128, seed=3)
+def test_a_shared_prefix_is_read_once(api):
+    """From the first sequence: what the others have in its place does not matter here."""
+    step = Step(api, [500, 520, 600, 77], [1, 9, 2, 3], 16, 2, 4, 128, 128, seed=3)
     share(step, [0, 3], [430], same_pages=False)
     for b in (1, 2):
         blk, slot = step.place(b, 0, 430)
