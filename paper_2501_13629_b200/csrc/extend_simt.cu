@@ -23,6 +23,11 @@ namespace diffqkv {
 namespace {
 
 constexpr int kRows = 32, kTok = 128, kThreads = 256;
+// Tokens of a tile of the windowed form: with 128-channel heads 64, so that an SM holds two blocks and not one (168 KB): 574
+// rows of 21 sequences in a window of 9 tokens, 32/4/8 heads, 48 us, not 80.  Where every block walks many tiles nothing is
+// gained (21 sequences of 8-16 rows over 550 tokens 179, not 190), so the plain form keeps its 128.
+template <int DQ, int DV, bool kWindow>
+constexpr int tile_tokens = kWindow && (DQ == 128 || DV == 128) ? 64 : kTok;
 constexpr int kMaxSplits = 16;
 
 struct SimtParams {
@@ -46,8 +51,9 @@ __device__ __forceinline__ bool rows_of(const SimtParams& p, int b, int& lo, int
   return ragged_rows(p.cu_q, p.cache.seqlens, b, p.total_q, p.cache.max_seqlen, lo, n, past);
 }
 
-// Where tokens k0 .. k0 + 127 lie: block and slot of each (block -1: not there), a thread per token.  Tokens that no row of
+// Where tokens k0 .. k0 + kTok - 1 lie: block and slot of each (block -1: not there), a thread per token.  Tokens that no row of
 // the tile sees are left out: those from `gap_at` on are `gap` further on in the cache.
+template <int kTok>
 __device__ __forceinline__ void place_tile(const SimtParams& p, int2* place, int b, int k0, int end, int gap_at, int gap) {
   if (threadIdx.x >= kTok) return;
   int tok = k0 + threadIdx.x;
@@ -67,8 +73,8 @@ __device__ __forceinline__ void place_tile(const SimtParams& p, int2* place, int
   place[threadIdx.x] = at;
 }
 
-// Copies the tokens of a tile, one head, into [128][D + 4] floats.
-template <typename T, int D>
+// Copies the tokens of a tile, one head, into [kTok][D + 4] floats.
+template <typename T, int D, int kTok>
 __device__ __forceinline__ void copy_tile(float* dst, const void* pool, long long s_blk, long long s_tok, long long head_off,
                                           const int2* place) {
   constexpr int kPer = 16 / sizeof(T), kVecs = D / kPer;
@@ -100,11 +106,12 @@ __device__ __forceinline__ void copy_tile(float* dst, const void* pool, long lon
 template <typename T, int DQ, int DV, bool kWindow>
 __global__ void __launch_bounds__(kThreads) extend_simt_kernel(const SimtParams p) {
   constexpr int kC = DV / 32;  // channels of V per lane
+  constexpr int kTok = tile_tokens<DQ, DV, kWindow>, kJ = kTok / 32;  // tokens of a tile, and of a lane
   extern __shared__ float4 smem4[];
   float* q_s = reinterpret_cast<float*>(smem4);      // [32][DQ]
-  float* k_s = q_s + kRows * DQ;                     // [128][DQ + 4]
-  float* v_s = k_s + kTok * (DQ + 4);                // [128][DV + 4]
-  float* p_s = v_s + kTok * (DV + 4);                // [32][128]
+  float* k_s = q_s + kRows * DQ;                     // [kTok][DQ + 4]
+  float* v_s = k_s + kTok * (DQ + 4);                // [kTok][DV + 4]
+  float* p_s = v_s + kTok * (DV + 4);                // [32][kTok]
   __shared__ int seq_s, tile_s, scan_s[kThreads / 32];
   __shared__ int2 place_s[2][kTok];  // of this tile's and of the next one's tokens
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -185,36 +192,36 @@ __global__ void __launch_bounds__(kThreads) extend_simt_kernel(const SimtParams 
   const long long k_head = (long long)hk * cv.k_sh, v_head = (long long)hv * cv.v_sh;
   int turn = 0;
   if (t0 < t1) {
-    place_tile(p, place_s[0], b, t0, t1, p.sinks, gap);
+    place_tile<kTok>(p, place_s[0], b, t0, t1, p.sinks, gap);
     __syncthreads();
-    copy_tile<T, DQ>(k_s, cv.k, cv.k_sb, cv.k_st, k_head, place_s[0]);
+    copy_tile<T, DQ, kTok>(k_s, cv.k, cv.k_sb, cv.k_st, k_head, place_s[0]);
     ptx::cp_async_commit();
   }
   const float* q_w = q_s + warp * 4 * DQ;
   float* p_w = p_s + warp * 4 * kTok;
   for (int k0 = t0; k0 < t1; k0 += kTok, turn ^= 1) {
-    copy_tile<T, DV>(v_s, cv.v, cv.v_sb, cv.v_st, v_head, place_s[turn]);
-    if (k0 + kTok < t1) place_tile(p, place_s[turn ^ 1], b, k0 + kTok, t1, p.sinks, gap);
+    copy_tile<T, DV, kTok>(v_s, cv.v, cv.v_sb, cv.v_st, v_head, place_s[turn]);
+    if (k0 + kTok < t1) place_tile<kTok>(p, place_s[turn ^ 1], b, k0 + kTok, t1, p.sinks, gap);
     ptx::cp_async_commit();
     ptx::cp_async_wait<1>();  // K of this tile
     __syncthreads();
     // ---- scores: rows warp * 4 + i, tokens lane + 32 j
-    float s[4][4];
+    float s[4][kJ];
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+      for (int j = 0; j < kJ; ++j) s[i][j] = 0.f;
 #pragma unroll 4
     for (int c = 0; c < DQ; c += 4) {
-      float4 a[4], x[4];
+      float4 a[4], x[kJ];
 #pragma unroll
       for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(q_w + i * DQ + c);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = *reinterpret_cast<const float4*>(k_s + (lane + 32 * j) * (DQ + 4) + c);
+      for (int j = 0; j < kJ; ++j) x[j] = *reinterpret_cast<const float4*>(k_s + (lane + 32 * j) * (DQ + 4) + c);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < kJ; ++j) {
           s[i][j] = fmaf(a[i].x, x[j].x, s[i][j]);
           s[i][j] = fmaf(a[i].y, x[j].y, s[i][j]);
           s[i][j] = fmaf(a[i].z, x[j].z, s[i][j]);
@@ -225,7 +232,7 @@ __global__ void __launch_bounds__(kThreads) extend_simt_kernel(const SimtParams 
     for (int i = 0; i < 4; ++i) {
       float top = -INFINITY;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < kJ; ++j) {
         int tok = k0 + lane + 32 * j;
         bool hidden = tok >= t1;
         if constexpr (kWindow) {
@@ -244,7 +251,7 @@ __global__ void __launch_bounds__(kThreads) extend_simt_kernel(const SimtParams 
       m[i] = next;
       float sum = 0.f;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < kJ; ++j) {
         const float w = exp2f(s[i][j] - ref);
         sum += w;
         p_w[i * kTok + lane + 32 * j] = w;
@@ -256,7 +263,7 @@ __global__ void __launch_bounds__(kThreads) extend_simt_kernel(const SimtParams 
     ptx::cp_async_wait<0>();  // V of this tile
     __syncthreads();          // everybody is through with K
     if (k0 + kTok < t1) {
-      copy_tile<T, DQ>(k_s, cv.k, cv.k_sb, cv.k_st, k_head, place_s[turn ^ 1]);
+      copy_tile<T, DQ, kTok>(k_s, cv.k, cv.k_sb, cv.k_st, k_head, place_s[turn ^ 1]);
       ptx::cp_async_commit();
     }
     // ---- O += P V: channels lane * kC ..
@@ -397,7 +404,7 @@ cudaError_t launch_extend_simt(const DecodeParams& d, const diffqkv_shape& s, co
   p.window = range ? range->window : 0; p.sinks = range ? range->sinks : 0;
   long long most = d.cache.max_seqlen;  // tokens that the rows of a tile see
   if (range && (long long)range->window + range->sinks + p.T - 1 < most) most = (long long)range->window + range->sinks + p.T - 1;
-  p.splits = split_count(s, (int)most, total_q, range ? 128 : 256);
+  p.splits = split_count(s, (int)most, total_q, most < d.cache.max_seqlen ? 128 : 256);
   p.split_tokens = (int)(((most + p.splits - 1) / p.splits + kTok - 1) / kTok * kTok);
   p.out = out; p.out_is_f32 = s.out_dtype == DIFFQKV_F32; p.lse = lse;
   p.part_lse = static_cast<float*>(workspace);
@@ -406,13 +413,16 @@ cudaError_t launch_extend_simt(const DecodeParams& d, const diffqkv_shape& s, co
   p.dev_status = d.dev_status;
   const long long tiles = (long long)total_q / p.T + s.batch;
   const dim3 grid((unsigned)(tiles < total_q ? tiles : total_q), (unsigned)(s.n_q / p.G), (unsigned)p.splits);
-  const size_t smem = sizeof(float) * ((size_t)kRows * s.d_qk + kTok * (s.d_qk + 4) + kTok * (s.d_v + 4) + kRows * kTok);
+  size_t smem = 0;
   void (*fn)(const SimtParams) = nullptr;
 #define DIFFQKV_SIMT_CASE(DQ, DV)                                                                                   \
-  if (s.d_qk == DQ && s.d_v == DV)                                                                                  \
+  if (s.d_qk == DQ && s.d_v == DV) {                                                                                \
+    const size_t tok = range ? tile_tokens<DQ, DV, true> : tile_tokens<DQ, DV, false>;                              \
+    smem = sizeof(float) * ((size_t)kRows * DQ + tok * (DQ + 4) + tok * (DV + 4) + kRows * tok);                    \
     fn = s.dtype == DIFFQKV_F32                                                                                     \
              ? (range ? extend_simt_kernel<float, DQ, DV, true> : extend_simt_kernel<float, DQ, DV, false>)         \
-             : (range ? extend_simt_kernel<__nv_bfloat16, DQ, DV, true> : extend_simt_kernel<__nv_bfloat16, DQ, DV, false>);
+             : (range ? extend_simt_kernel<__nv_bfloat16, DQ, DV, true> : extend_simt_kernel<__nv_bfloat16, DQ, DV, false>); \
+  }
   DIFFQKV_SIMT_CASE(64, 64) DIFFQKV_SIMT_CASE(64, 128) DIFFQKV_SIMT_CASE(128, 64) DIFFQKV_SIMT_CASE(128, 128)
 #undef DIFFQKV_SIMT_CASE
   cudaError_t err = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
