@@ -47,9 +47,9 @@
 // behind it, and extend_merge_kernel joins the two.  A step begins in one short piece of code in 32-bit arithmetic (see
 // ranged_start); a block's first request still goes out 16 thousand cycles, 9 us, after its start, nearly all of it code that
 // is fetched once, and an item costs 7-8 thousand cycles next to its tiles (2.5 of them the masks of its first and last tile).
-// The same four chunks in windows of 2k tokens: 284 us in a graph, 300 call by call, 750 TFLOP/s of what is seen; tensor pipe
-// 44 % active, special-function unit 45 %.  3k rows behind two prefixes of 3k-5k tokens, 64 and 128 channels: 288 us, 250 of
-// them here (power keeps the SMs at 1.4-1.6 GHz) and 36 of joining 98 MB of parts.
+// The same four chunks in windows of 2k tokens: 285 us in a graph, 298 call by call, 750 TFLOP/s of what is seen; tensor pipe
+// 44 % active, special-function unit 45 %.  3k rows behind two prefixes of 3k-5k tokens, 64 and 128 channels: 281 us (power
+// keeps the SMs at 1.4-1.6 GHz); with the prefixes shared 289, 36 of them the join of 98 MB of parts.
 // Tried and not kept: rows written 32 bytes a lane without the exchange of four lanes (329 -> 343 us: the same lines, and
 // none of it was instructions), a thread a barrier at the start (283 -> 289), two rows at a time in the join (36 -> 37), a way
 // of its own there for rows of whole items (36), four blocks of it an SM (34, but 4 x 4 single rows 24.2 -> 25.1).
