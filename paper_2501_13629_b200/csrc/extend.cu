@@ -1139,28 +1139,27 @@ extend_merge_kernel(const ExtendParams p, const ExtendList few, const int rows_e
   __shared__ ItemRef ref_s[kMergeRefs][2];
   const int t0 = blockIdx.x * rows_each, count = min(rows_each, p.total_q - t0);
   {
-    int b = -1, lo = 0, n = 0, past, g_lo = 0, g_hi = 0, prefix = -1;
-    for (int r = 0; r < count; ++r) {
+    for (int r = 0; r < count;) {  // a sequence at a time, all its rows here at once
+      int lo, n, past, g_lo = 0, g_hi = 0;
       const int t = t0 + r;
-      if (b < 0 || t >= lo + n) {  // the next row's sequence
-        b = ragged_sequence_of<kMergeThreads>(p.cu_q, p.seqlens, p.batch, p.total_q, p.max_seqlen, t, false, p.dev_status, lo,
-                                              n, past, [] {});
-        prefix = b < 0 ? -1 : group_prefix(p, b, lo, n, past, g_lo, g_hi);
-      }
-      if (threadIdx.x < 2) {
-        const int k = threadIdx.x, first = k == 0 ? g_lo : lo, rows = k == 0 ? g_hi - g_lo : n, in = t - first;
+      const int b = ragged_sequence_of<kMergeThreads>(p.cu_q, p.seqlens, p.batch, p.total_q, p.max_seqlen, t, false,
+                                                      p.dev_status, lo, n, past, [] {});
+      const int prefix = b < 0 ? -1 : group_prefix(p, b, lo, n, past, g_lo, g_hi), here = b < 0 ? 1 : min(count - r, lo + n - t);
+      for (int x = threadIdx.x; x < 2 * here; x += kMergeThreads) {
+        const int y = r + (x >> 1), k = x & 1, first = k == 0 ? g_lo : lo, rows = k == 0 ? g_hi - g_lo : n, in = t0 + y - first;
         const bool wide = rows > p.thin_max;
-        row_s[0][r].has = row_s[1][r].has = prefix < 0 ? 0 : prefix == 0 ? 1 : 2;
-        row_s[0][r].first[k] = row_s[1][r].first[k] = first;
-        row_s[0][r].rows[k] = row_s[1][r].rows[k] = rows * p.G;
+        row_s[0][y].has = row_s[1][y].has = prefix < 0 ? 0 : prefix == 0 ? 1 : 2;
+        row_s[0][y].first[k] = row_s[1][y].first[k] = first;
+        row_s[0][y].rows[k] = row_s[1][y].rows[k] = rows * p.G;
         if (wide) {  // see SeqOf
           const int blocks = min((rows + p.thin_max - 1) / max(p.thin_max, 1), kMidBlocks + 1), each = (rows + blocks - 1) / blocks;
-          row_s[0][r].first[k] += in / (2 * p.T) * (2 * p.T);
-          row_s[0][r].rows[k] = 0;
-          row_s[1][r].first[k] += in / each * each;
-          row_s[1][r].rows[k] = min(each, rows - in / each * each) * p.G;
+          row_s[0][y].first[k] += in / (2 * p.T) * (2 * p.T);
+          row_s[0][y].rows[k] = 0;
+          row_s[1][y].first[k] += in / each * each;
+          row_s[1][y].rows[k] = min(each, rows - in / each * each) * p.G;
         }
       }
+      r += here;
     }
   }
   __syncthreads();
