@@ -798,7 +798,8 @@ def diffqkv_extend_shared(q: torch.Tensor, cu_q: torch.Tensor, cache: KVCache, c
                           lse: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None,
                           out_dtype: Optional[torch.dtype] = None, stream: Optional[torch.cuda.Stream] = None):
     """diffqkv_extend for a batch in which the sequences cu_groups[g] .. cu_groups[g + 1] - 1 (int32 [groups + 1]) hold the
-    same first prefix_lens[g] tokens (int32 [groups]): these are read once, from the pages of the group's first sequence."""
+    same first prefix_lens[g] tokens (int32 [groups]): these are read once, from the pages of the group's first sequence,
+    where that saves more than joining the two parts of a row costs."""
     groups = prefix_lens.numel()
     return _extend("diffqkv_extend_shared", (_pack_prefixes(_ints(cu_groups, groups + 1), _ints(prefix_lens), groups),),
                    _raw.diffqkv_extend_shared_workspace_bytes, q, cu_q, cache, n_k, n_v, scale, workspace, out, lse,
