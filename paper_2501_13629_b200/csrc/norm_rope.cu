@@ -28,7 +28,7 @@ namespace {
 struct NormParams {
   const void* q_weight;
   const void* k_weight;
-  long long q_wst, k_wst;  // elements between heads
+  long long q_wst, k_wst;  // elements between heads; 0: one for all of them, or none
   float eps, offset, inv_d;
   int lanes, lanes_log2;   // of a head, a power of two
   int tasks, rot_tasks, rest;  // of a head: those that turn and, in vectors, what does not
@@ -361,7 +361,8 @@ cudaError_t launch_norm_rope_append(const void* q, const void* k_new, const void
   m.rot_tasks = p.rot / (2 * n); m.rest = (p.d_qk - p.rot) / n; m.tasks = m.rot_tasks + (m.rest + 1) / 2;
   m.v_magic = (65536 + s.d_v / n - 1) / (s.d_v / n);
   m.q_weight = norm.q_weight; m.k_weight = norm.k_weight;
-  m.q_wst = norm.q_head_stride; m.k_wst = norm.k_head_stride;
+  // (a weight that is not there has no heads of its own: the heads' places are reckoned from its address)
+  m.q_wst = norm.q_weight ? norm.q_head_stride : 0; m.k_wst = norm.k_weight ? norm.k_head_stride : 0;
   m.eps = norm.eps; m.offset = norm.weight_offset; m.inv_d = 1.f / (float)s.d_qk;
   m.lanes_log2 = 0;
   while (m.lanes_log2 < 5 && 1 << m.lanes_log2 < m.tasks) ++m.lanes_log2;

@@ -254,3 +254,39 @@ def test_a_captured_call_replays_with_other_lengths(api):
                 pos = torch.arange(past[b], past[b] + hi - lo, device="cuda")
                 check(out[lo:hi], q[lo:hi], w, 1e-6, 0.0, pos, inv, False, 1.0, f"q of sequence {b}")
         assert bool((out[cu[-1]:] == 9.0).all())
+
+
+@pytest.mark.parametrize("d_qk", [64, 128, 520, 1096])
+@pytest.mark.parametrize("offset", [0.0, 1.0])
+@pytest.mark.parametrize("given", ["neither", "q", "k"])
+def test_a_missing_weight_has_no_head_stride(api, d_qk, offset, given):
+    """Through the C structure: a stride beside a weight that is NULL changes nothing, for heads that their lanes hold and for
+    longer ones."""
+    step = Step(api, [5, 300], [3, 30], 12, 2, 4, d_qk, 64, pad=2, seed=1).fill(whole=False)
+    gen = torch.Generator("cuda").manual_seed(d_qk)
+    q, k, v = (torch.randn((step.total_q, h, d), generator=gen, device="cuda").to(BF16)
+               for h, d in ((12, d_qk), (2, d_qk), (4, 64)))
+    qw, kw = (torch.randn((h, d_qk), generator=gen, device="cuda").to(BF16) if given == name else None
+              for h, name in ((12, "q"), (2, "k")))
+    inv = api.rope_frequencies(16, 10000.0, device="cuda")[0]
+    pools = step.k.clone(), step.v.clone()
+    got = []
+    for stray in (0, d_qk, 8 * d_qk):
+        step.k.copy_(pools[0])
+        step.v.copy_(pools[1])
+        strides = [stray if w is None else d_qk for w in (qw, kw)]
+        norm = api._pack_norm(*(0 if w is None else w.data_ptr() for w in (qw, kw)), *strides, api.BF16, 1e-6, offset)
+        out, status = torch.full_like(q, 5.0), ints([0])
+        assert api._raw.diffqkv_norm_rope_append(
+            q.data_ptr(), k.data_ptr(), v.data_ptr(), step.cu.data_ptr(), step.total_q, 0, 0, 0, norm,
+            api._pack_rope(inv.data_ptr(), 0, 16, False, 1.0), api._cache_bytes(step.cache, 2, 4, d_qk, 64),
+            api._pack_shape(2, 12, 2, 4, d_qk, 64, api.BF16, api.BF16, 1.0), out.data_ptr(), status.data_ptr(),
+            torch.cuda.current_stream().cuda_stream) == api.OK
+        torch.cuda.synchronize()
+        assert int(status.item()) == 0
+        got.append((out, step.k.clone()))
+    pos = torch.arange(5, 8, device="cuda")
+    check(got[0][0][:3], q[:3], qw, 1e-6, offset, pos, inv, False, 1.0, "q")
+    for out, pool in got[1:]:
+        assert torch.equal(out, got[0][0])
+        assert torch.equal(pool.view(torch.int16), got[0][1].view(torch.int16))
