@@ -215,7 +215,10 @@ __device__ __forceinline__ bool group_rows(const ExtendParams& p, int g, int& lo
 // behind 8k 102, 122; single rows in pairs behind 400 tokens 22, 19, behind 1k 23, 25.
 constexpr int kShareTokens = 512, kShareLeast = 1024;
 constexpr float kShareLong = 1000.f;
-__device__ __forceinline__ bool worth_sharing(const ExtendParams& p, int rows, int seqs, int prefix) {
+// Never where the first sequence, from which a shared prefix is read, does not hold it (it may have no rows and be given up).
+__device__ __forceinline__ bool worth_sharing(const ExtendParams& p, int first, int end, int rows, int prefix) {
+  if (rows == 0 || prefix == 0 || p.seqlens[first] < prefix) return false;
+  const int seqs = end - first;
   if (rows <= seqs * p.thin_max) return (float)prefix * (seqs - 1) >= (float)kShareTokens;
   return (float)(prefix - kShareLeast) * p.T * seqs >= kShareLong * rows;
 }
@@ -231,7 +234,7 @@ __device__ __forceinline__ int group_prefix(const ExtendParams& p, int b, int lo
   if (b < p.cu_groups[g] || b >= p.cu_groups[g + 1]) return 0;
   int first, prefix;
   if (!group_rows(p, g, g_lo, g_hi, first, prefix) || prefix > past || lo < g_lo || lo + n > g_hi) return -1;
-  return worth_sharing(p, g_hi - g_lo, p.cu_groups[g + 1] - first, prefix) ? prefix : 0;
+  return worth_sharing(p, first, p.cu_groups[g + 1], g_hi - g_lo, prefix) ? prefix : 0;
 }
 
 // One sequence of the step as the list of long chunks has it.
@@ -287,7 +290,7 @@ struct SeqOf<true> {
       int hi;
       bad = false;  // of a group that does not fit every sequence with rows says so
       back = p.cu_groups[x + 1] < p.cu_groups[x];
-      n = group_rows(p, x, lo, hi, tab, past) && past > 0 && worth_sharing(p, hi - lo, p.cu_groups[x + 1] - tab, past) ? hi - lo : 0;
+      n = group_rows(p, x, lo, hi, tab, past) && worth_sharing(p, tab, p.cu_groups[x + 1], hi - lo, past) ? hi - lo : 0;
       if (n == 0) past = 0;
       end = past;
       dst = kDstPrefix;
@@ -386,8 +389,8 @@ __device__ __forceinline__ bool long_entry(const ExtendParams& p, int x) {
   int lo, hi;
   if (x < p.groups) {
     int first, prefix;
-    return group_rows(p, x, lo, hi, first, prefix) && prefix > 0 && hi - lo > p.thin_max &&
-           worth_sharing(p, hi - lo, p.cu_groups[x + 1] - first, prefix);
+    return group_rows(p, x, lo, hi, first, prefix) && hi - lo > p.thin_max &&
+           worth_sharing(p, first, p.cu_groups[x + 1], hi - lo, prefix);
   }
   return p.cu_q[x - p.groups + 1] - p.cu_q[x - p.groups] > p.thin_max;
 }

@@ -355,3 +355,24 @@ def test_random_steps(api, seed):
     step = Step(api, past, new, n_q, n_k, n_v, *dims, page=r.choice([8, 16, 32, 64, 128, 256]),
                 layout=r.choice(["paged", "paged", "token", "flat"]), pad=r.randint(0, 3), seed=seed, room=r.randint(0, 50))
     run(api, share(step, ends, prefix), ends, prefix)
+
+
+@pytest.mark.parametrize("layout", ["paged", "flat"])
+@pytest.mark.parametrize("first", [0, 5999, -1])
+@pytest.mark.parametrize("new", [[0, 1, 2], [0, 3, 120], [2, 1, 2], [3, 1, 90]])
+def test_a_first_sequence_without_the_prefix(api, layout, first, new):
+    """What it has behind its length are not the group's tokens: the others read their own."""
+    step = Step(api, [6000, 6100, 6050, 90], new + [5], 16, 2, 4, 128, 128, layout=layout, seed=sum(new), pad=2)
+    share(step, [0, 3], [6000], same_pages=False)
+    blk, slot = step.place(0, max(first, 0), 6000)
+    step.k[blk, :, slot] = 0.5  # left there by somebody else
+    step.v[blk, :, slot] = -3.0
+    if layout == "paged":
+        step.table[0, -(-max(first, 0) // step.page):] = -1
+    step.lens[0] = first
+    out, status = torch.full((step.total_q, 16, 128), 77.0, dtype=BF16, device="cuda"), ints([0])
+    api.diffqkv_extend_shared(step.q, step.cu, step.cache, ints([0, 3]), ints([6000]), 2, 4, 0.1, out=out, dev_status=status)
+    fits = first >= 0 and new[0] == 0  # (a length below 0 is reported of a sequence without rows too)
+    assert int(status.item()) == (0 if fits else 1 << api.ERR_INDEX)
+    check(step, out, None, 0.1, joined=True, only=[1, 2, 3])
+    assert bool((out[:new[0]] == 77.0).all()) and bool((out[step.rows:] == 77.0).all())
