@@ -330,7 +330,7 @@ struct SeqOf<true> {
   __device__ int mid(const ExtendParams& p) const {
     if (n == 0) return 0;
     if (p.thin_max == 0 || blocks > kMidBlocks || thin_tiles > kMidLong / kFewItemCost) return kMidLong;
-    return min(p.n_units * few_unit(p), kMidLong);
+    return min(min(p.n_units, kMidLong) * min(few_unit(p), kMidLong), kMidLong);  // (a unit alone may be 2^18)
   }
   // cost of one of extend_few.cu's tiles, by its groups of 16 rows: up to two, up to four, more
   __device__ int few_cost(const ExtendParams& p) const {
