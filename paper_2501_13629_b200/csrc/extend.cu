@@ -1153,7 +1153,7 @@ extend_merge_kernel(const ExtendParams p, const ExtendList few, const int rows_e
         row_s[0][y].first[k] = row_s[1][y].first[k] = first;
         row_s[0][y].rows[k] = row_s[1][y].rows[k] = rows * p.G;
         if (wide) {  // see SeqOf
-          const int blocks = min((rows + p.thin_max - 1) / max(p.thin_max, 1), kMidBlocks + 1), each = (rows + blocks - 1) / blocks;
+          const int blocks = few_blocks(p, rows), each = (rows + blocks - 1) / blocks;
           row_s[0][y].first[k] += in / (2 * p.T) * (2 * p.T);
           row_s[0][y].rows[k] = 0;
           row_s[1][y].first[k] += in / each * each;

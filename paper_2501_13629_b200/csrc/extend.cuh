@@ -237,6 +237,12 @@ __device__ __forceinline__ int group_prefix(const ExtendParams& p, int b, int lo
   return worth_sharing(p, first, p.cu_groups[g + 1], g_hi - g_lo, prefix) ? prefix : 0;
 }
 
+// Blocks that the kernel of few rows would cut n > thin_max rows into; one more than it takes, for more, and where a single
+// token's heads are too many for it (thin_max 0).
+__device__ __forceinline__ int few_blocks(const ExtendParams& p, int n) {
+  return p.thin_max == 0 ? kMidBlocks + 1 : min((n + p.thin_max - 1) / p.thin_max, kMidBlocks + 1);
+}
+
 // One sequence of the step as the list of long chunks has it.
 template <bool kRanged>
 struct SeqOf;
@@ -315,7 +321,7 @@ struct SeqOf<true> {
     thin_tiles = n > 0 ? (end + kFewT - 1) / kFewT - skip_few(p) : 0;
     if (n > p.thin_max) {
       items = (n + 2 * p.T - 1) / (2 * p.T);
-      blocks = min((n + p.thin_max - 1) / max(p.thin_max, 1), kMidBlocks + 1);
+      blocks = few_blocks(p, n);
       block_rows = (n + blocks - 1) / blocks;
     } else {
       n = 0;
@@ -329,7 +335,7 @@ struct SeqOf<true> {
   // the other kernel's cost of a long chunk
   __device__ int mid(const ExtendParams& p) const {
     if (n == 0) return 0;
-    if (p.thin_max == 0 || blocks > kMidBlocks || thin_tiles > kMidLong / kFewItemCost) return kMidLong;
+    if (blocks > kMidBlocks || thin_tiles > kMidLong / kFewItemCost) return kMidLong;
     return min(min(p.n_units, kMidLong) * min(few_unit(p), kMidLong), kMidLong);  // (a unit alone may be 2^18)
   }
   // cost of one of extend_few.cu's tiles, by its groups of 16 rows: up to two, up to four, more

@@ -35,3 +35,27 @@ def test_a_chunk_of_very_many_heads_whose_cost_passes_32_bits(api):
             bound = weight * mean_abs * (1 + weight)
             bound = bound + HALF_STEP[BF16] * (ref.abs() + bound)
             assert bool(((out[rows, h:h + 1].double() - ref).abs() <= bound).all()), (h, rows)
+
+
+@pytest.mark.parametrize("heads", [(256, 1, 2), (132, 1, 4), (256, 2, 1)])
+@pytest.mark.parametrize("past,new", [([300], [1]), ([300], [2]), ([300, 290, 40], [1, 2, 1]), ([0, 5], [1, 1]),
+                                      ([700, 650], [1, 130])])
+def test_head_groups_too_wide_for_few_rows(api, heads, past, new):
+    """A token's heads alone fill what the kernel of few rows has for a group: every chunk is a long one."""
+    step = Step(api, past, new, *heads, 64, 128, seed=sum(new), pad=2).fill()
+    for window, sinks in ((50, 3), (5000, 0)):
+        out, status = torch.full((step.total_q, heads[0], 128), 77.0, dtype=BF16, device="cuda"), ints([0])
+        forget(step, window, sinks)
+        api.diffqkv_extend_window(step.q, step.cu, step.cache, *heads[1:], 0.125, window, sinks=sinks, out=out, dev_status=status)
+        assert int(status.item()) == 0 and bool((out[step.rows:] == 77.0).all())
+        check(step, out, None, 0.125, window, sinks)
+        step = Step(api, past, new, *heads, 64, 128, seed=sum(new), pad=2).fill()
+    prefix = min(past)
+    for b in range(1, len(past)):
+        step.k_tok[b][:prefix], step.v_tok[b][:prefix] = step.k_tok[0][:prefix], step.v_tok[0][:prefix]
+    step.fill()
+    out, status = torch.full((step.total_q, heads[0], 128), 77.0, dtype=BF16, device="cuda"), ints([0])
+    api.diffqkv_extend_shared(step.q, step.cu, step.cache, ints([0, len(past)]), ints([prefix]), *heads[1:], 0.125, out=out,
+                              dev_status=status)
+    assert int(status.item()) == 0 and bool((out[step.rows:] == 77.0).all())
+    check(step, out, None, 0.125, joined=True)
