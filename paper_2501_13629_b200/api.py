@@ -876,12 +876,14 @@ def diffqkv_norm_rope_append(q: Optional[torch.Tensor], k_new: torch.Tensor, v_n
                              stream: Optional[torch.cuda.Stream] = None):
     """diffqkv_rope_append behind a root-mean-square norm of every q and k head: x / sqrt(mean x^2 + eps) * (weight_offset +
     weight).  Weights are [d_qk] or one for each head ([n_q, d_qk], [n_k, d_qk]), of q's type or both float32; None =
-    nothing but the norm."""
+    nothing but the norm.  Without q its weight is not looked at."""
     n_k, d_qk = k_new.shape[1:]
+    if q is None:
+        q_weight = None
     given = k_weight if k_weight is not None else q_weight
     dtype = k_new.dtype if given is None else given.dtype
     kw, k_stride = _head_weight("k_weight", k_weight, n_k, d_qk, dtype)
-    qw, q_stride = _head_weight("q_weight", q_weight, 0 if q is None else q.shape[1], d_qk, dtype)
+    qw, q_stride = (0, 0) if q is None else _head_weight("q_weight", q_weight, q.shape[1], d_qk, dtype)
     norm = _pack_norm(qw, kw, q_stride, k_stride, _DTYPES[dtype], eps, weight_offset)
     return _rope_append("diffqkv_norm_rope_append", (norm,), q, k_new, v_new, cu_q, cache, inv_freq, interleaved, magnitude,
                         positions, q_out, dev_status, stream, q_weight, k_weight)

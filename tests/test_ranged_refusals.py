@@ -217,3 +217,16 @@ def test_calls_on_the_host_are_refused(api):
     with pytest.raises(ValueError):
         api.diffqkv_norm_rope_append(z(5, 8, 64), z(5, 2, 64), z(5, 4, 64), ints(3), kv(api), None, None, None, 1e-6)
     assert api.launch_count() == before
+
+
+def test_the_queries_weight_where_there_are_no_queries(api, recorded):
+    """A step that only writes keys may be given the layer's two weights all the same."""
+    for qw in (z(64), z(8, 64), z(1, 64).expand(8, 64), None):
+        args = made(recorded, lambda: api.diffqkv_norm_rope_append(None, z(5, 2, 64), z(5, 4, 64), ints(3), kv(api), None, qw,
+                                                                   z(64), 1e-6, stream=STREAM))
+        s = api.QkNormStruct.from_buffer_copy(args[8])
+        assert s.q_weight is None and s.q_head_stride == 0 and s.k_weight is not None and s.weight_dtype == api.BF16
+        assert args[0] in (None, 0)
+    args = made(recorded, lambda: api.diffqkv_norm_rope_append(None, z(5, 2, 64), z(5, 4, 64), ints(3), kv(api), None,
+                                                               z(8, 64, dtype=F32), None, 1e-6, stream=STREAM))
+    assert api.QkNormStruct.from_buffer_copy(args[8]).q_weight is None
