@@ -91,6 +91,13 @@ void diffqkv_debug_decode_timeout(int64_t wait_limit_ns, int64_t skip_tile);
 void diffqkv_debug_extend_kernel(int32_t choice);
 int32_t diffqkv_last_extend_kernel(void);
 
+/*
+ * Test hook (process-wide host state): which groups' prefixes diffqkv_extend_shared reads once on the tensor cores, 0 = those
+ * of which that saves something (default), 1 = all that can be (the first sequence holds them), 2 = none.  Results differ only
+ * in rounding.
+ */
+void diffqkv_debug_extend_sharing(int32_t choice);
+
 #ifdef __cplusplus
 }
 #endif

@@ -39,7 +39,7 @@ EXPORTS = (
     "diffqkv_extend", "diffqkv_extend_workspace_bytes", "diffqkv_rope_append", "diffqkv_rope_frequencies",
     "diffqkv_pages_free", "diffqkv_pages_fork", "diffqkv_pages_fork_workspace_bytes", "diffqkv_pages_reserve",
     "diffqkv_pages_reserve_workspace_bytes", "diffqkv_pages_copy", "diffqkv_pages_compact",
-    "diffqkv_pages_compact_workspace_bytes", "diffqkv_debug_extend_kernel", "diffqkv_last_extend_kernel",
+    "diffqkv_pages_compact_workspace_bytes", "diffqkv_debug_extend_kernel", "diffqkv_last_extend_kernel", "diffqkv_debug_extend_sharing",
     "diffqkv_extend_window", "diffqkv_extend_window_workspace_bytes", "diffqkv_extend_shared", "diffqkv_extend_shared_workspace_bytes", "diffqkv_norm_rope_append",
 )
 
@@ -809,6 +809,11 @@ def diffqkv_extend_shared(q: torch.Tensor, cu_q: torch.Tensor, cache: KVCache, c
 def extend_kernel(choice: int) -> None:
     """Test hook: the kernel diffqkv_extend takes (0 automatic, 1 a block per row, 2 tiles on FMAs)."""
     _lib.diffqkv_debug_extend_kernel(C.c_int32(choice))
+
+
+def extend_sharing(choice: int) -> None:
+    """Test hook: the prefixes that diffqkv_extend_shared reads once (0 where that saves something, 1 all that can be, 2 none)."""
+    _lib.diffqkv_debug_extend_sharing(C.c_int32(choice))
 
 
 def last_extend_kernel() -> int:

@@ -440,10 +440,11 @@ diffqkv_status diffqkv_decode_topk(const void* q, const diffqkv_cache* cache, co
   return diffqkv_decode_topk_ids(q, cache, shape, topk, workspace, workspace_bytes, out, lse, nullptr, dev_status, stream);
 }
 
-static std::atomic<int> g_extend_choice{0}, g_last_extend_kernel{0};  // test hooks, see diffqkv_debug.h
+static std::atomic<int> g_extend_choice{0}, g_last_extend_kernel{0}, g_extend_sharing{0};  // test hooks, see diffqkv_debug.h
 
 void diffqkv_debug_extend_kernel(int32_t choice) { g_extend_choice = choice; }
 
+void diffqkv_debug_extend_sharing(int32_t choice) { g_extend_sharing = choice; }
 int32_t diffqkv_last_extend_kernel(void) { return g_last_extend_kernel; }
 
 size_t diffqkv_extend_workspace_bytes(const diffqkv_shape* shape, int32_t total_q) {
@@ -532,6 +533,7 @@ static diffqkv_status range_of(const diffqkv_prefixes* prefixes, ExtendRange* ra
   range->groups = prefixes->num_groups;
   range->cu_groups = prefixes->cu_seqs;
   range->prefix_lens = prefixes->lens;
+  range->share = g_extend_sharing;
   return DIFFQKV_OK;
 }
 

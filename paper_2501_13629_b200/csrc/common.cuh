@@ -207,6 +207,7 @@ struct ExtendRange {
   int groups;         // of sequences that share their first tokens; the window does not apply to these
   const int* cu_groups;
   const int* prefix_lens;
+  int share;          // which of their prefixes are read once: 0 where that saves something, 1 all that can be, 2 none
 };
 size_t extend_workspace_bytes(const diffqkv_shape& s, int total_q, bool ranged);
 size_t extend_groups_workspace_bytes(const diffqkv_shape& s, int total_q);  // on top of that

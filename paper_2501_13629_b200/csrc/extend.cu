@@ -1414,7 +1414,7 @@ cudaError_t launch_extend_lengths(const int* cu_q, int total_q, const diffqkv_ca
   ExtendParams p = {};
   p.cu_q = cu_q; p.seqlens = c.seqlens; p.max_seqlen = c.max_seqlen;
   p.batch = batch; p.total_q = total_q;
-  p.groups = range.groups; p.cu_groups = range.cu_groups; p.prefix_lens = range.prefix_lens;
+  p.groups = range.groups; p.cu_groups = range.cu_groups; p.prefix_lens = range.prefix_lens; p.share = 2;
   extend_lengths_kernel<<<(unsigned)((batch + 127) / 128), 128, 0, stream>>>(p, seqlens);
   count_launch();
   return cudaGetLastError();
@@ -1514,7 +1514,7 @@ cudaError_t launch_extend(const void* q, const int* cu_q, int total_q, const dif
     p.sink_tiles = (p.sinks + kKT - 1) / kKT;
     p.sink_few = (p.sinks + kFewT - 1) / kFewT;
     p.groups = range->groups; p.entries = range->groups + s.batch;
-    p.cu_groups = range->cu_groups; p.prefix_lens = range->prefix_lens;
+    p.cu_groups = range->cu_groups; p.prefix_lens = range->prefix_lens; p.share = range->share;
     if (p.groups > 0) place_buffers(s, pl, total_q, static_cast<char*>(workspace) + extend_workspace_bytes(s, total_q, true), &p);
   }
   const int thin_blocks = pl.thin_max > 0 ? pl.blocks : 0, blocks = pl.n_teams * pl.parts;

@@ -84,6 +84,7 @@ struct ExtendParams {
   int groups, entries;
   const int* cu_groups;
   const int* prefix_lens;
+  int share;            // see ExtendRange
   RowBuffer buffer[2];  // kDstPrefix - 1, kDstOwn - 1
   ItemRef* refs;        // [2][total_q][n_units], and one that says whether the step is left out, and whether its rows are all few
 };
@@ -218,6 +219,7 @@ constexpr float kShareLong = 1000.f;
 // Never where the first sequence, from which a shared prefix is read, does not hold it (it may have no rows and be given up).
 __device__ __forceinline__ bool worth_sharing(const ExtendParams& p, int first, int end, int rows, int prefix) {
   if (rows == 0 || prefix == 0 || p.seqlens[first] < prefix) return false;
+  if (p.share != 0) return p.share == 1;
   const int seqs = end - first;
   if (rows <= seqs * p.thin_max) return (float)prefix * (seqs - 1) >= (float)kShareTokens;
   return (float)(prefix - kShareLeast) * p.T * seqs >= kShareLong * rows;
