@@ -409,8 +409,8 @@ typedef struct {
  *   prefixes   every sequence of a group that has rows in the step has at least lens[g] tokens cached, in its own pages (or
  *              slab) as for diffqkv_extend; those of all sequences of a group are the same, usually the same pages.  A shared
  *              prefix is read from the group's FIRST sequence, which may have no rows itself; where that one holds fewer than
- *              lens[g] tokens (it has been given up), and where sharing would save nothing (short prefixes, long chunks, a
- *              group of one), every sequence reads its own.  A sequence whose group does not fit it (a prefix longer than its
+ *              lens[g] tokens (it has been given up), and where sharing would save nothing (short prefixes, long chunks, one
+ *              sequence alone with rows), every sequence reads its own.  A sequence whose group does not fit it (a prefix longer than its
  *              cache or than max_seqlen, or negative, an end of the group outside the batch, rows outside the group's) is
  *              reported as DIFFQKV_ERR_INDEX and skipped.
  *   workspace  diffqkv_extend_shared_workspace_bytes(shape, total_q) bytes, 256-byte aligned (it holds both parts of every

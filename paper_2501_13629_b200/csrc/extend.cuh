@@ -208,35 +208,66 @@ __device__ __forceinline__ bool group_rows(const ExtendParams& p, int g, int& lo
   hi = p.cu_q[end];
   return lo >= 0 && hi >= lo && hi <= p.total_q && prefix <= 0x7ffffe00 - (hi - lo);  // positions stay within 32 bits
 }
-// Whether a prefix of that many tokens is worth an entry of its own next to its sequences', which read it each otherwise.  It
-// costs items more, and two parts to every row that are joined.  With few rows to a sequence that is as much as reading some
-// hundred tokens more; long chunks are bound by their products, of which sharing saves the empty rows of their tiles alone.
-// Shared and not: 12 chunks of 96-192 rows of three groups behind 14-29 tokens 83, 58 us; 6 of 300-500 rows behind 2k tokens
-// 215, 201; 16 of 20-30 rows behind 1k 52, 46; 16 of 30-60 behind 4k 100, 112; 8 of 40-80 behind 16k 162, 239; two of 220
-// behind 8k 102, 122; single rows in pairs behind 400 tokens 22, 19, behind 1k 23, 25.
-constexpr int kShareTokens = 512, kShareLeast = 1024;
-constexpr float kShareLong = 1000.f;
+// Whether the prefix of a group, sequences first .. end - 1 with the rows lo .. hi - 1, is worth an entry of its own next to its
+// sequences', which read it each otherwise.  It costs items more, and two parts to every row that are joined, and saves the
+// reading of all sequences with rows but one.  With few rows to a sequence the cost is as much as reading some hundred tokens
+// more; long chunks are bound by their products, of which sharing saves the empty rows of their tiles alone.
+// Shared and not, in us, 32/4/8 heads of 128 channels behind 100 tokens of their own: 3 chunks of 100-140 rows behind 8k tokens
+// 84, 96; 2 of 150 behind 8k 75, 81; 4 of 500 behind 4k 206, 191; 8 of 260 behind 4k 205, 197; 16 of 40 behind 8k 124, 172; two
+// single rows behind 400 tokens 22, 19, behind 1k 23, 25.  Over 604 steps (2-16 chunks of 20-600 rows behind 1k-32k tokens, four
+// head layouts) the rule is 1.1 % slower in the mean than the better of the two; with 500 or 1000 for 700 1.2 and 1.3 %.
 // Never where the first sequence, from which a shared prefix is read, does not hold it (it may have no rows and be given up).
-__device__ __forceinline__ bool worth_sharing(const ExtendParams& p, int first, int end, int rows, int prefix) {
+constexpr int kShareTokens = 512, kShareLeast = 1024;
+constexpr float kShareLong = 700.f;
+constexpr int kShareLook = 64;  // sequences that are looked at, until enough have rows; those behind them are taken to have some
+__device__ __forceinline__ bool sharing_saves(const ExtendParams& p, int rows, int prefix, int readers) {  // stays true with more of them
+  if (rows <= readers * p.thin_max) return (float)prefix * (readers - 1) >= (float)kShareTokens;
+  return (float)(prefix - kShareLeast) * p.T * (readers - 1) >= kShareLong * rows;
+}
+__device__ __forceinline__ bool worth_sharing(const ExtendParams& p, int first, int end, int lo, int hi, int prefix) {
+  const int rows = hi - lo;
   if (rows == 0 || prefix == 0 || p.seqlens[first] < prefix) return false;
   if (p.share != 0) return p.share == 1;
-  const int seqs = end - first;
-  if (rows <= seqs * p.thin_max) return (float)prefix * (seqs - 1) >= (float)kShareTokens;
-  return (float)(prefix - kShareLeast) * p.T * seqs >= kShareLong * rows;
+  const int look = min(end, first + kShareLook);
+  int readers = min(end - first, rows), b = first - 1, at = lo;  // at first as many as there can be
+#pragma unroll 1
+  for (;;) {
+    const bool saves = sharing_saves(p, rows, prefix, readers);
+    if (b < first) {
+      if (!saves) return false;
+      b = first;
+      readers = 0;
+    } else if (saves || b == look) {
+      return saves;
+    }
+    while (b < look) {  // up to the next one with rows
+      const int next = p.cu_q[++b];
+      if (next <= at) continue;
+      at = next;
+      ++readers;
+      break;
+    }
+    if (b == look) readers += min(end - b, hi - at);
+  }
 }
-// Tokens of sequence b, whose rows are lo .. lo + n - 1 behind `past` tokens, that its group has for it (0 outside of all
-// groups, and where they are not shared); -1 when the group's rows or tokens do not hold those of the sequence.  The group's rows are g_lo .. g_hi - 1.
-__device__ __forceinline__ int group_prefix(const ExtendParams& p, int b, int lo, int n, int past, int& g_lo, int& g_hi) {
+// The group that sequence b is in, -1: none.
+__device__ __forceinline__ int group_of(const ExtendParams& p, int b) {
   int g = 0, z = p.groups;  // the last group that begins at or before b
-  if (z == 0) return 0;
+  if (z == 0) return -1;
   while (z - g > 1) {
     const int mid = (g + z) >> 1;
     if (p.cu_groups[mid] <= b) g = mid; else z = mid;
   }
-  if (b < p.cu_groups[g] || b >= p.cu_groups[g + 1]) return 0;
+  return b < p.cu_groups[g] || b >= p.cu_groups[g + 1] ? -1 : g;
+}
+// Tokens of sequence b, whose rows are lo .. lo + n - 1 behind `past` tokens, that its group has for it (0 outside of all
+// groups, and where they are not shared); -1 when the group's rows or tokens do not hold those of the sequence.  The group's rows are g_lo .. g_hi - 1.
+__device__ __forceinline__ int group_prefix(const ExtendParams& p, int b, int lo, int n, int past, int& g_lo, int& g_hi) {
+  const int g = group_of(p, b);
+  if (g < 0) return 0;
   int first, prefix;
   if (!group_rows(p, g, g_lo, g_hi, first, prefix) || prefix > past || lo < g_lo || lo + n > g_hi) return -1;
-  return worth_sharing(p, first, p.cu_groups[g + 1], g_hi - g_lo, prefix) ? prefix : 0;
+  return worth_sharing(p, first, p.cu_groups[g + 1], g_lo, g_hi, prefix) ? prefix : 0;
 }
 
 // Blocks that the kernel of few rows would cut n > thin_max rows into; one more than it takes, for more, and where a single
@@ -294,26 +325,35 @@ struct SeqOf<true> {
   __device__ void load(const ExtendParams& p, int x) {
     start = 0;
     dst = kDstOut;
-    if (x < p.groups) {  // every row of the group sees the whole prefix: as if it were cached before any of them
-      int hi;
-      bad = false;  // of a group that does not fit every sequence with rows says so
-      back = p.cu_groups[x + 1] < p.cu_groups[x];
-      n = group_rows(p, x, lo, hi, tab, past) && worth_sharing(p, tab, p.cu_groups[x + 1], hi - lo, past) ? hi - lo : 0;
-      if (n == 0) past = 0;
-      end = past;
-      dst = kDstPrefix;
-    } else {
+    int g = x, g_lo = 0, g_hi = 0, first = 0, prefix = 0;
+    bad = back = false;
+    if (x >= p.groups) {
       tab = x - p.groups;
       bad = !load_rows(p, tab, lo, n, past);
       back = bad && p.cu_q[tab + 1] < lo;
-      if (!bad && n > 0) {
-        int g_lo, g_hi;
-        start = group_prefix(p, tab, lo, n, past, g_lo, g_hi);
-        if (start < 0) {
-          bad = true;
-          n = start = past = 0;
-        }
-        if (start > 0) dst = kDstOwn;
+      g = n > 0 ? group_of(p, tab) : -1;
+    }
+    bool fits = true, shared = false;
+    if (g >= 0) {  // the same code for prefixes and sequences
+      fits = group_rows(p, g, g_lo, g_hi, first, prefix);
+      shared = fits && worth_sharing(p, first, p.cu_groups[g + 1], g_lo, g_hi, prefix);
+    }
+    if (x < p.groups) {  // every row of the group sees the whole prefix: as if it were cached before any of them
+      back = p.cu_groups[x + 1] < p.cu_groups[x];  // (of a group that does not fit every sequence with rows says so)
+      tab = first;
+      lo = g_lo;
+      n = shared ? g_hi - g_lo : 0;
+      past = end = shared ? prefix : 0;
+      dst = kDstPrefix;
+    } else {
+      if (g >= 0 && (!fits || prefix > past || lo < g_lo || lo + n > g_hi)) {
+        bad = true;
+        shared = false;
+        n = past = 0;
+      }
+      if (shared) {
+        start = prefix;
+        dst = kDstOwn;
       }
       end = past + n;
     }
@@ -392,13 +432,13 @@ struct SeqOf<true> {
 template <bool kRanged>
 __device__ __forceinline__ int entries_of(const ExtendParams& p) { return kRanged ? p.entries : p.batch; }
 
-// Whether an entry of a ranged step is for the kernel of long chunks, if it fits.
+// Whether an entry of a ranged step may be for the kernel of long chunks, if it fits.
 __device__ __forceinline__ bool long_entry(const ExtendParams& p, int x) {
   int lo, hi;
   if (x < p.groups) {
     int first, prefix;
-    return group_rows(p, x, lo, hi, first, prefix) && hi - lo > p.thin_max &&
-           worth_sharing(p, first, p.cu_groups[x + 1], hi - lo, prefix);
+    return group_rows(p, x, lo, hi, first, prefix) && hi - lo > p.thin_max && p.share != 2 &&
+           (p.share == 1 || sharing_saves(p, hi - lo, prefix, min(p.cu_groups[x + 1] - first, hi - lo)));
   }
   return p.cu_q[x - p.groups + 1] - p.cu_q[x - p.groups] > p.thin_max;
 }

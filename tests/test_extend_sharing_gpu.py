@@ -307,3 +307,52 @@ def test_the_hook(api):
         api.diffqkv_extend_shared(step.q, step.cu, step.cache, cu, lens, 2, 4, 0.1, out=out, dev_status=status)
         assert (int(status.item()) == 0) == shared
         assert bool(torch.isfinite(out[:2]).all()) and bool(torch.isfinite(out).all()) == shared
+
+
+def lends(api, past, new, prefix, heads="16/2/4", dims=(128, 128), slots=0):
+    """Whether a group's prefix is read once by itself: the first sequence, without rows, has NaN in its place, the others have
+    their own.  slots: sequences without rows behind it."""
+    api.extend_sharing(0)
+    step = Step(api, [prefix] + [prefix] * slots + past, [0] * (slots + 1) + new, *HEADS[heads], *dims, seed=prefix, pad=1)
+    groups = [0, slots + 1 + len(past)]
+    share(step, groups, [prefix], same_pages=False)
+    blk, slot = step.place(0, 0, prefix)
+    step.k[blk, :, slot] = math.nan
+    out = torch.full((step.total_q, step.n_q, step.d_v), 77.0, dtype=BF16, device="cuda")
+    api.diffqkv_extend_shared(step.q, step.cu, step.cache, ints(groups), ints([prefix]), step.n_k, step.n_v, 0.1, out=out)
+    gone = torch.isnan(out[:step.rows])
+    assert bool(gone.all()) or not bool(gone.any())
+    if not bool(gone.any()):
+        check(step, out, None, 0.1, joined=True)
+    return bool(gone.all())
+
+
+@pytest.mark.parametrize("new", [1, 2, 9, 100, 200])
+@pytest.mark.parametrize("slots", [0, 1, 63])
+def test_one_sequence_with_rows_reads_its_own(api, new, slots):
+    assert not lends(api, [8200], [new], 8192, slots=slots)
+
+
+@pytest.mark.parametrize("past,new", [(8192, 200), (8200, 480), (5000, 1), (5000, 17)])
+def test_a_group_of_one_is_none(api, past, new):
+    step = Step(api, [past, 70], [new, 3], 32, 4, 8, 128, 128, seed=new).fill()
+    out = [torch.empty((step.total_q, 32, 128), dtype=F32, device="cuda") for _ in range(3)]
+    for choice in range(3):
+        api.extend_sharing(choice)
+        api.diffqkv_extend_shared(step.q, step.cu, step.cache, ints([0, 1]), ints([5000]), 4, 8, 0.1, out=out[choice])
+    assert torch.equal(out[0], out[2]) and not torch.equal(out[0], out[1])
+
+
+@pytest.mark.parametrize("readers,prefix,shared", [(2, 511, False), (2, 512, True), (3, 255, False), (3, 256, True), (9, 63, False),
+                                                   (9, 64, True), (70, 7, False), (70, 8, True)])
+@pytest.mark.parametrize("slots", [0, 40, 200])
+def test_few_rows_share_by_their_sequences(api, readers, prefix, shared, slots):
+    """Sequences without rows do not count: among the first ones, that is; behind them as many as have rows at most."""
+    assert lends(api, [prefix + i for i in range(readers)], [1] * readers, prefix, slots=slots) == shared
+
+
+@pytest.mark.parametrize("readers,prefix,shared", [(2, 5398, False), (2, 5399, True), (5, 3758, False), (5, 3759, True), (2, 1024, False)])
+@pytest.mark.parametrize("slots", [0, 20])
+def test_long_chunks_share_by_their_sequences(api, readers, prefix, shared, slots):
+    """(prefix - 1024) 32 (readers - 1) >= 700 rows, in chunks of a hundred rows of four heads."""
+    assert lends(api, [prefix + i for i in range(readers)], [100] * readers, prefix, slots=slots) == shared
