@@ -481,10 +481,13 @@ diffqkv_status diffqkv_rope_append(const void *q, const void *k_new, const void 
 /*
  * diffqkv_norm_rope_append -- diffqkv_rope_append behind a root-mean-square norm of every q and k head, in the same launch:
  *     x <- x / sqrt(mean_c x_c^2 + eps) * (weight_offset + w_c)      over the d_qk channels of a head
- * and then the rotation, all in fp32, rounded once.  (Squares are summed in fp32, so channels have to stay below 1e18.)
+ * and then the rotation, all in fp32, rounded once.  Squares are summed in fp32: a head's sum of squares has to stay below 3.4e38
+ * (channels below 1.8e19 / sqrt(d_qk), 2e17 for 8192 of them) and, with eps = 0, its root mean square above 1e-18; with eps = 0 a
+ * head of zeros is NaN.
  *   q_weight, k_weight   [d_qk], or one for each head ([n_q, d_qk], [n_k, d_qk]) with a head stride of d_qk; NULL = all zero
  *                        where weight_offset is not 0, all one where it is
- *   *_head_stride        elements between the weights of two heads: 0 (one for all heads) or a multiple of 16 bytes, >= d_qk
+ *   *_head_stride        elements between the weights of two heads: 0 (one for all heads) or a multiple of 16 bytes, >= d_qk;
+ *                        not used beside a weight that is NULL
  * Everything else as diffqkv_rope_append (rot_dim 0 = norm and cache write alone).
  */
 typedef struct {

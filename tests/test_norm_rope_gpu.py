@@ -290,3 +290,13 @@ def test_a_missing_weight_has_no_head_stride(api, d_qk, offset, given):
     for out, pool in got[1:]:
         assert torch.equal(out, got[0][0])
         assert torch.equal(pool.view(torch.int16), got[0][1].view(torch.int16))
+
+
+@pytest.mark.parametrize("d_qk", [64, 128, 2048, 8192])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("end", ["large", "small"])
+def test_ends_of_the_range(api, d_qk, dtype, end):
+    """Sums of squares within a factor of four of what fp32 holds; heads of 2e-18 without an eps."""
+    std = 0.5 * math.sqrt(3.4e38 / d_qk) if end == "large" else 2e-18
+    step = Step(api, [3, 0], [4, 3], 4, 2, 2, d_qk, 64, seed=2, dtype=dtype)
+    run(api, step.fill(whole=False), 64, std=std, eps=0.0)
