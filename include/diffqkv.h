@@ -415,9 +415,11 @@ typedef struct {
  *              reported as DIFFQKV_ERR_INDEX and skipped.
  *   workspace  diffqkv_extend_shared_workspace_bytes(shape, total_q) bytes, 256-byte aligned (it holds both parts of every
  *              row in fp32)
- * Everything else as diffqkv_extend.  Launches as diffqkv_extend_window; where diffqkv_extend runs on FMAs, which bound it and
- * not the cache, every sequence reads all of its own tokens instead.  With a cu_q or a cu_seqs that decreases anywhere the
- * whole step may be left out.  Two calls that may run at the same time need a workspace each.
+ * Everything else as diffqkv_extend.  Launches as diffqkv_extend_window; where diffqkv_extend runs on FMAs (fp32, page sizes and
+ * heads that the tensor cores do not take) every sequence reads all of its own tokens.  With a cu_q or a cu_seqs that decreases
+ * anywhere the whole step may be left out.  Two calls that may run at the same time need a workspace each.
+ * It is for steps of many sequences with a few rows each behind a long prefix; steps of long chunks alone, which gain little or
+ * nothing, usually take less time with diffqkv_extend.
  */
 size_t diffqkv_extend_shared_workspace_bytes(const diffqkv_shape *shape, int32_t total_q);
 diffqkv_status diffqkv_extend_shared(const void *q, const int32_t *cu_q, int32_t total_q, const diffqkv_prefixes *prefixes,

@@ -486,7 +486,7 @@ static diffqkv_status extend_impl(const void* q, const int32_t* cu_q, int32_t to
   p.chunk = 0; p.splits = 1;
   p.o_partial = nullptr; p.lse_partial = nullptr;
   p.dev_status = dev_status;
-  if (range && range->groups > 0) {  // FMAs bound these kernels, not the cache: every sequence reads all of its own
+  if (range && range->groups > 0) {  // these kernels have no entries for prefixes: every sequence reads all of its own
     int* lengths = reinterpret_cast<int*>(static_cast<char*>(workspace) + extend_workspace_bytes(*shape, total_q, true));
     if (launch_extend_lengths(cu_q, total_q, *cache, shape->batch, *range, lengths, stream) != cudaSuccess) return DIFFQKV_ERR_CUDA;
     p.cache.seqlens = lengths;

@@ -48,8 +48,8 @@
 // ranged_start); a block's first request still goes out 16 thousand cycles, 9 us, after its start, nearly all of it code that
 // is fetched once, and an item costs 7-8 thousand cycles next to its tiles (2.5 of them the masks of its first and last tile).
 // The same four chunks in windows of 2k tokens: 285 us in a graph, 298 call by call, 750 TFLOP/s of what is seen; tensor pipe
-// 44 % active, special-function unit 45 %.  3k rows behind two prefixes of 3k-5k tokens, 64 and 128 channels: 276 us (power
-// keeps the SMs at 1.4-1.6 GHz); with the prefixes shared 289, 36 of them the join of 98 MB of parts.
+// 44 % active, special-function unit 45 %.  3k rows behind two prefixes of 3k-5k tokens, 64 and 128 channels: 274 us (power
+// keeps the SMs at 1.4-1.6 GHz); with the prefixes shared 284, some 36 of them the join of 98 MB of parts; the plain kernel 245.
 // Tried and not kept: rows written 32 bytes a lane without the exchange of four lanes (329 -> 343 us: the same lines, and
 // none of it was instructions), a thread a barrier at the start (283 -> 289), two rows at a time in the join (36 -> 37), a way
 // of its own there for rows of whole items (36), four blocks of it an SM (34, but 4 x 4 single rows 24.2 -> 25.1), rows with

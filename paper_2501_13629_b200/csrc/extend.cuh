@@ -212,10 +212,11 @@ __device__ __forceinline__ bool group_rows(const ExtendParams& p, int g, int& lo
 // sequences', which read it each otherwise.  It costs items more, and two parts to every row that are joined, and saves the
 // reading of all sequences with rows but one.  With few rows to a sequence the cost is as much as reading some hundred tokens
 // more; long chunks are bound by their products, of which sharing saves the empty rows of their tiles alone.
-// Shared and not, in us, 32/4/8 heads of 128 channels behind 100 tokens of their own: 3 chunks of 100-140 rows behind 8k tokens
-// 84, 96; 2 of 150 behind 8k 75, 81; 4 of 500 behind 4k 206, 191; 8 of 260 behind 4k 205, 197; 16 of 40 behind 8k 124, 172; two
+// Shared and not, in us, 32/4/8 heads of 128 channels with 100 tokens of their own: 3 chunks of 100-140 rows behind 8k tokens
+// 84, 96; 2 of 150 behind 8k 75, 81; 4 of 500 behind 4k 202, 190; 8 of 260 behind 4k 203, 195; 16 of 40 behind 8k 121, 172; two
 // single rows behind 400 tokens 22, 19, behind 1k 23, 25.  Over 604 steps (2-16 chunks of 20-600 rows behind 1k-32k tokens, four
-// head layouts) the rule is 1.1 % slower in the mean than the better of the two; with 500 or 1000 for 700 1.2 and 1.3 %.
+// head layouts) what the rule takes is 1.1 % slower in the mean than the better of the two; with 500 or 1000 for 700 1.2 and
+// 1.3 %.  To find out costs a step up to 1.5 us.
 // Never where the first sequence, from which a shared prefix is read, does not hold it (it may have no rows and be given up).
 constexpr int kShareTokens = 512, kShareLeast = 1024;
 constexpr float kShareLong = 700.f;

@@ -4,7 +4,7 @@
 // Such steps are short: a window of 4k tokens, the tokens behind a shared prefix.  extend_thin.cu's way, which plain steps
 // take, costs 18 us of starts, first tiles and ends however little there is to do, because every role's straight code is
 // fetched once (about 10 cycles an instruction); 16 sequences with a window of 1k tokens took it 24 us, of which the cache is
-// 4.  So here all warps but one run the same short loop, on warp-level products, and the same step takes 13 us.
+// 4.  So here all warps but one run the same short loop, on warp-level products, and the same step takes 16 us.
 //
 // Work: one flat list of (entry, block of rows, unit of heads, 64-token tile), where the tiles that no row sees are left out,
 // divided over one persistent block an SM, or over those that the step's long chunks leave; cut items leave partial rows as
@@ -23,7 +23,7 @@
 //
 // Bound, for up to two row groups, by memory (a 48 KB tile in 1.85 thousand cycles), for more by the warps' chain of products
 // and softmax (2.2 thousand for four, twice that for eight): 32 sequences of 2-5 rows of 32/4/8 heads behind windows of 4k
-// tokens (405 MB) take 80 us, 5.1 TB/s, the warp-level tensor pipe active 28 %.  Started, a
+// tokens (405 MB) take 83 us, 4.9 TB/s, the warp-level tensor pipe active 28 % (87 us with the join).  Started, a
 // block has its first tile after 9 thousand cycles; the step of 16 rows has little else.
 #include "attn_math.cuh"
 #include "extend.cuh"

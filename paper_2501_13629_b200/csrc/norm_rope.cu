@@ -12,10 +12,10 @@
 // lane (a channel and its partner; neighbours where pairs are neighbours or nothing turns), so that the sum of squares is
 // a few shuffles and the head never leaves its registers.  The coefficients of a row, a thread a pair, lie in shared memory,
 // where the lanes of a head read them without conflicts; weights and frequencies for them are read ahead too.
-// 11k rows of 32/4/8 heads of 128 channels, bf16 (272 MB): 59 us, 4.6 TB/s, against 48 for rope_append; instructions are
+// 12k rows of 32/4/8 heads of 128 channels, bf16 (272 MB): 59 us, 4.6 TB/s, against 50 for rope_append; instructions are
 // issued in three cycles of four.  With weight and turn applied one after the other to every head it was 72 us, with the
 // coefficients in registers and a head after another 90-105, with several rows to a block, the next one's vectors read as
-// registers fall free, 71-76, with 64 or 32 threads a row 60.  16 rows: 5.4 us.
+// registers fall free, 71-76, with 64 or 32 threads a row 60.  16 rows: 5.2 us.
 // Heads of more than 64 vectors are read a second time.
 #include "attn_math.cuh"
 #include "common.cuh"
